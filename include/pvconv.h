@@ -57,7 +57,12 @@ typedef enum {
 
 typedef enum { PVCONV_F32 = 0, PVCONV_BF16 = 1 } pvconv_dtype;
 
-typedef enum { PVCONV_ACT_NONE = 0, PVCONV_ACT_RELU = 1, PVCONV_ACT_LEAKY = 2 } pvconv_act;
+typedef enum {
+    PVCONV_ACT_NONE = 0,
+    PVCONV_ACT_RELU = 1,
+    PVCONV_ACT_LEAKY = 2,
+    PVCONV_ACT_SILU = 3 /* x / (1 + exp(-x)): taken by the group norm of pvconv_train.h only */
+} pvconv_act;
 
 /* Batch normalisation in inference form (running statistics), Section 4.1
  * "Feature Aggregation": y = gamma * (x - mean) / sqrt(var + eps) + beta.

@@ -1,4 +1,4 @@
-"""Thin Python binding of libpvconv (include/pvconv.h).
+"""Thin Python binding of libpvconv (include/pvconv.h, include/pvconv_train.h).
 
 Argument marshalling only: every function allocates its outputs (and any
 workspace) as torch tensors on the input's device, passes raw device pointers,
@@ -98,6 +98,36 @@ for _name, (_args, _res) in _SIGS.items():
     _fn.restype = _res
 
 EXPORTED = tuple(_SIGS)
+
+# include/pvconv_train.h
+_SIGS_TRAIN = {
+    "pvconv_group_norm_act_workspace_size": ([_I, _I, _I, _I], _SZ),
+    "pvconv_group_norm_act": ([_VP, _I, _I, _I, _I, _I, _I, _VP, _VP, _VP, _F, _I, _F, _VP, _I,
+                               _I, _VP, _VP, _SZ, _VP], _I),
+    "pvconv_group_norm_act_backward_workspace_size": ([_I, _I, _I, _I], _SZ),
+    "pvconv_group_norm_act_backward": ([_VP, _I, _I, _VP, _I, _I, _I, _I, _I, _I, _VP, _VP, _VP,
+                                        _VP, _I, _F, _VP, _I, _I, _VP, _VP, _VP, _SZ, _VP], _I),
+    "pvconv_fp8_quantize_weight": ([_VP, _I, _I, _I, _I, _VP, _VP, _VP, _VP, _VP], _I),
+    "pvconv_fp8_linear_workspace_size": ([_I, _I, _I], _SZ),
+    "pvconv_fp8_linear": ([_VP, _I, _I, _I, _I, _I, _VP, _VP, _VP, _I, _F, _VP, _I, _I, _VP,
+                           _SZ, _VP], _I),
+    "pvconv_fp8_linear_backward_workspace_size": ([_I, _I, _I], _SZ),
+    "pvconv_fp8_linear_backward": ([_VP, _I, _I, _VP, _I, _I, _I, _I, _I, _VP, _VP, _VP, _I, _I,
+                                    _VP, _VP, _VP, _SZ, _VP], _I),
+    "pvconv_distill_topk_workspace_size": ([_I, _I], _SZ),
+    "pvconv_distill_topk": ([_VP, _I, _I, _I, _I, _VP, _VP, _I, _VP, _F, _F, _VP, _VP, _VP, _VP,
+                             _I, _I, _VP, _SZ, _VP], _I),
+    "pvconv_distill_topk_backward": ([_VP, _I, _I, _I, _I, _VP, _VP, _I, _VP, _F, _F, _VP, _VP,
+                                      _VP, _I, _I, _VP], _I),
+}
+for _name, (_args, _res) in _SIGS_TRAIN.items():
+    _fn = getattr(_lib, _name)
+    _fn.argtypes = _args
+    _fn.restype = _res
+
+EXPORTED_TRAIN = tuple(_SIGS_TRAIN)
+ACT_NORM = dict(ACT, silu=3)  # the group norm's activations
+FP8_BLOCK = 128
 
 
 class PVConvError(RuntimeError):
@@ -560,6 +590,296 @@ def pvconv_act_bn_backward(dy: torch.Tensor, y: torch.Tensor, bn=None, act="leak
         _p(dy.contiguous()), _p(y.contiguous()), _dt(y), M, C,
         ctypes.byref(bns) if bn is not None else None, ACT[act], slope, _p(out), _stream(y)))
     return out
+
+
+# ----------------------------------------------------------------------------
+# include/pvconv_train.h: group norm, 8-bit linear layer, distillation loss
+# ----------------------------------------------------------------------------
+def _workspace(need: int, given: Optional[torch.Tensor], device):
+    """The caller's workspace where it is large enough, else a new one."""
+    if given is not None and given.numel() * given.element_size() >= need:
+        return given
+    return torch.empty(max(need, 256), dtype=torch.uint8, device=device)
+
+
+def _ws_bytes(t: torch.Tensor) -> int:
+    return t.numel() * t.element_size()
+
+
+def _same_device(first: torch.Tensor, *others):
+    for t in others:
+        if t is not None and t.device != first.device:
+            raise ValueError("all tensors must be on one device")
+
+
+def _vector(t: Optional[torch.Tensor], n: int, dtype, what: str):
+    """A contiguous [n] tensor of that dtype, or None."""
+    if t is not None and (t.dtype != dtype or tuple(t.shape) != (n,) or not t.is_contiguous()):
+        raise ValueError(f"{what} must be a contiguous [{n}] {dtype} tensor")
+    return t
+
+
+def _matrix_rows(t: torch.Tensor, ncols: int) -> tuple:
+    """(rows, row stride) of a [.., ncols] tensor whose rows are evenly spaced:
+    every leading dimension continues the one after it. Rows of one element or
+    none take the stride that a dense array has."""
+    if t.dim() < 1 or t.shape[-1] != ncols:
+        raise ValueError("channel count mismatch")
+    rows = 1
+    for d in t.shape[:-1]:
+        rows *= int(d)
+    if t.numel() == 0:
+        return rows, ncols
+    if ncols > 1 and t.stride(-1) != 1:
+        raise ValueError("channels must be the innermost, contiguous dimension")
+    ld, span = None, 0
+    for d, st in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+        if d == 1:
+            continue
+        if ld is None:
+            ld, span = st, st * d
+        elif st != span:
+            raise ValueError("rows must be evenly spaced")
+        else:
+            span = st * d
+    if ld is None:
+        ld = ncols
+    if ld < ncols:
+        raise ValueError("rows must not overlap")
+    return rows, ld
+
+
+def pvconv_group_norm_act(x: torch.Tensor, groups: int, gamma: torch.Tensor, beta: torch.Tensor,
+                          eps: float = 1e-5, act: str = "silu", slope: float = 0.1,
+                          lengths: Optional[torch.Tensor] = None, want_stats: bool = False,
+                          out: Optional[torch.Tensor] = None, out_dtype=None,
+                          workspace: Optional[torch.Tensor] = None):
+    """x [B][N][C] (rows evenly strided) -> y = act(group norm of x) [B][N][C] in
+    out_dtype (x's if None), and with want_stats (y, stats [B][groups][2] f32)
+    for the backward. lengths [B] int32: rows from lengths[b] on take no part
+    and give 0. out may be a column slice of a wider tensor."""
+    if x.dim() != 3:
+        raise ValueError("x must be [B][N][C]")
+    B, N, C = x.shape
+    _, ld = _matrix_rows(x, C)
+    _same_device(x, gamma, beta, lengths, out, workspace)
+    _vector(gamma, C, torch.float32, "gamma")
+    _vector(beta, C, torch.float32, "beta")
+    _vector(lengths, B, torch.int32, "lengths")
+    if out is None:
+        out = torch.empty((B, N, C), dtype=_torch_dt(out_dtype or x.dtype), device=x.device)
+    elif tuple(out.shape) != (B, N, C):
+        raise ValueError("out must have x's shape")
+    _, old = _matrix_rows(out, C)
+    if groups < 1 or C % groups:
+        raise ValueError("groups must divide the channels")
+    stats = torch.empty((B, groups, 2), dtype=torch.float32, device=x.device) if want_stats \
+        else None
+    ws = _workspace(_lib.pvconv_group_norm_act_workspace_size(B, N, C, groups), workspace,
+                    x.device)
+    _check("pvconv_group_norm_act", _lib.pvconv_group_norm_act(
+        _p(x), _dt(x), ld, B, N, C, groups, _p(lengths), _p(gamma), _p(beta), eps, ACT_NORM[act],
+        slope, _p(out), _dt(out), old, _p(stats), _p(ws), _ws_bytes(ws), _stream(x)))
+    return (out, stats) if want_stats else out
+
+
+def pvconv_group_norm_act_backward(dy: torch.Tensor, x: torch.Tensor, stats: torch.Tensor,
+                                   groups: int, gamma: torch.Tensor, beta: torch.Tensor,
+                                   act: str = "silu", slope: float = 0.1,
+                                   lengths: Optional[torch.Tensor] = None,
+                                   out: Optional[torch.Tensor] = None, out_dtype=None,
+                                   workspace: Optional[torch.Tensor] = None):
+    """dy, x [B][N][C] (rows evenly strided), stats of the forward -> (dx [B][N][C]
+    in out_dtype (x's if None), dgamma [C], dbeta [C] f32)."""
+    if x.dim() != 3 or dy.shape != x.shape:
+        raise ValueError("dy and x must be [B][N][C]")
+    B, N, C = x.shape
+    _, ld = _matrix_rows(x, C)
+    _, dld = _matrix_rows(dy, C)
+    _same_device(x, dy, stats, gamma, beta, lengths, out, workspace)
+    _vector(gamma, C, torch.float32, "gamma")
+    _vector(beta, C, torch.float32, "beta")
+    _vector(lengths, B, torch.int32, "lengths")
+    if groups < 1 or C % groups:
+        raise ValueError("groups must divide the channels")
+    if tuple(stats.shape) != (B, groups, 2) or stats.dtype != torch.float32 or \
+            not stats.is_contiguous():
+        raise ValueError("stats must be the forward's [B][groups][2] float32")
+    if out is None:
+        out = torch.empty((B, N, C), dtype=_torch_dt(out_dtype or x.dtype), device=x.device)
+    elif tuple(out.shape) != (B, N, C):
+        raise ValueError("out must have x's shape")
+    _, old = _matrix_rows(out, C)
+    dgamma = torch.empty((C,), dtype=torch.float32, device=x.device)
+    dbeta = torch.empty((C,), dtype=torch.float32, device=x.device)
+    ws = _workspace(_lib.pvconv_group_norm_act_backward_workspace_size(B, N, C, groups),
+                    workspace, x.device)
+    _check("pvconv_group_norm_act_backward", _lib.pvconv_group_norm_act_backward(
+        _p(dy), _dt(dy), dld, _p(x), _dt(x), ld, B, N, C, groups, _p(lengths), _p(stats),
+        _p(gamma), _p(beta), ACT_NORM[act], slope, _p(out), _dt(out), old, _p(dgamma), _p(dbeta),
+        _p(ws), _ws_bytes(ws), _stream(x)))
+    return out, dgamma, dbeta
+
+
+def _fp8_up(n: int) -> int:
+    return -(-n // FP8_BLOCK) * FP8_BLOCK
+
+
+def _fp8_operand(q: torch.Tensor, scale: torch.Tensor, cols: int, what: str):
+    """Checks a quantised weight [rows][cols up to 128s] and its scale bytes."""
+    kb = _fp8_up(cols) // FP8_BLOCK
+    if q.dim() != 2 or q.shape[1] != kb * FP8_BLOCK or not q.is_contiguous() or \
+            q.dtype not in (torch.uint8, torch.float8_e4m3fn):
+        raise ValueError(f"{what} must be contiguous [rows][{kb * FP8_BLOCK}] e4m3 bytes")
+    if tuple(scale.shape) != (_fp8_up(q.shape[0]) // FP8_BLOCK, kb) or \
+            scale.dtype != torch.uint8 or not scale.is_contiguous():
+        raise ValueError(f"{what}'s scale must be contiguous uint8, one per 128 x 128 block")
+
+
+def pvconv_fp8_quantize_weight(w: torch.Tensor, transposed: bool = False):
+    """w [N][K] -> (e4m3 [N][K128], scale bytes [N128/128][K128/128]), and with
+    transposed also the transpose (e4m3 [K][N128], scale [K128/128][N128/128])
+    that the backward takes. n128: n rounded up to a multiple of 128."""
+    if w.dim() != 2:
+        raise ValueError("w must be [N][K]")
+    N, K = w.shape
+    _, ld = _matrix_rows(w, K)
+    u8 = dict(dtype=torch.uint8, device=w.device)
+    nb, kb = _fp8_up(N) // FP8_BLOCK, _fp8_up(K) // FP8_BLOCK
+    f8 = dict(dtype=torch.float8_e4m3fn, device=w.device)
+    q, s = torch.empty((N, kb * FP8_BLOCK), **f8), torch.empty((nb, kb), **u8)
+    qt = st = None
+    if transposed:
+        qt, st = torch.empty((K, nb * FP8_BLOCK), **f8), torch.empty((kb, nb), **u8)
+    _check("pvconv_fp8_quantize_weight", _lib.pvconv_fp8_quantize_weight(
+        _p(w), _dt(w), ld, N, K, _p(q), _p(s), _p(qt), _p(st), _stream(w)))
+    return (q, s, qt, st) if transposed else (q, s)
+
+
+def pvconv_fp8_linear(x: torch.Tensor, weight: torch.Tensor, scale: torch.Tensor,
+                      bias: Optional[torch.Tensor] = None, act: str = "none", slope: float = 0.1,
+                      out: Optional[torch.Tensor] = None, out_dtype=None,
+                      workspace: Optional[torch.Tensor] = None):
+    """x [..][K] (rows evenly strided), a weight of pvconv_fp8_quantize_weight ->
+    act(x W^T + bias) [..][N] in out_dtype (x's if None)."""
+    K, N = x.shape[-1], weight.shape[0]
+    _fp8_operand(weight, scale, K, "weight")
+    _same_device(x, weight, scale, bias, out, workspace)
+    _vector(bias, N, torch.float32, "bias")
+    M, ld = _matrix_rows(x, K)
+    shape = tuple(x.shape[:-1]) + (N,)
+    if out is None:
+        out = torch.empty(shape, dtype=_torch_dt(out_dtype or x.dtype), device=x.device)
+    elif tuple(out.shape) != shape:
+        raise ValueError(f"out must be {shape}")
+    _, old = _matrix_rows(out, N)
+    ws = _workspace(_lib.pvconv_fp8_linear_workspace_size(M, K, N), workspace, x.device)
+    _check("pvconv_fp8_linear", _lib.pvconv_fp8_linear(
+        _p(x), _dt(x), ld, M, K, N, _p(weight), _p(scale), _p(bias), ACT[act], slope, _p(out),
+        _dt(out), old, _p(ws), _ws_bytes(ws), _stream(x)))
+    return out
+
+
+def pvconv_fp8_linear_backward(dy: torch.Tensor, x: Optional[torch.Tensor],
+                               weight_t: Optional[torch.Tensor],
+                               scale_t: Optional[torch.Tensor], want_dx: bool = True,
+                               want_dw: bool = True, want_dbias: bool = True, out_dtype=None,
+                               workspace: Optional[torch.Tensor] = None):
+    """dy [..][N], x [..][K], the transposed weight -> (dx [..][K] in out_dtype
+    (dy's if None), dw [N][K] f32, dbias [N] f32), None for what is not wanted.
+    x may be None without want_dw, the weight without want_dx."""
+    N = dy.shape[-1]
+    M, dld = _matrix_rows(dy, N)
+    if want_dw and x is None or want_dx and (weight_t is None or scale_t is None):
+        raise ValueError("dw needs x, dx the transposed weight")
+    if not (want_dx or want_dw or want_dbias):
+        raise ValueError("nothing is wanted")
+    K = x.shape[-1] if x is not None else weight_t.shape[0] if weight_t is not None else 1
+    _same_device(dy, x, weight_t, scale_t, workspace)
+    ld = 0
+    if x is not None:
+        rows, ld = _matrix_rows(x, K)
+        if rows != M:
+            raise ValueError("dy and x must have as many rows")
+    if want_dx:
+        _fp8_operand(weight_t, scale_t, N, "weight_t")
+        if weight_t.shape[0] != K:
+            raise ValueError("weight_t must be the transpose of [N][K]")
+    f32 = dict(dtype=torch.float32, device=dy.device)
+    dx = torch.empty(tuple(dy.shape[:-1]) + (K,), dtype=_torch_dt(out_dtype or dy.dtype),
+                     device=dy.device) if want_dx else None
+    dw = torch.empty((N, K), **f32) if want_dw else None
+    db = torch.empty((N,), **f32) if want_dbias else None
+    ws = _workspace(_lib.pvconv_fp8_linear_backward_workspace_size(M, K, N), workspace, dy.device)
+    _check("pvconv_fp8_linear_backward", _lib.pvconv_fp8_linear_backward(
+        _p(dy), _dt(dy), dld, _p(x) if want_dw else None, _dt(x) if x is not None else F32, ld, M,
+        K, N, _p(weight_t) if want_dx else None, _p(scale_t) if want_dx else None, _p(dx),
+        _dt(dx) if want_dx else F32, 0, _p(dw), _p(db), _p(ws), _ws_bytes(ws), _stream(dy)))
+    return dx, dw, db
+
+
+def _distill_args(z, t_val, t_class, labels):
+    if z.dim() != 2:
+        raise ValueError("z must be [M][V]")
+    M, V = z.shape
+    _, ld = _matrix_rows(z, V)
+    if t_val.dim() != 2 or t_val.shape[0] != M or t_val.shape != t_class.shape or \
+            t_val.dtype != torch.float32 or t_class.dtype != torch.int32 or \
+            not t_val.is_contiguous() or not t_class.is_contiguous():
+        raise ValueError("t_val and t_class must be contiguous [M][top] float32 and int32")
+    _vector(labels, M, torch.int32, "labels")
+    return M, V, ld, t_val.shape[1]
+
+
+def pvconv_distill_topk(z: torch.Tensor, t_val: torch.Tensor, t_class: torch.Tensor,
+                        labels: Optional[torch.Tensor] = None, temperature: float = 1.0,
+                        alpha: float = 1.0, row_weight: Optional[torch.Tensor] = None,
+                        want_grad: bool = False, out: Optional[torch.Tensor] = None,
+                        out_dtype=None, workspace: Optional[torch.Tensor] = None):
+    """z [M][V] (rows evenly strided), t_val, t_class [M][top], labels [M] int32 ->
+    (loss [M], lse [M][2]), and with want_grad (loss, lse, dz [M][V] in out_dtype
+    (z's if None)): the gradient of sum(row_weight * loss)."""
+    M, V, ld, top = _distill_args(z, t_val, t_class, labels)
+    _same_device(z, t_val, t_class, labels, row_weight, out, workspace)
+    _vector(row_weight, M, torch.float32, "row_weight")
+    loss = torch.empty((M,), dtype=torch.float32, device=z.device)
+    lse = torch.empty((M, 2), dtype=torch.float32, device=z.device)
+    dz, dld = None, 0
+    if want_grad:
+        dz = out if out is not None else torch.empty(
+            (M, V), dtype=_torch_dt(out_dtype or z.dtype), device=z.device)
+        if tuple(dz.shape) != (M, V):
+            raise ValueError("out must have z's shape")
+        _, dld = _matrix_rows(dz, V)
+    need = _lib.pvconv_distill_topk_workspace_size(M, V)
+    ws = _workspace(need, workspace, z.device) if need else None
+    _check("pvconv_distill_topk", _lib.pvconv_distill_topk(
+        _p(z), _dt(z), ld, M, V, _p(t_val), _p(t_class), top, _p(labels), temperature, alpha,
+        _p(row_weight), _p(loss), _p(lse), _p(dz), _dt(dz) if want_grad else F32, dld, _p(ws),
+        _ws_bytes(ws) if need else 0, _stream(z)))
+    return (loss, lse, dz) if want_grad else (loss, lse)
+
+
+def pvconv_distill_topk_backward(z: torch.Tensor, t_val: torch.Tensor, t_class: torch.Tensor,
+                                 lse: torch.Tensor, dloss: Optional[torch.Tensor] = None,
+                                 labels: Optional[torch.Tensor] = None, temperature: float = 1.0,
+                                 alpha: float = 1.0, out: Optional[torch.Tensor] = None,
+                                 out_dtype=None):
+    """The gradient dz [M][V] of sum(dloss * loss) from the forward's lse."""
+    M, V, ld, top = _distill_args(z, t_val, t_class, labels)
+    _same_device(z, t_val, t_class, labels, lse, dloss, out)
+    _vector(dloss, M, torch.float32, "dloss")
+    if tuple(lse.shape) != (M, 2) or lse.dtype != torch.float32 or not lse.is_contiguous():
+        raise ValueError("lse must be the forward's [M][2] float32")
+    dz = out if out is not None else torch.empty(
+        (M, V), dtype=_torch_dt(out_dtype or z.dtype), device=z.device)
+    if tuple(dz.shape) != (M, V):
+        raise ValueError("out must have z's shape")
+    _, dld = _matrix_rows(dz, V)
+    _check("pvconv_distill_topk_backward", _lib.pvconv_distill_topk_backward(
+        _p(z), _dt(z), ld, M, V, _p(t_val), _p(t_class), top, _p(labels), temperature, alpha,
+        _p(lse), _p(dloss), _p(dz), _dt(dz), dld, _stream(z)))
+    return dz
 
 
 class DeviceLayer:
