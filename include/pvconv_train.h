@@ -97,7 +97,8 @@ pvconv_status pvconv_fp8_quantize_weight(const void* w, pvconv_dtype w_dt, int w
 /*  x     [M][K] (x_dt), row stride x_ld                                     */
 /*  bias  [N] fp32 or NULL; act NONE, RELU or LEAKY (slope)                  */
 /*  y     out [M][N] (y_dt), row stride y_ld                                 */
-/* 1 <= K, N <= PVCONV_FP8_MAX_CHANNELS; M <= 2^30. weight 16-byte aligned.  */
+/* 1 <= K, N <= PVCONV_FP8_MAX_CHANNELS; M/128 * max(K, N)/128 (rounded up)  */
+/* <= 2^26. weight 16-byte aligned.                                          */
 size_t pvconv_fp8_linear_workspace_size(int M, int K, int N);
 pvconv_status pvconv_fp8_linear(const void* x, pvconv_dtype x_dt, int x_ld, int M, int K, int N,
                                 const uint8_t* weight, const uint8_t* scale, const float* bias,

@@ -27,7 +27,8 @@ inline bool norm_act_ok(pvconv_act a) { return act_ok(a) || a == PVCONV_ACT_SILU
 
 inline bool fp8_sizes_ok(int M, int K, int N) {
     return M >= 0 && M <= (1 << 30) && K >= 1 && N >= 1 && K <= PVCONV_FP8_MAX_CHANNELS &&
-           N <= PVCONV_FP8_MAX_CHANNELS;
+           N <= PVCONV_FP8_MAX_CHANNELS &&
+           (long long)pv_fp8_blocks(M) * pv_fp8_blocks(K > N ? K : N) <= (1LL << 26);
 }
 inline size_t fp8_bytes(int rows, int cols) {
     return (size_t)rows * pv_fp8_blocks(cols) * PVCONV_FP8_BLOCK;
