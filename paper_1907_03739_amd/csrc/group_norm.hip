@@ -12,6 +12,7 @@
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kRowsAhead = 4;  // rows a thread loads before it uses the first
 
 // How the work is dealt: items (cloud, slab of channels, chunk of rows).
 struct Deal {
@@ -23,10 +24,10 @@ struct Deal {
     size_t items;
 };
 
-// A slab is at most about 128 channels (or one group), so that the sums that
-// an item of the second launch adds stay few; chunks are small enough for
-// about kItems items and not smaller than kMinRows rows.
-constexpr int kSlab = 128, kItems = 2048, kMinRows = 16;
+// A slab is at most about 128 channels (or one group): 256 bytes of a bf16 row.
+// Chunks are for about kItems items, of kMinElements at least: an item adds the
+// sums of its cloud's chunks, which has to stay short beside its own rows.
+constexpr int kSlab = 128, kItems = 1024, kMinElements = 8192;
 
 Deal deal(int B, int N, int C, int groups) {
     Deal d;
@@ -37,12 +38,13 @@ Deal deal(int B, int N, int C, int groups) {
     d.slabs = (groups + k - 1) / k;
     const size_t per = (size_t)(B > 0 ? B : 1) * d.slabs;
     size_t chunks = (kItems + per - 1) / per;
-    const size_t most = (size_t)(N + kMinRows - 1) / kMinRows;
+    const int rows = (kMinElements + d.slab - 1) / d.slab;
+    const size_t most = ((size_t)N + rows - 1) / rows;
     if (chunks > most) chunks = most;
     if (chunks < 1) chunks = 1;
     d.chunk = (int)(((size_t)N + chunks - 1) / chunks);
     if (d.chunk < 1) d.chunk = 1;
-    d.chunks = (N + d.chunk - 1) / d.chunk;
+    d.chunks = (int)(((size_t)N + d.chunk - 1) / d.chunk);
     if (d.chunks < 1) d.chunks = 1;
     d.items = (size_t)B * d.slabs * d.chunks;
     return d;
@@ -53,11 +55,12 @@ Deal deal(int B, int N, int C, int groups) {
 template <int VEC>
 struct Place {
     int b, s, chunk, rows0, rows1, c0, width, cols, par, col, row, n;
+    // (arrays that fit the card have fewer than 2^32 items: 32-bit divisions)
     __device__ Place(size_t item, const Deal& d, int N, int C, const int32_t* lengths) {
-        chunk = (int)(item % d.chunks);
-        const size_t r = item / d.chunks;
-        s = (int)(r % d.slabs);
-        b = (int)(r / d.slabs);
+        const uint32_t r = (uint32_t)item / (uint32_t)d.chunks;
+        chunk = (int)((uint32_t)item - r * (uint32_t)d.chunks);
+        b = (int)(r / (uint32_t)d.slabs);
+        s = (int)(r - (uint32_t)b * (uint32_t)d.slabs);
         n = lengths ? min(max(lengths[b], 0), N) : N;
         c0 = s * d.slab;
         width = min(d.slab, C - c0);
@@ -72,31 +75,83 @@ struct Place {
     }
 };
 
-__device__ __forceinline__ float act_of(float v, int act, float slope) {
-    if (act == PVCONV_ACT_SILU) return v * __builtin_amdgcn_rcpf(1.f + __expf(-v));
-    return pv_activate(v, act, slope);
+// The types of the arrays of a call: all bf16, all fp32, or looked up per load.
+enum Types { kBf16, kF32, kMixed };
+// A vector of a row as it lies in memory, so that several can be in flight
+// before the first is turned into floats.
+template <int TYPES, int VEC>
+struct Raw {
+    static constexpr int kWords = TYPES == kBf16 ? (VEC + 1) / 2 : VEC;
+    uint32_t w[kWords];
+    __device__ __forceinline__ void load(const PvRows& x, size_t row, int c) {
+        const size_t at = row * x.ld + c;
+        if constexpr (TYPES == kBf16) {
+            const uint16_t* p = (const uint16_t*)x.p + at;
+            if constexpr (VEC == 1)
+                w[0] = *p;
+            else
+                __builtin_memcpy(w, __builtin_assume_aligned(p, VEC * 2), VEC * 2);
+        } else {
+            float v[VEC];
+            if (TYPES == kMixed && x.bf16)
+                pv_load_vec<true, VEC>(x.p, at, v);
+            else
+                pv_load_vec<false, VEC>(x.p, at, v);
+            __builtin_memcpy(w, v, VEC * 4);
+        }
+    }
+    __device__ __forceinline__ float get(int i) const {
+        if constexpr (TYPES == kBf16)
+            return __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+        else
+            return __uint_as_float(w[i]);
+    }
+};
+template <int TYPES, int VEC>
+__device__ __forceinline__ void store_row(const PvRows& x, size_t row, int c,
+                                          const float (&v)[VEC]) {
+    const size_t at = row * x.ld + c;
+    if (TYPES == kBf16 || (TYPES == kMixed && x.bf16))
+        pv_store_vec<true, VEC>(x.p, at, v);
+    else
+        pv_store_vec<false, VEC>(x.p, at, v);
 }
-__device__ __forceinline__ float dact_of(float v, int act, float slope) {
-    if (act == PVCONV_ACT_SILU) {
+
+// The activation and its derivative: SiLU, or a slope for v < 0 (1: none).
+template <bool SILU>
+__device__ __forceinline__ float act_of(float v, float neg) {
+    if (SILU) return v * __builtin_amdgcn_rcpf(1.f + __expf(-v));
+    return v >= 0.f ? v : v * neg;
+}
+template <bool SILU>
+__device__ __forceinline__ float dact_of(float v, float neg) {
+    if (SILU) {
         const float s = __builtin_amdgcn_rcpf(1.f + __expf(-v));
         return s * fmaf(v, 1.f - s, 1.f);
     }
-    if (act == PVCONV_ACT_NONE) return 1.f;
-    return v > 0.f ? 1.f : (act == PVCONV_ACT_LEAKY ? slope : 0.f);
+    return v > 0.f ? 1.f : neg;
 }
 
-// Sum over the workgroup's threads that hold `group`'s share, in a fixed
-// order: the wave that owns the group adds the entries lane-wise, then across.
 __device__ __forceinline__ double wave_sum(double v) {
 #pragma unroll
     for (int m = 1; m < 64; m <<= 1) v += __shfl_xor(v, m);
     return v;
 }
 
+template <int VEC>
+__device__ __forceinline__ void load_params(const PvNorm& n, int c, float (&ga)[VEC],
+                                            float (&be)[VEC]) {
+#pragma unroll
+    for (int i = 0; i < VEC; i++) {
+        ga[i] = n.gamma[c + i];
+        be[i] = n.beta[c + i];
+    }
+}
+
 // part[item of (b, slab, chunk)][group in slab] = (sum, sum of squares), in 64
 // bits: the subtraction that makes the variance of them loses nothing that 32
 // bits could hold.
-template <bool XB, int VEC>
+template <int TYPES, int VEC>
 __global__ __launch_bounds__(kThreads) void pv_gn_sums_kernel(PvNorm n, Deal d, PvRows x,
                                                               double2* part, int per) {
     __shared__ double2 red[kThreads];
@@ -108,14 +163,20 @@ __global__ __launch_bounds__(kThreads) void pv_gn_sums_kernel(PvNorm n, Deal d, 
             double s = 0., ss = 0.;
             const int c = p.c0 + (v0 + p.col) * VEC;
             if (v0 + p.col < vecs)
-                for (int k = p.rows0 + p.row; k < rows1; k += p.par) {
-                    float f[VEC];
-                    pv_load_vec<XB, VEC>(x.p, ((size_t)p.b * n.N + k) * x.ld + c, f);
+                for (int k = p.rows0 + p.row; k < rows1; k += p.par * kRowsAhead) {
+                    Raw<TYPES, VEC> f[kRowsAhead];
 #pragma unroll
-                    for (int i = 0; i < VEC; i++) {
-                        s += (double)f[i];
-                        ss = fma((double)f[i], (double)f[i], ss);
-                    }
+                    for (int u = 0; u < kRowsAhead; u++)
+                        f[u].load(x, (size_t)p.b * n.N + min(k + u * p.par, rows1 - 1), c);
+#pragma unroll
+                    for (int u = 0; u < kRowsAhead; u++)
+                        if (k + u * p.par < rows1)
+#pragma unroll
+                            for (int i = 0; i < VEC; i++) {
+                                const double v = (double)f[u].get(i);
+                                s += v;
+                                ss = fma(v, v, ss);
+                            }
                 }
             __syncthreads();
             red[threadIdx.x] = make_double2(s, ss);
@@ -123,7 +184,8 @@ __global__ __launch_bounds__(kThreads) void pv_gn_sums_kernel(PvNorm n, Deal d, 
             // the groups that this run of columns touches
             const int g0 = v0 / gv, g1 = min((v0 + p.cols + gv - 1) / gv, ng);
             for (int g = g0 + (threadIdx.x >> 6); g < g1; g += kThreads / 64) {
-                const int a = max(g * gv - v0, 0), z = min((g + 1) * gv - v0, min(p.cols, vecs - v0));
+                const int a = max(g * gv - v0, 0),
+                          z = min((g + 1) * gv - v0, min(p.cols, vecs - v0));
                 double t = 0., tt = 0.;
                 const int w = z - a, m = w * p.par;
                 for (int i = threadIdx.x & 63; i < m; i += 64) {
@@ -147,83 +209,87 @@ __global__ __launch_bounds__(kThreads) void pv_gn_sums_kernel(PvNorm n, Deal d, 
     }
 }
 
-// The statistics of the item's groups into st (mean, rstd), and out to `stats`
-// by the items of chunk 0.
-__device__ __forceinline__ void group_stats(const double2* part, int per, const Deal& d,
-                                            size_t item, int chunk, int ng, int n, float eps,
-                                            float2* st, float2* out) {
-    const double2* p = part + (item - chunk) * per;
-    for (int g = threadIdx.x >> 6; g < ng; g += kThreads / 64) {
-        double t = 0., tt = 0.;
-        for (int i = threadIdx.x & 63; i < d.chunks; i += 64) {
-            const double2 e = p[(size_t)i * per + g];
-            t += e.x;
-            tt += e.y;
-        }
-        t = wave_sum(t);
-        tt = wave_sum(tt);
-        if ((threadIdx.x & 63) == 0) {
-            const double cnt = (double)n * d.CG;
-            float2 r = make_float2(0.f, 0.f);
-            if (n > 0) {
-                const double mean = t / cnt, var = tt / cnt - mean * mean;
-                r.x = (float)mean;
-                r.y = (float)(1. / sqrt((var < 0. ? 0. : var) + (double)eps));
-            }
-            st[g] = r;
-            if (out && chunk == 0) out[g] = r;
-        }
+// A group's two sums over its cloud's chunks, by a wave, in a fixed order.
+__device__ __forceinline__ double2 add_chunks(const double2* part, int per, int chunks,
+                                              size_t first, int g) {
+    double t = 0., tt = 0.;
+    for (int i = threadIdx.x & 63; i < chunks; i += 64) {
+        const double2 e = part[(first + i) * per + g];
+        t += e.x;
+        tt += e.y;
     }
+    return make_double2(wave_sum(t), wave_sum(tt));
 }
 
-template <bool XB, bool YB, int VEC>
+__device__ __forceinline__ float2 stats_of(double sum, double squares, double count, float eps) {
+    if (count <= 0.) return make_float2(0.f, 0.f);
+    const double mean = sum / count, var = squares / count - mean * mean;
+    return make_float2((float)mean, (float)(1. / sqrt((var < 0. ? 0. : var) + (double)eps)));
+}
+
+template <int TYPES, bool SILU, int VEC>
 __global__ __launch_bounds__(kThreads) void pv_gn_apply_kernel(PvNorm n, Deal d, PvRows x,
-                                                               PvRows y, const double2* part,
-                                                               int per, float2* stats) {
+                                                               PvRows y, float neg,
+                                                               const double2* part, int per,
+                                                               float2* stats) {
     extern __shared__ float2 st[];
-    for (size_t item = blockIdx.x; item < d.items; item += gridDim.x) {
+    for (size_t i = blockIdx.x; i < d.items; i += gridDim.x) {
+        // from the last rows on: the first launch read them last
+        const size_t item = d.items - 1 - i;
         const Place<VEC> p(item, d, n.N, n.C, n.lengths);
         const int ng = p.width / d.CG, vecs = p.width / VEC;
+        const int last = min(p.rows1, p.n) - 1;  // the last row that is read
         __syncthreads();
-        group_stats(part, per, d, item, p.chunk, ng, p.n, n.eps, st,
-                    stats ? stats + (size_t)p.b * n.groups + p.c0 / d.CG : nullptr);
+        for (int g = threadIdx.x >> 6; g < ng; g += kThreads / 64) {
+            const double2 t = add_chunks(part, per, d.chunks, item - p.chunk, g);
+            if ((threadIdx.x & 63) == 0) {
+                st[g] = stats_of(t.x, t.y, (double)p.n * d.CG, n.eps);
+                if (stats && p.chunk == 0) stats[(size_t)p.b * n.groups + p.c0 / d.CG + g] = st[g];
+            }
+        }
         __syncthreads();
         for (int v = p.col; v < vecs; v += p.cols) {
             const int c = p.c0 + v * VEC;
             const float2 m = st[v * VEC / d.CG];
-            float a[VEC], be[VEC];
+            float ga[VEC], be[VEC];
+            load_params<VEC>(n, c, ga, be);
+            for (int k = p.rows0 + p.row; k < p.rows1; k += p.par * kRowsAhead) {
+                Raw<TYPES, VEC> f[kRowsAhead];
 #pragma unroll
-            for (int i = 0; i < VEC; i++) {
-                a[i] = n.gamma[c + i];
-                be[i] = n.beta[c + i];
-            }
-            for (int k = p.rows0 + p.row; k < p.rows1; k += p.par) {
-                const size_t at = (size_t)p.b * n.N + k;
-                float f[VEC];
-                if (k < p.n) {
-                    pv_load_vec<XB, VEC>(x.p, at * x.ld + c, f);
+                for (int u = 0; u < kRowsAhead; u++)
+                    f[u].load(x, (size_t)p.b * n.N + max(min(k + u * p.par, last), 0), c);
 #pragma unroll
-                    for (int i = 0; i < VEC; i++)
-                        f[i] = act_of(fmaf(a[i], (f[i] - m.x) * m.y, be[i]), n.act, n.slope);
-                } else {
+                for (int u = 0; u < kRowsAhead; u++) {
+                    const int ku = k + u * p.par;
+                    if (ku >= p.rows1) break;
+                    float r[VEC];
 #pragma unroll
-                    for (int i = 0; i < VEC; i++) f[i] = 0.f;
+                    for (int j = 0; j < VEC; j++)
+                        r[j] = act_of<SILU>(fmaf(ga[j], (f[u].get(j) - m.x) * m.y, be[j]), neg);
+                    if (ku > last)
+#pragma unroll
+                        for (int j = 0; j < VEC; j++) r[j] = 0.f;
+                    store_row<TYPES, VEC>(y, (size_t)p.b * n.N + ku, c, r);
                 }
-                pv_store_vec<YB, VEC>(y.p, at * y.ld + c, f);
             }
         }
     }
 }
 
-// part[b * chunks + chunk][c] = (sum dv xh, sum dv) over the chunk's rows.
-template <bool DB, bool XB, int VEC>
+// chan[b * chunks + chunk][c] = (sum dv xh, sum dv) over the chunk's rows, and
+// part[item][group in slab] = their sums over the group's channels, times
+// gamma: (sum gamma dv, sum gamma dv xh).
+template <int TYPES, bool SILU, int VEC>
 __global__ __launch_bounds__(kThreads) void pv_gn_bwd_sums_kernel(PvNorm n, Deal d, PvRows dy,
-                                                                  PvRows x, const float2* stats,
-                                                                  float2* part) {
+                                                                  PvRows x, float neg,
+                                                                  const float2* stats,
+                                                                  float2* chan, double2* part,
+                                                                  int per) {
     __shared__ float2 red[kThreads * VEC];
     for (size_t item = blockIdx.x; item < d.items; item += gridDim.x) {
         const Place<VEC> p(item, d, n.N, n.C, n.lengths);
         const int rows1 = min(p.rows1, p.n), vecs = p.width / VEC;
+        float2* out = chan + ((size_t)p.b * d.chunks + p.chunk) * n.C + p.c0;
         for (int v0 = 0; v0 < vecs; v0 += p.cols) {
             const int c = p.c0 + (v0 + p.col) * VEC;
             float s[VEC], h[VEC];
@@ -232,22 +298,26 @@ __global__ __launch_bounds__(kThreads) void pv_gn_bwd_sums_kernel(PvNorm n, Deal
             if (v0 + p.col < vecs) {
                 const float2 m = stats[(size_t)p.b * n.groups + c / d.CG];
                 float ga[VEC], be[VEC];
+                load_params<VEC>(n, c, ga, be);
+                for (int k = p.rows0 + p.row; k < rows1; k += p.par * kRowsAhead) {
+                    Raw<TYPES, VEC> f[kRowsAhead], g[kRowsAhead];
 #pragma unroll
-                for (int i = 0; i < VEC; i++) {
-                    ga[i] = n.gamma[c + i];
-                    be[i] = n.beta[c + i];
-                }
-                for (int k = p.rows0 + p.row; k < rows1; k += p.par) {
-                    const size_t at = (size_t)p.b * n.N + k;
-                    float f[VEC], g[VEC];
-                    pv_load_vec<XB, VEC>(x.p, at * x.ld + c, f);
-                    pv_load_vec<DB, VEC>(dy.p, at * dy.ld + c, g);
+                    for (int u = 0; u < kRowsAhead; u++) {
+                        const size_t row = (size_t)p.b * n.N + min(k + u * p.par, rows1 - 1);
+                        f[u].load(x, row, c);
+                        g[u].load(dy, row, c);
+                    }
 #pragma unroll
-                    for (int i = 0; i < VEC; i++) {
-                        const float xh = (f[i] - m.x) * m.y;
-                        const float dv = g[i] * dact_of(fmaf(ga[i], xh, be[i]), n.act, n.slope);
-                        s[i] += dv;
-                        h[i] = fmaf(dv, xh, h[i]);
+                    for (int u = 0; u < kRowsAhead; u++) {
+                        if (k + u * p.par >= rows1) break;
+#pragma unroll
+                        for (int i = 0; i < VEC; i++) {
+                            const float xh = (f[u].get(i) - m.x) * m.y;
+                            const float dv =
+                                g[u].get(i) * dact_of<SILU>(fmaf(ga[i], xh, be[i]), neg);
+                            s[i] += dv;
+                            h[i] = fmaf(dv, xh, h[i]);
+                        }
                     }
                 }
             }
@@ -263,60 +333,70 @@ __global__ __launch_bounds__(kThreads) void pv_gn_bwd_sums_kernel(PvNorm n, Deal
                     t.x += e.x;
                     t.y += e.y;
                 }
-                part[((size_t)p.b * d.chunks + p.chunk) * n.C + p.c0 + v0 * VEC + i] = t;
+                out[v0 * VEC + i] = t;
             }
+        }
+        __syncthreads();
+        for (int g = threadIdx.x >> 6; g < p.width / d.CG; g += kThreads / 64) {
+            double t = 0., u = 0.;
+            for (int i = threadIdx.x & 63; i < d.CG; i += 64) {
+                const float2 e = out[g * d.CG + i];
+                const double ga = (double)n.gamma[p.c0 + g * d.CG + i];
+                t = fma(ga, (double)e.y, t);
+                u = fma(ga, (double)e.x, u);
+            }
+            t = wave_sum(t);
+            u = wave_sum(u);
+            if ((threadIdx.x & 63) == 0) part[item * per + g] = make_double2(t, u);
         }
     }
 }
 
-// Items beyond d.items add the chunks' sums of 64 channels into dgamma, dbeta.
-template <bool DB, bool XB, bool OB, int VEC>
+// Items from d.items on add the chunks' sums of 16 channels into dgamma, dbeta:
+// 16 threads a channel, each a share of the chunks.
+constexpr int kParamChannels = 16;
+
+template <int TYPES, bool SILU, int VEC>
 __global__ __launch_bounds__(kThreads) void pv_gn_bwd_apply_kernel(
-    PvNorm n, Deal d, PvRows dy, PvRows x, PvRows dx, const float2* stats, const float2* part,
-    float* dgamma, float* dbeta, size_t items) {
-    extern __shared__ float2 gs[];  // per group of the slab: mean(gamma dv), mean(gamma dv xh)
+    PvNorm n, Deal d, PvRows dy, PvRows x, PvRows dx, float neg, const float2* stats,
+    const float2* chan, const double2* part, int per, float* dgamma, float* dbeta, size_t items) {
+    extern __shared__ float2 gs[];  // per group: mean(gamma dv), mean(gamma dv xh)
     __shared__ double2 red[kThreads];
-    for (size_t item = blockIdx.x; item < items; item += gridDim.x) {
-        if (item >= d.items) {
-            const int c = (int)(item - d.items) * 64 + (threadIdx.x & 63);
+    for (size_t i = blockIdx.x; i < items; i += gridDim.x) {
+        if (i >= d.items) {
+            const int ch = threadIdx.x % kParamChannels, share = threadIdx.x / kParamChannels;
+            const int c = (int)(i - d.items) * kParamChannels + ch;
             double t = 0., u = 0.;
             const size_t rows = (size_t)n.B * d.chunks;
             if (c < n.C)
-                for (size_t r = threadIdx.x >> 6; r < rows; r += kThreads / 64) {
-                    const float2 e = part[r * n.C + c];
+                for (size_t r = share; r < rows; r += kThreads / kParamChannels) {
+                    const float2 e = chan[r * n.C + c];
                     t += (double)e.x;
                     u += (double)e.y;
                 }
             __syncthreads();
             red[threadIdx.x] = make_double2(t, u);
             __syncthreads();
-            if (threadIdx.x < 64 && c < n.C) {
-                for (int w = 1; w < kThreads / 64; w++) {
-                    t += red[threadIdx.x + 64 * w].x;
-                    u += red[threadIdx.x + 64 * w].y;
+            if (share == 0 && c < n.C) {
+                for (int w = 1; w < kThreads / kParamChannels; w++) {
+                    t += red[ch + kParamChannels * w].x;
+                    u += red[ch + kParamChannels * w].y;
                 }
                 if (dgamma) dgamma[c] = (float)t;
                 if (dbeta) dbeta[c] = (float)u;
             }
             continue;
         }
+        const size_t item = d.items - 1 - i;
         const Place<VEC> p(item, d, n.N, n.C, n.lengths);
         const int ng = p.width / d.CG, vecs = p.width / VEC;
+        const int last = min(p.rows1, p.n) - 1;  // the last row that is read
         __syncthreads();
         for (int g = threadIdx.x >> 6; g < ng; g += kThreads / 64) {
-            double t = 0., u = 0.;
-            const int m = d.CG * d.chunks;
-            for (int i = threadIdx.x & 63; i < m; i += 64) {
-                const int c = p.c0 + g * d.CG + i % d.CG;
-                const float2 e = part[((size_t)p.b * d.chunks + i / d.CG) * n.C + c];
-                const double ga = (double)n.gamma[c];
-                t = fma(ga, (double)e.y, t);
-                u = fma(ga, (double)e.x, u);
-            }
-            t = wave_sum(t);
-            u = wave_sum(u);
+            const double2 t = add_chunks(part, per, d.chunks, item - p.chunk, g);
             const double cnt = p.n > 0 ? (double)p.n * d.CG : 1.;
-            if ((threadIdx.x & 63) == 0) gs[g] = make_float2((float)(t / cnt), (float)(u / cnt));
+            if ((threadIdx.x & 63) == 0)
+                gs[g] = make_float2((float)(t.x / cnt), (float)(t.y / cnt));
         }
         __syncthreads();
         for (int v = p.col; v < vecs; v += p.cols) {
@@ -324,28 +404,31 @@ __global__ __launch_bounds__(kThreads) void pv_gn_bwd_apply_kernel(
             const float2 q = gs[v * VEC / d.CG];
             const float2 m = stats[(size_t)p.b * n.groups + c / d.CG];
             float ga[VEC], be[VEC];
+            load_params<VEC>(n, c, ga, be);
+            for (int k = p.rows0 + p.row; k < p.rows1; k += p.par * kRowsAhead) {
+                Raw<TYPES, VEC> f[kRowsAhead], g[kRowsAhead];
 #pragma unroll
-            for (int i = 0; i < VEC; i++) {
-                ga[i] = n.gamma[c + i];
-                be[i] = n.beta[c + i];
-            }
-            for (int k = p.rows0 + p.row; k < p.rows1; k += p.par) {
-                const size_t at = (size_t)p.b * n.N + k;
-                float f[VEC], g[VEC];
-                if (k < p.n) {
-                    pv_load_vec<XB, VEC>(x.p, at * x.ld + c, f);
-                    pv_load_vec<DB, VEC>(dy.p, at * dy.ld + c, g);
-#pragma unroll
-                    for (int i = 0; i < VEC; i++) {
-                        const float xh = (f[i] - m.x) * m.y;
-                        const float dv = g[i] * dact_of(fmaf(ga[i], xh, be[i]), n.act, n.slope);
-                        f[i] = m.y * (fmaf(ga[i], dv, -q.x) - xh * q.y);
-                    }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < VEC; i++) f[i] = 0.f;
+                for (int u = 0; u < kRowsAhead; u++) {
+                    const size_t row = (size_t)p.b * n.N + max(min(k + u * p.par, last), 0);
+                    f[u].load(x, row, c);
+                    g[u].load(dy, row, c);
                 }
-                pv_store_vec<OB, VEC>(dx.p, at * dx.ld + c, f);
+#pragma unroll
+                for (int u = 0; u < kRowsAhead; u++) {
+                    const int ku = k + u * p.par;
+                    if (ku >= p.rows1) break;
+                    float r[VEC];
+#pragma unroll
+                    for (int j = 0; j < VEC; j++) {
+                        const float xh = (f[u].get(j) - m.x) * m.y;
+                        const float dv = g[u].get(j) * dact_of<SILU>(fmaf(ga[j], xh, be[j]), neg);
+                        r[j] = m.y * (fmaf(ga[j], dv, -q.x) - xh * q.y);
+                    }
+                    if (ku > last)
+#pragma unroll
+                        for (int j = 0; j < VEC; j++) r[j] = 0.f;
+                    store_row<TYPES, VEC>(dx, (size_t)p.b * n.N + ku, c, r);
+                }
             }
         }
     }
@@ -353,7 +436,7 @@ __global__ __launch_bounds__(kThreads) void pv_gn_bwd_apply_kernel(
 
 unsigned grid_of(size_t items) { return (unsigned)(items < (1u << 20) ? items : 1u << 20); }
 
-// Vector width: whole vectors in a group, a row and a slab, and aligned rows.
+// Vector width: whole vectors in a group and a row, and aligned rows.
 int width_for(int CG, const PvRows* r, int count) {
     int v = 8;
     for (int i = 0; i < count; i++) {
@@ -362,22 +445,38 @@ int width_for(int CG, const PvRows* r, int count) {
     }
     return v;
 }
+int types_of(const PvRows* r, int count) {
+    int bf16 = 0;
+    for (int i = 0; i < count; i++) bf16 += r[i].bf16 ? 1 : 0;
+    return bf16 == count ? kBf16 : (bf16 == 0 ? kF32 : kMixed);
+}
 
+// f with the call's types, activation and vector width as constants
 template <typename F>
-void with_vec(int v, F f) {
-    switch (v) {
-        case 8: f(std::integral_constant<int, 8>()); break;
-        case 4: f(std::integral_constant<int, 4>()); break;
-        case 2: f(std::integral_constant<int, 2>()); break;
-        default: f(std::integral_constant<int, 1>()); break;
+void with_kind(int types, bool silu, int vec, F f) {
+    auto vecs = [&](auto T, auto S) {
+        switch (vec) {
+            case 8: f(T, S, std::integral_constant<int, 8>()); break;
+            case 4: f(T, S, std::integral_constant<int, 4>()); break;
+            case 2: f(T, S, std::integral_constant<int, 2>()); break;
+            default: f(T, S, std::integral_constant<int, 1>()); break;
+        }
+    };
+    auto acts = [&](auto T) {
+        if (silu)
+            vecs(T, std::true_type());
+        else
+            vecs(T, std::false_type());
+    };
+    switch (types) {
+        case kBf16: acts(std::integral_constant<int, kBf16>()); break;
+        case kF32: acts(std::integral_constant<int, kF32>()); break;
+        default: acts(std::integral_constant<int, kMixed>()); break;
     }
 }
-template <typename F>
-void with_bool(bool b, F f) {
-    if (b)
-        f(std::true_type());
-    else
-        f(std::false_type());
+
+float negative_slope(const PvNorm& n) {
+    return n.act == PVCONV_ACT_LEAKY ? n.slope : (n.act == PVCONV_ACT_RELU ? 0.f : 1.f);
 }
 
 }  // namespace
@@ -389,7 +488,8 @@ size_t pv_group_norm_ws_bytes(int B, int N, int C, int groups) {
 
 size_t pv_group_norm_bwd_ws_bytes(int B, int N, int C, int groups) {
     const Deal d = deal(B, N, C, groups);
-    return pv_align256((size_t)B * d.chunks * C * sizeof(float2));
+    return pv_group_norm_ws_bytes(B, N, C, groups) +
+           pv_align256((size_t)B * d.chunks * C * sizeof(float2));
 }
 
 pvconv_status pv_launch_group_norm(const PvNorm& n, const PvRows& x, const PvRows& y,
@@ -397,19 +497,17 @@ pvconv_status pv_launch_group_norm(const PvNorm& n, const PvRows& x, const PvRow
     const Deal d = deal(n.B, n.N, n.C, n.groups);
     const PvRows all[2] = {x, y};
     const int per = d.slab / d.CG;
-    const unsigned grid = grid_of(d.items);
-    with_vec(width_for(d.CG, all, 2), [&](auto V) {
-        with_bool(x.bf16, [&](auto XB) {
-            constexpr int VEC = decltype(V)::value;
-            pv_gn_sums_kernel<decltype(XB)::value, VEC>
-                <<<grid, kThreads, 0, s>>>(n, d, x, (double2*)ws, per);
-            with_bool(y.bf16, [&](auto YB) {
-                pv_gn_apply_kernel<decltype(XB)::value, decltype(YB)::value, VEC>
-                    <<<grid, kThreads, per * sizeof(float2), s>>>(n, d, x, y, (const double2*)ws,
-                                                                  per, (float2*)stats);
-            });
-        });
-    });
+    const float neg = negative_slope(n);
+    with_kind(types_of(all, 2), n.act == PVCONV_ACT_SILU, width_for(d.CG, all, 2),
+              [&](auto T, auto S, auto V) {
+                  constexpr int TYPES = decltype(T)::value, VEC = decltype(V)::value;
+                  constexpr bool SILU = decltype(S)::value;
+                  pv_gn_sums_kernel<TYPES, VEC>
+                      <<<grid_of(d.items), kThreads, 0, s>>>(n, d, x, (double2*)ws, per);
+                  pv_gn_apply_kernel<TYPES, SILU, VEC>
+                      <<<grid_of(d.items), kThreads, per * sizeof(float2), s>>>(
+                          n, d, x, y, neg, (const double2*)ws, per, (float2*)stats);
+              });
     return pv_launch_status();
 }
 
@@ -421,25 +519,24 @@ pvconv_status pv_launch_group_norm_bwd(const PvNorm& norm, const PvRows& dy, con
     const Deal d = deal(n.B, n.N, n.C, n.groups);
     const PvRows all[3] = {dy, x, dx};
     const int per = d.slab / d.CG;
-    const size_t items = d.items + (dgamma || dbeta ? (size_t)(n.C + 63) / 64 : 0);
+    const size_t items =
+        d.items + (dgamma || dbeta ? ((size_t)n.C + kParamChannels - 1) / kParamChannels : 0);
     if (items == 0) return PVCONV_OK;
-    with_vec(width_for(d.CG, all, 3), [&](auto V) {
-        constexpr int VEC = decltype(V)::value;
-        with_bool(dy.bf16, [&](auto DB) {
-            with_bool(x.bf16, [&](auto XB) {
-                if (d.items)
-                    pv_gn_bwd_sums_kernel<decltype(DB)::value, decltype(XB)::value, VEC>
-                        <<<grid_of(d.items), kThreads, 0, s>>>(n, d, dy, x, (const float2*)stats,
-                                                               (float2*)ws);
-                with_bool(dx.bf16, [&](auto OB) {
-                    pv_gn_bwd_apply_kernel<decltype(DB)::value, decltype(XB)::value,
-                                           decltype(OB)::value, VEC>
-                        <<<grid_of(items), kThreads, per * sizeof(float2), s>>>(
-                            n, d, dy, x, dx, (const float2*)stats, (const float2*)ws, dgamma,
-                            dbeta, items);
-                });
-            });
-        });
-    });
+    double2* part = (double2*)ws;
+    float2* chan = (float2*)((char*)ws + pv_group_norm_ws_bytes(n.B, n.N, n.C, n.groups));
+    const float neg = negative_slope(n);
+    with_kind(types_of(all, 3), n.act == PVCONV_ACT_SILU, width_for(d.CG, all, 3),
+              [&](auto T, auto S, auto V) {
+                  constexpr int TYPES = decltype(T)::value, VEC = decltype(V)::value;
+                  constexpr bool SILU = decltype(S)::value;
+                  if (d.items)
+                      pv_gn_bwd_sums_kernel<TYPES, SILU, VEC>
+                          <<<grid_of(d.items), kThreads, 0, s>>>(
+                              n, d, dy, x, neg, (const float2*)stats, chan, part, per);
+                  pv_gn_bwd_apply_kernel<TYPES, SILU, VEC>
+                      <<<grid_of(items), kThreads, per * sizeof(float2), s>>>(
+                          n, d, dy, x, dx, neg, (const float2*)stats, chan, part, per, dgamma,
+                          dbeta, items);
+              });
     return pv_launch_status();
 }
