@@ -1,201 +1,457 @@
 // Distillation loss against a teacher's top logits, and its gradient
 // (pvconv_train.h).
 //
-// A team of threads owns a row: it takes the row's maximum and its sums of
-// exponentials at temperatures 1 and T in one pass, the teacher's term over the
-// stored entries, and writes the gradient in a second pass. Bound by HBM: z
-// read (twice where a gradient is written), dz written.
+// With m the row's maximum, s_T = sum exp((z - m) / T) and s_1 likewise at
+// temperature 1, lse_T = m / T + log s_T: the loss needs z at the stored entries
+// and the label beside them, the gradient of a logit is
+//   w (alpha T (exp(z / T - lse_T) - p) + (1 - alpha) (exp(z - lse_1) - [label])).
+// Bound by HBM: z read once and, where the gradient is taken, dz written.
+// Rows of few classes stay in the registers of 16 lanes or of a wave, from the
+// one read to the gradient. Rows of many take a workgroup, which goes over them
+// once with a running maximum and sums a thread and, for the gradient, a
+// second time, when they still lie in the caches.
+#include <type_traits>
+
 #include "pv_train.h"
 
 namespace {
 
-constexpr int kThreads = 256;
-
 __device__ __forceinline__ bool bad_class(int c, int V) { return (unsigned)c >= (unsigned)V; }
 
-// Reductions over a team: TEAM consecutive threads, a power of two up to a
-// wave, or the whole workgroup (through LDS, in wave order).
-template <int TEAM, typename Op>
-__device__ __forceinline__ float team_reduce(float v, Op op, float* lds) {
-#pragma unroll
-    for (int m = 1; m < (TEAM < 64 ? TEAM : 64); m <<= 1) v = op(v, __shfl_xor(v, m));
-    if constexpr (TEAM > 64) {
-        __syncthreads();
-        if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
-        __syncthreads();
-        v = lds[0];
-#pragma unroll
-        for (int w = 1; w < TEAM / 64; w++) v = op(v, lds[w]);
-    }
-    return v;
-}
 struct Max {
     __device__ float operator()(float a, float b) const { return fmaxf(a, b); }
 };
 struct Add {
     __device__ float operator()(float a, float b) const { return a + b; }
 };
-
-// The teacher's side of a row: maximum and sum of its present entries at
-// temperature T (has: some entry has weight).
-struct Teacher {
-    float max, inv;
-    bool has;
-};
-template <int TEAM>
-__device__ __forceinline__ Teacher teacher_of(const PvDistill& d, size_t row, int lane, float tau,
-                                              float* lds) {
-    float m = -INFINITY, s = 0.f;
-    for (int j = lane; j < d.top; j += TEAM)
-        if (!bad_class(d.t_class[row * d.top + j], d.V))
-            m = fmaxf(m, d.t_val[row * d.top + j] * tau);
-    m = team_reduce<TEAM>(m, Max(), lds);
-    const float base = m == -INFINITY ? 0.f : m;
-    for (int j = lane; j < d.top; j += TEAM)
-        if (!bad_class(d.t_class[row * d.top + j], d.V))
-            s += __expf(d.t_val[row * d.top + j] * tau - base);
-    s = team_reduce<TEAM>(s, Add(), lds);
-    // s is 0 only where every present value is -inf; a NaN keeps its row NaN
-    return Teacher{base, s == 0.f ? 0.f : 1.f / s, !(s == 0.f)};
+// Reduction over LANES consecutive lanes; every one gets the result.
+template <int LANES, typename Op>
+__device__ __forceinline__ float lanes_reduce(float v, Op op) {
+#pragma unroll
+    for (int m = 1; m < LANES; m <<= 1) v = op(v, __shfl_xor(v, m));
+    return v;
 }
 
-struct Weights {  // of the two terms for a row
-    float kl, ce;
+// What a row's terms weigh, and its label.
+struct Terms {
+    float kl, ce;  // alpha T, 1 - alpha, or 0 for a term that the row lacks
     int label;
 };
 
-// The gradient of one logit before the entries of its class: w_kl T q + w_ce q1.
-__device__ __forceinline__ float soft_grad(float z, float tau, const Weights& w, float lse1,
+__device__ __forceinline__ float log_of(float s) { return __logf(s); }
+
+struct Args {
+    PvDistill d;
+    float tau;            // 1 / T
+    bool soft, hard;      // alpha > 0; labels and alpha < 1
+    const float* weight;  // row_weight or dloss
+    float* loss;
+    float* lse;           // out of a forward, or the statistics of the gradient alone
+    PvRows dz;
+};
+
+// The gradient of a logit before the entries of its class. The branches are the
+// call's, not the row's: a row that lacks a term weighs it 0, and its
+// exponential is finite.
+__device__ __forceinline__ float soft_grad(float z, const Args& a, const Terms& w, float lse1,
                                            float lset) {
     float g = 0.f;
-    if (w.kl != 0.f) g = w.kl * __expf(fmaf(z, tau, -lset));
-    if (w.ce != 0.f) g = fmaf(w.ce, __expf(z - lse1), g);
+    if (a.soft) g = w.kl * __expf(fmaf(z, a.tau, -lset));
+    if (a.hard) g = fmaf(w.ce, __expf(z - lse1), g);
     return g;
 }
 
-// dz of a row from its statistics. The entries' and the label's classes get
-// their whole value from the thread that owns the entry, after the others.
-template <int TEAM>
-__device__ __forceinline__ void row_gradient(const PvDistill& d, size_t row, int lane, float tau,
-                                             const Teacher& t, const Weights& w, float lse1,
-                                             float lset, float scale, bool empty,
-                                             const PvRows& dz) {
-    const size_t in = row * d.z.ld, out = row * dz.ld;
-    const bool zero = scale == 0.f || empty;
-    for (int c = lane; c < d.V; c += TEAM)
-        pv_store_one(dz.p, dz.bf16, out + c,
-                     zero ? 0.f
-                          : scale * soft_grad(pv_load_one(d.z.p, d.z.bf16, in + c), tau, w, lse1,
-                                              lset));
-    if (zero) return;
-    if constexpr (TEAM > 64) __syncthreads();
-    const int entries = w.kl != 0.f ? d.top : 0;
-    for (int j = lane; j <= entries; j += TEAM) {
-        const int c = j < entries ? d.t_class[row * d.top + j] : (w.ce != 0.f ? w.label : -1);
-        if (bad_class(c, d.V)) continue;
-        float p = 0.f;
-        for (int i = 0; i < entries; i++)
-            if (d.t_class[row * d.top + i] == c)
-                p += __expf(d.t_val[row * d.top + i] * tau - t.max);
-        float g = soft_grad(pv_load_one(d.z.p, d.z.bf16, in + c), tau, w, lse1, lset) -
-                  w.kl * p * t.inv;
-        if (w.ce != 0.f && c == w.label) g -= w.ce;
-        pv_store_one(dz.p, dz.bf16, out + c, scale * g);
-    }
-}
+// ---------------------------------------------------------------------------
+// Few classes: TEAM lanes hold a row, E logits each (class e * TEAM + lane).
+// STATS: loss and statistics are computed, else read. GRAD: dz is written.
+// ---------------------------------------------------------------------------
+constexpr int kThreads = 256;
 
-__device__ __forceinline__ Weights weights_of(const PvDistill& d, size_t row, bool has) {
-    Weights w;
-    w.label = d.labels ? d.labels[row] : -1;
-    w.kl = has ? d.alpha * d.temperature : 0.f;
-    w.ce = bad_class(w.label, d.V) ? 0.f : 1.f - d.alpha;
-    return w;
-}
-
-template <int TEAM>
-__global__ __launch_bounds__(kThreads) void pv_distill_kernel(PvDistill d, const float* weight,
-                                                              float* loss, float* lse,
-                                                              PvRows dz) {
-    __shared__ float lds[kThreads / 64];
+template <int TEAM, int E, bool BF16, bool STATS, bool GRAD>
+__global__ __launch_bounds__(kThreads) void pv_distill_short_kernel(Args a) {
+    const PvDistill& d = a.d;
     const int lane = threadIdx.x % TEAM;
-    const float tau = 1.f / d.temperature;
-    const bool soft = d.alpha > 0.f, hard = d.labels && d.alpha < 1.f;
-    for (size_t row = (size_t)blockIdx.x * (kThreads / TEAM) + threadIdx.x / TEAM; row < (size_t)d.M;
-         row += (size_t)gridDim.x * (kThreads / TEAM)) {
-        const size_t in = row * d.z.ld;
-        float m = -INFINITY, s1 = 0.f, st = 0.f;
-        for (int c = lane; c < d.V; c += TEAM) {
-            const float z = pv_load_one(d.z.p, d.z.bf16, in + c);
-            if (z > m) {
-                const float e = m - z;
-                s1 *= __expf(e);
-                st *= __expf(e * tau);
-                m = z;
-            }
-            const float e = z == -INFINITY ? -INFINITY : z - m;
-            s1 += __expf(e);
-            st += __expf(e * tau);
+    const size_t step = (size_t)gridDim.x * (kThreads / TEAM);
+    // teams of a wave run the same number of rounds: their shuffles stay whole
+    const size_t first = (size_t)blockIdx.x * (kThreads / TEAM) + threadIdx.x / TEAM;
+    for (size_t row0 = (size_t)blockIdx.x * (kThreads / TEAM); row0 < (size_t)d.M; row0 += step) {
+        const size_t at = row0 + (first - (size_t)blockIdx.x * (kThreads / TEAM));
+        const bool live = at < (size_t)d.M;
+        const size_t row = live ? at : (size_t)d.M - 1;
+        float z[E];
+#pragma unroll
+        for (int e = 0; e < E; e++) {
+            const int c = e * TEAM + lane;
+            z[e] = c < d.V ? pv_load_one(d.z.p, BF16, row * d.z.ld + c) : -INFINITY;
         }
-        const float top = team_reduce<TEAM>(m, Max(), lds);
-        const float e = m == -INFINITY ? -INFINITY : m - top;
-        // a NaN in s1, st survives the rescaling
-        s1 = team_reduce<TEAM>(s1 * __expf(e), Add(), lds);
-        st = team_reduce<TEAM>(st * __expf(e * tau), Add(), lds);
-        const bool empty = s1 == 0.f;
-        const float lse1 = top + __logf(s1), lset = top * tau + __logf(st);
-        const Teacher t = soft ? teacher_of<TEAM>(d, row, lane, tau, lds) : Teacher{0.f, 0.f, false};
-        const Weights w = weights_of(d, row, t.has);
+        Terms w{0.f, 0.f, d.labels ? d.labels[row] : -1};
+        if (a.hard && !bad_class(w.label, d.V)) w.ce = 1.f - d.alpha;
+
+        // the teacher's entries at temperature T: maximum and sum
+        float tmax = -INFINITY, tsum = 0.f;
+        if (a.soft) {
+            for (int j = lane; j < d.top; j += TEAM)
+                if (!bad_class(d.t_class[row * d.top + j], d.V))
+                    tmax = fmaxf(tmax, d.t_val[row * d.top + j] * a.tau);
+            tmax = lanes_reduce<TEAM>(tmax, Max());
+            if (tmax == -INFINITY) tmax = 0.f;
+            for (int j = lane; j < d.top; j += TEAM)
+                if (!bad_class(d.t_class[row * d.top + j], d.V))
+                    tsum += __expf(d.t_val[row * d.top + j] * a.tau - tmax);
+            tsum = lanes_reduce<TEAM>(tsum, Add());
+            // 0 only without an entry of weight; a NaN stays
+            if (!(tsum == 0.f)) w.kl = d.alpha * d.temperature;
+        }
+        const float tinv = 1.f / tsum;
+
+        float lse1, lset;
+        bool empty;
+        if constexpr (STATS) {
+            float m = -INFINITY, s1 = 0.f, st = 0.f;
+#pragma unroll
+            for (int e = 0; e < E; e++) m = fmaxf(m, z[e]);
+            m = lanes_reduce<TEAM>(m, Max());
+#pragma unroll
+            for (int e = 0; e < E; e++) {
+                const float u = z[e] == -INFINITY ? -INFINITY : z[e] - m;
+                if (a.hard) s1 += __expf(u);
+                if (a.soft) st += __expf(u * a.tau);
+            }
+            if (a.hard) s1 = lanes_reduce<TEAM>(s1, Add());
+            if (a.soft) st = lanes_reduce<TEAM>(st, Add());
+            empty = m == -INFINITY && !(s1 != s1) && !(st != st);
+            lse1 = a.hard ? m + log_of(s1) : 0.f;
+            lset = a.soft ? m * a.tau + log_of(st) : 0.f;
+        } else {
+            lse1 = a.lse[2 * row];
+            lset = a.lse[2 * row + 1];
+            empty = lse1 == -INFINITY || lset == -INFINITY;
+        }
+
+        const float scale = GRAD ? (a.weight ? a.weight[row] : 1.f) : 0.f;
+        const bool zero = scale == 0.f || empty;
+        if constexpr (GRAD) {
+#pragma unroll
+            for (int e = 0; e < E; e++) {
+                const int c = e * TEAM + lane;
+                if (c < d.V && live)
+                    pv_store_one(a.dz.p, a.dz.bf16, row * a.dz.ld + c,
+                                 zero ? 0.f : scale * soft_grad(z[e], a, w, lse1, lset));
+            }
+        }
+        // the entries: their part of the loss, and the whole gradient of their
+        // classes, stored after the lines above (same wave, same address order)
         float kl = 0.f;
-        if (w.kl != 0.f && !empty)
-            for (int j = lane; j < d.top; j += TEAM) {
-                const int c = d.t_class[row * d.top + j];
-                if (bad_class(c, d.V)) continue;
-                const float u = d.t_val[row * d.top + j] * tau - t.max;
-                const float p = __expf(u) * t.inv;
-                const float z = pv_load_one(d.z.p, d.z.bf16, in + c);
-                if (!(p == 0.f)) kl += p * (u + __logf(t.inv) - (z * tau - lset));
+        const int entries = w.kl != 0.f ? d.top : 0;
+        for (int j0 = 0; j0 <= entries; j0 += TEAM) {
+            const int j = j0 + lane;
+            const int c = j < entries ? d.t_class[row * d.top + j]
+                                      : (j == entries && w.ce != 0.f ? w.label : -1);
+            const bool have = !bad_class(c, d.V);
+            const float zc = have ? pv_load_one(d.z.p, BF16, row * d.z.ld + c) : 0.f;
+            if (STATS && have && j < entries && !empty) {
+                const float u = d.t_val[row * d.top + j] * a.tau - tmax, p = __expf(u) * tinv;
+                if (!(p == 0.f)) kl += p * (u - log_of(tsum) - fmaf(zc, a.tau, -lset));
             }
-        kl = team_reduce<TEAM>(kl, Add(), lds);
-        if (lane == 0) {
-            float l = 0.f;
-            if (!empty) {
-                l = w.kl * d.temperature * kl;
-                if (w.ce != 0.f) l += w.ce * (lse1 - pv_load_one(d.z.p, d.z.bf16, in + w.label));
-            }
-            loss[row] = l;
-            if (lse) {
-                lse[2 * row] = hard ? lse1 : 0.f;
-                lse[2 * row + 1] = soft ? lset : 0.f;
+            if (GRAD && have && !zero && live) {
+                float p = 0.f;
+                for (int i = 0; i < entries; i++)
+                    if (d.t_class[row * d.top + i] == c)
+                        p += __expf(d.t_val[row * d.top + i] * a.tau - tmax);
+                float g = soft_grad(zc, a, w, lse1, lset);
+                if (entries) g -= w.kl * p * tinv;
+                if (w.ce != 0.f && c == w.label) g -= w.ce;
+                pv_store_one(a.dz.p, a.dz.bf16, row * a.dz.ld + c, scale * g);
             }
         }
-        if (dz.p)
-            row_gradient<TEAM>(d, row, lane, tau, t, w, lse1, lset, weight ? weight[row] : 1.f,
-                               empty, dz);
+        if constexpr (STATS) {
+            kl = lanes_reduce<TEAM>(kl, Add());
+            if (lane == 0 && live) {
+                float l = 0.f;
+                if (!empty) {
+                    l = w.kl * d.temperature * kl;
+                    if (w.ce != 0.f)
+                        l += w.ce * (lse1 - pv_load_one(d.z.p, BF16, row * d.z.ld + w.label));
+                }
+                a.loss[row] = l;
+                if (a.lse) {
+                    a.lse[2 * row] = lse1;
+                    a.lse[2 * row + 1] = lset;
+                }
+            }
+        }
     }
 }
 
-template <int TEAM>
-__global__ __launch_bounds__(kThreads) void pv_distill_bwd_kernel(PvDistill d, const float* lse,
-                                                                  const float* dloss, PvRows dz) {
-    __shared__ float lds[kThreads / 64];
-    const int lane = threadIdx.x % TEAM;
-    const float tau = 1.f / d.temperature;
-    const bool soft = d.alpha > 0.f;
-    for (size_t row = (size_t)blockIdx.x * (kThreads / TEAM) + threadIdx.x / TEAM; row < (size_t)d.M;
-         row += (size_t)gridDim.x * (kThreads / TEAM)) {
-        const float lse1 = lse[2 * row], lset = lse[2 * row + 1];
-        const Teacher t = soft ? teacher_of<TEAM>(d, row, lane, tau, lds) : Teacher{0.f, 0.f, false};
-        const Weights w = weights_of(d, row, t.has);
-        // the statistics of a row of -inf are -inf
-        const bool empty = lse1 == -INFINITY || lset == -INFINITY;
-        row_gradient<TEAM>(d, row, lane, tau, t, w, lse1, lset, dloss ? dloss[row] : 1.f, empty,
-                           dz);
+// ---------------------------------------------------------------------------
+// Many classes: a workgroup of T threads a row, 16-byte vectors from the row's
+// first 16-byte boundary on, the elements before and after one a thread. Rows
+// of z and dz rarely share that boundary (an odd number of classes): the pass
+// that reads alone goes by z's, the pass that writes by dz's.
+// ---------------------------------------------------------------------------
+constexpr int kAhead = 4;  // vectors in flight a thread
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef u32x4 u32x4_any __attribute__((aligned(2)));  // at any element
+
+template <bool BF16>
+struct Vec {
+    static constexpr int N = BF16 ? 8 : 4;
+    u32x4 w;
+    __device__ __forceinline__ float get(int i) const {
+        const uint32_t u = w[BF16 ? i / 2 : i];
+        return __uint_as_float(BF16 ? (i & 1 ? u & 0xffff0000u : u << 16) : u);
+    }
+};
+
+// Where a row's vectors lie: on the 16-byte boundaries of `by` (es bytes an
+// element).
+template <bool BF16>
+struct RowSpan {
+    const char* p;
+    int head, vecs, tail;  // elements, vectors, elements
+    __device__ RowSpan(const PvRows& x, size_t row, int V, const void* by, int es) {
+        p = (const char*)x.p + row * x.ld * (BF16 ? 2 : 4);
+        head = min((int)((16 - ((uintptr_t)by & 15)) & 15) / es, V);
+        vecs = (V - head) / Vec<BF16>::N;
+        tail = V - head - vecs * Vec<BF16>::N;
+    }
+    // OWN: the boundaries are the row's own
+    template <bool OWN>
+    __device__ __forceinline__ Vec<BF16> vec(int i) const {
+        const char* q = p + head * (BF16 ? 2 : 4) + (size_t)i * 16;
+        if constexpr (OWN)
+            return {*(const u32x4*)q};
+        else
+            return {*(const u32x4_any*)q};
+    }
+    __device__ __forceinline__ int first(int i) const { return head + i * Vec<BF16>::N; }
+    // the element that this thread takes beside the vectors, or -1
+    __device__ __forceinline__ int odd(int t) const {
+        if (t < head) return t;
+        const int u = t - head;
+        return u < tail ? head + vecs * Vec<BF16>::N + u : -1;
+    }
+};
+
+// Running maximum and sums of a thread.
+struct Running {
+    float m = -INFINITY, s1 = 0.f, st = 0.f;
+    __device__ __forceinline__ void raise(float to, const Args& a) {
+        if (to > m) {
+            const float e = m - to;
+            s1 *= __expf(e);
+            st *= __expf(e * a.tau);
+            m = to;
+        }
+    }
+    __device__ __forceinline__ void add(float z, const Args& a) {
+        // -inf - -inf is no number: a row that starts with -inf
+        const float e = z == -INFINITY ? -INFINITY : z - m;
+        if (a.hard) s1 += __expf(e);
+        if (a.soft) st += __expf(e * a.tau);
+    }
+};
+
+template <int T, typename Op>
+__device__ __forceinline__ float group_reduce(float v, Op op, float* lds) {
+    v = lanes_reduce<64>(v, op);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = lds[0];
+#pragma unroll
+    for (int w = 1; w < T / 64; w++) v = op(v, lds[w]);
+    return v;
+}
+
+template <int T, bool BF16, bool STATS, bool GRAD>
+__global__ __launch_bounds__(T) void pv_distill_long_kernel(Args a) {
+    __shared__ float lds[T / 64];
+    __shared__ float ep[PVCONV_MAX_TOP];  // exp of the entries
+    __shared__ int ec[PVCONV_MAX_TOP];    // their classes, -1 for an absent one
+    const PvDistill& d = a.d;
+    const int t = threadIdx.x;
+    for (size_t row = blockIdx.x; row < (size_t)d.M; row += gridDim.x) {
+        constexpr int zs = BF16 ? 2 : 4;
+        const RowSpan<BF16> r(d.z, row, d.V, (const char*)d.z.p + row * d.z.ld * zs, zs);
+        Terms w{0.f, 0.f, d.labels ? d.labels[row] : -1};
+        if (a.hard && !bad_class(w.label, d.V)) w.ce = 1.f - d.alpha;
+        // a thread an entry (T >= PVCONV_MAX_TOP)
+        const bool mine = a.soft && t < d.top && !bad_class(d.t_class[row * d.top + t], d.V);
+        const int c_mine = mine ? d.t_class[row * d.top + t] : -1;
+        const float v_mine = mine ? d.t_val[row * d.top + t] * a.tau : -INFINITY;
+
+        float lse1 = 0.f, lset = 0.f;
+        bool empty;
+        if constexpr (STATS) {
+            Running s;
+            for (int i = t; i < r.vecs; i += T * kAhead) {
+                Vec<BF16> v[kAhead];
+#pragma unroll
+                for (int u = 0; u < kAhead; u++) v[u] = r.template vec<true>(min(i + u * T, r.vecs - 1));
+                float m = -INFINITY;
+#pragma unroll
+                for (int u = 0; u < kAhead; u++)
+#pragma unroll
+                    for (int k = 0; k < Vec<BF16>::N; k++) m = fmaxf(m, v[u].get(k));
+                s.raise(m, a);
+#pragma unroll
+                for (int u = 0; u < kAhead; u++)
+                    if (i + u * T < r.vecs) {
+#pragma unroll
+                        for (int k = 0; k < Vec<BF16>::N; k++) s.add(v[u].get(k), a);
+                    }
+            }
+            const int odd = r.odd(t);
+            if (odd >= 0) {
+                const float z = pv_load_one(r.p, BF16, odd);
+                s.raise(z, a);
+                s.add(z, a);
+            }
+            const float m = group_reduce<T>(s.m, Max(), lds);
+            const float e = s.m == -INFINITY ? -INFINITY : s.m - m;
+            const float s1 = a.hard ? group_reduce<T>(s.s1 * __expf(e), Add(), lds) : 0.f;
+            const float st = a.soft ? group_reduce<T>(s.st * __expf(e * a.tau), Add(), lds) : 0.f;
+            empty = m == -INFINITY && !(s1 != s1) && !(st != st);
+            if (a.hard) lse1 = m + log_of(s1);
+            if (a.soft) lset = m * a.tau + log_of(st);
+        } else {
+            lse1 = a.lse[2 * row];
+            lset = a.lse[2 * row + 1];
+            empty = lse1 == -INFINITY || lset == -INFINITY;
+        }
+
+        float p = 0.f, tsum = 0.f, tmax = 0.f;
+        if (a.soft) {
+            tmax = group_reduce<T>(v_mine, Max(), lds);
+            if (tmax == -INFINITY) tmax = 0.f;
+            p = mine ? __expf(v_mine - tmax) : 0.f;
+            tsum = group_reduce<T>(p, Add(), lds);
+            if (!(tsum == 0.f)) w.kl = d.alpha * d.temperature;
+        }
+        const float tinv = 1.f / tsum;
+        if constexpr (STATS) {
+            float kl = 0.f;
+            if (mine && w.kl != 0.f && !empty && !(p * tinv == 0.f))
+                kl = p * tinv * (v_mine - tmax - log_of(tsum) -
+                                 fmaf(pv_load_one(r.p, BF16, c_mine), a.tau, -lset));
+            kl = group_reduce<T>(kl, Add(), lds);
+            if (t == 0) {
+                float l = 0.f;
+                if (!empty) {
+                    l = w.kl * d.temperature * kl;
+                    if (w.ce != 0.f) l += w.ce * (lse1 - pv_load_one(r.p, BF16, w.label));
+                }
+                a.loss[row] = l;
+                if (a.lse) {
+                    a.lse[2 * row] = lse1;
+                    a.lse[2 * row + 1] = lset;
+                }
+            }
+        }
+        if constexpr (GRAD) {
+            const float scale = a.weight ? a.weight[row] : 1.f;
+            const bool zero = scale == 0.f || empty;
+            const int es = a.dz.bf16 ? 2 : 4;
+            char* out = (char*)a.dz.p + row * a.dz.ld * es;
+            const RowSpan<BF16> o(d.z, row, d.V, out, es);
+            for (int i = t; i < o.vecs; i += T * kAhead) {
+                Vec<BF16> v[kAhead];
+#pragma unroll
+                for (int u = 0; u < kAhead; u++) v[u] = o.template vec<false>(min(i + u * T, o.vecs - 1));
+#pragma unroll
+                for (int u = 0; u < kAhead; u++) {
+                    if (i + u * T >= o.vecs) continue;
+                    float g[Vec<BF16>::N];
+#pragma unroll
+                    for (int k = 0; k < Vec<BF16>::N; k++)
+                        g[k] = scale * soft_grad(v[u].get(k), a, w, lse1, lset);
+                    if (zero)
+#pragma unroll
+                        for (int k = 0; k < Vec<BF16>::N; k++) g[k] = 0.f;
+                    char* to = out + (size_t)o.first(i + u * T) * es;
+                    if (a.dz.bf16) {
+                        uint32_t q[Vec<BF16>::N / 2];
+#pragma unroll
+                        for (int k = 0; k < Vec<BF16>::N / 2; k++)
+                            q[k] = pv_pack_bf16x2(g[2 * k], g[2 * k + 1]);
+                        if constexpr (BF16)
+                            *(uint4*)to = make_uint4(q[0], q[1], q[2], q[3]);
+                        else  // 4 of fp32 logits: 8 bytes
+                            *(uint2*)to = make_uint2(q[0], q[1]);
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < Vec<BF16>::N; k += 4)
+                            ((float4*)to)[k / 4] = make_float4(g[k], g[k + 1], g[k + 2], g[k + 3]);
+                    }
+                }
+            }
+            const int odd = o.odd(t);
+            if (odd >= 0)
+                pv_store_one(out, a.dz.bf16, odd,
+                             zero ? 0.f
+                                  : scale * soft_grad(pv_load_one(r.p, BF16, odd), a, w, lse1,
+                                                      lset));
+            // the classes of the entries and of the label take their whole value
+            // from the thread of the entry, after the stores above
+            if (t < PVCONV_MAX_TOP) {
+                ec[t] = c_mine;
+                ep[t] = p;
+            }
+            __syncthreads();
+            const int c = t < d.top ? c_mine : (t == d.top && w.ce != 0.f ? w.label : -1);
+            if (!zero && c >= 0) {
+                float sum = 0.f;
+                if (w.kl != 0.f)
+                    for (int i = 0; i < d.top; i++) sum += ec[i] == c ? ep[i] : 0.f;
+                float g = soft_grad(pv_load_one(r.p, BF16, c), a, w, lse1, lset);
+                if (w.kl != 0.f) g -= w.kl * sum * tinv;
+                if (w.ce != 0.f && c == w.label) g -= w.ce;
+                pv_store_one(out, a.dz.bf16, c, scale * g);
+            }
+            // (the next row's first reduction is a barrier before ec is written)
+        }
     }
 }
 
-constexpr int kTeamV = 1024;  // classes from which a workgroup owns a row
+// ---------------------------------------------------------------------------
+// From kLongV classes on a workgroup owns a row: 1024 threads where rows are too
+// few to fill the chip with 256.
+constexpr int kLongV = 1025, kFewRows = 512, kWideV = 8192;
 
-unsigned grid_of(size_t blocks) { return (unsigned)(blocks < 65536 ? blocks : 65536); }
+template <typename F>
+void with_bool(bool b, F f) {
+    if (b)
+        f(std::true_type());
+    else
+        f(std::false_type());
+}
+
+template <bool STATS, bool GRAD>
+pvconv_status launch(const Args& a, hipStream_t s) {
+    const size_t M = a.d.M;
+    auto grid = [](size_t n) { return (unsigned)(n < (1u << 18) ? n : 1u << 18); };
+    with_bool(a.d.z.bf16, [&](auto B) {
+        constexpr bool BF16 = decltype(B)::value;
+        if (a.d.V >= kLongV) {
+            if (M <= kFewRows && a.d.V >= kWideV)
+                pv_distill_long_kernel<1024, BF16, STATS, GRAD><<<grid(M), 1024, 0, s>>>(a);
+            else
+                pv_distill_long_kernel<512, BF16, STATS, GRAD><<<grid(M), 512, 0, s>>>(a);
+        } else if (a.d.V <= 64) {
+            pv_distill_short_kernel<16, 4, BF16, STATS, GRAD>
+                <<<grid((M + 15) / 16), kThreads, 0, s>>>(a);
+        } else if (a.d.V <= 256) {
+            pv_distill_short_kernel<16, 16, BF16, STATS, GRAD>
+                <<<grid((M + 15) / 16), kThreads, 0, s>>>(a);
+        } else {
+            pv_distill_short_kernel<64, 16, BF16, STATS, GRAD>
+                <<<grid((M + 3) / 4), kThreads, 0, s>>>(a);
+        }
+    });
+    return pv_launch_status();
+}
 
 }  // namespace
 
@@ -208,19 +464,14 @@ size_t pv_distill_ws_bytes(int M, int V) {
 pvconv_status pv_launch_distill(const PvDistill& d, const float* row_weight, float* loss,
                                 float* lse, const PvRows& dz, void* ws, hipStream_t s) {
     (void)ws;
-    if (d.V >= kTeamV)
-        pv_distill_kernel<kThreads><<<grid_of(d.M), kThreads, 0, s>>>(d, row_weight, loss, lse, dz);
-    else
-        pv_distill_kernel<16><<<grid_of((d.M + 15) / 16), kThreads, 0, s>>>(d, row_weight, loss,
-                                                                            lse, dz);
-    return pv_launch_status();
+    const Args a{d, 1.f / d.temperature, d.alpha > 0.f, d.labels && d.alpha < 1.f, row_weight, loss,
+                 lse, dz};
+    return dz.p ? launch<true, true>(a, s) : launch<true, false>(a, s);
 }
 
 pvconv_status pv_launch_distill_bwd(const PvDistill& d, const float* lse, const float* dloss,
                                     const PvRows& dz, hipStream_t s) {
-    if (d.V >= kTeamV)
-        pv_distill_bwd_kernel<kThreads><<<grid_of(d.M), kThreads, 0, s>>>(d, lse, dloss, dz);
-    else
-        pv_distill_bwd_kernel<16><<<grid_of((d.M + 15) / 16), kThreads, 0, s>>>(d, lse, dloss, dz);
-    return pv_launch_status();
+    const Args a{d, 1.f / d.temperature, d.alpha > 0.f, d.labels && d.alpha < 1.f, dloss, nullptr,
+                 (float*)lse, dz};
+    return launch<false, true>(a, s);
 }

@@ -7,6 +7,7 @@
 #include <type_traits>
 
 #include "pv_train.h"
+#include "pv_wave.h"
 
 namespace {
 
@@ -217,7 +218,7 @@ struct Product {
     const uint8_t* sb;  // at (n / step) * sb_row + block * sb_blk
     int step;
     size_t sb_row, sb_blk;
-    int N, blocks;
+    int N, blocks, K;
     int per, splits;    // blocks a split takes
     const float* bias;
     int act;
@@ -229,6 +230,8 @@ constexpr int kTile = 128;
 
 __device__ __forceinline__ int a_key(int row) { return row & 7; }
 __device__ __forceinline__ int b_key(int row) { return (row & 3) | ((row >> 2) & 4); }
+// of the fragments that take rows 8 (r >> 2) + 4 j + (r & 3)
+__device__ __forceinline__ int w_key(int row) { return (row & 3) | ((row >> 1) & 4); }
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -247,47 +250,49 @@ __device__ __forceinline__ bf16x8 to_bf16(uint32_t lo, uint32_t hi, uint32_t byt
     return u.v;
 }
 
-// 16 consecutive outputs of a row from column n on
-__device__ __forceinline__ void store16(const Product& p, int split, int m, int n,
-                                        const float (&v)[16], bool vec) {
+// W (8 or 16) consecutive outputs of a row from column n on
+template <int W>
+__device__ __forceinline__ void store_run(const Product& p, int split, int m, int n,
+                                          const float (&v)[W], bool vec) {
     if (p.splits > 1) {
         float* o = p.partial + ((size_t)split * p.M + m) * p.N + n;
-        if (vec && n + 16 <= p.N) {
+        if (vec && n + W <= p.N) {
 #pragma unroll
-            for (int i = 0; i < 4; i++)
+            for (int i = 0; i < W / 4; i++)
                 *(float4*)(o + 4 * i) = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2],
                                                     v[4 * i + 3]);
         } else {
 #pragma unroll
-            for (int i = 0; i < 16; i++)
+            for (int i = 0; i < W; i++)
                 if (n + i < p.N) o[i] = v[i];
         }
         return;
     }
-    float r[16];
+    float r[W];
 #pragma unroll
-    for (int i = 0; i < 16; i++) {
+    for (int i = 0; i < W; i++) {
         const float add = p.bias && n + i < p.N ? p.bias[n + i] : 0.f;
         r[i] = pv_activate(v[i] + add, p.act, p.slope);
     }
     const size_t at = (size_t)m * p.out.ld + n;
-    if (vec && n + 16 <= p.N) {
+    if (vec && n + W <= p.N) {
         if (p.out.bf16) {
-            uint32_t w[8];
+            uint32_t w[W / 2];
 #pragma unroll
-            for (int i = 0; i < 8; i++) w[i] = pv_pack_bf16x2(r[2 * i], r[2 * i + 1]);
+            for (int i = 0; i < W / 2; i++) w[i] = pv_pack_bf16x2(r[2 * i], r[2 * i + 1]);
             uint4* o = (uint4*)((uint16_t*)p.out.p + at);
-            o[0] = make_uint4(w[0], w[1], w[2], w[3]);
-            o[1] = make_uint4(w[4], w[5], w[6], w[7]);
+#pragma unroll
+            for (int i = 0; i < W / 8; i++)
+                o[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
         } else {
             float4* o = (float4*)((float*)p.out.p + at);
 #pragma unroll
-            for (int i = 0; i < 4; i++)
+            for (int i = 0; i < W / 4; i++)
                 o[i] = make_float4(r[4 * i], r[4 * i + 1], r[4 * i + 2], r[4 * i + 3]);
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < 16; i++)
+        for (int i = 0; i < W; i++)
             if (n + i < p.N) pv_store_one(p.out.p, p.out.bf16, at + i, r[i]);
     }
 }
@@ -432,7 +437,301 @@ __global__ __launch_bounds__(kThreads, 2) void pv_fp8_tile_kernel(Product p, boo
         for (int j = 0; j < 4; j++)
 #pragma unroll
             for (int e = 0; e < 4; e++) v[4 * j + e] = acc[j][i][e];
-        if (m < p.M) store16(p, split, m, n0 + wn + 16 * h, v, vec);
+        if (m < p.M) store_run<16>(p, split, m, n0 + wn + 16 * h, v, vec);
+    }
+}
+
+// The product of rows that are quantised on the way in: x is read once from
+// memory as it is, and no quantised copy of it exists.
+//
+// Eight waves side by side, 64 rows by 32 columns each (those beyond the last
+// column quantise, and multiply nothing): two a SIMD, one's quantising beside
+// the other's products. A block's slices of x and of the weight come into
+// registers two blocks ahead. 16 lanes hold a row's 128 values, take their
+// largest by DPP moves, and put the bytes into LDS with the row's scale; the
+// weight goes through LDS as it is, loaded by whole rows of 128 bytes (as
+// fragments straight from the L2, 16 bytes of 64 rows a load, it took 25 us of 64
+// at 16384 x 4928 -> 256). The barrier of a block waits for LDS alone, never for
+// the loads under way.
+struct Fused {
+    PvRows x;
+    int M, K;
+    const uint8_t* w;   // [N][blocks * 128]
+    const uint8_t* sw;  // [N / 128][blocks]
+};
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+template <bool XB>
+struct XVec {  // eight consecutive values of a row
+    typedef u32x4 at_any __attribute__((aligned(2)));
+    u32x4 w[XB ? 1 : 2];
+    __device__ __forceinline__ float get(int i) const {
+        if constexpr (XB)
+            return __uint_as_float(i & 1 ? w[0][i / 2] & 0xffff0000u : w[0][i / 2] << 16);
+        else
+            return __uint_as_float(w[i / 4][i % 4]);
+    }
+    // The vector at column c0, or the row's last eight columns where it reaches
+    // past them (K >= 8): no branch parts a block's loads.
+    __device__ __forceinline__ void load(const PvRows& x, size_t row, int c0, int K) {
+        const char* p = (const char*)x.p + (row * x.ld + min(c0, K - 8)) * (XB ? 2 : 4);
+        w[0] = *(const at_any*)p;
+        if constexpr (!XB) w[1] = *(const at_any*)(p + 16);
+    }
+    // Values loaded `by` columns early: moved into place, zeros after the row's end.
+    __device__ __forceinline__ void move_down(int by) {
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 8; i++) x[i] = get(i);
+#pragma unroll
+        for (int s = 4; s; s >>= 1) {
+#pragma unroll
+            for (int i = 0; i < 8; i++) x[i] = by & s ? (i + s < 8 ? x[i + s] : 0.f) : x[i];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            const uint32_t u = by >= 8 ? 0u : __float_as_uint(x[i]);
+            if constexpr (!XB)
+                w[i / 4][i % 4] = u;
+            else
+                w[0][i / 2] = i & 1 ? w[0][i / 2] | u : u >> 16;
+        }
+    }
+    // The largest magnitude's bits; at least infinity's where a value may not be
+    // finite.
+    __device__ __forceinline__ uint32_t top() const {
+        if constexpr (XB) {
+            typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+            u16x2 m = {0, 0};
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                const uint32_t u = w[0][i] & 0x7fff7fffu;
+                u16x2 v;
+                __builtin_memcpy(&v, &u, 4);
+                m = __builtin_elementwise_max(m, v);
+            }
+            return (uint32_t)(m[0] > m[1] ? m[0] : m[1]) << 16;
+        } else {
+            float m = 0.f;  // a NaN is passed over
+#pragma unroll
+            for (int i = 0; i < 8; i++) m = fmaxf(m, fabsf(get(i)));
+            return __float_as_uint(m);
+        }
+    }
+    __device__ __forceinline__ uint32_t finite_top() const {
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 8; i++) m = max(m, finite_bits(get(i)));
+        return m;
+    }
+    // The eight as e4m3 of v / scale, a power of two: nearest, ties to even; what
+    // is not finite gives NaN.
+    __device__ __forceinline__ uint2 bytes(float scale) const {
+        typedef short i16x2 __attribute__((ext_vector_type(2)));
+        i16x2 q[2] = {{0, 0}, {0, 0}};
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+            if constexpr (XB) {
+                bf16x2 a, b;
+                const uint32_t u = w[0][2 * i], v = w[0][2 * i + 1];
+                __builtin_memcpy(&a, &u, 4);
+                __builtin_memcpy(&b, &v, 4);
+                q[i] = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(q[i], a, scale, false);
+                q[i] = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(q[i], b, scale, true);
+            } else {
+                q[i] = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(q[i], get(4 * i), get(4 * i + 1),
+                                                                scale, false);
+                q[i] = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(q[i], get(4 * i + 2),
+                                                                get(4 * i + 3), scale, true);
+            }
+        }
+        uint2 r;
+        __builtin_memcpy(&r, q, 8);
+        return r;
+    }
+};
+
+// max over 16 consecutive lanes
+template <int CTRL>
+__device__ __forceinline__ uint32_t max_dpp(uint32_t v) {
+    return max(v, dpp_u32<CTRL, 0xf>(v));
+}
+
+constexpr int kFusedM = 64, kFusedTileN = 256, kFusedThreads = 512, kFusedWaves = 2;
+
+template <bool XB, bool EXACT>
+__global__ __launch_bounds__(kFusedThreads, kFusedWaves) void pv_fp8_fused_kernel(Fused f,
+                                                                                 Product p,
+                                                                                 bool vec) {
+    constexpr int BM = kFusedM, BN = kFusedTileN;
+    // vectors of x a thread; fragments of the weight a wave; its loads a wave
+    constexpr int V = BM * 16 / kFusedThreads, J = 2, W = BN * kB / 16 / kFusedThreads;
+    __shared__ __align__(16) uint8_t lw[2][BN * kB];
+    __shared__ __align__(16) uint8_t la[2][BM * kB];
+    __shared__ __align__(16) uint8_t ls[2][BM];
+    __shared__ uint8_t lsw[BN / kB][PVCONV_FP8_MAX_CHANNELS / kB];  // the weight's scales
+    const int mt = (f.M + BM - 1) / BM, nt = (p.N + BN - 1) / BN;
+    // tiles of one row of tiles run side by side on one XCD, as above
+    const size_t total = (size_t)mt * nt * p.splits, run = (total + 7) / 8;
+    const size_t idx = (size_t)(blockIdx.x & 7) * run + (blockIdx.x >> 3);
+    if ((blockIdx.x >> 3) >= run || idx >= total) return;
+    const int split = (int)(idx / ((size_t)mt * nt));
+    const int t = (int)(idx % ((size_t)mt * nt));
+    const int m0 = t / nt * BM, n0 = t % nt * BN;
+    const int k0 = split * p.per, k1 = min(k0 + p.per, p.blocks);
+
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r = lane & 15, h = lane >> 4;
+    const int wn = wave * 32;  // the wave's columns of the tile
+    const bool multiplies = n0 + wn < p.N;
+    const int xr = threadIdx.x >> 4, xc = (threadIdx.x & 15) * 8;  // row (+ 32 v), column
+    for (int i = threadIdx.x; i < BN / kB * (k1 - k0); i += kFusedThreads) {
+        const int row = i / (k1 - k0), k = i - row * (k1 - k0);
+        lsw[row][k] = f.sw[(size_t)min(n0 / kB + row, (p.N - 1) / kB) * p.blocks + k0 + k];
+    }
+    XVec<XB> xs[2][V];
+    auto fetch_x = [&](XVec<XB>(&to)[V], int k) {
+#pragma unroll
+        for (int v = 0; v < V; v++)
+            to[v].load(f.x, (size_t)min(m0 + xr + (kFusedThreads / 16) * v, f.M - 1), k * kB + xc, f.K);
+    };
+    auto quantise = [&](const XVec<XB>(&from)[V], int k, uint8_t* to, uint8_t* scales) {
+        XVec<XB> x[V];
+        uint32_t top[V], all = 0;
+#pragma unroll
+        for (int v = 0; v < V; v++) x[v] = from[v];
+        if ((k + 1) * kB > f.K) {  // the row's last block
+#pragma unroll
+            for (int v = 0; v < V; v++) x[v].move_down(max(k * kB + xc - (f.K - 8), 0));
+        }
+#pragma unroll
+        for (int v = 0; v < V; v++) {
+            top[v] = x[v].top();
+            all = max(all, top[v]);
+        }
+        if (__builtin_expect(__any(all >= 0x7f800000u), 0)) {
+#pragma unroll
+            for (int v = 0; v < V; v++) top[v] = x[v].finite_top();
+        }
+#pragma unroll
+        for (int v = 0; v < V; v++) top[v] = max_dpp<0xB1>(top[v]);   // quad_perm [1,0,3,2]
+#pragma unroll
+        for (int v = 0; v < V; v++) top[v] = max_dpp<0x4E>(top[v]);   // quad_perm [2,3,0,1]
+#pragma unroll
+        for (int v = 0; v < V; v++) top[v] = max_dpp<0x141>(top[v]);  // row_half_mirror
+#pragma unroll
+        for (int v = 0; v < V; v++) top[v] = max_dpp<0x140>(top[v]);  // row_mirror
+#pragma unroll
+        for (int v = 0; v < V; v++) {
+            // block_exponent + 127, but that zeros may take any scale here
+            const int byte = max((int)((top[v] + 0x1fffffu) >> 23) - 8, 1);
+            const int row = xr + (kFusedThreads / 16) * v;
+            *(uint2*)(to + row * kB + ((xc >> 4) ^ a_key(row)) * 16 + (xc & 8)) =
+                x[v].bytes(__uint_as_float((uint32_t)byte << 23));
+            // row = 16 i + r: byte i of dword r
+            if (xc == 0) scales[(row & 15) * 4 + (row >> 4)] = (uint8_t)byte;
+        }
+    };
+    // this thread's pieces of the weight's slice: eight threads a row
+    const int wr = threadIdx.x >> 3, wc = threadIdx.x & 7;
+    const uint8_t* gw[W];
+#pragma unroll
+    for (int q = 0; q < W; q++)
+        gw[q] = f.w + (size_t)min(n0 + wr + kFusedThreads / 8 * q, p.N - 1) * p.blocks * kB + wc * 16;
+    u32x4 ws[2][W];
+    auto fetch_w = [&](u32x4(&to)[W], int k) {
+#pragma unroll
+        for (int q = 0; q < W; q++) to[q] = *(const u32x4*)(gw[q] + (size_t)k * kB);
+    };
+    auto put_w = [&](const u32x4(&from)[W], uint8_t* to) {
+#pragma unroll
+        for (int q = 0; q < W; q++) {
+            const int row = wr + kFusedThreads / 8 * q;
+            *(u32x4*)(to + row * kB + (wc ^ w_key(row)) * 16) = from[q];
+        }
+    };
+    pv_f32x4 acc[J][4];  // [fragment of the weight][fragment of x]
+#pragma unroll
+    for (int j = 0; j < J; j++)
+#pragma unroll
+        for (int i = 0; i < 4; i++) acc[j][i] = pv_f32x4{0.f, 0.f, 0.f, 0.f};
+    union Frag {
+        u32x4 u[2];
+        i32x8 v;
+    };
+    auto multiply = [&](const uint8_t* lwx, const uint8_t* lx, const uint8_t* lsx, int sw) {
+        Frag fa[4], fw[J];
+#pragma unroll
+        for (int j = 0; j < J; j++) {
+            const int row = wn + 8 * (r >> 2) + 4 * j + (r & 3);
+            fw[j].u[0] = *(const u32x4*)(lwx + row * kB + ((2 * h) ^ w_key(row)) * 16);
+            fw[j].u[1] = *(const u32x4*)(lwx + row * kB + ((2 * h + 1) ^ w_key(row)) * 16);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const int row = 16 * i + r;
+            fa[i].u[0] = *(const u32x4*)(lx + row * kB + ((2 * h) ^ a_key(row)) * 16);
+            fa[i].u[1] = *(const u32x4*)(lx + row * kB + ((2 * h + 1) ^ a_key(row)) * 16);
+        }
+        const uint32_t sa = *(const uint32_t*)(lsx + 4 * r);
+        if constexpr (!EXACT) {
+#pragma unroll
+            for (int j = 0; j < J; j++)
+#pragma unroll
+                for (int i = 0; i < 4; i++)
+                    acc[j][i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+                        fw[j].v, fa[i].v, acc[j][i], 0, 0, 0, sw, 0, (int)(sa >> (8 * i)));
+        } else {
+#pragma unroll
+            for (int q = 0; q < 4; q++) {
+                bf16x8 va[4];
+#pragma unroll
+                for (int i = 0; i < 4; i++)
+                    va[i] = to_bf16(fa[i].v[2 * q], fa[i].v[2 * q + 1], sa >> (8 * i) & 255u);
+#pragma unroll
+                for (int j = 0; j < J; j++) {
+                    const bf16x8 vb = to_bf16(fw[j].v[2 * q], fw[j].v[2 * q + 1], sw);
+#pragma unroll
+                    for (int i = 0; i < 4; i++)
+                        acc[j][i] =
+                            __builtin_amdgcn_mfma_f32_16x16x32_bf16(vb, va[i], acc[j][i], 0, 0, 0);
+                }
+            }
+        }
+    };
+    // Block k. Its loads are not under conditions (past the last block they fetch
+    // that one again): the waits then count the loads under way exactly. Loads
+    // return in order, and x, the slower one, is asked for last.
+    auto block = [&](int k, int st, XVec<XB>(&x_free)[V], u32x4(&w_free)[W]) {
+        pv_lds_barrier();
+        fetch_w(w_free, min(k + 2, k1 - 1));
+        fetch_x(x_free, min(k + 2, k1 - 1));
+        if (multiplies && k < k1) multiply(lw[st], la[st], ls[st], lsw[wn / kB][k - k0]);
+    };
+    fetch_w(ws[0], k0);
+    fetch_x(xs[0], k0);
+    fetch_w(ws[1], min(k0 + 1, k1 - 1));
+    fetch_x(xs[1], min(k0 + 1, k1 - 1));
+    put_w(ws[0], lw[0]);
+    quantise(xs[0], k0, la[0], ls[0]);
+    // (one way out: where blocks are odd in number, the last half multiplies
+    // nothing)
+    for (int k = k0; k < k1; k += 2) {
+        block(k, 0, xs[0], ws[0]);
+        put_w(ws[1], lw[1]);
+        quantise(xs[1], k + 1, la[1], ls[1]);
+        block(k + 1, 1, xs[1], ws[1]);
+        put_w(ws[0], lw[0]);
+        quantise(xs[0], k + 2, la[0], ls[0]);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        const int m = m0 + 16 * i + r;
+        float v[4 * J];
+#pragma unroll
+        for (int j = 0; j < J; j++)
+#pragma unroll
+            for (int e = 0; e < 4; e++) v[4 * j + e] = acc[j][i][e];
+        if (m < f.M && multiplies) store_run<8>(p, split, m, n0 + wn + 8 * h, v, vec);
     }
 }
 
@@ -450,14 +749,21 @@ __global__ __launch_bounds__(kThreads) void pv_fp8_join_kernel(Product p) {
     }
 }
 
-// dbias from the blocks' column sums, in block order
+// dbias from the blocks' column sums, in a fixed order: 16 columns a workgroup,
+// 16 threads a column
 __global__ __launch_bounds__(kThreads) void pv_fp8_bias_kernel(const float* sum, int blocks, int N,
                                                                float* dbias) {
-    const int c = blockIdx.x * kThreads + threadIdx.x;
-    if (c >= N) return;
+    __shared__ double part[kThreads];
+    const int c = blockIdx.x * 16 + (threadIdx.x & 15);
     double s = 0.;
-    for (int i = 0; i < blocks; i++) s += (double)sum[(size_t)i * N + c];
-    dbias[c] = (float)s;
+    if (c < N)
+        for (int i = threadIdx.x >> 4; i < blocks; i += 16) s += (double)sum[(size_t)i * N + c];
+    part[threadIdx.x] = s;
+    __syncthreads();
+    if (threadIdx.x < 16 && c < N) {
+        for (int w = 1; w < 16; w++) s += part[threadIdx.x + 16 * w];
+        dbias[c] = (float)s;
+    }
 }
 
 // the weight's gradient of no rows
@@ -493,8 +799,9 @@ struct Carve {
 // How many ways a product's blocks are split: one where its tiles fill the
 // chip, else enough for about kWanted workgroups of two blocks or more.
 constexpr int kWanted = 512;
-void plan_splits(int M, int N, int blocks, int* per, int* splits) {
-    const size_t tiles = (size_t)((M + kTile - 1) / kTile) * ((N + kTile - 1) / kTile);
+constexpr int kFusedN = 1024;
+void plan_splits(int M, int N, int bm, int bn, int blocks, int* per, int* splits) {
+    const size_t tiles = (size_t)((M + bm - 1) / bm) * ((N + bn - 1) / bn);
     *per = blocks;
     if (tiles > 0 && tiles < kWanted / 2 && blocks > 1) {
         const int most = (blocks + 1) / 2;
@@ -504,11 +811,14 @@ void plan_splits(int M, int N, int blocks, int* per, int* splits) {
     }
     *splits = blocks > 1 ? (blocks + *per - 1) / *per : 1;
 }
-size_t partial_bytes(int M, int N, int blocks) {
+size_t partial_bytes(int M, int N, int bm, int bn, int blocks) {
     int per, splits;
-    plan_splits(M, N, blocks, &per, &splits);
+    plan_splits(M, N, bm, bn, blocks, &per, &splits);
     return splits > 1 ? (size_t)splits * M * N * 4 : 0;
 }
+
+// Whether rows are quantised on the way into the product.
+bool fused(int K, int N) { return K >= 8 && N <= kFusedN; }
 
 struct FwdWs {
     Quantised x;
@@ -518,8 +828,10 @@ struct FwdWs {
 FwdWs carve_fwd(void* base, int M, int K, int N) {
     Carve c{(char*)base, 0};
     FwdWs w;
-    w.x = c.rows(M, K);
-    w.partial = (float*)c.take(partial_bytes(M, N, pv_fp8_blocks(K)));
+    w.x = fused(K, N) ? Quantised{nullptr, nullptr} : c.rows(M, K);
+    w.partial = (float*)c.take(fused(K, N)
+                                   ? partial_bytes(M, N, kFusedM, kFusedTileN, pv_fp8_blocks(K))
+                                   : partial_bytes(M, N, kTile, kTile, pv_fp8_blocks(K)));
     w.total = c.off;
     return w;
 }
@@ -536,7 +848,8 @@ BwdWs carve_bwd(void* base, int M, int K, int N) {
     w.dyt = c.rows(N, M);
     w.xt = c.rows(K, M);
     w.sum = (float*)c.take((size_t)pv_fp8_blocks(M) * N * 4);
-    const size_t px = partial_bytes(M, K, pv_fp8_blocks(N)), pw = partial_bytes(N, K, pv_fp8_blocks(M));
+    const size_t px = partial_bytes(M, K, kTile, kTile, pv_fp8_blocks(N)),
+                 pw = partial_bytes(N, K, kTile, kTile, pv_fp8_blocks(M));
     w.partial = (float*)c.take(px > pw ? px : pw);
     w.total = c.off;
     return w;
@@ -561,16 +874,38 @@ void launch_quantise(const Quantise& z, hipStream_t s) {
     });
 }
 
+bool vector_rows(const Product& p) {
+    return p.splits > 1 ? p.N % 4 == 0
+                        : pv_aligned16(p.out.p) && p.out.ld % (p.out.bf16 ? 8 : 4) == 0;
+}
+
 void launch_product(Product p, hipStream_t s) {
-    plan_splits(p.M, p.N, p.blocks, &p.per, &p.splits);
+    plan_splits(p.M, p.N, kTile, kTile, p.blocks, &p.per, &p.splits);
     const size_t total = (size_t)((p.M + kTile - 1) / kTile) * ((p.N + kTile - 1) / kTile) * p.splits;
     const unsigned grid = (unsigned)((total + 7) / 8 * 8);
-    const bool vec = p.splits > 1 ? p.N % 4 == 0
-                                  : pv_aligned16(p.out.p) && p.out.ld % (p.out.bf16 ? 8 : 4) == 0;
+    const bool vec = vector_rows(p);
     if (p.out.bf16)
         pv_fp8_tile_kernel<false><<<grid, kThreads, 0, s>>>(p, vec);
     else
         pv_fp8_tile_kernel<true><<<grid, kThreads, 0, s>>>(p, vec);
+    if (p.splits > 1)
+        pv_fp8_join_kernel<<<grid_of(((size_t)p.M * p.N + kThreads - 1) / kThreads), kThreads, 0,
+                             s>>>(p);
+}
+
+void launch_fused(const PvRows& x, Product p, hipStream_t s) {
+    plan_splits(p.M, p.N, kFusedM, kFusedTileN, p.blocks, &p.per, &p.splits);
+    const size_t total = (size_t)((p.M + kFusedM - 1) / kFusedM) *
+                         ((p.N + kFusedTileN - 1) / kFusedTileN) * p.splits;
+    const unsigned grid = (unsigned)((total + 7) / 8 * 8);
+    const bool vec = vector_rows(p);
+    const Fused f{x, p.M, p.K, p.b, p.sb};
+    with_bool(x.bf16, [&](auto XB) {
+        with_bool(!p.out.bf16, [&](auto EXACT) {
+            pv_fp8_fused_kernel<decltype(XB)::value, decltype(EXACT)::value>
+                <<<grid, kFusedThreads, 0, s>>>(f, p, vec);
+        });
+    });
     if (p.splits > 1)
         pv_fp8_join_kernel<<<grid_of(((size_t)p.M * p.N + kThreads - 1) / kThreads), kThreads, 0,
                              s>>>(p);
@@ -611,12 +946,17 @@ pvconv_status pv_launch_fp8_linear(const PvRows& x, int M, int K, int N, const u
                                    const uint8_t* scale, const float* bias, int act, float slope,
                                    const PvRows& y, void* ws, hipStream_t s) {
     const FwdWs w = carve_fwd(ws, M, K, N);
-    launch_quantise<kRows>(Quantise{x, M, K, w.x.q, w.x.scale, nullptr, nullptr, nullptr}, s);
     Product p = with_weight(w.x, M, weight, scale, N, pv_fp8_blocks(K), y, w.partial);
+    p.K = K;
     p.bias = bias;
     p.act = act;
     p.slope = slope;
-    launch_product(p, s);
+    if (fused(K, N)) {
+        launch_fused(x, p, s);
+    } else {
+        launch_quantise<kRows>(Quantise{x, M, K, w.x.q, w.x.scale, nullptr, nullptr, nullptr}, s);
+        launch_product(p, s);
+    }
     return pv_launch_status();
 }
 
@@ -663,6 +1003,6 @@ pvconv_status pv_launch_fp8_linear_bwd(const PvRows& dy, const PvRows& x, int M,
             dw, (size_t)N * K);
     }
     if (dbias)
-        pv_fp8_bias_kernel<<<(N + kThreads - 1) / kThreads, kThreads, 0, s>>>(w.sum, mb, N, dbias);
+        pv_fp8_bias_kernel<<<(N + 15) / 16, kThreads, 0, s>>>(w.sum, mb, N, dbias);
     return pv_launch_status();
 }
