@@ -49,10 +49,13 @@ __device__ __forceinline__ uint32_t pack_scaled(float a, float b, float c, float
 
 // The quantisers: a workgroup takes a tile of 128 x 128 into registers, eight
 // columns by eight rows a thread, and writes it in any of
-//   kRows    q[r][cb * 128 ..], scales per row and 128 columns: scale[cb][r]
-//   kCols    qt[c][rb * 128 ..], scales per column and 128 rows: scale_t[rb][c]
-//   kBlock   both, one scale for the tile: scale[rb][cb], scale_t[cb][rb]
+//   kRows    q[cb][r][128], scales per row and 128 columns: scale[cb][r]
+//   kCols    qt[rb][c][128], scales per column and 128 rows: scale_t[rb][c]
+//   kBlock   both as the weight's layouts, q[r][cb * 128 ..], qt[c][rb * 128 ..],
+//            one scale for the tile: scale[rb][cb], scale_t[cb][rb]
 //   kSum     sum[rb][c]: the tile's plain column sums
+// (Block by block, a product's slices are whole: by rows, they would lie a
+// power of two apart where M is one, on few of the memory's channels.)
 // Bound by HBM: one read of x, a byte a value out; the transposed bytes turn
 // around in LDS so that their stores are rows of 128 bytes.
 enum { kRows = 1, kCols = 2, kBlock = 4, kSum = 8 };
@@ -122,7 +125,7 @@ __global__ __launch_bounds__(kThreads) void pv_fp8_quantise_kernel(Quantise z) {
             w.x = pack_scaled(v[r][0], v[r][1], v[r][2], v[r][3], f);
             w.y = pack_scaled(v[r][4], v[r][5], v[r][6], v[r][7], f);
             if (row < z.M) {
-                *(uint2*)(z.q + ((size_t)row * cbs + cb) * kB + cg * 8) = w;
+                *(uint2*)(z.q + ((size_t)cb * z.M + row) * kB + cg * 8) = w;
                 if (cg == 0) z.scale[(size_t)cb * z.M + row] = (uint8_t)(e + 127);
             }
         }
@@ -178,7 +181,9 @@ __global__ __launch_bounds__(kThreads) void pv_fp8_quantise_kernel(Quantise z) {
         __syncthreads();
         const int c = threadIdx.x >> 1, h = (threadIdx.x & 1) * 16;
         if (z.qt && cb * kB + c < z.C) {
-            uint4* to = (uint4*)(z.qt + ((size_t)(cb * kB + c) * rbs + rb) * kB + h * 4);
+            const size_t piece = (WHAT & kBlock) ? (size_t)(cb * kB + c) * rbs + rb
+                                                 : (size_t)rb * z.C + cb * kB + c;
+            uint4* to = (uint4*)(z.qt + piece * kB + h * 4);
 #pragma unroll
             for (int i = 0; i < 4; i++) {
                 const uint32_t* t = turn + c * kPitch + h + 4 * i;
@@ -211,10 +216,11 @@ __global__ __launch_bounds__(kThreads) void pv_fp8_quantise_kernel(Quantise z) {
 // LDS rows are 128 bytes, in 16-byte pieces exchanged by a key of the row
 // (a_key, b_key), so that the lanes of a fragment read fall on all the banks.
 struct Product {
-    const uint8_t* a;   // [M][blocks * 128]
+    const uint8_t* a;   // [blocks][M][128]
     const uint8_t* sa;  // [blocks][M]
     int M;
-    const uint8_t* b;   // [N][blocks * 128]
+    const uint8_t* b;   // block k of row n at n * b_row + k * b_blk
+    size_t b_row, b_blk;
     const uint8_t* sb;  // at (n / step) * sb_row + block * sb_blk
     int step;
     size_t sb_row, sb_blk;
@@ -250,7 +256,15 @@ __device__ __forceinline__ bf16x8 to_bf16(uint32_t lo, uint32_t hi, uint32_t byt
     return u.v;
 }
 
-// W (8 or 16) consecutive outputs of a row from column n on
+// the bias of W consecutive columns from n on (splits get it when they join)
+template <int W>
+__device__ __forceinline__ void load_bias(const Product& p, int n, float (&b)[W]) {
+    const bool have = p.bias && p.splits == 1;
+#pragma unroll
+    for (int i = 0; i < W; i++) b[i] = have ? p.bias[min(n + i, p.N - 1)] : 0.f;
+}
+
+// W (8 or 16) consecutive outputs of a row, their bias added, from column n on
 template <int W>
 __device__ __forceinline__ void store_run(const Product& p, int split, int m, int n,
                                           const float (&v)[W], bool vec) {
@@ -270,10 +284,7 @@ __device__ __forceinline__ void store_run(const Product& p, int split, int m, in
     }
     float r[W];
 #pragma unroll
-    for (int i = 0; i < W; i++) {
-        const float add = p.bias && n + i < p.N ? p.bias[n + i] : 0.f;
-        r[i] = pv_activate(v[i] + add, p.act, p.slope);
-    }
+    for (int i = 0; i < W; i++) r[i] = pv_activate(v[i], p.act, p.slope);
     const size_t at = (size_t)m * p.out.ld + n;
     if (vec && n + W <= p.N) {
         if (p.out.bf16) {
@@ -325,9 +336,8 @@ __global__ __launch_bounds__(kThreads, 2) void pv_fp8_tile_kernel(Product p, boo
 #pragma unroll
     for (int q = 0; q < 4; q++) {
         const int piece = (wave * 4 + q) * 64 + lane, row = piece >> 3, c = piece & 7;
-        ga[q] = p.a + (size_t)min(m0 + row, p.M - 1) * p.blocks * kB + (size_t)k0 * kB +
-                (c ^ a_key(row)) * 16;
-        gb[q] = p.b + (size_t)min(n0 + row, p.N - 1) * p.blocks * kB + (size_t)k0 * kB +
+        ga[q] = p.a + ((size_t)k0 * p.M + min(m0 + row, p.M - 1)) * kB + (c ^ a_key(row)) * 16;
+        gb[q] = p.b + (size_t)min(n0 + row, p.N - 1) * p.b_row + k0 * p.b_blk +
                 (c ^ b_key(row)) * 16;
     }
     const uint8_t* gs;
@@ -359,8 +369,8 @@ __global__ __launch_bounds__(kThreads, 2) void pv_fp8_tile_kernel(Product p, boo
                 (const void __attribute__((address_space(1)))*)gb[q],
                 (void __attribute__((address_space(3)))*)(lb + (wave * 4 + q) * 1024), 16, 0,
                 0);
-            ga[q] += kB;
-            gb[q] += kB;
+            ga[q] += (size_t)p.M * kB;
+            gb[q] += p.b_blk;
         }
     };
     pv_f32x4 acc[4][4];  // [fragment of b][fragment of a]
@@ -390,10 +400,10 @@ __global__ __launch_bounds__(kThreads, 2) void pv_fp8_tile_kernel(Product p, boo
                 uint4 u[2];
                 i32x8 v;
             } f, g;
-            f.u[0] = *(const uint4*)(la + ra * kB + ((2 * h) ^ a_key(ra)) * 16);
-            f.u[1] = *(const uint4*)(la + ra * kB + ((2 * h + 1) ^ a_key(ra)) * 16);
-            g.u[0] = *(const uint4*)(lb + rb * kB + ((2 * h) ^ b_key(rb)) * 16);
-            g.u[1] = *(const uint4*)(lb + rb * kB + ((2 * h + 1) ^ b_key(rb)) * 16);
+            f.u[0] = *(const uint4*)(la + ra * kB + (h ^ a_key(ra)) * 16);
+            f.u[1] = *(const uint4*)(la + ra * kB + ((h + 4) ^ a_key(ra)) * 16);
+            g.u[0] = *(const uint4*)(lb + rb * kB + (h ^ b_key(rb)) * 16);
+            g.u[1] = *(const uint4*)(lb + rb * kB + ((h + 4) ^ b_key(rb)) * 16);
             fa[i] = f.v;
             fb[i] = g.v;
         }
@@ -429,6 +439,8 @@ __global__ __launch_bounds__(kThreads, 2) void pv_fp8_tile_kernel(Product p, boo
         block(k, la0, lb0, ls0, la1, lb1);
         if (k + 1 < k1) block(k + 1, la1, lb1, ls1, la0, lb0);
     }
+    float bias[16];
+    load_bias<16>(p, n0 + wn + 16 * h, bias);
 #pragma unroll
     for (int i = 0; i < 4; i++) {
         const int m = m0 + wm + 16 * i + r;
@@ -436,7 +448,7 @@ __global__ __launch_bounds__(kThreads, 2) void pv_fp8_tile_kernel(Product p, boo
 #pragma unroll
         for (int j = 0; j < 4; j++)
 #pragma unroll
-            for (int e = 0; e < 4; e++) v[4 * j + e] = acc[j][i][e];
+            for (int e = 0; e < 4; e++) v[4 * j + e] = acc[j][i][e] + bias[4 * j + e];
         if (m < p.M) store_run<16>(p, split, m, n0 + wn + 16 * h, v, vec);
     }
 }
@@ -557,6 +569,101 @@ __device__ __forceinline__ uint32_t max_dpp(uint32_t v) {
     return max(v, dpp_u32<CTRL, 0xf>(v));
 }
 
+// A block's 64 rows of x, from registers (THREADS threads, 16 of them a row) into
+// LDS as bytes with their scales.
+template <int THREADS, bool XB>
+__device__ __forceinline__ void quantise_slice(const XVec<XB> (&from)[1024 / THREADS], int k, int K,
+                                               uint8_t* to, uint8_t* scales) {
+    constexpr int V = 1024 / THREADS;
+    const int xr = threadIdx.x >> 4, xc = (threadIdx.x & 15) * 8;
+    XVec<XB> x[V];
+    uint32_t top[V], all = 0;
+#pragma unroll
+    for (int v = 0; v < V; v++) x[v] = from[v];
+    if ((k + 1) * kB > K) {  // the row's last block
+#pragma unroll
+        for (int v = 0; v < V; v++) x[v].move_down(max(k * kB + xc - (K - 8), 0));
+    }
+#pragma unroll
+    for (int v = 0; v < V; v++) {
+        top[v] = x[v].top();
+        all = max(all, top[v]);
+    }
+    if (__builtin_expect(__any(all >= 0x7f800000u), 0)) {
+#pragma unroll
+        for (int v = 0; v < V; v++) top[v] = x[v].finite_top();
+    }
+#pragma unroll
+    for (int v = 0; v < V; v++) top[v] = max_dpp<0xB1>(top[v]);  // quad_perm [1,0,3,2]
+#pragma unroll
+    for (int v = 0; v < V; v++) top[v] = max_dpp<0x4E>(top[v]);  // quad_perm [2,3,0,1]
+#pragma unroll
+    for (int v = 0; v < V; v++) top[v] = max_dpp<0x141>(top[v]);  // row_half_mirror
+#pragma unroll
+    for (int v = 0; v < V; v++) top[v] = max_dpp<0x140>(top[v]);  // row_mirror
+#pragma unroll
+    for (int v = 0; v < V; v++) {
+        // block_exponent + 127, but that zeros may take any scale here
+        const int byte = max((int)((top[v] + 0x1fffffu) >> 23) - 8, 1);
+        const int row = xr + (THREADS / 16) * v;
+        *(uint2*)(to + row * kB + ((xc >> 4) ^ a_key(row)) * 16 + (xc & 8)) =
+            x[v].bytes(__uint_as_float((uint32_t)byte << 23));
+        // row = 16 i + r: byte i of dword r
+        if (xc == 0) scales[(row & 15) * 4 + (row >> 4)] = (uint8_t)byte;
+    }
+}
+
+union Frag {
+    u32x4 u[2];
+    i32x8 v;
+};
+// acc += the wave's 16 J columns of the weight (rows wn + 4 J (r >> 2) + 4 j +
+// (r & 3) of its slice lw, keyed by w_key) times the 64 rows of x (lx, scales
+// lsx), sw the weight's scale.
+template <int J, bool EXACT>
+__device__ __forceinline__ void multiply_slices(pv_f32x4 (&acc)[J][4], const uint8_t* lw, int wn,
+                                                const uint8_t* lx, const uint8_t* lsx, int sw) {
+    const int r = threadIdx.x & 15, h = (threadIdx.x & 63) >> 4;
+    Frag fa[4], fw[J];
+#pragma unroll
+    for (int j = 0; j < J; j++) {
+        const int row = wn + 4 * J * (r >> 2) + 4 * j + (r & 3);
+        fw[j].u[0] = *(const u32x4*)(lw + row * kB + (h ^ w_key(row)) * 16);
+        fw[j].u[1] = *(const u32x4*)(lw + row * kB + ((h + 4) ^ w_key(row)) * 16);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        const int row = 16 * i + r;
+        fa[i].u[0] = *(const u32x4*)(lx + row * kB + (h ^ a_key(row)) * 16);
+        fa[i].u[1] = *(const u32x4*)(lx + row * kB + ((h + 4) ^ a_key(row)) * 16);
+    }
+    const uint32_t sa = *(const uint32_t*)(lsx + 4 * r);
+    if constexpr (!EXACT) {
+#pragma unroll
+        for (int j = 0; j < J; j++)
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+                acc[j][i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+                    fw[j].v, fa[i].v, acc[j][i], 0, 0, 0, sw, 0, (int)(sa >> (8 * i)));
+    } else {
+#pragma unroll
+        for (int q = 0; q < 4; q++) {
+            bf16x8 va[4];
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+                va[i] = to_bf16(fa[i].v[2 * q], fa[i].v[2 * q + 1], sa >> (8 * i) & 255u);
+#pragma unroll
+            for (int j = 0; j < J; j++) {
+                const bf16x8 vb = to_bf16(fw[j].v[2 * q], fw[j].v[2 * q + 1], sw);
+#pragma unroll
+                for (int i = 0; i < 4; i++)
+                    acc[j][i] =
+                        __builtin_amdgcn_mfma_f32_16x16x32_bf16(vb, va[i], acc[j][i], 0, 0, 0);
+            }
+        }
+    }
+}
+
 constexpr int kFusedM = 64, kFusedTileN = 256, kFusedThreads = 512, kFusedWaves = 2;
 
 template <bool XB, bool EXACT>
@@ -595,41 +702,7 @@ __global__ __launch_bounds__(kFusedThreads, kFusedWaves) void pv_fp8_fused_kerne
             to[v].load(f.x, (size_t)min(m0 + xr + (kFusedThreads / 16) * v, f.M - 1), k * kB + xc, f.K);
     };
     auto quantise = [&](const XVec<XB>(&from)[V], int k, uint8_t* to, uint8_t* scales) {
-        XVec<XB> x[V];
-        uint32_t top[V], all = 0;
-#pragma unroll
-        for (int v = 0; v < V; v++) x[v] = from[v];
-        if ((k + 1) * kB > f.K) {  // the row's last block
-#pragma unroll
-            for (int v = 0; v < V; v++) x[v].move_down(max(k * kB + xc - (f.K - 8), 0));
-        }
-#pragma unroll
-        for (int v = 0; v < V; v++) {
-            top[v] = x[v].top();
-            all = max(all, top[v]);
-        }
-        if (__builtin_expect(__any(all >= 0x7f800000u), 0)) {
-#pragma unroll
-            for (int v = 0; v < V; v++) top[v] = x[v].finite_top();
-        }
-#pragma unroll
-        for (int v = 0; v < V; v++) top[v] = max_dpp<0xB1>(top[v]);   // quad_perm [1,0,3,2]
-#pragma unroll
-        for (int v = 0; v < V; v++) top[v] = max_dpp<0x4E>(top[v]);   // quad_perm [2,3,0,1]
-#pragma unroll
-        for (int v = 0; v < V; v++) top[v] = max_dpp<0x141>(top[v]);  // row_half_mirror
-#pragma unroll
-        for (int v = 0; v < V; v++) top[v] = max_dpp<0x140>(top[v]);  // row_mirror
-#pragma unroll
-        for (int v = 0; v < V; v++) {
-            // block_exponent + 127, but that zeros may take any scale here
-            const int byte = max((int)((top[v] + 0x1fffffu) >> 23) - 8, 1);
-            const int row = xr + (kFusedThreads / 16) * v;
-            *(uint2*)(to + row * kB + ((xc >> 4) ^ a_key(row)) * 16 + (xc & 8)) =
-                x[v].bytes(__uint_as_float((uint32_t)byte << 23));
-            // row = 16 i + r: byte i of dword r
-            if (xc == 0) scales[(row & 15) * 4 + (row >> 4)] = (uint8_t)byte;
-        }
+        quantise_slice<kFusedThreads>(from, k, f.K, to, scales);
     };
     // this thread's pieces of the weight's slice: eight threads a row
     const int wr = threadIdx.x >> 3, wc = threadIdx.x & 7;
@@ -654,50 +727,6 @@ __global__ __launch_bounds__(kFusedThreads, kFusedWaves) void pv_fp8_fused_kerne
     for (int j = 0; j < J; j++)
 #pragma unroll
         for (int i = 0; i < 4; i++) acc[j][i] = pv_f32x4{0.f, 0.f, 0.f, 0.f};
-    union Frag {
-        u32x4 u[2];
-        i32x8 v;
-    };
-    auto multiply = [&](const uint8_t* lwx, const uint8_t* lx, const uint8_t* lsx, int sw) {
-        Frag fa[4], fw[J];
-#pragma unroll
-        for (int j = 0; j < J; j++) {
-            const int row = wn + 8 * (r >> 2) + 4 * j + (r & 3);
-            fw[j].u[0] = *(const u32x4*)(lwx + row * kB + ((2 * h) ^ w_key(row)) * 16);
-            fw[j].u[1] = *(const u32x4*)(lwx + row * kB + ((2 * h + 1) ^ w_key(row)) * 16);
-        }
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-            const int row = 16 * i + r;
-            fa[i].u[0] = *(const u32x4*)(lx + row * kB + ((2 * h) ^ a_key(row)) * 16);
-            fa[i].u[1] = *(const u32x4*)(lx + row * kB + ((2 * h + 1) ^ a_key(row)) * 16);
-        }
-        const uint32_t sa = *(const uint32_t*)(lsx + 4 * r);
-        if constexpr (!EXACT) {
-#pragma unroll
-            for (int j = 0; j < J; j++)
-#pragma unroll
-                for (int i = 0; i < 4; i++)
-                    acc[j][i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
-                        fw[j].v, fa[i].v, acc[j][i], 0, 0, 0, sw, 0, (int)(sa >> (8 * i)));
-        } else {
-#pragma unroll
-            for (int q = 0; q < 4; q++) {
-                bf16x8 va[4];
-#pragma unroll
-                for (int i = 0; i < 4; i++)
-                    va[i] = to_bf16(fa[i].v[2 * q], fa[i].v[2 * q + 1], sa >> (8 * i) & 255u);
-#pragma unroll
-                for (int j = 0; j < J; j++) {
-                    const bf16x8 vb = to_bf16(fw[j].v[2 * q], fw[j].v[2 * q + 1], sw);
-#pragma unroll
-                    for (int i = 0; i < 4; i++)
-                        acc[j][i] =
-                            __builtin_amdgcn_mfma_f32_16x16x32_bf16(vb, va[i], acc[j][i], 0, 0, 0);
-                }
-            }
-        }
-    };
     // Block k. Its loads are not under conditions (past the last block they fetch
     // that one again): the waits then count the loads under way exactly. Loads
     // return in order, and x, the slower one, is asked for last.
@@ -705,7 +734,8 @@ __global__ __launch_bounds__(kFusedThreads, kFusedWaves) void pv_fp8_fused_kerne
         pv_lds_barrier();
         fetch_w(w_free, min(k + 2, k1 - 1));
         fetch_x(x_free, min(k + 2, k1 - 1));
-        if (multiplies && k < k1) multiply(lw[st], la[st], ls[st], lsw[wn / kB][k - k0]);
+        if (multiplies && k < k1)
+            multiply_slices<J, EXACT>(acc, lw[st], wn, la[st], ls[st], lsw[wn / kB][k - k0]);
     };
     fetch_w(ws[0], k0);
     fetch_x(xs[0], k0);
@@ -723,6 +753,8 @@ __global__ __launch_bounds__(kFusedThreads, kFusedWaves) void pv_fp8_fused_kerne
         put_w(ws[0], lw[0]);
         quantise(xs[0], k + 2, la[0], ls[0]);
     }
+    float bias[4 * J];
+    load_bias<4 * J>(p, n0 + wn + 8 * h, bias);
 #pragma unroll
     for (int i = 0; i < 4; i++) {
         const int m = m0 + 16 * i + r;
@@ -730,8 +762,124 @@ __global__ __launch_bounds__(kFusedThreads, kFusedWaves) void pv_fp8_fused_kerne
 #pragma unroll
         for (int j = 0; j < J; j++)
 #pragma unroll
-            for (int e = 0; e < 4; e++) v[4 * j + e] = acc[j][i][e];
+            for (int e = 0; e < 4; e++) v[4 * j + e] = acc[j][i][e] + bias[4 * j + e];
         if (m < f.M && multiplies) store_run<8>(p, split, m, n0 + wn + 8 * h, v, vec);
+    }
+}
+
+// The same for rows short enough to stay: a workgroup quantises its 64 rows
+// whole into LDS once (up to kResidentBlocks blocks of 8 KB) and goes over a
+// share of the columns, 128 at a time, the weight's slices flowing through two
+// stages without a stop from one tile of columns to the next. x is read once
+// for all of the share, the outputs are the traffic. Four waves side by side, 64
+// rows by 32 columns each.
+constexpr int kResidentThreads = 256, kResidentN = 128, kResidentBlocks = 8;
+constexpr int kResidentShare = 16;  // tiles of columns a workgroup at most: their bias lies in LDS
+
+template <bool XB, bool EXACT>
+__global__ __launch_bounds__(kResidentThreads, 2) void pv_fp8_resident_kernel(Fused f, Product p,
+                                                                             bool vec, int share) {
+    constexpr int BM = kFusedM, BN = kResidentN, T = kResidentThreads;
+    constexpr int V = BM * 16 / T, J = 2, W = BN * kB / 16 / T;
+    __shared__ __align__(16) uint8_t lw[2][BN * kB];
+    __shared__ __align__(16) uint8_t ls[kResidentBlocks][BM];
+    __shared__ uint8_t lsw[kResidentShare * kResidentBlocks];  // a scale a step
+    __shared__ __align__(16) float lbias[kResidentShare * BN];
+    extern __shared__ __align__(16) uint8_t la[];  // [blocks][BM * 128]
+    const int nt = (p.N + BN - 1) / BN, shares = (nt + share - 1) / share;
+    const int m0 = (int)(blockIdx.x / shares) * BM, t0 = (int)(blockIdx.x % shares) * share;
+    const int steps = (min(t0 + share, nt) - t0) * p.blocks;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r = lane & 15, h = lane >> 4;
+    const int wn = wave * 32;
+
+    const int wr = threadIdx.x >> 3, wc = threadIdx.x & 7;
+    u32x4 ws[2][W];
+    // The steps in order: the blocks of a tile of columns, then the next tile's
+    // (past the last step, that one again).
+    const uint8_t* gw[W];
+    auto rows_of = [&](int t) {
+#pragma unroll
+        for (int q = 0; q < W; q++)
+            gw[q] = f.w + (size_t)min(t * BN + wr + T / 8 * q, p.N - 1) * p.blocks * kB + wc * 16;
+    };
+    int fs = 0, ft = t0, fk = 0;
+    auto fetch_w = [&](u32x4(&to)[W]) {
+#pragma unroll
+        for (int q = 0; q < W; q++) to[q] = *(const u32x4*)(gw[q] + (size_t)fk * kB);
+        if (++fs < steps) {
+            if (++fk == p.blocks) {
+                fk = 0;
+                rows_of(++ft);
+            }
+        }
+    };
+    rows_of(t0);
+    auto put_w = [&](const u32x4(&from)[W], uint8_t* to) {
+#pragma unroll
+        for (int q = 0; q < W; q++) {
+            const int row = wr + T / 8 * q;
+            *(u32x4*)(to + row * kB + (wc ^ w_key(row)) * 16) = from[q];
+        }
+    };
+    fetch_w(ws[0]);
+    fetch_w(ws[1]);
+    for (int i = threadIdx.x; i < steps; i += T) lsw[i] = f.sw[(size_t)t0 * p.blocks + i];
+    for (int i = threadIdx.x; i < share * BN; i += T)
+        lbias[i] = p.bias ? p.bias[min(t0 * BN + i, p.N - 1)] : 0.f;
+    XVec<XB> xs[2][V];
+    auto fetch_x = [&](XVec<XB>(&to)[V], int k) {
+#pragma unroll
+        for (int v = 0; v < V; v++)
+            to[v].load(f.x, (size_t)min(m0 + (int)(threadIdx.x >> 4) + (T / 16) * v, f.M - 1),
+                       min(k, p.blocks - 1) * kB + (threadIdx.x & 15) * 8, f.K);
+    };
+    fetch_x(xs[0], 0);
+    fetch_x(xs[1], 1);
+    for (int k = 0; k < p.blocks; k += 2) {
+        quantise_slice<T>(xs[0], k, f.K, la + (size_t)k * BM * kB, ls[k]);
+        fetch_x(xs[0], k + 2);
+        if (k + 1 < p.blocks)
+            quantise_slice<T>(xs[1], k + 1, f.K, la + (size_t)(k + 1) * BM * kB, ls[k + 1]);
+        fetch_x(xs[1], k + 3);
+    }
+    pv_f32x4 acc[J][4];
+    int t = t0, k = 0;
+    auto step = [&](int s, const uint8_t* lws, u32x4(&w_free)[W], const u32x4(&w_next)[W],
+                    uint8_t* lw_next) {
+        pv_lds_barrier();
+        fetch_w(w_free);
+        if (k == 0) {
+#pragma unroll
+            for (int j = 0; j < J; j++)
+#pragma unroll
+                for (int i = 0; i < 4; i++) acc[j][i] = pv_f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+        if (s < steps && t * BN + wn < p.N)
+            multiply_slices<J, EXACT>(acc, lws, wn, la + (size_t)k * BM * kB, ls[k],
+                                      lsw[s]);
+        put_w(w_next, lw_next);
+        if (++k < p.blocks) return;
+        if (s < steps && t * BN + wn < p.N) {
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                const int m = m0 + 16 * i + r;
+                float v[4 * J];
+#pragma unroll
+                for (int j = 0; j < J; j++)
+#pragma unroll
+                    for (int e = 0; e < 4; e++)
+                        v[4 * j + e] = acc[j][i][e] +
+                                       lbias[(t - t0) * BN + wn + 8 * h + 4 * j + e];
+                if (m < f.M) store_run<8>(p, 0, m, t * BN + wn + 8 * h, v, vec);
+            }
+        }
+        k = 0;
+        t++;
+    };
+    put_w(ws[0], lw[0]);
+    for (int s = 0; s < steps; s += 2) {
+        step(s, lw[0], ws[0], ws[1], lw[1]);
+        step(s + 1, lw[1], ws[1], ws[0], lw[0]);
     }
 }
 
@@ -797,7 +945,8 @@ struct Carve {
     }
 };
 // How many ways a product's blocks are split: one where its tiles fill the
-// chip, else enough for about kWanted workgroups of two blocks or more.
+// chip, else enough for kWanted workgroups at most (two a CU: more would wait
+// for a second round), of two blocks or more.
 constexpr int kWanted = 512;
 constexpr int kFusedN = 1024;
 void plan_splits(int M, int N, int bm, int bn, int blocks, int* per, int* splits) {
@@ -805,7 +954,7 @@ void plan_splits(int M, int N, int bm, int bn, int blocks, int* per, int* splits
     *per = blocks;
     if (tiles > 0 && tiles < kWanted / 2 && blocks > 1) {
         const int most = (blocks + 1) / 2;
-        int n = (int)((kWanted + tiles - 1) / tiles);
+        int n = (int)(kWanted / tiles);
         n = n < 1 ? 1 : (n > most ? most : n);
         *per = (blocks + n - 1) / n;
     }
@@ -817,40 +966,45 @@ size_t partial_bytes(int M, int N, int bm, int bn, int blocks) {
     return splits > 1 ? (size_t)splits * M * N * 4 : 0;
 }
 
-// Whether rows are quantised on the way into the product.
-bool fused(int K, int N) { return K >= 8 && N <= kFusedN; }
+// How a product of rows by a weight runs: rows that stay in LDS, rows quantised
+// on the way in, or the quantiser and the product apart (also rows of fewer
+// channels than a vector).
+enum Path { kResident, kFused, kApart };
+Path path_of(int K, int N) {
+    if (K < 8) return kApart;
+    if (N > kFusedTileN && pv_fp8_blocks(K) <= kResidentBlocks) return kResident;
+    return N <= kFusedN ? kFused : kApart;
+}
 
-struct FwdWs {
+struct RowsWs {  // of a product of rows by a weight
     Quantised x;
     float* partial;
-    size_t total;
 };
-FwdWs carve_fwd(void* base, int M, int K, int N) {
-    Carve c{(char*)base, 0};
-    FwdWs w;
-    w.x = fused(K, N) ? Quantised{nullptr, nullptr} : c.rows(M, K);
-    w.partial = (float*)c.take(fused(K, N)
-                                   ? partial_bytes(M, N, kFusedM, kFusedTileN, pv_fp8_blocks(K))
-                                   : partial_bytes(M, N, kTile, kTile, pv_fp8_blocks(K)));
-    w.total = c.off;
+RowsWs carve_rows(Carve& c, int M, int K, int N) {
+    const Path path = path_of(K, N);
+    RowsWs w{{nullptr, nullptr}, nullptr};
+    if (path == kApart) w.x = c.rows(M, K);
+    if (path != kResident)
+        w.partial = (float*)c.take(
+            path == kFused ? partial_bytes(M, N, kFusedM, kFusedTileN, pv_fp8_blocks(K))
+                           : partial_bytes(M, N, kTile, kTile, pv_fp8_blocks(K)));
     return w;
 }
 struct BwdWs {
-    Quantised dy, dyt, xt;
+    RowsWs dx;
+    Quantised dyt, xt;
     float* sum;
-    float* partial;  // dx's, then dw's
+    float* partial;  // dw's
     size_t total;
 };
 BwdWs carve_bwd(void* base, int M, int K, int N) {
     Carve c{(char*)base, 0};
     BwdWs w;
-    w.dy = c.rows(M, N);
+    w.dx = carve_rows(c, M, N, K);
     w.dyt = c.rows(N, M);
     w.xt = c.rows(K, M);
     w.sum = (float*)c.take((size_t)pv_fp8_blocks(M) * N * 4);
-    const size_t px = partial_bytes(M, K, kTile, kTile, pv_fp8_blocks(N)),
-                 pw = partial_bytes(N, K, kTile, kTile, pv_fp8_blocks(M));
-    w.partial = (float*)c.take(px > pw ? px : pw);
+    w.partial = (float*)c.take(partial_bytes(N, K, kTile, kTile, pv_fp8_blocks(M)));
     w.total = c.off;
     return w;
 }
@@ -911,6 +1065,25 @@ void launch_fused(const PvRows& x, Product p, hipStream_t s) {
                              s>>>(p);
 }
 
+void launch_resident(const PvRows& x, const Product& p, hipStream_t s) {
+    // shares of the columns: enough workgroups for the chip, few rows quantised twice
+    const int mt = (p.M + kFusedM - 1) / kFusedM, nt = (p.N + kResidentN - 1) / kResidentN;
+    const int least = (nt + kResidentShare - 1) / kResidentShare;
+    int shares = kWanted / mt;
+    shares = shares < least ? least : (shares > nt ? nt : shares);
+    const int share = (nt + shares - 1) / shares;
+    shares = (nt + share - 1) / share;
+    const bool vec = vector_rows(p);
+    const Fused f{x, p.M, p.K, p.b, p.sb};
+    with_bool(x.bf16, [&](auto XB) {
+        with_bool(!p.out.bf16, [&](auto EXACT) {
+            pv_fp8_resident_kernel<decltype(XB)::value, decltype(EXACT)::value>
+                <<<(unsigned)((size_t)mt * shares), kResidentThreads,
+                   (size_t)p.blocks * kFusedM * kB, s>>>(f, p, vec, share);
+        });
+    });
+}
+
 // The weight (or its transpose) as the product's second operand.
 Product with_weight(const Quantised& a, int M, const uint8_t* w, const uint8_t* sw, int N,
                     int blocks, const PvRows& out, float* partial) {
@@ -919,6 +1092,8 @@ Product with_weight(const Quantised& a, int M, const uint8_t* w, const uint8_t* 
     p.sa = a.scale;
     p.M = M;
     p.b = w;
+    p.b_row = (size_t)blocks * kB;
+    p.b_blk = kB;
     p.sb = sw;
     p.step = kB;
     p.sb_row = blocks;
@@ -931,6 +1106,27 @@ Product with_weight(const Quantised& a, int M, const uint8_t* w, const uint8_t* 
     return p;
 }
 
+// out = act( Q(x) W^T + bias )
+void launch_rows_product(const PvRows& x, int M, int K, int N, const uint8_t* weight,
+                         const uint8_t* scale, const float* bias, int act, float slope,
+                         const PvRows& out, const RowsWs& w, hipStream_t s) {
+    Product p = with_weight(w.x, M, weight, scale, N, pv_fp8_blocks(K), out, w.partial);
+    p.K = K;
+    p.bias = bias;
+    p.act = act;
+    p.slope = slope;
+    p.splits = 1;
+    switch (path_of(K, N)) {
+        case kResident: launch_resident(x, p, s); break;
+        case kFused: launch_fused(x, p, s); break;
+        case kApart:
+            launch_quantise<kRows>(
+                Quantise{x, M, K, w.x.q, w.x.scale, nullptr, nullptr, nullptr}, s);
+            launch_product(p, s);
+            break;
+    }
+}
+
 }  // namespace
 
 pvconv_status pv_launch_fp8_quantize_weight(const PvRows& w, int N, int K, uint8_t* q,
@@ -940,23 +1136,17 @@ pvconv_status pv_launch_fp8_quantize_weight(const PvRows& w, int N, int K, uint8
     return pv_launch_status();
 }
 
-size_t pv_fp8_linear_ws_bytes(int M, int K, int N) { return carve_fwd(nullptr, M, K, N).total; }
+size_t pv_fp8_linear_ws_bytes(int M, int K, int N) {
+    Carve c{nullptr, 0};
+    carve_rows(c, M, K, N);
+    return c.off;
+}
 
 pvconv_status pv_launch_fp8_linear(const PvRows& x, int M, int K, int N, const uint8_t* weight,
                                    const uint8_t* scale, const float* bias, int act, float slope,
                                    const PvRows& y, void* ws, hipStream_t s) {
-    const FwdWs w = carve_fwd(ws, M, K, N);
-    Product p = with_weight(w.x, M, weight, scale, N, pv_fp8_blocks(K), y, w.partial);
-    p.K = K;
-    p.bias = bias;
-    p.act = act;
-    p.slope = slope;
-    if (fused(K, N)) {
-        launch_fused(x, p, s);
-    } else {
-        launch_quantise<kRows>(Quantise{x, M, K, w.x.q, w.x.scale, nullptr, nullptr, nullptr}, s);
-        launch_product(p, s);
-    }
+    Carve c{(char*)ws, 0};
+    launch_rows_product(x, M, K, N, weight, scale, bias, act, slope, y, carve_rows(c, M, K, N), s);
     return pv_launch_status();
 }
 
@@ -968,19 +1158,18 @@ pvconv_status pv_launch_fp8_linear_bwd(const PvRows& dy, const PvRows& x, int M,
                                        hipStream_t s) {
     const BwdWs w = carve_bwd(ws, M, K, N);
     const int mb = pv_fp8_blocks(M);
-    if (M) {
-        const Quantise z{dy, M, N, w.dy.q, w.dy.scale, w.dyt.q, w.dyt.scale, w.sum};
-        if (dx.p && dw && dbias)
-            launch_quantise<kRows | kCols | kSum>(z, s);
-        else {
-            if (dx.p) launch_quantise<kRows>(z, s);
-            if (dw) launch_quantise<kCols>(z, s);
-            if (dbias) launch_quantise<kSum>(z, s);
-        }
-    }
     if (dx.p && M)
-        launch_product(with_weight(w.dy, M, weight_t, scale_t, K, pv_fp8_blocks(N), dx, w.partial),
-                       s);
+        launch_rows_product(dy, M, N, K, weight_t, scale_t, nullptr, PVCONV_ACT_NONE, 0.f, dx, w.dx,
+                            s);
+    if (M) {
+        const Quantise z{dy, M, N, nullptr, nullptr, w.dyt.q, w.dyt.scale, w.sum};
+        if (dw && dbias)
+            launch_quantise<kCols | kSum>(z, s);
+        else if (dw)
+            launch_quantise<kCols>(z, s);
+        else if (dbias)
+            launch_quantise<kSum>(z, s);
+    }
     if (dw && M) {
         launch_quantise<kCols>(Quantise{x, M, K, nullptr, nullptr, w.xt.q, w.xt.scale, nullptr}, s);
         Product p{};
@@ -988,6 +1177,8 @@ pvconv_status pv_launch_fp8_linear_bwd(const PvRows& dy, const PvRows& x, int M,
         p.sa = w.dyt.scale;
         p.M = N;
         p.b = w.xt.q;
+        p.b_row = kB;
+        p.b_blk = (size_t)K * kB;
         p.sb = w.xt.scale;
         p.step = 1;
         p.sb_row = 1;
