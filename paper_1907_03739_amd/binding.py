@@ -596,39 +596,69 @@ def pvconv_act_bn_backward(dy: torch.Tensor, y: torch.Tensor, bn=None, act="leak
 # include/pvconv_train.h: group norm, 8-bit linear layer, distillation loss
 # ----------------------------------------------------------------------------
 def _workspace(need: int, given: Optional[torch.Tensor], device):
-    """The caller's workspace where it is large enough, else a new one."""
+    """The caller's workspace where it is large enough, else a new one; None
+    where none is needed."""
+    if need == 0:
+        return None
     if given is not None and given.numel() * given.element_size() >= need:
         return given
-    return torch.empty(max(need, 256), dtype=torch.uint8, device=device)
+    return torch.empty(need, dtype=torch.uint8, device=device)
 
 
-def _ws_bytes(t: torch.Tensor) -> int:
-    return t.numel() * t.element_size()
+# These calls run in a few microseconds, as do their kernels at the smallest
+# sizes: pointers go to ctypes as plain integers, dense tensors are recognised
+# before any stride is looked at, and each check is made once.
+def _ws_size(ws: Optional[torch.Tensor]) -> int:
+    return 0 if ws is None else ws.numel() * ws.element_size()
 
 
-def _same_device(first: torch.Tensor, *others):
-    for t in others:
-        if t is not None and t.device != first.device:
+def _ptr(t: Optional[torch.Tensor]):
+    return None if t is None else t.data_ptr()
+
+
+def _raw_stream(device) -> int:
+    return torch.cuda.current_stream(device).cuda_stream
+
+
+# the handle without a Stream object around it, where torch offers it (0.1 for 2 us)
+_handle_of = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+if _handle_of is not None:
+    def _raw_stream(device) -> int:  # noqa: F811
+        return _handle_of(device.index)
+
+
+def _like(t: torch.Tensor, dtype):
+    """A new dense tensor of t's shape in that dtype (t's if None)."""
+    if (dtype is None or dtype is t.dtype) and t.is_contiguous():
+        return torch.empty_like(t)
+    return torch.empty(t.shape, dtype=_torch_dt(dtype or t.dtype), device=t.device)
+
+
+def _on_device(device, *tensors):
+    for t in tensors:
+        if t is not None and t.device != device:
             raise ValueError("all tensors must be on one device")
 
 
 def _vector(t: Optional[torch.Tensor], n: int, dtype, what: str):
-    """A contiguous [n] tensor of that dtype, or None."""
-    if t is not None and (t.dtype != dtype or tuple(t.shape) != (n,) or not t.is_contiguous()):
+    """A contiguous [n] tensor of that dtype, or None; its pointer."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
         raise ValueError(f"{what} must be a contiguous [{n}] {dtype} tensor")
-    return t
+    return t.data_ptr()
 
 
 def _matrix_rows(t: torch.Tensor, ncols: int) -> tuple:
     """(rows, row stride) of a [.., ncols] tensor whose rows are evenly spaced:
-    every leading dimension continues the one after it. Rows of one element or
-    none take the stride that a dense array has."""
+    every leading dimension continues the one after it. A single row, or none,
+    takes the stride that a dense array has."""
     if t.dim() < 1 or t.shape[-1] != ncols:
         raise ValueError("channel count mismatch")
     rows = 1
     for d in t.shape[:-1]:
-        rows *= int(d)
-    if t.numel() == 0:
+        rows *= d
+    if t.is_contiguous() or rows == 0:
         return rows, ncols
     if ncols > 1 and t.stride(-1) != 1:
         raise ValueError("channels must be the innermost, contiguous dimension")
@@ -662,12 +692,12 @@ def pvconv_group_norm_act(x: torch.Tensor, groups: int, gamma: torch.Tensor, bet
         raise ValueError("x must be [B][N][C]")
     B, N, C = x.shape
     _, ld = _matrix_rows(x, C)
-    _same_device(x, gamma, beta, lengths, out, workspace)
-    _vector(gamma, C, torch.float32, "gamma")
-    _vector(beta, C, torch.float32, "beta")
-    _vector(lengths, B, torch.int32, "lengths")
+    _on_device(x.device, gamma, beta, lengths, out, workspace)
+    gamma_p = _vector(gamma, C, torch.float32, "gamma")
+    beta_p = _vector(beta, C, torch.float32, "beta")
+    lengths_p = _vector(lengths, B, torch.int32, "lengths")
     if out is None:
-        out = torch.empty((B, N, C), dtype=_torch_dt(out_dtype or x.dtype), device=x.device)
+        out = _like(x, out_dtype)
     elif tuple(out.shape) != (B, N, C):
         raise ValueError("out must have x's shape")
     _, old = _matrix_rows(out, C)
@@ -678,8 +708,8 @@ def pvconv_group_norm_act(x: torch.Tensor, groups: int, gamma: torch.Tensor, bet
     ws = _workspace(_lib.pvconv_group_norm_act_workspace_size(B, N, C, groups), workspace,
                     x.device)
     _check("pvconv_group_norm_act", _lib.pvconv_group_norm_act(
-        _p(x), _dt(x), ld, B, N, C, groups, _p(lengths), _p(gamma), _p(beta), eps, ACT_NORM[act],
-        slope, _p(out), _dt(out), old, _p(stats), _p(ws), _ws_bytes(ws), _stream(x)))
+        _ptr(x), _dt(x), ld, B, N, C, groups, lengths_p, gamma_p, beta_p, eps, ACT_NORM[act],
+        slope, _ptr(out), _dt(out), old, _ptr(stats), _ptr(ws), _ws_size(ws), _raw_stream(x.device)))
     return (out, stats) if want_stats else out
 
 
@@ -696,17 +726,17 @@ def pvconv_group_norm_act_backward(dy: torch.Tensor, x: torch.Tensor, stats: tor
     B, N, C = x.shape
     _, ld = _matrix_rows(x, C)
     _, dld = _matrix_rows(dy, C)
-    _same_device(x, dy, stats, gamma, beta, lengths, out, workspace)
-    _vector(gamma, C, torch.float32, "gamma")
-    _vector(beta, C, torch.float32, "beta")
-    _vector(lengths, B, torch.int32, "lengths")
+    _on_device(x.device, dy, stats, gamma, beta, lengths, out, workspace)
+    gamma_p = _vector(gamma, C, torch.float32, "gamma")
+    beta_p = _vector(beta, C, torch.float32, "beta")
+    lengths_p = _vector(lengths, B, torch.int32, "lengths")
     if groups < 1 or C % groups:
         raise ValueError("groups must divide the channels")
     if tuple(stats.shape) != (B, groups, 2) or stats.dtype != torch.float32 or \
             not stats.is_contiguous():
         raise ValueError("stats must be the forward's [B][groups][2] float32")
     if out is None:
-        out = torch.empty((B, N, C), dtype=_torch_dt(out_dtype or x.dtype), device=x.device)
+        out = _like(x, out_dtype)
     elif tuple(out.shape) != (B, N, C):
         raise ValueError("out must have x's shape")
     _, old = _matrix_rows(out, C)
@@ -715,9 +745,9 @@ def pvconv_group_norm_act_backward(dy: torch.Tensor, x: torch.Tensor, stats: tor
     ws = _workspace(_lib.pvconv_group_norm_act_backward_workspace_size(B, N, C, groups),
                     workspace, x.device)
     _check("pvconv_group_norm_act_backward", _lib.pvconv_group_norm_act_backward(
-        _p(dy), _dt(dy), dld, _p(x), _dt(x), ld, B, N, C, groups, _p(lengths), _p(stats),
-        _p(gamma), _p(beta), ACT_NORM[act], slope, _p(out), _dt(out), old, _p(dgamma), _p(dbeta),
-        _p(ws), _ws_bytes(ws), _stream(x)))
+        _ptr(dy), _dt(dy), dld, _ptr(x), _dt(x), ld, B, N, C, groups, lengths_p, _ptr(stats),
+        gamma_p, beta_p, ACT_NORM[act], slope, _ptr(out), _dt(out), old, _ptr(dgamma), _ptr(dbeta),
+        _ptr(ws), _ws_size(ws), _raw_stream(x.device)))
     return out, dgamma, dbeta
 
 
@@ -752,7 +782,7 @@ def pvconv_fp8_quantize_weight(w: torch.Tensor, transposed: bool = False):
     if transposed:
         qt, st = torch.empty((K, nb * FP8_BLOCK), **f8), torch.empty((kb, nb), **u8)
     _check("pvconv_fp8_quantize_weight", _lib.pvconv_fp8_quantize_weight(
-        _p(w), _dt(w), ld, N, K, _p(q), _p(s), _p(qt), _p(st), _stream(w)))
+        _ptr(w), _dt(w), ld, N, K, _ptr(q), _ptr(s), _ptr(qt), _ptr(st), _raw_stream(w.device)))
     return (q, s, qt, st) if transposed else (q, s)
 
 
@@ -764,8 +794,8 @@ def pvconv_fp8_linear(x: torch.Tensor, weight: torch.Tensor, scale: torch.Tensor
     act(x W^T + bias) [..][N] in out_dtype (x's if None)."""
     K, N = x.shape[-1], weight.shape[0]
     _fp8_operand(weight, scale, K, "weight")
-    _same_device(x, weight, scale, bias, out, workspace)
-    _vector(bias, N, torch.float32, "bias")
+    _on_device(x.device, weight, scale, bias, out, workspace)
+    bias_p = _vector(bias, N, torch.float32, "bias")
     M, ld = _matrix_rows(x, K)
     shape = tuple(x.shape[:-1]) + (N,)
     if out is None:
@@ -775,8 +805,8 @@ def pvconv_fp8_linear(x: torch.Tensor, weight: torch.Tensor, scale: torch.Tensor
     _, old = _matrix_rows(out, N)
     ws = _workspace(_lib.pvconv_fp8_linear_workspace_size(M, K, N), workspace, x.device)
     _check("pvconv_fp8_linear", _lib.pvconv_fp8_linear(
-        _p(x), _dt(x), ld, M, K, N, _p(weight), _p(scale), _p(bias), ACT[act], slope, _p(out),
-        _dt(out), old, _p(ws), _ws_bytes(ws), _stream(x)))
+        _ptr(x), _dt(x), ld, M, K, N, _ptr(weight), _ptr(scale), bias_p, ACT[act], slope, _ptr(out),
+        _dt(out), old, _ptr(ws), _ws_size(ws), _raw_stream(x.device)))
     return out
 
 
@@ -795,7 +825,7 @@ def pvconv_fp8_linear_backward(dy: torch.Tensor, x: Optional[torch.Tensor],
     if not (want_dx or want_dw or want_dbias):
         raise ValueError("nothing is wanted")
     K = x.shape[-1] if x is not None else weight_t.shape[0] if weight_t is not None else 1
-    _same_device(dy, x, weight_t, scale_t, workspace)
+    _on_device(dy.device, x, weight_t, scale_t, workspace)
     ld = 0
     if x is not None:
         rows, ld = _matrix_rows(x, K)
@@ -812,9 +842,9 @@ def pvconv_fp8_linear_backward(dy: torch.Tensor, x: Optional[torch.Tensor],
     db = torch.empty((N,), **f32) if want_dbias else None
     ws = _workspace(_lib.pvconv_fp8_linear_backward_workspace_size(M, K, N), workspace, dy.device)
     _check("pvconv_fp8_linear_backward", _lib.pvconv_fp8_linear_backward(
-        _p(dy), _dt(dy), dld, _p(x) if want_dw else None, _dt(x) if x is not None else F32, ld, M,
-        K, N, _p(weight_t) if want_dx else None, _p(scale_t) if want_dx else None, _p(dx),
-        _dt(dx) if want_dx else F32, 0, _p(dw), _p(db), _p(ws), _ws_bytes(ws), _stream(dy)))
+        _ptr(dy), _dt(dy), dld, _ptr(x) if want_dw else None, _dt(x) if x is not None else F32, ld, M,
+        K, N, _ptr(weight_t) if want_dx else None, _ptr(scale_t) if want_dx else None, _ptr(dx),
+        _dt(dx) if want_dx else F32, 0, _ptr(dw), _ptr(db), _ptr(ws), _ws_size(ws), _raw_stream(dy.device)))
     return dx, dw, db
 
 
@@ -827,8 +857,7 @@ def _distill_args(z, t_val, t_class, labels):
             t_val.dtype != torch.float32 or t_class.dtype != torch.int32 or \
             not t_val.is_contiguous() or not t_class.is_contiguous():
         raise ValueError("t_val and t_class must be contiguous [M][top] float32 and int32")
-    _vector(labels, M, torch.int32, "labels")
-    return M, V, ld, t_val.shape[1]
+    return M, V, ld, t_val.shape[1], _vector(labels, M, torch.int32, "labels")
 
 
 def pvconv_distill_topk(z: torch.Tensor, t_val: torch.Tensor, t_class: torch.Tensor,
@@ -839,24 +868,23 @@ def pvconv_distill_topk(z: torch.Tensor, t_val: torch.Tensor, t_class: torch.Ten
     """z [M][V] (rows evenly strided), t_val, t_class [M][top], labels [M] int32 ->
     (loss [M], lse [M][2]), and with want_grad (loss, lse, dz [M][V] in out_dtype
     (z's if None)): the gradient of sum(row_weight * loss)."""
-    M, V, ld, top = _distill_args(z, t_val, t_class, labels)
-    _same_device(z, t_val, t_class, labels, row_weight, out, workspace)
-    _vector(row_weight, M, torch.float32, "row_weight")
+    M, V, ld, top, labels_p = _distill_args(z, t_val, t_class, labels)
+    _on_device(z.device, t_val, t_class, labels, row_weight, out, workspace)
+    weight_p = _vector(row_weight, M, torch.float32, "row_weight")
     loss = torch.empty((M,), dtype=torch.float32, device=z.device)
     lse = torch.empty((M, 2), dtype=torch.float32, device=z.device)
     dz, dld = None, 0
     if want_grad:
-        dz = out if out is not None else torch.empty(
-            (M, V), dtype=_torch_dt(out_dtype or z.dtype), device=z.device)
+        dz = out if out is not None else _like(z, out_dtype)
         if tuple(dz.shape) != (M, V):
             raise ValueError("out must have z's shape")
         _, dld = _matrix_rows(dz, V)
     need = _lib.pvconv_distill_topk_workspace_size(M, V)
-    ws = _workspace(need, workspace, z.device) if need else None
+    ws = _workspace(need, workspace, z.device)
     _check("pvconv_distill_topk", _lib.pvconv_distill_topk(
-        _p(z), _dt(z), ld, M, V, _p(t_val), _p(t_class), top, _p(labels), temperature, alpha,
-        _p(row_weight), _p(loss), _p(lse), _p(dz), _dt(dz) if want_grad else F32, dld, _p(ws),
-        _ws_bytes(ws) if need else 0, _stream(z)))
+        _ptr(z), _dt(z), ld, M, V, _ptr(t_val), _ptr(t_class), top, labels_p, temperature, alpha,
+        weight_p, _ptr(loss), _ptr(lse), _ptr(dz), _dt(dz) if want_grad else F32, dld, _ptr(ws),
+        _ws_size(ws), _raw_stream(z.device)))
     return (loss, lse, dz) if want_grad else (loss, lse)
 
 
@@ -866,19 +894,18 @@ def pvconv_distill_topk_backward(z: torch.Tensor, t_val: torch.Tensor, t_class: 
                                  alpha: float = 1.0, out: Optional[torch.Tensor] = None,
                                  out_dtype=None):
     """The gradient dz [M][V] of sum(dloss * loss) from the forward's lse."""
-    M, V, ld, top = _distill_args(z, t_val, t_class, labels)
-    _same_device(z, t_val, t_class, labels, lse, dloss, out)
-    _vector(dloss, M, torch.float32, "dloss")
+    M, V, ld, top, labels_p = _distill_args(z, t_val, t_class, labels)
+    _on_device(z.device, t_val, t_class, labels, lse, dloss, out)
+    dloss_p = _vector(dloss, M, torch.float32, "dloss")
     if tuple(lse.shape) != (M, 2) or lse.dtype != torch.float32 or not lse.is_contiguous():
         raise ValueError("lse must be the forward's [M][2] float32")
-    dz = out if out is not None else torch.empty(
-        (M, V), dtype=_torch_dt(out_dtype or z.dtype), device=z.device)
+    dz = out if out is not None else _like(z, out_dtype)
     if tuple(dz.shape) != (M, V):
         raise ValueError("out must have z's shape")
     _, dld = _matrix_rows(dz, V)
     _check("pvconv_distill_topk_backward", _lib.pvconv_distill_topk_backward(
-        _p(z), _dt(z), ld, M, V, _p(t_val), _p(t_class), top, _p(labels), temperature, alpha,
-        _p(lse), _p(dloss), _p(dz), _dt(dz), dld, _stream(z)))
+        _ptr(z), _dt(z), ld, M, V, _ptr(t_val), _ptr(t_class), top, labels_p, temperature, alpha,
+        _ptr(lse), dloss_p, _ptr(dz), _dt(dz), dld, _raw_stream(z.device)))
     return dz
 
 

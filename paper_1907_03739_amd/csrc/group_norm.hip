@@ -1,10 +1,12 @@
 // Group normalisation with an activation, channels last, and its gradients
 // (pvconv_train.h).
 //
-// Two launches a direction. The first sums a share ("chunk") of a cloud's rows
-// over a slab of whole groups; the second adds the chunks' sums of its groups
-// in a fixed order and applies them to a chunk of rows. Bound by HBM: x (and
-// dy) read twice, y (dx) written once.
+// A group of a cloud that fits the registers of a workgroup is read once, by one
+// launch a direction (pv_gn_held_*: up to 8192 vectors). Larger ones take two
+// launches: the first sums a share ("chunk") of a cloud's rows over a slab of
+// whole groups; the second adds the chunks' sums of its groups in a fixed order
+// and applies them to a chunk of rows. Bound by HBM: there x (and dy) are read
+// twice, y (dx) is written once.
 #include <type_traits>
 
 #include "pv_train.h"
@@ -434,29 +436,267 @@ __global__ __launch_bounds__(kThreads) void pv_gn_bwd_apply_kernel(
     }
 }
 
+// ---------------------------------------------------------------------------
+// Groups held in registers: a workgroup of T threads a (cloud, group), U vectors
+// a thread, rows in parallel over the threads. The mean is summed first, the
+// squares about it then, both from the registers.
+// ---------------------------------------------------------------------------
+template <int T>
+__device__ __forceinline__ double2 group_sum(double a, double b, double2* lds) {
+    a = wave_sum(a);
+    b = wave_sum(b);
+    if constexpr (T > 64) {
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = make_double2(a, b);
+        __syncthreads();
+        a = b = 0.;
+#pragma unroll
+        for (int w = 0; w < T / 64; w++) {
+            a += lds[w].x;
+            b += lds[w].y;
+        }
+    }
+    return make_double2(a, b);
+}
+
+template <int T, int VEC>
+struct Held {
+    int b, g, c, n, par, row;  // cloud, group, first channel, valid rows; this thread's place
+    bool active;
+    __device__ Held(const PvNorm& p, size_t item) {
+        g = (int)((uint32_t)item % (uint32_t)p.groups);
+        b = (int)((uint32_t)item / (uint32_t)p.groups);
+        n = p.lengths ? min(max(p.lengths[b], 0), p.N) : p.N;
+        const int CG = p.C / p.groups, cols = CG / VEC;
+        par = T / cols;
+        row = threadIdx.x / cols;
+        active = row < par;
+        c = g * CG + (threadIdx.x - row * cols) * VEC;
+    }
+};
+
+// Workgroups go round the XCDs: each XCD takes a run of (cloud, group), so that
+// the groups of a cloud, whose rows share cache lines, share an L2.
+__device__ __forceinline__ size_t run_of_xcd(size_t items) {
+    const size_t run = (items + 7) / 8;
+    const size_t i = (size_t)(blockIdx.x & 7) * run + (blockIdx.x >> 3);
+    return (blockIdx.x >> 3) < run && i < items ? i : items;
+}
+
+template <int T, int U, int TYPES, bool SILU, int VEC>
+__global__ __launch_bounds__(T) void pv_gn_held_kernel(PvNorm n, PvRows x, PvRows y, float neg,
+                                                       float2* stats) {
+    __shared__ double2 lds[T / 64];
+    const size_t item = run_of_xcd((size_t)n.B * n.groups);
+    if (item >= (size_t)n.B * n.groups) return;
+    const Held<T, VEC> p(n, item);
+    Raw<TYPES, VEC> f[U];
+    float ga[VEC], be[VEC];
+    if (p.active) {
+        load_params<VEC>(n, p.c, ga, be);
+#pragma unroll
+        for (int u = 0; u < U; u++)
+            f[u].load(x, (size_t)p.b * n.N + max(min(p.row + u * p.par, p.n - 1), 0), p.c);
+    }
+    double s = 0.;
+    if (p.active)
+#pragma unroll
+        for (int u = 0; u < U; u++)
+            if (p.row + u * p.par < p.n)
+#pragma unroll
+                for (int i = 0; i < VEC; i++) s += (double)f[u].get(i);
+    const double cnt = (double)p.n * (n.C / n.groups);
+    const double mean = cnt > 0. ? group_sum<T>(s, 0., lds).x / cnt : 0.;
+    const float m = (float)mean;
+    float q = 0.f;
+    if (p.active)
+#pragma unroll
+        for (int u = 0; u < U; u++)
+            if (p.row + u * p.par < p.n)
+#pragma unroll
+                for (int i = 0; i < VEC; i++) {
+                    const float d = f[u].get(i) - m;
+                    q = fmaf(d, d, q);
+                }
+    float2 st = make_float2(0.f, 0.f);
+    if (cnt > 0.) {
+        const double off = mean - (double)m;
+        const double var = group_sum<T>((double)q, 0., lds).x / cnt - off * off;
+        st = make_float2(m, (float)(1. / sqrt((var < 0. ? 0. : var) + (double)n.eps)));
+    }
+    if (stats && threadIdx.x == 0) stats[item] = st;
+    if (!p.active) return;
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+        const int k = p.row + u * p.par;
+        if (k >= n.N) continue;
+        float r[VEC];
+#pragma unroll
+        for (int i = 0; i < VEC; i++)
+            r[i] = act_of<SILU>(fmaf(ga[i], (f[u].get(i) - st.x) * st.y, be[i]), neg);
+        if (k >= p.n)
+#pragma unroll
+            for (int i = 0; i < VEC; i++) r[i] = 0.f;
+        store_row<TYPES, VEC>(y, (size_t)p.b * n.N + k, p.c, r);
+    }
+}
+
+// chan[b][c] = (sum dv xh, sum dv), or dgamma and dbeta themselves of one cloud.
+template <int T, int U, int TYPES, bool SILU, int VEC>
+__global__ __launch_bounds__(T) void pv_gn_held_bwd_kernel(PvNorm n, PvRows dy, PvRows x, PvRows dx,
+                                                           float neg, const float2* stats,
+                                                           float2* chan, float* dgamma,
+                                                           float* dbeta) {
+    __shared__ double2 lds[T / 64];
+    extern __shared__ float2 red[];  // [T * VEC]
+    const size_t item = run_of_xcd((size_t)n.B * n.groups);
+    if (item >= (size_t)n.B * n.groups) return;
+    const Held<T, VEC> p(n, item);
+    const int CG = n.C / n.groups;
+    const float2 st = stats[item];
+    Raw<TYPES, VEC> f[U], g[U];
+    float ga[VEC], be[VEC], h[VEC], s[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; i++) h[i] = s[i] = 0.f;
+    double t = 0., tt = 0.;
+    if (p.active) {
+        load_params<VEC>(n, p.c, ga, be);
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            const size_t row = (size_t)p.b * n.N + max(min(p.row + u * p.par, p.n - 1), 0);
+            f[u].load(x, row, p.c);
+            g[u].load(dy, row, p.c);
+        }
+#pragma unroll
+        for (int u = 0; u < U; u++)
+            if (p.row + u * p.par < p.n)
+#pragma unroll
+                for (int i = 0; i < VEC; i++) {
+                    const float xh = (f[u].get(i) - st.x) * st.y;
+                    const float dv = g[u].get(i) * dact_of<SILU>(fmaf(ga[i], xh, be[i]), neg);
+                    s[i] += dv;
+                    h[i] = fmaf(dv, xh, h[i]);
+                }
+#pragma unroll
+        for (int i = 0; i < VEC; i++) {
+            t = fma((double)ga[i], (double)s[i], t);
+            tt = fma((double)ga[i], (double)h[i], tt);
+            red[threadIdx.x * VEC + i] = make_float2(h[i], s[i]);
+        }
+    }
+    const double2 sum = group_sum<T>(t, tt, lds);  // (also the barrier after red)
+    // the channels' sums over the rows in parallel: shares of them a thread each,
+    // then a wave a channel over the shares
+    const int parts = min(min(T / CG, 64), p.par);
+    auto keep = [&](int i, double a, double b) {
+        const int c = p.g * CG + i;
+        if (chan) {
+            chan[(size_t)p.b * n.C + c] = make_float2((float)a, (float)b);
+        } else {
+            if (dgamma) dgamma[c] = (float)a;
+            if (dbeta) dbeta[c] = (float)b;
+        }
+    };
+    if (parts > 1) {
+        const int i = threadIdx.x % CG, part = threadIdx.x / CG;
+        float2 e = make_float2(0.f, 0.f);
+        if (part < parts)
+            for (int r = part; r < p.par; r += parts) {
+                e.x += red[r * CG + i].x;
+                e.y += red[r * CG + i].y;
+            }
+        __syncthreads();
+        if (part < parts) red[part * CG + i] = e;
+        __syncthreads();
+        const int lane = threadIdx.x & 63;
+        for (int c = threadIdx.x >> 6; c < CG; c += T / 64) {
+            const float2 v = lane < parts ? red[lane * CG + c] : make_float2(0.f, 0.f);
+            const double a = wave_sum((double)v.x), b = wave_sum((double)v.y);
+            if (lane == 0) keep(c, a, b);
+        }
+    } else {
+        for (int i = threadIdx.x; i < CG; i += T) {
+            double a = 0., b = 0.;
+            for (int r = 0; r < p.par; r++) {
+                a += (double)red[r * CG + i].x;
+                b += (double)red[r * CG + i].y;
+            }
+            keep(i, a, b);
+        }
+    }
+    if (!p.active) return;
+    const double cnt = p.n > 0 ? (double)p.n * CG : 1.;
+    const float m1 = (float)(sum.x / cnt), m2 = (float)(sum.y / cnt);
+    load_params<VEC>(n, p.c, ga, be);  // (again: not held over the sums)
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+        const int k = p.row + u * p.par;
+        if (k >= n.N) continue;
+        float r[VEC];
+#pragma unroll
+        for (int i = 0; i < VEC; i++) {
+            const float xh = (f[u].get(i) - st.x) * st.y;
+            const float dv = g[u].get(i) * dact_of<SILU>(fmaf(ga[i], xh, be[i]), neg);
+            r[i] = st.y * (fmaf(ga[i], dv, -m1) - xh * m2);
+        }
+        if (k >= p.n)
+#pragma unroll
+            for (int i = 0; i < VEC; i++) r[i] = 0.f;
+        store_row<TYPES, VEC>(dx, (size_t)p.b * n.N + k, p.c, r);
+    }
+}
+
+// dgamma, dbeta from the clouds' sums, 16 channels a workgroup, in cloud order
+__global__ __launch_bounds__(kThreads) void pv_gn_params_kernel(int B, int C, const float2* chan,
+                                                                float* dgamma, float* dbeta) {
+    __shared__ double2 red[kThreads];
+    const int ch = threadIdx.x % kParamChannels, share = threadIdx.x / kParamChannels;
+    const int c = blockIdx.x * kParamChannels + ch;
+    double t = 0., u = 0.;
+    if (c < C)
+        for (int r = share; r < B; r += kThreads / kParamChannels) {
+            const float2 e = chan[(size_t)r * C + c];
+            t += (double)e.x;
+            u += (double)e.y;
+        }
+    red[threadIdx.x] = make_double2(t, u);
+    __syncthreads();
+    if (share == 0 && c < C) {
+        for (int w = 1; w < kThreads / kParamChannels; w++) {
+            t += red[ch + kParamChannels * w].x;
+            u += red[ch + kParamChannels * w].y;
+        }
+        if (dgamma) dgamma[c] = (float)t;
+        if (dbeta) dbeta[c] = (float)u;
+    }
+}
+
 unsigned grid_of(size_t items) { return (unsigned)(items < (1u << 20) ? items : 1u << 20); }
 
-// Vector width: whole vectors in a group and a row, and aligned rows.
-int width_for(int CG, const PvRows* r, int count) {
-    int v = 8;
-    for (int i = 0; i < count; i++) {
-        const int w = pv_vec_width(8, r[i].bf16 ? 2 : 4, r[i].p, CG, r[i].ld);
-        v = w < v ? w : v;
-    }
-    return v;
-}
 int types_of(const PvRows* r, int count) {
     int bf16 = 0;
     for (int i = 0; i < count; i++) bf16 += r[i].bf16 ? 1 : 0;
     return bf16 == count ? kBf16 : (bf16 == 0 ? kF32 : kMixed);
 }
-
+// Vector width: whole vectors in a group and a row, aligned rows, 16 bytes at
+// most of the widest type.
+int width_for(int CG, const PvRows* r, int count) {
+    const int most = types_of(r, count) == kBf16 ? 8 : 4;
+    int v = most;
+    for (int i = 0; i < count; i++) {
+        const int w = pv_vec_width(most, r[i].bf16 ? 2 : 4, r[i].p, CG, r[i].ld);
+        v = w < v ? w : v;
+    }
+    return v;
+}
 // f with the call's types, activation and vector width as constants
 template <typename F>
 void with_kind(int types, bool silu, int vec, F f) {
     auto vecs = [&](auto T, auto S) {
         switch (vec) {
-            case 8: f(T, S, std::integral_constant<int, 8>()); break;
+            case 8:
+                if constexpr (decltype(T)::value == kBf16) f(T, S, std::integral_constant<int, 8>());
+                break;
             case 4: f(T, S, std::integral_constant<int, 4>()); break;
             case 2: f(T, S, std::integral_constant<int, 2>()); break;
             default: f(T, S, std::integral_constant<int, 1>()); break;
@@ -473,6 +713,19 @@ void with_kind(int types, bool silu, int vec, F f) {
         case kF32: acts(std::integral_constant<int, kF32>()); break;
         default: acts(std::integral_constant<int, kMixed>()); break;
     }
+}
+
+// Whether a group fits the registers of a workgroup, and of which: vectors a
+// thread of 256 (kSmallU) or of 1024 (kLargeU, kLargeBwdU: a gradient holds x and
+// dy). One (cloud, group) a workgroup, up to 2^31 of them.
+constexpr int kSmallT = 256, kSmallU = 2, kLargeT = 1024, kLargeU = 8, kLargeBwdU = 4;
+enum Hold { kNot, kSmall, kLarge };
+Hold hold_of(const PvNorm& n, int vec, int large_u) {
+    if (n.N < 1 || (size_t)n.B * n.groups >= (1u << 31) - 8) return kNot;
+    const int cols = n.C / n.groups / vec;
+    if (cols <= kSmallT && n.N <= kSmallT / cols * kSmallU) return kSmall;
+    if (cols <= kLargeT && n.N <= kLargeT / cols * large_u) return kLarge;
+    return kNot;
 }
 
 float negative_slope(const PvNorm& n) {
@@ -502,6 +755,18 @@ pvconv_status pv_launch_group_norm(const PvNorm& n, const PvRows& x, const PvRow
               [&](auto T, auto S, auto V) {
                   constexpr int TYPES = decltype(T)::value, VEC = decltype(V)::value;
                   constexpr bool SILU = decltype(S)::value;
+                  const unsigned held = (unsigned)(((size_t)n.B * n.groups + 7) / 8 * 8);
+                  switch (hold_of(n, VEC, kLargeU)) {
+                      case kSmall:
+                          pv_gn_held_kernel<kSmallT, kSmallU, TYPES, SILU, VEC>
+                              <<<held, kSmallT, 0, s>>>(n, x, y, neg, (float2*)stats);
+                          return;
+                      case kLarge:
+                          pv_gn_held_kernel<kLargeT, kLargeU, TYPES, SILU, VEC>
+                              <<<held, kLargeT, 0, s>>>(n, x, y, neg, (float2*)stats);
+                          return;
+                      case kNot: break;
+                  }
                   pv_gn_sums_kernel<TYPES, VEC>
                       <<<grid_of(d.items), kThreads, 0, s>>>(n, d, x, (double2*)ws, per);
                   pv_gn_apply_kernel<TYPES, SILU, VEC>
@@ -529,6 +794,23 @@ pvconv_status pv_launch_group_norm_bwd(const PvNorm& norm, const PvRows& dy, con
               [&](auto T, auto S, auto V) {
                   constexpr int TYPES = decltype(T)::value, VEC = decltype(V)::value;
                   constexpr bool SILU = decltype(S)::value;
+                  const Hold hold = n.B ? hold_of(n, VEC, kLargeBwdU) : kNot;
+                  if (hold != kNot) {
+                      const unsigned held = (unsigned)(((size_t)n.B * n.groups + 7) / 8 * 8);
+                      float2* sums = n.B > 1 ? (float2*)ws : nullptr;
+                      if (hold == kSmall)
+                          pv_gn_held_bwd_kernel<kSmallT, kSmallU, TYPES, SILU, VEC>
+                              <<<held, kSmallT, kSmallT * VEC * sizeof(float2), s>>>(
+                                  n, dy, x, dx, neg, (const float2*)stats, sums, dgamma, dbeta);
+                      else
+                          pv_gn_held_bwd_kernel<kLargeT, kLargeBwdU, TYPES, SILU, VEC>
+                              <<<held, kLargeT, kLargeT * VEC * sizeof(float2), s>>>(
+                                  n, dy, x, dx, neg, (const float2*)stats, sums, dgamma, dbeta);
+                      if (sums && (dgamma || dbeta))
+                          pv_gn_params_kernel<<<(n.C + kParamChannels - 1) / kParamChannels,
+                                                kThreads, 0, s>>>(n.B, n.C, sums, dgamma, dbeta);
+                      return;
+                  }
                   if (d.items)
                       pv_gn_bwd_sums_kernel<TYPES, SILU, VEC>
                           <<<grid_of(d.items), kThreads, 0, s>>>(
