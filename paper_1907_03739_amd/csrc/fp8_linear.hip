@@ -29,22 +29,124 @@ __device__ __forceinline__ uint32_t finite_bits(float v) {
     const uint32_t u = __float_as_uint(v) & 0x7fffffffu;
     return u < 0x7f800000u ? u : 0u;
 }
-// a value that is not finite becomes NaN
-__device__ __forceinline__ float nan_unless_finite(float v) {
-    return (__float_as_uint(v) & 0x7fffffffu) < 0x7f800000u ? v : __uint_as_float(0x7fc00000u);
+// Four values of v / scale, a power of two, as e4m3 bytes: nearest, ties to even;
+// what is not finite gives NaN.
+typedef short i16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t pack_scaled(float a, float b, float c, float d, float scale) {
+    i16x2 q = {0, 0};
+    q = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(q, a, b, scale, false);
+    q = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(q, c, d, scale, true);
+    uint32_t r;
+    __builtin_memcpy(&r, &q, 4);
+    return r;
 }
 
-// Four values, already scaled, as e4m3 bytes (round to nearest even).
-__device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d) {
-    int r = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
-    r = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, r, true);
-    return (uint32_t)r;
-}
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
-// The same of values still to be scaled by f; not finite: NaN.
-__device__ __forceinline__ uint32_t pack_scaled(float a, float b, float c, float d, float f) {
-    return pack_e4m3(nan_unless_finite(a) * f, nan_unless_finite(b) * f, nan_unless_finite(c) * f,
-                     nan_unless_finite(d) * f);
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+template <bool XB>
+struct XVec {  // eight consecutive values of a row
+    typedef u32x4 at_any __attribute__((aligned(2)));
+    u32x4 w[XB ? 1 : 2];
+    __device__ __forceinline__ float get(int i) const {
+        if constexpr (XB)
+            return __uint_as_float(i & 1 ? w[0][i / 2] & 0xffff0000u : w[0][i / 2] << 16);
+        else
+            return __uint_as_float(w[i / 4][i % 4]);
+    }
+    // The vector at column c0, or the row's last eight columns where it reaches
+    // past them (K >= 8): no branch parts a block's loads.
+    __device__ __forceinline__ void load(const PvRows& x, size_t row, int c0, int K) {
+        const char* p = (const char*)x.p + (row * x.ld + min(c0, K - 8)) * (XB ? 2 : 4);
+        w[0] = *(const at_any*)p;
+        if constexpr (!XB) w[1] = *(const at_any*)(p + 16);
+    }
+    __device__ __forceinline__ void set(const uint32_t (&e)[8]) {  // bits of floats
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            if constexpr (!XB)
+                w[i / 4][i % 4] = e[i];
+            else
+                w[0][i / 2] = i & 1 ? w[0][i / 2] | e[i] : e[i] >> 16;
+        }
+    }
+    __device__ __forceinline__ void clear() {
+        w[0] = u32x4{0, 0, 0, 0};
+        if constexpr (!XB) w[1] = u32x4{0, 0, 0, 0};
+    }
+    // Values loaded `by` columns early: moved into place, zeros after the row's end.
+    __device__ __forceinline__ void move_down(int by) {
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 8; i++) x[i] = get(i);
+#pragma unroll
+        for (int s = 4; s; s >>= 1) {
+#pragma unroll
+            for (int i = 0; i < 8; i++) x[i] = by & s ? (i + s < 8 ? x[i + s] : 0.f) : x[i];
+        }
+        uint32_t e[8];
+#pragma unroll
+        for (int i = 0; i < 8; i++) e[i] = by >= 8 ? 0u : __float_as_uint(x[i]);
+        set(e);
+    }
+    // The largest magnitude's bits; at least infinity's where a value may not be
+    // finite.
+    __device__ __forceinline__ uint32_t top() const {
+        if constexpr (XB) {
+            typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+            u16x2 m = {0, 0};
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                const uint32_t u = w[0][i] & 0x7fff7fffu;
+                u16x2 v;
+                __builtin_memcpy(&v, &u, 4);
+                m = __builtin_elementwise_max(m, v);
+            }
+            return (uint32_t)(m[0] > m[1] ? m[0] : m[1]) << 16;
+        } else {
+            float m = 0.f;  // a NaN is passed over
+#pragma unroll
+            for (int i = 0; i < 8; i++) m = fmaxf(m, fabsf(get(i)));
+            return __float_as_uint(m);
+        }
+    }
+    __device__ __forceinline__ uint32_t finite_top() const {
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 8; i++) m = max(m, finite_bits(get(i)));
+        return m;
+    }
+    // The eight as e4m3 of v / scale, a power of two: nearest, ties to even; what
+    // is not finite gives NaN.
+    __device__ __forceinline__ uint2 bytes(float scale) const {
+        i16x2 q[2] = {{0, 0}, {0, 0}};
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+            if constexpr (XB) {
+                bf16x2 a, b;
+                const uint32_t u = w[0][2 * i], v = w[0][2 * i + 1];
+                __builtin_memcpy(&a, &u, 4);
+                __builtin_memcpy(&b, &v, 4);
+                q[i] = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(q[i], a, scale, false);
+                q[i] = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(q[i], b, scale, true);
+            } else {
+                q[i] = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(q[i], get(4 * i), get(4 * i + 1),
+                                                                scale, false);
+                q[i] = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(q[i], get(4 * i + 2),
+                                                                get(4 * i + 3), scale, true);
+            }
+        }
+        uint2 r;
+        __builtin_memcpy(&r, q, 8);
+        return r;
+    }
+};
+
+// max over 16 consecutive lanes
+template <int CTRL>
+__device__ __forceinline__ uint32_t max_dpp(uint32_t v) {
+    return max(v, dpp_u32<CTRL, 0xf>(v));
 }
 
 // The quantisers: a workgroup takes a tile of 128 x 128 into registers, eight
@@ -58,7 +160,7 @@ __device__ __forceinline__ uint32_t pack_scaled(float a, float b, float c, float
 // power of two apart where M is one, on few of the memory's channels.)
 // Bound by HBM: one read of x, a byte a value out; the transposed bytes turn
 // around in LDS so that their stores are rows of 128 bytes.
-enum { kRows = 1, kCols = 2, kBlock = 4, kSum = 8 };
+enum { kRows = 1, kCols = 2, kBlock = 4, kSum = 8 };  // kSum: where `sum` is set
 struct Quantise {
     PvRows x;
     int M, C;      // rows, columns
@@ -68,6 +170,11 @@ struct Quantise {
     uint8_t* scale_t;
     float* sum;
 };
+// One launch quantises a's tiles, then b's (of b.x.p set).
+struct QuantiseJobs {
+    Quantise a, b;
+    int tiles_a;
+};
 constexpr int kPitch = 33;  // dwords a transposed column in LDS (32 and one to spread the banks)
 
 __device__ __forceinline__ uint32_t max_over_row16(uint32_t v) {  // 16 consecutive lanes
@@ -76,37 +183,53 @@ __device__ __forceinline__ uint32_t max_over_row16(uint32_t v) {  // 16 consecut
     return v;
 }
 
-template <bool XB, bool VEC, int WHAT>
-__global__ __launch_bounds__(kThreads) void pv_fp8_quantise_kernel(Quantise z) {
+template <bool XB, bool NARROW, int WHAT>
+__global__ __launch_bounds__(kThreads) void pv_fp8_quantise_kernel(QuantiseJobs jobs) {
     constexpr bool kT = (WHAT & (kCols | kBlock)) != 0;
     __shared__ uint32_t turn[kT ? kB * kPitch : 1];
     __shared__ uint32_t tops[4][kB];
     __shared__ float sums[(WHAT & kSum) ? 4 : 1][kB];
+    const bool second = (int)blockIdx.x >= jobs.tiles_a;
+    const Quantise z = second ? jobs.b : jobs.a;
+    const int tile = (int)blockIdx.x - (second ? jobs.tiles_a : 0);
     const int cbs = pv_fp8_blocks(z.C), rbs = pv_fp8_blocks(z.M);
-    const int rb = blockIdx.x / cbs, cb = blockIdx.x % cbs;
+    const int rb = tile / cbs, cb = tile % cbs;
     const int wave = threadIdx.x >> 6, cg = threadIdx.x & 15, rg = threadIdx.x >> 4;
     const int c0 = cb * kB + cg * 8;
     // row of the tile: half * 64 + rg * 4 + j
-    float v[8][8];
+    XVec<XB> x[8];
 #pragma unroll
     for (int r = 0; r < 8; r++) {
         const int row = rb * kB + (r >> 2) * 64 + rg * 4 + (r & 3);
-        const size_t at = (size_t)row * z.x.ld + c0;
-        if (row < z.M && VEC && c0 + 8 <= z.C) {
-            pv_load_vec<XB, 8>(z.x.p, at, v[r]);
-        } else {
+        const size_t from = min(row, z.M - 1);
+        if constexpr (NARROW) {  // rows of fewer channels than a vector
+            uint32_t e[8];
 #pragma unroll
-            for (int i = 0; i < 8; i++)
-                v[r][i] = row < z.M && c0 + i < z.C ? pv_load_one(z.x.p, XB, at + i) : 0.f;
+            for (int i = 0; i < 8; i++) {
+                const float f = pv_load_one(z.x.p, XB, from * z.x.ld + min(c0 + i, z.C - 1));
+                e[i] = c0 + i < z.C ? __float_as_uint(f) : 0u;
+            }
+            x[r].set(e);
+        } else {
+            x[r].load(z.x, from, c0, z.C);
         }
     }
-    if constexpr (WHAT & kSum) {
+    if (!NARROW && (cb + 1) * kB > z.C) {  // the row's last block
+#pragma unroll
+        for (int r = 0; r < 8; r++) x[r].move_down(max(c0 - (z.C - 8), 0));
+    }
+    if ((rb + 1) * kB > z.M) {  // rows past the last: zeros
+#pragma unroll
+        for (int r = 0; r < 8; r++)
+            if (rb * kB + (r >> 2) * 64 + rg * 4 + (r & 3) >= z.M) x[r].clear();
+    }
+    if ((WHAT & kSum) && z.sum) {
         float t[8];
 #pragma unroll
         for (int i = 0; i < 8; i++) {
             t[i] = 0.f;
 #pragma unroll
-            for (int r = 0; r < 8; r++) t[i] += v[r][i];
+            for (int r = 0; r < 8; r++) t[i] += x[r].get(i);
             t[i] += __shfl_xor(t[i], 16);
             t[i] += __shfl_xor(t[i], 32);
             if ((threadIdx.x & 48) == 0) sums[wave][cg * 8 + i] = t[i];
@@ -115,15 +238,9 @@ __global__ __launch_bounds__(kThreads) void pv_fp8_quantise_kernel(Quantise z) {
     if constexpr (WHAT & kRows) {
 #pragma unroll
         for (int r = 0; r < 8; r++) {
-            uint32_t top = 0;
-#pragma unroll
-            for (int i = 0; i < 8; i++) top = max(top, finite_bits(v[r][i]));
-            const int e = block_exponent(max_over_row16(top));
-            const float f = two_to(-e);
+            const int e = block_exponent(max_over_row16(x[r].finite_top()));
             const int row = rb * kB + (r >> 2) * 64 + rg * 4 + (r & 3);
-            uint2 w;
-            w.x = pack_scaled(v[r][0], v[r][1], v[r][2], v[r][3], f);
-            w.y = pack_scaled(v[r][4], v[r][5], v[r][6], v[r][7], f);
+            const uint2 w = x[r].bytes(two_to(e));
             if (row < z.M) {
                 *(uint2*)(z.q + ((size_t)cb * z.M + row) * kB + cg * 8) = w;
                 if (cg == 0) z.scale[(size_t)cb * z.M + row] = (uint8_t)(e + 127);
@@ -135,7 +252,7 @@ __global__ __launch_bounds__(kThreads) void pv_fp8_quantise_kernel(Quantise z) {
         for (int i = 0; i < 8; i++) {
             uint32_t top = 0;
 #pragma unroll
-            for (int r = 0; r < 8; r++) top = max(top, finite_bits(v[r][i]));
+            for (int r = 0; r < 8; r++) top = max(top, finite_bits(x[r].get(i)));
             top = max(top, (uint32_t)__shfl_xor((int)top, 16));
             top = max(top, (uint32_t)__shfl_xor((int)top, 32));
             if ((threadIdx.x & 48) == 0) tops[wave][cg * 8 + i] = top;
@@ -157,20 +274,19 @@ __global__ __launch_bounds__(kThreads) void pv_fp8_quantise_kernel(Quantise z) {
                               ? tile_e
                               : block_exponent(max(max(tops[0][c], tops[1][c]),
                                                    max(tops[2][c], tops[3][c])));
-            const float f = two_to(-e);
-            turn[c * kPitch + rg] = pack_scaled(v[0][i], v[1][i], v[2][i], v[3][i], f);
-            turn[c * kPitch + 16 + rg] = pack_scaled(v[4][i], v[5][i], v[6][i], v[7][i], f);
+            const float f = two_to(e);
+            turn[c * kPitch + rg] =
+                pack_scaled(x[0].get(i), x[1].get(i), x[2].get(i), x[3].get(i), f);
+            turn[c * kPitch + 16 + rg] =
+                pack_scaled(x[4].get(i), x[5].get(i), x[6].get(i), x[7].get(i), f);
             if (!(WHAT & kBlock) && rg == 0 && cb * kB + c < z.C)
                 z.scale_t[(size_t)rb * z.C + cb * kB + c] = (uint8_t)(e + 127);
         }
         if constexpr (WHAT & kBlock) {
-            const float f = two_to(-tile_e);
 #pragma unroll
             for (int r = 0; r < 8; r++) {
                 const int row = rb * kB + (r >> 2) * 64 + rg * 4 + (r & 3);
-                uint2 w;
-                w.x = pack_scaled(v[r][0], v[r][1], v[r][2], v[r][3], f);
-                w.y = pack_scaled(v[r][4], v[r][5], v[r][6], v[r][7], f);
+                const uint2 w = x[r].bytes(two_to(tile_e));
                 if (row < z.M) *(uint2*)(z.q + ((size_t)row * cbs + cb) * kB + cg * 8) = w;
             }
             if (threadIdx.x == 0) {
@@ -191,7 +307,7 @@ __global__ __launch_bounds__(kThreads) void pv_fp8_quantise_kernel(Quantise z) {
             }
         }
     }
-    if constexpr (WHAT & kSum) {
+    if ((WHAT & kSum) && z.sum) {
         __syncthreads();
         const int c = threadIdx.x;
         if (c < kB && cb * kB + c < z.C)
@@ -231,6 +347,11 @@ struct Product {
     float slope;
     PvRows out;
     float* partial;     // [splits][M][N] where splits > 1
+    // extra workgroups of the tiled product: dbias [bias_n] from the blocks' column
+    // sums [bias_blocks][bias_n]
+    const float* sum;
+    int bias_n, bias_blocks;
+    float* dbias;
 };
 constexpr int kTile = 128;
 
@@ -238,9 +359,6 @@ __device__ __forceinline__ int a_key(int row) { return row & 7; }
 __device__ __forceinline__ int b_key(int row) { return (row & 3) | ((row >> 2) & 4); }
 // of the fragments that take rows 8 (r >> 2) + 4 j + (r & 3)
 __device__ __forceinline__ int w_key(int row) { return (row & 3) | ((row >> 1) & 4); }
-
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 // Eight e4m3 bytes times 2^(byte - 127), as bf16.
 __device__ __forceinline__ bf16x8 to_bf16(uint32_t lo, uint32_t hi, uint32_t byte) {
@@ -308,8 +426,25 @@ __device__ __forceinline__ void store_run(const Product& p, int split, int m, in
     }
 }
 
+// dbias from the blocks' column sums, in a fixed order: 16 columns a workgroup,
+// 16 threads a column.
+constexpr int kBiasColumns = 16;
+__device__ __forceinline__ void sum_bias(const Product& p, int group, double* part) {
+    const int c = group * kBiasColumns + (threadIdx.x & 15);
+    double s = 0.;
+    if (c < p.bias_n)
+        for (int i = threadIdx.x >> 4; i < p.bias_blocks; i += 16)
+            s += (double)p.sum[(size_t)i * p.bias_n + c];
+    part[threadIdx.x] = s;
+    __syncthreads();
+    if (threadIdx.x < 16 && c < p.bias_n) {
+        for (int w = 1; w < 16; w++) s += part[threadIdx.x + 16 * w];
+        p.dbias[c] = (float)s;
+    }
+}
+
 template <bool EXACT>
-__global__ __launch_bounds__(kThreads, 2) void pv_fp8_tile_kernel(Product p, bool vec) {
+__global__ __launch_bounds__(kThreads, 2) void pv_fp8_tile_kernel(Product p, bool vec, int tiles) {
     // two stages, arrays of their own: the loads into one are then seen not to
     // touch what is read of the other, and are not waited for
     __shared__ __align__(16) uint8_t la0[kTile * kB], la1[kTile * kB];
@@ -318,6 +453,10 @@ __global__ __launch_bounds__(kThreads, 2) void pv_fp8_tile_kernel(Product p, boo
     // holds the bytes of the four fragments' row r
     __shared__ __align__(16) uint8_t ls0[2 * kTile], ls1[2 * kTile];
     const int mt = (p.M + kTile - 1) / kTile, nt = (p.N + kTile - 1) / kTile;
+    if ((int)blockIdx.x >= tiles) {
+        sum_bias(p, (int)blockIdx.x - tiles, (double*)la0);
+        return;
+    }
     // Workgroups go round the XCDs; each XCD takes a run of tiles, the columns
     // of a row of tiles next to one another, so that its L2 serves a's rows.
     const size_t total = (size_t)mt * nt * p.splits, run = (total + 7) / 8;
@@ -471,103 +610,6 @@ struct Fused {
     const uint8_t* w;   // [N][blocks * 128]
     const uint8_t* sw;  // [N / 128][blocks]
 };
-
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-template <bool XB>
-struct XVec {  // eight consecutive values of a row
-    typedef u32x4 at_any __attribute__((aligned(2)));
-    u32x4 w[XB ? 1 : 2];
-    __device__ __forceinline__ float get(int i) const {
-        if constexpr (XB)
-            return __uint_as_float(i & 1 ? w[0][i / 2] & 0xffff0000u : w[0][i / 2] << 16);
-        else
-            return __uint_as_float(w[i / 4][i % 4]);
-    }
-    // The vector at column c0, or the row's last eight columns where it reaches
-    // past them (K >= 8): no branch parts a block's loads.
-    __device__ __forceinline__ void load(const PvRows& x, size_t row, int c0, int K) {
-        const char* p = (const char*)x.p + (row * x.ld + min(c0, K - 8)) * (XB ? 2 : 4);
-        w[0] = *(const at_any*)p;
-        if constexpr (!XB) w[1] = *(const at_any*)(p + 16);
-    }
-    // Values loaded `by` columns early: moved into place, zeros after the row's end.
-    __device__ __forceinline__ void move_down(int by) {
-        float x[8];
-#pragma unroll
-        for (int i = 0; i < 8; i++) x[i] = get(i);
-#pragma unroll
-        for (int s = 4; s; s >>= 1) {
-#pragma unroll
-            for (int i = 0; i < 8; i++) x[i] = by & s ? (i + s < 8 ? x[i + s] : 0.f) : x[i];
-        }
-#pragma unroll
-        for (int i = 0; i < 8; i++) {
-            const uint32_t u = by >= 8 ? 0u : __float_as_uint(x[i]);
-            if constexpr (!XB)
-                w[i / 4][i % 4] = u;
-            else
-                w[0][i / 2] = i & 1 ? w[0][i / 2] | u : u >> 16;
-        }
-    }
-    // The largest magnitude's bits; at least infinity's where a value may not be
-    // finite.
-    __device__ __forceinline__ uint32_t top() const {
-        if constexpr (XB) {
-            typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
-            u16x2 m = {0, 0};
-#pragma unroll
-            for (int i = 0; i < 4; i++) {
-                const uint32_t u = w[0][i] & 0x7fff7fffu;
-                u16x2 v;
-                __builtin_memcpy(&v, &u, 4);
-                m = __builtin_elementwise_max(m, v);
-            }
-            return (uint32_t)(m[0] > m[1] ? m[0] : m[1]) << 16;
-        } else {
-            float m = 0.f;  // a NaN is passed over
-#pragma unroll
-            for (int i = 0; i < 8; i++) m = fmaxf(m, fabsf(get(i)));
-            return __float_as_uint(m);
-        }
-    }
-    __device__ __forceinline__ uint32_t finite_top() const {
-        uint32_t m = 0;
-#pragma unroll
-        for (int i = 0; i < 8; i++) m = max(m, finite_bits(get(i)));
-        return m;
-    }
-    // The eight as e4m3 of v / scale, a power of two: nearest, ties to even; what
-    // is not finite gives NaN.
-    __device__ __forceinline__ uint2 bytes(float scale) const {
-        typedef short i16x2 __attribute__((ext_vector_type(2)));
-        i16x2 q[2] = {{0, 0}, {0, 0}};
-#pragma unroll
-        for (int i = 0; i < 2; i++) {
-            if constexpr (XB) {
-                bf16x2 a, b;
-                const uint32_t u = w[0][2 * i], v = w[0][2 * i + 1];
-                __builtin_memcpy(&a, &u, 4);
-                __builtin_memcpy(&b, &v, 4);
-                q[i] = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(q[i], a, scale, false);
-                q[i] = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(q[i], b, scale, true);
-            } else {
-                q[i] = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(q[i], get(4 * i), get(4 * i + 1),
-                                                                scale, false);
-                q[i] = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(q[i], get(4 * i + 2),
-                                                                get(4 * i + 3), scale, true);
-            }
-        }
-        uint2 r;
-        __builtin_memcpy(&r, q, 8);
-        return r;
-    }
-};
-
-// max over 16 consecutive lanes
-template <int CTRL>
-__device__ __forceinline__ uint32_t max_dpp(uint32_t v) {
-    return max(v, dpp_u32<CTRL, 0xf>(v));
-}
 
 // A block's 64 rows of x, from registers (THREADS threads, 16 of them a row) into
 // LDS as bytes with their scales.
@@ -883,6 +925,92 @@ __global__ __launch_bounds__(kResidentThreads, 2) void pv_fp8_resident_kernel(Fu
     }
 }
 
+// Few rows: a workgroup takes 16 rows by 16 columns, its eight waves a share of
+// the blocks each, whose sums meet in LDS in wave order: one launch, and the
+// weight's bytes spread over as many workgroups as there are 16 columns. A wave
+// quantises its blocks of x in registers, where they are its matrix operand:
+// lane (r, h) holds row r's values 16 h .. and 64 + 16 h .. of the block.
+constexpr int kFewThreads = 512, kFewRows = 32;
+
+template <bool XB, bool EXACT>
+__global__ __launch_bounds__(kFewThreads) void pv_fp8_few_kernel(Fused f, Product p) {
+    constexpr int kWaves = kFewThreads / 64;
+    __shared__ float part[kWaves][256];
+    const int nt = (p.N + 15) / 16;
+    const int m0 = (int)(blockIdx.x / nt) * 16, n0 = (int)(blockIdx.x % nt) * 16;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r = lane & 15, h = lane >> 4;
+    const size_t row = min(m0 + r, f.M - 1);
+    const int n = min(n0 + r, p.N - 1);
+    const uint8_t* gw = f.w + (size_t)n * p.blocks * kB + h * 16;
+    const uint8_t* gs = f.sw + (size_t)(n / kB) * p.blocks;
+    struct Block {
+        XVec<XB> x[4];
+        Frag w;
+        int sw;
+    };
+    auto fetch = [&](Block& b, int k) {
+        k = min(k, p.blocks - 1);
+        b.w.u[0] = *(const u32x4*)(gw + (size_t)k * kB);
+        b.w.u[1] = *(const u32x4*)(gw + (size_t)k * kB + 64);
+        b.sw = gs[k];
+#pragma unroll
+        for (int v = 0; v < 4; v++)
+            b.x[v].load(f.x, row, k * kB + (v >> 1) * 64 + h * 16 + (v & 1) * 8, f.K);
+    };
+    pv_f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    auto multiply = [&](Block& b, int k) {
+        if ((k + 1) * kB > f.K) {
+#pragma unroll
+            for (int v = 0; v < 4; v++)
+                b.x[v].move_down(
+                    max(k * kB + (v >> 1) * 64 + h * 16 + (v & 1) * 8 - (f.K - 8), 0));
+        }
+        uint32_t top = 0;
+#pragma unroll
+        for (int v = 0; v < 4; v++) top = max(top, b.x[v].finite_top());
+        top = max(top, (uint32_t)__shfl_xor((int)top, 16));
+        top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+        const int byte = block_exponent(top) + 127;
+        Frag a;
+#pragma unroll
+        for (int v = 0; v < 4; v++) {
+            const uint2 q = b.x[v].bytes(__uint_as_float((uint32_t)byte << 23));
+            a.v[2 * v] = (int)q.x;
+            a.v[2 * v + 1] = (int)q.y;
+        }
+        if constexpr (!EXACT) {
+            acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b.w.v, a.v, acc, 0, 0, 0, b.sw,
+                                                                   0, byte);
+        } else {
+#pragma unroll
+            for (int q = 0; q < 4; q++)
+                acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                    to_bf16(b.w.v[2 * q], b.w.v[2 * q + 1], b.sw),
+                    to_bf16(a.v[2 * q], a.v[2 * q + 1], byte), acc, 0, 0, 0);
+        }
+    };
+    Block b0, b1;
+    fetch(b0, wave);
+    for (int k = wave; k < p.blocks; k += 2 * kWaves) {
+        fetch(b1, k + kWaves);
+        multiply(b0, k);
+        fetch(b0, k + 2 * kWaves);
+        if (k + kWaves < p.blocks) multiply(b1, k + kWaves);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; i++) part[wave][r * 16 + 4 * h + i] = acc[i];
+    __syncthreads();
+    const int m = m0 + (int)(threadIdx.x >> 4), c = n0 + (int)(threadIdx.x & 15);
+    if (threadIdx.x < 256 && m < f.M && c < p.N) {
+        float v = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWaves; w++) v += part[w][threadIdx.x];
+        if (p.bias) v += p.bias[c];
+        pv_store_one(p.out.p, p.out.bf16, (size_t)m * p.out.ld + c,
+                     pv_activate(v, p.act, p.slope));
+    }
+}
+
 // out = act( the splits' sums in order + bias )
 __global__ __launch_bounds__(kThreads) void pv_fp8_join_kernel(Product p) {
     const size_t total = (size_t)p.M * p.N;
@@ -897,21 +1025,10 @@ __global__ __launch_bounds__(kThreads) void pv_fp8_join_kernel(Product p) {
     }
 }
 
-// dbias from the blocks' column sums, in a fixed order: 16 columns a workgroup,
-// 16 threads a column
-__global__ __launch_bounds__(kThreads) void pv_fp8_bias_kernel(const float* sum, int blocks, int N,
-                                                               float* dbias) {
+// dbias alone
+__global__ __launch_bounds__(kThreads) void pv_fp8_bias_kernel(Product p) {
     __shared__ double part[kThreads];
-    const int c = blockIdx.x * 16 + (threadIdx.x & 15);
-    double s = 0.;
-    if (c < N)
-        for (int i = threadIdx.x >> 4; i < blocks; i += 16) s += (double)sum[(size_t)i * N + c];
-    part[threadIdx.x] = s;
-    __syncthreads();
-    if (threadIdx.x < 16 && c < N) {
-        for (int w = 1; w < 16; w++) s += part[threadIdx.x + 16 * w];
-        dbias[c] = (float)s;
-    }
+    sum_bias(p, blockIdx.x, part);
 }
 
 // the weight's gradient of no rows
@@ -946,19 +1063,20 @@ struct Carve {
 };
 // How many ways a product's blocks are split: one where its tiles fill the
 // chip, else enough for kWanted workgroups at most (two a CU: more would wait
-// for a second round), of two blocks or more.
-constexpr int kWanted = 512;
+// for a second round), of kLeast
+// blocks or more (joining costs a launch, a block some half a microsecond).
+constexpr int kWanted = 512, kLeast = 6;
 constexpr int kFusedN = 1024;
 void plan_splits(int M, int N, int bm, int bn, int blocks, int* per, int* splits) {
     const size_t tiles = (size_t)((M + bm - 1) / bm) * ((N + bn - 1) / bn);
     *per = blocks;
-    if (tiles > 0 && tiles < kWanted / 2 && blocks > 1) {
-        const int most = (blocks + 1) / 2;
+    if (tiles > 0 && tiles < kWanted / 2 && blocks >= 2 * kLeast) {
+        const int most = blocks / kLeast;
         int n = (int)(kWanted / tiles);
         n = n < 1 ? 1 : (n > most ? most : n);
         *per = (blocks + n - 1) / n;
     }
-    *splits = blocks > 1 ? (blocks + *per - 1) / *per : 1;
+    *splits = *per ? (blocks + *per - 1) / *per : 1;
 }
 size_t partial_bytes(int M, int N, int bm, int bn, int blocks) {
     int per, splits;
@@ -966,12 +1084,13 @@ size_t partial_bytes(int M, int N, int bm, int bn, int blocks) {
     return splits > 1 ? (size_t)splits * M * N * 4 : 0;
 }
 
-// How a product of rows by a weight runs: rows that stay in LDS, rows quantised
-// on the way in, or the quantiser and the product apart (also rows of fewer
-// channels than a vector).
-enum Path { kResident, kFused, kApart };
-Path path_of(int K, int N) {
+// How a product of rows by a weight runs: few rows, rows that stay in LDS, rows
+// quantised on the way in, or the quantiser and the product apart (also rows of
+// fewer channels than a vector).
+enum Path { kFew, kResident, kFused, kApart };
+Path path_of(int M, int K, int N) {
     if (K < 8) return kApart;
+    if (M <= kFewRows) return kFew;
     if (N > kFusedTileN && pv_fp8_blocks(K) <= kResidentBlocks) return kResident;
     return N <= kFusedN ? kFused : kApart;
 }
@@ -981,10 +1100,10 @@ struct RowsWs {  // of a product of rows by a weight
     float* partial;
 };
 RowsWs carve_rows(Carve& c, int M, int K, int N) {
-    const Path path = path_of(K, N);
+    const Path path = path_of(M, K, N);
     RowsWs w{{nullptr, nullptr}, nullptr};
     if (path == kApart) w.x = c.rows(M, K);
-    if (path != kResident)
+    if (path == kFused || path == kApart)
         w.partial = (float*)c.take(
             path == kFused ? partial_bytes(M, N, kFusedM, kFusedTileN, pv_fp8_blocks(K))
                            : partial_bytes(M, N, kTile, kTile, pv_fp8_blocks(K)));
@@ -1018,12 +1137,19 @@ void with_bool(bool b, F f) {
 }
 
 template <int WHAT>
-void launch_quantise(const Quantise& z, hipStream_t s) {
-    const size_t tiles = (size_t)pv_fp8_blocks(z.M) * pv_fp8_blocks(z.C);
-    with_bool(z.x.bf16, [&](auto XB) {
-        with_bool(pv_vec_width(8, z.x.bf16 ? 2 : 4, z.x.p, 8, z.x.ld) == 8, [&](auto VEC) {
-            pv_fp8_quantise_kernel<decltype(XB)::value, decltype(VEC)::value, WHAT>
-                <<<(unsigned)tiles, kThreads, 0, s>>>(z);
+void launch_quantise(const Quantise& a, hipStream_t s, const Quantise* b = nullptr) {
+    auto tiles = [](const Quantise& z) { return pv_fp8_blocks(z.M) * pv_fp8_blocks(z.C); };
+    if (b && (a.x.bf16 != b->x.bf16 || (a.C < 8) != (b->C < 8))) {
+        launch_quantise<WHAT>(a, s);
+        launch_quantise<WHAT>(*b, s);
+        return;
+    }
+    const QuantiseJobs jobs{a, b ? *b : a, tiles(a)};
+    const unsigned grid = (unsigned)(tiles(a) + (b ? tiles(*b) : 0));
+    with_bool(a.x.bf16, [&](auto XB) {
+        with_bool(a.C < 8, [&](auto NARROW) {
+            pv_fp8_quantise_kernel<decltype(XB)::value, decltype(NARROW)::value, WHAT>
+                <<<grid, kThreads, 0, s>>>(jobs);
         });
     });
 }
@@ -1038,10 +1164,11 @@ void launch_product(Product p, hipStream_t s) {
     const size_t total = (size_t)((p.M + kTile - 1) / kTile) * ((p.N + kTile - 1) / kTile) * p.splits;
     const unsigned grid = (unsigned)((total + 7) / 8 * 8);
     const bool vec = vector_rows(p);
+    const unsigned more = p.dbias ? (unsigned)((p.bias_n + kBiasColumns - 1) / kBiasColumns) : 0;
     if (p.out.bf16)
-        pv_fp8_tile_kernel<false><<<grid, kThreads, 0, s>>>(p, vec);
+        pv_fp8_tile_kernel<false><<<grid + more, kThreads, 0, s>>>(p, vec, (int)grid);
     else
-        pv_fp8_tile_kernel<true><<<grid, kThreads, 0, s>>>(p, vec);
+        pv_fp8_tile_kernel<true><<<grid + more, kThreads, 0, s>>>(p, vec, (int)grid);
     if (p.splits > 1)
         pv_fp8_join_kernel<<<grid_of(((size_t)p.M * p.N + kThreads - 1) / kThreads), kThreads, 0,
                              s>>>(p);
@@ -1063,6 +1190,17 @@ void launch_fused(const PvRows& x, Product p, hipStream_t s) {
     if (p.splits > 1)
         pv_fp8_join_kernel<<<grid_of(((size_t)p.M * p.N + kThreads - 1) / kThreads), kThreads, 0,
                              s>>>(p);
+}
+
+void launch_few(const PvRows& x, const Product& p, hipStream_t s) {
+    const Fused f{x, p.M, p.K, p.b, p.sb};
+    const unsigned grid = (unsigned)(((p.M + 15) / 16) * ((p.N + 15) / 16));
+    with_bool(x.bf16, [&](auto XB) {
+        with_bool(!p.out.bf16, [&](auto EXACT) {
+            pv_fp8_few_kernel<decltype(XB)::value, decltype(EXACT)::value>
+                <<<grid, kFewThreads, 0, s>>>(f, p);
+        });
+    });
 }
 
 void launch_resident(const PvRows& x, const Product& p, hipStream_t s) {
@@ -1116,7 +1254,8 @@ void launch_rows_product(const PvRows& x, int M, int K, int N, const uint8_t* we
     p.act = act;
     p.slope = slope;
     p.splits = 1;
-    switch (path_of(K, N)) {
+    switch (path_of(M, K, N)) {
+        case kFew: launch_few(x, p, s); break;
         case kResident: launch_resident(x, p, s); break;
         case kFused: launch_fused(x, p, s); break;
         case kApart:
@@ -1161,17 +1300,13 @@ pvconv_status pv_launch_fp8_linear_bwd(const PvRows& dy, const PvRows& x, int M,
     if (dx.p && M)
         launch_rows_product(dy, M, N, K, weight_t, scale_t, nullptr, PVCONV_ACT_NONE, 0.f, dx, w.dx,
                             s);
-    if (M) {
-        const Quantise z{dy, M, N, nullptr, nullptr, w.dyt.q, w.dyt.scale, w.sum};
-        if (dw && dbias)
-            launch_quantise<kCols | kSum>(z, s);
-        else if (dw)
-            launch_quantise<kCols>(z, s);
-        else if (dbias)
-            launch_quantise<kSum>(z, s);
-    }
+    const Quantise zy{dy, M, N, nullptr, nullptr, w.dyt.q, w.dyt.scale, dbias ? w.sum : nullptr};
+    const Quantise zx{x, M, K, nullptr, nullptr, w.xt.q, w.xt.scale, nullptr};
+    if (dw && M)
+        launch_quantise<kCols | kSum>(zy, s, &zx);
+    else if (dbias && M)
+        launch_quantise<kSum>(zy, s);
     if (dw && M) {
-        launch_quantise<kCols>(Quantise{x, M, K, nullptr, nullptr, w.xt.q, w.xt.scale, nullptr}, s);
         Product p{};
         p.a = w.dyt.q;
         p.sa = w.dyt.scale;
@@ -1188,12 +1323,22 @@ pvconv_status pv_launch_fp8_linear_bwd(const PvRows& dy, const PvRows& x, int M,
         p.act = PVCONV_ACT_NONE;
         p.out = PvRows{dw, false, K};
         p.partial = w.partial;
+        p.sum = w.sum;
+        p.bias_n = N;
+        p.bias_blocks = mb;
+        p.dbias = dbias;
         launch_product(p, s);
     } else if (dw) {
         pv_fp8_zero_kernel<<<grid_of(((size_t)N * K + kThreads - 1) / kThreads), kThreads, 0, s>>>(
             dw, (size_t)N * K);
     }
-    if (dbias)
-        pv_fp8_bias_kernel<<<(N + 15) / 16, kThreads, 0, s>>>(w.sum, mb, N, dbias);
+    if (dbias && !(dw && M)) {
+        Product p{};
+        p.sum = w.sum;
+        p.bias_n = N;
+        p.bias_blocks = mb;
+        p.dbias = dbias;
+        pv_fp8_bias_kernel<<<(N + kBiasColumns - 1) / kBiasColumns, kThreads, 0, s>>>(p);
+    }
     return pv_launch_status();
 }
