@@ -133,7 +133,7 @@ pvconv_status pvconv_fp8_linear_backward(const void* dy, pvconv_dtype dy_dt, int
 /* present values -inf), the second for a label outside [0, V) or labels     */
 /* NULL; both 0, and no gradient, for a row whose logits are all -inf. An    */
 /* entry with p_j = 0 adds nothing; entries of one class add up. A NaN or    */
-/* +inf logit makes its row NaN.                                             */
+/* +inf logit makes the terms of its row NaN.                                */
 /*  z        [M][V] (z_dt), row stride z_ld                                  */
 /*  t_val    [M][top] fp32, t_class [M][top] int32, contiguous               */
 /*  labels   [M] int32 or NULL;  temperature > 0;  0 <= alpha <= 1           */

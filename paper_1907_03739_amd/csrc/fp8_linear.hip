@@ -929,8 +929,10 @@ __global__ __launch_bounds__(kResidentThreads, 2) void pv_fp8_resident_kernel(Fu
 // the blocks each, whose sums meet in LDS in wave order: one launch, and the
 // weight's bytes spread over as many workgroups as there are 16 columns. A wave
 // quantises its blocks of x in registers, where they are its matrix operand:
-// lane (r, h) holds row r's values 16 h .. and 64 + 16 h .. of the block.
-constexpr int kFewThreads = 512, kFewRows = 32;
+// lane (r, h) holds row r's values 16 h .. and 64 + 16 h .. of the block. It ends
+// after the latency of a wave's few blocks: 2.6 to 4.2 us for one row of 128 to
+// 2048 channels, 7.7 of 4928.
+constexpr int kFewThreads = 512;
 
 template <bool XB, bool EXACT>
 __global__ __launch_bounds__(kFewThreads) void pv_fp8_few_kernel(Fused f, Product p) {
@@ -1086,11 +1088,15 @@ size_t partial_bytes(int M, int N, int bm, int bn, int blocks) {
 
 // How a product of rows by a weight runs: few rows, rows that stay in LDS, rows
 // quantised on the way in, or the quantiser and the product apart (also rows of
-// fewer channels than a vector).
+// fewer channels than a vector). Few: as long as each of its workgroups has a CU
+// to itself (bf16, few / else, us: 256 x 2048 -> 256, 256 workgroups, 6.0 / 13.9;
+// 512 rows 10.0 / 14.1; 512 x 4928 -> 256 20.3 / 15.5; 128 x 512 -> 2048, 1024
+// workgroups, 10.1 / 6.6).
+constexpr int kFewTiles = 256;
 enum Path { kFew, kResident, kFused, kApart };
 Path path_of(int M, int K, int N) {
     if (K < 8) return kApart;
-    if (M <= kFewRows) return kFew;
+    if ((size_t)((M + 15) / 16) * ((N + 15) / 16) <= kFewTiles) return kFew;
     if (N > kFusedTileN && pv_fp8_blocks(K) <= kResidentBlocks) return kResident;
     return N <= kFusedN ? kFused : kApart;
 }

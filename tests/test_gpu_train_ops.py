@@ -276,6 +276,13 @@ PRODUCT = [
     (4099, 384, 256, "bf16", "bf16", "relu", True, 0, 0),
     (300, 4928, 256, "bf16", "f32", "none", True, 0, 0),
     (40000, 64, 13, "f32", "f32", "none", True, 0, 0),
+    (2500, 1024, 700, "bf16", "bf16", "relu", True, 0, 0),   # rows of 8 blocks that stay in LDS
+    (700, 1000, 2500, "f32", "bf16", "none", True, 3, 0),    # more columns than one share
+    (3000, 512, 2304, "bf16", "bf16", "leaky", False, 0, 8),
+    (600, 1100, 1030, "bf16", "bf16", "none", True, 0, 0),   # quantiser and product apart
+    (5000, 7, 300, "f32", "f32", "relu", True, 2, 0),        # fewer channels than a vector
+    (40, 4, 9, "bf16", "bf16", "none", True, 0, 0),
+    (600, 2900, 100, "bf16", "bf16", "none", True, 1, 1),    # odd strides, a ragged last block
 ]
 
 
