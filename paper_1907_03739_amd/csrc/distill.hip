@@ -419,9 +419,13 @@ __global__ __launch_bounds__(T) void pv_distill_long_kernel(Args a) {
 }
 
 // ---------------------------------------------------------------------------
-// From kLongV classes on a workgroup owns a row: 1024 threads where rows are too
-// few to fill the chip with 256.
-constexpr int kLongV = 1025, kFewRows = 512, kWideV = 8192;
+// Rows of up to 2048 classes stay in registers, with as many lanes as leave each
+// 4 to 32 logits (the loss over 80 MB of fp32 logits, 16 lanes / the rule: 13
+// classes 204 / 72 us, 50 classes 57 / 38; 1500 classes 74 / 27 against a workgroup
+// a row). From kLongV on a workgroup owns a row: 256 threads (2500 classes, loss
+// and gradient: 76 us with 512, 43), 512 from kMidV on (49999: loss 133 us, 124),
+// 1024 where rows are too few to fill the chip.
+constexpr int kLongV = 2049, kFewRows = 512, kWideV = 8192, kMidV = 32768;
 
 template <typename F>
 void with_bool(bool b, F f) {
@@ -430,6 +434,9 @@ void with_bool(bool b, F f) {
     else
         f(std::false_type());
 }
+
+template <int N>
+using Int = std::integral_constant<int, N>;
 
 template <bool STATS, bool GRAD>
 pvconv_status launch(const Args& a, hipStream_t s) {
@@ -440,17 +447,31 @@ pvconv_status launch(const Args& a, hipStream_t s) {
         if (a.d.V >= kLongV) {
             if (M <= kFewRows && a.d.V >= kWideV)
                 pv_distill_long_kernel<1024, BF16, STATS, GRAD><<<grid(M), 1024, 0, s>>>(a);
+            else if (a.d.V < kMidV && a.d.top < 256)  // (a thread an entry and one for the label)
+                pv_distill_long_kernel<256, BF16, STATS, GRAD><<<grid(M), 256, 0, s>>>(a);
             else
                 pv_distill_long_kernel<512, BF16, STATS, GRAD><<<grid(M), 512, 0, s>>>(a);
-        } else if (a.d.V <= 64) {
-            pv_distill_short_kernel<16, 4, BF16, STATS, GRAD>
-                <<<grid((M + 15) / 16), kThreads, 0, s>>>(a);
-        } else if (a.d.V <= 256) {
-            pv_distill_short_kernel<16, 16, BF16, STATS, GRAD>
-                <<<grid((M + 15) / 16), kThreads, 0, s>>>(a);
         } else {
-            pv_distill_short_kernel<64, 16, BF16, STATS, GRAD>
-                <<<grid((M + 3) / 4), kThreads, 0, s>>>(a);
+            auto rows = [&](auto T, auto E) {
+                constexpr int TEAM = decltype(T)::value;
+                pv_distill_short_kernel<TEAM, decltype(E)::value, BF16, STATS, GRAD>
+                    <<<grid((M + kThreads / TEAM - 1) / (kThreads / TEAM)), kThreads, 0, s>>>(a);
+            };
+            const int V = a.d.V;
+            if (V <= 16)
+                rows(Int<4>(), Int<4>());
+            else if (V <= 64)
+                rows(Int<8>(), Int<8>());
+            else if (V <= 128)
+                rows(Int<16>(), Int<8>());
+            else if (V <= 256)
+                rows(Int<16>(), Int<16>());
+            else if (V <= 512)
+                rows(Int<64>(), Int<8>());
+            else if (V <= 1024)
+                rows(Int<64>(), Int<16>());
+            else
+                rows(Int<64>(), Int<32>());
         }
     });
     return pv_launch_status();

@@ -387,6 +387,15 @@ DISTILL = [
     (5, 4097, 256, "bf16", 2.0, 0.5, True, 1, 0),
     (3, 32001, 32, "bf16", 1.0, 1.0, False, 0, 0),
     (2, 70001, 64, "f32", 1.5, 0.5, True, 0, 0),
+    (37, 16, 16, "f32", 2.0, 0.5, True, 0, 0),       # the widths between two kinds of team
+    (37, 17, 9, "bf16", 2.0, 0.5, True, 1, 0),
+    (33, 128, 70, "f32", 1.0, 0.5, True, 0, 3),
+    (33, 129, 5, "f32", 2.0, 0.5, True, 0, 0),
+    (9, 512, 200, "bf16", 2.0, 0.5, True, 0, 0),
+    (9, 513, 7, "f32", 2.0, 0.5, True, 3, 0),
+    (5, 2048, 64, "f32", 2.0, 0.5, True, 0, 0),
+    (5, 2049, 255, "bf16", 2.0, 0.5, True, 5, 1),
+    (6, 3000, 256, "f32", 2.0, 0.5, True, 0, 0),     # an entry a thread, and one for the label
     (300, 9001, 16, "bf16", 1.5, 0.5, True, 0, 1),
 ]
 
