@@ -357,8 +357,11 @@ constexpr int kTile = 128;
 
 __device__ __forceinline__ int a_key(int row) { return row & 7; }
 __device__ __forceinline__ int b_key(int row) { return (row & 3) | ((row >> 2) & 4); }
-// of the fragments that take rows 8 (r >> 2) + 4 j + (r & 3)
-__device__ __forceinline__ int w_key(int row) { return (row & 3) | ((row >> 1) & 4); }
+// of J fragments that take rows 4 J (r >> 2) + 4 j + (r & 3)
+template <int J>
+__device__ __forceinline__ int w_key(int row) {
+    return (row & 3) | ((row >> (J == 2 ? 1 : 2)) & 4);
+}
 
 // Eight e4m3 bytes times 2^(byte - 127), as bf16.
 __device__ __forceinline__ bf16x8 to_bf16(uint32_t lo, uint32_t hi, uint32_t byte) {
@@ -595,7 +598,9 @@ __global__ __launch_bounds__(kThreads, 2) void pv_fp8_tile_kernel(Product p, boo
 // The product of rows that are quantised on the way in: x is read once from
 // memory as it is, and no quantised copy of it exists.
 //
-// Eight waves side by side, 64 rows by 32 columns each (those beyond the last
+// Eight waves side by side, 64 rows by 32 columns each, or two by four of 64 by 64
+// (MW = 2, where such tiles fill the chip: the same LDS reads feed twice the
+// products) (those beyond the last
 // column quantise, and multiply nothing): two a SIMD, one's quantising beside
 // the other's products. A block's slices of x and of the weight come into
 // registers two blocks ahead. 16 lanes hold a row's 128 values, take their
@@ -611,12 +616,11 @@ struct Fused {
     const uint8_t* sw;  // [N / 128][blocks]
 };
 
-// A block's 64 rows of x, from registers (THREADS threads, 16 of them a row) into
-// LDS as bytes with their scales.
-template <int THREADS, bool XB>
-__device__ __forceinline__ void quantise_slice(const XVec<XB> (&from)[1024 / THREADS], int k, int K,
+// A block's rows of x, from registers (THREADS threads, 16 of them a row, V rows a
+// thread) into LDS as bytes with their scales.
+template <int THREADS, int V, bool XB>
+__device__ __forceinline__ void quantise_slice(const XVec<XB> (&from)[V], int k, int K,
                                                uint8_t* to, uint8_t* scales) {
-    constexpr int V = 1024 / THREADS;
     const int xr = threadIdx.x >> 4, xc = (threadIdx.x & 15) * 8;
     XVec<XB> x[V];
     uint32_t top[V], all = 0;
@@ -650,8 +654,8 @@ __device__ __forceinline__ void quantise_slice(const XVec<XB> (&from)[1024 / THR
         const int row = xr + (THREADS / 16) * v;
         *(uint2*)(to + row * kB + ((xc >> 4) ^ a_key(row)) * 16 + (xc & 8)) =
             x[v].bytes(__uint_as_float((uint32_t)byte << 23));
-        // row = 16 i + r: byte i of dword r
-        if (xc == 0) scales[(row & 15) * 4 + (row >> 4)] = (uint8_t)byte;
+        // row = 64 w + 16 i + r: byte i of dword r of the 64
+        if (xc == 0) scales[(row & ~63) + (row & 15) * 4 + ((row >> 4) & 3)] = (uint8_t)byte;
     }
 }
 
@@ -670,8 +674,8 @@ __device__ __forceinline__ void multiply_slices(pv_f32x4 (&acc)[J][4], const uin
 #pragma unroll
     for (int j = 0; j < J; j++) {
         const int row = wn + 4 * J * (r >> 2) + 4 * j + (r & 3);
-        fw[j].u[0] = *(const u32x4*)(lw + row * kB + (h ^ w_key(row)) * 16);
-        fw[j].u[1] = *(const u32x4*)(lw + row * kB + ((h + 4) ^ w_key(row)) * 16);
+        fw[j].u[0] = *(const u32x4*)(lw + row * kB + (h ^ w_key<J>(row)) * 16);
+        fw[j].u[1] = *(const u32x4*)(lw + row * kB + ((h + 4) ^ w_key<J>(row)) * 16);
     }
 #pragma unroll
     for (int i = 0; i < 4; i++) {
@@ -708,13 +712,13 @@ __device__ __forceinline__ void multiply_slices(pv_f32x4 (&acc)[J][4], const uin
 
 constexpr int kFusedM = 64, kFusedTileN = 256, kFusedThreads = 512, kFusedWaves = 2;
 
-template <bool XB, bool EXACT>
+template <int MW, bool XB, bool EXACT>
 __global__ __launch_bounds__(kFusedThreads, kFusedWaves) void pv_fp8_fused_kernel(Fused f,
                                                                                  Product p,
                                                                                  bool vec) {
-    constexpr int BM = kFusedM, BN = kFusedTileN;
+    constexpr int BM = kFusedM * MW, BN = kFusedTileN;
     // vectors of x a thread; fragments of the weight a wave; its loads a wave
-    constexpr int V = BM * 16 / kFusedThreads, J = 2, W = BN * kB / 16 / kFusedThreads;
+    constexpr int V = BM * 16 / kFusedThreads, J = 2 * MW, W = BN * kB / 16 / kFusedThreads;
     __shared__ __align__(16) uint8_t lw[2][BN * kB];
     __shared__ __align__(16) uint8_t la[2][BM * kB];
     __shared__ __align__(16) uint8_t ls[2][BM];
@@ -730,7 +734,8 @@ __global__ __launch_bounds__(kFusedThreads, kFusedWaves) void pv_fp8_fused_kerne
     const int k0 = split * p.per, k1 = min(k0 + p.per, p.blocks);
 
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r = lane & 15, h = lane >> 4;
-    const int wn = wave * 32;  // the wave's columns of the tile
+    // the wave's rows and columns of the tile
+    const int wm = wave % MW * 64, wn = wave / MW * (32 * MW);
     const bool multiplies = n0 + wn < p.N;
     const int xr = threadIdx.x >> 4, xc = (threadIdx.x & 15) * 8;  // row (+ 32 v), column
     for (int i = threadIdx.x; i < BN / kB * (k1 - k0); i += kFusedThreads) {
@@ -744,7 +749,7 @@ __global__ __launch_bounds__(kFusedThreads, kFusedWaves) void pv_fp8_fused_kerne
             to[v].load(f.x, (size_t)min(m0 + xr + (kFusedThreads / 16) * v, f.M - 1), k * kB + xc, f.K);
     };
     auto quantise = [&](const XVec<XB>(&from)[V], int k, uint8_t* to, uint8_t* scales) {
-        quantise_slice<kFusedThreads>(from, k, f.K, to, scales);
+        quantise_slice<kFusedThreads, V>(from, k, f.K, to, scales);
     };
     // this thread's pieces of the weight's slice: eight threads a row
     const int wr = threadIdx.x >> 3, wc = threadIdx.x & 7;
@@ -761,7 +766,7 @@ __global__ __launch_bounds__(kFusedThreads, kFusedWaves) void pv_fp8_fused_kerne
 #pragma unroll
         for (int q = 0; q < W; q++) {
             const int row = wr + kFusedThreads / 8 * q;
-            *(u32x4*)(to + row * kB + (wc ^ w_key(row)) * 16) = from[q];
+            *(u32x4*)(to + row * kB + (wc ^ w_key<J>(row)) * 16) = from[q];
         }
     };
     pv_f32x4 acc[J][4];  // [fragment of the weight][fragment of x]
@@ -777,7 +782,8 @@ __global__ __launch_bounds__(kFusedThreads, kFusedWaves) void pv_fp8_fused_kerne
         fetch_w(w_free, min(k + 2, k1 - 1));
         fetch_x(x_free, min(k + 2, k1 - 1));
         if (multiplies && k < k1)
-            multiply_slices<J, EXACT>(acc, lw[st], wn, la[st], ls[st], lsw[wn / kB][k - k0]);
+            multiply_slices<J, EXACT>(acc, lw[st], wn, la[st] + wm * kB, ls[st] + wm,
+                                      lsw[wn / kB][k - k0]);
     };
     fetch_w(ws[0], k0);
     fetch_x(xs[0], k0);
@@ -796,16 +802,16 @@ __global__ __launch_bounds__(kFusedThreads, kFusedWaves) void pv_fp8_fused_kerne
         quantise(xs[0], k + 2, la[0], ls[0]);
     }
     float bias[4 * J];
-    load_bias<4 * J>(p, n0 + wn + 8 * h, bias);
+    load_bias<4 * J>(p, n0 + wn + 4 * J * h, bias);
 #pragma unroll
     for (int i = 0; i < 4; i++) {
-        const int m = m0 + 16 * i + r;
+        const int m = m0 + wm + 16 * i + r;
         float v[4 * J];
 #pragma unroll
         for (int j = 0; j < J; j++)
 #pragma unroll
             for (int e = 0; e < 4; e++) v[4 * j + e] = acc[j][i][e] + bias[4 * j + e];
-        if (m < f.M && multiplies) store_run<8>(p, split, m, n0 + wn + 8 * h, v, vec);
+        if (m < f.M && multiplies) store_run<4 * J>(p, split, m, n0 + wn + 4 * J * h, v, vec);
     }
 }
 
@@ -860,7 +866,7 @@ __global__ __launch_bounds__(kResidentThreads, 2) void pv_fp8_resident_kernel(Fu
 #pragma unroll
         for (int q = 0; q < W; q++) {
             const int row = wr + T / 8 * q;
-            *(u32x4*)(to + row * kB + (wc ^ w_key(row)) * 16) = from[q];
+            *(u32x4*)(to + row * kB + (wc ^ w_key<J>(row)) * 16) = from[q];
         }
     };
     fetch_w(ws[0]);
@@ -878,10 +884,10 @@ __global__ __launch_bounds__(kResidentThreads, 2) void pv_fp8_resident_kernel(Fu
     fetch_x(xs[0], 0);
     fetch_x(xs[1], 1);
     for (int k = 0; k < p.blocks; k += 2) {
-        quantise_slice<T>(xs[0], k, f.K, la + (size_t)k * BM * kB, ls[k]);
+        quantise_slice<T, V>(xs[0], k, f.K, la + (size_t)k * BM * kB, ls[k]);
         fetch_x(xs[0], k + 2);
         if (k + 1 < p.blocks)
-            quantise_slice<T>(xs[1], k + 1, f.K, la + (size_t)(k + 1) * BM * kB, ls[k + 1]);
+            quantise_slice<T, V>(xs[1], k + 1, f.K, la + (size_t)(k + 1) * BM * kB, ls[k + 1]);
         fetch_x(xs[1], k + 3);
     }
     pv_f32x4 acc[J][4];
@@ -1180,17 +1186,32 @@ void launch_product(Product p, hipStream_t s) {
                              s>>>(p);
 }
 
+// 128 rows a workgroup where those fill the chip (and bf16 x: the slices of fp32
+// need the registers of 64).
+bool fused_wide(const PvRows& x, int M, int N) {
+    return x.bf16 && (size_t)(M / (2 * kFusedM)) * ((N + kFusedTileN - 1) / kFusedTileN) >=
+                         kWanted / 2;
+}
+
 void launch_fused(const PvRows& x, Product p, hipStream_t s) {
+    const bool wide = fused_wide(x, p.M, p.N);
+    const int bm = wide ? 2 * kFusedM : kFusedM;
     plan_splits(p.M, p.N, kFusedM, kFusedTileN, p.blocks, &p.per, &p.splits);
-    const size_t total = (size_t)((p.M + kFusedM - 1) / kFusedM) *
-                         ((p.N + kFusedTileN - 1) / kFusedTileN) * p.splits;
+    const size_t total =
+        (size_t)((p.M + bm - 1) / bm) * ((p.N + kFusedTileN - 1) / kFusedTileN) * p.splits;
     const unsigned grid = (unsigned)((total + 7) / 8 * 8);
     const bool vec = vector_rows(p);
     const Fused f{x, p.M, p.K, p.b, p.sb};
     with_bool(x.bf16, [&](auto XB) {
         with_bool(!p.out.bf16, [&](auto EXACT) {
-            pv_fp8_fused_kernel<decltype(XB)::value, decltype(EXACT)::value>
-                <<<grid, kFusedThreads, 0, s>>>(f, p, vec);
+            constexpr bool kXB = decltype(XB)::value, kExact = decltype(EXACT)::value;
+            if constexpr (kXB) {
+                if (wide) {
+                    pv_fp8_fused_kernel<2, kXB, kExact><<<grid, kFusedThreads, 0, s>>>(f, p, vec);
+                    return;
+                }
+            }
+            pv_fp8_fused_kernel<1, kXB, kExact><<<grid, kFusedThreads, 0, s>>>(f, p, vec);
         });
     });
     if (p.splits > 1)

@@ -283,6 +283,9 @@ PRODUCT = [
     (5000, 7, 300, "f32", "f32", "relu", True, 2, 0),        # fewer channels than a vector
     (40, 4, 9, "bf16", "bf16", "none", True, 0, 0),
     (600, 2900, 100, "bf16", "bf16", "none", True, 1, 1),    # odd strides, a ragged last block
+    (33001, 200, 70, "bf16", "bf16", "relu", True, 0, 0),    # tiles of 128 rows
+    (33001, 141, 200, "bf16", "f32", "none", True, 3, 1),
+    (8300, 1100, 1000, "bf16", "bf16", "leaky", False, 0, 0),
 ]
 
 
