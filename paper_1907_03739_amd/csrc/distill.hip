@@ -69,6 +69,8 @@ constexpr int kThreads = 256;
 
 template <int TEAM, int E, bool BF16, bool STATS, bool GRAD>
 __global__ __launch_bounds__(kThreads) void pv_distill_short_kernel(Args a) {
+    // (of gradients: the last entry that signed a class)
+    __shared__ uint16_t owner[GRAD ? kThreads / TEAM : 1][GRAD ? TEAM * E : 1];
     const PvDistill& d = a.d;
     const int lane = threadIdx.x % TEAM;
     const size_t step = (size_t)gridDim.x * (kThreads / TEAM);
@@ -143,25 +145,50 @@ __global__ __launch_bounds__(kThreads) void pv_distill_short_kernel(Args a) {
         // classes, stored after the lines above (same wave, same address order)
         float kl = 0.f;
         const int entries = w.kl != 0.f ? d.top : 0;
+        volatile uint16_t* own = owner[threadIdx.x / TEAM];
+        bool repeated = false;
+        if (GRAD && entries) {
+            // Each entry signs its class; one that finds another's name there shares
+            // its class. Only then is every entry compared with every other.
+            for (int j = lane; j < entries; j += TEAM) {
+                const int c = d.t_class[row * d.top + j];
+                if (!bad_class(c, d.V)) own[c] = (uint16_t)j;
+            }
+            __builtin_amdgcn_wave_barrier();
+            for (int j = lane; j < entries; j += TEAM) {
+                const int c = d.t_class[row * d.top + j];
+                if (!bad_class(c, d.V)) repeated |= own[c] != (uint16_t)j;
+            }
+            constexpr uint64_t kMask = TEAM == 64 ? ~0ull : (1ull << (TEAM & 63)) - 1;
+            repeated = (__ballot(repeated) >> ((threadIdx.x & 63) / TEAM * TEAM) & kMask) != 0;
+        }
         for (int j0 = 0; j0 <= entries; j0 += TEAM) {
             const int j = j0 + lane;
             const int c = j < entries ? d.t_class[row * d.top + j]
                                       : (j == entries && w.ce != 0.f ? w.label : -1);
             const bool have = !bad_class(c, d.V);
             const float zc = have ? pv_load_one(d.z.p, BF16, row * d.z.ld + c) : 0.f;
-            if (STATS && have && j < entries && !empty) {
-                const float u = d.t_val[row * d.top + j] * a.tau - tmax, p = __expf(u) * tinv;
-                if (!(p == 0.f)) kl += p * (u - log_of(tsum) - fmaf(zc, a.tau, -lset));
-            }
+            const float u = have && j < entries ? d.t_val[row * d.top + j] * a.tau - tmax : 0.f;
+            float p = have && j < entries ? __expf(u) * tinv : 0.f;
+            if (STATS && have && j < entries && !empty && !(p == 0.f))
+                kl += p * (u - log_of(tsum) - fmaf(zc, a.tau, -lset));
             if (GRAD && have && !zero && live) {
-                float p = 0.f;
-                for (int i = 0; i < entries; i++)
-                    if (d.t_class[row * d.top + i] == c)
-                        p += __expf(d.t_val[row * d.top + i] * a.tau - tmax);
+                bool mine = true;
+                if (repeated) {
+                    p = 0.f;
+                    for (int i = 0; i < entries; i++)
+                        if (d.t_class[row * d.top + i] == c)
+                            p += __expf(d.t_val[row * d.top + i] * a.tau - tmax);
+                    p *= tinv;
+                } else if (j == entries && entries) {
+                    // the label's class, unless an entry of that class writes it
+                    const int o = own[c];
+                    mine = !(o < entries && d.t_class[row * d.top + o] == c);
+                }
                 float g = soft_grad(zc, a, w, lse1, lset);
-                if (entries) g -= w.kl * p * tinv;
+                if (entries) g -= w.kl * p;
                 if (w.ce != 0.f && c == w.label) g -= w.ce;
-                pv_store_one(a.dz.p, a.dz.bf16, row * a.dz.ld + c, scale * g);
+                if (mine) pv_store_one(a.dz.p, a.dz.bf16, row * a.dz.ld + c, scale * g);
             }
         }
         if constexpr (STATS) {

@@ -385,47 +385,51 @@ __device__ __forceinline__ void load_bias(const Product& p, int n, float (&b)[W]
     for (int i = 0; i < W; i++) b[i] = have ? p.bias[min(n + i, p.N - 1)] : 0.f;
 }
 
-// W (8 or 16) consecutive outputs of a row, their bias added, from column n on
+// W (8 or 16) consecutive outputs of a row, their bias added, from column n on: 16
+// bytes a store wherever the row begins (an odd number of columns leaves most rows
+// on no boundary: 26421 x 77 -> 1298 took 90 us by single elements).
+typedef u32x4 u32x4_any __attribute__((aligned(2)));
 template <int W>
 __device__ __forceinline__ void store_run(const Product& p, int split, int m, int n,
-                                          const float (&v)[W], bool vec) {
-    if (p.splits > 1) {
-        float* o = p.partial + ((size_t)split * p.M + m) * p.N + n;
-        if (vec && n + W <= p.N) {
+                                          const float (&v)[W]) {
+    const bool whole = n + W <= p.N;
+    auto floats = [&](float* o, const float (&f)[W]) {
+        if (whole) {
 #pragma unroll
             for (int i = 0; i < W / 4; i++)
-                *(float4*)(o + 4 * i) = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2],
-                                                    v[4 * i + 3]);
+                *(u32x4_any*)(o + 4 * i) =
+                    u32x4{__float_as_uint(f[4 * i]), __float_as_uint(f[4 * i + 1]),
+                          __float_as_uint(f[4 * i + 2]), __float_as_uint(f[4 * i + 3])};
         } else {
 #pragma unroll
             for (int i = 0; i < W; i++)
-                if (n + i < p.N) o[i] = v[i];
+                if (n + i < p.N) o[i] = f[i];
         }
+    };
+    if (p.splits > 1) {
+        floats(p.partial + ((size_t)split * p.M + m) * p.N + n, v);
         return;
     }
     float r[W];
 #pragma unroll
     for (int i = 0; i < W; i++) r[i] = pv_activate(v[i], p.act, p.slope);
     const size_t at = (size_t)m * p.out.ld + n;
-    if (vec && n + W <= p.N) {
-        if (p.out.bf16) {
-            uint32_t w[W / 2];
+    if (!p.out.bf16) {
+        floats((float*)p.out.p + at, r);
+        return;
+    }
+    uint16_t* o = (uint16_t*)p.out.p + at;
+    if (whole) {
+        uint32_t w[W / 2];
 #pragma unroll
-            for (int i = 0; i < W / 2; i++) w[i] = pv_pack_bf16x2(r[2 * i], r[2 * i + 1]);
-            uint4* o = (uint4*)((uint16_t*)p.out.p + at);
+        for (int i = 0; i < W / 2; i++) w[i] = pv_pack_bf16x2(r[2 * i], r[2 * i + 1]);
 #pragma unroll
-            for (int i = 0; i < W / 8; i++)
-                o[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
-        } else {
-            float4* o = (float4*)((float*)p.out.p + at);
-#pragma unroll
-            for (int i = 0; i < W / 4; i++)
-                o[i] = make_float4(r[4 * i], r[4 * i + 1], r[4 * i + 2], r[4 * i + 3]);
-        }
+        for (int i = 0; i < W / 8; i++)
+            *(u32x4_any*)(o + 8 * i) = u32x4{w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]};
     } else {
 #pragma unroll
         for (int i = 0; i < W; i++)
-            if (n + i < p.N) pv_store_one(p.out.p, p.out.bf16, at + i, r[i]);
+            if (n + i < p.N) o[i] = pv_f32_to_bf16(r[i]);
     }
 }
 
@@ -447,7 +451,7 @@ __device__ __forceinline__ void sum_bias(const Product& p, int group, double* pa
 }
 
 template <bool EXACT>
-__global__ __launch_bounds__(kThreads, 2) void pv_fp8_tile_kernel(Product p, bool vec, int tiles) {
+__global__ __launch_bounds__(kThreads, 2) void pv_fp8_tile_kernel(Product p, int tiles) {
     // two stages, arrays of their own: the loads into one are then seen not to
     // touch what is read of the other, and are not waited for
     __shared__ __align__(16) uint8_t la0[kTile * kB], la1[kTile * kB];
@@ -591,7 +595,7 @@ __global__ __launch_bounds__(kThreads, 2) void pv_fp8_tile_kernel(Product p, boo
         for (int j = 0; j < 4; j++)
 #pragma unroll
             for (int e = 0; e < 4; e++) v[4 * j + e] = acc[j][i][e] + bias[4 * j + e];
-        if (m < p.M) store_run<16>(p, split, m, n0 + wn + 16 * h, v, vec);
+        if (m < p.M) store_run<16>(p, split, m, n0 + wn + 16 * h, v);
     }
 }
 
@@ -714,8 +718,7 @@ constexpr int kFusedM = 64, kFusedTileN = 256, kFusedThreads = 512, kFusedWaves 
 
 template <int MW, bool XB, bool EXACT>
 __global__ __launch_bounds__(kFusedThreads, kFusedWaves) void pv_fp8_fused_kernel(Fused f,
-                                                                                 Product p,
-                                                                                 bool vec) {
+                                                                                 Product p) {
     constexpr int BM = kFusedM * MW, BN = kFusedTileN;
     // vectors of x a thread; fragments of the weight a wave; its loads a wave
     constexpr int V = BM * 16 / kFusedThreads, J = 2 * MW, W = BN * kB / 16 / kFusedThreads;
@@ -811,7 +814,7 @@ __global__ __launch_bounds__(kFusedThreads, kFusedWaves) void pv_fp8_fused_kerne
         for (int j = 0; j < J; j++)
 #pragma unroll
             for (int e = 0; e < 4; e++) v[4 * j + e] = acc[j][i][e] + bias[4 * j + e];
-        if (m < f.M && multiplies) store_run<4 * J>(p, split, m, n0 + wn + 4 * J * h, v, vec);
+        if (m < f.M && multiplies) store_run<4 * J>(p, split, m, n0 + wn + 4 * J * h, v);
     }
 }
 
@@ -826,7 +829,7 @@ constexpr int kResidentShare = 16;  // tiles of columns a workgroup at most: the
 
 template <bool XB, bool EXACT>
 __global__ __launch_bounds__(kResidentThreads, 2) void pv_fp8_resident_kernel(Fused f, Product p,
-                                                                             bool vec, int share) {
+                                                                             int share) {
     constexpr int BM = kFusedM, BN = kResidentN, T = kResidentThreads;
     constexpr int V = BM * 16 / T, J = 2, W = BN * kB / 16 / T;
     __shared__ __align__(16) uint8_t lw[2][BN * kB];
@@ -918,7 +921,7 @@ __global__ __launch_bounds__(kResidentThreads, 2) void pv_fp8_resident_kernel(Fu
                     for (int e = 0; e < 4; e++)
                         v[4 * j + e] = acc[j][i][e] +
                                        lbias[(t - t0) * BN + wn + 8 * h + 4 * j + e];
-                if (m < f.M) store_run<8>(p, 0, m, t * BN + wn + 8 * h, v, vec);
+                if (m < f.M) store_run<8>(p, 0, m, t * BN + wn + 8 * h, v);
             }
         }
         k = 0;
@@ -1166,21 +1169,15 @@ void launch_quantise(const Quantise& a, hipStream_t s, const Quantise* b = nullp
     });
 }
 
-bool vector_rows(const Product& p) {
-    return p.splits > 1 ? p.N % 4 == 0
-                        : pv_aligned16(p.out.p) && p.out.ld % (p.out.bf16 ? 8 : 4) == 0;
-}
-
 void launch_product(Product p, hipStream_t s) {
     plan_splits(p.M, p.N, kTile, kTile, p.blocks, &p.per, &p.splits);
     const size_t total = (size_t)((p.M + kTile - 1) / kTile) * ((p.N + kTile - 1) / kTile) * p.splits;
     const unsigned grid = (unsigned)((total + 7) / 8 * 8);
-    const bool vec = vector_rows(p);
     const unsigned more = p.dbias ? (unsigned)((p.bias_n + kBiasColumns - 1) / kBiasColumns) : 0;
     if (p.out.bf16)
-        pv_fp8_tile_kernel<false><<<grid + more, kThreads, 0, s>>>(p, vec, (int)grid);
+        pv_fp8_tile_kernel<false><<<grid + more, kThreads, 0, s>>>(p, (int)grid);
     else
-        pv_fp8_tile_kernel<true><<<grid + more, kThreads, 0, s>>>(p, vec, (int)grid);
+        pv_fp8_tile_kernel<true><<<grid + more, kThreads, 0, s>>>(p, (int)grid);
     if (p.splits > 1)
         pv_fp8_join_kernel<<<grid_of(((size_t)p.M * p.N + kThreads - 1) / kThreads), kThreads, 0,
                              s>>>(p);
@@ -1200,18 +1197,17 @@ void launch_fused(const PvRows& x, Product p, hipStream_t s) {
     const size_t total =
         (size_t)((p.M + bm - 1) / bm) * ((p.N + kFusedTileN - 1) / kFusedTileN) * p.splits;
     const unsigned grid = (unsigned)((total + 7) / 8 * 8);
-    const bool vec = vector_rows(p);
     const Fused f{x, p.M, p.K, p.b, p.sb};
     with_bool(x.bf16, [&](auto XB) {
         with_bool(!p.out.bf16, [&](auto EXACT) {
             constexpr bool kXB = decltype(XB)::value, kExact = decltype(EXACT)::value;
             if constexpr (kXB) {
                 if (wide) {
-                    pv_fp8_fused_kernel<2, kXB, kExact><<<grid, kFusedThreads, 0, s>>>(f, p, vec);
+                    pv_fp8_fused_kernel<2, kXB, kExact><<<grid, kFusedThreads, 0, s>>>(f, p);
                     return;
                 }
             }
-            pv_fp8_fused_kernel<1, kXB, kExact><<<grid, kFusedThreads, 0, s>>>(f, p, vec);
+            pv_fp8_fused_kernel<1, kXB, kExact><<<grid, kFusedThreads, 0, s>>>(f, p);
         });
     });
     if (p.splits > 1)
@@ -1238,13 +1234,12 @@ void launch_resident(const PvRows& x, const Product& p, hipStream_t s) {
     shares = shares < least ? least : (shares > nt ? nt : shares);
     const int share = (nt + shares - 1) / shares;
     shares = (nt + share - 1) / share;
-    const bool vec = vector_rows(p);
     const Fused f{x, p.M, p.K, p.b, p.sb};
     with_bool(x.bf16, [&](auto XB) {
         with_bool(!p.out.bf16, [&](auto EXACT) {
             pv_fp8_resident_kernel<decltype(XB)::value, decltype(EXACT)::value>
                 <<<(unsigned)((size_t)mt * shares), kResidentThreads,
-                   (size_t)p.blocks * kFusedM * kB, s>>>(f, p, vec, share);
+                   (size_t)p.blocks * kFusedM * kB, s>>>(f, p, share);
         });
     });
 }

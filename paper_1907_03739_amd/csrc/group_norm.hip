@@ -26,16 +26,22 @@ struct Deal {
     size_t items;
 };
 
-// A slab is at most about 128 channels (or one group): 256 bytes of a bf16 row.
+// A slab is at most about 128 channels (or one group): 256 bytes of a bf16 row; of
+// groups that are no whole vectors, as many as make whole ones, up to kMixedSlab.
 // Chunks are for about kItems items, of kMinElements at least: an item adds the
 // sums of its cloud's chunks, which has to stay short beside its own rows.
-constexpr int kSlab = 128, kItems = 1024, kMinElements = 8192;
+constexpr int kSlab = 128, kMixedSlab = 256, kItems = 1024, kMinElements = 8192;
 
 Deal deal(int B, int N, int C, int groups) {
     Deal d;
     d.CG = C / groups;
     int k = kSlab / d.CG;
     k = k < 1 ? 1 : (k > groups ? groups : k);
+    const int odd = d.CG % 8 == 0 ? 1 : (d.CG % 4 == 0 ? 2 : (d.CG % 2 == 0 ? 4 : 8));
+    if (odd > 1 && (size_t)odd * d.CG <= kMixedSlab) {
+        k = k < odd ? odd : k / odd * odd;
+        k = k > groups ? groups : k;
+    }
     d.slab = k * d.CG;
     d.slabs = (groups + k - 1) / k;
     const size_t per = (size_t)(B > 0 ? B : 1) * d.slabs;
@@ -221,6 +227,74 @@ __global__ __launch_bounds__(kThreads) void pv_gn_sums_kernel(PvNorm n, Deal d, 
     }
 }
 
+// The same where groups are no whole vectors (MIX in the kernels below): sums a
+// channel, then a group. The slab is one run of vectors.
+template <int TYPES, int VEC>
+__global__ __launch_bounds__(kThreads) void pv_gn_mixed_sums_kernel(PvNorm n, Deal d, PvRows x,
+                                                                    double2* part, int per) {
+    __shared__ double2 red[kThreads * VEC];
+    __shared__ double2 chan[kMixedSlab];
+    for (size_t item = blockIdx.x; item < d.items; item += gridDim.x) {
+        const Place<VEC> p(item, d, n.N, n.C, n.lengths);
+        const int rows1 = min(p.rows1, p.n), c = p.c0 + p.col * VEC;
+        double s[VEC], ss[VEC];
+#pragma unroll
+        for (int i = 0; i < VEC; i++) s[i] = ss[i] = 0.;
+        for (int k = p.rows0 + p.row; k < rows1; k += p.par * kRowsAhead) {
+            Raw<TYPES, VEC> f[kRowsAhead];
+#pragma unroll
+            for (int u = 0; u < kRowsAhead; u++)
+                f[u].template load<true>(
+                    x, (size_t)p.b * n.N + min(k + u * p.par, rows1 - 1), c);
+#pragma unroll
+            for (int u = 0; u < kRowsAhead; u++)
+                if (k + u * p.par < rows1)
+#pragma unroll
+                    for (int i = 0; i < VEC; i++) {
+                        const double v = (double)f[u].get(i);
+                        s[i] += v;
+                        ss[i] = fma(v, v, ss[i]);
+                    }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < VEC; i++) red[threadIdx.x * VEC + i] = make_double2(s[i], ss[i]);
+        __syncthreads();
+        for (int i = threadIdx.x; i < p.width; i += kThreads) {
+            double t = 0., tt = 0.;
+            for (int r = 0; r < p.par; r++) {
+                t += red[r * p.width + i].x;
+                tt += red[r * p.width + i].y;
+            }
+            chan[i] = make_double2(t, tt);
+        }
+        __syncthreads();
+        for (int g = threadIdx.x >> 6; g < p.width / d.CG; g += kThreads / 64) {
+            double t = 0., tt = 0.;
+            for (int i = threadIdx.x & 63; i < d.CG; i += 64) {
+                t += chan[g * d.CG + i].x;
+                tt += chan[g * d.CG + i].y;
+            }
+            t = wave_sum(t);
+            tt = wave_sum(tt);
+            if ((threadIdx.x & 63) == 0) part[item * per + g] = make_double2(t, tt);
+        }
+    }
+}
+
+// The pairs of the groups that channels c .. lie in.
+template <bool MIX, int VEC>
+__device__ __forceinline__ void of_groups(const float2* v, int c, int CG, float (&a)[VEC],
+                                          float (&b)[VEC]) {
+    const float2 first = v[c / CG];
+#pragma unroll
+    for (int i = 0; i < VEC; i++) {
+        const float2 e = MIX ? v[(c + i) / CG] : first;
+        a[i] = e.x;
+        b[i] = e.y;
+    }
+}
+
 // A group's two sums over its cloud's chunks, by a wave, in a fixed order.
 __device__ __forceinline__ double2 add_chunks(const double2* part, int per, int chunks,
                                               size_t first, int g) {
@@ -239,7 +313,7 @@ __device__ __forceinline__ float2 stats_of(double sum, double squares, double co
     return make_float2((float)mean, (float)(1. / sqrt((var < 0. ? 0. : var) + (double)eps)));
 }
 
-template <int TYPES, bool SILU, int VEC>
+template <int TYPES, bool SILU, int VEC, bool MIX>
 __global__ __launch_bounds__(kThreads) void pv_gn_apply_kernel(PvNorm n, Deal d, PvRows x,
                                                                PvRows y, float neg,
                                                                const double2* part, int per,
@@ -260,8 +334,8 @@ __global__ __launch_bounds__(kThreads) void pv_gn_apply_kernel(PvNorm n, Deal d,
         __syncthreads();
         for (int v = p.col; v < vecs; v += p.cols) {
             const int c = p.c0 + v * VEC;
-            const float2 m = st[v * VEC / d.CG];
-            float ga[VEC], be[VEC];
+            float mean[VEC], rstd[VEC], ga[VEC], be[VEC];
+            of_groups<MIX, VEC>(st, v * VEC, d.CG, mean, rstd);
             load_params<VEC>(n, c, ga, be);
             for (int k = p.rows0 + p.row; k < p.rows1; k += p.par * kRowsAhead) {
                 Raw<TYPES, VEC> f[kRowsAhead];
@@ -276,7 +350,8 @@ __global__ __launch_bounds__(kThreads) void pv_gn_apply_kernel(PvNorm n, Deal d,
                     float r[VEC];
 #pragma unroll
                     for (int j = 0; j < VEC; j++)
-                        r[j] = act_of<SILU>(fmaf(ga[j], (f[u].get(j) - m.x) * m.y, be[j]), neg);
+                        r[j] = act_of<SILU>(
+                            fmaf(ga[j], (f[u].get(j) - mean[j]) * rstd[j], be[j]), neg);
                     if (ku > last)
 #pragma unroll
                         for (int j = 0; j < VEC; j++) r[j] = 0.f;
@@ -290,7 +365,7 @@ __global__ __launch_bounds__(kThreads) void pv_gn_apply_kernel(PvNorm n, Deal d,
 // chan[b * chunks + chunk][c] = (sum dv xh, sum dv) over the chunk's rows, and
 // part[item][group in slab] = their sums over the group's channels, times
 // gamma: (sum gamma dv, sum gamma dv xh).
-template <int TYPES, bool SILU, int VEC>
+template <int TYPES, bool SILU, int VEC, bool MIX>
 __global__ __launch_bounds__(kThreads) void pv_gn_bwd_sums_kernel(PvNorm n, Deal d, PvRows dy,
                                                                   PvRows x, float neg,
                                                                   const float2* stats,
@@ -307,8 +382,8 @@ __global__ __launch_bounds__(kThreads) void pv_gn_bwd_sums_kernel(PvNorm n, Deal
 #pragma unroll
             for (int i = 0; i < VEC; i++) s[i] = h[i] = 0.f;
             if (v0 + p.col < vecs) {
-                const float2 m = stats[(size_t)p.b * n.groups + c / d.CG];
-                float ga[VEC], be[VEC];
+                float mean[VEC], rstd[VEC], ga[VEC], be[VEC];
+                of_groups<MIX, VEC>(stats + (size_t)p.b * n.groups, c, d.CG, mean, rstd);
                 load_params<VEC>(n, c, ga, be);
                 for (int k = p.rows0 + p.row; k < rows1; k += p.par * kRowsAhead) {
                     Raw<TYPES, VEC> f[kRowsAhead], g[kRowsAhead];
@@ -323,7 +398,7 @@ __global__ __launch_bounds__(kThreads) void pv_gn_bwd_sums_kernel(PvNorm n, Deal
                         if (k + u * p.par >= rows1) break;
 #pragma unroll
                         for (int i = 0; i < VEC; i++) {
-                            const float xh = (f[u].get(i) - m.x) * m.y;
+                            const float xh = (f[u].get(i) - mean[i]) * rstd[i];
                             const float dv =
                                 g[u].get(i) * dact_of<SILU>(fmaf(ga[i], xh, be[i]), neg);
                             s[i] += dv;
@@ -400,7 +475,7 @@ __device__ __forceinline__ void add_params(size_t rows, int C, const float2* cha
     }
 }
 
-template <int TYPES, bool SILU, int VEC>
+template <int TYPES, bool SILU, int VEC, bool MIX>
 __global__ __launch_bounds__(kThreads) void pv_gn_bwd_apply_kernel(
     PvNorm n, Deal d, PvRows dy, PvRows x, PvRows dx, float neg, const float2* stats,
     const float2* chan, const double2* part, int per, float* dgamma, float* dbeta, unsigned params) {
@@ -424,9 +499,9 @@ __global__ __launch_bounds__(kThreads) void pv_gn_bwd_apply_kernel(
         __syncthreads();
         for (int v = p.col; v < vecs; v += p.cols) {
             const int c = p.c0 + v * VEC;
-            const float2 q = gs[v * VEC / d.CG];
-            const float2 m = stats[(size_t)p.b * n.groups + c / d.CG];
-            float ga[VEC], be[VEC];
+            float m1[VEC], m2[VEC], mean[VEC], rstd[VEC], ga[VEC], be[VEC];
+            of_groups<MIX, VEC>(gs, v * VEC, d.CG, m1, m2);
+            of_groups<MIX, VEC>(stats + (size_t)p.b * n.groups, c, d.CG, mean, rstd);
             load_params<VEC>(n, c, ga, be);
             for (int k = p.rows0 + p.row; k < p.rows1; k += p.par * kRowsAhead) {
                 Raw<TYPES, VEC> f[kRowsAhead], g[kRowsAhead];
@@ -443,9 +518,9 @@ __global__ __launch_bounds__(kThreads) void pv_gn_bwd_apply_kernel(
                     float r[VEC];
 #pragma unroll
                     for (int j = 0; j < VEC; j++) {
-                        const float xh = (f[u].get(j) - m.x) * m.y;
+                        const float xh = (f[u].get(j) - mean[j]) * rstd[j];
                         const float dv = g[u].get(j) * dact_of<SILU>(fmaf(ga[j], xh, be[j]), neg);
-                        r[j] = m.y * (fmaf(ga[j], dv, -q.x) - xh * q.y);
+                        r[j] = rstd[j] * (fmaf(ga[j], dv, -m1[j]) - xh * m2[j]);
                     }
                     if (ku > last)
 #pragma unroll
@@ -692,6 +767,18 @@ int width_for(int CG, const PvRows* r, int count) {
     }
     return v;
 }
+// The vector width of the two launches: vectors across groups (MIX) where those of
+// a group are narrower and a slab is whole vectors.
+struct Width {
+    int vec;
+    bool mix;
+};
+Width width_of_rows(const Deal& d, int C, const PvRows* r, int count) {
+    const int own = width_for(d.CG, r, count), rows = width_for(C, r, count);
+    if (rows > own && d.slab <= kMixedSlab && d.slab % rows == 0) return {rows, true};
+    return {own, false};
+}
+
 // f with the call's types, activation and vector width as constants
 template <typename F>
 void with_kind(int types, bool silu, int vec, F f) {
@@ -754,28 +841,40 @@ pvconv_status pv_launch_group_norm(const PvNorm& n, const PvRows& x, const PvRow
     const PvRows all[2] = {x, y};
     const int per = d.slab / d.CG;
     const float neg = negative_slope(n);
-    with_kind(types_of(all, 2), n.act == PVCONV_ACT_SILU, width_for(d.CG, all, 2),
-              [&](auto T, auto S, auto V) {
-                  constexpr int TYPES = decltype(T)::value, VEC = decltype(V)::value;
-                  constexpr bool SILU = decltype(S)::value;
-                  const unsigned held = (unsigned)(((size_t)n.B * n.groups + 7) / 8 * 8);
-                  switch (hold_of(n, VEC, kLargeU)) {
-                      case kSmall:
-                          pv_gn_held_kernel<kSmallT, kSmallU, TYPES, SILU, VEC>
-                              <<<held, kSmallT, 0, s>>>(n, x, y, neg, (float2*)stats);
-                          return;
-                      case kLarge:
-                          pv_gn_held_kernel<kLargeT, kLargeU, TYPES, SILU, VEC>
-                              <<<held, kLargeT, 0, s>>>(n, x, y, neg, (float2*)stats);
-                          return;
-                      case kNot: break;
-                  }
-                  pv_gn_sums_kernel<TYPES, VEC>
-                      <<<grid_of(d.items), kThreads, 0, s>>>(n, d, x, (double2*)ws, per);
-                  pv_gn_apply_kernel<TYPES, SILU, VEC>
-                      <<<grid_of(d.items), kThreads, per * sizeof(float2), s>>>(
-                          n, d, x, y, neg, (const double2*)ws, per, (float2*)stats);
-              });
+    const int types = types_of(all, 2), own = width_for(d.CG, all, 2);
+    const bool silu = n.act == PVCONV_ACT_SILU;
+    const Hold hold = hold_of(n, own, kLargeU);
+    if (hold != kNot) {
+        with_kind(types, silu, own, [&](auto T, auto S, auto V) {
+            constexpr int TYPES = decltype(T)::value, VEC = decltype(V)::value;
+            constexpr bool SILU = decltype(S)::value;
+            const unsigned held = (unsigned)(((size_t)n.B * n.groups + 7) / 8 * 8);
+            if (hold == kSmall)
+                pv_gn_held_kernel<kSmallT, kSmallU, TYPES, SILU, VEC>
+                    <<<held, kSmallT, 0, s>>>(n, x, y, neg, (float2*)stats);
+            else
+                pv_gn_held_kernel<kLargeT, kLargeU, TYPES, SILU, VEC>
+                    <<<held, kLargeT, 0, s>>>(n, x, y, neg, (float2*)stats);
+        });
+        return pv_launch_status();
+    }
+    const Width w = width_of_rows(d, n.C, all, 2);
+    with_kind(types, silu, w.vec, [&](auto T, auto S, auto V) {
+        constexpr int TYPES = decltype(T)::value, VEC = decltype(V)::value;
+        constexpr bool SILU = decltype(S)::value;
+        const unsigned grid = grid_of(d.items);
+        const size_t lds = per * sizeof(float2);
+        double2* part = (double2*)ws;
+        if (w.mix) {
+            pv_gn_mixed_sums_kernel<TYPES, VEC><<<grid, kThreads, 0, s>>>(n, d, x, part, per);
+            pv_gn_apply_kernel<TYPES, SILU, VEC, true>
+                <<<grid, kThreads, lds, s>>>(n, d, x, y, neg, part, per, (float2*)stats);
+        } else {
+            pv_gn_sums_kernel<TYPES, VEC><<<grid, kThreads, 0, s>>>(n, d, x, part, per);
+            pv_gn_apply_kernel<TYPES, SILU, VEC, false>
+                <<<grid, kThreads, lds, s>>>(n, d, x, y, neg, part, per, (float2*)stats);
+        }
+    });
     return pv_launch_status();
 }
 
@@ -793,35 +892,45 @@ pvconv_status pv_launch_group_norm_bwd(const PvNorm& norm, const PvRows& dy, con
     double2* part = (double2*)ws;
     float2* chan = (float2*)((char*)ws + pv_group_norm_ws_bytes(n.B, n.N, n.C, n.groups));
     const float neg = negative_slope(n);
-    with_kind(types_of(all, 3), n.act == PVCONV_ACT_SILU, width_for(d.CG, all, 3),
-              [&](auto T, auto S, auto V) {
-                  constexpr int TYPES = decltype(T)::value, VEC = decltype(V)::value;
-                  constexpr bool SILU = decltype(S)::value;
-                  const Hold hold = n.B ? hold_of(n, VEC, kLargeBwdU) : kNot;
-                  if (hold != kNot) {
-                      const unsigned held = (unsigned)(((size_t)n.B * n.groups + 7) / 8 * 8);
-                      float2* sums = n.B > 1 ? (float2*)ws : nullptr;
-                      if (hold == kSmall)
-                          pv_gn_held_bwd_kernel<kSmallT, kSmallU, TYPES, SILU, VEC>
-                              <<<held, kSmallT, kSmallT * VEC * sizeof(float2), s>>>(
-                                  n, dy, x, dx, neg, (const float2*)stats, sums, dgamma, dbeta);
-                      else
-                          pv_gn_held_bwd_kernel<kLargeT, kLargeBwdU, TYPES, SILU, VEC>
-                              <<<held, kLargeT, kLargeT * VEC * sizeof(float2), s>>>(
-                                  n, dy, x, dx, neg, (const float2*)stats, sums, dgamma, dbeta);
-                      if (sums && (dgamma || dbeta))
-                          pv_gn_params_kernel<<<(n.C + kParamChannels - 1) / kParamChannels,
-                                                kThreads, 0, s>>>(n.B, n.C, sums, dgamma, dbeta);
-                      return;
-                  }
-                  if (d.items)
-                      pv_gn_bwd_sums_kernel<TYPES, SILU, VEC>
-                          <<<grid_of(d.items), kThreads, 0, s>>>(
-                              n, d, dy, x, neg, (const float2*)stats, chan, part, per);
-                  pv_gn_bwd_apply_kernel<TYPES, SILU, VEC>
-                      <<<grid_of(d.items) + params, kThreads, per * sizeof(float2), s>>>(
-                          n, d, dy, x, dx, neg, (const float2*)stats, chan, part, per, dgamma,
-                          dbeta, params);
-              });
+    const int types = types_of(all, 3), own = width_for(d.CG, all, 3);
+    const bool silu = n.act == PVCONV_ACT_SILU;
+    const Hold hold = n.B ? hold_of(n, own, kLargeBwdU) : kNot;
+    const float2* st = (const float2*)stats;
+    if (hold != kNot) {
+        float2* sums = n.B > 1 ? (float2*)ws : nullptr;
+        with_kind(types, silu, own, [&](auto T, auto S, auto V) {
+            constexpr int TYPES = decltype(T)::value, VEC = decltype(V)::value;
+            constexpr bool SILU = decltype(S)::value;
+            const unsigned held = (unsigned)(((size_t)n.B * n.groups + 7) / 8 * 8);
+            if (hold == kSmall)
+                pv_gn_held_bwd_kernel<kSmallT, kSmallU, TYPES, SILU, VEC>
+                    <<<held, kSmallT, kSmallT * VEC * sizeof(float2), s>>>(
+                        n, dy, x, dx, neg, st, sums, dgamma, dbeta);
+            else
+                pv_gn_held_bwd_kernel<kLargeT, kLargeBwdU, TYPES, SILU, VEC>
+                    <<<held, kLargeT, kLargeT * VEC * sizeof(float2), s>>>(
+                        n, dy, x, dx, neg, st, sums, dgamma, dbeta);
+        });
+        if (sums && params)
+            pv_gn_params_kernel<<<params, kThreads, 0, s>>>(n.B, n.C, sums, dgamma, dbeta);
+        return pv_launch_status();
+    }
+    const Width w = width_of_rows(d, n.C, all, 3);
+    with_kind(types, silu, w.vec, [&](auto T, auto S, auto V) {
+        constexpr int TYPES = decltype(T)::value, VEC = decltype(V)::value;
+        constexpr bool SILU = decltype(S)::value;
+        auto go = [&](auto MIX) {
+            if (d.items)
+                pv_gn_bwd_sums_kernel<TYPES, SILU, VEC, decltype(MIX)::value>
+                    <<<grid_of(d.items), kThreads, 0, s>>>(n, d, dy, x, neg, st, chan, part, per);
+            pv_gn_bwd_apply_kernel<TYPES, SILU, VEC, decltype(MIX)::value>
+                <<<grid_of(d.items) + params, kThreads, per * sizeof(float2), s>>>(
+                    n, d, dy, x, dx, neg, st, chan, part, per, dgamma, dbeta, params);
+        };
+        if (w.mix)
+            go(std::true_type());
+        else
+            go(std::false_type());
+    });
     return pv_launch_status();
 }

@@ -83,6 +83,11 @@ GN = [
     (70, 3, 24, 2, "f32", "f32", "silu", None, 0, 0),        # many small clouds
     (1, 40000, 16, 2, "bf16", "bf16", "relu", None, 8, 0),   # a long cloud
     (2, 33, 35, 5, "bf16", "bf16", "silu", None, 2, 1),      # odd rows: no vectors
+    (1, 30000, 96, 32, "f32", "f32", "relu", None, 0, 0),    # vectors across groups of 3
+    (2, 21000, 72, 24, "bf16", "bf16", "silu", [21000, 50], 0, 0),
+    (1, 20000, 30, 2, "bf16", "f32", "leaky", None, 2, 0),   # 15 channels a group
+    (2, 9000, 200, 8, "bf16", "bf16", "silu", None, 8, 8),   # 25 channels a group
+    (1, 70000, 132, 3, "f32", "f32", "none", [65537], 0, 0),
 ]
 
 
