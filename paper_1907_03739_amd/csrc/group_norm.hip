@@ -29,8 +29,9 @@ struct Deal {
 // A slab is at most about 128 channels (or one group): 256 bytes of a bf16 row; of
 // groups that are no whole vectors, as many as make whole ones, up to kMixedSlab.
 // Chunks are for about kItems items, of kMinElements at least: an item adds the
-// sums of its cloud's chunks, which has to stay short beside its own rows.
-constexpr int kSlab = 128, kMixedSlab = 256, kItems = 1024, kMinElements = 8192;
+// sums of its cloud's chunks (kSums pairs at most, 128 KB from the L2), which has
+// to stay short beside its own rows.
+constexpr int kSlab = 128, kMixedSlab = 256, kItems = 1024, kSums = 8192, kMinElements = 8192;
 
 Deal deal(int B, int N, int C, int groups) {
     Deal d;
@@ -46,6 +47,7 @@ Deal deal(int B, int N, int C, int groups) {
     d.slabs = (groups + k - 1) / k;
     const size_t per = (size_t)(B > 0 ? B : 1) * d.slabs;
     size_t chunks = (kItems + per - 1) / per;
+    if (chunks > (size_t)kSums / k) chunks = kSums / k < 1 ? 1 : kSums / k;
     const int rows = (kMinElements + d.slab - 1) / d.slab;
     const size_t most = ((size_t)N + rows - 1) / rows;
     if (chunks > most) chunks = most;
