@@ -540,6 +540,19 @@ __global__ __launch_bounds__(kThreads) void pv_gn_bwd_apply_kernel(
 // squares about it then, both from the registers.
 // ---------------------------------------------------------------------------
 template <int T>
+__device__ __forceinline__ double group_sum(double a, double* lds) {
+    a = wave_sum(a);
+    if constexpr (T > 64) {
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = a;
+        __syncthreads();
+        a = 0.;
+#pragma unroll
+        for (int w = 0; w < T / 64; w++) a += lds[w];
+    }
+    return a;
+}
+template <int T>
 __device__ __forceinline__ double2 group_sum(double a, double b, double2* lds) {
     a = wave_sum(a);
     b = wave_sum(b);
@@ -584,7 +597,7 @@ __device__ __forceinline__ size_t run_of_xcd(size_t items) {
 template <int T, int U, int TYPES, bool SILU, int VEC>
 __global__ __launch_bounds__(T) void pv_gn_held_kernel(PvNorm n, PvRows x, PvRows y, float neg,
                                                        float2* stats) {
-    __shared__ double2 lds[T / 64];
+    __shared__ double lds[T / 64];
     const size_t item = run_of_xcd((size_t)n.B * n.groups);
     if (item >= (size_t)n.B * n.groups) return;
     const Held<T, VEC> p(n, item);
@@ -600,11 +613,22 @@ __global__ __launch_bounds__(T) void pv_gn_held_kernel(PvNorm n, PvRows x, PvRow
     if (p.active)
 #pragma unroll
         for (int u = 0; u < U; u++)
-            if (p.row + u * p.par < p.n)
+            if (p.row + u * p.par < p.n) {
+                // the mean of a vector of bf16 in fp32: values of 8 bits, which it adds
+                // without loss unless they lie 2^13 apart
+                float v = 0.f;
 #pragma unroll
-                for (int i = 0; i < VEC; i++) s += (double)f[u].get(i);
+                for (int i = 0; i < VEC; i++) {
+                    if (TYPES == kBf16)
+                        v = fmaf(f[u].get(i), 1.f / VEC, v);
+                    else
+                        s += (double)f[u].get(i);
+                }
+                if (TYPES == kBf16) s += (double)v;
+            }
+    if (TYPES == kBf16) s *= VEC;
     const double cnt = (double)p.n * (n.C / n.groups);
-    const double mean = cnt > 0. ? group_sum<T>(s, 0., lds).x / cnt : 0.;
+    const double mean = cnt > 0. ? group_sum<T>(s, lds) / cnt : 0.;
     const float m = (float)mean;
     float q = 0.f;
     if (p.active)
@@ -619,7 +643,7 @@ __global__ __launch_bounds__(T) void pv_gn_held_kernel(PvNorm n, PvRows x, PvRow
     float2 st = make_float2(0.f, 0.f);
     if (cnt > 0.) {
         const double off = mean - (double)m;
-        const double var = group_sum<T>((double)q, 0., lds).x / cnt - off * off;
+        const double var = group_sum<T>((double)q, lds) / cnt - off * off;
         st = make_float2(m, (float)(1. / sqrt((var < 0. ? 0. : var) + (double)n.eps)));
     }
     if (stats && threadIdx.x == 0) stats[item] = st;
@@ -652,7 +676,11 @@ __global__ __launch_bounds__(T) void pv_gn_held_bwd_kernel(PvNorm n, PvRows dy, 
     const Held<T, VEC> p(n, item);
     const int CG = n.C / n.groups;
     const float2 st = stats[item];
+    // dy times the activation's derivative: held from the sums on, of four vectors of 8
+    // of two (more would spill)
+    constexpr int kKept = U * VEC > 24 ? U / 2 : U;
     Raw<TYPES, VEC> f[U], g[U];
+    float kept[kKept][VEC];
     float ga[VEC], be[VEC], h[VEC], s[VEC];
 #pragma unroll
     for (int i = 0; i < VEC; i++) h[i] = s[i] = 0.f;
@@ -674,6 +702,7 @@ __global__ __launch_bounds__(T) void pv_gn_held_bwd_kernel(PvNorm n, PvRows dy, 
                     const float dv = g[u].get(i) * dact_of<SILU>(fmaf(ga[i], xh, be[i]), neg);
                     s[i] += dv;
                     h[i] = fmaf(dv, xh, h[i]);
+                    if (u < kKept) kept[u][i] = dv;
                 }
 #pragma unroll
         for (int i = 0; i < VEC; i++) {
@@ -734,7 +763,9 @@ __global__ __launch_bounds__(T) void pv_gn_held_bwd_kernel(PvNorm n, PvRows dy, 
 #pragma unroll
         for (int i = 0; i < VEC; i++) {
             const float xh = (f[u].get(i) - st.x) * st.y;
-            const float dv = g[u].get(i) * dact_of<SILU>(fmaf(ga[i], xh, be[i]), neg);
+            const float dv =
+                u < kKept ? kept[u < kKept ? u : 0][i]
+                          : g[u].get(i) * dact_of<SILU>(fmaf(ga[i], xh, be[i]), neg);
             r[i] = st.y * (fmaf(ga[i], dv, -m1) - xh * m2);
         }
         if (k >= p.n)
