@@ -6,10 +6,10 @@
 // and the label beside them, the gradient of a logit is
 //   w (alpha T (exp(z / T - lse_T) - p) + (1 - alpha) (exp(z - lse_1) - [label])).
 // Bound by HBM: z read once and, where the gradient is taken, dz written.
-// Rows of few classes stay in the registers of 16 lanes or of a wave, from the
-// one read to the gradient. Rows of many take a workgroup, which goes over them
-// once with a running maximum and sums a thread and, for the gradient, a
-// second time, when they still lie in the caches.
+// Rows of up to 2048 classes stay in the registers of 4 to 64 lanes, from the one
+// read to the gradient. Rows of more take a workgroup, which goes over them once
+// with a running maximum and sums a thread and, for the gradient, a second time,
+// when they still lie in the caches.
 #include <type_traits>
 
 #include "pv_train.h"
@@ -64,6 +64,8 @@ __device__ __forceinline__ float soft_grad(float z, const Args& a, const Terms& 
 // ---------------------------------------------------------------------------
 // Few classes: TEAM lanes hold a row, E logits each (class e * TEAM + lane).
 // STATS: loss and statistics are computed, else read. GRAD: dz is written.
+// 16384 x 50, top 8, fp32, loss and gradient: 7.9 us, of which 1.5 would move the
+// bytes: bound by a row's chain of reductions and entries.
 // ---------------------------------------------------------------------------
 constexpr int kThreads = 256;
 
@@ -215,6 +217,7 @@ __global__ __launch_bounds__(kThreads) void pv_distill_short_kernel(Args a) {
 // first 16-byte boundary on, the elements before and after one a thread. Rows
 // of z and dz rarely share that boundary (an odd number of classes): the pass
 // that reads alone goes by z's, the pass that writes by dz's.
+// 4096 x 49999, top 64, bf16: loss 104 us (3.9 TB/s), gradient 197 (4.2 TB/s).
 // ---------------------------------------------------------------------------
 constexpr int kAhead = 4;  // vectors in flight a thread
 
