@@ -843,14 +843,17 @@ void with_kind(int types, bool silu, int vec, F f) {
 
 // Whether a group fits the registers of a workgroup, and of which: vectors a
 // thread of 256 (kSmallU) or of 1024 (kLargeU, kLargeBwdU: a gradient holds x and
-// dy). One (cloud, group) a workgroup, up to 2^31 of them.
+// dy). One (cloud, group) a workgroup, as many as a launch of fewer than 2^32
+// threads holds.
 constexpr int kSmallT = 256, kSmallU = 2, kLargeT = 1024, kLargeU = 8, kLargeBwdU = 4;
 enum Hold { kNot, kSmall, kLarge };
 Hold hold_of(const PvNorm& n, int vec, int large_u) {
-    if (n.N < 1 || (size_t)n.B * n.groups >= (1u << 31) - 8) return kNot;
+    if (n.N < 1) return kNot;
+    const size_t items = ((size_t)n.B * n.groups + 7) / 8 * 8;
+    auto launches = [&](int threads) { return items * threads <= 0xffffffffu; };
     const int cols = n.C / n.groups / vec;
-    if (cols <= kSmallT && n.N <= kSmallT / cols * kSmallU) return kSmall;
-    if (cols <= kLargeT && n.N <= kLargeT / cols * large_u) return kLarge;
+    if (cols <= kSmallT && n.N <= kSmallT / cols * kSmallU) return launches(kSmallT) ? kSmall : kNot;
+    if (cols <= kLargeT && n.N <= kLargeT / cols * large_u) return launches(kLargeT) ? kLarge : kNot;
     return kNot;
 }
 

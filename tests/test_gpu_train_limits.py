@@ -1,0 +1,73 @@
+"""The training and 8-bit operators at sizes whose launches come near what HIP
+takes (fewer than 2^32 threads): every declared size runs."""
+import numpy as np
+import pytest
+import torch
+
+import _train_ref as ref
+from paper_1907_03739_amd import binding as pv
+from _helpers import host
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+
+
+@pytest.fixture(autouse=True)
+def _gpu_case(request):
+    assert torch.cuda.is_available(), "GPU tests need an MI355X"
+    print(f"\n[gpu case] {request.node.nodeid}", flush=True)
+    yield
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+
+
+def randn(*shape, seed, dtype=torch.bfloat16, scale=1.0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return torch.randn(*shape, device="cuda", generator=g, dtype=dtype).mul_(scale)
+
+
+# 2^24 groups of two channels (256 threads each would be 2^32), 2^22 groups of 513
+# rows (1024 threads each)
+@pytest.mark.parametrize("B,N,C,G", [(1 << 20, 1, 32, 16), (1 << 20, 513, 4, 4)])
+def test_group_norm_of_very_many_groups(B, N, C, G):
+    x, dy = randn(B, N, C, seed=1), randn(B, N, C, seed=2)
+    ga, be = 1 + 0.1 * randn(C, seed=3, dtype=torch.float32), 0.5 * randn(C, seed=4, dtype=torch.float32)
+    y, st = pv.pvconv_group_norm_act(x, G, ga, be, want_stats=True)
+    dx, dg, db = pv.pvconv_group_norm_act_backward(dy, x, st, G, ga, be)
+    sums, sizes = np.zeros((2, C)), np.zeros((2, C))
+    step = max(1, (1 << 22) // (N * C))
+    # whole clouds at both ends and in between; every cloud where they are short
+    runs = range(0, B, step) if N == 1 else (0, B // 2 + 3, B - step)
+    gd, bd = host(ga), host(be)
+    for b in runs:
+        xs, ds = host(x[b:b + step]), host(dy[b:b + step])
+        n, W = xs.shape[0], C // G
+        u = xs.reshape(n, N, G, W)
+        mean = u.mean((1, 3), keepdims=True)
+        r = 1 / np.sqrt(((u - mean) ** 2).mean((1, 3), keepdims=True) + 1e-5)
+        xh = ((u - mean) * r).reshape(n, N, C)
+        v = xh * gd + bd
+        want = ref.act(v, "silu", 0.0)
+        rr = np.broadcast_to(r, u.shape).reshape(n, N, C)
+        mag = (np.abs(xs) + np.abs(np.broadcast_to(mean, u.shape).reshape(n, N, C))) * rr * np.abs(gd) \
+            + np.abs(bd)
+        got = host(y[b:b + step])
+        assert (np.abs(got - want) <= 16 * U * mag + 2.0 ** -8 * np.abs(want)).all()
+        dv = ds * ref.dact(v, "silu", 0.0)
+        sums += [(dv * xh).sum((0, 1)), dv.sum((0, 1))]
+        size = np.abs(ds) * ref.dact_magnitude(v, "silu", 0.0)
+        sizes += [(size * np.abs(xh)).sum((0, 1)), size.sum((0, 1))]
+        h = (gd * dv).reshape(u.shape)
+        xg = xh.reshape(u.shape)
+        m1, m2 = h.mean((1, 3), keepdims=True), (h * xg).mean((1, 3), keepdims=True)
+        want = (r * (h - m1 - xg * m2)).reshape(n, N, C)
+        # as the other tests of this gradient: 64 u of the terms' largest of the cloud,
+        # and what an error of x - mean and rstd leaves in xh, by which dv is evaluated
+        size = rr * np.abs(gd * ds) * 1.1
+        cloud = size.max((1, 2), keepdims=True)
+        floor = 64 * U * (size + cloud * (1 + mag))
+        got = host(dx[b:b + step])
+        assert (np.abs(got - want) <= floor + 2.0 ** -8 * np.abs(want)).all()
+    if N == 1:
+        assert (np.abs(host(dg) - sums[0]) <= 64 * U * sizes[0]).all()
+        assert (np.abs(host(db) - sums[1]) <= 64 * U * sizes[1]).all()
