@@ -10,6 +10,7 @@
 // their way into the product (pv_fp8_few_, _resident_, _fused_kernel: path_of has
 // the rule); the weight's gradient, whose blocks run along the rows, takes them
 // transposed out of the workspace (pv_fp8_quantise_, _tile_kernel).
+#include <initializer_list>
 #include <type_traits>
 
 #include "pv_train.h"
@@ -1178,22 +1179,52 @@ void with_bool(bool b, F f) {
         f(std::false_type());
 }
 
+int tiles_of(const Quantise& z) { return pv_fp8_blocks(z.M) * pv_fp8_blocks(z.C); }
+
 template <int WHAT>
 void launch_quantise(const Quantise& a, hipStream_t s, const Quantise* b = nullptr) {
-    auto tiles = [](const Quantise& z) { return pv_fp8_blocks(z.M) * pv_fp8_blocks(z.C); };
     if (b && (a.x.bf16 != b->x.bf16 || (a.C < 8) != (b->C < 8))) {
         launch_quantise<WHAT>(a, s);
         launch_quantise<WHAT>(*b, s);
         return;
     }
-    const QuantiseJobs jobs{a, b ? *b : a, tiles(a)};
-    const unsigned grid = (unsigned)(tiles(a) + (b ? tiles(*b) : 0));
+    const QuantiseJobs jobs{a, b ? *b : a, tiles_of(a)};
+    const unsigned grid = (unsigned)(tiles_of(a) + (b ? tiles_of(*b) : 0));
     with_bool(a.x.bf16, [&](auto XB) {
         with_bool(a.C < 8, [&](auto NARROW) {
             pv_fp8_quantise_kernel<decltype(XB)::value, decltype(NARROW)::value, WHAT>
                 <<<grid, kThreads, 0, s>>>(jobs);
         });
     });
+}
+
+// HIP takes fewer than 2^32 threads a launch: what would need more than kMostThreads
+// runs in parts, rows after rows.
+constexpr size_t kMostThreads = (size_t)1 << 31;
+
+// The columns of a (and b), in blocks along the rows, or their sums.
+template <int WHAT>
+void launch_columns(const Quantise& a, hipStream_t s, const Quantise* b = nullptr) {
+    static_assert((WHAT & (kRows | kBlock)) == 0, "a part's rows lie on their own");
+    const size_t tiles = (size_t)tiles_of(a) + (b ? tiles_of(*b) : 0);
+    if (tiles * kThreads <= kMostThreads) {
+        launch_quantise<WHAT>(a, s, b);
+        return;
+    }
+    for (const Quantise* z : {&a, b}) {
+        if (!z) continue;
+        const int cbs = pv_fp8_blocks(z->C), rbs = pv_fp8_blocks(z->M);
+        const int run = (int)(kMostThreads / kThreads / cbs);
+        for (int rb = 0; rb < rbs; rb += run) {
+            Quantise part = *z;
+            part.x.p = (char*)z->x.p + (size_t)rb * kB * z->x.ld * (z->x.bf16 ? 2 : 4);
+            part.M = (rb + run < rbs ? (rb + run) * kB : z->M) - rb * kB;
+            if (z->qt) part.qt = z->qt + (size_t)rb * z->C * kB;
+            if (z->scale_t) part.scale_t = z->scale_t + (size_t)rb * z->C;
+            if (z->sum) part.sum = z->sum + (size_t)rb * z->C;
+            launch_quantise<WHAT>(part, s);
+        }
+    }
 }
 
 void launch_product(Product p, hipStream_t s) {
@@ -1293,25 +1324,43 @@ Product with_weight(const Quantised& a, int M, const uint8_t* w, const uint8_t* 
     return p;
 }
 
+// Rows a part of a product takes: all of them unless its launches might need more
+// than kMostThreads (512 threads for 64 rows x 128 columns of x or y at most). Parts
+// are then alike, far larger than what any rule below or path_of looks at.
+int rows_a_part(int M, int K, int N) {
+    const size_t threads =
+        ((size_t)M + kFusedM - 1) / kFusedM * pv_fp8_blocks(K > N ? K : N) * kFusedThreads;
+    const size_t parts = (threads + kMostThreads - 1) / kMostThreads;
+    return parts <= 1 ? M : pv_fp8_blocks((int)(((size_t)M + parts - 1) / parts)) * kB;
+}
+
 // out = act( Q(x) W^T + bias )
 void launch_rows_product(const PvRows& x, int M, int K, int N, const uint8_t* weight,
                          const uint8_t* scale, const float* bias, int act, float slope,
                          const PvRows& out, const RowsWs& w, hipStream_t s) {
-    Product p = with_weight(w.x, M, weight, scale, N, pv_fp8_blocks(K), out, w.partial);
-    p.K = K;
-    p.bias = bias;
-    p.act = act;
-    p.slope = slope;
-    p.splits = 1;
-    switch (path_of(M, K, N)) {
-        case kFew: launch_few(x, p, s); break;
-        case kResident: launch_resident(x, p, s); break;
-        case kFused: launch_fused(x, p, s); break;
-        case kApart:
-            launch_quantise<kRows>(
-                Quantise{x, M, K, w.x.q, w.x.scale, nullptr, nullptr, nullptr}, s);
-            launch_product(p, s);
-            break;
+    const Path path = path_of(M, K, N);
+    const int rows = rows_a_part(M, K, N);
+    for (int m = 0; m < M; m += rows) {
+        const int n = rows < M - m ? rows : M - m;
+        PvRows xm = x, ym = out;
+        xm.p = (char*)x.p + (size_t)m * x.ld * (x.bf16 ? 2 : 4);
+        ym.p = (char*)out.p + (size_t)m * out.ld * (out.bf16 ? 2 : 4);
+        Product p = with_weight(w.x, n, weight, scale, N, pv_fp8_blocks(K), ym, w.partial);
+        p.K = K;
+        p.bias = bias;
+        p.act = act;
+        p.slope = slope;
+        p.splits = 1;
+        switch (path) {
+            case kFew: launch_few(xm, p, s); break;
+            case kResident: launch_resident(xm, p, s); break;
+            case kFused: launch_fused(xm, p, s); break;
+            case kApart:
+                launch_quantise<kRows>(
+                    Quantise{xm, n, K, w.x.q, w.x.scale, nullptr, nullptr, nullptr}, s);
+                launch_product(p, s);
+                break;
+        }
     }
 }
 
@@ -1352,9 +1401,9 @@ pvconv_status pv_launch_fp8_linear_bwd(const PvRows& dy, const PvRows& x, int M,
     const Quantise zy{dy, M, N, nullptr, nullptr, w.dyt.q, w.dyt.scale, dbias ? w.sum : nullptr};
     const Quantise zx{x, M, K, nullptr, nullptr, w.xt.q, w.xt.scale, nullptr};
     if (dw && M)
-        launch_quantise<kCols | kSum>(zy, s, &zx);
+        launch_columns<kCols | kSum>(zy, s, &zx);
     else if (dbias && M)
-        launch_quantise<kSum>(zy, s);
+        launch_columns<kSum>(zy, s);
     if (dw && M) {
         Product p{};
         p.a = w.dyt.q;

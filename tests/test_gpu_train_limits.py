@@ -71,3 +71,37 @@ def test_group_norm_of_very_many_groups(B, N, C, G):
     if N == 1:
         assert (np.abs(host(dg) - sums[0]) <= 64 * U * sizes[0]).all()
         assert (np.abs(host(db) - sums[1]) <= 64 * U * sizes[1]).all()
+
+
+def test_fp8_linear_of_very_many_rows():
+    # 2^23 tiles of 64 rows, 512 threads each: 2^32
+    M, K, N = 1 << 29, 8, 3
+    x = randn(M, K, seed=1, dtype=torch.float32)
+    w = randn(N, K, seed=2, dtype=torch.float32)
+    q, s = pv.pvconv_fp8_quantize_weight(w)
+    qw = ref.quantise_weight(host(w))[0]
+    y = pv.pvconv_fp8_linear(x, q, s, out_dtype=torch.bfloat16)
+    for m in (0, M // 4 - 500, M // 2 - 500, M - 1000):
+        qx = ref.quantise(host(x[m:m + 1000]), 1)[0]
+        want, mag = qx @ qw.T, np.abs(qx) @ np.abs(qw).T
+        got = host(y[m:m + 1000])
+        assert (np.abs(got - want) <= 2.0 ** -12 * mag + 2.0 ** -8 * np.abs(want)).all()
+
+
+def test_fp8_gradients_of_very_many_rows():
+    # 2^24 tiles of 128 rows of dy and x, 256 threads each: 2^32
+    M = 1 << 30
+    dy = torch.zeros(M, 1, device="cuda", dtype=torch.bfloat16)
+    at = [0, 1, 127, 128, M // 2 - 1, M // 2, M // 4 * 3, M - 129, M - 1]
+    dy[at] = torch.arange(1.0, len(at) + 1, device="cuda", dtype=torch.bfloat16)[:, None]
+    x = torch.full((M, 1), 0.5, device="cuda", dtype=torch.bfloat16)
+    total = len(at) * (len(at) + 1) / 2
+    _, _, qt, st = pv.pvconv_fp8_quantize_weight(torch.full((1, 1), 1.5, device="cuda"),
+                                                 transposed=True)
+    # every value here is one of e4m3's, and every sum exact
+    dx, dw, db = pv.pvconv_fp8_linear_backward(dy, x, qt, st)
+    assert dw.item() == 0.5 * total and db.item() == total
+    assert torch.equal(dx, dy * 1.5)
+    del dx
+    db = pv.pvconv_fp8_linear_backward(dy, None, None, None, want_dx=False, want_dw=False)[2]
+    assert db.item() == total
