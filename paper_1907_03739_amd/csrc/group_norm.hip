@@ -616,39 +616,25 @@ __global__ __launch_bounds__(T) void pv_gn_held_kernel(PvNorm n, PvRows x, PvRow
     if (p.active)
 #pragma unroll
         for (int u = 0; u < U; u++)
-            if (p.row + u * p.par < p.n) {
-                // the mean of a vector of bf16 in fp32: values of 8 bits, which it adds
-                // without loss unless they lie 2^13 apart
-                float v = 0.f;
+            if (p.row + u * p.par < p.n)
 #pragma unroll
-                for (int i = 0; i < VEC; i++) {
-                    if (TYPES == kBf16)
-                        v = fmaf(f[u].get(i), 1.f / VEC, v);
-                    else
-                        s += (double)f[u].get(i);
-                }
-                if (TYPES == kBf16) s += (double)v;
-            }
-    if (TYPES == kBf16) s *= VEC;
+                for (int i = 0; i < VEC; i++) s += (double)f[u].get(i);
     const double cnt = (double)p.n * (n.C / n.groups);
     const double mean = cnt > 0. ? group_sum<T>(s, lds) / cnt : 0.;
-    const float m = (float)mean;
-    float q = 0.f;
+    double q = 0.;
     if (p.active)
 #pragma unroll
         for (int u = 0; u < U; u++)
             if (p.row + u * p.par < p.n)
 #pragma unroll
                 for (int i = 0; i < VEC; i++) {
-                    const float d = f[u].get(i) - m;
-                    q = fmaf(d, d, q);
+                    const double d = (double)f[u].get(i) - mean;
+                    q = fma(d, d, q);
                 }
     float2 st = make_float2(0.f, 0.f);
-    if (cnt > 0.) {
-        const double off = mean - (double)m;
-        const double var = group_sum<T>((double)q, lds) / cnt - off * off;
-        st = make_float2(m, (float)(1. / sqrt((var < 0. ? 0. : var) + (double)n.eps)));
-    }
+    if (cnt > 0.)
+        st = make_float2((float)mean,
+                         (float)(1. / sqrt(group_sum<T>(q, lds) / cnt + (double)n.eps)));
     if (stats && threadIdx.x == 0) stats[item] = st;
     if (!p.active) return;
 #pragma unroll

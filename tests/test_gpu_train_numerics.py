@@ -1,0 +1,61 @@
+"""The training and 8-bit operators where few digits or little range are left:
+statistics of far means, huge and tiny spreads, on each of the group norm's forms
+(the first rows of N below are groups that a workgroup holds, the last are summed
+in chunks)."""
+import numpy as np
+import pytest
+import torch
+
+import _train_ref as ref
+from paper_1907_03739_amd import binding as pv
+from _helpers import host
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+TD = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+@pytest.fixture(autouse=True)
+def _gpu_case(request):
+    assert torch.cuda.is_available(), "GPU tests need an MI355X"
+    print(f"\n[gpu case] {request.node.nodeid}", flush=True)
+    yield
+    torch.cuda.synchronize()
+
+
+def put(a, dt="f32"):
+    return torch.as_tensor(np.asarray(a, np.float32)).cuda().to(TD[dt])
+
+
+# 16 channels in 2 groups: vectors of 8 (bf16) or 4; 21 in 3: single elements across
+# groups of 7
+@pytest.mark.parametrize("N", [5, 200, 3000, 20000])
+@pytest.mark.parametrize("C,G", [(16, 2), (21, 3)])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("scale", [2.0 ** 63, 2.0 ** -83])
+def test_group_norm_statistics_keep_their_range(N, C, G, dt, scale):
+    # squares of these are beyond, or below, what 32 bits hold
+    rng = np.random.default_rng(N + C)
+    xt = put(rng.normal(size=(2, N, C)) * scale, dt)
+    x = host(xt)
+    one, zero = put(np.ones(C)), put(np.zeros(C))
+    y, st = pv.pvconv_group_norm_act(xt, G, one, zero, eps=0.0, act="none", want_stats=True,
+                                     out_dtype=torch.float32)
+    ry, rs = ref.group_norm(x, G, np.ones(C), np.zeros(C), 0.0, "none", 0.0)
+    assert (np.abs(host(st)[..., 1] - rs[..., 1]) <= 1e-6 * rs[..., 1]).all()
+    mag = np.abs(x) * np.repeat(rs[..., 1], C // G, 1)[:, None] + 1
+    assert (np.abs(host(y) - ry) <= 16 * U * mag).all()
+
+
+@pytest.mark.parametrize("N", [5, 200, 3000, 20000])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_group_norm_means_of_terms_that_cancel(N, dt):
+    # 2^33 and its negative beside small whole numbers: the mean, of 64-bit sums
+    # that lose nothing here, rounds once
+    rng = np.random.default_rng(N)
+    x = rng.integers(1, 9, (2, N, 16)).astype(np.float64)
+    x[..., 1::8], x[..., 6::8] = 2.0 ** 33, -(2.0 ** 33)
+    st = pv.pvconv_group_norm_act(put(x, dt), 2, put(np.ones(16)), put(np.zeros(16)),
+                                  want_stats=True)[1]
+    rs = ref.group_norm(x, 2, np.ones(16), np.zeros(16), 1e-5, "none", 0.0)[1]
+    assert (np.abs(host(st)[..., 0] - rs[..., 0]) <= 4 * U * np.abs(rs[..., 0])).all()
