@@ -168,9 +168,20 @@ __device__ __forceinline__ void load_params(const PvNorm& n, int c, float (&ga)[
     }
 }
 
-// part[item of (b, slab, chunk)][group in slab] = (sum, sum of squares), in 64
-// bits: the subtraction that makes the variance of them loses nothing that 32
-// bits could hold.
+// The value that a group's sums are about: its first channel of the cloud's first
+// row. Without it, E[x^2] - mean^2 would lose the square of mean / spread, which
+// leaves no digit of the variance where a mean is 2^26 spreads away; about an element
+// of the group both terms are of the spread's size (unless that element lies as far
+// from the others). The difference of two 32-bit values keeps 53 bits.
+template <int TYPES>
+__device__ __forceinline__ double pivot_of(const PvRows& x, int b, const PvNorm& n, int c) {
+    Raw<TYPES, 1> f;
+    f.load(x, (size_t)b * n.N, c);
+    return (double)f.get(0);
+}
+
+// part[item of (b, slab, chunk)][group in slab] = sums of x - pivot and of its
+// square, in 64 bits.
 template <int TYPES, int VEC>
 __global__ __launch_bounds__(kThreads) void pv_gn_sums_kernel(PvNorm n, Deal d, PvRows x,
                                                               double2* part, int per) {
@@ -182,7 +193,8 @@ __global__ __launch_bounds__(kThreads) void pv_gn_sums_kernel(PvNorm n, Deal d, 
         for (int v0 = 0; v0 < vecs; v0 += p.cols) {
             double s = 0., ss = 0.;
             const int c = p.c0 + (v0 + p.col) * VEC;
-            if (v0 + p.col < vecs)
+            if (v0 + p.col < vecs && p.rows0 < rows1) {
+                const double pivot = pivot_of<TYPES>(x, p.b, n, c / d.CG * d.CG);
                 for (int k = p.rows0 + p.row; k < rows1; k += p.par * kRowsAhead) {
                     Raw<TYPES, VEC> f[kRowsAhead];
 #pragma unroll
@@ -194,11 +206,12 @@ __global__ __launch_bounds__(kThreads) void pv_gn_sums_kernel(PvNorm n, Deal d, 
                         if (k + u * p.par < rows1)
 #pragma unroll
                             for (int i = 0; i < VEC; i++) {
-                                const double v = (double)f[u].get(i);
+                                const double v = (double)f[u].get(i) - pivot;
                                 s += v;
                                 ss = fma(v, v, ss);
                             }
                 }
+            }
             __syncthreads();
             red[threadIdx.x] = make_double2(s, ss);
             __syncthreads();
@@ -240,9 +253,12 @@ __global__ __launch_bounds__(kThreads) void pv_gn_mixed_sums_kernel(PvNorm n, De
     for (size_t item = blockIdx.x; item < d.items; item += gridDim.x) {
         const Place<VEC> p(item, d, n.N, n.C, n.lengths);
         const int rows1 = min(p.rows1, p.n), c = p.c0 + p.col * VEC;
-        double s[VEC], ss[VEC];
+        double s[VEC], ss[VEC], pivot[VEC];
 #pragma unroll
-        for (int i = 0; i < VEC; i++) s[i] = ss[i] = 0.;
+        for (int i = 0; i < VEC; i++) {
+            s[i] = ss[i] = 0.;
+            pivot[i] = n.N > 0 ? pivot_of<TYPES>(x, p.b, n, (c + i) / d.CG * d.CG) : 0.;
+        }
         for (int k = p.rows0 + p.row; k < rows1; k += p.par * kRowsAhead) {
             Raw<TYPES, VEC> f[kRowsAhead];
 #pragma unroll
@@ -254,7 +270,7 @@ __global__ __launch_bounds__(kThreads) void pv_gn_mixed_sums_kernel(PvNorm n, De
                 if (k + u * p.par < rows1)
 #pragma unroll
                     for (int i = 0; i < VEC; i++) {
-                        const double v = (double)f[u].get(i);
+                        const double v = (double)f[u].get(i) - pivot[i];
                         s[i] += v;
                         ss[i] = fma(v, v, ss[i]);
                     }
@@ -310,10 +326,11 @@ __device__ __forceinline__ double2 add_chunks(const double2* part, int per, int 
     return make_double2(wave_sum(t), wave_sum(tt));
 }
 
-__device__ __forceinline__ float2 stats_of(double sum, double squares, double count, float eps) {
-    if (count <= 0.) return make_float2(0.f, 0.f);
-    const double mean = sum / count, var = squares / count - mean * mean;
-    return make_float2((float)mean, (float)(1. / sqrt((var < 0. ? 0. : var) + (double)eps)));
+__device__ __forceinline__ float2 stats_of(double sum, double squares, double pivot, double count,
+                                           float eps) {
+    const double off = sum / count, var = squares / count - off * off;
+    return make_float2((float)(pivot + off),
+                       (float)(1. / sqrt((var < 0. ? 0. : var) + (double)eps)));
 }
 
 template <int TYPES, bool SILU, int VEC, bool MIX>
@@ -330,7 +347,10 @@ __global__ __launch_bounds__(kThreads) void pv_gn_apply_kernel(PvNorm n, Deal d,
         for (int g = threadIdx.x >> 6; g < ng; g += kThreads / 64) {
             const double2 t = add_chunks(part, per, d.chunks, item - p.chunk, g);
             if ((threadIdx.x & 63) == 0) {
-                st[g] = stats_of(t.x, t.y, (double)p.n * d.CG, n.eps);
+                st[g] = make_float2(0.f, 0.f);
+                if (p.n > 0)
+                    st[g] = stats_of(t.x, t.y, pivot_of<TYPES>(x, p.b, n, p.c0 + g * d.CG),
+                                     (double)p.n * d.CG, n.eps);
                 if (stats && p.chunk == 0) stats[(size_t)p.b * n.groups + p.c0 / d.CG + g] = st[g];
             }
         }

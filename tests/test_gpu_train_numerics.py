@@ -59,3 +59,26 @@ def test_group_norm_means_of_terms_that_cancel(N, dt):
                                   want_stats=True)[1]
     rs = ref.group_norm(x, 2, np.ones(16), np.zeros(16), 1e-5, "none", 0.0)[1]
     assert (np.abs(host(st)[..., 0] - rs[..., 0]) <= 4 * U * np.abs(rs[..., 0])).all()
+
+
+@pytest.mark.parametrize("N", [5, 200, 3000, 20000])
+@pytest.mark.parametrize("C,G", [(16, 2), (21, 3), (40, 40)])
+@pytest.mark.parametrize("first", [0, 1])
+def test_group_norm_spread_beside_a_very_far_mean(N, C, G, first):
+    # values of 2^22 + 0 .. 7.5: E[x^2] - mean^2 in 64 bits has 9 binary digits left.
+    # first = 1: an empty cloud, and rows past a cloud's length that are NaN, beside it
+    rng = np.random.default_rng(N)
+    x = 2.0 ** 22 + rng.integers(0, 16, (2, N, C)) / 2
+    lengths, xt = None, put(x)
+    if first:
+        lengths = [0, N - N // 3]
+        xt[0], xt[1, lengths[1]:] = float("nan"), float("nan")
+    lt = None if lengths is None else torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    y, st = pv.pvconv_group_norm_act(xt, G, put(np.ones(C)), put(np.zeros(C)), lengths=lt,
+                                     want_stats=True)
+    rs = ref.group_norm(x, G, np.ones(C), np.zeros(C), 1e-5, "none", 0.0, lengths)[1]
+    assert (np.abs(host(st)[..., 0] - rs[..., 0]) <= 4 * U * np.abs(rs[..., 0])).all()
+    assert (np.abs(host(st)[..., 1] - rs[..., 1]) <= 1e-6 * rs[..., 1]).all()
+    if first:
+        assert (y[0] == 0).all() and (y[1, lengths[1]:] == 0).all()
+    assert torch.isfinite(y).all()
