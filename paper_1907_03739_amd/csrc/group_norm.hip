@@ -847,19 +847,46 @@ void with_kind(int types, bool silu, int vec, F f) {
     }
 }
 
-// Whether a group fits the registers of a workgroup, and of which: vectors a
+// Whether a group is held in the registers of a workgroup, and of which: vectors a
 // thread of 256 (kSmallU) or of 1024 (kLargeU, kLargeBwdU: a gradient holds x and
-// dy). One (cloud, group) a workgroup, as many as a launch of fewer than 2^32
-// threads holds.
+// dy), one (cloud, group) a workgroup. Where it fits, it is held unless the two
+// launches are faster (us, held / two launches, bf16 but where noted):
+// - Forward, 256 threads: workgroups for more than one round of the chip that are
+//   less than half full, several to an item of the two launches (16384 x 1 x 128, 8
+//   groups: 237 / 87; 4096 x 16 x 128, 8 groups: 64 / 34; but 256 x 64 x 128, 8
+//   groups: 7.9 / 9.4, and 65536 x 3 x 64 in one group, fp32: 117 / 210).
+// - Forward, 1024 threads: more than two workgroups a CU (256 x 512 x 128, 8
+//   groups: 49 / 28), or few of them with much to read each (1 x 8192 x 64, 8 groups:
+//   17.0 / 9.6; but 1 x 4096 x 128, 32 groups: 10.5 / 16.9).
+// - Gradient: a workgroup adds its channels' sums one after another, so groups of
+//   more than 32 channels (64 x 3 x 512, 8 groups, fp32: 15 / 8), many workgroups
+//   (16384 x 1 x 128, 8 groups: 1020 / 176; of 1024 threads, 256 x 512 x 128, 8
+//   groups: 68 / 41), unless they are full (64 x 256 x 256, 32 groups, fp32: 19 / 28);
+//   and few with much to read each (4 x 2048 x 128, 8 groups: 15.6 / 12.2; 32 clouds:
+//   21 / 27).
 constexpr int kSmallT = 256, kSmallU = 2, kLargeT = 1024, kLargeU = 8, kLargeBwdU = 4;
+constexpr int kHeldChannels = 32;  // of a group whose gradient is held
 enum Hold { kNot, kSmall, kLarge };
-Hold hold_of(const PvNorm& n, int vec, int large_u) {
+Hold hold_of(const PvNorm& n, const Deal& d, int vec, bool gradient) {
     if (n.N < 1) return kNot;
-    const size_t items = ((size_t)n.B * n.groups + 7) / 8 * 8;
-    auto launches = [&](int threads) { return items * threads <= 0xffffffffu; };
-    const int cols = n.C / n.groups / vec;
-    if (cols <= kSmallT && n.N <= kSmallT / cols * kSmallU) return launches(kSmallT) ? kSmall : kNot;
-    if (cols <= kLargeT && n.N <= kLargeT / cols * large_u) return launches(kLargeT) ? kLarge : kNot;
+    const size_t groups = (size_t)n.B * n.groups;  // workgroups
+    const int cols = d.CG / vec;
+    if (cols <= kSmallT && n.N <= kSmallT / cols * kSmallU) {
+        const int vectors = n.N * cols;
+        const bool held =
+            gradient ? (d.CG <= kHeldChannels && groups <= 2048 && groups * d.CG <= 8192) ||
+                           (d.CG <= 8 && vec >= 4 && vectors >= kSmallT * 3 / 2)
+                     : groups <= 4096 || vectors >= kSmallT || groups <= 3 * d.items;
+        // HIP takes fewer than 2^32 threads a launch
+        return held && (groups + 7) / 8 * 8 * kSmallT <= 0xffffffffu ? kSmall : kNot;
+    }
+    if (cols <= kLargeT && n.N <= kLargeT / cols * (gradient ? kLargeBwdU : kLargeU)) {
+        const int values = n.N * d.CG;
+        const bool held = groups <= 512 &&
+                          (gradient ? d.CG <= kHeldChannels && (values <= 16384 || groups >= 192)
+                                    : values <= 32768 || groups >= 96);
+        return held ? kLarge : kNot;
+    }
     return kNot;
 }
 
@@ -888,7 +915,7 @@ pvconv_status pv_launch_group_norm(const PvNorm& n, const PvRows& x, const PvRow
     const float neg = negative_slope(n);
     const int types = types_of(all, 2), own = width_for(d.CG, all, 2);
     const bool silu = n.act == PVCONV_ACT_SILU;
-    const Hold hold = hold_of(n, own, kLargeU);
+    const Hold hold = hold_of(n, d, own, false);
     if (hold != kNot) {
         with_kind(types, silu, own, [&](auto T, auto S, auto V) {
             constexpr int TYPES = decltype(T)::value, VEC = decltype(V)::value;
@@ -939,7 +966,7 @@ pvconv_status pv_launch_group_norm_bwd(const PvNorm& norm, const PvRows& dy, con
     const float neg = negative_slope(n);
     const int types = types_of(all, 3), own = width_for(d.CG, all, 3);
     const bool silu = n.act == PVCONV_ACT_SILU;
-    const Hold hold = n.B ? hold_of(n, own, kLargeBwdU) : kNot;
+    const Hold hold = n.B ? hold_of(n, d, own, true) : kNot;
     const float2* st = (const float2*)stats;
     if (hold != kNot) {
         float2* sums = n.B > 1 ? (float2*)ws : nullptr;

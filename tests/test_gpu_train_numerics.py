@@ -82,3 +82,21 @@ def test_group_norm_spread_beside_a_very_far_mean(N, C, G, first):
     if first:
         assert (y[0] == 0).all() and (y[1, lengths[1]:] == 0).all()
     assert torch.isfinite(y).all()
+
+
+# both sides of each rule that chooses between a group in a workgroup's registers and
+# the sums in chunks, forward or gradient
+@pytest.mark.parametrize("B,N,C,G,dt,lengths", [
+    (512, 1, 128, 8, "bf16", None), (513, 1, 128, 8, "bf16", None),   # 4096 groups
+    (4096, 3, 64, 2, "f32", None),
+    (64, 3, 128, 8, "bf16", None), (65, 3, 128, 8, "bf16", None),     # 8192 channels
+    (2, 5, 264, 8, "f32", None), (2, 5, 256, 8, "f32", None),         # 33 and 32 a group
+    (64, 256, 256, 32, "f32", None), (65, 191, 256, 32, "f32", None),  # full workgroups
+    (64, 512, 128, 8, "bf16", None), (65, 512, 128, 8, "bf16", None),  # 512 groups
+    (11, 4096, 64, 8, "bf16", None), (1, 4097, 64, 8, "bf16", [4000]),  # 32768 values a group
+    (12, 2048, 128, 8, "bf16", None), (24, 2048, 128, 8, "bf16", None),
+    (23, 2048, 128, 8, "bf16", None), (2, 1024, 128, 8, "bf16", [1024, 3]),
+])
+def test_group_norm_on_both_sides_of_its_rules(B, N, C, G, dt, lengths):
+    import test_gpu_train_ops as ops
+    ops.test_group_norm_forward_and_gradients(B, N, C, G, dt, dt, "silu", lengths, 0, 0)
