@@ -93,13 +93,13 @@ enum Types { kBf16, kF32, kMixed };
 template <int TYPES, int VEC>
 struct Raw {
     static constexpr int kWords = TYPES == kBf16 ? (VEC + 1) / 2 : VEC;
+    static constexpr bool kStreams = TYPES != kMixed && kWords == 4;
     uint32_t w[kWords];
-    // ONCE: past the caches' normal order, for the two launches, whose reads of a
-    // line lie far apart (16 x 32768 x 128 bf16, forward and backward: 218 -> 209 us)
+    // ONCE: past the caches' normal order (streams() has the rule)
     template <bool ONCE = false>
     __device__ __forceinline__ void load(const PvRows& x, size_t row, int c) {
         const size_t at = row * x.ld + c;
-        if constexpr (ONCE && TYPES != kMixed && kWords == 4) {
+        if constexpr (ONCE && kStreams) {
             typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
             const u32x4 v = __builtin_nontemporal_load(
                 (const u32x4*)((const char*)x.p + at * (TYPES == kBf16 ? 2 : 4)));
@@ -182,7 +182,7 @@ __device__ __forceinline__ double pivot_of(const PvRows& x, int b, const PvNorm&
 
 // part[item of (b, slab, chunk)][group in slab] = sums of x - pivot and of its
 // square, in 64 bits.
-template <int TYPES, int VEC>
+template <int TYPES, int VEC, bool ONCE>
 __global__ __launch_bounds__(kThreads) void pv_gn_sums_kernel(PvNorm n, Deal d, PvRows x,
                                                               double2* part, int per) {
     __shared__ double2 red[kThreads];
@@ -199,7 +199,7 @@ __global__ __launch_bounds__(kThreads) void pv_gn_sums_kernel(PvNorm n, Deal d, 
                     Raw<TYPES, VEC> f[kRowsAhead];
 #pragma unroll
                     for (int u = 0; u < kRowsAhead; u++)
-                        f[u].template load<true>(
+                        f[u].template load<ONCE>(
                             x, (size_t)p.b * n.N + min(k + u * p.par, rows1 - 1), c);
 #pragma unroll
                     for (int u = 0; u < kRowsAhead; u++)
@@ -245,7 +245,7 @@ __global__ __launch_bounds__(kThreads) void pv_gn_sums_kernel(PvNorm n, Deal d, 
 
 // The same where groups are no whole vectors (MIX in the kernels below): sums a
 // channel, then a group. The slab is one run of vectors.
-template <int TYPES, int VEC>
+template <int TYPES, int VEC, bool ONCE>
 __global__ __launch_bounds__(kThreads) void pv_gn_mixed_sums_kernel(PvNorm n, Deal d, PvRows x,
                                                                     double2* part, int per) {
     __shared__ double2 red[kThreads * VEC];
@@ -263,7 +263,7 @@ __global__ __launch_bounds__(kThreads) void pv_gn_mixed_sums_kernel(PvNorm n, De
             Raw<TYPES, VEC> f[kRowsAhead];
 #pragma unroll
             for (int u = 0; u < kRowsAhead; u++)
-                f[u].template load<true>(
+                f[u].template load<ONCE>(
                     x, (size_t)p.b * n.N + min(k + u * p.par, rows1 - 1), c);
 #pragma unroll
             for (int u = 0; u < kRowsAhead; u++)
@@ -333,7 +333,7 @@ __device__ __forceinline__ float2 stats_of(double sum, double squares, double pi
                        (float)(1. / sqrt((var < 0. ? 0. : var) + (double)eps)));
 }
 
-template <int TYPES, bool SILU, int VEC, bool MIX>
+template <int TYPES, bool SILU, int VEC, bool MIX, bool ONCE>
 __global__ __launch_bounds__(kThreads) void pv_gn_apply_kernel(PvNorm n, Deal d, PvRows x,
                                                                PvRows y, float neg,
                                                                const double2* part, int per,
@@ -364,7 +364,7 @@ __global__ __launch_bounds__(kThreads) void pv_gn_apply_kernel(PvNorm n, Deal d,
                 Raw<TYPES, VEC> f[kRowsAhead];
 #pragma unroll
                 for (int u = 0; u < kRowsAhead; u++)
-                    f[u].template load<true>(
+                    f[u].template load<ONCE>(
                         x, (size_t)p.b * n.N + max(min(k + u * p.par, last), 0), c);
 #pragma unroll
                 for (int u = 0; u < kRowsAhead; u++) {
@@ -388,7 +388,7 @@ __global__ __launch_bounds__(kThreads) void pv_gn_apply_kernel(PvNorm n, Deal d,
 // chan[b * chunks + chunk][c] = (sum dv xh, sum dv) over the chunk's rows, and
 // part[item][group in slab] = their sums over the group's channels, times
 // gamma: (sum gamma dv, sum gamma dv xh).
-template <int TYPES, bool SILU, int VEC, bool MIX>
+template <int TYPES, bool SILU, int VEC, bool MIX, bool ONCE>
 __global__ __launch_bounds__(kThreads) void pv_gn_bwd_sums_kernel(PvNorm n, Deal d, PvRows dy,
                                                                   PvRows x, float neg,
                                                                   const float2* stats,
@@ -413,8 +413,8 @@ __global__ __launch_bounds__(kThreads) void pv_gn_bwd_sums_kernel(PvNorm n, Deal
 #pragma unroll
                     for (int u = 0; u < kRowsAhead; u++) {
                         const size_t row = (size_t)p.b * n.N + min(k + u * p.par, rows1 - 1);
-                        f[u].template load<true>(x, row, c);
-                        g[u].template load<true>(dy, row, c);
+                        f[u].template load<ONCE>(x, row, c);
+                        g[u].template load<ONCE>(dy, row, c);
                     }
 #pragma unroll
                     for (int u = 0; u < kRowsAhead; u++) {
@@ -498,7 +498,7 @@ __device__ __forceinline__ void add_params(size_t rows, int C, const float2* cha
     }
 }
 
-template <int TYPES, bool SILU, int VEC, bool MIX>
+template <int TYPES, bool SILU, int VEC, bool MIX, bool ONCE>
 __global__ __launch_bounds__(kThreads) void pv_gn_bwd_apply_kernel(
     PvNorm n, Deal d, PvRows dy, PvRows x, PvRows dx, float neg, const float2* stats,
     const float2* chan, const double2* part, int per, float* dgamma, float* dbeta, unsigned params) {
@@ -531,8 +531,8 @@ __global__ __launch_bounds__(kThreads) void pv_gn_bwd_apply_kernel(
 #pragma unroll
                 for (int u = 0; u < kRowsAhead; u++) {
                     const size_t row = (size_t)p.b * n.N + max(min(k + u * p.par, last), 0);
-                    f[u].template load<true>(x, row, c);
-                    g[u].template load<true>(dy, row, c);
+                    f[u].template load<ONCE>(x, row, c);
+                    g[u].template load<ONCE>(dy, row, c);
                 }
 #pragma unroll
                 for (int u = 0; u < kRowsAhead; u++) {
@@ -847,6 +847,30 @@ void with_kind(int types, bool silu, int vec, F f) {
     }
 }
 
+// Whether the two launches, whose reads of a line lie far apart, read past the
+// caches' normal order: where what both read is more than the Infinity Cache holds
+// (us, streaming / not: 32 x 32768 x 128 bf16 134 / 164, gradient 247 / 283, 16 of them
+// 129 / 139; but their forward, 134 MB of x, 74 / 69, 12 x 23929 x 96 fp32, 16 groups,
+// 72 / 65, gradient 118 / 109, 1 x 61059 x 96 fp32, 32 groups, 38 / 31, gradient 61 / 49).
+constexpr size_t kInfinityCache = (size_t)256 << 20;
+bool streams(const PvNorm& n, const PvRows* read, int count) {
+    size_t bytes = 0;
+    for (int i = 0; i < count; i++)
+        bytes += (size_t)n.B * n.N * n.C * (read[i].bf16 ? 2 : 4);
+    return bytes >= kInfinityCache;
+}
+// f with whether to stream as a constant, for vectors that can
+template <int TYPES, int VEC, typename F>
+void with_stream(bool once, F f) {
+    if constexpr (Raw<TYPES, VEC>::kStreams) {
+        if (once) {
+            f(std::true_type());
+            return;
+        }
+    }
+    f(std::false_type());
+}
+
 // Whether a group is held in the registers of a workgroup, and of which: vectors a
 // thread of 256 (kSmallU) or of 1024 (kLargeU, kLargeBwdU: a gradient holds x and
 // dy), one (cloud, group) a workgroup. Where it fits, it is held unless the two
@@ -931,21 +955,26 @@ pvconv_status pv_launch_group_norm(const PvNorm& n, const PvRows& x, const PvRow
         return pv_launch_status();
     }
     const Width w = width_of_rows(d, n.C, all, 2);
+    const bool once = streams(n, all, 1);
     with_kind(types, silu, w.vec, [&](auto T, auto S, auto V) {
         constexpr int TYPES = decltype(T)::value, VEC = decltype(V)::value;
         constexpr bool SILU = decltype(S)::value;
         const unsigned grid = grid_of(d.items);
         const size_t lds = per * sizeof(float2);
         double2* part = (double2*)ws;
-        if (w.mix) {
-            pv_gn_mixed_sums_kernel<TYPES, VEC><<<grid, kThreads, 0, s>>>(n, d, x, part, per);
-            pv_gn_apply_kernel<TYPES, SILU, VEC, true>
-                <<<grid, kThreads, lds, s>>>(n, d, x, y, neg, part, per, (float2*)stats);
-        } else {
-            pv_gn_sums_kernel<TYPES, VEC><<<grid, kThreads, 0, s>>>(n, d, x, part, per);
-            pv_gn_apply_kernel<TYPES, SILU, VEC, false>
-                <<<grid, kThreads, lds, s>>>(n, d, x, y, neg, part, per, (float2*)stats);
-        }
+        with_stream<TYPES, VEC>(once, [&](auto O) {
+            constexpr bool ONCE = decltype(O)::value;
+            if (w.mix) {
+                pv_gn_mixed_sums_kernel<TYPES, VEC, ONCE>
+                    <<<grid, kThreads, 0, s>>>(n, d, x, part, per);
+                pv_gn_apply_kernel<TYPES, SILU, VEC, true, ONCE>
+                    <<<grid, kThreads, lds, s>>>(n, d, x, y, neg, part, per, (float2*)stats);
+            } else {
+                pv_gn_sums_kernel<TYPES, VEC, ONCE><<<grid, kThreads, 0, s>>>(n, d, x, part, per);
+                pv_gn_apply_kernel<TYPES, SILU, VEC, false, ONCE>
+                    <<<grid, kThreads, lds, s>>>(n, d, x, y, neg, part, per, (float2*)stats);
+            }
+        });
     });
     return pv_launch_status();
 }
@@ -988,21 +1017,25 @@ pvconv_status pv_launch_group_norm_bwd(const PvNorm& norm, const PvRows& dy, con
         return pv_launch_status();
     }
     const Width w = width_of_rows(d, n.C, all, 3);
+    const bool once = streams(n, all, 2);
     with_kind(types, silu, w.vec, [&](auto T, auto S, auto V) {
         constexpr int TYPES = decltype(T)::value, VEC = decltype(V)::value;
         constexpr bool SILU = decltype(S)::value;
-        auto go = [&](auto MIX) {
+        auto go = [&](auto M, auto O) {
+            constexpr bool MIX = decltype(M)::value, ONCE = decltype(O)::value;
             if (d.items)
-                pv_gn_bwd_sums_kernel<TYPES, SILU, VEC, decltype(MIX)::value>
+                pv_gn_bwd_sums_kernel<TYPES, SILU, VEC, MIX, ONCE>
                     <<<grid_of(d.items), kThreads, 0, s>>>(n, d, dy, x, neg, st, chan, part, per);
-            pv_gn_bwd_apply_kernel<TYPES, SILU, VEC, decltype(MIX)::value>
+            pv_gn_bwd_apply_kernel<TYPES, SILU, VEC, MIX, ONCE>
                 <<<grid_of(d.items) + params, kThreads, per * sizeof(float2), s>>>(
                     n, d, dy, x, dx, neg, st, chan, part, per, dgamma, dbeta, params);
         };
-        if (w.mix)
-            go(std::true_type());
-        else
-            go(std::false_type());
+        with_stream<TYPES, VEC>(once, [&](auto O) {
+            if (w.mix)
+                go(std::true_type(), O);
+            else
+                go(std::false_type(), O);
+        });
     });
     return pv_launch_status();
 }

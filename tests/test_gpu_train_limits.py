@@ -105,3 +105,36 @@ def test_fp8_gradients_of_very_many_rows():
     del dx
     db = pv.pvconv_fp8_linear_backward(dy, None, None, None, want_dx=False, want_dw=False)[2]
     assert db.item() == total
+
+
+# x (and dy) of 256 MiB and more, which are read past the caches' order: every cloud as
+# it comes out alone, where they are not, in fp32
+@pytest.mark.parametrize("B,N,C,G,dt", [(40, 32768, 128, 8, torch.bfloat16),
+                                        (12, 65536, 96, 32, torch.float32)])
+def test_group_norm_of_more_than_the_caches_hold(B, N, C, G, dt):
+    x, dy = randn(B, N, C, seed=5, dtype=dt), randn(B, N, C, seed=6, dtype=dt)
+    assert x.numel() * x.element_size() >= 1 << 28
+    ga, be = 1 + 0.1 * randn(C, seed=7, dtype=torch.float32), 0.5 * randn(C, seed=8, dtype=torch.float32)
+    y, st = pv.pvconv_group_norm_act(x, G, ga, be, want_stats=True)
+    dx, dg, db = pv.pvconv_group_norm_act_backward(dy, x, st, G, ga, be)
+    f32 = torch.float32
+    step = 2.0 ** -8 if dt == torch.bfloat16 else 0.0
+    sums, sizes = torch.zeros(2, C, dtype=torch.float64, device="cuda"), torch.zeros(2, C, device="cuda")
+    for b in range(B):
+        xb, db_ = x[b:b + 1], dy[b:b + 1]
+        y1, st1 = pv.pvconv_group_norm_act(xb, G, ga, be, want_stats=True, out_dtype=f32)
+        # one rounding of 64-bit sums whose order may differ
+        assert torch.allclose(st1, st[b:b + 1], rtol=4 * U, atol=4 * U)
+        dx1, dg1, db1 = pv.pvconv_group_norm_act_backward(db_, xb, st1, G, ga, be, out_dtype=f32)
+        mean, r = (st1[0, :, i].repeat_interleave(C // G) for i in (0, 1))
+        xs = xb[0].float().abs()
+        mag = (xs + mean.abs()) * r * ga.abs() + be.abs()
+        # each side is within the bounds that the tests against the oracle hold it to
+        assert ((y1 - y[b]).float().abs() <= 32 * U * mag + step * y1.float().abs()).all()
+        size = r * (ga * db_[0].float()).abs() * 1.1
+        floor = 128 * U * (size + size.max() * (1 + (xs + mean.abs()) * r))
+        assert ((dx1 - dx[b]).float().abs() <= floor + step * dx1.float().abs()).all()
+        sums += torch.stack([dg1, db1]).double()
+        dv = db_[0].float().abs() * 1.1
+        sizes += torch.stack([(dv * (xs + mean.abs()) * r).sum(0), dv.sum(0)])
+    assert ((sums - torch.stack([dg, db])).abs() <= 128 * U * sizes).all()
