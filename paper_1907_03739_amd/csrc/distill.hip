@@ -246,8 +246,8 @@ struct RowSpan {
         vecs = (V - head) / Vec<BF16>::N;
         tail = V - head - vecs * Vec<BF16>::N;
     }
-    // OWN: the boundaries are the row's own. ONCE: nothing reads it again soon, so
-    // it goes past the caches' normal order (124 -> 104 us over 410 MB).
+    // OWN: the boundaries are the row's own. ONCE: past the caches' normal order
+    // (streams() has the rule).
     template <bool OWN, bool ONCE = false>
     __device__ __forceinline__ Vec<BF16> vec(int i) const {
         const char* q = p + head * (BF16 ? 2 : 4) + (size_t)i * 16;
@@ -298,7 +298,7 @@ __device__ __forceinline__ float group_reduce(float v, Op op, float* lds) {
     return v;
 }
 
-template <int T, bool BF16, bool STATS, bool GRAD>
+template <int T, bool BF16, bool STATS, bool GRAD, bool ONCE>
 __global__ __launch_bounds__(T) void pv_distill_long_kernel(Args a) {
     __shared__ float lds[T / 64];
     __shared__ float ep[PVCONV_MAX_TOP];  // exp of the entries
@@ -322,7 +322,7 @@ __global__ __launch_bounds__(T) void pv_distill_long_kernel(Args a) {
             for (int i = t; i < r.vecs; i += T * kAhead) {
                 Vec<BF16> v[kAhead];
 #pragma unroll
-                for (int u = 0; u < kAhead; u++) v[u] = r.template vec<true, !GRAD>(min(i + u * T, r.vecs - 1));
+                for (int u = 0; u < kAhead; u++) v[u] = r.template vec<true, ONCE>(min(i + u * T, r.vecs - 1));
                 float m = -INFINITY;
 #pragma unroll
                 for (int u = 0; u < kAhead; u++)
@@ -468,6 +468,14 @@ void with_bool(bool b, F f) {
 template <int N>
 using Int = std::integral_constant<int, N>;
 
+// Whether a loss alone reads z past the caches' normal order: where z is more than
+// the Infinity Cache holds, so that neither what wrote it nor the gradient that
+// follows shares it (us, streaming / not: 4096 x 49999 bf16, 410 MB, 93 / 95; 2048 rows
+// of them 50 / 45, 8192 x 5000, 82 MB, 36 / 31, with the gradient's call 73 / 66).
+bool streams(const PvDistill& d) {
+    return (size_t)d.M * d.V * (d.z.bf16 ? 2 : 4) >= (size_t)256 << 20;
+}
+
 template <bool STATS, bool GRAD>
 pvconv_status launch(const Args& a, hipStream_t s) {
     const size_t M = a.d.M;
@@ -475,12 +483,26 @@ pvconv_status launch(const Args& a, hipStream_t s) {
     with_bool(a.d.z.bf16, [&](auto B) {
         constexpr bool BF16 = decltype(B)::value;
         if (a.d.V >= kLongV) {
+            auto wide = [&](auto T, auto O) {
+                constexpr int THREADS = decltype(T)::value;
+                pv_distill_long_kernel<THREADS, BF16, STATS, GRAD, decltype(O)::value>
+                    <<<grid(M), THREADS, 0, s>>>(a);
+            };
+            auto rows = [&](auto T) {
+                if constexpr (STATS && !GRAD) {
+                    if (streams(a.d)) {
+                        wide(T, std::true_type());
+                        return;
+                    }
+                }
+                wide(T, std::false_type());
+            };
             if (M <= kFewRows && a.d.V >= kWideV)
-                pv_distill_long_kernel<1024, BF16, STATS, GRAD><<<grid(M), 1024, 0, s>>>(a);
+                rows(Int<1024>());
             else if (a.d.V < kMidV && a.d.top < 256)  // (a thread an entry and one for the label)
-                pv_distill_long_kernel<256, BF16, STATS, GRAD><<<grid(M), 256, 0, s>>>(a);
+                rows(Int<256>());
             else
-                pv_distill_long_kernel<512, BF16, STATS, GRAD><<<grid(M), 512, 0, s>>>(a);
+                rows(Int<512>());
         } else {
             auto rows = [&](auto T, auto E) {
                 constexpr int TEAM = decltype(T)::value;

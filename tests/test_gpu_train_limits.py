@@ -138,3 +138,20 @@ def test_group_norm_of_more_than_the_caches_hold(B, N, C, G, dt):
         dv = db_[0].float().abs() * 1.1
         sizes += torch.stack([(dv * (xs + mean.abs()) * r).sum(0), dv.sum(0)])
     assert ((sums - torch.stack([dg, db])).abs() <= 128 * U * sizes).all()
+
+
+def test_distill_of_more_logits_than_the_caches_hold():
+    # 256 MiB and more, which the loss alone reads past the caches' order: the loss that
+    # comes with a gradient reads them in order
+    M, V, top = 2700, 50001, 8
+    z = randn(M, V, seed=9, scale=3.0)
+    assert z.numel() * 2 >= 1 << 28
+    tv, tc = torch.topk(z.float(), top)
+    kw = dict(labels=tc[:, 3].int().contiguous(), temperature=2.0, alpha=0.5)
+    loss, lse = pv.pvconv_distill_topk(z, tv, tc.int(), **kw)
+    loss2, lse2, _ = pv.pvconv_distill_topk(z, tv, tc.int(), want_grad=True, **kw)
+    assert torch.equal(loss, loss2) and torch.equal(lse, lse2)
+    for m in (0, M // 2, M - 1):
+        want = ref.distill(host(z[m:m + 1]), host(tv[m:m + 1]), tc[m:m + 1].cpu().numpy(),
+                           kw["labels"][m:m + 1].cpu().numpy(), 2.0, 0.5)[0][0]
+        assert abs(loss[m].item() - want) <= 1e-5 * (1 + 4 * 4 + abs(want))
