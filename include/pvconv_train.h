@@ -133,14 +133,21 @@ pvconv_status pvconv_fp8_linear_backward(const void* dy, pvconv_dtype dy_dt, int
 /* present values -inf), the second for a label outside [0, V) or labels     */
 /* NULL; both 0, and no gradient, for a row whose logits are all -inf. An    */
 /* entry with p_j = 0 adds nothing; entries of one class add up. A NaN or    */
-/* +inf logit makes the terms of its row NaN.                                */
+/* +inf logit makes the terms of its row NaN. Where alpha > 0, z / T is      */
+/* taken in 32 bits: at T < 1 a logit may be infinite over T, and counts as  */
+/* that.                                                                     */
 /*  z        [M][V] (z_dt), row stride z_ld                                  */
 /*  t_val    [M][top] fp32, t_class [M][top] int32, contiguous               */
-/*  labels   [M] int32 or NULL;  temperature > 0;  0 <= alpha <= 1           */
+/*  labels   [M] int32 or NULL;  temperature > 0, it and its inverse finite  */
+/*           in 32 bits;  0 <= alpha <= 1                                    */
 /*  loss     out [M] fp32                                                    */
 /*  lse      out [M][2] fp32 or NULL: logsumexp(z), logsumexp(z / T), 0 in   */
 /*           the place of one whose term has no weight (labels NULL or       */
 /*           alpha = 1; alpha = 0)                                           */
+/*           Loss and gradient are of these 32-bit values and carry their    */
+/*           rounding: q of a row whose maximum is of size 2^k is good to    */
+/*           2^(k-24). Rows masked whole by a type's lowest value have no    */
+/*           digit left; mask them by -inf, or give them the weight 0.       */
 /*  dz       out [M][V] (dz_dt), row stride dz_ld, or NULL: row_weight[m]    */
 /*           (1 if NULL) times d loss_m / d z. A row of weight 0 is 0.       */
 /* 1 <= V <= PVCONV_MAX_CLASSES, 1 <= top <= PVCONV_MAX_TOP, M <= 2^30.      */

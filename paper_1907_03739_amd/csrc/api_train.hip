@@ -40,7 +40,8 @@ pvconv_status check_distill(const void* z, pvconv_dtype z_dt, int& z_ld, int M, 
     if (M < 0 || M > (1 << 30) || V < 1 || V > PVCONV_MAX_CLASSES || top < 1 ||
         top > PVCONV_MAX_TOP || !dtype_ok(z_dt))
         return PVCONV_EINVAL;
-    if (!(temperature > 0.f) || isinf(temperature) || !(alpha >= 0.f && alpha <= 1.f))
+    if (!(temperature > 0.f) || isinf(temperature) || isinf(1.f / temperature) ||
+        !(alpha >= 0.f && alpha <= 1.f))
         return PVCONV_EINVAL;
     if (z_ld == 0) z_ld = V;
     if (z_ld < V) return PVCONV_EINVAL;

@@ -50,6 +50,12 @@ struct Args {
     PvRows dz;
 };
 
+// Whether a row has no logit left: its maximum is -inf, or is -inf over T, as the
+// saved lse of the row then is too. A NaN stays one.
+__device__ __forceinline__ bool is_empty(float m, float s1, float st, const Args& a) {
+    return (m == -INFINITY || (a.soft && m * a.tau == -INFINITY)) && !(s1 != s1) && !(st != st);
+}
+
 // The gradient of a logit before the entries of its class. The branches are the
 // call's, not the row's: a row that lacks a term weighs it 0, and its
 // exponential is finite.
@@ -91,17 +97,18 @@ __global__ __launch_bounds__(kThreads) void pv_distill_short_kernel(Args a) {
         Terms w{0.f, 0.f, d.labels ? d.labels[row] : -1};
         if (a.hard && !bad_class(w.label, d.V)) w.ce = 1.f - d.alpha;
 
-        // the teacher's entries at temperature T: maximum and sum
+        // the teacher's entries: maximum, and sum at temperature T (of differences: an
+        // entry over T may be beyond 32 bits)
         float tmax = -INFINITY, tsum = 0.f;
         if (a.soft) {
             for (int j = lane; j < d.top; j += TEAM)
                 if (!bad_class(d.t_class[row * d.top + j], d.V))
-                    tmax = fmaxf(tmax, d.t_val[row * d.top + j] * a.tau);
+                    tmax = fmaxf(tmax, d.t_val[row * d.top + j]);
             tmax = lanes_reduce<TEAM>(tmax, Max());
             if (tmax == -INFINITY) tmax = 0.f;
             for (int j = lane; j < d.top; j += TEAM)
                 if (!bad_class(d.t_class[row * d.top + j], d.V))
-                    tsum += __expf(d.t_val[row * d.top + j] * a.tau - tmax);
+                    tsum += __expf((d.t_val[row * d.top + j] - tmax) * a.tau);
             tsum = lanes_reduce<TEAM>(tsum, Add());
             // 0 only without an entry of weight; a NaN stays
             if (!(tsum == 0.f)) w.kl = d.alpha * d.temperature;
@@ -123,7 +130,7 @@ __global__ __launch_bounds__(kThreads) void pv_distill_short_kernel(Args a) {
             }
             if (a.hard) s1 = lanes_reduce<TEAM>(s1, Add());
             if (a.soft) st = lanes_reduce<TEAM>(st, Add());
-            empty = m == -INFINITY && !(s1 != s1) && !(st != st);
+            empty = is_empty(m, s1, st, a);
             lse1 = a.hard ? m + log_of(s1) : 0.f;
             lset = a.soft ? m * a.tau + log_of(st) : 0.f;
         } else {
@@ -170,7 +177,7 @@ __global__ __launch_bounds__(kThreads) void pv_distill_short_kernel(Args a) {
                                       : (j == entries && w.ce != 0.f ? w.label : -1);
             const bool have = !bad_class(c, d.V);
             const float zc = have ? pv_load_one(d.z.p, BF16, row * d.z.ld + c) : 0.f;
-            const float u = have && j < entries ? d.t_val[row * d.top + j] * a.tau - tmax : 0.f;
+            const float u = have && j < entries ? (d.t_val[row * d.top + j] - tmax) * a.tau : 0.f;
             float p = have && j < entries ? __expf(u) * tinv : 0.f;
             if (STATS && have && j < entries && !empty && !(p == 0.f))
                 kl += p * (u - log_of(tsum) - fmaf(zc, a.tau, -lset));
@@ -180,7 +187,7 @@ __global__ __launch_bounds__(kThreads) void pv_distill_short_kernel(Args a) {
                     p = 0.f;
                     for (int i = 0; i < entries; i++)
                         if (d.t_class[row * d.top + i] == c)
-                            p += __expf(d.t_val[row * d.top + i] * a.tau - tmax);
+                            p += __expf((d.t_val[row * d.top + i] - tmax) * a.tau);
                     p *= tinv;
                 } else if (j == entries && entries) {
                     // the label's class, unless an entry of that class writes it
@@ -313,7 +320,7 @@ __global__ __launch_bounds__(T) void pv_distill_long_kernel(Args a) {
         // a thread an entry (T >= PVCONV_MAX_TOP)
         const bool mine = a.soft && t < d.top && !bad_class(d.t_class[row * d.top + t], d.V);
         const int c_mine = mine ? d.t_class[row * d.top + t] : -1;
-        const float v_mine = mine ? d.t_val[row * d.top + t] * a.tau : -INFINITY;
+        const float v_mine = mine ? d.t_val[row * d.top + t] : -INFINITY;
 
         float lse1 = 0.f, lset = 0.f;
         bool empty;
@@ -346,7 +353,7 @@ __global__ __launch_bounds__(T) void pv_distill_long_kernel(Args a) {
             const float e = s.m == -INFINITY ? -INFINITY : s.m - m;
             const float s1 = a.hard ? group_reduce<T>(s.s1 * __expf(e), Add(), lds) : 0.f;
             const float st = a.soft ? group_reduce<T>(s.st * __expf(e * a.tau), Add(), lds) : 0.f;
-            empty = m == -INFINITY && !(s1 != s1) && !(st != st);
+            empty = is_empty(m, s1, st, a);
             if (a.hard) lse1 = m + log_of(s1);
             if (a.soft) lset = m * a.tau + log_of(st);
         } else {
@@ -359,7 +366,7 @@ __global__ __launch_bounds__(T) void pv_distill_long_kernel(Args a) {
         if (a.soft) {
             tmax = group_reduce<T>(v_mine, Max(), lds);
             if (tmax == -INFINITY) tmax = 0.f;
-            p = mine ? __expf(v_mine - tmax) : 0.f;
+            p = mine ? __expf((v_mine - tmax) * a.tau) : 0.f;
             tsum = group_reduce<T>(p, Add(), lds);
             if (!(tsum == 0.f)) w.kl = d.alpha * d.temperature;
         }
@@ -367,7 +374,7 @@ __global__ __launch_bounds__(T) void pv_distill_long_kernel(Args a) {
         if constexpr (STATS) {
             float kl = 0.f;
             if (mine && w.kl != 0.f && !empty && !(p * tinv == 0.f))
-                kl = p * tinv * (v_mine - tmax - log_of(tsum) -
+                kl = p * tinv * ((v_mine - tmax) * a.tau - log_of(tsum) -
                                  fmaf(pv_load_one(r.p, BF16, c_mine), a.tau, -lset));
             kl = group_reduce<T>(kl, Add(), lds);
             if (t == 0) {

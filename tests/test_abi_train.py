@@ -204,3 +204,8 @@ def test_binding_refuses_before_the_library():
             bad()
     with pytest.raises(TypeError):
         b._dt(x.half())
+
+
+@pytest.mark.parametrize("temp", [1e-45, 2.0 ** -128])
+def test_distill_rejects_a_temperature_without_an_inverse(temp):
+    assert _dis(temp=temp) == EINVAL and _dis(temp=temp, M=0) == EINVAL

@@ -100,3 +100,37 @@ def test_group_norm_spread_beside_a_very_far_mean(N, C, G, first):
 def test_group_norm_on_both_sides_of_its_rules(B, N, C, G, dt, lengths):
     import test_gpu_train_ops as ops
     ops.test_group_norm_forward_and_gradients(B, N, C, G, dt, dt, "silu", lengths, 0, 0)
+
+
+# the type's lowest value as a mask of whole rows, where 1 / T > 1 takes it beyond the
+# type: rows of lanes, and of a workgroup
+@pytest.mark.parametrize("V", [13, 700, 5000])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("alpha", [1.0, 0.5])
+def test_distill_lowest_values_at_a_low_temperature(V, dt, alpha):
+    rng = np.random.default_rng(V)
+    M, top, T = 6, 4, 0.5
+    zt = put(rng.normal(size=(M, V)), dt)
+    lowest = torch.finfo(zt.dtype).min
+    zt[1] = lowest                              # nothing left over T: 0, no gradient
+    zt[2, 3:] = lowest
+    val = rng.normal(size=(M, top)).astype(np.float32)
+    val[3] = np.finfo(np.float32).min           # a teacher of it: uniform
+    val[4, 1:] = np.finfo(np.float32).min
+    cls = np.tile(np.arange(top, dtype=np.int32), (M, 1))
+    cls[2] = [0, 1, 2, -1]
+    labels = np.zeros(M, np.int32)
+    tv, tc, lt = (torch.as_tensor(a).cuda() for a in (val, cls, labels))
+    kw = dict(labels=lt, temperature=T, alpha=alpha)
+    loss, _, dz = pv.pvconv_distill_topk(zt, tv, tc, want_grad=True, **kw)
+    loss2, lse = pv.pvconv_distill_topk(zt, tv, tc, **kw)
+    dz2 = pv.pvconv_distill_topk_backward(zt, tv, tc, lse, **kw)
+    # (equal entries, given to the oracle as zeros: at their own size even 64 bits would
+    # not hold log 4 beside them)
+    tval = np.where(np.arange(M)[:, None] == 3, 0.0, val.astype(np.float64))
+    rl, rg = ref.distill(host(zt), tval, cls, labels, T, alpha)
+    rl[1], rg[1] = 0, 0
+    step = 2.0 ** -8 if dt == "bf16" else 0.0
+    for l, g in ((loss, dz), (loss2, dz2)):
+        assert (np.abs(host(l) - rl) <= 2e-5 * (1 + 4 * T * T + np.abs(rl))).all()
+        assert (np.abs(host(g) - rg) <= 2e-5 * (1 + T) + step * np.abs(rg)).all()
