@@ -48,33 +48,40 @@ class DeviceStudent:
         return [*self.weights, self.bias, *self.gamma, *self.beta]
 
     # -- serving --
+    def _model(self):
+        return ([pv.pvconv_fp8_quantize_weight(w) for w in self.weights], self.bias, self.gamma,
+                self.beta)
+
     def freeze(self):
-        """Quantises the weights for logits(); again after they have changed."""
-        self._served = [pv.pvconv_fp8_quantize_weight(w) for w in self.weights]
+        """Keeps the model as it is now for logits(): the weights quantised once,
+        and a copy of every other parameter. Again after training has changed it."""
+        quantised, bias, gamma, beta = self._model()
+        self._served = (quantised, bias.clone(), [t.clone() for t in gamma],
+                        [t.clone() for t in beta])
 
     def logits(self, x: torch.Tensor, lengths: Optional[torch.Tensor] = None) -> torch.Tensor:
         """x [B][N][C_in] (rows evenly strided; one point is N = 1) -> logits
-        [B][N][classes] f32 with the weights of the last freeze()."""
-        if self._served is None:
-            self.freeze()
-        return self._forward(x, self._served, lengths, None)
+        [B][N][classes] f32 of the model as the last freeze() kept it. Before any,
+        of the parameters as they are now, the weights quantised on every call."""
+        return self._forward(x, self._served or self._model(), lengths, None)
 
-    def _forward(self, x, quantised, lengths, saved):
+    def _forward(self, x, model, lengths, saved):
+        quantised, bias, gamma, beta = model
         h = x
         for i, (w, s) in enumerate(quantised[:-1]):
             z = pv.pvconv_fp8_linear(h, w, s, out_dtype=torch.bfloat16)
             kw = dict(eps=self.eps, act=self.act, slope=self.slope, lengths=lengths)
             if saved is None:
-                y = pv.pvconv_group_norm_act(z, self.groups, self.gamma[i], self.beta[i], **kw)
+                y = pv.pvconv_group_norm_act(z, self.groups, gamma[i], beta[i], **kw)
             else:
-                y, stats = pv.pvconv_group_norm_act(z, self.groups, self.gamma[i], self.beta[i],
+                y, stats = pv.pvconv_group_norm_act(z, self.groups, gamma[i], beta[i],
                                                     want_stats=True, **kw)
                 saved.append((h, z, stats))
             h = y
         w, s = quantised[-1]
         if saved is not None:
             saved.append((h,))
-        return pv.pvconv_fp8_linear(h, w, s, bias=self.bias, out_dtype=torch.float32)
+        return pv.pvconv_fp8_linear(h, w, s, bias=bias, out_dtype=torch.float32)
 
     # -- training --
     def step(self, x: torch.Tensor, t_val: torch.Tensor, t_class: torch.Tensor,
@@ -84,11 +91,13 @@ class DeviceStudent:
         """Forward and backward of sum(row_weight * loss): x [B][N][C_in], the
         teacher's t_val, t_class [B*N][top], labels [B*N] int32 -> (loss [B*N],
         gradients in the order of parameters(), dx [B][N][C_in] or None). Give the
-        points past a cloud's length the weight 0."""
+        points past a cloud's length the weight 0, and finite x: the first weight's
+        gradient multiplies their rows of x by 0."""
         B, N, _ = x.shape
         q = [pv.pvconv_fp8_quantize_weight(w, transposed=True) for w in self.weights]
         saved = []
-        z = self._forward(x, [(w, s) for w, s, _, _ in q], lengths, saved)
+        z = self._forward(x, ([(w, s) for w, s, _, _ in q], self.bias, self.gamma, self.beta),
+                          lengths, saved)
         loss, _, dz = pv.pvconv_distill_topk(
             z.view(B * N, -1), t_val, t_class, labels=labels, temperature=temperature,
             alpha=alpha, row_weight=row_weight, want_grad=True, out_dtype=torch.bfloat16)

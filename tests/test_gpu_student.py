@@ -92,3 +92,29 @@ def test_student_learns_its_teacher_and_serves_it():
     # a cloud served alone gives its own rows
     alone = st.logits(x[1:2])
     assert torch.allclose(alone[0], served[1], rtol=2e-2, atol=2e-2)
+
+
+def test_served_model_is_one_model():
+    # training goes on in place between two answers: the kept model answers as before,
+    # in every parameter, until it is kept anew
+    x, tv, tc, labels = _inputs(seed=4)
+    st = DeviceStudent([40, 32, 24, 13], groups=4, seed=3)
+    first = st.logits(x)
+    st.freeze()
+    kept = st.logits(x)
+    assert torch.equal(kept, first)
+    g = torch.Generator(device="cuda").manual_seed(5)
+    for p in st.parameters():
+        p.add_(torch.randn(p.shape, device="cuda", generator=g), alpha=0.3)
+    assert torch.equal(st.logits(x), kept)
+    st.freeze()
+    changed = st.logits(x)
+    assert not torch.equal(changed, kept)
+    # what the present parameters give without freeze()
+    live = DeviceStudent([40, 32, 24, 13], groups=4, seed=9)
+    for a, b in zip(live.parameters(), st.parameters()):
+        a.copy_(b)
+    assert torch.equal(live.logits(x), changed)
+    for p in live.parameters():
+        p.mul_(0.5)
+    assert not torch.equal(live.logits(x), changed)
