@@ -151,6 +151,8 @@ pvconv_status pvconv_fp8_linear_backward(const void* dy, pvconv_dtype dy_dt, int
 /*  dz       out [M][V] (dz_dt), row stride dz_ld, or NULL: row_weight[m]    */
 /*           (1 if NULL) times d loss_m / d z. A row of weight 0 is 0.       */
 /* 1 <= V <= PVCONV_MAX_CLASSES, 1 <= top <= PVCONV_MAX_TOP, M <= 2^30.      */
+/* The workspace size is 0 and the workspace is not looked at: sums stay in  */
+/* registers and LDS.                                                        */
 /* ------------------------------------------------------------------------- */
 size_t pvconv_distill_topk_workspace_size(int M, int V);
 pvconv_status pvconv_distill_topk(const void* z, pvconv_dtype z_dt, int z_ld, int M, int V,

@@ -867,7 +867,8 @@ def pvconv_distill_topk(z: torch.Tensor, t_val: torch.Tensor, t_class: torch.Ten
                         out_dtype=None, workspace: Optional[torch.Tensor] = None):
     """z [M][V] (rows evenly strided), t_val, t_class [M][top], labels [M] int32 ->
     (loss [M], lse [M][2]), and with want_grad (loss, lse, dz [M][V] in out_dtype
-    (z's if None)): the gradient of sum(row_weight * loss)."""
+    (z's if None)): the gradient of sum(row_weight * loss). A workspace is taken as by
+    the other calls; none is needed."""
     M, V, ld, top, labels_p = _distill_args(z, t_val, t_class, labels)
     _on_device(z.device, t_val, t_class, labels, row_weight, out, workspace)
     weight_p = _vector(row_weight, M, torch.float32, "row_weight")
@@ -879,12 +880,10 @@ def pvconv_distill_topk(z: torch.Tensor, t_val: torch.Tensor, t_class: torch.Ten
         if tuple(dz.shape) != (M, V):
             raise ValueError("out must have z's shape")
         _, dld = _matrix_rows(dz, V)
-    need = _lib.pvconv_distill_topk_workspace_size(M, V)
-    ws = _workspace(need, workspace, z.device)
     _check("pvconv_distill_topk", _lib.pvconv_distill_topk(
         _ptr(z), _dt(z), ld, M, V, _ptr(t_val), _ptr(t_class), top, labels_p, temperature, alpha,
-        weight_p, _ptr(loss), _ptr(lse), _ptr(dz), _dt(dz) if want_grad else F32, dld, _ptr(ws),
-        _ws_size(ws), _raw_stream(z.device)))
+        weight_p, _ptr(loss), _ptr(lse), _ptr(dz), _dt(dz) if want_grad else F32, dld, None, 0,
+        _raw_stream(z.device)))
     return (loss, lse, dz) if want_grad else (loss, lse)
 
 

@@ -257,18 +257,13 @@ pvconv_status pvconv_fp8_linear_backward(const void* dy, pvconv_dtype dy_dt, int
         PvRows{dx, dx_dt == PVCONV_BF16, dx_ld}, dw, dbias, workspace, as_stream(stream));
 }
 
-size_t pvconv_distill_topk_workspace_size(int M, int V) {
-    return M >= 0 && M <= (1 << 30) && V >= 1 && V <= PVCONV_MAX_CLASSES
-               ? pv_distill_ws_bytes(M, V)
-               : 0;
-}
+size_t pvconv_distill_topk_workspace_size(int, int) { return 0; }
 
 pvconv_status pvconv_distill_topk(const void* z, pvconv_dtype z_dt, int z_ld, int M, int V,
                                   const float* t_val, const int32_t* t_class, int top,
                                   const int32_t* labels, float temperature, float alpha,
                                   const float* row_weight, float* loss, float* lse, void* dz,
-                                  pvconv_dtype dz_dt, int dz_ld, void* workspace,
-                                  size_t workspace_bytes, void* stream) {
+                                  pvconv_dtype dz_dt, int dz_ld, void*, size_t, void* stream) {
     pvconv_status st =
         check_distill(z, z_dt, z_ld, M, V, t_val, t_class, top, labels, temperature, alpha);
     if (st != PVCONV_OK) return st;
@@ -292,12 +287,10 @@ pvconv_status pvconv_distill_topk(const void* z, pvconv_dtype z_dt, int z_ld, in
         bytes_overlap(lse, eb, row_weight, row_weight ? lb : 0) ||
         bytes_overlap(dz, db, row_weight, row_weight ? lb : 0))
         return PVCONV_EINVAL;
-    st = check_ws(workspace, workspace_bytes, pv_distill_ws_bytes(M, V));
-    if (st != PVCONV_OK) return st;
     return pv_launch_distill(PvDistill{PvRows{(void*)z, z_dt == PVCONV_BF16, z_ld}, M, V, t_val,
                                        t_class, top, labels, temperature, alpha},
                              row_weight, loss, lse, PvRows{dz, dz_dt == PVCONV_BF16, dz_ld},
-                             workspace, as_stream(stream));
+                             as_stream(stream));
 }
 
 pvconv_status pvconv_distill_topk_backward(const void* z, pvconv_dtype z_dt, int z_ld, int M,

@@ -538,15 +538,8 @@ pvconv_status launch(const Args& a, hipStream_t s) {
 
 }  // namespace
 
-size_t pv_distill_ws_bytes(int M, int V) {
-    (void)M;
-    (void)V;
-    return 0;
-}
-
 pvconv_status pv_launch_distill(const PvDistill& d, const float* row_weight, float* loss,
-                                float* lse, const PvRows& dz, void* ws, hipStream_t s) {
-    (void)ws;
+                                float* lse, const PvRows& dz, hipStream_t s) {
     const Args a{d, 1.f / d.temperature, d.alpha > 0.f, d.labels && d.alpha < 1.f, row_weight, loss,
                  lse, dz};
     return dz.p ? launch<true, true>(a, s) : launch<true, false>(a, s);

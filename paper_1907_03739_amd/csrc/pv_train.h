@@ -115,9 +115,8 @@ struct PvDistill {
     const int32_t* labels;
     float temperature, alpha;
 };
-size_t pv_distill_ws_bytes(int M, int V);
 // loss (and lse) and, where dz.p is set, the gradient of row_weight
 pvconv_status pv_launch_distill(const PvDistill& d, const float* row_weight, float* loss,
-                                float* lse, const PvRows& dz, void* ws, hipStream_t s);
+                                float* lse, const PvRows& dz, hipStream_t s);
 pvconv_status pv_launch_distill_bwd(const PvDistill& d, const float* lse, const float* dloss,
                                     const PvRows& dz, hipStream_t s);
