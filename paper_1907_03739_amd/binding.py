@@ -601,6 +601,8 @@ def _workspace(need: int, given: Optional[torch.Tensor], device):
     if need == 0:
         return None
     if given is not None and given.numel() * given.element_size() >= need:
+        if not given.is_contiguous():
+            raise ValueError("workspace must be contiguous")
         return given
     return torch.empty(need, dtype=torch.uint8, device=device)
 

@@ -209,3 +209,13 @@ def test_binding_refuses_before_the_library():
 @pytest.mark.parametrize("temp", [1e-45, 2.0 ** -128])
 def test_distill_rejects_a_temperature_without_an_inverse(temp):
     assert _dis(temp=temp) == EINVAL and _dis(temp=temp, M=0) == EINVAL
+
+
+def test_binding_refuses_a_workspace_that_is_not_whole():
+    # many elements that are one byte of memory
+    x, v = torch.zeros(2, 5, 8), torch.zeros(8)
+    ws = torch.zeros(1, dtype=torch.uint8).expand(1 << 20)
+    with pytest.raises(ValueError):
+        b.pvconv_group_norm_act(x, 2, v, v, workspace=ws)
+    with pytest.raises(ValueError):
+        b.pvconv_fp8_linear_backward(x, x, None, None, want_dx=False, workspace=ws)
