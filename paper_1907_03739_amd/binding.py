@@ -651,6 +651,9 @@ def _vector(t: Optional[torch.Tensor], n: int, dtype, what: str):
     return t.data_ptr()
 
 
+_MOST_INT = (1 << 31) - 1  # sizes and strides are C ints
+
+
 def _matrix_rows(t: torch.Tensor, ncols: int) -> tuple:
     """(rows, row stride) of a [.., ncols] tensor whose rows are evenly spaced:
     every leading dimension continues the one after it. A single row, or none,
@@ -660,6 +663,8 @@ def _matrix_rows(t: torch.Tensor, ncols: int) -> tuple:
     rows = 1
     for d in t.shape[:-1]:
         rows *= d
+    if rows > _MOST_INT or ncols > _MOST_INT:  # (ctypes would cut them to 32 bits)
+        raise ValueError("more than 2^31 - 1 rows or channels")
     if t.is_contiguous() or rows == 0:
         return rows, ncols
     if ncols > 1 and t.stride(-1) != 1:
@@ -678,6 +683,8 @@ def _matrix_rows(t: torch.Tensor, ncols: int) -> tuple:
         ld = ncols
     if ld < ncols:
         raise ValueError("rows must not overlap")
+    if ld > _MOST_INT:
+        raise ValueError("rows more than 2^31 - 1 elements apart")
     return rows, ld
 
 

@@ -219,3 +219,21 @@ def test_binding_refuses_a_workspace_that_is_not_whole():
         b.pvconv_group_norm_act(x, 2, v, v, workspace=ws)
     with pytest.raises(ValueError):
         b.pvconv_fp8_linear_backward(x, x, None, None, want_dx=False, workspace=ws)
+
+
+def test_binding_refuses_sizes_beyond_a_c_int():
+    # ctypes would pass their low 32 bits: 2^32 + 5 rows as 5
+    v, one = torch.zeros(8), torch.zeros(1)
+    bf = dict(dtype=torch.bfloat16, device="meta")
+    rows = torch.empty(((1 << 32) + 5, 1), **bf)
+    apart = torch.empty_strided((2, 3, 8), (3 * ((1 << 32) + 8), (1 << 32) + 8, 1), **bf)
+    q, s = torch.zeros(4, 128, dtype=torch.uint8), torch.zeros(1, 1, dtype=torch.uint8)
+    for bad in (lambda: b.pvconv_group_norm_act(rows.view(-1, 1, 1), 1, one, one),
+                lambda: b.pvconv_group_norm_act(apart, 2, v, v),
+                lambda: b.pvconv_fp8_linear(rows, q.to("meta"), s.to("meta")),
+                lambda: b.pvconv_fp8_linear(apart, q.to("meta"), s.to("meta")),
+                lambda: b.pvconv_fp8_linear_backward(rows, None, None, None, False, False),
+                lambda: b.pvconv_fp8_quantize_weight(rows),
+                lambda: b.pvconv_distill_topk(rows, rows.float(), rows.int())):
+        with pytest.raises(ValueError, match="2\\^31"):
+            bad()
