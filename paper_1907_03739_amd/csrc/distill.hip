@@ -477,8 +477,9 @@ using Int = std::integral_constant<int, N>;
 
 // Whether a loss alone reads z past the caches' normal order: where z is more than
 // the Infinity Cache holds, so that neither what wrote it nor the gradient that
-// follows shares it (us, streaming / not: 4096 x 49999 bf16, 410 MB, 93 / 95; 2048 rows
-// of them 50 / 45, 8192 x 5000, 82 MB, 36 / 31, with the gradient's call 73 / 66).
+// follows shares it (us, streaming / not, of a z that was just written: 8192 x 5000
+// bf16, 82 MB, 31 / 27, with the gradient's call 66 / 58; 2048 x 49999, 205 MB, 42 / 38;
+// 4096 x 49999, 410 MB, 77 / 100, with the gradient's call 237 / 273).
 bool streams(const PvDistill& d) {
     return (size_t)d.M * d.V * (d.z.bf16 ? 2 : 4) >= (size_t)256 << 20;
 }

@@ -848,16 +848,17 @@ void with_kind(int types, bool silu, int vec, F f) {
 }
 
 // Whether the two launches, whose reads of a line lie far apart, read past the
-// caches' normal order: where what both read is more than the Infinity Cache holds
-// (us, streaming / not: 32 x 32768 x 128 bf16 134 / 164, gradient 247 / 283, 16 of them
-// 129 / 139; but their forward, 134 MB of x, 74 / 69, 12 x 23929 x 96 fp32, 16 groups,
-// 72 / 65, gradient 118 / 109, 1 x 61059 x 96 fp32, 32 groups, 38 / 31, gradient 61 / 49).
-constexpr size_t kInfinityCache = (size_t)256 << 20;
-bool streams(const PvNorm& n, const PvRows* read, int count) {
-    size_t bytes = 0;
-    for (int i = 0; i < count; i++)
-        bytes += (size_t)n.B * n.N * n.C * (read[i].bf16 ? 2 : 4);
-    return bytes >= kInfinityCache;
+// caches' normal order: where x and what is streamed beside it (y, or a gradient's dy)
+// come near what the Infinity Cache holds (256 MiB). us, streaming / not, of an input
+// that was just written and of one that comes from memory:
+//   forward     8 x 32768 x 128 bf16 (x 64 MB) 37.4 / 36.7, 42.6 / 42.2; 12 of them
+//               55 / 54, 63 / 68; 16: 65 / 70, 74 / 89; 32: 129 / 142, 133 / 168
+//   gradient    6: 55.4 / 54.8, 55.5 / 58.0; 12: 104 / 104, 105 / 119; 16: 122 / 125,
+//               127 / 144; 32: 240 / 281, 241 / 279; 12 x 24000 x 96 fp32: 126 / 124,
+//               130 / 139 (and 130 / 119 where both lie in the cache)
+constexpr size_t kStreamBytes = (size_t)224 << 20;
+bool streams(const PvNorm& n, const PvRows& a, const PvRows& b) {
+    return (size_t)n.B * n.N * n.C * ((a.bf16 ? 2 : 4) + (b.bf16 ? 2 : 4)) >= kStreamBytes;
 }
 // f with whether to stream as a constant, for vectors that can
 template <int TYPES, int VEC, typename F>
@@ -955,7 +956,7 @@ pvconv_status pv_launch_group_norm(const PvNorm& n, const PvRows& x, const PvRow
         return pv_launch_status();
     }
     const Width w = width_of_rows(d, n.C, all, 2);
-    const bool once = streams(n, all, 1);
+    const bool once = streams(n, x, y);
     with_kind(types, silu, w.vec, [&](auto T, auto S, auto V) {
         constexpr int TYPES = decltype(T)::value, VEC = decltype(V)::value;
         constexpr bool SILU = decltype(S)::value;
@@ -1017,7 +1018,7 @@ pvconv_status pv_launch_group_norm_bwd(const PvNorm& norm, const PvRows& dy, con
         return pv_launch_status();
     }
     const Width w = width_of_rows(d, n.C, all, 3);
-    const bool once = streams(n, all, 2);
+    const bool once = streams(n, dy, x);
     with_kind(types, silu, w.vec, [&](auto T, auto S, auto V) {
         constexpr int TYPES = decltype(T)::value, VEC = decltype(V)::value;
         constexpr bool SILU = decltype(S)::value;
