@@ -881,25 +881,31 @@ void with_stream(bool once, F f) {
 //   groups: 237 / 87; 4096 x 16 x 128, 8 groups: 64 / 34; but 256 x 64 x 128, 8
 //   groups: 7.9 / 9.4, and 65536 x 3 x 64 in one group, fp32: 117 / 210).
 // - Forward, 1024 threads: more than two workgroups a CU (256 x 512 x 128, 8
-//   groups: 49 / 28), or few of them with much to read each (1 x 8192 x 64, 8 groups:
-//   17.0 / 9.6; but 1 x 4096 x 128, 32 groups: 10.5 / 16.9).
-// - Gradient: a workgroup adds its channels' sums one after another, so groups of
-//   more than 32 channels (64 x 3 x 512, 8 groups, fp32: 15 / 8), many workgroups
+//   groups: 49 / 28; where both go by single elements more than four, 31 x 1000 x
+//   96 of wider rows, 32 groups: 19 / 29), or few of them with much to read each
+//   (1 x 8192 x 64, 8 groups: 17.0 / 9.6; but 1 x 4096 x 128, 32 groups: 10.5 / 16.9).
+// - Gradient: where a workgroup adds its channels' sums a wave a channel, groups of
+//   more than 32 channels (64 x 3 x 512, 8 groups, fp32: 15 / 8; but 1 x 1 x 1088 in 8
+//   groups, whose threads add a channel each: 4.1 / 7.8, 512 x 20 x 640 in 4 groups:
+//   19 / 25); many workgroups
 //   (16384 x 1 x 128, 8 groups: 1020 / 176; of 1024 threads, 256 x 512 x 128, 8
-//   groups: 68 / 41), unless they are full (64 x 256 x 256, 32 groups, fp32: 19 / 28);
+//   groups: 68 / 41) unless they are full (64 x 256 x 256, 32 groups, fp32: 19 / 28);
 //   and few with much to read each (4 x 2048 x 128, 8 groups: 15.6 / 12.2; 32 clouds:
 //   21 / 27).
 constexpr int kSmallT = 256, kSmallU = 2, kLargeT = 1024, kLargeU = 8, kLargeBwdU = 4;
-constexpr int kHeldChannels = 32;  // of a group whose gradient is held
+constexpr int kHeldChannels = 32;
 enum Hold { kNot, kSmall, kLarge };
 Hold hold_of(const PvNorm& n, const Deal& d, int vec, bool gradient) {
     if (n.N < 1) return kNot;
     const size_t groups = (size_t)n.B * n.groups;  // workgroups
     const int cols = d.CG / vec;
+    // a thread adds a channel's sums of a gradient (else a wave does)
+    auto by_threads = [&](int threads) { return d.CG > threads / 2 || cols > threads / 2; };
     if (cols <= kSmallT && n.N <= kSmallT / cols * kSmallU) {
         const int vectors = n.N * cols;
         const bool held =
-            gradient ? (d.CG <= kHeldChannels && groups <= 2048 && groups * d.CG <= 8192) ||
+            gradient ? by_threads(kSmallT) ||
+                           (d.CG <= kHeldChannels && groups <= 2048 && groups * d.CG <= 8192) ||
                            (d.CG <= 8 && vec >= 4 && vectors >= kSmallT * 3 / 2)
                      : groups <= 4096 || vectors >= kSmallT || groups <= 3 * d.items;
         // HIP takes fewer than 2^32 threads a launch
@@ -907,8 +913,10 @@ Hold hold_of(const PvNorm& n, const Deal& d, int vec, bool gradient) {
     }
     if (cols <= kLargeT && n.N <= kLargeT / cols * (gradient ? kLargeBwdU : kLargeU)) {
         const int values = n.N * d.CG;
-        const bool held = groups <= 512 &&
-                          (gradient ? d.CG <= kHeldChannels && (values <= 16384 || groups >= 192)
+        const size_t most = vec > 1 ? 512 : gradient ? 768 : 1024;
+        const bool held = groups <= most &&
+                          (gradient ? (d.CG <= kHeldChannels || by_threads(kLargeT)) &&
+                                          (values <= 16384 || groups >= 192)
                                     : values <= 32768 || groups >= 96);
         return held ? kLarge : kNot;
     }

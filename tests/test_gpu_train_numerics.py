@@ -96,6 +96,8 @@ def test_group_norm_spread_beside_a_very_far_mean(N, C, G, first):
     (11, 4096, 64, 8, "bf16", None), (1, 4097, 64, 8, "bf16", [4000]),  # 32768 values a group
     (12, 2048, 128, 8, "bf16", None), (24, 2048, 128, 8, "bf16", None),
     (23, 2048, 128, 8, "bf16", None), (2, 1024, 128, 8, "bf16", [1024, 3]),
+    (32, 900, 96, 32, "f32", None), (24, 700, 96, 32, "bf16", None),  # single elements
+    (300, 2, 459, 3, "f32", None), (2, 6, 1088, 8, "bf16", [6, 1]),  # a thread a channel
 ])
 def test_group_norm_on_both_sides_of_its_rules(B, N, C, G, dt, lengths):
     import test_gpu_train_ops as ops
