@@ -5,7 +5,9 @@
 // temperature 1, lse_T = m / T + log s_T: the loss needs z at the stored entries
 // and the label beside them, the gradient of a logit is
 //   w (alpha T (exp(z / T - lse_T) - p) + (1 - alpha) (exp(z - lse_1) - [label])).
-// Bound by HBM: z read once and, where the gradient is taken, dz written.
+// z is read once and, where the gradient is taken, dz written. A long row's loss is
+// bound by vector issue (two exponentials, a guard and a maximum a logit), its gradient
+// by memory.
 // Rows of up to 2048 classes stay in the registers of 4 to 64 lanes, from the one
 // read to the gradient. Rows of more take a workgroup, which goes over them once
 // with a running maximum and sums a thread and, for the gradient, a second time,
@@ -224,7 +226,8 @@ __global__ __launch_bounds__(kThreads) void pv_distill_short_kernel(Args a) {
 // first 16-byte boundary on, the elements before and after one a thread. Rows
 // of z and dz rarely share that boundary (an odd number of classes): the pass
 // that reads alone goes by z's, the pass that writes by dz's.
-// 4096 x 49999, top 64, bf16: loss 104 us (3.9 TB/s), gradient 197 (4.2 TB/s).
+// 4096 x 49999, top 64, bf16: loss 104 us (3.9 TB/s; the SIMDs issue vector
+// instructions in 93 % of the cycles), gradient 197 (4.2 TB/s, 50 %); both in one call 226.
 // ---------------------------------------------------------------------------
 constexpr int kAhead = 4;  // vectors in flight a thread
 

@@ -4,7 +4,9 @@
 // With s_b = 2^e_b the scale of a block of 128 values and q = round(v / s_b) in
 // e4m3: out[m][n] = act( sum over blocks b of s_b(m) s_b(n) q(m) . q(n) + bias_n ).
 // The scaled matrix instruction of gfx950 (16x16x128) spans one block: it takes the
-// blocks' two scales as they are, and its sums stay fp32.
+// blocks' two scales as they are, adds the block's products on a grid of the largest
+// of them, and the blocks in fp32 (pv_fp8_tile_kernel has what that means for which
+// outputs).
 //
 // A layer's forward and the gradient of its input quantise the rows of x or dy on
 // their way into the product (pv_fp8_few_, _resident_, _fused_kernel: path_of has
@@ -333,17 +335,21 @@ __global__ __launch_bounds__(kThreads) void pv_fp8_quantise_kernel(QuantiseJobs 
 //
 // EXACT: the fp8 instruction adds a block's products on a grid set by the
 // largest of them: about 5e-5 of a sum of values spread over e4m3's range.
-// bf16 outputs, which round 40 times coarser, take it; fp32 outputs turn the
-// bytes, with their scales, into bf16 (exact: four digits and a power of two)
-// and use the bf16 instruction, whose sums are good to fp32, at half the rate.
+// bf16 outputs, which round 40 times coarser, take it (their error against 64 bits
+// is that of one rounding; with exact sums 16384 x 4928 -> 256 would take 65 us for
+// 48, 16384 x 512 -> 2048 55 for 38, 32768 x 2304 -> 512 93 for 65); fp32 outputs turn
+// the bytes, with their scales, into bf16 (four digits and a power of two: exact from
+// 2^-133 up) and use the bf16 instruction, whose sums are good to fp32, at half the
+// rate.
 //
 // LDS rows are 128 bytes, in 16-byte pieces exchanged by a key of the row
 // (a_key, b_key), so that the lanes of a fragment read fall on all the banks.
 //
 // The weight's gradient of 32768 rows, 2304 x 512: 77 Gflop in bf16 in 87 us, 0.89
-// PFLOP/s of the 1.1 that a library product reaches; 58 % of the waves' cycles issue
-// matrix instructions. (The conversions are not its bound: 89 us without them; on
-// the fp8 instruction it would take 63.)
+// PFLOP/s of the 1.88 that a loop of these instructions alone reaches and of a
+// library product's 1.1; 58 % of the waves' cycles issue matrix instructions. (The
+// conversions are not its bound: 89 us without them; on the fp8 instruction it would
+// take 63.) Bound by the latency of a slice at two workgroups a CU.
 struct Product {
     const uint8_t* a;   // [blocks][M][128]
     const uint8_t* sa;  // [blocks][M]
@@ -376,7 +382,8 @@ __device__ __forceinline__ int w_key(int row) {
     return (row & 3) | ((row >> (J == 2 ? 1 : 2)) & 4);
 }
 
-// Eight e4m3 bytes times 2^(byte - 127), as bf16.
+// Eight e4m3 bytes times 2^(byte - 127), as bf16 (which ends at 2^-133: a byte of 1 and
+// less than 2^-7 times its scale is rounded to that grid).
 __device__ __forceinline__ bf16x8 to_bf16(uint32_t lo, uint32_t hi, uint32_t byte) {
     const float f = __uint_as_float(byte << 23);
     union {

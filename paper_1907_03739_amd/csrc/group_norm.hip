@@ -2,12 +2,12 @@
 // (pvconv_train.h).
 //
 // A group of a cloud that fits the registers of a workgroup is read once, by one
-// launch a direction (pv_gn_held_*: up to 8192 vectors). Larger ones take two
-// launches: the first sums a share ("chunk") of a cloud's rows over a slab of
-// whole groups; the second adds the chunks' sums of its groups in a fixed order
-// and applies them to a chunk of rows. Bound by HBM: there x (and dy) are read
-// twice, y (dx) is written once. 16 x 32768 x 128, 8 groups, bf16: sums 27 us (5.0
-// TB/s) and apply 48 (5.6), backward 61 (4.4) and 74 (5.4).
+// launch a direction (pv_gn_held_*: up to 8192 vectors), where hold_of finds that
+// faster. The others take two launches: the first sums a share ("chunk") of a
+// cloud's rows over a slab of whole groups; the second adds the chunks' sums of its
+// groups in a fixed order and applies them to a chunk of rows. Bound by HBM: there
+// x (and dy) are read twice, y (dx) is written once. 16 x 32768 x 128, 8 groups,
+// bf16: sums 27 us (4.9 TB/s) and apply 47 (5.7), backward 58 (4.6) and 72 (5.6).
 #include <type_traits>
 
 #include "pv_train.h"
@@ -559,8 +559,9 @@ __global__ __launch_bounds__(kThreads) void pv_gn_bwd_apply_kernel(
 // Groups held in registers: a workgroup of T threads a (cloud, group), U vectors
 // a thread, rows in parallel over the threads. The mean is summed first, the
 // squares about it then, both from the registers.
-// 16 x 2048 x 128, 8 groups, bf16: 11.8 us, backward 15.9, of which 3 and 5 would
-// move the bytes: bound by a workgroup's chain of load, two sums and store, one a CU.
+// 16 x 2048 x 128, 8 groups, bf16: 12.5 us, of which 3 would move the bytes; 32 clouds
+// of them: 14.6, backward 21: bound by a workgroup's chain of load, two sums and
+// store, one a CU.
 // ---------------------------------------------------------------------------
 template <int T>
 __device__ __forceinline__ double group_sum(double a, double* lds) {
