@@ -1,8 +1,9 @@
 /*
  * pvconv_train.h -- C ABI of the operators around the networks' point MLPs
  * that training and 8-bit serving use: group normalisation with an activation,
- * a linear layer in 8-bit floating point, and the distillation loss against a
- * teacher's top logits, each with its gradients.
+ * linear layers in 8-bit floating point and in 8-bit integers, the distillation
+ * loss against a teacher's top logits, and the cross entropy of a linear layer,
+ * each with its gradients.
  *
  * The conventions of pvconv.h hold for every call here: device pointers owned
  * by the caller, rows of channels with a row stride in elements (`*_ld`, 0
@@ -129,6 +130,71 @@ pvconv_status pvconv_fp8_linear_backward(const void* dy, pvconv_dtype dy_dt, int
                                          const uint8_t* scale_t, void* dx, pvconv_dtype dx_dt,
                                          int dx_ld, float* dw, float* dbias, void* workspace,
                                          size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------- */
+/* Linear layer in 8-bit integers, a scale for each row of x and for each row */
+/* (output channel) of the weight.                                           */
+/*                                                                           */
+/* A row v is quantised with the scale s, the smallest bf16 number >= 2^-126 */
+/* with 127 s >= its largest |v|: q = the whole number nearest to v / s, ties */
+/* to even (in real arithmetic: any implementation gives these bytes). A row */
+/* that holds a NaN or an infinity has the scale NaN and q = 0.              */
+/* Eight bits of a scale cost at most 2^-7 of the range and make products of */
+/* scales, and of a scale and a bf16 value, exact.                           */
+/*                                                                           */
+/* Layout: q [R][K128] bytes, scale [R] fp32 (K128 = K rounded up to a       */
+/* multiple of PVCONV_INT8_BLOCK; padding is written as zero and has to be). */
+/* Byte arrays are 16-byte aligned.                                          */
+/* ------------------------------------------------------------------------- */
+#define PVCONV_INT8_BLOCK 128         /* quantised rows are whole blocks */
+#define PVCONV_INT8_MAX_CHANNELS 65536
+
+/* x [R][K] (x_dt), row stride x_ld -> q, scale: of a weight [N][K], of rows. */
+/* 0 <= R <= 2^30, 1 <= K <= PVCONV_INT8_MAX_CHANNELS.                       */
+pvconv_status pvconv_int8_quantize(const void* x, pvconv_dtype x_dt, int x_ld, int R, int K,
+                                   int8_t* q, float* scale, void* stream);
+
+/* y[m,n] = act( s_m scale_n sum_k q[m,k] weight[n,k] + bias_n ), q and s of x's */
+/* rows. The sums are exact integers, rounded once to fp32.                  */
+/*  x     [M][K] (x_dt), row stride x_ld                                     */
+/*  bias  [N] fp32 or NULL; act NONE, RELU or LEAKY (slope)                  */
+/*  y     out [M][N] (y_dt), row stride y_ld                                 */
+/*  rows, row_scale  out: x's quantised rows, kept for the backward and for  */
+/*        pvconv_int8_linear_rows in x's place, or NULL (both)               */
+/* 1 <= K, N <= PVCONV_INT8_MAX_CHANNELS; M/128 * max(K, N)/128 (rounded up) */
+/* <= 2^26.                                                                  */
+size_t pvconv_int8_linear_workspace_size(int M, int K, int N);
+pvconv_status pvconv_int8_linear(const void* x, pvconv_dtype x_dt, int x_ld, int M, int K, int N,
+                                 const int8_t* weight, const float* scale, const float* bias,
+                                 pvconv_act act, float slope, void* y, pvconv_dtype y_dt,
+                                 int y_ld, int8_t* rows, float* row_scale, void* workspace,
+                                 size_t workspace_bytes, void* stream);
+
+/* The same layer of rows that are quantised already: the bits of the call that */
+/* quantised them.                                                           */
+size_t pvconv_int8_linear_rows_workspace_size(int M, int K, int N);
+pvconv_status pvconv_int8_linear_rows(const int8_t* rows, const float* row_scale, int M, int K,
+                                      int N, const int8_t* weight, const float* scale,
+                                      const float* bias, pvconv_act act, float slope, void* y,
+                                      pvconv_dtype y_dt, int y_ld, void* workspace,
+                                      size_t workspace_bytes, void* stream);
+
+/* The gradients of y = x W^T + bias at the quantised values x = s q, W =    */
+/* scale weight, from the kept rows:                                         */
+/*   dx[m,k] = sum_n dy[m,n] scale_n weight[n,k]                             */
+/*   dw[n,k] = sum_m dy[m,n] row_scale_m rows[m,k],  dbias_n = sum_m dy[m,n] */
+/* An fp32 output has fp32 sums of products good to 24 bits; for a bf16 dx,  */
+/* dy scale_n is rounded to bf16 first.                                      */
+/*  dy [M][N] (dy_dt), dy_ld; dx out [M][K] (dx_dt), dx_ld, or NULL (weight, */
+/*  scale then unused); dw out [N][K] fp32 or NULL (rows, row_scale then     */
+/*  unused); dbias out [N] fp32 or NULL                                      */
+size_t pvconv_int8_linear_backward_workspace_size(int M, int K, int N);
+pvconv_status pvconv_int8_linear_backward(const void* dy, pvconv_dtype dy_dt, int dy_ld,
+                                          const int8_t* rows, const float* row_scale, int M,
+                                          int K, int N, const int8_t* weight,
+                                          const float* scale, void* dx, pvconv_dtype dx_dt,
+                                          int dx_ld, float* dw, float* dbias, void* workspace,
+                                          size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------- */
 /* Distillation from a teacher's top logits.                                 */

@@ -15,7 +15,9 @@ _BINDING_NAMES = (
     "pvconv_forward", "pvconv_forward_workspace_size", "pvconv_maxpool", "pvconv_point_mlp",
     "pvconv_voxelize",
     "pvconv_group_norm_act", "pvconv_group_norm_act_backward", "pvconv_fp8_quantize_weight",
-    "pvconv_fp8_linear", "pvconv_fp8_linear_backward", "pvconv_distill_topk",
+    "pvconv_fp8_linear", "pvconv_fp8_linear_backward", "pvconv_int8_quantize",
+    "pvconv_int8_linear", "pvconv_int8_linear_rows", "pvconv_int8_linear_backward",
+    "pvconv_distill_topk",
     "pvconv_distill_topk_backward",
 )
 

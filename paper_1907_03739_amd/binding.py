@@ -114,6 +114,16 @@ _SIGS_TRAIN = {
     "pvconv_fp8_linear_backward_workspace_size": ([_I, _I, _I], _SZ),
     "pvconv_fp8_linear_backward": ([_VP, _I, _I, _VP, _I, _I, _I, _I, _I, _VP, _VP, _VP, _I, _I,
                                     _VP, _VP, _VP, _SZ, _VP], _I),
+    "pvconv_int8_quantize": ([_VP, _I, _I, _I, _I, _VP, _VP, _VP], _I),
+    "pvconv_int8_linear_workspace_size": ([_I, _I, _I], _SZ),
+    "pvconv_int8_linear": ([_VP, _I, _I, _I, _I, _I, _VP, _VP, _VP, _I, _F, _VP, _I, _I, _VP,
+                            _VP, _VP, _SZ, _VP], _I),
+    "pvconv_int8_linear_rows_workspace_size": ([_I, _I, _I], _SZ),
+    "pvconv_int8_linear_rows": ([_VP, _VP, _I, _I, _I, _VP, _VP, _VP, _I, _F, _VP, _I, _I, _VP,
+                                 _SZ, _VP], _I),
+    "pvconv_int8_linear_backward_workspace_size": ([_I, _I, _I], _SZ),
+    "pvconv_int8_linear_backward": ([_VP, _I, _I, _VP, _VP, _I, _I, _I, _VP, _VP, _VP, _I, _I,
+                                     _VP, _VP, _VP, _SZ, _VP], _I),
     "pvconv_distill_topk_workspace_size": ([_I, _I], _SZ),
     "pvconv_distill_topk": ([_VP, _I, _I, _I, _I, _VP, _VP, _I, _VP, _F, _F, _VP, _VP, _VP, _VP,
                              _I, _I, _VP, _SZ, _VP], _I),
@@ -128,6 +138,7 @@ for _name, (_args, _res) in _SIGS_TRAIN.items():
 EXPORTED_TRAIN = tuple(_SIGS_TRAIN)
 ACT_NORM = dict(ACT, silu=3)  # the group norm's activations
 FP8_BLOCK = 128
+INT8_BLOCK = 128  # quantised rows are whole blocks
 
 
 class PVConvError(RuntimeError):
@@ -593,7 +604,7 @@ def pvconv_act_bn_backward(dy: torch.Tensor, y: torch.Tensor, bn=None, act="leak
 
 
 # ----------------------------------------------------------------------------
-# include/pvconv_train.h: group norm, 8-bit linear layer, distillation loss
+# include/pvconv_train.h: group norm, 8-bit linear layers, losses
 # ----------------------------------------------------------------------------
 def _workspace(need: int, given: Optional[torch.Tensor], device):
     """The caller's workspace where it is large enough, else a new one; None
@@ -854,6 +865,129 @@ def pvconv_fp8_linear_backward(dy: torch.Tensor, x: Optional[torch.Tensor],
         _ptr(dy), _dt(dy), dld, _ptr(x) if want_dw else None, _dt(x) if x is not None else F32, ld, M,
         K, N, _ptr(weight_t) if want_dx else None, _ptr(scale_t) if want_dx else None, _ptr(dx),
         _dt(dx) if want_dx else F32, 0, _ptr(dw), _ptr(db), _ptr(ws), _ws_size(ws), _raw_stream(dy.device)))
+    return dx, dw, db
+
+
+def _int8_up(n: int) -> int:
+    return -(-n // INT8_BLOCK) * INT8_BLOCK
+
+
+def _int8_operand(q: torch.Tensor, scale: torch.Tensor, cols: int, what: str):
+    """Checks quantised rows [R][cols up to 128s] and their scales [R]."""
+    if q.dim() != 2 or q.shape[1] != _int8_up(cols) or not q.is_contiguous() or \
+            q.dtype != torch.int8:
+        raise ValueError(f"{what} must be contiguous [..][{_int8_up(cols)}] int8")
+    _vector(scale, q.shape[0], torch.float32, f"{what}'s scale")
+
+
+def pvconv_int8_quantize(x: torch.Tensor):
+    """x [..][K] (rows evenly strided), a weight [N][K] or rows of features -> (int8
+    [R][K128], scale [R] f32): a scale for each row. K128: K rounded up to a multiple
+    of 128, zeros from K on."""
+    K = x.shape[-1]
+    R, ld = _matrix_rows(x, K)
+    q = torch.empty((R, _int8_up(K)), dtype=torch.int8, device=x.device)
+    scale = torch.empty((R,), dtype=torch.float32, device=x.device)
+    _check("pvconv_int8_quantize", _lib.pvconv_int8_quantize(
+        _ptr(x), _dt(x), ld, R, K, _ptr(q), _ptr(scale), _raw_stream(x.device)))
+    return q, scale
+
+
+def pvconv_int8_linear(x: torch.Tensor, weight: torch.Tensor, scale: torch.Tensor,
+                       bias: Optional[torch.Tensor] = None, act: str = "none", slope: float = 0.1,
+                       out: Optional[torch.Tensor] = None, out_dtype=None,
+                       want_rows: bool = False, workspace: Optional[torch.Tensor] = None):
+    """x [..][K] (rows evenly strided), a weight of pvconv_int8_quantize -> act(x W^T
+    + bias) [..][N] in out_dtype (x's if None), and with want_rows (y, rows [M][K128]
+    int8, row_scale [M]): x's quantised rows, which the backward and
+    pvconv_int8_linear_rows take in x's place."""
+    K, N = x.shape[-1], weight.shape[0]
+    _int8_operand(weight, scale, K, "weight")
+    _on_device(x.device, weight, scale, bias, out, workspace)
+    bias_p = _vector(bias, N, torch.float32, "bias")
+    M, ld = _matrix_rows(x, K)
+    shape = tuple(x.shape[:-1]) + (N,)
+    if out is None:
+        out = torch.empty(shape, dtype=_torch_dt(out_dtype or x.dtype), device=x.device)
+    elif tuple(out.shape) != shape:
+        raise ValueError(f"out must be {shape}")
+    _, old = _matrix_rows(out, N)
+    rows = row_scale = None
+    size = _lib.pvconv_int8_linear_workspace_size
+    if want_rows:
+        rows = torch.empty((M, _int8_up(K)), dtype=torch.int8, device=x.device)
+        row_scale = torch.empty((M,), dtype=torch.float32, device=x.device)
+        size = _lib.pvconv_int8_linear_rows_workspace_size
+    ws = _workspace(size(M, K, N), workspace, x.device)
+    _check("pvconv_int8_linear", _lib.pvconv_int8_linear(
+        _ptr(x), _dt(x), ld, M, K, N, _ptr(weight), _ptr(scale), bias_p, ACT[act], slope, _ptr(out),
+        _dt(out), old, _ptr(rows), _ptr(row_scale), _ptr(ws), _ws_size(ws), _raw_stream(x.device)))
+    return (out, rows, row_scale) if want_rows else out
+
+
+def pvconv_int8_linear_rows(rows: torch.Tensor, row_scale: torch.Tensor, weight: torch.Tensor,
+                            scale: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                            act: str = "none", slope: float = 0.1,
+                            out: Optional[torch.Tensor] = None, out_dtype=torch.float32,
+                            workspace: Optional[torch.Tensor] = None):
+    """Quantised rows [M][K128], row_scale [M] in x's place -> [M][N] in out_dtype: the
+    bits that pvconv_int8_linear gave of the rows that it kept."""
+    if rows.dim() != 2 or weight.dim() != 2 or rows.shape[1] != weight.shape[1]:
+        raise ValueError("rows and weight must have as many channels")
+    K, N = rows.shape[1], weight.shape[0]
+    _int8_operand(rows, row_scale, K, "rows")
+    _int8_operand(weight, scale, K, "weight")
+    _on_device(rows.device, row_scale, weight, scale, bias, out, workspace)
+    bias_p = _vector(bias, N, torch.float32, "bias")
+    M = rows.shape[0]
+    if out is None:
+        out = torch.empty((M, N), dtype=_torch_dt(out_dtype), device=rows.device)
+    elif out.dim() < 2 or out.shape[-1] != N or out.numel() != M * N:
+        raise ValueError(f"out must be {M} rows of {N}")
+    _, old = _matrix_rows(out, N)
+    ws = _workspace(_lib.pvconv_int8_linear_rows_workspace_size(M, K, N), workspace, rows.device)
+    _check("pvconv_int8_linear_rows", _lib.pvconv_int8_linear_rows(
+        _ptr(rows), _ptr(row_scale), M, K, N, _ptr(weight), _ptr(scale), bias_p, ACT[act], slope,
+        _ptr(out), _dt(out), old, _ptr(ws), _ws_size(ws), _raw_stream(rows.device)))
+    return out
+
+
+def pvconv_int8_linear_backward(dy: torch.Tensor, rows: Optional[torch.Tensor],
+                                row_scale: Optional[torch.Tensor],
+                                weight: Optional[torch.Tensor], scale: Optional[torch.Tensor],
+                                channels: int, want_dx: bool = True, want_dw: bool = True,
+                                want_dbias: bool = True, out_dtype=None,
+                                workspace: Optional[torch.Tensor] = None):
+    """dy [..][N], the kept rows [M][K128] of x [..][K = channels], the quantised weight ->
+    (dx [..][K] in out_dtype (dy's if None), dw [N][K] f32, dbias [N] f32), None for what
+    is not wanted. rows may be None without want_dw, the weight without want_dx."""
+    N, K = dy.shape[-1], channels
+    M, dld = _matrix_rows(dy, N)
+    if want_dw and (rows is None or row_scale is None) or \
+            want_dx and (weight is None or scale is None):
+        raise ValueError("dw needs the kept rows, dx the weight")
+    if not (want_dx or want_dw or want_dbias):
+        raise ValueError("nothing is wanted")
+    _on_device(dy.device, rows, row_scale, weight, scale, workspace)
+    if want_dw:
+        _int8_operand(rows, row_scale, K, "rows")
+        if rows.shape[0] != M:
+            raise ValueError("dy and rows must have as many rows")
+    if want_dx:
+        _int8_operand(weight, scale, K, "weight")
+        if weight.shape[0] != N:
+            raise ValueError("dy must have the weight's output channels")
+    f32 = dict(dtype=torch.float32, device=dy.device)
+    dx = torch.empty(tuple(dy.shape[:-1]) + (K,), dtype=_torch_dt(out_dtype or dy.dtype),
+                     device=dy.device) if want_dx else None
+    dw = torch.empty((N, K), **f32) if want_dw else None
+    db = torch.empty((N,), **f32) if want_dbias else None
+    ws = _workspace(_lib.pvconv_int8_linear_backward_workspace_size(M, K, N), workspace, dy.device)
+    _check("pvconv_int8_linear_backward", _lib.pvconv_int8_linear_backward(
+        _ptr(dy), _dt(dy), dld, _ptr(rows) if want_dw else None,
+        _ptr(row_scale) if want_dw else None, M, K, N, _ptr(weight) if want_dx else None,
+        _ptr(scale) if want_dx else None, _ptr(dx), _dt(dx) if want_dx else F32, 0, _ptr(dw),
+        _ptr(db), _ptr(ws), _ws_size(ws), _raw_stream(dy.device)))
     return dx, dw, db
 
 

@@ -34,6 +34,37 @@ inline size_t fp8_bytes(int rows, int cols) {
     return (size_t)rows * pv_fp8_blocks(cols) * PVCONV_FP8_BLOCK;
 }
 
+inline bool int8_sizes_ok(int M, int K, int N) {
+    const auto blocks = [](int n) { return ((long long)n + PVCONV_INT8_BLOCK - 1) / PVCONV_INT8_BLOCK; };
+    return M >= 0 && M <= (1 << 30) && K >= 1 && N >= 1 && K <= PVCONV_INT8_MAX_CHANNELS &&
+           N <= PVCONV_INT8_MAX_CHANNELS && blocks(M) * blocks(K > N ? K : N) <= (1LL << 26);
+}
+inline size_t int8_bytes(int rows, int cols) {
+    return (size_t)rows * (((size_t)cols + PVCONV_INT8_BLOCK - 1) / PVCONV_INT8_BLOCK) *
+           PVCONV_INT8_BLOCK;
+}
+
+// Byte ranges of which none may overlap an output.
+struct Ranges {
+    const void* p[16];
+    size_t bytes[16];
+    int n = 0;
+    void add(const void* q, size_t b) {
+        if (q && b) {
+            p[n] = q;
+            bytes[n++] = b;
+        }
+    }
+    // adds an output; false where it overlaps what is there
+    bool output(const void* q, size_t b) {
+        if (!q || !b) return true;
+        for (int i = 0; i < n; i++)
+            if (bytes_overlap(q, b, p[i], bytes[i])) return false;
+        add(q, b);
+        return true;
+    }
+};
+
 pvconv_status check_distill(const void* z, pvconv_dtype z_dt, int& z_ld, int M, int V,
                             const float* t_val, const int32_t* t_class, int top,
                             const int32_t* labels, float temperature, float alpha) {
@@ -255,6 +286,135 @@ pvconv_status pvconv_fp8_linear_backward(const void* dy, pvconv_dtype dy_dt, int
         PvRows{(void*)dy, dy_dt == PVCONV_BF16, dy_ld},
         PvRows{(void*)x, x_dt == PVCONV_BF16, x_ld}, M, K, N, weight_t, scale_t,
         PvRows{dx, dx_dt == PVCONV_BF16, dx_ld}, dw, dbias, workspace, as_stream(stream));
+}
+
+pvconv_status pvconv_int8_quantize(const void* x, pvconv_dtype x_dt, int x_ld, int R, int K,
+                                   int8_t* q, float* scale, void* stream) {
+    if (!int8_sizes_ok(0, K, 1) || R < 0 || R > (1 << 30) || !dtype_ok(x_dt)) return PVCONV_EINVAL;
+    if (x_ld == 0) x_ld = K;
+    if (x_ld < K) return PVCONV_EINVAL;
+    if (R == 0) return PVCONV_OK;
+    if (!x || !q || !scale || misaligned(x, esize(x_dt)) || misaligned(q, 16) ||
+        misaligned(scale, 4))
+        return PVCONV_EINVAL;
+    Ranges r;
+    r.add(x, row_bytes(R, K, x_ld, x_dt));
+    if (!r.output(q, int8_bytes(R, K)) || !r.output(scale, (size_t)R * 4)) return PVCONV_EINVAL;
+    return pv_launch_int8_quantize(PvRows{(void*)x, x_dt == PVCONV_BF16, x_ld}, R, K, q, scale,
+                                   as_stream(stream));
+}
+
+size_t pvconv_int8_linear_workspace_size(int M, int K, int N) {
+    return int8_sizes_ok(M, K, N) ? pv_int8_linear_ws_bytes(M, K, N, false) : 0;
+}
+size_t pvconv_int8_linear_rows_workspace_size(int M, int K, int N) {
+    return int8_sizes_ok(M, K, N) ? pv_int8_linear_ws_bytes(M, K, N, true) : 0;
+}
+
+pvconv_status pvconv_int8_linear(const void* x, pvconv_dtype x_dt, int x_ld, int M, int K, int N,
+                                 const int8_t* weight, const float* scale, const float* bias,
+                                 pvconv_act act, float slope, void* y, pvconv_dtype y_dt,
+                                 int y_ld, int8_t* rows, float* row_scale, void* workspace,
+                                 size_t workspace_bytes, void* stream) {
+    if (!int8_sizes_ok(M, K, N) || !dtype_ok(x_dt) || !dtype_ok(y_dt) || !act_ok(act))
+        return PVCONV_EINVAL;
+    if (x_ld == 0) x_ld = K;
+    if (y_ld == 0) y_ld = N;
+    if (x_ld < K || y_ld < N || (!rows) != (!row_scale)) return PVCONV_EINVAL;
+    if (M == 0) return PVCONV_OK;
+    if (!x || !weight || !scale || !y) return PVCONV_EINVAL;
+    if (misaligned(x, esize(x_dt)) || misaligned(weight, 16) || misaligned(scale, 4) ||
+        misaligned(bias, 4) || misaligned(y, esize(y_dt)) || misaligned(rows, 16) ||
+        misaligned(row_scale, 4))
+        return PVCONV_EINVAL;
+    Ranges r;
+    r.add(weight, int8_bytes(N, K));
+    r.add(scale, (size_t)N * 4);
+    r.add(bias, (size_t)N * 4);
+    if (overlap(x, M, K, x_ld, x_dt, y, N, y_ld, y_dt) ||
+        !r.output(y, row_bytes(M, N, y_ld, y_dt)))
+        return PVCONV_EINVAL;
+    r.add(x, row_bytes(M, K, x_ld, x_dt));
+    if (!r.output(rows, int8_bytes(M, K)) || !r.output(row_scale, (size_t)M * 4))
+        return PVCONV_EINVAL;
+    const pvconv_status st = check_ws(workspace, workspace_bytes,
+                                      pv_int8_linear_ws_bytes(M, K, N, rows != nullptr));
+    if (st != PVCONV_OK) return st;
+    return pv_launch_int8_linear(PvRows{(void*)x, x_dt == PVCONV_BF16, x_ld}, M, K, N, weight,
+                                 scale, bias, act, slope, PvRows{y, y_dt == PVCONV_BF16, y_ld},
+                                 rows, row_scale, workspace, as_stream(stream));
+}
+
+pvconv_status pvconv_int8_linear_rows(const int8_t* rows, const float* row_scale, int M, int K,
+                                      int N, const int8_t* weight, const float* scale,
+                                      const float* bias, pvconv_act act, float slope, void* y,
+                                      pvconv_dtype y_dt, int y_ld, void* workspace,
+                                      size_t workspace_bytes, void* stream) {
+    if (!int8_sizes_ok(M, K, N) || !dtype_ok(y_dt) || !act_ok(act)) return PVCONV_EINVAL;
+    if (y_ld == 0) y_ld = N;
+    if (y_ld < N) return PVCONV_EINVAL;
+    if (M == 0) return PVCONV_OK;
+    if (!rows || !row_scale || !weight || !scale || !y) return PVCONV_EINVAL;
+    if (misaligned(rows, 16) || misaligned(row_scale, 4) || misaligned(weight, 16) ||
+        misaligned(scale, 4) || misaligned(bias, 4) || misaligned(y, esize(y_dt)))
+        return PVCONV_EINVAL;
+    Ranges r;
+    r.add(rows, int8_bytes(M, K));
+    r.add(row_scale, (size_t)M * 4);
+    r.add(weight, int8_bytes(N, K));
+    r.add(scale, (size_t)N * 4);
+    r.add(bias, (size_t)N * 4);
+    if (!r.output(y, row_bytes(M, N, y_ld, y_dt))) return PVCONV_EINVAL;
+    const pvconv_status st =
+        check_ws(workspace, workspace_bytes, pv_int8_linear_ws_bytes(M, K, N, true));
+    if (st != PVCONV_OK) return st;
+    return pv_launch_int8_linear_rows(rows, row_scale, M, K, N, weight, scale, bias, act, slope,
+                                      PvRows{y, y_dt == PVCONV_BF16, y_ld}, workspace,
+                                      as_stream(stream));
+}
+
+size_t pvconv_int8_linear_backward_workspace_size(int M, int K, int N) {
+    return int8_sizes_ok(M, K, N) ? pv_int8_linear_bwd_ws_bytes(M, K, N) : 0;
+}
+
+pvconv_status pvconv_int8_linear_backward(const void* dy, pvconv_dtype dy_dt, int dy_ld,
+                                          const int8_t* rows, const float* row_scale, int M,
+                                          int K, int N, const int8_t* weight,
+                                          const float* scale, void* dx, pvconv_dtype dx_dt,
+                                          int dx_ld, float* dw, float* dbias, void* workspace,
+                                          size_t workspace_bytes, void* stream) {
+    if (!int8_sizes_ok(M, K, N) || !dtype_ok(dy_dt) || !dtype_ok(dx_dt)) return PVCONV_EINVAL;
+    if (dy_ld == 0) dy_ld = N;
+    if (dx_ld == 0) dx_ld = K;
+    if (dy_ld < N || dx_ld < K || (!dx && !dw && !dbias)) return PVCONV_EINVAL;
+    if (M == 0 && !dw && !dbias) return PVCONV_OK;
+    if (M > 0 && (!dy || (dw && (!rows || !row_scale)) || (dx && (!weight || !scale))))
+        return PVCONV_EINVAL;
+    if (misaligned(dy, esize(dy_dt)) || misaligned(rows, 16) || misaligned(row_scale, 4) ||
+        misaligned(weight, 16) || misaligned(scale, 4) || misaligned(dx, esize(dx_dt)) ||
+        misaligned(dw, 4) || misaligned(dbias, 4))
+        return PVCONV_EINVAL;
+    Ranges r;
+    if (dw) {
+        r.add(rows, int8_bytes(M, K));
+        r.add(row_scale, (size_t)M * 4);
+    }
+    if (dx) {
+        r.add(weight, int8_bytes(N, K));
+        r.add(scale, (size_t)N * 4);
+    }
+    if ((dx && overlap(dy, M, N, dy_ld, dy_dt, dx, K, dx_ld, dx_dt)) ||
+        !r.output(dx, row_bytes(M, K, dx_ld, dx_dt)))
+        return PVCONV_EINVAL;
+    r.add(dy, row_bytes(M, N, dy_ld, dy_dt));
+    if (!r.output(dw, (size_t)N * K * 4) || !r.output(dbias, (size_t)N * 4)) return PVCONV_EINVAL;
+    const pvconv_status st =
+        check_ws(workspace, workspace_bytes, pv_int8_linear_bwd_ws_bytes(M, K, N));
+    if (st != PVCONV_OK) return st;
+    return pv_launch_int8_linear_bwd(PvRows{(void*)dy, dy_dt == PVCONV_BF16, dy_ld}, rows,
+                                     row_scale, M, K, N, weight, scale,
+                                     PvRows{dx, dx_dt == PVCONV_BF16, dx_ld}, dw, dbias,
+                                     workspace, as_stream(stream));
 }
 
 size_t pvconv_distill_topk_workspace_size(int, int) { return 0; }

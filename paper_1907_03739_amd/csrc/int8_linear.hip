@@ -1,0 +1,445 @@
+// Linear layer in 8-bit integers, a scale for each row of x and of the weight, and
+// its gradients from the quantised rows (pvconv_train.h).
+//
+// With s the scale of a row, the smallest bf16 number with 127 s >= its largest
+// magnitude, and q = round(v / s): out[m][n] = act(s_m s_n sum_k q[m][k] q[n][k] +
+// bias_n). The integer sums are exact, s_m s_n (16 bits) too: a result is rounded
+// when the sum becomes a float, by its scale, its bias and its type.
+#include "pv_product.h"
+#include "pv_wave.h"
+
+namespace {
+
+constexpr int kThreads = 256;
+
+// The row's scale from its largest magnitude's bits; NaN where a value is not finite.
+__device__ __forceinline__ float row_scale_of(uint32_t top) {
+    if (top >= 0x7f800000u) return __uint_as_float(0x7fc00000u);
+    const float a = __uint_as_float(top);
+    // a / 127 cut to eight bits, the next such number where 127 times it (fifteen
+    // bits: exact) falls short
+    uint32_t s = __float_as_uint(fmaxf(a / 127.f, 0x1p-126f)) & 0xffff0000u;
+    if (127.f * __uint_as_float(s) < a) s += 0x10000u;
+    return __uint_as_float(s);
+}
+
+// q = the whole number nearest to v / s, ties to even, as the low byte of the result.
+// v * inv is off by less than one step; the remainder v - q s is exact (q s has fifteen
+// bits), so that comparing it with s / 2 settles every border.
+__device__ __forceinline__ uint32_t quantise(float v, float s, float inv, float half) {
+    const float t = __builtin_fmaf(v, inv, 0x1.8p23f);  // rounds to a whole number
+    const float e = __builtin_fmaf(-(t - 0x1.8p23f), s, v);
+    uint32_t q = __float_as_uint(t);
+    if (__builtin_fabsf(e) >= half && (__builtin_fabsf(e) > half || (q & 1u)))
+        q += e > 0.f ? 1u : ~0u;
+    return q & 255u;
+}
+
+// N consecutive values of a row as bits of floats, zeros past its end.
+template <bool XB>
+__device__ __forceinline__ void load8(const PvRows& x, size_t row, int c0, int K, float (&v)[8]) {
+    if (c0 + 8 <= K) {
+        if constexpr (XB) {
+            const pv_u32x4 w = *(const pv_u32x4_any*)((const uint16_t*)x.p + row * x.ld + c0);
+#pragma unroll
+            for (int i = 0; i < 8; i++)
+                v[i] = __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+        } else {
+            const float* p = (const float*)x.p + row * x.ld + c0;
+            const pv_u32x4 w = *(const pv_u32x4_any*)p, y = *(const pv_u32x4_any*)(p + 4);
+#pragma unroll
+            for (int i = 0; i < 8; i++) v[i] = __uint_as_float(i < 4 ? w[i] : y[i - 4]);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; i++)
+            v[i] = c0 + i < K ? pv_load_one(x.p, XB, row * x.ld + c0 + i) : 0.f;
+    }
+}
+__device__ __forceinline__ uint32_t top8(const float (&v)[8]) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; i++) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
+    return m;
+}
+__device__ __forceinline__ uint2 bytes8(const float (&v)[8], float s) {
+    uint2 o = {0, 0};
+    if (!(s == s)) return o;
+    const float inv = 1.f / s, half = 0.5f * s;
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        o.x |= quantise(v[i], s, inv, half) << (8 * i);
+        o.y |= quantise(v[4 + i], s, inv, half) << (8 * i);
+    }
+    return o;
+}
+
+struct MaxBits {
+    __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t b) const {
+        return max(a, b);
+    }
+};
+
+// A row in the registers of a team of TEAM lanes (a wave, or the workgroup): V vectors
+// of eight a lane. A longer row is read twice.
+template <bool XB, int TEAM, int V>
+__global__ __launch_bounds__(kThreads) void pv_int8_quantise_kernel(PvRows x, int M, int K,
+                                                                    int8_t* q, float* scale) {
+    __shared__ uint32_t tops[kThreads / 64];
+    const int K128 = (K + kSlice - 1) / kSlice * kSlice, lane = threadIdx.x % TEAM;
+    constexpr int kRows = kThreads / TEAM;
+    for (size_t row0 = (size_t)blockIdx.x * kRows; row0 < (size_t)M;
+         row0 += (size_t)gridDim.x * kRows) {
+        const size_t row = row0 + threadIdx.x / TEAM;
+        const bool live = row < (size_t)M;
+        float v[V][8];
+        uint32_t top = 0;
+        if (live) {
+#pragma unroll
+            for (int u = 0; u < V; u++) load8<XB>(x, row, (u * TEAM + lane) * 8, K, v[u]);
+#pragma unroll
+            for (int u = 0; u < V; u++) top = max(top, top8(v[u]));
+            for (int c0 = (V * TEAM + lane) * 8; c0 < K; c0 += TEAM * 8) {
+                float w[8];
+                load8<XB>(x, row, c0, K, w);
+                top = max(top, top8(w));
+            }
+        }
+        top = wave_reduce(top, MaxBits());
+        if constexpr (TEAM > 64) {
+            tops[threadIdx.x >> 6] = top;
+            __syncthreads();
+#pragma unroll
+            for (int w = 0; w < kThreads / 64; w++) top = max(top, tops[w]);
+            __syncthreads();
+        }
+        if (!live) continue;
+        const float s = row_scale_of(top);
+        if (lane == 0) scale[row] = s;
+        int8_t* o = q + row * K128;
+#pragma unroll
+        for (int u = 0; u < V; u++) {
+            const int c0 = (u * TEAM + lane) * 8;
+            if (c0 < K128) *(uint2*)(o + c0) = bytes8(v[u], s);
+        }
+        for (int c0 = (V * TEAM + lane) * 8; c0 < K128; c0 += TEAM * 8) {
+            float w[8];
+            load8<XB>(x, row, c0, K, w);
+            *(uint2*)(o + c0) = bytes8(w, s);
+        }
+    }
+}
+
+// act of a layer: what is not a number stays so
+__device__ __forceinline__ float activate(float v, float neg, bool relu) {
+    return v < 0.f ? (relu ? 0.f : v * neg) : v;
+}
+
+struct LinearEpi {
+    static constexpr bool kLds = false;
+    const float* row_scale;
+    const float* col_scale;
+    const float* bias;
+    PvRows out;
+    float neg;
+    bool relu;
+    // acc s_m s_n + b, the same operations wherever it is formed: kept rows give the
+    // bits of the call that quantised them. The scales' product is exact unless it
+    // leaves the 32-bit range.
+    __device__ __forceinline__ static bool tame(float s) { return s >= 0x1p-60f && s <= 0x1p60f; }
+    __device__ __forceinline__ static float value(int acc, float sm, float sn, float b,
+                                                  bool fast) {
+        if (fast) return __builtin_fmaf((float)acc, sm * sn, b);
+        return (float)((double)acc * ((double)sm * (double)sn) + (double)b);
+    }
+    template <int MI>
+    __device__ __forceinline__ void tile(const PvProduct& p, int mw, int nw, int lane,
+                                         const pv_i32x4 (&acc)[4][MI], uint8_t*) const {
+        const int r = lane & 15, n = nw + 16 * (lane >> 4);
+        float sn[16], b[16];
+        bool fast = true;
+#pragma unroll
+        for (int c = 0; c < 16; c++) {
+            const int at = min(n + c, p.N - 1);
+            sn[c] = col_scale[at];
+            b[c] = bias ? bias[at] : 0.f;
+            fast = fast && tame(sn[c]);
+        }
+#pragma unroll
+        for (int i = 0; i < MI; i++) {
+            const int m = mw + 16 * i + r;
+            if (m >= p.M) continue;
+            const float sm = row_scale[m];
+            float v[16];
+            if (fast && tame(sm)) {
+#pragma unroll
+                for (int c = 0; c < 16; c++)
+                    v[c] = value(acc[c >> 2][i][c & 3], sm, sn[c], b[c], true);
+            } else {
+#pragma unroll
+                for (int c = 0; c < 16; c++)
+                    v[c] = value(acc[c >> 2][i][c & 3], sm, sn[c], b[c],
+                                 tame(sm) && tame(sn[c]));
+            }
+#pragma unroll
+            for (int c = 0; c < 16; c++) v[c] = activate(v[c], neg, relu);
+            pv_store_run<16>(out, m, n, p.N, v);
+        }
+    }
+    __device__ __forceinline__ void one(int m, int n, int acc) const {
+        const float sm = row_scale[m], sn = col_scale[n];
+        const float v = value(acc, sm, sn, bias ? bias[n] : 0.f, tame(sm) && tame(sn));
+        pv_store_one(out.p, out.bf16, (size_t)m * out.ld + n, activate(v, neg, relu));
+    }
+};
+
+// Few rows: a workgroup takes 16 rows by 16 columns. Its eight waves take the rows'
+// largest values, then a share of the 64-value pieces each, which a wave quantises in
+// registers where they are its matrix operand: lane (r, h) holds row r's values 16 h ..
+// of a piece. Their sums meet in LDS; one launch, no workspace.
+constexpr int kFewThreads = 512;
+template <bool XB>
+__global__ __launch_bounds__(kFewThreads) void pv_int8_few_kernel(PvRows x, int M, int K, int N,
+                                                                  const int8_t* w,
+                                                                  LinearEpi epi) {
+    constexpr int kWaves = kFewThreads / 64;
+    __shared__ float scales[16];
+    __shared__ int part[kWaves][256];
+    const int K128 = (K + kSlice - 1) / kSlice * kSlice, pieces = (K + 63) / 64;
+    const int nt = (N + 15) / 16;
+    const int m0 = (int)(blockIdx.x / nt) * 16, n0 = (int)(blockIdx.x % nt) * 16;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r = lane & 15, h = lane >> 4;
+    const int rows = min(16, M - m0);
+    for (int i = wave; i < 16; i += kWaves) {
+        uint32_t top = 0;
+        if (i < rows)
+            for (int c0 = lane * 8; c0 < K; c0 += 512) {
+                float v[8];
+                load8<XB>(x, m0 + i, c0, K, v);
+                top = max(top, top8(v));
+            }
+        top = wave_reduce(top, MaxBits());
+        if (lane == 0) scales[i] = row_scale_of(top);
+    }
+    __syncthreads();
+    const float s = scales[r];
+    const size_t row = min(m0 + r, M - 1);
+    const int8_t* gw = w + (size_t)min(n0 + r, N - 1) * K128 + h * 16;
+    pv_i32x4 acc = {0, 0, 0, 0};
+    for (int k = wave; k < pieces; k += kWaves) {
+        const pv_i32x4 fw = *(const pv_i32x4*)(gw + k * 64);
+        float v[2][8];
+        load8<XB>(x, row, k * 64 + h * 16, K, v[0]);
+        load8<XB>(x, row, k * 64 + h * 16 + 8, K, v[1]);
+        const uint2 a = bytes8(v[0], s), b = bytes8(v[1], s);
+        const pv_i32x4 fx = {(int)a.x, (int)a.y, (int)b.x, (int)b.y};
+        acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw, fx, acc, 0, 0, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; i++) part[wave][r * 16 + 4 * h + i] = acc[i];
+    __syncthreads();
+    const int i = threadIdx.x >> 4, c = threadIdx.x & 15;
+    if (threadIdx.x < 256 && i < rows && n0 + c < N) {
+        int sum = 0;
+#pragma unroll
+        for (int u = 0; u < kWaves; u++) sum += part[u][threadIdx.x];
+        const float sm = scales[i], sn = epi.col_scale[n0 + c];
+        const float v = LinearEpi::value(sum, sm, sn, epi.bias ? epi.bias[n0 + c] : 0.f,
+                                         LinearEpi::tame(sm) && LinearEpi::tame(sn));
+        pv_store_one(epi.out.p, epi.out.bf16, (size_t)(m0 + i) * epi.out.ld + n0 + c,
+                     activate(v, epi.neg, epi.relu));
+    }
+}
+// as long as each of its workgroups has a CU to itself
+constexpr int kFewTiles = 256;
+bool few(int M, int N) { return (size_t)((M + 15) / 16) * ((N + 15) / 16) <= kFewTiles; }
+
+PvProduct product_of(const int8_t* q, int M, int K, const int8_t* w, int N) {
+    PvProduct p{};
+    const size_t pitch = pv_up(K, kSlice);
+    p.a = PvPanel{(const uint8_t*)q, pitch, 0, 1};
+    p.b = PvPanel{(const uint8_t*)w, pitch, 0, 1};
+    p.M = M;
+    p.N = N;
+    p.slices = pv_slices(K, kSlice);
+    pv_pairs(p, 1, 1);
+    if (N <= 64)
+        pv_plan_splits(p, PvTileN::TM, PvTileN::TN, 8);
+    else
+        pv_plan_splits(p, PvTileM::TM, PvTileM::TN, 8);
+    return p;
+}
+
+struct LinearWs {
+    int8_t* q;
+    float* scale;
+    uint32_t* partial;
+    size_t total;
+};
+LinearWs carve_linear(void* base, int M, int K, int N, bool rows_given) {
+    PvCarve c{(char*)base, 0};
+    LinearWs w{nullptr, nullptr, nullptr, 0};
+    if (!rows_given) {
+        w.q = (int8_t*)c.take((size_t)M * pv_up(K, kSlice));
+        w.scale = (float*)c.take((size_t)M * 4);
+    }
+    w.partial = (uint32_t*)c.take(pv_partial_bytes(product_of(nullptr, M, K, nullptr, N)));
+    w.total = c.off;
+    return w;
+}
+
+// Parts that a gradient's scaled operand needs: one rounded part for a bf16 result,
+// the two that hold 8 by 8 bits for a bf16 dy, three for 32 bits.
+int parts_of(bool out_bf16, bool dy_bf16) { return out_bf16 ? 1 : dy_bf16 ? 2 : 3; }
+
+struct BwdWs {
+    PvPanel dys, wt, dyt, qt;
+    PvProduct dx, dw;
+    float* sums;
+    size_t total;
+};
+BwdWs carve_bwd(void* base, int M, int K, int N, bool dy_bf16, bool dx_bf16, bool want_dx,
+                bool want_dw, bool want_db) {
+    PvCarve c{(char*)base, 0};
+    BwdWs w{};
+    auto product = [&](PvProduct& p, const PvPanel& a, const PvPanel& b, int rows, int cols,
+                       int depth) {
+        p.a = a;
+        p.b = b;
+        p.M = rows;
+        p.N = cols;
+        p.slices = pv_slices(depth, 64);
+        pv_pairs(p, a.parts, b.parts);
+        pv_plan_plain(p);
+        p.partial = (uint32_t*)c.take(pv_partial_bytes(p));
+    };
+    if (want_dx && M > 0) {
+        w.dys = pv_take_panel(c, M, N, parts_of(dx_bf16, dy_bf16));
+        w.wt = pv_take_panel(c, K, N, 1);
+        product(w.dx, w.dys, w.wt, M, K, N);
+    }
+    if (want_dw) {
+        w.dyt = pv_take_panel(c, N, M, parts_of(false, dy_bf16));
+        w.qt = pv_take_panel(c, K, M, 1);
+        product(w.dw, w.dyt, w.qt, N, K, M);
+    }
+    if (want_db) w.sums = (float*)c.take(pv_column_sum_bytes(M, N));
+    w.total = c.off;
+    return w;
+}
+
+template <bool XB>
+void run_quantise(const PvRows& x, int M, int K, int8_t* q, float* scale, hipStream_t s) {
+    const int rows = K <= 2048 ? 4 : 1;
+    const dim3 grid(pv_blocks(M, rows));
+    if (K <= 512)
+        hipLaunchKernelGGL((pv_int8_quantise_kernel<XB, 64, 1>), grid, dim3(kThreads), 0, s, x, M,
+                           K, q, scale);
+    else if (K <= 2048)
+        hipLaunchKernelGGL((pv_int8_quantise_kernel<XB, 64, 4>), grid, dim3(kThreads), 0, s, x, M,
+                           K, q, scale);
+    else
+        hipLaunchKernelGGL((pv_int8_quantise_kernel<XB, 256, 4>), grid, dim3(kThreads), 0, s, x, M,
+                           K, q, scale);
+}
+
+}  // namespace
+
+pvconv_status pv_launch_int8_quantize(const PvRows& x, int M, int K, int8_t* q, float* scale,
+                                      hipStream_t s) {
+    if (x.bf16)
+        run_quantise<true>(x, M, K, q, scale, s);
+    else
+        run_quantise<false>(x, M, K, q, scale, s);
+    return pv_launch_status();
+}
+
+size_t pv_int8_linear_ws_bytes(int M, int K, int N, bool rows_given) {
+    if (!rows_given && few(M, N)) return carve_linear(nullptr, M, K, N, false).total;
+    return carve_linear(nullptr, M, K, N, rows_given).total;
+}
+
+static pvconv_status run_rows(const int8_t* q, const float* scale, int M, int K, int N,
+                              const int8_t* weight, const LinearEpi& epi, uint32_t* partial,
+                              hipStream_t s) {
+    PvProduct p = product_of(q, M, K, weight, N);
+    p.partial = partial;
+    if (N <= 64)
+        pv_run_tiles<true, PvTileN>(p, epi, s);
+    else
+        pv_run_tiles<true, PvTileM>(p, epi, s);
+    return pv_launch_status();
+}
+
+static LinearEpi epi_of(const float* row_scale, const float* weight_scale, const float* bias,
+                        int act, float slope, const PvRows& y) {
+    return LinearEpi{row_scale, weight_scale, bias, y,
+                     act == PVCONV_ACT_LEAKY ? slope : 1.f, act == PVCONV_ACT_RELU};
+}
+
+pvconv_status pv_launch_int8_linear(const PvRows& x, int M, int K, int N, const int8_t* weight,
+                                    const float* scale, const float* bias, int act, float slope,
+                                    const PvRows& y, int8_t* rows, float* row_scale, void* ws,
+                                    hipStream_t s) {
+    LinearEpi epi = epi_of(row_scale, scale, bias, act, slope, y);
+    if (!rows && few(M, N)) {
+        const dim3 grid((unsigned)((M + 15) / 16 * ((N + 15) / 16)));
+        if (x.bf16)
+            hipLaunchKernelGGL((pv_int8_few_kernel<true>), grid, dim3(kFewThreads), 0, s, x, M, K,
+                               N, weight, epi);
+        else
+            hipLaunchKernelGGL((pv_int8_few_kernel<false>), grid, dim3(kFewThreads), 0, s, x, M, K,
+                               N, weight, epi);
+        return pv_launch_status();
+    }
+    const LinearWs w = carve_linear(ws, M, K, N, rows != nullptr);
+    if (!rows) {
+        rows = w.q;
+        row_scale = w.scale;
+        epi.row_scale = w.scale;
+    }
+    const pvconv_status st = pv_launch_int8_quantize(x, M, K, rows, row_scale, s);
+    if (st != PVCONV_OK) return st;
+    return run_rows(rows, row_scale, M, K, N, weight, epi, w.partial, s);
+}
+
+pvconv_status pv_launch_int8_linear_rows(const int8_t* rows, const float* row_scale, int M, int K,
+                                         int N, const int8_t* weight, const float* scale,
+                                         const float* bias, int act, float slope, const PvRows& y,
+                                         void* ws, hipStream_t s) {
+    const LinearWs w = carve_linear(ws, M, K, N, true);
+    return run_rows(rows, row_scale, M, K, N, weight,
+                    epi_of(row_scale, scale, bias, act, slope, y), w.partial, s);
+}
+
+size_t pv_int8_linear_bwd_ws_bytes(int M, int K, int N) {
+    // the most that any of the types and outputs takes
+    return carve_bwd(nullptr, M, K, N, false, false, true, true, true).total;
+}
+
+pvconv_status pv_launch_int8_linear_bwd(const PvRows& dy, const int8_t* rows,
+                                        const float* row_scale, int M, int K, int N,
+                                        const int8_t* weight, const float* scale,
+                                        const PvRows& dx, float* dw, float* dbias, void* ws,
+                                        hipStream_t s) {
+    const BwdWs w = carve_bwd(ws, M, K, N, dy.bf16, dx.bf16, dx.p != nullptr, dw != nullptr,
+                              dbias != nullptr);
+    const PvKind kind = dy.bf16 ? kPvBf16 : kPvF32;
+    const size_t qk = pv_up(K, kSlice);
+    if (dx.p && M > 0) {
+        PvPack a = pv_pack_of(dy.p, kind, dy.ld, M, N, w.dys);
+        a.col_scale = scale;
+        pv_launch_pack(a, s);
+        pv_launch_pack_transposed(pv_pack_of(weight, kPvInt8, qk, N, K, w.wt), s);
+        pv_launch_plain(w.dx, PvPlain{dx, nullptr}, s);
+    }
+    if (dw) {
+        PvPack a = pv_pack_of(dy.p, kind, dy.ld, M, N, w.dyt);
+        a.row_scale = row_scale;
+        pv_launch_pack_transposed(a, s);
+        pv_launch_pack_transposed(pv_pack_of(rows, kPvInt8, qk, M, K, w.qt), s);
+        pv_launch_plain(w.dw, PvPlain{PvRows{dw, false, K}, nullptr}, s);
+    }
+    if (dbias) pv_launch_column_sum(dy, M, N, w.sums, dbias, s);
+    return pv_launch_status();
+}

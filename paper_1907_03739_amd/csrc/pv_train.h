@@ -1,5 +1,5 @@
 // Internal interface and device helpers of the operators declared in
-// pvconv_train.h: group norm, the 8-bit linear layer, the distillation loss.
+// pvconv_train.h: group norm, the 8-bit linear layers, the losses.
 #pragma once
 
 #include "pv_common.h"
@@ -104,6 +104,26 @@ pvconv_status pv_launch_fp8_linear_bwd(const PvRows& dy, const PvRows& x, int M,
                                        const uint8_t* weight_t, const uint8_t* scale_t,
                                        const PvRows& dx, float* dw, float* dbias, void* ws,
                                        hipStream_t s);
+
+// ---- linear layer in 8-bit integers (int8_linear.hip) ----------------------
+pvconv_status pv_launch_int8_quantize(const PvRows& x, int M, int K, int8_t* q, float* scale,
+                                      hipStream_t s);
+size_t pv_int8_linear_ws_bytes(int M, int K, int N, bool rows_given);
+// rows, row_scale: where the quantised x is kept, or NULL
+pvconv_status pv_launch_int8_linear(const PvRows& x, int M, int K, int N, const int8_t* weight,
+                                    const float* scale, const float* bias, int act, float slope,
+                                    const PvRows& y, int8_t* rows, float* row_scale, void* ws,
+                                    hipStream_t s);
+pvconv_status pv_launch_int8_linear_rows(const int8_t* rows, const float* row_scale, int M, int K,
+                                         int N, const int8_t* weight, const float* scale,
+                                         const float* bias, int act, float slope, const PvRows& y,
+                                         void* ws, hipStream_t s);
+size_t pv_int8_linear_bwd_ws_bytes(int M, int K, int N);
+pvconv_status pv_launch_int8_linear_bwd(const PvRows& dy, const int8_t* rows,
+                                        const float* row_scale, int M, int K, int N,
+                                        const int8_t* weight, const float* scale,
+                                        const PvRows& dx, float* dw, float* dbias, void* ws,
+                                        hipStream_t s);
 
 // ---- distillation loss (distill.hip) ---------------------------------------
 struct PvDistill {
