@@ -246,6 +246,50 @@ pvconv_status pvconv_distill_topk_backward(const void* z, pvconv_dtype z_dt, int
                                            void* dz, pvconv_dtype dz_dt, int dz_ld,
                                            void* stream);
 
+/* ------------------------------------------------------------------------- */
+/* Softmax cross entropy of a linear layer's outputs, without the logits.    */
+/*                                                                           */
+/* With z = x W^T + bias (never in memory whole: a piece of the classes at a  */
+/* time), a row m of label l:                                                */
+/*   lse_m = logsumexp(z_m),  loss_m = lse_m - z_ml,                         */
+/*   dz_m = row_weight_m (softmax(z_m) - onehot(l)),                         */
+/*   dx = dz W,  dw = dz^T x,  dbias_v = sum_m dz[m,v].                      */
+/* A label outside [0, V): loss and dz are 0. So they are for a row whose    */
+/* logits are all -inf; a class whose logit is -inf (by its bias) takes no   */
+/* part. A NaN or +inf logit makes its row's lse, loss and dz NaN. A row of  */
+/* weight 0 has dz = 0; x and W should be finite all the same, as dz         */
+/* multiplies them.                                                          */
+/* fp32 operands are multiplied to 24 bits, bf16 ones exactly, sums are fp32. */
+/* For a bf16 dx (dw), dz and W (x) are rounded to bf16 first; for an fp32   */
+/* one, dz is taken to 24 bits.                                              */
+/*  x       [M][K] (x_dt), row stride x_ld;  w [V][K] (w_dt), row stride w_ld */
+/*  bias    [V] fp32 or NULL;  labels [M] int32;  row_weight [M] fp32 or     */
+/*          NULL (1)                                                         */
+/*  loss    out [M] fp32;  lse out [M] fp32 or NULL, for the backward        */
+/*  dx      out [M][K] (dx_dt), dx_ld;  dw out [V][K] (dw_dt), contiguous;   */
+/*          dbias out [V] fp32; each NULL where not wanted                   */
+/* 0 <= M <= 2^24, 1 <= K <= PVCONV_CE_MAX_CHANNELS, 1 <= V <=               */
+/* PVCONV_MAX_CLASSES. The workspace sizes are those of a call with every    */
+/* gradient (want_grad) or none; for a backward, want_grad.                  */
+/* ------------------------------------------------------------------------- */
+#define PVCONV_CE_MAX_CHANNELS 65536
+size_t pvconv_linear_cross_entropy_workspace_size(int M, int K, int V, pvconv_dtype x_dt,
+                                                  pvconv_dtype w_dt, pvconv_dtype dx_dt,
+                                                  pvconv_dtype dw_dt, int want_grad);
+pvconv_status pvconv_linear_cross_entropy(
+    const void* x, pvconv_dtype x_dt, int x_ld, const void* w, pvconv_dtype w_dt, int w_ld, int M,
+    int K, int V, const float* bias, const int32_t* labels, const float* row_weight, float* loss,
+    float* lse, void* dx, pvconv_dtype dx_dt, int dx_ld, void* dw, pvconv_dtype dw_dt,
+    float* dbias, void* workspace, size_t workspace_bytes, void* stream);
+
+/* The gradients alone, from the lse of a forward with the same x, w and bias; */
+/* dloss [M] fp32 (or NULL: 1) in the place of row_weight.                   */
+pvconv_status pvconv_linear_cross_entropy_backward(
+    const void* x, pvconv_dtype x_dt, int x_ld, const void* w, pvconv_dtype w_dt, int w_ld, int M,
+    int K, int V, const float* bias, const int32_t* labels, const float* lse, const float* dloss,
+    void* dx, pvconv_dtype dx_dt, int dx_ld, void* dw, pvconv_dtype dw_dt, float* dbias,
+    void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -18,7 +18,8 @@ _BINDING_NAMES = (
     "pvconv_fp8_linear", "pvconv_fp8_linear_backward", "pvconv_int8_quantize",
     "pvconv_int8_linear", "pvconv_int8_linear_rows", "pvconv_int8_linear_backward",
     "pvconv_distill_topk",
-    "pvconv_distill_topk_backward",
+    "pvconv_distill_topk_backward", "pvconv_linear_cross_entropy",
+    "pvconv_linear_cross_entropy_backward",
 )
 
 __all__ = list(_BINDING_NAMES) + ["DeviceNetwork", "DeviceStudent"]

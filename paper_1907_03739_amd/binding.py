@@ -124,6 +124,12 @@ _SIGS_TRAIN = {
     "pvconv_int8_linear_backward_workspace_size": ([_I, _I, _I], _SZ),
     "pvconv_int8_linear_backward": ([_VP, _I, _I, _VP, _VP, _I, _I, _I, _VP, _VP, _VP, _I, _I,
                                      _VP, _VP, _VP, _SZ, _VP], _I),
+    "pvconv_linear_cross_entropy_workspace_size": ([_I] * 8, _SZ),
+    "pvconv_linear_cross_entropy": ([_VP, _I, _I, _VP, _I, _I, _I, _I, _I, _VP, _VP, _VP, _VP,
+                                     _VP, _VP, _I, _I, _VP, _I, _VP, _VP, _SZ, _VP], _I),
+    "pvconv_linear_cross_entropy_backward": ([_VP, _I, _I, _VP, _I, _I, _I, _I, _I, _VP, _VP,
+                                              _VP, _VP, _VP, _I, _I, _VP, _I, _VP, _VP, _SZ,
+                                              _VP], _I),
     "pvconv_distill_topk_workspace_size": ([_I, _I], _SZ),
     "pvconv_distill_topk": ([_VP, _I, _I, _I, _I, _VP, _VP, _I, _VP, _F, _F, _VP, _VP, _VP, _VP,
                              _I, _I, _VP, _SZ, _VP], _I),
@@ -1049,6 +1055,85 @@ def pvconv_distill_topk_backward(z: torch.Tensor, t_val: torch.Tensor, t_class: 
         _ptr(z), _dt(z), ld, M, V, _ptr(t_val), _ptr(t_class), top, labels_p, temperature, alpha,
         _ptr(lse), dloss_p, _ptr(dz), _dt(dz), dld, _raw_stream(z.device)))
     return dz
+
+
+def _ce_args(x, w, labels, bias, out_dtype, dw_dtype):
+    if x.dim() < 2 or w.dim() != 2:
+        raise ValueError("x must be [..][K], w [V][K]")
+    V, K = w.shape
+    M, ld = _matrix_rows(x, K)
+    _, wld = _matrix_rows(w, K)
+    xd, wd = _dt(x), _dt(w)
+    if out_dtype is not None:
+        out_dtype = _torch_dt(out_dtype)
+    if dw_dtype is not None:
+        dw_dtype = _torch_dt(dw_dtype)
+    return (M, K, V, ld, wld, xd, wd, _vector(labels, M, torch.int32, "labels"),
+            _vector(bias, V, torch.float32, "bias"), out_dtype or x.dtype, dw_dtype or w.dtype)
+
+
+def _ce_grads(x, M, K, V, dxt, dwt, want_dx, want_dw, want_dbias):
+    new = dict(device=x.device)
+    return (torch.empty(x.shape, dtype=dxt, **new) if want_dx else None,
+            torch.empty((V, K), dtype=dwt, **new) if want_dw else None,
+            torch.empty((V,), dtype=torch.float32, **new) if want_dbias else None)
+
+
+def pvconv_linear_cross_entropy(x: torch.Tensor, w: torch.Tensor, labels: torch.Tensor,
+                                bias: Optional[torch.Tensor] = None,
+                                row_weight: Optional[torch.Tensor] = None,
+                                want_grad: bool = False, want_dx: bool = True,
+                                want_dw: bool = True, want_dbias: bool = True, out_dtype=None,
+                                dw_dtype=None, workspace: Optional[torch.Tensor] = None):
+    """The cross entropy of labels with softmax(x W^T + bias), without the logits: x
+    [..][K] (rows evenly strided, M in all), w [V][K], labels [M] int32 (outside [0, V):
+    no loss, no gradient), bias [V] f32 -> (loss [M], lse [M]) f32, and with want_grad
+    (loss, lse, dx [..][K] in out_dtype (x's if None), dw [V][K] in dw_dtype (w's if
+    None), dbias [V] f32): the gradients of sum(row_weight * loss), None for what is not
+    wanted."""
+    M, K, V, ld, wld, xd, wd, labels_p, bias_p, dxt, dwt = _ce_args(x, w, labels, bias, out_dtype,
+                                                                   dw_dtype)
+    _on_device(x.device, w, labels, bias, row_weight, workspace)
+    weight_p = _vector(row_weight, M, torch.float32, "row_weight")
+    if want_grad and not (want_dx or want_dw or want_dbias):
+        raise ValueError("nothing is wanted")
+    loss = torch.empty((M,), dtype=torch.float32, device=x.device)
+    lse = torch.empty((M,), dtype=torch.float32, device=x.device)
+    dx, dw, db = _ce_grads(x, M, K, V, dxt, dwt, want_dx, want_dw, want_dbias) if want_grad \
+        else (None, None, None)
+    dxd, dwd = F32 if dxt is torch.float32 else BF16, F32 if dwt is torch.float32 else BF16
+    ws = _workspace(_lib.pvconv_linear_cross_entropy_workspace_size(
+        M, K, V, xd, wd, dxd, dwd, want_grad), workspace, x.device)
+    _check("pvconv_linear_cross_entropy", _lib.pvconv_linear_cross_entropy(
+        _ptr(x), xd, ld, _ptr(w), wd, wld, M, K, V, bias_p, labels_p, weight_p, _ptr(loss),
+        _ptr(lse), _ptr(dx), dxd, 0, _ptr(dw), dwd, _ptr(db), _ptr(ws), _ws_size(ws),
+        _raw_stream(x.device)))
+    return (loss, lse, dx, dw, db) if want_grad else (loss, lse)
+
+
+def pvconv_linear_cross_entropy_backward(x: torch.Tensor, w: torch.Tensor, labels: torch.Tensor,
+                                         lse: torch.Tensor,
+                                         dloss: Optional[torch.Tensor] = None,
+                                         bias: Optional[torch.Tensor] = None,
+                                         want_dx: bool = True, want_dw: bool = True,
+                                         want_dbias: bool = True, out_dtype=None, dw_dtype=None,
+                                         workspace: Optional[torch.Tensor] = None):
+    """The gradients (dx, dw, dbias) of sum(dloss * loss) from the forward's lse."""
+    M, K, V, ld, wld, xd, wd, labels_p, bias_p, dxt, dwt = _ce_args(x, w, labels, bias, out_dtype,
+                                                                   dw_dtype)
+    _on_device(x.device, w, labels, lse, dloss, bias, workspace)
+    dloss_p = _vector(dloss, M, torch.float32, "dloss")
+    lse_p = _vector(lse, M, torch.float32, "lse")
+    if not (want_dx or want_dw or want_dbias):
+        raise ValueError("nothing is wanted")
+    dx, dw, db = _ce_grads(x, M, K, V, dxt, dwt, want_dx, want_dw, want_dbias)
+    dxd, dwd = F32 if dxt is torch.float32 else BF16, F32 if dwt is torch.float32 else BF16
+    ws = _workspace(_lib.pvconv_linear_cross_entropy_workspace_size(
+        M, K, V, xd, wd, dxd, dwd, True), workspace, x.device)
+    _check("pvconv_linear_cross_entropy_backward", _lib.pvconv_linear_cross_entropy_backward(
+        _ptr(x), xd, ld, _ptr(w), wd, wld, M, K, V, bias_p, labels_p, lse_p, dloss_p, _ptr(dx),
+        dxd, 0, _ptr(dw), dwd, _ptr(db), _ptr(ws), _ws_size(ws), _raw_stream(x.device)))
+    return dx, dw, db
 
 
 class DeviceLayer:

@@ -65,6 +65,45 @@ struct Ranges {
     }
 };
 
+inline bool ce_sizes_ok(int M, int K, int V) {
+    return M >= 0 && M <= (1 << 24) && K >= 1 && K <= PVCONV_CE_MAX_CHANNELS && V >= 1 &&
+           V <= PVCONV_MAX_CLASSES;
+}
+// The arguments that a forward and a backward share; `r` gets the inputs' ranges.
+pvconv_status check_ce(PvLinearCe& a, pvconv_dtype x_dt, pvconv_dtype w_dt, pvconv_dtype dx_dt,
+                       pvconv_dtype dw_dt, Ranges& r) {
+    if (!ce_sizes_ok(a.M, a.K, a.V) || !dtype_ok(x_dt) || !dtype_ok(w_dt) || !dtype_ok(dx_dt) ||
+        !dtype_ok(dw_dt))
+        return PVCONV_EINVAL;
+    if (a.x.ld == 0) a.x.ld = a.K;
+    if (a.w.ld == 0) a.w.ld = a.K;
+    if (a.dx.ld == 0) a.dx.ld = a.K;
+    if (a.x.ld < a.K || a.w.ld < a.K || a.dx.ld < a.K) return PVCONV_EINVAL;
+    a.dw.ld = a.K;
+    a.x.bf16 = x_dt == PVCONV_BF16;
+    a.w.bf16 = w_dt == PVCONV_BF16;
+    a.dx.bf16 = dx_dt == PVCONV_BF16;
+    a.dw.bf16 = dw_dt == PVCONV_BF16;
+    if (a.M > 0 && (!a.x.p || !a.w.p || !a.labels)) return PVCONV_EINVAL;
+    if (misaligned(a.x.p, esize(x_dt)) || misaligned(a.w.p, esize(w_dt)) ||
+        misaligned(a.bias, 4) || misaligned(a.labels, 4) || misaligned(a.weight, 4) ||
+        misaligned(a.loss, 4) || misaligned(a.lse, 4) || misaligned(a.dx.p, esize(dx_dt)) ||
+        misaligned(a.dw.p, esize(dw_dt)) || misaligned(a.dbias, 4))
+        return PVCONV_EINVAL;
+    const size_t mb = (size_t)a.M * 4, vb = (size_t)a.V * 4;
+    r.add(a.w.p, row_bytes(a.V, a.K, a.w.ld, w_dt));
+    r.add(a.bias, vb);
+    r.add(a.labels, mb);
+    r.add(a.weight, mb);
+    if (a.dx.p && (overlap(a.x.p, a.M, a.K, a.x.ld, x_dt, a.dx.p, a.K, a.dx.ld, dx_dt) ||
+                   !r.output(a.dx.p, row_bytes(a.M, a.K, a.dx.ld, dx_dt))))
+        return PVCONV_EINVAL;
+    r.add(a.x.p, row_bytes(a.M, a.K, a.x.ld, x_dt));
+    if (!r.output(a.dw.p, row_bytes(a.V, a.K, a.K, dw_dt)) || !r.output(a.dbias, vb))
+        return PVCONV_EINVAL;
+    return PVCONV_OK;
+}
+
 pvconv_status check_distill(const void* z, pvconv_dtype z_dt, int& z_ld, int M, int V,
                             const float* t_val, const int32_t* t_class, int top,
                             const int32_t* labels, float temperature, float alpha) {
@@ -474,6 +513,65 @@ pvconv_status pvconv_distill_topk_backward(const void* z, pvconv_dtype z_dt, int
                                            t_val, t_class, top, labels, temperature, alpha},
                                  lse, dloss, PvRows{dz, dz_dt == PVCONV_BF16, dz_ld},
                                  as_stream(stream));
+}
+
+size_t pvconv_linear_cross_entropy_workspace_size(int M, int K, int V, pvconv_dtype x_dt,
+                                                  pvconv_dtype w_dt, pvconv_dtype dx_dt,
+                                                  pvconv_dtype dw_dt, int want_grad) {
+    if (!ce_sizes_ok(M, K, V) || !dtype_ok(x_dt) || !dtype_ok(w_dt) || !dtype_ok(dx_dt) ||
+        !dtype_ok(dw_dt))
+        return 0;
+    PvLinearCe a{};
+    float some;  // a gradient that is wanted: any address
+    a.M = M;
+    a.K = K;
+    a.V = V;
+    a.x.bf16 = x_dt == PVCONV_BF16;
+    a.w.bf16 = w_dt == PVCONV_BF16;
+    a.dx = PvRows{want_grad ? &some : nullptr, dx_dt == PVCONV_BF16, K};
+    a.dw = PvRows{want_grad ? &some : nullptr, dw_dt == PVCONV_BF16, K};
+    a.dbias = want_grad ? &some : nullptr;
+    return pv_linear_ce_ws_bytes(a, true, want_grad != 0);
+}
+
+pvconv_status pvconv_linear_cross_entropy(
+    const void* x, pvconv_dtype x_dt, int x_ld, const void* w, pvconv_dtype w_dt, int w_ld, int M,
+    int K, int V, const float* bias, const int32_t* labels, const float* row_weight, float* loss,
+    float* lse, void* dx, pvconv_dtype dx_dt, int dx_ld, void* dw, pvconv_dtype dw_dt,
+    float* dbias, void* workspace, size_t workspace_bytes, void* stream) {
+    PvLinearCe a{PvRows{(void*)x, false, x_ld}, PvRows{(void*)w, false, w_ld}, M, K, V, bias,
+                 labels, row_weight, loss, lse, PvRows{dx, false, dx_ld}, PvRows{dw, false, 0},
+                 dbias};
+    Ranges r;
+    pvconv_status st = check_ce(a, x_dt, w_dt, dx_dt, dw_dt, r);
+    if (st != PVCONV_OK) return st;
+    if (M == 0 && !dw && !dbias) return PVCONV_OK;
+    if (M > 0 && !loss) return PVCONV_EINVAL;
+    if (!r.output(loss, (size_t)M * 4) || !r.output(lse, (size_t)M * 4)) return PVCONV_EINVAL;
+    st = check_ws(workspace, workspace_bytes,
+                  pv_linear_ce_ws_bytes(a, true, dx || dw || dbias));
+    if (st != PVCONV_OK) return st;
+    return pv_launch_linear_ce(a, true, workspace, as_stream(stream));
+}
+
+pvconv_status pvconv_linear_cross_entropy_backward(
+    const void* x, pvconv_dtype x_dt, int x_ld, const void* w, pvconv_dtype w_dt, int w_ld, int M,
+    int K, int V, const float* bias, const int32_t* labels, const float* lse, const float* dloss,
+    void* dx, pvconv_dtype dx_dt, int dx_ld, void* dw, pvconv_dtype dw_dt, float* dbias,
+    void* workspace, size_t workspace_bytes, void* stream) {
+    PvLinearCe a{PvRows{(void*)x, false, x_ld}, PvRows{(void*)w, false, w_ld}, M, K, V, bias,
+                 labels, dloss, nullptr, (float*)lse, PvRows{dx, false, dx_ld},
+                 PvRows{dw, false, 0}, dbias};
+    Ranges r;
+    if (M > 0 && lse) r.add(lse, (size_t)M * 4);
+    pvconv_status st = check_ce(a, x_dt, w_dt, dx_dt, dw_dt, r);
+    if (st != PVCONV_OK) return st;
+    if (!dx && !dw && !dbias) return PVCONV_EINVAL;
+    if (M == 0 && !dw && !dbias) return PVCONV_OK;
+    if (M > 0 && !lse) return PVCONV_EINVAL;
+    st = check_ws(workspace, workspace_bytes, pv_linear_ce_ws_bytes(a, false, true));
+    if (st != PVCONV_OK) return st;
+    return pv_launch_linear_ce(a, false, workspace, as_stream(stream));
 }
 
 }  // extern "C"

@@ -1,0 +1,487 @@
+// Cross entropy of labels with the softmax of a linear layer's outputs, z = x W^T +
+// bias, and its gradients, without the logits in memory (pvconv_train.h).
+//
+// Forward: tiles of the product keep their logits in registers and leave a row's
+// maximum and its sum of exponentials for each 64 classes (and the label's logit);
+// the rows' statistics are joined in a second launch. Backward: the product again,
+// whose epilogue turns a logit into dz = weight (exp(z - lse) - [class = label]), in a
+// piece of the vocabulary at a time and in both orders, dz and its transpose, in bf16
+// parts: dx += dz W and dW = dz^T x are then plain products. Up to 64 classes, a wave
+// holds whole rows: loss and dz come from one product.
+#include "pv_product.h"
+#include "pv_wave.h"
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr float kInf = __builtin_huge_valf();
+
+struct DzPanel {  // where dz goes: bf16 parts, rows of a pitch in bytes (p NULL: nowhere)
+    uint8_t* p;
+    size_t pitch, part_bytes;
+    int parts;
+};
+
+struct Ce {
+    const float* bias;      // of the piece's first class, or NULL
+    const int32_t* labels;
+    int v0, V;              // the piece's first class; all classes
+    float2* stats;          // [M][nb]: maximum, sum of exponentials about it
+    int nb;
+    float* zlab;            // [M]: the label's logit
+    float* loss;
+    float* lse;
+    const float* weight;    // [M] or NULL
+    DzPanel dz, dzt;        // [M][piece], [piece][M]
+    float* sums;            // [row blocks][piece]: dz summed over a wave's rows, or NULL
+};
+
+__device__ __forceinline__ float lanes_max(float v) {  // over the lanes of a row
+    v = fmaxf(v, __shfl_xor(v, 16));
+    return fmaxf(v, __shfl_xor(v, 32));
+}
+__device__ __forceinline__ float lanes_sum(float v) {
+    v += __shfl_xor(v, 16);
+    return v + __shfl_xor(v, 32);
+}
+
+// The next bf16 part of v, which leaves v - part (dz is finite, or NaN whole).
+__device__ __forceinline__ uint32_t next_part2(float& a, float& b) {
+    const uint32_t w = pv_pack_bf16x2(a, b);
+    a -= __uint_as_float(w << 16);
+    b -= __uint_as_float(w & 0xffff0000u);
+    return w;
+}
+
+enum Mode { kStats, kWhole, kGrad };
+
+template <int MODE>
+struct CeEpi {
+    static constexpr bool kLds = MODE != kStats;
+    Ce c;
+
+    // dz of two times sixteen rows of a wave (row 16 i + r, sixteen columns a lane),
+    // part by part: rows by 32-byte runs, columns through LDS
+    __device__ __forceinline__ void store(const PvProduct& p, int m, int mw, int nw, int lane,
+                                          float (&d)[2][16], uint8_t* lds) const {
+        const int r = lane & 15, h = lane >> 4, n = nw + 16 * h;
+        const int parts = max(c.dz.p ? c.dz.parts : 0, c.dzt.p ? c.dzt.parts : 0);
+        for (int part = 0; part < parts; part++) {
+            uint32_t w[2][8];
+#pragma unroll
+            for (int i = 0; i < 2; i++)
+#pragma unroll
+                for (int q = 0; q < 8; q++) w[i][q] = next_part2(d[i][2 * q], d[i][2 * q + 1]);
+            if (c.dz.p && part < c.dz.parts && (size_t)n * 2 < c.dz.pitch) {
+#pragma unroll
+                for (int i = 0; i < 2; i++) {
+                    if (m + 16 * i >= p.M) continue;
+                    pv_u32x4* o = (pv_u32x4*)(c.dz.p + part * c.dz.part_bytes +
+                                              (size_t)(m + 16 * i) * c.dz.pitch + (size_t)n * 2);
+                    o[0] = pv_u32x4{w[i][0], w[i][1], w[i][2], w[i][3]};
+                    o[1] = pv_u32x4{w[i][4], w[i][5], w[i][6], w[i][7]};
+                }
+            }
+            if (!c.dzt.p || part >= c.dzt.parts) continue;
+            // [64 columns][32 rows] of bf16; 16-byte pieces at piece ^ (column >> 4)
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int i = 0; i < 2; i++)
+#pragma unroll
+                for (int q = 0; q < 8; q++) {
+                    const int at = (((2 * i + (r >> 3)) ^ h) << 4) + (r & 7) * 2;
+                    *(uint16_t*)(lds + (16 * h + 2 * q) * 64 + at) = (uint16_t)w[i][q];
+                    *(uint16_t*)(lds + (16 * h + 2 * q + 1) * 64 + at) = (uint16_t)(w[i][q] >> 16);
+                }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int u = 0; u < 4; u++) {
+                const int col = u * 16 + (lane >> 2), piece = lane & 3;
+                const pv_u32x4 v = *(const pv_u32x4*)(lds + col * 64 + ((piece ^ u) << 4));
+                const size_t at = (size_t)(mw + 8 * piece) * 2;
+                if (nw + col < p.N && at < c.dzt.pitch)
+                    *(pv_u32x4*)(c.dzt.p + part * c.dzt.part_bytes +
+                                 (size_t)(nw + col) * c.dzt.pitch + at) = v;
+            }
+        }
+    }
+
+    template <int MI>
+    __device__ __forceinline__ void tile(const PvProduct& p, int mw, int nw, int lane,
+                                         const pv_f32x4 (&acc)[4][MI], uint8_t* lds) const {
+        const int r = lane & 15, h = lane >> 4, n = nw + 16 * h;
+        float b[16], cs[16];
+#pragma unroll
+        for (int q = 0; q < 16; q++) {
+            b[q] = c.bias ? c.bias[min(n + q, p.N - 1)] : 0.f;
+            cs[q] = 0.f;
+        }
+        const bool grads = MODE == kGrad || (MODE == kWhole && (c.dz.p || c.dzt.p || c.sums));
+#pragma unroll
+        for (int i0 = 0; i0 < MI; i0 += 2) {
+            float d[2][16];
+#pragma unroll
+            for (int i = 0; i < 2; i++) {
+                const int m = mw + 16 * (i0 + i) + r, mc = min(m, p.M - 1);
+                const int label = c.labels[mc], at = label - c.v0 - n;
+                const bool known = label >= 0 && label < c.V;
+                float z[16];
+#pragma unroll
+                for (int q = 0; q < 16; q++) {
+                    z[q] = acc[q >> 2][i0 + i][q & 3] + b[q];
+                    // columns past the last hold a copy of it: a logit that is not a
+                    // number there would stay one
+                    if (n + q >= p.N) z[q] = -kInf;
+                }
+                float lse = 0.f;
+                if constexpr (MODE != kGrad) {
+                    float top = z[0];
+#pragma unroll
+                    for (int q = 1; q < 16; q++) top = fmaxf(top, z[q]);
+                    top = lanes_max(top);
+                    // (every logit -inf, or not a number: fmaxf passes NaN over)
+                    const float about = top == -kInf ? 0.f : top;
+                    float sum = 0.f, zl = 0.f;
+#pragma unroll
+                    for (int q = 0; q < 16; q++) {
+                        sum += __expf(z[q] - about);
+                        if (q == at) zl = z[q];
+                    }
+                    sum = lanes_sum(sum);
+                    if constexpr (MODE == kStats) {
+                        if (m < p.M) {
+                            if (h == 0 && nw < p.N)
+                                c.stats[(size_t)m * c.nb + (unsigned)nw / 64] =
+                                    make_float2(top, sum);
+                            if (known && (unsigned)at < 16u) c.zlab[m] = zl;
+                        }
+                    } else {
+                        lse = sum == 0.f ? -kInf : about + logf(sum);
+                        zl = lanes_sum(known && (unsigned)at < 16u ? zl : 0.f);
+                        if (m < p.M && h == 0) {
+                            c.lse[m] = lse;
+                            c.loss[m] = known && lse != -kInf ? lse - zl : 0.f;
+                        }
+                    }
+                } else {
+                    lse = c.lse[mc];
+                }
+                if (grads) {
+                    float g = m < p.M && known && lse != -kInf ? 1.f : 0.f;
+                    if (g != 0.f && c.weight) g = c.weight[mc];
+#pragma unroll
+                    for (int q = 0; q < 16; q++) {
+                        const float e = __expf(z[q] - lse) - (q == at ? 1.f : 0.f);
+                        d[i][q] = g == 0.f ? 0.f : n + q < p.N ? g * e : 0.f;
+                        cs[q] += d[i][q];
+                    }
+                }
+            }
+            if (MODE != kStats && grads)
+                store(p, mw + 16 * i0 + r, mw + 16 * i0, nw, lane, d, lds);
+        }
+        if (MODE != kStats && grads && c.sums) {
+            // over the 16 rows of lanes: halves of the columns change places, so that
+            // lane r is left with column r's sum
+#pragma unroll
+            for (int w = 8; w; w >>= 1) {
+                const bool up = r & w;
+#pragma unroll
+                for (int q = 0; q < w; q++) {
+                    const float keep = up ? cs[q + w] : cs[q], give = up ? cs[q] : cs[q + w];
+                    cs[q] = keep + __shfl_xor(give, w);
+                }
+            }
+            const int block = mw / (16 * MI);
+            if (n + r < p.N) c.sums[(size_t)block * p.N + n + r] = cs[0];
+        }
+    }
+    __device__ __forceinline__ void one(int, int, float) const {}  // never split
+};
+
+// A row's statistics over the piece's blocks (TEAM lanes a row), joined with those of
+// the pieces before it (run), and at the last piece lse and loss.
+struct Join {
+    const float2* stats;
+    int nb, M, V;
+    float2* run;
+    bool first, last;
+    const int32_t* labels;
+    const float* zlab;
+    float* loss;
+    float* lse;
+};
+template <int TEAM>
+__global__ __launch_bounds__(kThreads) void pv_ce_join_kernel(Join j) {
+    constexpr int kRows = kThreads / TEAM;
+    const int lane = threadIdx.x % TEAM;
+    for (size_t row0 = (size_t)blockIdx.x * kRows; row0 < (size_t)j.M;
+         row0 += (size_t)gridDim.x * kRows) {
+        const size_t m = min(row0 + threadIdx.x / TEAM, (size_t)j.M - 1);
+        float top = -kInf, sum = 0.f;
+        auto add = [&](float t, float s) {
+            const float to = fmaxf(top, t);
+            const float about = to == -kInf ? 0.f : to;
+            // -inf about a finite value: exp gives 0. Sums that are not numbers stay so.
+            sum = sum * __expf(top - about) + s * __expf(t - about);
+            top = to;
+        };
+        for (int k = lane; k < j.nb; k += TEAM) {
+            const float2 v = j.stats[m * j.nb + k];
+            add(v.x, v.y);
+        }
+#pragma unroll
+        for (int w = 1; w < TEAM; w <<= 1) {
+            const float t = __shfl_xor(top, w), s = __shfl_xor(sum, w);
+            add(t, s);
+        }
+        if (lane || row0 + threadIdx.x / TEAM >= (size_t)j.M) continue;
+        if (!j.first) add(j.run[m].x, j.run[m].y);
+        if (!j.last) {
+            j.run[m] = make_float2(top, sum);
+            continue;
+        }
+        const float lse = sum == 0.f ? -kInf : (top == -kInf ? 0.f : top) + logf(sum);
+        const int label = j.labels[m];
+        j.lse[m] = lse;
+        j.loss[m] = label >= 0 && label < j.V && lse != -kInf ? lse - j.zlab[m] : 0.f;
+    }
+}
+
+// ---- the plan --------------------------------------------------------------
+constexpr int kWholeClasses = 64;
+// dz of a piece: at most this many bytes of all its parts, at least this many classes
+// (each piece reads and writes the 32-bit sums of dx)
+constexpr size_t kPieceBytes = (size_t)1 << 29;
+constexpr int kLeastClasses = 2048;
+// statistics of a piece of the forward
+constexpr size_t kStatsBytes = (size_t)1 << 26;
+
+int parts_of(bool bf16) { return bf16 ? 1 : 3; }
+
+struct Plan {
+    PvPanel x, w;             // what the logits are products of
+    bool pack_x, pack_w;
+    bool whole;
+    int forward_classes, classes;  // a piece's
+    PvPanel dz, dzt, wt, xt;
+    PvProduct dx, dw;         // of a piece of `classes`
+    float2 *stats, *run;
+    float *zlab, *lse, *sums, *acc;
+    int blocks;               // of dbias's partial sums
+    uint32_t* partial;
+    size_t total;
+};
+
+bool direct(const PvRows& r, int K) {
+    return r.bf16 && K % 64 == 0 && r.ld % 8 == 0 && pv_aligned16(r.p);
+}
+
+int row_blocks(int M, bool narrow) {
+    return narrow ? (int)pv_up(M, PvTileN::TM) / (16 * PvTileN::MI)
+                  : (int)pv_up(M, PvTileM::TM) / (16 * PvTileM::MI);
+}
+
+Plan carve(void* base, const PvLinearCe& a, bool forward, bool grads, bool may_direct) {
+    PvCarve c{(char*)base, 0};
+    Plan p{};
+    p.whole = a.V <= kWholeClasses;
+    auto operand = [&](const PvRows& r, int rows, PvPanel& to, bool& pack) {
+        pack = !(may_direct && direct(r, a.K));
+        if (pack)
+            to = pv_take_panel(c, rows, a.K, parts_of(r.bf16));
+        else
+            to = PvPanel{(const uint8_t*)r.p, (size_t)r.ld * 2, 0, 1};
+    };
+    operand(a.x, a.M, p.x, p.pack_x);
+    operand(a.w, a.V, p.w, p.pack_w);
+    if (forward) {
+        if (!p.whole) {
+            const size_t most = kStatsBytes / 8 / (a.M > 0 ? a.M : 1) * 64;
+            p.forward_classes =
+                most >= (size_t)a.V ? a.V : (int)(most < 4096 ? 4096 : most / 128 * 128);
+            if (p.forward_classes > a.V) p.forward_classes = a.V;
+            p.stats = (float2*)c.take((size_t)a.M * ((p.forward_classes + 63) / 64) * 8);
+            p.run = (float2*)c.take((size_t)a.M * 8);
+            p.zlab = (float*)c.take((size_t)a.M * 4);
+        }
+        p.lse = (float*)c.take((size_t)a.M * 4);
+    }
+    if (!grads) {
+        p.total = c.off;
+        return p;
+    }
+    const bool want_dx = a.dx.p != nullptr, want_dw = a.dw.p != nullptr;
+    const int px = parts_of(a.dx.bf16), pw = parts_of(a.dw.bf16);
+    // (of both, wanted or not: the workspace of fewer gradients is then no larger)
+    const size_t per = pv_up(a.M > 0 ? a.M : 1, 64) * 2 * (px + pw);
+    size_t n = kPieceBytes / per / 256 * 256;
+    if (n < (size_t)kLeastClasses) n = kLeastClasses;
+    p.classes = n >= (size_t)a.V ? a.V : (int)n;
+    auto product = [&](PvProduct& q, const PvPanel& x, const PvPanel& y, int rows, int cols,
+                       int depth) {
+        q.a = x;
+        q.b = y;
+        q.M = rows;
+        q.N = cols;
+        q.slices = pv_slices(depth, 64);
+        pv_pairs(q, x.parts, y.parts);
+        pv_plan_plain(q);
+    };
+    // the splits' sums of a whole piece and of the last one, which may have fewer classes
+    size_t partial = 0;
+    const int tail = a.V % p.classes;
+    auto sums = [&](PvProduct q) {
+        const size_t b = pv_partial_bytes(q);
+        partial = partial > b ? partial : b;
+    };
+    if (want_dx) {
+        p.dz = pv_take_panel(c, a.M, p.classes, px);
+        p.wt = pv_take_panel(c, a.K, p.classes, a.dx.bf16 ? 1 : parts_of(a.w.bf16));
+        product(p.dx, p.dz, p.wt, a.M, a.K, p.classes);
+        sums(p.dx);
+        if (tail) {
+            PvProduct q = p.dx;
+            q.slices = pv_slices(tail, 64);
+            pv_plan_plain(q);
+            sums(q);
+        }
+        if (p.classes < a.V) p.acc = (float*)c.take((size_t)a.M * a.K * 4);
+    }
+    if (want_dw) {
+        p.dzt = pv_take_panel(c, p.classes, a.M, pw);
+        p.xt = pv_take_panel(c, a.K, a.M, a.dw.bf16 ? 1 : parts_of(a.x.bf16));
+        product(p.dw, p.dzt, p.xt, p.classes, a.K, a.M);
+        sums(p.dw);
+        if (tail) {
+            PvProduct q = p.dw;
+            q.M = tail;
+            pv_plan_plain(q);
+            sums(q);
+        }
+    }
+    p.partial = (uint32_t*)c.take(partial);
+    if (a.dbias) {
+        p.blocks = row_blocks(a.M, p.whole);
+        p.sums = (float*)c.take((size_t)p.blocks * p.classes * 4);
+    }
+    p.total = c.off;
+    return p;
+}
+
+template <int MODE>
+void run_logits(const PvProduct& p, const Ce& c, bool narrow, hipStream_t s) {
+    const CeEpi<MODE> epi{c};
+    if (MODE == kWhole || narrow)
+        pv_run_tiles<false, PvTileN>(p, epi, s);
+    else
+        pv_run_tiles<false, PvTileM>(p, epi, s);
+}
+
+}  // namespace
+
+size_t pv_linear_ce_ws_bytes(const PvLinearCe& a, bool forward, bool grads) {
+    return carve(nullptr, a, forward, grads, false).total;
+}
+
+pvconv_status pv_launch_linear_ce(const PvLinearCe& a, bool forward, void* ws, hipStream_t s) {
+    const bool grads = a.dx.p || a.dw.p || a.dbias;
+    const Plan p = carve(ws, a, forward, grads, true);
+    float* lse = a.lse ? a.lse : p.lse;
+    auto kind = [](const PvRows& r) { return r.bf16 ? kPvBf16 : kPvF32; };
+    if (p.pack_x) pv_launch_pack(pv_pack_of(a.x.p, kind(a.x), a.x.ld, a.M, a.K, p.x), s);
+    if (p.pack_w && a.M > 0)
+        pv_launch_pack(pv_pack_of(a.w.p, kind(a.w), a.w.ld, a.V, a.K, p.w), s);
+    // the product of a run of classes, whose epilogue is given
+    auto logits = [&](int v0, int n) {
+        PvProduct q{};
+        q.a = p.x;
+        q.b = p.w;
+        q.b.p += (size_t)v0 * p.w.pitch;
+        q.M = a.M;
+        q.N = n;
+        q.slices = pv_slices(a.K, 64);
+        pv_pairs(q, p.x.parts, p.w.parts);
+        q.per = q.slices * q.pairs;
+        q.splits = 1;
+        return q;
+    };
+    Ce c{};
+    c.labels = a.labels;
+    c.V = a.V;
+    c.weight = a.weight;
+    c.lse = lse;
+    c.loss = a.loss;
+    auto panel = [](const PvPanel& q) {
+        return DzPanel{(uint8_t*)q.p, q.pitch, q.part_bytes, q.parts};
+    };
+    if (forward && !p.whole) {
+        for (int v0 = 0; v0 < a.V; v0 += p.forward_classes) {
+            const int n = a.V - v0 < p.forward_classes ? a.V - v0 : p.forward_classes;
+            c.v0 = v0;
+            c.bias = a.bias ? a.bias + v0 : nullptr;
+            c.stats = p.stats;
+            c.nb = (n + 63) / 64;
+            c.zlab = p.zlab;
+            run_logits<kStats>(logits(v0, n), c, false, s);
+            const Join j{p.stats, c.nb, a.M, a.V, p.run, v0 == 0, v0 + n == a.V, a.labels, p.zlab,
+                         a.loss, lse};
+            if (a.M > 0) {
+                if (c.nb <= 8)
+                    hipLaunchKernelGGL((pv_ce_join_kernel<1>), dim3(pv_blocks(a.M, kThreads)),
+                                       dim3(kThreads), 0, s, j);
+                else
+                    hipLaunchKernelGGL((pv_ce_join_kernel<64>), dim3(pv_blocks(a.M, 4)),
+                                       dim3(kThreads), 0, s, j);
+            }
+        }
+    } else if (forward && !grads) {
+        c.bias = a.bias;
+        run_logits<kWhole>(logits(0, a.V), c, true, s);
+    }
+    if (!grads) return pv_launch_status();
+    if (a.dw.p) pv_launch_pack_transposed(pv_pack_of(a.x.p, kind(a.x), a.x.ld, a.M, a.K, p.xt), s);
+    for (int v0 = 0; v0 < a.V; v0 += p.classes) {
+        const int n = a.V - v0 < p.classes ? a.V - v0 : p.classes;
+        c.v0 = v0;
+        c.bias = a.bias ? a.bias + v0 : nullptr;
+        c.sums = p.sums;
+        PvPanel dz = p.dz, dzt = p.dzt, wt = p.wt;
+        dz.pitch = wt.pitch = pv_up(n, 64) * 2;
+        c.dz = panel(dz);
+        c.dzt = panel(dzt);
+        if (p.whole && forward)
+            run_logits<kWhole>(logits(v0, n), c, true, s);
+        else
+            run_logits<kGrad>(logits(v0, n), c, p.whole, s);
+        if (a.dx.p && a.M > 0) {
+            const size_t es = a.w.bf16 ? 2 : 4;
+            pv_launch_pack_transposed(
+                pv_pack_of((const char*)a.w.p + (size_t)v0 * a.w.ld * es, kind(a.w), a.w.ld, n,
+                           a.K, wt),
+                s);
+            PvProduct q = p.dx;
+            q.a = dz;
+            q.b = wt;
+            q.slices = pv_slices(n, 64);
+            pv_plan_plain(q);
+            q.partial = p.partial;
+            const bool last = v0 + n == a.V;
+            pv_launch_plain(q, PvPlain{last ? a.dx : PvRows{p.acc, false, a.K},
+                                       v0 ? p.acc : nullptr}, s);
+        }
+        if (a.dw.p) {
+            PvProduct q = p.dw;
+            q.M = n;
+            pv_plan_plain(q);
+            q.partial = p.partial;
+            const size_t es = a.dw.bf16 ? 2 : 4;
+            pv_launch_plain(q, PvPlain{PvRows{(char*)a.dw.p + (size_t)v0 * a.dw.ld * es,
+                                              a.dw.bf16, a.dw.ld}, nullptr}, s);
+        }
+        if (a.dbias) pv_launch_sum_parts(p.sums, p.blocks, n, a.dbias + v0, s);
+    }
+    return pv_launch_status();
+}

@@ -204,6 +204,10 @@ void pv_launch_plain(const PvProduct& p, const PvPlain& e, hipStream_t s) {
         pv_run_tiles<false, PvTileM>(p, epi, s);
 }
 
+void pv_launch_sum_parts(const float* partial, int parts, int N, float* out, hipStream_t s) {
+    hipLaunchKernelGGL(pv_sum_parts_kernel, dim3((N + 15) / 16), dim3(kThreads), 0, s, partial,
+                       parts, N, out);
+}
 size_t pv_column_sum_bytes(int M, int N) { return (size_t)((M + kSumRows - 1) / kSumRows) * N * 4; }
 void pv_launch_column_sum(const PvRows& x, int M, int N, float* partial, float* out,
                           hipStream_t s) {
@@ -211,6 +215,5 @@ void pv_launch_column_sum(const PvRows& x, int M, int N, float* partial, float* 
     if (parts)
         hipLaunchKernelGGL(pv_column_sum_kernel, dim3(pv_blocks((size_t)parts * ((N + 63) / 64), 1)),
                            dim3(kThreads), 0, s, x, M, N, partial);
-    hipLaunchKernelGGL(pv_sum_parts_kernel, dim3((N + 15) / 16), dim3(kThreads), 0, s, partial,
-                       parts, N, out);
+    pv_launch_sum_parts(partial, parts, N, out, s);
 }

@@ -368,7 +368,9 @@ static inline PvPack pv_pack_of(const void* src, PvKind kind, size_t ld, int R, 
                   to.part_bytes};
 }
 
-// Column sums of rows of channels in a fixed order (a linear layer's bias gradient).
+// Sums [parts][N] joined in a fixed order, and column sums of rows of channels (a linear
+// layer's bias gradient).
+void pv_launch_sum_parts(const float* partial, int parts, int N, float* out, hipStream_t s);
 size_t pv_column_sum_bytes(int M, int N);
 void pv_launch_column_sum(const PvRows& x, int M, int N, float* partial, float* out,
                           hipStream_t s);

@@ -125,6 +125,21 @@ pvconv_status pv_launch_int8_linear_bwd(const PvRows& dy, const int8_t* rows,
                                         const PvRows& dx, float* dw, float* dbias, void* ws,
                                         hipStream_t s);
 
+// ---- cross entropy of a linear layer (linear_ce.hip) -----------------------
+struct PvLinearCe {
+    PvRows x, w;      // [M][K], [V][K]
+    int M, K, V;
+    const float* bias;
+    const int32_t* labels;
+    const float* weight;
+    float* loss;      // of a forward
+    float* lse;       // of a forward (or NULL); of a backward, its input
+    PvRows dx, dw;    // p NULL: not wanted
+    float* dbias;
+};
+size_t pv_linear_ce_ws_bytes(const PvLinearCe& a, bool forward, bool grads);
+pvconv_status pv_launch_linear_ce(const PvLinearCe& a, bool forward, void* ws, hipStream_t s);
+
 // ---- distillation loss (distill.hip) ---------------------------------------
 struct PvDistill {
     PvRows z;
