@@ -160,7 +160,8 @@ pvconv_status pvconv_int8_quantize(const void* x, pvconv_dtype x_dt, int x_ld, i
 /*  bias  [N] fp32 or NULL; act NONE, RELU or LEAKY (slope)                  */
 /*  y     out [M][N] (y_dt), row stride y_ld                                 */
 /*  rows, row_scale  out: x's quantised rows, kept for the backward and for  */
-/*        pvconv_int8_linear_rows in x's place, or NULL (both)               */
+/*        pvconv_int8_linear_rows in x's place, or NULL (both). A call that  */
+/*        keeps them takes pvconv_int8_linear_rows_workspace_size.           */
 /* 1 <= K, N <= PVCONV_INT8_MAX_CHANNELS; M/128 * max(K, N)/128 (rounded up) */
 /* <= 2^26.                                                                  */
 size_t pvconv_int8_linear_workspace_size(int M, int K, int N);
@@ -183,8 +184,9 @@ pvconv_status pvconv_int8_linear_rows(const int8_t* rows, const float* row_scale
 /* scale weight, from the kept rows:                                         */
 /*   dx[m,k] = sum_n dy[m,n] scale_n weight[n,k]                             */
 /*   dw[n,k] = sum_m dy[m,n] row_scale_m rows[m,k],  dbias_n = sum_m dy[m,n] */
-/* An fp32 output has fp32 sums of products good to 24 bits; for a bf16 dx,  */
-/* dy scale_n is rounded to bf16 first.                                      */
+/* An fp32 output has fp32 sums of products good to 24 bits; for a bf16 dx of */
+/* more than 256 rows, dy scale_n is rounded to bf16 first (of fewer: to 16  */
+/* bits).                                                                    */
 /*  dy [M][N] (dy_dt), dy_ld; dx out [M][K] (dx_dt), dx_ld, or NULL (weight, */
 /*  scale then unused); dw out [N][K] fp32 or NULL (rows, row_scale then     */
 /*  unused); dbias out [N] fp32 or NULL                                      */
@@ -260,8 +262,9 @@ pvconv_status pvconv_distill_topk_backward(const void* z, pvconv_dtype z_dt, int
 /* weight 0 has dz = 0; x and W should be finite all the same, as dz         */
 /* multiplies them.                                                          */
 /* fp32 operands are multiplied to 24 bits, bf16 ones exactly, sums are fp32. */
-/* For a bf16 dx (dw), dz and W (x) are rounded to bf16 first; for an fp32   */
-/* one, dz is taken to 24 bits.                                              */
+/* For a bf16 dx (dw) of more than 256 rows, dz is rounded to bf16 first; of */
+/* fewer, and the other factor always, to 16 bits. For an fp32 one, dz is    */
+/* taken to 24 bits.                                                         */
 /*  x       [M][K] (x_dt), row stride x_ld;  w [V][K] (w_dt), row stride w_ld */
 /*  bias    [V] fp32 or NULL;  labels [M] int32;  row_weight [M] fp32 or     */
 /*          NULL (1)                                                         */

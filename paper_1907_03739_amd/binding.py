@@ -1063,6 +1063,8 @@ def _ce_args(x, w, labels, bias, out_dtype, dw_dtype):
     V, K = w.shape
     M, ld = _matrix_rows(x, K)
     _, wld = _matrix_rows(w, K)
+    if labels is None:
+        raise ValueError("a cross entropy needs labels")
     xd, wd = _dt(x), _dt(w)
     if out_dtype is not None:
         out_dtype = _torch_dt(out_dtype)
@@ -1124,6 +1126,8 @@ def pvconv_linear_cross_entropy_backward(x: torch.Tensor, w: torch.Tensor, label
     _on_device(x.device, w, labels, lse, dloss, bias, workspace)
     dloss_p = _vector(dloss, M, torch.float32, "dloss")
     lse_p = _vector(lse, M, torch.float32, "lse")
+    if lse_p is None:
+        raise ValueError("the backward needs the forward's lse")
     if not (want_dx or want_dw or want_dbias):
         raise ValueError("nothing is wanted")
     dx, dw, db = _ce_grads(x, M, K, V, dxt, dwt, want_dx, want_dw, want_dbias)

@@ -288,9 +288,14 @@ LinearWs carve_linear(void* base, int M, int K, int N, bool rows_given) {
     return w;
 }
 
-// Parts that a gradient's scaled operand needs: one rounded part for a bf16 result,
-// the two that hold 8 by 8 bits for a bf16 dy, three for 32 bits.
-int parts_of(bool out_bf16, bool dy_bf16) { return out_bf16 ? 1 : dy_bf16 ? 2 : 3; }
+// Parts that a gradient's scaled operand needs: one rounded part for a bf16 result of
+// rows enough to average it, else the two that hold 8 by 8 bits for a bf16 dy, three for
+// 32 bits.
+constexpr int kFewRows = 256;
+int parts_of(bool out_bf16, bool dy_bf16, int M) {
+    if (out_bf16) return M <= kFewRows ? 2 : 1;
+    return dy_bf16 ? 2 : 3;
+}
 
 struct BwdWs {
     PvPanel dys, wt, dyt, qt;
@@ -314,12 +319,12 @@ BwdWs carve_bwd(void* base, int M, int K, int N, bool dy_bf16, bool dx_bf16, boo
         p.partial = (uint32_t*)c.take(pv_partial_bytes(p));
     };
     if (want_dx && M > 0) {
-        w.dys = pv_take_panel(c, M, N, parts_of(dx_bf16, dy_bf16));
+        w.dys = pv_take_panel(c, M, N, parts_of(dx_bf16, dy_bf16, M));
         w.wt = pv_take_panel(c, K, N, 1);
         product(w.dx, w.dys, w.wt, M, K, N);
     }
     if (want_dw) {
-        w.dyt = pv_take_panel(c, N, M, parts_of(false, dy_bf16));
+        w.dyt = pv_take_panel(c, N, M, parts_of(false, dy_bf16, M));
         w.qt = pv_take_panel(c, K, M, 1);
         product(w.dw, w.dyt, w.qt, N, K, M);
     }
@@ -355,7 +360,7 @@ pvconv_status pv_launch_int8_quantize(const PvRows& x, int M, int K, int8_t* q, 
 }
 
 size_t pv_int8_linear_ws_bytes(int M, int K, int N, bool rows_given) {
-    if (!rows_given && few(M, N)) return carve_linear(nullptr, M, K, N, false).total;
+    if (!rows_given && few(M, N)) return 0;
     return carve_linear(nullptr, M, K, N, rows_given).total;
 }
 

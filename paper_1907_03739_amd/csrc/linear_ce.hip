@@ -260,6 +260,12 @@ constexpr int kLeastClasses = 2048;
 constexpr size_t kStatsBytes = (size_t)1 << 26;
 
 int parts_of(bool bf16) { return bf16 ? 1 : 3; }
+// Parts of dz for a gradient: 24 bits for an fp32 one; one rounding for a bf16 one, two
+// parts where few rows would not average it (a row's dz at its label scales its whole
+// gradient). The other factor of a bf16 gradient is rounded to 16 bits.
+constexpr int kFewRows = 256;
+int dz_parts_of(bool bf16, int M) { return !bf16 ? 3 : M <= kFewRows ? 2 : 1; }
+int factor_parts_of(bool out_bf16, bool bf16) { return bf16 ? 1 : out_bf16 ? 2 : 3; }
 
 struct Plan {
     PvPanel x, w;             // what the logits are products of
@@ -314,7 +320,7 @@ Plan carve(void* base, const PvLinearCe& a, bool forward, bool grads, bool may_d
         return p;
     }
     const bool want_dx = a.dx.p != nullptr, want_dw = a.dw.p != nullptr;
-    const int px = parts_of(a.dx.bf16), pw = parts_of(a.dw.bf16);
+    const int px = dz_parts_of(a.dx.bf16, a.M), pw = dz_parts_of(a.dw.bf16, a.M);
     // (of both, wanted or not: the workspace of fewer gradients is then no larger)
     const size_t per = pv_up(a.M > 0 ? a.M : 1, 64) * 2 * (px + pw);
     size_t n = kPieceBytes / per / 256 * 256;
@@ -339,7 +345,7 @@ Plan carve(void* base, const PvLinearCe& a, bool forward, bool grads, bool may_d
     };
     if (want_dx) {
         p.dz = pv_take_panel(c, a.M, p.classes, px);
-        p.wt = pv_take_panel(c, a.K, p.classes, a.dx.bf16 ? 1 : parts_of(a.w.bf16));
+        p.wt = pv_take_panel(c, a.K, p.classes, factor_parts_of(a.dx.bf16, a.w.bf16));
         product(p.dx, p.dz, p.wt, a.M, a.K, p.classes);
         sums(p.dx);
         if (tail) {
@@ -352,7 +358,7 @@ Plan carve(void* base, const PvLinearCe& a, bool forward, bool grads, bool may_d
     }
     if (want_dw) {
         p.dzt = pv_take_panel(c, p.classes, a.M, pw);
-        p.xt = pv_take_panel(c, a.K, a.M, a.dw.bf16 ? 1 : parts_of(a.x.bf16));
+        p.xt = pv_take_panel(c, a.K, a.M, factor_parts_of(a.dw.bf16, a.x.bf16));
         product(p.dw, p.dzt, p.xt, p.classes, a.K, a.M);
         sums(p.dw);
         if (tail) {

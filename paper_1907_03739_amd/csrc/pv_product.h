@@ -36,11 +36,13 @@ struct PvProduct {
     uint32_t first, count;  // the tiles of this launch (pv_run_tiles)
 };
 
-// The pairs of parts of two operands that a product needs.
+// The pairs of parts of two operands that a product needs: to 24 bits, or to 16 where
+// neither has three parts.
 static inline void pv_pairs(PvProduct& p, int parts_a, int parts_b) {
     p.pairs = 0;
     p.pa = p.pb = 0;
-    for (int order = 0; order < 3; order++)
+    const int orders = parts_a < 3 && parts_b < 3 ? 2 : 3;
+    for (int order = 0; order < orders; order++)
         for (int i = 0; i <= order; i++) {
             const int j = order - i;
             if (i >= parts_a || j >= parts_b) continue;

@@ -1,13 +1,22 @@
 """A student head: a narrow shared MLP on per-point features, trained against a
-segmentation network's top logits and served in 8-bit floating point.
+segmentation network's top logits or against labels, and served in 8 bits.
 
-Each hidden layer is an 8-bit linear layer (a power-of-two scale for each block
-of 128), then group norm over a cloud's points with an activation; the last is
-an 8-bit linear layer with a bias. A training step is the forward, the
-distillation loss of the logits against the stored top entries of the teacher,
-mixed with the labels' cross-entropy, and the backward of every layer. Weights
-are fp32 masters, quantised once a step, and once for serving; activations and
-their gradients are bf16, logits and parameter gradients fp32.
+Each hidden layer is an 8-bit linear layer, then group norm over a cloud's points
+with an activation; the last is an 8-bit linear layer with a bias. The linear
+layers are in 8-bit floating point (a power-of-two scale for each block of 128)
+or in 8-bit integers (a scale for each point and each output channel). A training
+step is the forward, a loss, and the backward of every layer. The loss is that of
+the logits against the stored top entries of a teacher, mixed with the labels'
+cross-entropy (step), or the labels' cross-entropy alone, which takes the last
+layer with it and never stores a logit (step_labels). Weights are fp32 masters,
+quantised once a step, and once for serving; activations and their gradients are
+bf16, logits and parameter gradients fp32.
+
+Between forward and backward a layer in 8-bit floating point keeps its input and
+its output before the norm, in bf16. A layer in 8-bit integers keeps the quantised
+rows of its input, a quarter of those bytes: the backward multiplies them again
+for the output, which has the forward's bits, and takes the weight's gradient from
+them.
 
 Every arithmetic step runs in libpvconv through the calls of the binding; this
 module only lays out device buffers and orders the calls.
@@ -24,10 +33,15 @@ from . import binding as pv
 class DeviceStudent:
     """widths: input channels, the hidden layers' channels, classes. groups divides
     every hidden width. weights [C_out][C_in] and the last layer's bias, gamma and
-    beta are the tensors that a training program updates in place."""
+    beta are the tensors that a training program updates in place. layers: "fp8" or
+    "int8"."""
 
     def __init__(self, widths: Sequence[int], groups: int = 8, act: str = "silu",
-                 eps: float = 1e-5, slope: float = 0.1, seed: int = 0, device="cuda"):
+                 eps: float = 1e-5, slope: float = 0.1, seed: int = 0, device="cuda",
+                 layers: str = "fp8"):
+        if layers not in ("fp8", "int8"):
+            raise ValueError('layers must be "fp8" or "int8"')
+        self.layers = layers
         if len(widths) < 2:
             raise ValueError("a student needs its input width and its classes")
         if any(w % groups for w in widths[1:-1]):
@@ -48,9 +62,12 @@ class DeviceStudent:
         return [*self.weights, self.bias, *self.gamma, *self.beta]
 
     # -- serving --
+    def _quantize(self, w):
+        return pv.pvconv_int8_quantize(w) if self.layers == "int8" else \
+            pv.pvconv_fp8_quantize_weight(w)
+
     def _model(self):
-        return ([pv.pvconv_fp8_quantize_weight(w) for w in self.weights], self.bias, self.gamma,
-                self.beta)
+        return ([self._quantize(w) for w in self.weights], self.bias, self.gamma, self.beta)
 
     def freeze(self):
         """Keeps the model as it is now for logits(): the weights quantised once,
@@ -65,25 +82,69 @@ class DeviceStudent:
         of the parameters as they are now, the weights quantised on every call."""
         return self._forward(x, self._served or self._model(), lengths, None)
 
-    def _forward(self, x, model, lengths, saved):
-        quantised, bias, gamma, beta = model
+    def _linear(self, h, q, saved, **kw):
+        """A linear layer of h; with saved, what its backward needs is appended."""
+        if self.layers == "fp8":
+            if saved is not None:
+                saved.append((h,))
+            return pv.pvconv_fp8_linear(h, q[0], q[1], **kw)
+        if saved is None:
+            return pv.pvconv_int8_linear(h, q[0], q[1], **kw)
+        z, rows, scale = pv.pvconv_int8_linear(h, q[0], q[1], want_rows=True, **kw)
+        saved.append((rows, scale))
+        return z
+
+    def _hidden(self, x, model, lengths, saved):
+        quantised, _, gamma, beta = model
         h = x
-        for i, (w, s) in enumerate(quantised[:-1]):
-            z = pv.pvconv_fp8_linear(h, w, s, out_dtype=torch.bfloat16)
+        for i, q in enumerate(quantised[:len(gamma)]):
+            z = self._linear(h, q, saved, out_dtype=torch.bfloat16)
             kw = dict(eps=self.eps, act=self.act, slope=self.slope, lengths=lengths)
             if saved is None:
                 y = pv.pvconv_group_norm_act(z, self.groups, gamma[i], beta[i], **kw)
             else:
                 y, stats = pv.pvconv_group_norm_act(z, self.groups, gamma[i], beta[i],
                                                     want_stats=True, **kw)
-                saved.append((h, z, stats))
+                saved[i] += (stats,) if self.layers == "int8" else (z, stats)
             h = y
-        w, s = quantised[-1]
-        if saved is not None:
-            saved.append((h,))
-        return pv.pvconv_fp8_linear(h, w, s, bias=bias, out_dtype=torch.float32)
+        return h
+
+    def _forward(self, x, model, lengths, saved):
+        h = self._hidden(x, model, lengths, saved)
+        return self._linear(h, model[0][-1], saved, bias=model[1], out_dtype=torch.float32)
 
     # -- training --
+    def _train_model(self, count):
+        """The first `count` weights quantised, with what their gradients take."""
+        q = [pv.pvconv_int8_quantize(w) if self.layers == "int8" else
+             pv.pvconv_fp8_quantize_weight(w, transposed=True) for w in self.weights[:count]]
+        return q, self.bias, self.gamma, self.beta
+
+    def _linear_backward(self, i, dy, q, saved, **kw):
+        if self.layers == "fp8":
+            return pv.pvconv_fp8_linear_backward(dy, saved[i][0], q[i][2], q[i][3], **kw)
+        return pv.pvconv_int8_linear_backward(dy, saved[i][0], saved[i][1], q[i][0], q[i][1],
+                                              self.widths[i], **kw)
+
+    def _hidden_backward(self, dy, q, saved, lengths, dws, want_dx):
+        """From dy, the gradient of the hidden layers' output: fills dws, returns
+        (dgammas, dbetas, dx)."""
+        n = len(self.gamma)
+        dgammas, dbetas = [None] * n, [None] * n
+        for i in reversed(range(n)):
+            stats = saved[i][-1]
+            if self.layers == "int8":  # the output before the norm again, bit for bit
+                z = pv.pvconv_int8_linear_rows(saved[i][0], saved[i][1], q[i][0], q[i][1],
+                                               out_dtype=torch.bfloat16).view(dy.shape)
+            else:
+                z = saved[i][1]
+            dy, dgammas[i], dbetas[i] = pv.pvconv_group_norm_act_backward(
+                dy, z, stats, self.groups, self.gamma[i], self.beta[i], act=self.act,
+                slope=self.slope, lengths=lengths)
+            dy, dws[i], _ = self._linear_backward(i, dy, q, saved, want_dx=i > 0 or want_dx,
+                                                  want_dbias=False)
+        return dgammas, dbetas, dy
+
     def step(self, x: torch.Tensor, t_val: torch.Tensor, t_class: torch.Tensor,
              labels: Optional[torch.Tensor] = None, temperature: float = 2.0,
              alpha: float = 1.0, row_weight: Optional[torch.Tensor] = None,
@@ -94,25 +155,32 @@ class DeviceStudent:
         points past a cloud's length the weight 0, and finite x: the first weight's
         gradient multiplies their rows of x by 0."""
         B, N, _ = x.shape
-        q = [pv.pvconv_fp8_quantize_weight(w, transposed=True) for w in self.weights]
+        model = self._train_model(len(self.weights))
         saved = []
-        z = self._forward(x, ([(w, s) for w, s, _, _ in q], self.bias, self.gamma, self.beta),
-                          lengths, saved)
+        z = self._forward(x, model, lengths, saved)
         loss, _, dz = pv.pvconv_distill_topk(
             z.view(B * N, -1), t_val, t_class, labels=labels, temperature=temperature,
             alpha=alpha, row_weight=row_weight, want_grad=True, out_dtype=torch.bfloat16)
         n = len(self.weights)
-        dws, dgammas, dbetas = [None] * n, [None] * (n - 1), [None] * (n - 1)
-        dy, dbias = dz.view(B, N, -1), None
-        for i in reversed(range(n)):
-            if i < n - 1:
-                _, pre, stats = saved[i]
-                dy, dgammas[i], dbetas[i] = pv.pvconv_group_norm_act_backward(
-                    dy, pre, stats, self.groups, self.gamma[i], self.beta[i], act=self.act,
-                    slope=self.slope, lengths=lengths)
-            last = i == n - 1
-            dx, dws[i], db = pv.pvconv_fp8_linear_backward(
-                dy, saved[i][0], q[i][2], q[i][3], want_dx=i > 0 or want_dx, want_dbias=last)
-            dbias = db if last else dbias
-            dy = dx
-        return loss, [*dws, dbias, *dgammas, *dbetas], dy
+        dws = [None] * n
+        dy, dws[-1], dbias = self._linear_backward(n - 1, dz.view(B, N, -1), model[0], saved,
+                                                   want_dx=n > 1 or want_dx, want_dbias=True)
+        dgammas, dbetas, dx = self._hidden_backward(dy, model[0], saved, lengths, dws, want_dx)
+        return loss, [*dws, dbias, *dgammas, *dbetas], dx
+
+    def step_labels(self, x: torch.Tensor, labels: torch.Tensor,
+                    row_weight: Optional[torch.Tensor] = None,
+                    lengths: Optional[torch.Tensor] = None, want_dx: bool = False):
+        """Forward and backward of sum(row_weight * cross-entropy of the labels):
+        labels [B*N] int32, outside the classes: no loss, no gradient -> what step()
+        returns. The last layer multiplies its fp32 weight as it is, and its logits
+        are never stored. The points past a cloud's length as for step()."""
+        model = self._train_model(len(self.gamma))
+        saved = []
+        h = self._hidden(x, model, lengths, saved)
+        loss, _, dy, dw, dbias = pv.pvconv_linear_cross_entropy(
+            h, self.weights[-1], labels, bias=self.bias, row_weight=row_weight, want_grad=True,
+            want_dx=len(self.gamma) > 0 or want_dx)
+        dws = [None] * len(self.gamma) + [dw]
+        dgammas, dbetas, dx = self._hidden_backward(dy, model[0], saved, lengths, dws, want_dx)
+        return loss, [*dws, dbias, *dgammas, *dbetas], dx
