@@ -136,7 +136,6 @@ __device__ __forceinline__ float activate(float v, float neg, bool relu) {
 }
 
 struct LinearEpi {
-    static constexpr bool kLds = false;
     const float* row_scale;
     const float* col_scale;
     const float* bias;
@@ -263,10 +262,7 @@ PvProduct product_of(const int8_t* q, int M, int K, const int8_t* w, int N) {
     p.N = N;
     p.slices = pv_slices(K, kSlice);
     pv_pairs(p, 1, 1);
-    if (N <= 64)
-        pv_plan_splits(p, PvTileN::TM, PvTileN::TN, 8);
-    else
-        pv_plan_splits(p, PvTileM::TM, PvTileM::TN, 8);
+    pv_plan_splits(p, 8);
     return p;
 }
 
@@ -315,7 +311,7 @@ BwdWs carve_bwd(void* base, int M, int K, int N, bool dy_bf16, bool dx_bf16, boo
         p.N = cols;
         p.slices = pv_slices(depth, 64);
         pv_pairs(p, a.parts, b.parts);
-        pv_plan_plain(p);
+        pv_plan_splits(p, 8);
         p.partial = (uint32_t*)c.take(pv_partial_bytes(p));
     };
     if (want_dx && M > 0) {
@@ -369,10 +365,7 @@ static pvconv_status run_rows(const int8_t* q, const float* scale, int M, int K,
                               hipStream_t s) {
     PvProduct p = product_of(q, M, K, weight, N);
     p.partial = partial;
-    if (N <= 64)
-        pv_run_tiles<true, PvTileN>(p, epi, s);
-    else
-        pv_run_tiles<true, PvTileM>(p, epi, s);
+    pv_run_product<true>(p, epi, s);
     return pv_launch_status();
 }
 

@@ -55,56 +55,49 @@ __device__ __forceinline__ uint32_t next_part2(float& a, float& b) {
 
 enum Mode { kStats, kWhole, kGrad };
 
-template <int MODE>
+// PARTS: dz in more than one bf16 part somewhere (what remains of it is then held too).
+template <int MODE, bool PARTS>
 struct CeEpi {
-    static constexpr bool kLds = MODE != kStats;
     Ce c;
 
-    // dz of two times sixteen rows of a wave (row 16 i + r, sixteen columns a lane),
-    // part by part: rows by 32-byte runs, columns through LDS
-    __device__ __forceinline__ void store(const PvProduct& p, int m, int mw, int nw, int lane,
-                                          float (&d)[2][16], uint8_t* lds) const {
+    // One part of dz of two times sixteen rows of a wave (row 16 i + r, sixteen columns a
+    // lane): rows by 32-byte runs, columns through LDS
+    __device__ __forceinline__ void store(const PvProduct& p, int part, int m, int mw, int nw,
+                                          int lane, const uint32_t (&w)[2][8],
+                                          uint8_t* lds) const {
         const int r = lane & 15, h = lane >> 4, n = nw + 16 * h;
-        const int parts = max(c.dz.p ? c.dz.parts : 0, c.dzt.p ? c.dzt.parts : 0);
-        for (int part = 0; part < parts; part++) {
-            uint32_t w[2][8];
+        if (c.dz.p && part < c.dz.parts && (size_t)n * 2 < c.dz.pitch) {
 #pragma unroll
-            for (int i = 0; i < 2; i++)
-#pragma unroll
-                for (int q = 0; q < 8; q++) w[i][q] = next_part2(d[i][2 * q], d[i][2 * q + 1]);
-            if (c.dz.p && part < c.dz.parts && (size_t)n * 2 < c.dz.pitch) {
-#pragma unroll
-                for (int i = 0; i < 2; i++) {
-                    if (m + 16 * i >= p.M) continue;
-                    pv_u32x4* o = (pv_u32x4*)(c.dz.p + part * c.dz.part_bytes +
-                                              (size_t)(m + 16 * i) * c.dz.pitch + (size_t)n * 2);
-                    o[0] = pv_u32x4{w[i][0], w[i][1], w[i][2], w[i][3]};
-                    o[1] = pv_u32x4{w[i][4], w[i][5], w[i][6], w[i][7]};
-                }
+            for (int i = 0; i < 2; i++) {
+                if (m + 16 * i >= p.M) continue;
+                pv_u32x4* o = (pv_u32x4*)(c.dz.p + part * c.dz.part_bytes +
+                                          (size_t)(m + 16 * i) * c.dz.pitch + (size_t)n * 2);
+                o[0] = pv_u32x4{w[i][0], w[i][1], w[i][2], w[i][3]};
+                o[1] = pv_u32x4{w[i][4], w[i][5], w[i][6], w[i][7]};
             }
-            if (!c.dzt.p || part >= c.dzt.parts) continue;
-            // [64 columns][32 rows] of bf16; 16-byte pieces at piece ^ (column >> 4)
-            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-            __builtin_amdgcn_wave_barrier();
+        }
+        if (!c.dzt.p || part >= c.dzt.parts) return;
+        // [64 columns][32 rows] of bf16; 16-byte pieces at piece ^ (column >> 4)
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
 #pragma unroll
-            for (int i = 0; i < 2; i++)
+        for (int i = 0; i < 2; i++)
 #pragma unroll
-                for (int q = 0; q < 8; q++) {
-                    const int at = (((2 * i + (r >> 3)) ^ h) << 4) + (r & 7) * 2;
-                    *(uint16_t*)(lds + (16 * h + 2 * q) * 64 + at) = (uint16_t)w[i][q];
-                    *(uint16_t*)(lds + (16 * h + 2 * q + 1) * 64 + at) = (uint16_t)(w[i][q] >> 16);
-                }
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            __builtin_amdgcn_wave_barrier();
-#pragma unroll
-            for (int u = 0; u < 4; u++) {
-                const int col = u * 16 + (lane >> 2), piece = lane & 3;
-                const pv_u32x4 v = *(const pv_u32x4*)(lds + col * 64 + ((piece ^ u) << 4));
-                const size_t at = (size_t)(mw + 8 * piece) * 2;
-                if (nw + col < p.N && at < c.dzt.pitch)
-                    *(pv_u32x4*)(c.dzt.p + part * c.dzt.part_bytes +
-                                 (size_t)(nw + col) * c.dzt.pitch + at) = v;
+            for (int q = 0; q < 8; q++) {
+                const int at = (((2 * i + (r >> 3)) ^ h) << 4) + (r & 7) * 2;
+                *(uint16_t*)(lds + (16 * h + 2 * q) * 64 + at) = (uint16_t)w[i][q];
+                *(uint16_t*)(lds + (16 * h + 2 * q + 1) * 64 + at) = (uint16_t)(w[i][q] >> 16);
             }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int u = 0; u < 4; u++) {
+            const int col = u * 16 + (lane >> 2), piece = lane & 3;
+            const pv_u32x4 v = *(const pv_u32x4*)(lds + col * 64 + ((piece ^ u) << 4));
+            const size_t at = (size_t)(mw + 8 * piece) * 2;
+            if (nw + col < p.N && at < c.dzt.pitch)
+                *(pv_u32x4*)(c.dzt.p + part * c.dzt.part_bytes + (size_t)(nw + col) * c.dzt.pitch +
+                             at) = v;
         }
     }
 
@@ -121,9 +114,11 @@ struct CeEpi {
         const bool grads = MODE == kGrad || (MODE == kWhole && (c.dz.p || c.dzt.p || c.sums));
 #pragma unroll
         for (int i0 = 0; i0 < MI; i0 += 2) {
-            float d[2][16];
+            uint32_t w[2][8];
+            float d[PARTS ? 2 : 1][16];
 #pragma unroll
             for (int i = 0; i < 2; i++) {
+                float(&di)[16] = d[PARTS ? i : 0];
                 const int m = mw + 16 * (i0 + i) + r, mc = min(m, p.M - 1);
                 const int label = c.labels[mc], at = label - c.v0 - n;
                 const bool known = label >= 0 && label < c.V;
@@ -174,13 +169,28 @@ struct CeEpi {
 #pragma unroll
                     for (int q = 0; q < 16; q++) {
                         const float e = __expf(z[q] - lse) - (q == at ? 1.f : 0.f);
-                        d[i][q] = g == 0.f ? 0.f : n + q < p.N ? g * e : 0.f;
-                        cs[q] += d[i][q];
+                        di[q] = g == 0.f ? 0.f : n + q < p.N ? g * e : 0.f;
+                        cs[q] += di[q];
+                    }
+#pragma unroll
+                    for (int q = 0; q < 8; q++) w[i][q] = next_part2(di[2 * q], di[2 * q + 1]);
+                }
+            }
+            if (MODE != kStats && grads) {
+                const int m = mw + 16 * i0;
+                store(p, 0, m + r, m, nw, lane, w, lds);
+                if constexpr (PARTS) {
+                    const int parts = max(c.dz.p ? c.dz.parts : 0, c.dzt.p ? c.dzt.parts : 0);
+                    for (int part = 1; part < parts; part++) {
+#pragma unroll
+                        for (int i = 0; i < 2; i++)
+#pragma unroll
+                            for (int q = 0; q < 8; q++)
+                                w[i][q] = next_part2(d[i][2 * q], d[i][2 * q + 1]);
+                        store(p, part, m + r, m, nw, lane, w, lds);
                     }
                 }
             }
-            if (MODE != kStats && grads)
-                store(p, mw + 16 * i0 + r, mw + 16 * i0, nw, lane, d, lds);
         }
         if (MODE != kStats && grads && c.sums) {
             // over the 16 rows of lanes: halves of the columns change places, so that
@@ -270,13 +280,12 @@ int factor_parts_of(bool out_bf16, bool bf16) { return bf16 ? 1 : out_bf16 ? 2 :
 struct Plan {
     PvPanel x, w;             // what the logits are products of
     bool pack_x, pack_w;
-    bool whole;
+    bool whole, parts;  // parts: dz in more than one
     int forward_classes, classes;  // a piece's
     PvPanel dz, dzt, wt, xt;
     PvProduct dx, dw;         // of a piece of `classes`
     float2 *stats, *run;
     float *zlab, *lse, *sums, *acc;
-    int blocks;               // of dbias's partial sums
     uint32_t* partial;
     size_t total;
 };
@@ -285,9 +294,24 @@ bool direct(const PvRows& r, int K) {
     return r.bf16 && K % 64 == 0 && r.ld % 8 == 0 && pv_aligned16(r.p);
 }
 
-int row_blocks(int M, bool narrow) {
-    return narrow ? (int)pv_up(M, PvTileN::TM) / (16 * PvTileN::MI)
-                  : (int)pv_up(M, PvTileM::TM) / (16 * PvTileM::MI);
+template <class T>
+int row_blocks_of(int M) {
+    return (int)(pv_up(M, T::TM) / (16 * T::MI));
+}
+// Up to 64 classes a wave has whole rows: tiles of 64 columns. Beside the sums of the
+// largest tiles there are no registers for dz, of middle ones none for parts of it.
+int size_of(int M, int n, bool whole, bool grad, bool parts) {
+    if (whole) return pv_tiles_of(M, n, 128, 64) >= 128 ? kPvN : kPvS;
+    const int size = pv_size_of(M, n);
+    return size == kPvL && grad ? (parts ? kPvM : kPvG) : size;
+}
+int row_blocks(int M, int size) {  // as many as waves have rows
+    switch (size) {
+        case kPvG: return row_blocks_of<PvTileG>(M);
+        case kPvM: return row_blocks_of<PvTileM>(M);
+        case kPvN: return row_blocks_of<PvTileN>(M);
+        default: return row_blocks_of<PvTileS>(M);
+    }
 }
 
 Plan carve(void* base, const PvLinearCe& a, bool forward, bool grads, bool may_direct) {
@@ -326,6 +350,7 @@ Plan carve(void* base, const PvLinearCe& a, bool forward, bool grads, bool may_d
     size_t n = kPieceBytes / per / 256 * 256;
     if (n < (size_t)kLeastClasses) n = kLeastClasses;
     p.classes = n >= (size_t)a.V ? a.V : (int)n;
+    p.parts = px > 1 || pw > 1;
     auto product = [&](PvProduct& q, const PvPanel& x, const PvPanel& y, int rows, int cols,
                        int depth) {
         q.a = x;
@@ -334,7 +359,7 @@ Plan carve(void* base, const PvLinearCe& a, bool forward, bool grads, bool may_d
         q.N = cols;
         q.slices = pv_slices(depth, 64);
         pv_pairs(q, x.parts, y.parts);
-        pv_plan_plain(q);
+        pv_plan_splits(q, 8);
     };
     // the splits' sums of a whole piece and of the last one, which may have fewer classes
     size_t partial = 0;
@@ -351,7 +376,7 @@ Plan carve(void* base, const PvLinearCe& a, bool forward, bool grads, bool may_d
         if (tail) {
             PvProduct q = p.dx;
             q.slices = pv_slices(tail, 64);
-            pv_plan_plain(q);
+            pv_plan_splits(q, 8);
             sums(q);
         }
         if (p.classes < a.V) p.acc = (float*)c.take((size_t)a.M * a.K * 4);
@@ -364,26 +389,39 @@ Plan carve(void* base, const PvLinearCe& a, bool forward, bool grads, bool may_d
         if (tail) {
             PvProduct q = p.dw;
             q.M = tail;
-            pv_plan_plain(q);
+            pv_plan_splits(q, 8);
             sums(q);
         }
     }
     p.partial = (uint32_t*)c.take(partial);
     if (a.dbias) {
-        p.blocks = row_blocks(a.M, p.whole);
-        p.sums = (float*)c.take((size_t)p.blocks * p.classes * 4);
+        // (of a smaller last piece too, whose tiles may be smaller)
+        const size_t b = (size_t)row_blocks(a.M, size_of(a.M, p.classes, p.whole, true, p.parts)) * p.classes,
+                     t = tail ? (size_t)row_blocks(a.M, size_of(a.M, tail, p.whole, true, p.parts)) * tail : 0;
+        p.sums = (float*)c.take((b > t ? b : t) * 4);
     }
     p.total = c.off;
     return p;
 }
 
 template <int MODE>
-void run_logits(const PvProduct& p, const Ce& c, bool narrow, hipStream_t s) {
-    const CeEpi<MODE> epi{c};
-    if (MODE == kWhole || narrow)
-        pv_run_tiles<false, PvTileN>(p, epi, s);
-    else
-        pv_run_tiles<false, PvTileM>(p, epi, s);
+void run_logits(const PvProduct& p, const Ce& c, bool parts, hipStream_t s) {
+    if constexpr (MODE == kStats) {
+        pv_run_product<false>(p, CeEpi<MODE, false>{c}, s);
+    } else if (p.size == kPvS || p.size == kPvN) {  // all that whole rows take
+        const CeEpi<MODE, true> epi{c};
+        if (p.size == kPvN)
+            pv_run_tiles<false, PvTileN>(p, epi, s);
+        else
+            pv_run_tiles<false, PvTileS>(p, epi, s);
+    } else if constexpr (MODE == kGrad) {
+        if (parts)
+            pv_run_tiles<false, PvTileM>(p, CeEpi<MODE, true>{c}, s);
+        else if (p.size == kPvM)
+            pv_run_tiles<false, PvTileM>(p, CeEpi<MODE, false>{c}, s);
+        else
+            pv_run_tiles<false, PvTileG>(p, CeEpi<MODE, false>{c}, s);
+    }
 }
 
 }  // namespace
@@ -401,7 +439,7 @@ pvconv_status pv_launch_linear_ce(const PvLinearCe& a, bool forward, void* ws, h
     if (p.pack_w && a.M > 0)
         pv_launch_pack(pv_pack_of(a.w.p, kind(a.w), a.w.ld, a.V, a.K, p.w), s);
     // the product of a run of classes, whose epilogue is given
-    auto logits = [&](int v0, int n) {
+    auto logits = [&](int v0, int n, bool grad) {
         PvProduct q{};
         q.a = p.x;
         q.b = p.w;
@@ -412,6 +450,7 @@ pvconv_status pv_launch_linear_ce(const PvLinearCe& a, bool forward, void* ws, h
         pv_pairs(q, p.x.parts, p.w.parts);
         q.per = q.slices * q.pairs;
         q.splits = 1;
+        q.size = size_of(a.M, n, p.whole, grad, p.parts);
         return q;
     };
     Ce c{};
@@ -431,7 +470,7 @@ pvconv_status pv_launch_linear_ce(const PvLinearCe& a, bool forward, void* ws, h
             c.stats = p.stats;
             c.nb = (n + 63) / 64;
             c.zlab = p.zlab;
-            run_logits<kStats>(logits(v0, n), c, false, s);
+            run_logits<kStats>(logits(v0, n, false), c, false, s);
             const Join j{p.stats, c.nb, a.M, a.V, p.run, v0 == 0, v0 + n == a.V, a.labels, p.zlab,
                          a.loss, lse};
             if (a.M > 0) {
@@ -445,7 +484,7 @@ pvconv_status pv_launch_linear_ce(const PvLinearCe& a, bool forward, void* ws, h
         }
     } else if (forward && !grads) {
         c.bias = a.bias;
-        run_logits<kWhole>(logits(0, a.V), c, true, s);
+        run_logits<kWhole>(logits(0, a.V, false), c, false, s);
     }
     if (!grads) return pv_launch_status();
     if (a.dw.p) pv_launch_pack_transposed(pv_pack_of(a.x.p, kind(a.x), a.x.ld, a.M, a.K, p.xt), s);
@@ -458,10 +497,11 @@ pvconv_status pv_launch_linear_ce(const PvLinearCe& a, bool forward, void* ws, h
         dz.pitch = wt.pitch = pv_up(n, 64) * 2;
         c.dz = panel(dz);
         c.dzt = panel(dzt);
+        const PvProduct z = logits(v0, n, true);
         if (p.whole && forward)
-            run_logits<kWhole>(logits(v0, n), c, true, s);
+            run_logits<kWhole>(z, c, p.parts, s);
         else
-            run_logits<kGrad>(logits(v0, n), c, p.whole, s);
+            run_logits<kGrad>(z, c, p.parts, s);
         if (a.dx.p && a.M > 0) {
             const size_t es = a.w.bf16 ? 2 : 4;
             pv_launch_pack_transposed(
@@ -472,7 +512,7 @@ pvconv_status pv_launch_linear_ce(const PvLinearCe& a, bool forward, void* ws, h
             q.a = dz;
             q.b = wt;
             q.slices = pv_slices(n, 64);
-            pv_plan_plain(q);
+            pv_plan_splits(q, 8);
             q.partial = p.partial;
             const bool last = v0 + n == a.V;
             pv_launch_plain(q, PvPlain{last ? a.dx : PvRows{p.acc, false, a.K},
@@ -481,13 +521,13 @@ pvconv_status pv_launch_linear_ce(const PvLinearCe& a, bool forward, void* ws, h
         if (a.dw.p) {
             PvProduct q = p.dw;
             q.M = n;
-            pv_plan_plain(q);
+            pv_plan_splits(q, 8);
             q.partial = p.partial;
             const size_t es = a.dw.bf16 ? 2 : 4;
             pv_launch_plain(q, PvPlain{PvRows{(char*)a.dw.p + (size_t)v0 * a.dw.ld * es,
                                               a.dw.bf16, a.dw.ld}, nullptr}, s);
         }
-        if (a.dbias) pv_launch_sum_parts(p.sums, p.blocks, n, a.dbias + v0, s);
+        if (a.dbias) pv_launch_sum_parts(p.sums, row_blocks(a.M, z.size), n, a.dbias + v0, s);
     }
     return pv_launch_status();
 }

@@ -109,7 +109,6 @@ __global__ __launch_bounds__(kThreads) void pv_pack_transposed_kernel(PvPack k) 
 }
 
 struct PlainEpi {
-    static constexpr bool kLds = false;
     PvPlain e;
     template <int MI>
     __device__ __forceinline__ void tile(const PvProduct& p, int mw, int nw, int lane,
@@ -121,9 +120,21 @@ struct PlainEpi {
             if (m >= p.M) continue;
             float v[16];
 #pragma unroll
-            for (int c = 0; c < 16; c++) {
-                v[c] = acc[c >> 2][i][c & 3];
-                if (e.add && n + c < p.N) v[c] += e.add[(size_t)m * p.N + n + c];
+            for (int c = 0; c < 16; c++) v[c] = acc[c >> 2][i][c & 3];
+            if (e.add) {
+                const float* from = e.add + (size_t)m * p.N + n;
+#pragma unroll
+                for (int c = 0; c < 16; c += 4) {
+                    if (n + c + 4 <= p.N) {
+                        const pv_u32x4 w = *(const pv_u32x4_any*)(from + c);
+#pragma unroll
+                        for (int u = 0; u < 4; u++) v[c + u] += __uint_as_float(w[u]);
+                    } else {
+#pragma unroll
+                        for (int u = 0; u < 4; u++)
+                            if (n + c + u < p.N) v[c + u] += from[c + u];
+                    }
+                }
             }
             pv_store_run<16>(e.out, m, n, p.N, v);
         }
@@ -190,18 +201,8 @@ void pv_launch_pack_transposed(const PvPack& k, hipStream_t s) {
                        k);
 }
 
-void pv_plan_plain(PvProduct& p) {
-    if (p.N <= 64)
-        pv_plan_splits(p, PvTileN::TM, PvTileN::TN, 8);
-    else
-        pv_plan_splits(p, PvTileM::TM, PvTileM::TN, 8);
-}
 void pv_launch_plain(const PvProduct& p, const PvPlain& e, hipStream_t s) {
-    const PlainEpi epi{e, p.N};
-    if (p.N <= 64)
-        pv_run_tiles<false, PvTileN>(p, epi, s);
-    else
-        pv_run_tiles<false, PvTileM>(p, epi, s);
+    pv_run_product<false>(p, PlainEpi{e, p.N}, s);
 }
 
 void pv_launch_sum_parts(const float* partial, int parts, int N, float* out, hipStream_t s) {

@@ -9,6 +9,9 @@
 // other); hh + hm + mh + mm + hl + lh leaves out terms below 2^-26 of a product.
 #pragma once
 
+#include <type_traits>
+#include <utility>
+
 #include "pv_train.h"
 
 typedef int pv_i32x4 __attribute__((ext_vector_type(4)));
@@ -34,6 +37,7 @@ struct PvProduct {
     int splits, per;     // slices (of all pairs) a split; partial sums where splits > 1
     uint32_t* partial;   // [splits][M][N], 32-bit words
     uint32_t first, count;  // the tiles of this launch (pv_run_tiles)
+    int size;            // PvSize
 };
 
 // The pairs of parts of two operands that a product needs: to 24 bits, or to 16 where
@@ -52,31 +56,32 @@ static inline void pv_pairs(PvProduct& p, int parts_a, int parts_b) {
         }
 }
 
-// Tiles: WM x WN waves of 16 MI rows by 64 columns each.
-template <int WM_, int WN_, int MI_>
+// Tiles: WM x WN waves of 16 MI rows by 64 columns each; ST stages of slices in LDS, ST -
+// 1 of them under way while one is multiplied.
+template <int WM_, int WN_, int MI_, int ST_, int PER_CU_, int KB_ = 128>
 struct PvTile {
-    static constexpr int WM = WM_, WN = WN_, MI = MI_;
+    static constexpr int WM = WM_, WN = WN_, MI = MI_, ST = ST_;
+    static constexpr int KB = KB_;  // bytes of a row that a stage holds
     static constexpr int TM = WM * MI * 16, TN = WN * 64, kThreads = 64 * WM * WN;
+    static constexpr int kWorkgroups = 256 * PER_CU_;  // that the chip holds at once
 };
-typedef PvTile<2, 2, 4> PvTileM;  // 128 x 128, two workgroups a CU
-typedef PvTile<4, 1, 2> PvTileN;  // 128 x 64: few columns
-typedef PvTile<2, 4, 8> PvTileL;  // 256 x 256
+typedef PvTile<2, 4, 8, 2, 1> PvTileL;  // 256 x 256
+typedef PvTile<4, 2, 4, 3, 1> PvTileG;  // 256 x 128: half the sums in registers
+typedef PvTile<2, 2, 4, 4, 1> PvTileM;  // 128 x 128
+typedef PvTile<4, 1, 2, 4, 1> PvTileN;  // 128 x 64: few columns
+typedef PvTile<2, 1, 2, 4, 2> PvTileS;  // 64 x 64: few tiles
 
-// Workgroups go round the XCDs; each XCD takes a run of tiles, eight tiles of rows
-// by the columns in turn, so that its L2 serves both operands.
+// The tile of index idx: eight tiles of rows by the columns in turn, so that an XCD,
+// which works on neighbours at a time, has both operands in its L2.
 template <class T>
-__device__ __forceinline__ bool pv_tile_of(const PvProduct& p, int& split, int& m0, int& n0) {
+__device__ __forceinline__ void pv_tile_of(const PvProduct& p, uint32_t idx, int& split, int& m0,
+                                           int& n0) {
     const uint32_t mt = (uint32_t)(p.M + T::TM - 1) / T::TM, nt = (uint32_t)(p.N + T::TN - 1) / T::TN;
-    const uint32_t run = (p.count + 7) / 8;
-    uint32_t idx = (blockIdx.x & 7) * run + (blockIdx.x >> 3);
-    if ((blockIdx.x >> 3) >= run || idx >= p.count) return false;
-    idx += p.first;
     split = (int)(idx / (mt * nt));
     const uint32_t t = idx % (mt * nt), g = t / (8 * nt), r = t - g * 8 * nt;
     const uint32_t gm = min(8u, mt - g * 8);
     m0 = (int)((g * 8 + r % gm) * T::TM);
     n0 = (int)(r / gm * T::TN);
-    return true;
 }
 
 template <bool I8>
@@ -88,129 +93,216 @@ struct PvAcc<true> {
     typedef pv_i32x4 type;
 };
 
-// 16-byte pieces of a 128-byte row are kept at piece ^ key(row) in LDS: the rows that
-// eight neighbouring lanes read differ in it (rows of a: consecutive; rows of b: 16
-// (r >> 2) + 4 j + (r & 3), which leaves a lane 16 consecutive columns of the result).
-__device__ __forceinline__ int pv_key_a(int row) { return row & 7; }
-__device__ __forceinline__ int pv_key_b(int row) { return (row & 3) | ((row >> 2) & 4); }
+// 16-byte pieces of a stage's row are kept at piece ^ key(row) in LDS, so that the rows
+// which eight neighbouring lanes read lie in different banks (rows of a: consecutive; rows
+// of b: 16 (r >> 2) + 4 j + (r & 3), which leaves a lane 16 consecutive columns of the
+// result).
+template <int KB>
+__device__ __forceinline__ int pv_key_a(int row) {
+    return KB == 128 ? row & 7 : (row >> 1) & 3;
+}
+template <int KB>
+__device__ __forceinline__ int pv_key_b(int row) {
+    return KB == 128 ? (row & 3) | ((row >> 2) & 4) : ((row >> 1) & 1) | ((row >> 3) & 2);
+}
+
+// f(0), .. f(N - 1) with the index as a constant: arrays that it indexes stay in registers
+template <class F, int... I>
+__device__ __forceinline__ void pv_each(std::integer_sequence<int, I...>, const F& f) {
+    (f(std::integral_constant<int, I>()), ...);
+}
+template <int N, class F>
+__device__ __forceinline__ void pv_each(const F& f) {
+    pv_each(std::make_integer_sequence<int, N>(), f);
+}
+
+// s_waitcnt of at most VM loads under way, and none of LDS
+template <int VM>
+__device__ __forceinline__ void pv_wait_loads() {
+    static_assert(VM < 64, "six bits");
+    __builtin_amdgcn_s_waitcnt((VM & 15) | (7 << 4) | ((VM >> 4) << 14));
+}
 
 // The epilogue gets acc[j][i][e]: row mw + 16 i + r, column nw + 16 h + 4 j + e (r =
-// lane & 15, h = lane >> 4), and LDS of 4 KB a wave once nothing reads it.
+// lane & 15, h = lane >> 4), and 4 KB of LDS a wave that nothing else uses then. A
+// workgroup takes several tiles in turn: the first slices of the next one are under way
+// during the epilogue.
 template <bool I8, class T, class Epi>
-__global__ __launch_bounds__(T::kThreads, 2) void pv_product_kernel(PvProduct p, Epi epi) {
-    // two stages, arrays of their own: the loads into one are then seen not to
-    // touch what is read of the other, and are not waited for
-    __shared__ __align__(16) uint8_t la0[T::TM * kSlice], la1[T::TM * kSlice];
-    __shared__ __align__(16) uint8_t lb0[T::TN * kSlice], lb1[T::TN * kSlice];
+__global__ __launch_bounds__(T::kThreads, T::kThreads* T::kWorkgroups / 256 / 256) void
+pv_product_kernel(PvProduct p, Epi epi) {
+    // stages, arrays of their own: the loads into one are then seen not to touch what is
+    // read of another, and are not waited for
+    constexpr int KB = T::KB, SA = T::TM * KB, SB = T::TN * KB, ST = T::ST;
+    constexpr int PR = KB / 16;  // pieces of a row
+    __shared__ __align__(16) uint8_t la0[SA], la1[SA], la2[ST > 2 ? SA : 16], la3[ST > 3 ? SA : 16];
+    __shared__ __align__(16) uint8_t lb0[SB], lb1[SB], lb2[ST > 2 ? SB : 16], lb3[ST > 3 ? SB : 16];
+    constexpr int kPer = kSlice / KB;  // stages of a slice
     typedef typename PvAcc<I8>::type Acc;
-    constexpr int MI = T::MI, QA = T::TM * 8 / T::kThreads, QB = T::TN * 8 / T::kThreads;
-    int split, m0, n0;
-    if (!pv_tile_of<T>(p, split, m0, n0)) return;
-    const int t0 = split * p.per, t1 = min(t0 + p.per, p.slices * p.pairs);
+    constexpr int MI = T::MI, QA = T::TM * PR / T::kThreads, QB = T::TN * PR / T::kThreads;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r = lane & 15, h = lane >> 4;
     const int wm = wave % T::WM * (16 * MI), wn = wave / T::WM * 64;
+    // each XCD (workgroups go round them) takes a run of the launch's tiles
+    const uint32_t run = (p.count + 7) / 8, step = gridDim.x >> 3;
+    const uint32_t end = min(run * ((blockIdx.x & 7) + 1), p.count);
+    uint32_t idx = run * (blockIdx.x & 7) + (blockIdx.x >> 3);
+    if (idx >= end) return;
 
+    int split, m0, n0, t0, t1, pair, k;
     const uint8_t* ga[QA];
     const uint8_t* gb[QB];
+    auto enter = [&]() {
+        pv_tile_of<T>(p, p.first + idx, split, m0, n0);
+        t0 = split * p.per;
+        t1 = min(t0 + p.per, p.slices * p.pairs) * kPer;
+        pair = t0 / max(p.slices, 1);
+        k = (t0 - pair * p.slices) * kPer;
+        t0 *= kPer;
 #pragma unroll
-    for (int q = 0; q < QA; q++) {
-        const int piece = (wave * QA + q) * 64 + lane, row = piece >> 3, c = piece & 7;
-        ga[q] = p.a.p + (size_t)min(m0 + row, p.M - 1) * p.a.pitch + (c ^ pv_key_a(row)) * 16;
-    }
+        for (int q = 0; q < QA; q++) {
+            const int piece = (wave * QA + q) * 64 + lane, row = piece / PR, c = piece % PR;
+            ga[q] = p.a.p + (size_t)min(m0 + row, p.M - 1) * p.a.pitch + (c ^ pv_key_a<KB>(row)) * 16;
+        }
 #pragma unroll
-    for (int q = 0; q < QB; q++) {
-        const int piece = (wave * QB + q) * 64 + lane, row = piece >> 3, c = piece & 7;
-        gb[q] = p.b.p + (size_t)min(n0 + row, p.N - 1) * p.b.pitch + (c ^ pv_key_b(row)) * 16;
-    }
-    int pair = t0 / max(p.slices, 1), k = t0 - pair * p.slices;
-    auto fetch = [&](uint8_t* la, uint8_t* lb) {
-        const size_t oa = ((p.pa >> (4 * pair)) & 15) * p.a.part_bytes + (size_t)k * kSlice;
-        const size_t ob = ((p.pb >> (4 * pair)) & 15) * p.b.part_bytes + (size_t)k * kSlice;
-#pragma unroll
-        for (int q = 0; q < QA; q++)
+        for (int q = 0; q < QB; q++) {
+            const int piece = (wave * QB + q) * 64 + lane, row = piece / PR, c = piece % PR;
+            gb[q] = p.b.p + (size_t)min(n0 + row, p.N - 1) * p.b.pitch + (c ^ pv_key_b<KB>(row)) * 16;
+        }
+    };
+    // load q of the QA + QB of a slice; the last one moves on to the next slice
+    auto fetch_one = [&](int q, uint8_t* la, uint8_t* lb) {
+        if (q < QA) {
+            const size_t oa = ((p.pa >> (4 * pair)) & 15) * p.a.part_bytes + (size_t)k * KB;
             __builtin_amdgcn_global_load_lds(
-                (const void __attribute__((address_space(1)))*)(ga[q] + oa),
+                (const void __attribute__((address_space(1)))*)(ga[q < QA ? q : 0] + oa),
                 (void __attribute__((address_space(3)))*)(la + (wave * QA + q) * 1024), 16, 0, 0);
-#pragma unroll
-        for (int q = 0; q < QB; q++)
+        } else {
+            const size_t ob = ((p.pb >> (4 * pair)) & 15) * p.b.part_bytes + (size_t)k * KB;
             __builtin_amdgcn_global_load_lds(
-                (const void __attribute__((address_space(1)))*)(gb[q] + ob),
-                (void __attribute__((address_space(3)))*)(lb + (wave * QB + q) * 1024), 16, 0, 0);
-        if (++k == p.slices) {
+                (const void __attribute__((address_space(1)))*)(gb[q < QA ? 0 : q - QA] + ob),
+                (void __attribute__((address_space(3)))*)(lb + (wave * QB + q - QA) * 1024), 16, 0,
+                0);
+        }
+        if (q == QA + QB - 1 && ++k == p.slices * kPer) {
             k = 0;
             pair++;
         }
     };
-    Acc acc[4][MI];
+    auto fetch = [&](uint8_t* la, uint8_t* lb) {
 #pragma unroll
-    for (int j = 0; j < 4; j++)
+        for (int q = 0; q < QA + QB; q++) fetch_one(q, la, lb);
+    };
+    auto first = [&]() {  // the first ST - 1 slices of a tile
+        if (t0 < t1) fetch(la0, lb0);
+        if (ST > 2 && t0 + 1 < t1) fetch(la1, lb1);
+        if (ST > 3 && t0 + 2 < t1) fetch(la2, lb2);
+    };
+    enter();
+    first();
+    for (;;) {
+        Acc acc[4][MI];
 #pragma unroll
-        for (int i = 0; i < MI; i++) acc[j][i] = Acc{0, 0, 0, 0};
-
-    auto slice = [&](int t, const uint8_t* la, const uint8_t* lb, uint8_t* na, uint8_t* nb) {
-        __builtin_amdgcn_s_waitcnt(0);  // this wave's part of the slices has landed
-        __syncthreads();
-        if (t + 1 < t1) fetch(na, nb);
+        for (int j = 0; j < 4; j++)
 #pragma unroll
-        for (int half = 0; half < 2; half++) {
+            for (int i = 0; i < MI; i++) acc[j][i] = Acc{0, 0, 0, 0};
+        auto load_a = [&](const uint8_t* la, int i, int half) {
+            const int row = wm + 16 * i + r;
+            return *(const pv_u32x4*)(la + row * KB + ((h + 4 * half) ^ pv_key_a<KB>(row)) * 16);
+        };
+        auto load_b = [&](const uint8_t* lb, int j, int half) {
+            const int row = wn + 16 * (r >> 2) + 4 * j + (r & 3);
+            return *(const pv_u32x4*)(lb + row * KB + ((h + 4 * half) ^ pv_key_b<KB>(row)) * 16);
+        };
+        // The products of a slice in la, lb. The loads of a later one go between them: at
+        // once, they would hold every wave up for the time that they take to be issued.
+        auto multiply = [&](const uint8_t* la, const uint8_t* lb, uint8_t* na, uint8_t* nb,
+                            bool fetching) {
+            constexpr int Q = QA + QB;
             pv_u32x4 fa[MI], fb[4];
-#pragma unroll
-            for (int j = 0; j < 4; j++) {
-                const int row = wn + 16 * (r >> 2) + 4 * j + (r & 3);
-                fb[j] = *(const pv_u32x4*)(lb + row * kSlice +
-                                           ((h + 4 * half) ^ pv_key_b(row)) * 16);
+            pv_each<4>([&](auto j) { fb[j] = load_b(lb, j, 0); });
+            pv_each<MI>([&](auto i) { fa[i] = load_a(la, i, 0); });
+            pv_each<KB / 64>([&](auto half) {
+                pv_each<MI>([&](auto i) {
+                    pv_each<4>([&](auto j) {
+                        if constexpr (I8) {
+                            acc[j][i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(
+                                (pv_i32x4)fb[j], (pv_i32x4)fa[i], acc[j][i], 0, 0, 0);
+                        } else {
+                            pv_b16x8 va, vb;
+                            __builtin_memcpy(&va, &fa[i], 16);
+                            __builtin_memcpy(&vb, &fb[j], 16);
+                            acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vb, va, acc[j][i],
+                                                                                0, 0, 0);
+                        }
+                    });
+                    if constexpr (half == 0) {
+                        if constexpr (KB == 128) {
+                            if constexpr (i == MI - 1)
+                                pv_each<4>([&](auto j) { fb[j] = load_b(lb, j, 1); });
+                            fa[i] = load_a(la, i, 1);
+                        }
+                        constexpr int q0 = i * Q / MI, q1 = (i + 1) * Q / MI;
+                        if (fetching) pv_each<q1 - q0>([&](auto q) { fetch_one(q + q0, na, nb); });
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                });
+            });
+        };
+        // one slice, in la, lb; na, nb, read before this barrier, take the one ST - 1 on
+        auto slice = [&](int t, const uint8_t* la, const uint8_t* lb, uint8_t* na, uint8_t* nb) {
+            if (t + ST - 2 < t1)  // this wave's part of it has landed
+                pv_wait_loads<(ST - 2) * (QA + QB)>();
+            else
+                pv_wait_loads<0>();
+            pv_lds_barrier();
+            multiply(la, lb, na, nb, t + ST - 1 < t1);
+        };
+        for (int t = t0; t < t1; t += ST) {
+            if constexpr (ST == 2) {
+                slice(t, la0, lb0, la1, lb1);
+                if (t + 1 < t1) slice(t + 1, la1, lb1, la0, lb0);
+            } else if constexpr (ST == 3) {
+                slice(t, la0, lb0, la2, lb2);
+                if (t + 1 < t1) slice(t + 1, la1, lb1, la0, lb0);
+                if (t + 2 < t1) slice(t + 2, la2, lb2, la1, lb1);
+            } else {
+                slice(t, la0, lb0, la3, lb3);
+                if (t + 1 < t1) slice(t + 1, la1, lb1, la0, lb0);
+                if (t + 2 < t1) slice(t + 2, la2, lb2, la1, lb1);
+                if (t + 3 < t1) slice(t + 3, la3, lb3, la2, lb2);
             }
+        }
+        const int em = m0 + wm, en = n0 + wn, es = split;
+        idx += step;
+        const bool more = idx < end;
+        pv_lds_barrier();  // nothing reads the stages any more
+        if (more) {
+            enter();
+            first();
+        }
+        if (p.splits > 1) {
+            uint32_t* part = p.partial + (size_t)es * p.M * p.N;
 #pragma unroll
             for (int i = 0; i < MI; i++) {
-                const int row = wm + 16 * i + r;
-                fa[i] = *(const pv_u32x4*)(la + row * kSlice +
-                                           ((h + 4 * half) ^ pv_key_a(row)) * 16);
-            }
-#pragma unroll
-            for (int i = 0; i < MI; i++)
+                const int m = em + 16 * i + r, n = en + 16 * h;
+                if (m >= p.M) continue;
+                uint32_t* o = part + (size_t)m * p.N + n;
 #pragma unroll
                 for (int j = 0; j < 4; j++) {
-                    if constexpr (I8) {
-                        acc[j][i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(
-                            (pv_i32x4)fb[j], (pv_i32x4)fa[i], acc[j][i], 0, 0, 0);
-                    } else {
-                        pv_b16x8 va, vb;
-                        __builtin_memcpy(&va, &fa[i], 16);
-                        __builtin_memcpy(&vb, &fb[j], 16);
-                        acc[j][i] =
-                            __builtin_amdgcn_mfma_f32_16x16x32_bf16(vb, va, acc[j][i], 0, 0, 0);
-                    }
+                    pv_u32x4 v;
+                    __builtin_memcpy(&v, &acc[j][i], 16);
+                    if (n + 4 * j + 4 <= p.N)
+                        *(pv_u32x4_any*)(o + 4 * j) = v;
+                    else
+#pragma unroll
+                        for (int e = 0; e < 4; e++)
+                            if (n + 4 * j + e < p.N) o[4 * j + e] = v[e];
                 }
-        }
-    };
-    if (t0 < t1) fetch(la0, lb0);
-    for (int t = t0; t < t1; t += 2) {
-        slice(t, la0, lb0, la1, lb1);
-        if (t + 1 < t1) slice(t + 1, la1, lb1, la0, lb0);
-    }
-    if (p.splits > 1) {
-        uint32_t* part = p.partial + (size_t)split * p.M * p.N;
-#pragma unroll
-        for (int i = 0; i < MI; i++) {
-            const int m = m0 + wm + 16 * i + r, n = n0 + wn + 16 * h;
-            if (m >= p.M) continue;
-            uint32_t* o = part + (size_t)m * p.N + n;
-#pragma unroll
-            for (int j = 0; j < 4; j++) {
-                pv_u32x4 v;
-                __builtin_memcpy(&v, &acc[j][i], 16);
-                if (n + 4 * j + 4 <= p.N)
-                    *(pv_u32x4_any*)(o + 4 * j) = v;
-                else
-#pragma unroll
-                    for (int e = 0; e < 4; e++)
-                        if (n + 4 * j + e < p.N) o[4 * j + e] = v[e];
             }
+        } else {
+            epi.template tile<MI>(p, em, en, lane, acc, (ST == 2 ? la1 : ST == 3 ? la2 : la3) + wave * 4096);
         }
-        return;
+        if (!more) return;
     }
-    if constexpr (Epi::kLds) __syncthreads();
-    epi.template tile<MI>(p, m0 + wm, n0 + wn, lane, acc, la0 + wave * 4096);
 }
 
 // W (4 or 16) consecutive values of a row from column n on, wherever the row begins.
@@ -251,19 +343,36 @@ __device__ __forceinline__ void pv_store_run(const PvRows& out, int m, int n, in
 }
 
 // ---- splits ----------------------------------------------------------------
-// How many ways a product's slices are split: one where its tiles fill the chip,
-// else enough for two workgroups a CU at most, of `least` slices or more.
-static inline void pv_plan_splits(PvProduct& p, int tm, int tn, int least) {
-    const size_t tiles = (size_t)((p.M + tm - 1) / tm) * ((p.N + tn - 1) / tn);
+// How many ways a product's slices are split, and into which tiles: unsplit where its
+// tiles fill the chip, else enough for a workgroup a CU at most, of `least` slices or
+// more.
+enum PvSize { kPvS, kPvN, kPvM, kPvG, kPvL };
+static inline size_t pv_tiles_of(int M, int N, int tm, int tn) {
+    return (size_t)((M + tm - 1) / tm) * ((N + tn - 1) / tn);
+}
+static inline void pv_plan_splits(PvProduct& p, int least) {
     const int all = p.slices * p.pairs;
+    PvSize size = kPvS;
+    size_t tiles = pv_tiles_of(p.M, p.N, 64, 64);
+    if (p.N > 128 && pv_tiles_of(p.M, p.N, 256, 256) * (all / 32 + 1) >= 192) {
+        size = kPvL;
+        tiles = pv_tiles_of(p.M, p.N, 256, 256);
+    } else if (p.N > 64 && pv_tiles_of(p.M, p.N, 128, 128) * (all / 16 + 1) >= 128) {
+        size = kPvM;
+        tiles = pv_tiles_of(p.M, p.N, 128, 128);
+    } else if (p.N <= 64 && pv_tiles_of(p.M, p.N, 128, 64) * (all / 16 + 1) >= 128) {
+        size = kPvN;
+        tiles = pv_tiles_of(p.M, p.N, 128, 64);
+    }
     p.per = all;
-    if (tiles > 0 && tiles < 256 && all >= 2 * least) {
+    if (tiles > 0 && tiles <= 128 && all >= 2 * least) {
         const int most = all / least;
-        int n = (int)(512 / tiles);
+        int n = (int)(256 / tiles);
         n = n < 1 ? 1 : (n > most ? most : n);
         p.per = (all + n - 1) / n;
     }
     p.splits = p.per ? (all + p.per - 1) / p.per : 1;
+    p.size = size;
 }
 static inline size_t pv_partial_bytes(const PvProduct& p) {
     return p.splits > 1 ? (size_t)p.splits * p.M * p.N * 4 : 0;
@@ -304,20 +413,43 @@ static inline unsigned pv_blocks(size_t items, int per) {
     return (unsigned)(b < 1 ? 1 : (b < (1u << 16) ? b : 1u << 16));
 }
 
-constexpr size_t kPvTilesALaunch = 1u << 22;  // a launch has fewer than 2^32 threads
+constexpr size_t kPvTilesALaunch = (size_t)1 << 30;
+template <class T>
+static inline size_t pv_tiles(const PvProduct& p) {
+    return (size_t)((p.M + T::TM - 1) / T::TM) * ((p.N + T::TN - 1) / T::TN) * p.splits;
+}
 template <bool I8, class T, class Epi>
 static void pv_run_tiles(PvProduct p, const Epi& epi, hipStream_t s) {
-    const size_t tiles =
-        (size_t)((p.M + T::TM - 1) / T::TM) * ((p.N + T::TN - 1) / T::TN) * p.splits;
+    const size_t tiles = pv_tiles<T>(p);
     for (size_t t = 0; t < tiles; t += kPvTilesALaunch) {
         p.first = (uint32_t)t;
         p.count = (uint32_t)(tiles - t < kPvTilesALaunch ? tiles - t : kPvTilesALaunch);
-        hipLaunchKernelGGL((pv_product_kernel<I8, T, Epi>), dim3((p.count + 7) / 8 * 8),
-                           dim3(T::kThreads), 0, s, p, epi);
+        const unsigned most = (p.count + 7) / 8 * 8;
+        hipLaunchKernelGGL((pv_product_kernel<I8, T, Epi>),
+                           dim3(most < T::kWorkgroups ? most : T::kWorkgroups), dim3(T::kThreads),
+                           0, s, p, epi);
     }
     if (p.splits > 1)
         hipLaunchKernelGGL((pv_join_kernel<I8, Epi>), dim3(pv_blocks((size_t)p.M * p.N, 256)),
                            dim3(256), 0, s, p, epi);
+}
+
+// The tiles of a product that is never split: large ones where they fill the chip, and
+// smaller the fewer there are of them.
+static inline PvSize pv_size_of(int M, int N) {
+    if (N > 128 && pv_tiles_of(M, N, 256, 256) >= 192) return kPvL;
+    if (N > 64 && pv_tiles_of(M, N, 128, 128) >= 128) return kPvM;
+    return N <= 64 && pv_tiles_of(M, N, 128, 64) >= 128 ? kPvN : kPvS;
+}
+template <bool I8, class Epi>
+static void pv_run_product(const PvProduct& p, const Epi& epi, hipStream_t s) {
+    switch (p.size) {
+        case kPvL: pv_run_tiles<I8, PvTileL>(p, epi, s); break;
+        case kPvG: pv_run_tiles<I8, PvTileG>(p, epi, s); break;
+        case kPvM: pv_run_tiles<I8, PvTileM>(p, epi, s); break;
+        case kPvN: pv_run_tiles<I8, PvTileN>(p, epi, s); break;
+        default: pv_run_tiles<I8, PvTileS>(p, epi, s);
+    }
 }
 
 // ---- operands (product.hip) ------------------------------------------------
@@ -343,7 +475,6 @@ struct PvPlain {
     PvRows out;
     const float* add;
 };
-void pv_plan_plain(PvProduct& p);
 void pv_launch_plain(const PvProduct& p, const PvPlain& e, hipStream_t s);
 
 // Pieces of a workspace, one behind another.
