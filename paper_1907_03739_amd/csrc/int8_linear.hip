@@ -153,16 +153,16 @@ struct LinearEpi {
     }
     template <int MI>
     __device__ __forceinline__ void tile(const PvProduct& p, int mw, int nw, int lane,
-                                         const pv_i32x4 (&acc)[4][MI], uint8_t*) const {
-        const int r = lane & 15, n = nw + 16 * (lane >> 4);
+                                         const pv_i32x4 (&acc)[4][MI]) const {
+        const int r = lane & 15, nb = nw + 8 * (lane >> 4);
         float sn[16], b[16];
         bool fast = true;
 #pragma unroll
-        for (int c = 0; c < 16; c++) {
-            const int at = min(n + c, p.N - 1);
-            sn[c] = col_scale[at];
-            b[c] = bias ? bias[at] : 0.f;
-            fast = fast && tame(sn[c]);
+        for (int q = 0; q < 16; q++) {
+            const int at = min(pv_col(nb, q), p.N - 1);
+            sn[q] = col_scale[at];
+            b[q] = bias ? bias[at] : 0.f;
+            fast = fast && tame(sn[q]);
         }
 #pragma unroll
         for (int i = 0; i < MI; i++) {
@@ -172,17 +172,17 @@ struct LinearEpi {
             float v[16];
             if (fast && tame(sm)) {
 #pragma unroll
-                for (int c = 0; c < 16; c++)
-                    v[c] = value(acc[c >> 2][i][c & 3], sm, sn[c], b[c], true);
+                for (int q = 0; q < 16; q++)
+                    v[q] = value(acc[q >> 2][i][q & 3], sm, sn[q], b[q], true);
             } else {
 #pragma unroll
-                for (int c = 0; c < 16; c++)
-                    v[c] = value(acc[c >> 2][i][c & 3], sm, sn[c], b[c],
-                                 tame(sm) && tame(sn[c]));
+                for (int q = 0; q < 16; q++)
+                    v[q] = value(acc[q >> 2][i][q & 3], sm, sn[q], b[q],
+                                 tame(sm) && tame(sn[q]));
             }
 #pragma unroll
-            for (int c = 0; c < 16; c++) v[c] = activate(v[c], neg, relu);
-            pv_store_run<16>(out, m, n, p.N, v);
+            for (int q = 0; q < 16; q++) v[q] = activate(v[q], neg, relu);
+            pv_store_runs(out, m, nb, p.N, v);
         }
     }
     __device__ __forceinline__ void one(int m, int n, int acc) const {
@@ -256,13 +256,13 @@ bool few(int M, int N) { return (size_t)((M + 15) / 16) * ((N + 15) / 16) <= kFe
 PvProduct product_of(const int8_t* q, int M, int K, const int8_t* w, int N) {
     PvProduct p{};
     const size_t pitch = pv_up(K, kSlice);
-    p.a = PvPanel{(const uint8_t*)q, pitch, 0, 1};
-    p.b = PvPanel{(const uint8_t*)w, pitch, 0, 1};
+    p.a = PvPanel{(const uint8_t*)q, pitch, 0, 1, M};
+    p.b = PvPanel{(const uint8_t*)w, pitch, 0, 1, N};
     p.M = M;
     p.N = N;
     p.slices = pv_slices(K, kSlice);
     pv_pairs(p, 1, 1);
-    pv_plan_splits(p, 8);
+    pv_plan(p, true);
     return p;
 }
 
@@ -294,7 +294,7 @@ int parts_of(bool out_bf16, bool dy_bf16, int M) {
 }
 
 struct BwdWs {
-    PvPanel dys, wt, dyt, qt;
+    PvPanel dys, w, dym, q;
     PvProduct dx, dw;
     float* sums;
     size_t total;
@@ -309,22 +309,22 @@ BwdWs carve_bwd(void* base, int M, int K, int N, bool dy_bf16, bool dx_bf16, boo
         p.b = b;
         p.M = rows;
         p.N = cols;
-        p.slices = pv_slices(depth, 64);
+        p.slices = pv_slices(depth, kDeep);
         pv_pairs(p, a.parts, b.parts);
-        pv_plan_splits(p, 8);
+        pv_plan(p, true);
         p.partial = (uint32_t*)c.take(pv_partial_bytes(p));
     };
     if (want_dx && M > 0) {
         w.dys = pv_take_panel(c, M, N, parts_of(dx_bf16, dy_bf16, M));
-        w.wt = pv_take_panel(c, K, N, 1);
-        product(w.dx, w.dys, w.wt, M, K, N);
+        w.w = pv_take_panel(c, N, K, 1);
+        product(w.dx, w.dys, w.w, M, K, N);
     }
-    if (want_dw) {
-        w.dyt = pv_take_panel(c, N, M, parts_of(false, dy_bf16, M));
-        w.qt = pv_take_panel(c, K, M, 1);
-        product(w.dw, w.dyt, w.qt, N, K, M);
+    if (want_dw) {  // both operands across k: dy's rows are padded with zeros
+        w.dym = pv_take_panel(c, (int)pv_up(M, kDeep), N, parts_of(false, dy_bf16, M));
+        w.q = pv_take_panel(c, M, K, 1);
+        product(w.dw, w.dym, w.q, N, K, M);
     }
-    if (want_db) w.sums = (float*)c.take(pv_column_sum_bytes(M, N));
+    if (want_db) w.sums = (float*)c.take((size_t)pv_sum_runs(M) * N * 4);
     w.total = c.off;
     return w;
 }
@@ -365,7 +365,7 @@ static pvconv_status run_rows(const int8_t* q, const float* scale, int M, int K,
                               hipStream_t s) {
     PvProduct p = product_of(q, M, K, weight, N);
     p.partial = partial;
-    pv_run_product<true>(p, epi, s);
+    pv_run_product<true, false, false>(p, epi, s);
     return pv_launch_status();
 }
 
@@ -411,8 +411,13 @@ pvconv_status pv_launch_int8_linear_rows(const int8_t* rows, const float* row_sc
 }
 
 size_t pv_int8_linear_bwd_ws_bytes(int M, int K, int N) {
-    // the most that any of the types and outputs takes
-    return carve_bwd(nullptr, M, K, N, false, false, true, true, true).total;
+    size_t most = 0;  // that any of the types takes
+    for (int types = 0; types < 4; types++) {
+        const size_t n =
+            carve_bwd(nullptr, M, K, N, types & 1, types & 2, true, true, true).total;
+        most = most > n ? most : n;
+    }
+    return most;
 }
 
 pvconv_status pv_launch_int8_linear_bwd(const PvRows& dy, const int8_t* rows,
@@ -424,20 +429,24 @@ pvconv_status pv_launch_int8_linear_bwd(const PvRows& dy, const int8_t* rows,
                               dbias != nullptr);
     const PvKind kind = dy.bf16 ? kPvBf16 : kPvF32;
     const size_t qk = pv_up(K, kSlice);
-    if (dx.p && M > 0) {
+    const bool want_dx = dx.p && M > 0;
+    PvPacks packs{};
+    if (want_dx) {
         PvPack a = pv_pack_of(dy.p, kind, dy.ld, M, N, w.dys);
         a.col_scale = scale;
-        pv_launch_pack(a, s);
-        pv_launch_pack_transposed(pv_pack_of(weight, kPvInt8, qk, N, K, w.wt), s);
-        pv_launch_plain(w.dx, PvPlain{dx, nullptr}, s);
+        packs.add(a);
+        packs.add(pv_pack_of(weight, kPvInt8, qk, N, K, w.w));
     }
-    if (dw) {
-        PvPack a = pv_pack_of(dy.p, kind, dy.ld, M, N, w.dyt);
+    if (dw && M > 0) {
+        PvPack a = pv_pack_of(dy.p, kind, dy.ld, M, N, w.dym);
         a.row_scale = row_scale;
-        pv_launch_pack_transposed(a, s);
-        pv_launch_pack_transposed(pv_pack_of(rows, kPvInt8, qk, M, K, w.qt), s);
-        pv_launch_plain(w.dw, PvPlain{PvRows{dw, false, K}, nullptr}, s);
+        packs.add(a);
+        packs.add(pv_pack_of(rows, kPvInt8, qk, M, K, w.q));
     }
-    if (dbias) pv_launch_column_sum(dy, M, N, w.sums, dbias, s);
+    if (dbias && M > 0) packs.add(pv_sums_of(dy, M, N, w.sums));
+    pv_launch_packs(packs, s);
+    if (want_dx) pv_launch_plain(w.dx, false, PvPlain{dx, nullptr}, s);
+    if (dw) pv_launch_plain(w.dw, true, PvPlain{PvRows{dw, false, K}, nullptr}, s);
+    if (dbias) pv_launch_sum_runs(w.sums, pv_sum_runs(M), N, dbias, s);
     return pv_launch_status();
 }

@@ -4,10 +4,10 @@
 // Forward: tiles of the product keep their logits in registers and leave a row's
 // maximum and its sum of exponentials for each 64 classes (and the label's logit);
 // the rows' statistics are joined in a second launch. Backward: the product again,
-// whose epilogue turns a logit into dz = weight (exp(z - lse) - [class = label]), in a
-// piece of the vocabulary at a time and in both orders, dz and its transpose, in bf16
-// parts: dx += dz W and dW = dz^T x are then plain products. Up to 64 classes, a wave
-// holds whole rows: loss and dz come from one product.
+// whose epilogue turns a logit into dz = weight (exp(z - lse) - [class = label]), in
+// bf16 parts, for a piece of the vocabulary at a time: dx += dz W and dW = dz^T x are
+// then plain products, of W, dz and x as they lie (pv_product.h). Up to 64 classes, a
+// wave holds whole rows: loss and dz come from one product.
 #include "pv_product.h"
 #include "pv_wave.h"
 
@@ -19,7 +19,7 @@ constexpr float kInf = __builtin_huge_valf();
 struct DzPanel {  // where dz goes: bf16 parts, rows of a pitch in bytes (p NULL: nowhere)
     uint8_t* p;
     size_t pitch, part_bytes;
-    int parts;
+    int parts, rows;  // zeros from the last row on
 };
 
 struct Ce {
@@ -32,7 +32,7 @@ struct Ce {
     float* loss;
     float* lse;
     const float* weight;    // [M] or NULL
-    DzPanel dz, dzt;        // [M][piece], [piece][M]
+    DzPanel dz;             // [M][piece]
     float* sums;            // [row blocks][piece]: dz summed over a wave's rows, or NULL
 };
 
@@ -60,141 +60,97 @@ template <int MODE, bool PARTS>
 struct CeEpi {
     Ce c;
 
-    // One part of dz of two times sixteen rows of a wave (row 16 i + r, sixteen columns a
-    // lane): rows by 32-byte runs, columns through LDS
-    __device__ __forceinline__ void store(const PvProduct& p, int part, int m, int mw, int nw,
-                                          int lane, const uint32_t (&w)[2][8],
-                                          uint8_t* lds) const {
-        const int r = lane & 15, h = lane >> 4, n = nw + 16 * h;
-        if (c.dz.p && part < c.dz.parts && (size_t)n * 2 < c.dz.pitch) {
+    // one part of dz of a row: two runs of eight classes a lane
+    __device__ __forceinline__ void store(int part, int m, int nb, float (&d)[16]) const {
 #pragma unroll
-            for (int i = 0; i < 2; i++) {
-                if (m + 16 * i >= p.M) continue;
-                pv_u32x4* o = (pv_u32x4*)(c.dz.p + part * c.dz.part_bytes +
-                                          (size_t)(m + 16 * i) * c.dz.pitch + (size_t)n * 2);
-                o[0] = pv_u32x4{w[i][0], w[i][1], w[i][2], w[i][3]};
-                o[1] = pv_u32x4{w[i][4], w[i][5], w[i][6], w[i][7]};
-            }
-        }
-        if (!c.dzt.p || part >= c.dzt.parts) return;
-        // [64 columns][32 rows] of bf16; 16-byte pieces at piece ^ (column >> 4)
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-        __builtin_amdgcn_wave_barrier();
+        for (int a = 0; a < 2; a++) {
+            pv_u32x4 w;
 #pragma unroll
-        for (int i = 0; i < 2; i++)
-#pragma unroll
-            for (int q = 0; q < 8; q++) {
-                const int at = (((2 * i + (r >> 3)) ^ h) << 4) + (r & 7) * 2;
-                *(uint16_t*)(lds + (16 * h + 2 * q) * 64 + at) = (uint16_t)w[i][q];
-                *(uint16_t*)(lds + (16 * h + 2 * q + 1) * 64 + at) = (uint16_t)(w[i][q] >> 16);
-            }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-#pragma unroll
-        for (int u = 0; u < 4; u++) {
-            const int col = u * 16 + (lane >> 2), piece = lane & 3;
-            const pv_u32x4 v = *(const pv_u32x4*)(lds + col * 64 + ((piece ^ u) << 4));
-            const size_t at = (size_t)(mw + 8 * piece) * 2;
-            if (nw + col < p.N && at < c.dzt.pitch)
-                *(pv_u32x4*)(c.dzt.p + part * c.dzt.part_bytes + (size_t)(nw + col) * c.dzt.pitch +
-                             at) = v;
+            for (int q = 0; q < 4; q++) w[q] = next_part2(d[8 * a + 2 * q], d[8 * a + 2 * q + 1]);
+            const size_t at = (size_t)(nb + 32 * a) * 2;
+            if (m < c.dz.rows && at < c.dz.pitch)
+                *(pv_u32x4*)(c.dz.p + part * c.dz.part_bytes + (size_t)m * c.dz.pitch + at) = w;
         }
     }
 
     template <int MI>
     __device__ __forceinline__ void tile(const PvProduct& p, int mw, int nw, int lane,
-                                         const pv_f32x4 (&acc)[4][MI], uint8_t* lds) const {
-        const int r = lane & 15, h = lane >> 4, n = nw + 16 * h;
+                                         const pv_f32x4 (&acc)[4][MI]) const {
+        const int r = lane & 15, h = lane >> 4, nb = nw + 8 * h;
         float b[16], cs[16];
 #pragma unroll
         for (int q = 0; q < 16; q++) {
-            b[q] = c.bias ? c.bias[min(n + q, p.N - 1)] : 0.f;
+            b[q] = c.bias ? c.bias[min(pv_col(nb, q), p.N - 1)] : 0.f;
             cs[q] = 0.f;
         }
-        const bool grads = MODE == kGrad || (MODE == kWhole && (c.dz.p || c.dzt.p || c.sums));
+        const bool grads = MODE == kGrad || (MODE == kWhole && (c.dz.p || c.sums));
 #pragma unroll
-        for (int i0 = 0; i0 < MI; i0 += 2) {
-            uint32_t w[2][8];
-            float d[PARTS ? 2 : 1][16];
+        for (int i = 0; i < MI; i++) {
+            const int m = mw + 16 * i + r, mc = min(m, p.M - 1);
+            const int label = c.labels[mc];
+            const bool known = label >= 0 && label < c.V;
+            // which of the lane's sixteen classes the label is, if any
+            const unsigned to = (unsigned)label - (unsigned)(c.v0 + nb);
+            const int at = to < 8u ? (int)to : to - 32u < 8u ? (int)to - 24 : -1;
+            float z[16];
 #pragma unroll
-            for (int i = 0; i < 2; i++) {
-                float(&di)[16] = d[PARTS ? i : 0];
-                const int m = mw + 16 * (i0 + i) + r, mc = min(m, p.M - 1);
-                const int label = c.labels[mc], at = label - c.v0 - n;
-                const bool known = label >= 0 && label < c.V;
-                float z[16];
+            for (int q = 0; q < 16; q++) {
+                z[q] = acc[q >> 2][i][q & 3] + b[q];
+                // columns past the last hold a copy of it: a logit that is not a number
+                // there would stay one
+                if (pv_col(nb, q) >= p.N) z[q] = -kInf;
+            }
+            float lse = 0.f;
+            if constexpr (MODE != kGrad) {
+                float top = z[0];
+#pragma unroll
+                for (int q = 1; q < 16; q++) top = fmaxf(top, z[q]);
+                top = lanes_max(top);
+                // (every logit -inf, or not a number: fmaxf passes NaN over)
+                const float about = top == -kInf ? 0.f : top;
+                float sum = 0.f, zl = 0.f;
 #pragma unroll
                 for (int q = 0; q < 16; q++) {
-                    z[q] = acc[q >> 2][i0 + i][q & 3] + b[q];
-                    // columns past the last hold a copy of it: a logit that is not a
-                    // number there would stay one
-                    if (n + q >= p.N) z[q] = -kInf;
+                    sum += __expf(z[q] - about);
+                    if (q == at) zl = z[q];
                 }
-                float lse = 0.f;
-                if constexpr (MODE != kGrad) {
-                    float top = z[0];
-#pragma unroll
-                    for (int q = 1; q < 16; q++) top = fmaxf(top, z[q]);
-                    top = lanes_max(top);
-                    // (every logit -inf, or not a number: fmaxf passes NaN over)
-                    const float about = top == -kInf ? 0.f : top;
-                    float sum = 0.f, zl = 0.f;
-#pragma unroll
-                    for (int q = 0; q < 16; q++) {
-                        sum += __expf(z[q] - about);
-                        if (q == at) zl = z[q];
-                    }
-                    sum = lanes_sum(sum);
-                    if constexpr (MODE == kStats) {
-                        if (m < p.M) {
-                            if (h == 0 && nw < p.N)
-                                c.stats[(size_t)m * c.nb + (unsigned)nw / 64] =
-                                    make_float2(top, sum);
-                            if (known && (unsigned)at < 16u) c.zlab[m] = zl;
-                        }
-                    } else {
-                        lse = sum == 0.f ? -kInf : about + logf(sum);
-                        zl = lanes_sum(known && (unsigned)at < 16u ? zl : 0.f);
-                        if (m < p.M && h == 0) {
-                            c.lse[m] = lse;
-                            c.loss[m] = known && lse != -kInf ? lse - zl : 0.f;
-                        }
+                sum = lanes_sum(sum);
+                if constexpr (MODE == kStats) {
+                    if (m < p.M) {
+                        if (h == 0 && nw < p.N)
+                            c.stats[(size_t)m * c.nb + (unsigned)nw / 64] = make_float2(top, sum);
+                        if (known && at >= 0) c.zlab[m] = zl;
                     }
                 } else {
-                    lse = c.lse[mc];
-                }
-                if (grads) {
-                    float g = m < p.M && known && lse != -kInf ? 1.f : 0.f;
-                    if (g != 0.f && c.weight) g = c.weight[mc];
-#pragma unroll
-                    for (int q = 0; q < 16; q++) {
-                        const float e = __expf(z[q] - lse) - (q == at ? 1.f : 0.f);
-                        di[q] = g == 0.f ? 0.f : n + q < p.N ? g * e : 0.f;
-                        cs[q] += di[q];
+                    lse = sum == 0.f ? -kInf : about + logf(sum);
+                    zl = lanes_sum(known && at >= 0 ? zl : 0.f);
+                    if (m < p.M && h == 0) {
+                        c.lse[m] = lse;
+                        c.loss[m] = known && lse != -kInf ? lse - zl : 0.f;
                     }
-#pragma unroll
-                    for (int q = 0; q < 8; q++) w[i][q] = next_part2(di[2 * q], di[2 * q + 1]);
                 }
+            } else {
+                lse = c.lse[mc];
             }
             if (MODE != kStats && grads) {
-                const int m = mw + 16 * i0;
-                store(p, 0, m + r, m, nw, lane, w, lds);
-                if constexpr (PARTS) {
-                    const int parts = max(c.dz.p ? c.dz.parts : 0, c.dzt.p ? c.dzt.parts : 0);
-                    for (int part = 1; part < parts; part++) {
+                float g = m < p.M && known && lse != -kInf ? 1.f : 0.f;
+                if (g != 0.f && c.weight) g = c.weight[mc];
 #pragma unroll
-                        for (int i = 0; i < 2; i++)
-#pragma unroll
-                            for (int q = 0; q < 8; q++)
-                                w[i][q] = next_part2(d[i][2 * q], d[i][2 * q + 1]);
-                        store(p, part, m + r, m, nw, lane, w, lds);
-                    }
+                for (int q = 0; q < 16; q++) {
+                    const float e = __expf(z[q] - lse) - (q == at ? 1.f : 0.f);
+                    z[q] = g == 0.f || pv_col(nb, q) >= p.N ? 0.f : g * e;
+                    cs[q] += z[q];
+                }
+                if (c.dz.p) {
+                    store(0, m, nb, z);
+                    if constexpr (PARTS)
+                        for (int part = 1; part < c.dz.parts; part++) store(part, m, nb, z);
                 }
             }
         }
         if (MODE != kStats && grads && c.sums) {
             // over the 16 rows of lanes: halves of the columns change places, so that
-            // lane r is left with column r's sum
+            // lane r is left with the sum of column r
 #pragma unroll
             for (int w = 8; w; w >>= 1) {
                 const bool up = r & w;
@@ -204,8 +160,8 @@ struct CeEpi {
                     cs[q] = keep + __shfl_xor(give, w);
                 }
             }
-            const int block = mw / (16 * MI);
-            if (n + r < p.N) c.sums[(size_t)block * p.N + n + r] = cs[0];
+            const int block = mw / (16 * MI), n = pv_col(nb, r);
+            if (n < p.N) c.sums[(size_t)block * p.N + n] = cs[0];
         }
     }
     __device__ __forceinline__ void one(int, int, float) const {}  // never split
@@ -278,11 +234,12 @@ int dz_parts_of(bool bf16, int M) { return !bf16 ? 3 : M <= kFewRows ? 2 : 1; }
 int factor_parts_of(bool out_bf16, bool bf16) { return bf16 ? 1 : out_bf16 ? 2 : 3; }
 
 struct Plan {
-    PvPanel x, w;             // what the logits are products of
+    PvPanel x, w;             // what every product takes
     bool pack_x, pack_w;
-    bool whole, parts;  // parts: dz in more than one
+    bool whole, parts;        // parts: dz in more than one
+    unsigned grad_sizes;
     int forward_classes, classes;  // a piece's
-    PvPanel dz, dzt, wt, xt;
+    PvPanel dz;
     PvProduct dx, dw;         // of a piece of `classes`
     float2 *stats, *run;
     float *zlab, *lse, *sums, *acc;
@@ -298,20 +255,37 @@ template <class T>
 int row_blocks_of(int M) {
     return (int)(pv_up(M, T::TM) / (16 * T::MI));
 }
-// Up to 64 classes a wave has whole rows: tiles of 64 columns. Beside the sums of the
-// largest tiles there are no registers for dz, of middle ones none for parts of it.
-int size_of(int M, int n, bool whole, bool grad, bool parts) {
-    if (whole) return pv_tiles_of(M, n, 128, 64) >= 128 ? kPvN : kPvS;
-    const int size = pv_size_of(M, n);
-    return size == kPvL && grad ? (parts ? kPvM : kPvG) : size;
-}
 int row_blocks(int M, int size) {  // as many as waves have rows
     switch (size) {
+        case kPvL: return row_blocks_of<PvTileL>(M);
         case kPvG: return row_blocks_of<PvTileG>(M);
         case kPvM: return row_blocks_of<PvTileM>(M);
         case kPvN: return row_blocks_of<PvTileN>(M);
         default: return row_blocks_of<PvTileS>(M);
     }
+}
+// The tiles of an epilogue. A wave that has whole rows has all of 64 columns; beside the
+// sums of the largest tiles there are no registers for dz, of the next none for what its
+// first part leaves.
+constexpr unsigned sizes_of(int mode, bool parts) {
+    const unsigned narrow = 1u << kPvS | 1u << kPvN;
+    if (mode == kWhole) return narrow;
+    if (mode == kStats) return kPvAnySize;
+    return narrow | 1u << kPvM | (parts ? 0u : 1u << kPvG);
+}
+// The product of x with n classes from v0 on.
+PvProduct logits_of(const PvPanel& x, const PvPanel& w, int M, int K, int v0, int n,
+                    unsigned sizes) {
+    PvProduct q{};
+    q.a = x;
+    q.b = w;
+    q.b.p += (size_t)v0 * w.pitch;
+    q.M = M;
+    q.N = n;
+    q.slices = pv_slices(K, kDeep);
+    pv_pairs(q, x.parts, w.parts);
+    pv_plan(q, false, sizes);
+    return q;
 }
 
 Plan carve(void* base, const PvLinearCe& a, bool forward, bool grads, bool may_direct) {
@@ -323,7 +297,7 @@ Plan carve(void* base, const PvLinearCe& a, bool forward, bool grads, bool may_d
         if (pack)
             to = pv_take_panel(c, rows, a.K, parts_of(r.bf16));
         else
-            to = PvPanel{(const uint8_t*)r.p, (size_t)r.ld * 2, 0, 1};
+            to = PvPanel{(const uint8_t*)r.p, (size_t)r.ld * 2, 0, 1, rows};
     };
     operand(a.x, a.M, p.x, p.pack_x);
     operand(a.w, a.V, p.w, p.pack_w);
@@ -346,20 +320,21 @@ Plan carve(void* base, const PvLinearCe& a, bool forward, bool grads, bool may_d
     const bool want_dx = a.dx.p != nullptr, want_dw = a.dw.p != nullptr;
     const int px = dz_parts_of(a.dx.bf16, a.M), pw = dz_parts_of(a.dw.bf16, a.M);
     // (of both, wanted or not: the workspace of fewer gradients is then no larger)
-    const size_t per = pv_up(a.M > 0 ? a.M : 1, 64) * 2 * (px + pw);
+    const size_t per = pv_up(a.M > 0 ? a.M : 1, 64) * 2 * (px > pw ? px : pw);
     size_t n = kPieceBytes / per / 256 * 256;
     if (n < (size_t)kLeastClasses) n = kLeastClasses;
     p.classes = n >= (size_t)a.V ? a.V : (int)n;
     p.parts = px > 1 || pw > 1;
+    p.grad_sizes = sizes_of(p.whole ? kWhole : kGrad, p.parts);
     auto product = [&](PvProduct& q, const PvPanel& x, const PvPanel& y, int rows, int cols,
                        int depth) {
         q.a = x;
         q.b = y;
         q.M = rows;
         q.N = cols;
-        q.slices = pv_slices(depth, 64);
+        q.slices = pv_slices(depth, kDeep);
         pv_pairs(q, x.parts, y.parts);
-        pv_plan_splits(q, 8);
+        pv_plan(q, true);
     };
     // the splits' sums of a whole piece and of the last one, which may have fewer classes
     size_t partial = 0;
@@ -368,36 +343,44 @@ Plan carve(void* base, const PvLinearCe& a, bool forward, bool grads, bool may_d
         const size_t b = pv_partial_bytes(q);
         partial = partial > b ? partial : b;
     };
+    const int pz = want_dx && want_dw ? (px > pw ? px : pw) : want_dx ? px : pw;
+    if (want_dx || want_dw)
+        p.dz = pv_take_panel(c, (int)pv_up(a.M, kDeep), p.classes, pz);
     if (want_dx) {
-        p.dz = pv_take_panel(c, a.M, p.classes, px);
-        p.wt = pv_take_panel(c, a.K, p.classes, factor_parts_of(a.dx.bf16, a.w.bf16));
-        product(p.dx, p.dz, p.wt, a.M, a.K, p.classes);
+        PvPanel dz = p.dz, w = p.w;
+        dz.parts = px;
+        if (a.dx.bf16 && w.parts > 2) w.parts = 2;
+        product(p.dx, dz, w, a.M, a.K, p.classes);
         sums(p.dx);
         if (tail) {
             PvProduct q = p.dx;
-            q.slices = pv_slices(tail, 64);
-            pv_plan_splits(q, 8);
+            q.slices = pv_slices(tail, kDeep);
+            pv_plan(q, true);
             sums(q);
         }
         if (p.classes < a.V) p.acc = (float*)c.take((size_t)a.M * a.K * 4);
     }
     if (want_dw) {
-        p.dzt = pv_take_panel(c, p.classes, a.M, pw);
-        p.xt = pv_take_panel(c, a.K, a.M, factor_parts_of(a.dw.bf16, a.x.bf16));
-        product(p.dw, p.dzt, p.xt, p.classes, a.K, a.M);
+        PvPanel dz = p.dz, x = p.x;
+        dz.parts = pw;
+        if (a.dw.bf16 && x.parts > 2) x.parts = 2;
+        product(p.dw, dz, x, p.classes, a.K, a.M);
         sums(p.dw);
         if (tail) {
             PvProduct q = p.dw;
             q.M = tail;
-            pv_plan_splits(q, 8);
+            pv_plan(q, true);
             sums(q);
         }
     }
     p.partial = (uint32_t*)c.take(partial);
     if (a.dbias) {
         // (of a smaller last piece too, whose tiles may be smaller)
-        const size_t b = (size_t)row_blocks(a.M, size_of(a.M, p.classes, p.whole, true, p.parts)) * p.classes,
-                     t = tail ? (size_t)row_blocks(a.M, size_of(a.M, tail, p.whole, true, p.parts)) * tail : 0;
+        const auto need = [&](int n) {
+            const PvProduct q = logits_of(p.x, p.w, a.M, a.K, 0, n, p.grad_sizes);
+            return (size_t)row_blocks(a.M, q.size) * n;
+        };
+        const size_t b = need(p.classes), t = tail ? need(tail) : 0;
         p.sums = (float*)c.take((b > t ? b : t) * 4);
     }
     p.total = c.off;
@@ -406,21 +389,14 @@ Plan carve(void* base, const PvLinearCe& a, bool forward, bool grads, bool may_d
 
 template <int MODE>
 void run_logits(const PvProduct& p, const Ce& c, bool parts, hipStream_t s) {
-    if constexpr (MODE == kStats) {
-        pv_run_product<false>(p, CeEpi<MODE, false>{c}, s);
-    } else if (p.size == kPvS || p.size == kPvN) {  // all that whole rows take
-        const CeEpi<MODE, true> epi{c};
-        if (p.size == kPvN)
-            pv_run_tiles<false, PvTileN>(p, epi, s);
-        else
-            pv_run_tiles<false, PvTileS>(p, epi, s);
-    } else if constexpr (MODE == kGrad) {
-        if (parts)
-            pv_run_tiles<false, PvTileM>(p, CeEpi<MODE, true>{c}, s);
-        else if (p.size == kPvM)
-            pv_run_tiles<false, PvTileM>(p, CeEpi<MODE, false>{c}, s);
-        else
-            pv_run_tiles<false, PvTileG>(p, CeEpi<MODE, false>{c}, s);
+    if constexpr (MODE == kWhole) {
+        pv_run_product<false, false, false, sizes_of(MODE, true)>(p, CeEpi<MODE, true>{c}, s);
+    } else if constexpr (MODE == kStats) {
+        pv_run_product<false, false, false>(p, CeEpi<MODE, false>{c}, s);
+    } else if (parts) {
+        pv_run_product<false, false, false, sizes_of(MODE, true)>(p, CeEpi<MODE, true>{c}, s);
+    } else {
+        pv_run_product<false, false, false, sizes_of(MODE, false)>(p, CeEpi<MODE, false>{c}, s);
     }
 }
 
@@ -435,23 +411,12 @@ pvconv_status pv_launch_linear_ce(const PvLinearCe& a, bool forward, void* ws, h
     const Plan p = carve(ws, a, forward, grads, true);
     float* lse = a.lse ? a.lse : p.lse;
     auto kind = [](const PvRows& r) { return r.bf16 ? kPvBf16 : kPvF32; };
-    if (p.pack_x) pv_launch_pack(pv_pack_of(a.x.p, kind(a.x), a.x.ld, a.M, a.K, p.x), s);
-    if (p.pack_w && a.M > 0)
-        pv_launch_pack(pv_pack_of(a.w.p, kind(a.w), a.w.ld, a.V, a.K, p.w), s);
-    // the product of a run of classes, whose epilogue is given
-    auto logits = [&](int v0, int n, bool grad) {
-        PvProduct q{};
-        q.a = p.x;
-        q.b = p.w;
-        q.b.p += (size_t)v0 * p.w.pitch;
-        q.M = a.M;
-        q.N = n;
-        q.slices = pv_slices(a.K, 64);
-        pv_pairs(q, p.x.parts, p.w.parts);
-        q.per = q.slices * q.pairs;
-        q.splits = 1;
-        q.size = size_of(a.M, n, p.whole, grad, p.parts);
-        return q;
+    PvPacks packs{};
+    if (p.pack_x && a.M > 0) packs.add(pv_pack_of(a.x.p, kind(a.x), a.x.ld, a.M, a.K, p.x));
+    if (p.pack_w && a.M > 0) packs.add(pv_pack_of(a.w.p, kind(a.w), a.w.ld, a.V, a.K, p.w));
+    pv_launch_packs(packs, s);
+    auto logits = [&](int v0, int n, unsigned sizes) {
+        return logits_of(p.x, p.w, a.M, a.K, v0, n, sizes);
     };
     Ce c{};
     c.labels = a.labels;
@@ -459,9 +424,6 @@ pvconv_status pv_launch_linear_ce(const PvLinearCe& a, bool forward, void* ws, h
     c.weight = a.weight;
     c.lse = lse;
     c.loss = a.loss;
-    auto panel = [](const PvPanel& q) {
-        return DzPanel{(uint8_t*)q.p, q.pitch, q.part_bytes, q.parts};
-    };
     if (forward && !p.whole) {
         for (int v0 = 0; v0 < a.V; v0 += p.forward_classes) {
             const int n = a.V - v0 < p.forward_classes ? a.V - v0 : p.forward_classes;
@@ -470,7 +432,7 @@ pvconv_status pv_launch_linear_ce(const PvLinearCe& a, bool forward, void* ws, h
             c.stats = p.stats;
             c.nb = (n + 63) / 64;
             c.zlab = p.zlab;
-            run_logits<kStats>(logits(v0, n, false), c, false, s);
+            run_logits<kStats>(logits(v0, n, kPvAnySize), c, false, s);
             const Join j{p.stats, c.nb, a.M, a.V, p.run, v0 == 0, v0 + n == a.V, a.labels, p.zlab,
                          a.loss, lse};
             if (a.M > 0) {
@@ -484,50 +446,44 @@ pvconv_status pv_launch_linear_ce(const PvLinearCe& a, bool forward, void* ws, h
         }
     } else if (forward && !grads) {
         c.bias = a.bias;
-        run_logits<kWhole>(logits(0, a.V, false), c, false, s);
+        run_logits<kWhole>(logits(0, a.V, sizes_of(kWhole, true)), c, false, s);
     }
     if (!grads) return pv_launch_status();
-    if (a.dw.p) pv_launch_pack_transposed(pv_pack_of(a.x.p, kind(a.x), a.x.ld, a.M, a.K, p.xt), s);
     for (int v0 = 0; v0 < a.V; v0 += p.classes) {
         const int n = a.V - v0 < p.classes ? a.V - v0 : p.classes;
         c.v0 = v0;
         c.bias = a.bias ? a.bias + v0 : nullptr;
         c.sums = p.sums;
-        PvPanel dz = p.dz, dzt = p.dzt, wt = p.wt;
-        dz.pitch = wt.pitch = pv_up(n, 64) * 2;
-        c.dz = panel(dz);
-        c.dzt = panel(dzt);
-        const PvProduct z = logits(v0, n, true);
+        const size_t pitch = pv_up(n, 64) * 2;
+        c.dz = DzPanel{(uint8_t*)p.dz.p, pitch, p.dz.part_bytes, p.dz.parts, p.dz.rows};
+        const PvProduct z = logits(v0, n, p.grad_sizes);
         if (p.whole && forward)
             run_logits<kWhole>(z, c, p.parts, s);
         else
             run_logits<kGrad>(z, c, p.parts, s);
         if (a.dx.p && a.M > 0) {
-            const size_t es = a.w.bf16 ? 2 : 4;
-            pv_launch_pack_transposed(
-                pv_pack_of((const char*)a.w.p + (size_t)v0 * a.w.ld * es, kind(a.w), a.w.ld, n,
-                           a.K, wt),
-                s);
             PvProduct q = p.dx;
-            q.a = dz;
-            q.b = wt;
-            q.slices = pv_slices(n, 64);
-            pv_plan_splits(q, 8);
+            q.a.pitch = pitch;
+            q.b.p += (size_t)v0 * q.b.pitch;
+            q.b.rows = n;
+            q.slices = pv_slices(n, kDeep);
+            pv_plan(q, true);
             q.partial = p.partial;
             const bool last = v0 + n == a.V;
-            pv_launch_plain(q, PvPlain{last ? a.dx : PvRows{p.acc, false, a.K},
-                                       v0 ? p.acc : nullptr}, s);
+            pv_launch_plain(q, false, PvPlain{last ? a.dx : PvRows{p.acc, false, a.K},
+                                              v0 ? p.acc : nullptr}, s);
         }
         if (a.dw.p) {
             PvProduct q = p.dw;
+            q.a.pitch = pitch;
             q.M = n;
-            pv_plan_splits(q, 8);
+            pv_plan(q, true);
             q.partial = p.partial;
             const size_t es = a.dw.bf16 ? 2 : 4;
-            pv_launch_plain(q, PvPlain{PvRows{(char*)a.dw.p + (size_t)v0 * a.dw.ld * es,
-                                              a.dw.bf16, a.dw.ld}, nullptr}, s);
+            pv_launch_plain(q, true, PvPlain{PvRows{(char*)a.dw.p + (size_t)v0 * a.dw.ld * es,
+                                                    a.dw.bf16, a.dw.ld}, nullptr}, s);
         }
-        if (a.dbias) pv_launch_sum_parts(p.sums, row_blocks(a.M, z.size), n, a.dbias + v0, s);
+        if (a.dbias) pv_launch_sum_runs(p.sums, row_blocks(a.M, z.size), n, a.dbias + v0, s);
     }
     return pv_launch_status();
 }

@@ -1,7 +1,11 @@
-// Products a b^T of two row-major operands on the matrix cores, whose rows are
-// whole slices of 128 bytes: 64 bf16 values (fp32 sums) or 128 8-bit integers
-// (32-bit integer sums). The 8-bit integer layer and the linear cross entropy
-// give it their epilogues.
+// Products on the matrix cores, out[m][n] = sum_k a(m, k) b(n, k), of 64 bf16 values
+// (fp32 sums) or 128 8-bit integers (32-bit integer sums) a slice. The 8-bit integer
+// layer and the linear cross entropy give it their operands and epilogues.
+//
+// An operand lies along k (a row of memory is a row of the operand, whole slices of 128
+// bytes, zeros behind its end) or across it (bf16 only: a row of memory is one k, as x and
+// dy are for x^T dy; the LDS loads transpose). Of an operand across k the rows past its
+// last are read as that one, so that the other operand's have to be zero there.
 //
 // A 32-bit value can be an operand in up to three bf16 parts, h = bf16(v), m =
 // bf16(v - h), l = bf16(v - h - m): 24 bits in all. The product of such operands
@@ -18,26 +22,29 @@ typedef int pv_i32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t pv_u32x4 __attribute__((ext_vector_type(4)));
 typedef pv_u32x4 pv_u32x4_any __attribute__((aligned(2)));
 typedef __bf16 pv_b16x8 __attribute__((ext_vector_type(8)));
+typedef short pv_s16x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kSlice = 128;  // bytes
+constexpr int kSlice = 128;  // bytes of a row along k
+constexpr int kDeep = 64;    // k of a slice of bf16
 
-__host__ __device__ static inline int pv_slices(int n, int per) { return (n + per - 1) / per; }
+static inline int pv_slices(int n, int per) { return (n + per - 1) / per; }
 static inline size_t pv_up(size_t n, size_t to) { return (n + to - 1) / to * to; }
 
 struct PvPanel {  // rows at p + part * part_bytes + row * pitch
     const uint8_t* p;
     size_t pitch, part_bytes;
     int parts;
+    int rows;  // that may be read (used across k)
 };
 struct PvProduct {
     PvPanel a, b;
     int M, N, slices;
     int pairs;
     uint32_t pa, pb;     // pair t multiplies part (pa >> 4t) & 15 of a by that of b
+    int size;            // PvSize
     int splits, per;     // slices (of all pairs) a split; partial sums where splits > 1
     uint32_t* partial;   // [splits][M][N], 32-bit words
     uint32_t first, count;  // the tiles of this launch (pv_run_tiles)
-    int size;            // PvSize
 };
 
 // The pairs of parts of two operands that a product needs: to 24 bits, or to 16 where
@@ -58,18 +65,18 @@ static inline void pv_pairs(PvProduct& p, int parts_a, int parts_b) {
 
 // Tiles: WM x WN waves of 16 MI rows by 64 columns each; ST stages of slices in LDS, ST -
 // 1 of them under way while one is multiplied.
-template <int WM_, int WN_, int MI_, int ST_, int PER_CU_, int KB_ = 128>
+template <int WM_, int WN_, int MI_, int ST_, int PER_CU_>
 struct PvTile {
     static constexpr int WM = WM_, WN = WN_, MI = MI_, ST = ST_;
-    static constexpr int KB = KB_;  // bytes of a row that a stage holds
     static constexpr int TM = WM * MI * 16, TN = WN * 64, kThreads = 64 * WM * WN;
     static constexpr int kWorkgroups = 256 * PER_CU_;  // that the chip holds at once
 };
 typedef PvTile<2, 4, 8, 2, 1> PvTileL;  // 256 x 256
-typedef PvTile<4, 2, 4, 3, 1> PvTileG;  // 256 x 128: half the sums in registers
+typedef PvTile<4, 2, 4, 3, 1> PvTileG;  // 256 x 128
 typedef PvTile<2, 2, 4, 4, 1> PvTileM;  // 128 x 128
-typedef PvTile<4, 1, 2, 4, 1> PvTileN;  // 128 x 64: few columns
-typedef PvTile<2, 1, 2, 4, 2> PvTileS;  // 64 x 64: few tiles
+typedef PvTile<4, 1, 2, 4, 1> PvTileN;  // 128 x 64
+typedef PvTile<2, 1, 2, 4, 2> PvTileS;  // 64 x 64
+enum PvSize { kPvS, kPvN, kPvM, kPvG, kPvL };
 
 // The tile of index idx: eight tiles of rows by the columns in turn, so that an XCD,
 // which works on neighbours at a time, has both operands in its L2.
@@ -93,17 +100,17 @@ struct PvAcc<true> {
     typedef pv_i32x4 type;
 };
 
-// 16-byte pieces of a stage's row are kept at piece ^ key(row) in LDS, so that the rows
-// which eight neighbouring lanes read lie in different banks (rows of a: consecutive; rows
-// of b: 16 (r >> 2) + 4 j + (r & 3), which leaves a lane 16 consecutive columns of the
-// result).
-template <int KB>
-__device__ __forceinline__ int pv_key_a(int row) {
-    return KB == 128 ? row & 7 : (row >> 1) & 3;
-}
-template <int KB>
-__device__ __forceinline__ int pv_key_b(int row) {
-    return KB == 128 ? (row & 3) | ((row >> 2) & 4) : ((row >> 1) & 1) | ((row >> 3) & 2);
+// LDS holds an operand along k as [row][128 bytes], its 16-byte pieces at piece ^
+// key(row): the rows that eight neighbouring lanes read lie in different banks. (Of a
+// those are consecutive, of b the rows 32 (j >> 1) + 8 (r >> 2) + 4 (j & 1) + (r & 3),
+// which leaves a lane two runs of eight columns of the result.) An operand across k is
+// [k][columns], its 32-byte chunks (sixteen columns) at chunk ^ key(k): a transposing load
+// takes 32 bytes of sixteen k's.
+__device__ __forceinline__ int pv_key_a(int row) { return row & 7; }
+__device__ __forceinline__ int pv_key_b(int row) { return (row & 3) | ((row >> 1) & 4); }
+template <int COLS>
+__device__ __forceinline__ int pv_key_across(int k) {
+    return COLS >= 128 ? (k & 3) | ((k >> 1) & 4) : ((k >> 1) & 1) | ((k >> 2) & 2);
 }
 
 // f(0), .. f(N - 1) with the index as a constant: arrays that it indexes stay in registers
@@ -123,22 +130,77 @@ __device__ __forceinline__ void pv_wait_loads() {
     __builtin_amdgcn_s_waitcnt((VM & 15) | (7 << 4) | ((VM >> 4) << 14));
 }
 
-// The epilogue gets acc[j][i][e]: row mw + 16 i + r, column nw + 16 h + 4 j + e (r =
-// lane & 15, h = lane >> 4), and 4 KB of LDS a wave that nothing else uses then. A
-// workgroup takes several tiles in turn: the first slices of the next one are under way
-// during the epilogue.
-template <bool I8, class T, class Epi>
+// Where the loads of an operand's slices come from: SIZE rows (columns, across k) from
+// `at` on of the `limit` that it has, Q loads of 16 bytes a lane.
+template <bool ACROSS, bool B, int SIZE, int THREADS>
+struct PvSource {
+    static constexpr int Q = SIZE * 8 / THREADS;
+    static constexpr int kPieces = ACROSS ? SIZE / 8 : 8;  // of a row in LDS
+    const uint8_t* g[Q];
+    __device__ __forceinline__ static int row_of(int q, int wave, int lane) {
+        return ((wave * Q + q) * 64 + lane) / kPieces;
+    }
+    __device__ __forceinline__ void enter(const PvPanel& p, int at, int limit, int wave,
+                                          int lane) {
+#pragma unroll
+        for (int q = 0; q < Q; q++) {
+            const int row = row_of(q, wave, lane), c = lane % kPieces;
+            if constexpr (ACROSS) {
+                const int col = ((((c >> 1) ^ pv_key_across<SIZE>(row)) << 1) + (c & 1)) * 8;
+                g[q] = p.p + (size_t)min(at + col, ((limit + 7) & ~7) - 8) * 2;
+            } else {
+                const int key = B ? pv_key_b(row) : pv_key_a(row);
+                g[q] = p.p + (size_t)min(at + row, limit - 1) * p.pitch + (c ^ key) * 16;
+            }
+        }
+    }
+    __device__ __forceinline__ void load(const PvPanel& p, int part, int k, int q, int wave,
+                                         int lane, uint8_t* lds) const {
+        const uint8_t* from = g[q] + part * p.part_bytes;
+        if constexpr (ACROSS)
+            from += (size_t)min(k * kDeep + row_of(q, wave, lane), p.rows - 1) * p.pitch;
+        else
+            from += (size_t)k * kSlice;
+        __builtin_amdgcn_global_load_lds(
+            (const void __attribute__((address_space(1)))*)from,
+            (void __attribute__((address_space(3)))*)(lds + (wave * Q + q) * 1024), 16, 0, 0);
+    }
+};
+
+// The matrix operand of a lane out of an operand across k: eight k's of one of sixteen
+// columns, whose four groups of four begin at the columns `col` of the lanes 0 .. 3.
+template <int COLS>
+__device__ __forceinline__ pv_u32x4 pv_load_across(const uint8_t* lds, int k0, int col, int lane) {
+    pv_u32x4 v;
+#pragma unroll
+    for (int s = 0; s < 2; s++) {
+        const int k = k0 + 8 * (lane >> 4) + 4 * s + ((lane >> 2) & 3);
+        const uint8_t* p = lds + k * (COLS * 2) +
+                           (((col >> 4) ^ pv_key_across<COLS>(k)) << 5) + (col & 15) * 2;
+        const pv_s16x4 t = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (pv_s16x4 __attribute__((address_space(3)))*)p);
+        uint32_t u[2];
+        __builtin_memcpy(u, &t, 8);
+        v[2 * s] = u[0];
+        v[2 * s + 1] = u[1];
+    }
+    return v;
+}
+
+// The epilogue gets acc[j][i][e]: row mw + 16 i + r, column nw + 32 (j >> 1) + 8 h + 4
+// (j & 1) + e (r = lane & 15, h = lane >> 4). A workgroup takes several tiles in turn: the
+// first slices of the next one are under way during the epilogue.
+template <bool I8, bool TA, bool TB, class T, class Epi>
 __global__ __launch_bounds__(T::kThreads, T::kThreads* T::kWorkgroups / 256 / 256) void
 pv_product_kernel(PvProduct p, Epi epi) {
+    static_assert(!I8 || (!TA && !TB), "the transposing loads are of 16 bits");
     // stages, arrays of their own: the loads into one are then seen not to touch what is
     // read of another, and are not waited for
-    constexpr int KB = T::KB, SA = T::TM * KB, SB = T::TN * KB, ST = T::ST;
-    constexpr int PR = KB / 16;  // pieces of a row
+    constexpr int SA = T::TM * kSlice, SB = T::TN * kSlice, ST = T::ST;
     __shared__ __align__(16) uint8_t la0[SA], la1[SA], la2[ST > 2 ? SA : 16], la3[ST > 3 ? SA : 16];
     __shared__ __align__(16) uint8_t lb0[SB], lb1[SB], lb2[ST > 2 ? SB : 16], lb3[ST > 3 ? SB : 16];
-    constexpr int kPer = kSlice / KB;  // stages of a slice
     typedef typename PvAcc<I8>::type Acc;
-    constexpr int MI = T::MI, QA = T::TM * PR / T::kThreads, QB = T::TN * PR / T::kThreads;
+    constexpr int MI = T::MI;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r = lane & 15, h = lane >> 4;
     const int wm = wave % T::WM * (16 * MI), wn = wave / T::WM * 64;
     // each XCD (workgroups go round them) takes a run of the launch's tiles
@@ -148,53 +210,53 @@ pv_product_kernel(PvProduct p, Epi epi) {
     if (idx >= end) return;
 
     int split, m0, n0, t0, t1, pair, k;
-    const uint8_t* ga[QA];
-    const uint8_t* gb[QB];
+    PvSource<TA, false, T::TM, T::kThreads> from_a;
+    PvSource<TB, true, T::TN, T::kThreads> from_b;
+    constexpr int QA = decltype(from_a)::Q, QB = decltype(from_b)::Q, Q = QA + QB;
     auto enter = [&]() {
         pv_tile_of<T>(p, p.first + idx, split, m0, n0);
         t0 = split * p.per;
-        t1 = min(t0 + p.per, p.slices * p.pairs) * kPer;
+        t1 = min(t0 + p.per, p.slices * p.pairs);
         pair = t0 / max(p.slices, 1);
-        k = (t0 - pair * p.slices) * kPer;
-        t0 *= kPer;
-#pragma unroll
-        for (int q = 0; q < QA; q++) {
-            const int piece = (wave * QA + q) * 64 + lane, row = piece / PR, c = piece % PR;
-            ga[q] = p.a.p + (size_t)min(m0 + row, p.M - 1) * p.a.pitch + (c ^ pv_key_a<KB>(row)) * 16;
-        }
-#pragma unroll
-        for (int q = 0; q < QB; q++) {
-            const int piece = (wave * QB + q) * 64 + lane, row = piece / PR, c = piece % PR;
-            gb[q] = p.b.p + (size_t)min(n0 + row, p.N - 1) * p.b.pitch + (c ^ pv_key_b<KB>(row)) * 16;
-        }
+        k = t0 - pair * p.slices;
+        from_a.enter(p.a, m0, p.M, wave, lane);
+        from_b.enter(p.b, n0, p.N, wave, lane);
     };
-    // load q of the QA + QB of a slice; the last one moves on to the next slice
-    auto fetch_one = [&](int q, uint8_t* la, uint8_t* lb) {
-        if (q < QA) {
-            const size_t oa = ((p.pa >> (4 * pair)) & 15) * p.a.part_bytes + (size_t)k * KB;
-            __builtin_amdgcn_global_load_lds(
-                (const void __attribute__((address_space(1)))*)(ga[q < QA ? q : 0] + oa),
-                (void __attribute__((address_space(3)))*)(la + (wave * QA + q) * 1024), 16, 0, 0);
-        } else {
-            const size_t ob = ((p.pb >> (4 * pair)) & 15) * p.b.part_bytes + (size_t)k * KB;
-            __builtin_amdgcn_global_load_lds(
-                (const void __attribute__((address_space(1)))*)(gb[q < QA ? 0 : q - QA] + ob),
-                (void __attribute__((address_space(3)))*)(lb + (wave * QB + q - QA) * 1024), 16, 0,
-                0);
-        }
-        if (q == QA + QB - 1 && ++k == p.slices * kPer) {
+    // load q of a slice's Q; the last one moves on to the next slice
+    auto fetch_one = [&](auto q, uint8_t* la, uint8_t* lb) {
+        if constexpr (q < QA)
+            from_a.load(p.a, (p.pa >> (4 * pair)) & 15, k, q, wave, lane, la);
+        else
+            from_b.load(p.b, (p.pb >> (4 * pair)) & 15, k, q - QA, wave, lane, lb);
+        if (q == Q - 1 && ++k == p.slices) {
             k = 0;
             pair++;
         }
     };
     auto fetch = [&](uint8_t* la, uint8_t* lb) {
-#pragma unroll
-        for (int q = 0; q < QA + QB; q++) fetch_one(q, la, lb);
+        pv_each<Q>([&](auto q) { fetch_one(q, la, lb); });
     };
     auto first = [&]() {  // the first ST - 1 slices of a tile
         if (t0 < t1) fetch(la0, lb0);
         if (ST > 2 && t0 + 1 < t1) fetch(la1, lb1);
         if (ST > 3 && t0 + 2 < t1) fetch(la2, lb2);
+    };
+    auto load_a = [&](const uint8_t* la, int i, int half) {
+        if constexpr (TA) {
+            return pv_load_across<T::TM>(la, 32 * half, wm + 16 * i + 4 * (lane & 3), lane);
+        } else {
+            const int row = wm + 16 * i + r;
+            return *(const pv_u32x4*)(la + row * kSlice + ((h + 4 * half) ^ pv_key_a(row)) * 16);
+        }
+    };
+    auto load_b = [&](const uint8_t* lb, int j, int half) {
+        if constexpr (TB) {
+            return pv_load_across<T::TN>(
+                lb, 32 * half, wn + 32 * (j >> 1) + 8 * (lane & 3) + 4 * (j & 1), lane);
+        } else {
+            const int row = wn + 32 * (j >> 1) + 8 * (r >> 2) + 4 * (j & 1) + (r & 3);
+            return *(const pv_u32x4*)(lb + row * kSlice + ((h + 4 * half) ^ pv_key_b(row)) * 16);
+        }
     };
     enter();
     first();
@@ -204,23 +266,14 @@ pv_product_kernel(PvProduct p, Epi epi) {
         for (int j = 0; j < 4; j++)
 #pragma unroll
             for (int i = 0; i < MI; i++) acc[j][i] = Acc{0, 0, 0, 0};
-        auto load_a = [&](const uint8_t* la, int i, int half) {
-            const int row = wm + 16 * i + r;
-            return *(const pv_u32x4*)(la + row * KB + ((h + 4 * half) ^ pv_key_a<KB>(row)) * 16);
-        };
-        auto load_b = [&](const uint8_t* lb, int j, int half) {
-            const int row = wn + 16 * (r >> 2) + 4 * j + (r & 3);
-            return *(const pv_u32x4*)(lb + row * KB + ((h + 4 * half) ^ pv_key_b<KB>(row)) * 16);
-        };
         // The products of a slice in la, lb. The loads of a later one go between them: at
         // once, they would hold every wave up for the time that they take to be issued.
         auto multiply = [&](const uint8_t* la, const uint8_t* lb, uint8_t* na, uint8_t* nb,
                             bool fetching) {
-            constexpr int Q = QA + QB;
             pv_u32x4 fa[MI], fb[4];
             pv_each<4>([&](auto j) { fb[j] = load_b(lb, j, 0); });
             pv_each<MI>([&](auto i) { fa[i] = load_a(la, i, 0); });
-            pv_each<KB / 64>([&](auto half) {
+            pv_each<2>([&](auto half) {
                 pv_each<MI>([&](auto i) {
                     pv_each<4>([&](auto j) {
                         if constexpr (I8) {
@@ -235,13 +288,14 @@ pv_product_kernel(PvProduct p, Epi epi) {
                         }
                     });
                     if constexpr (half == 0) {
-                        if constexpr (KB == 128) {
-                            if constexpr (i == MI - 1)
-                                pv_each<4>([&](auto j) { fb[j] = load_b(lb, j, 1); });
-                            fa[i] = load_a(la, i, 1);
-                        }
+                        if constexpr (i == MI - 1)
+                            pv_each<4>([&](auto j) { fb[j] = load_b(lb, j, 1); });
+                        fa[i] = load_a(la, i, 1);
                         constexpr int q0 = i * Q / MI, q1 = (i + 1) * Q / MI;
-                        if (fetching) pv_each<q1 - q0>([&](auto q) { fetch_one(q + q0, na, nb); });
+                        if (fetching)
+                            pv_each<q1 - q0>([&](auto q) {
+                                fetch_one(std::integral_constant<int, q0 + q>(), na, nb);
+                            });
                     }
                     __builtin_amdgcn_sched_barrier(0);
                 });
@@ -250,7 +304,7 @@ pv_product_kernel(PvProduct p, Epi epi) {
         // one slice, in la, lb; na, nb, read before this barrier, take the one ST - 1 on
         auto slice = [&](int t, const uint8_t* la, const uint8_t* lb, uint8_t* na, uint8_t* nb) {
             if (t + ST - 2 < t1)  // this wave's part of it has landed
-                pv_wait_loads<(ST - 2) * (QA + QB)>();
+                pv_wait_loads<(ST - 2) * Q>();
             else
                 pv_wait_loads<0>();
             pv_lds_barrier();
@@ -274,8 +328,8 @@ pv_product_kernel(PvProduct p, Epi epi) {
         const int em = m0 + wm, en = n0 + wn, es = split;
         idx += step;
         const bool more = idx < end;
-        pv_lds_barrier();  // nothing reads the stages any more
         if (more) {
+            pv_lds_barrier();  // nothing reads the stages any more
             enter();
             first();
         }
@@ -283,96 +337,108 @@ pv_product_kernel(PvProduct p, Epi epi) {
             uint32_t* part = p.partial + (size_t)es * p.M * p.N;
 #pragma unroll
             for (int i = 0; i < MI; i++) {
-                const int m = em + 16 * i + r, n = en + 16 * h;
+                const int m = em + 16 * i + r;
                 if (m >= p.M) continue;
-                uint32_t* o = part + (size_t)m * p.N + n;
 #pragma unroll
                 for (int j = 0; j < 4; j++) {
+                    const int n = en + 32 * (j >> 1) + 8 * h + 4 * (j & 1);
+                    uint32_t* o = part + (size_t)m * p.N + n;
                     pv_u32x4 v;
                     __builtin_memcpy(&v, &acc[j][i], 16);
-                    if (n + 4 * j + 4 <= p.N)
-                        *(pv_u32x4_any*)(o + 4 * j) = v;
+                    if (n + 4 <= p.N)
+                        *(pv_u32x4_any*)o = v;
                     else
 #pragma unroll
                         for (int e = 0; e < 4; e++)
-                            if (n + 4 * j + e < p.N) o[4 * j + e] = v[e];
+                            if (n + e < p.N) o[e] = v[e];
                 }
             }
         } else {
-            epi.template tile<MI>(p, em, en, lane, acc, (ST == 2 ? la1 : ST == 3 ? la2 : la3) + wave * 4096);
+            epi.template tile<MI>(p, em, en, lane, acc);
         }
         if (!more) return;
     }
 }
+// The column of value q (of sixteen) of a lane whose first one is nb = nw + 8 h: acc[q >>
+// 2][i][q & 3].
+__device__ __forceinline__ int pv_col(int nb, int q) { return nb + 32 * (q >> 3) + (q & 7); }
 
-// W (4 or 16) consecutive values of a row from column n on, wherever the row begins.
-template <int W>
-__device__ __forceinline__ void pv_store_run(const PvRows& out, int m, int n, int N,
-                                             const float (&v)[W]) {
-    const size_t at = (size_t)m * out.ld + n;
-    const bool whole = n + W <= N;
-    if (out.bf16) {
-        uint16_t* o = (uint16_t*)out.p + at;
-        if (whole) {
-            uint32_t w[W / 2];
+// A lane's sixteen values of a row, two runs of eight, wherever the row begins.
+__device__ __forceinline__ void pv_store_runs(const PvRows& out, int m, int nb, int N,
+                                              const float (&v)[16]) {
 #pragma unroll
-            for (int i = 0; i < W / 2; i++) w[i] = pv_pack_bf16x2(v[2 * i], v[2 * i + 1]);
+    for (int a = 0; a < 2; a++) {
+        const int n = nb + 32 * a;
+        const size_t at = (size_t)m * out.ld + n;
+        const bool whole = n + 8 <= N;
+        if (out.bf16) {
+            uint16_t* o = (uint16_t*)out.p + at;
+            if (whole) {
+                pv_u32x4 w;
 #pragma unroll
-            for (int i = 0; i < W / 8; i++)
-                *(pv_u32x4_any*)(o + 8 * i) =
-                    pv_u32x4{w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]};
+                for (int i = 0; i < 4; i++)
+                    w[i] = pv_pack_bf16x2(v[8 * a + 2 * i], v[8 * a + 2 * i + 1]);
+                *(pv_u32x4_any*)o = w;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; i++)
+                    if (n + i < N) o[i] = pv_f32_to_bf16(v[8 * a + i]);
+            }
         } else {
+            float* o = (float*)out.p + at;
+            if (whole) {
 #pragma unroll
-            for (int i = 0; i < W; i++)
-                if (n + i < N) o[i] = pv_f32_to_bf16(v[i]);
-        }
-    } else {
-        float* o = (float*)out.p + at;
-        if (whole) {
+                for (int i = 0; i < 8; i += 4)
+                    *(pv_u32x4_any*)(o + i) = pv_u32x4{
+                        __float_as_uint(v[8 * a + i]), __float_as_uint(v[8 * a + i + 1]),
+                        __float_as_uint(v[8 * a + i + 2]), __float_as_uint(v[8 * a + i + 3])};
+            } else {
 #pragma unroll
-            for (int i = 0; i < W / 4; i++)
-                *(pv_u32x4_any*)(o + 4 * i) =
-                    pv_u32x4{__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]),
-                             __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3])};
-        } else {
-#pragma unroll
-            for (int i = 0; i < W; i++)
-                if (n + i < N) o[i] = v[i];
+                for (int i = 0; i < 8; i++)
+                    if (n + i < N) o[i] = v[8 * a + i];
+            }
         }
     }
 }
 
-// ---- splits ----------------------------------------------------------------
-// How many ways a product's slices are split, and into which tiles: unsplit where its
-// tiles fill the chip, else enough for a workgroup a CU at most, of `least` slices or
-// more.
-enum PvSize { kPvS, kPvN, kPvM, kPvG, kPvL };
+// ---- tiles and splits ------------------------------------------------------
 static inline size_t pv_tiles_of(int M, int N, int tm, int tn) {
     return (size_t)((M + tm - 1) / tm) * ((N + tn - 1) / tn);
 }
-static inline void pv_plan_splits(PvProduct& p, int least) {
+// The tiles that a product takes and how many ways its slices are split, by the time that
+// each choice is expected to take: rounds of workgroups, each its slices and an epilogue,
+// and the splits' sums written, read and joined.
+struct PvSizeCost {
+    int size, tm, tn, slots;
+    float slice, rest;  // us
+};
+static constexpr PvSizeCost kPvCosts[] = {
+    {kPvL, PvTileL::TM, PvTileL::TN, PvTileL::kWorkgroups, 1.75f, 5.f},
+    {kPvG, PvTileG::TM, PvTileG::TN, PvTileG::kWorkgroups, 1.0f, 4.f},
+    {kPvM, PvTileM::TM, PvTileM::TN, PvTileM::kWorkgroups, 0.6f, 3.f},
+    {kPvN, PvTileN::TM, PvTileN::TN, PvTileN::kWorkgroups, 0.4f, 2.5f},
+    {kPvS, PvTileS::TM, PvTileS::TN, PvTileS::kWorkgroups, 0.4f, 2.5f},
+};
+static inline void pv_plan(PvProduct& p, bool may_split, unsigned sizes = 31) {
     const int all = p.slices * p.pairs;
-    PvSize size = kPvS;
-    size_t tiles = pv_tiles_of(p.M, p.N, 64, 64);
-    if (p.N > 128 && pv_tiles_of(p.M, p.N, 256, 256) * (all / 32 + 1) >= 192) {
-        size = kPvL;
-        tiles = pv_tiles_of(p.M, p.N, 256, 256);
-    } else if (p.N > 64 && pv_tiles_of(p.M, p.N, 128, 128) * (all / 16 + 1) >= 128) {
-        size = kPvM;
-        tiles = pv_tiles_of(p.M, p.N, 128, 128);
-    } else if (p.N <= 64 && pv_tiles_of(p.M, p.N, 128, 64) * (all / 16 + 1) >= 128) {
-        size = kPvN;
-        tiles = pv_tiles_of(p.M, p.N, 128, 64);
+    float best = 0.f;
+    for (const PvSizeCost& c : kPvCosts) {
+        if (!(sizes >> c.size & 1)) continue;
+        const size_t tiles = pv_tiles_of(p.M, p.N, c.tm, c.tn);
+        for (int n = 1; n == 1 || (may_split && n <= 256 && all / n >= 4); n += n < 8 ? 1 : n / 4) {
+            const int per = n == 1 ? all : (all + n - 1) / n;
+            const int splits = per ? (all + per - 1) / per : 1;
+            const size_t rounds = (tiles * splits + c.slots - 1) / c.slots;
+            float us = (float)rounds * ((float)per * c.slice + c.rest);
+            if (splits > 1) us += 3.f + (float)splits * (float)p.M * (float)p.N * (8.f / 4e6f);
+            if (best == 0.f || us < best) {
+                best = us;
+                p.size = c.size;
+                p.per = per;
+                p.splits = splits;
+            }
+        }
     }
-    p.per = all;
-    if (tiles > 0 && tiles <= 128 && all >= 2 * least) {
-        const int most = all / least;
-        int n = (int)(256 / tiles);
-        n = n < 1 ? 1 : (n > most ? most : n);
-        p.per = (all + n - 1) / n;
-    }
-    p.splits = p.per ? (all + p.per - 1) / p.per : 1;
-    p.size = size;
 }
 static inline size_t pv_partial_bytes(const PvProduct& p) {
     return p.splits > 1 ? (size_t)p.splits * p.M * p.N * 4 : 0;
@@ -414,18 +480,14 @@ static inline unsigned pv_blocks(size_t items, int per) {
 }
 
 constexpr size_t kPvTilesALaunch = (size_t)1 << 30;
-template <class T>
-static inline size_t pv_tiles(const PvProduct& p) {
-    return (size_t)((p.M + T::TM - 1) / T::TM) * ((p.N + T::TN - 1) / T::TN) * p.splits;
-}
-template <bool I8, class T, class Epi>
+template <bool I8, bool TA, bool TB, class T, class Epi>
 static void pv_run_tiles(PvProduct p, const Epi& epi, hipStream_t s) {
-    const size_t tiles = pv_tiles<T>(p);
+    const size_t tiles = pv_tiles_of(p.M, p.N, T::TM, T::TN) * p.splits;
     for (size_t t = 0; t < tiles; t += kPvTilesALaunch) {
         p.first = (uint32_t)t;
         p.count = (uint32_t)(tiles - t < kPvTilesALaunch ? tiles - t : kPvTilesALaunch);
         const unsigned most = (p.count + 7) / 8 * 8;
-        hipLaunchKernelGGL((pv_product_kernel<I8, T, Epi>),
+        hipLaunchKernelGGL((pv_product_kernel<I8, TA, TB, T, Epi>),
                            dim3(most < T::kWorkgroups ? most : T::kWorkgroups), dim3(T::kThreads),
                            0, s, p, epi);
     }
@@ -433,23 +495,20 @@ static void pv_run_tiles(PvProduct p, const Epi& epi, hipStream_t s) {
         hipLaunchKernelGGL((pv_join_kernel<I8, Epi>), dim3(pv_blocks((size_t)p.M * p.N, 256)),
                            dim3(256), 0, s, p, epi);
 }
-
-// The tiles of a product that is never split: large ones where they fill the chip, and
-// smaller the fewer there are of them.
-static inline PvSize pv_size_of(int M, int N) {
-    if (N > 128 && pv_tiles_of(M, N, 256, 256) >= 192) return kPvL;
-    if (N > 64 && pv_tiles_of(M, N, 128, 128) >= 128) return kPvM;
-    return N <= 64 && pv_tiles_of(M, N, 128, 64) >= 128 ? kPvN : kPvS;
-}
-template <bool I8, class Epi>
+// SIZES: the tiles (1 << PvSize) that the plan may have chosen
+constexpr unsigned kPvAnySize = 31;
+template <bool I8, bool TA, bool TB, unsigned SIZES = kPvAnySize, class Epi>
 static void pv_run_product(const PvProduct& p, const Epi& epi, hipStream_t s) {
-    switch (p.size) {
-        case kPvL: pv_run_tiles<I8, PvTileL>(p, epi, s); break;
-        case kPvG: pv_run_tiles<I8, PvTileG>(p, epi, s); break;
-        case kPvM: pv_run_tiles<I8, PvTileM>(p, epi, s); break;
-        case kPvN: pv_run_tiles<I8, PvTileN>(p, epi, s); break;
-        default: pv_run_tiles<I8, PvTileS>(p, epi, s);
-    }
+    if constexpr (SIZES >> kPvL & 1)
+        if (p.size == kPvL) pv_run_tiles<I8, TA, TB, PvTileL>(p, epi, s);
+    if constexpr (SIZES >> kPvG & 1)
+        if (p.size == kPvG) pv_run_tiles<I8, TA, TB, PvTileG>(p, epi, s);
+    if constexpr (SIZES >> kPvM & 1)
+        if (p.size == kPvM) pv_run_tiles<I8, TA, TB, PvTileM>(p, epi, s);
+    if constexpr (SIZES >> kPvN & 1)
+        if (p.size == kPvN) pv_run_tiles<I8, TA, TB, PvTileN>(p, epi, s);
+    if constexpr (SIZES >> kPvS & 1)
+        if (p.size == kPvS) pv_run_tiles<I8, TA, TB, PvTileS>(p, epi, s);
 }
 
 // ---- operands (product.hip) ------------------------------------------------
@@ -462,20 +521,32 @@ struct PvPack {
     const float* row_scale;  // or NULL
     const float* col_scale;  // or NULL
     int parts;
-    uint8_t* dst;
-    size_t pitch;            // bytes; padded with zeros up to it
-    size_t part_bytes;
+    uint8_t* dst;            // [part][rows][pitch bytes], zeros from R and C on
+    size_t pitch, part_bytes;
+    int rows;
+    float* sums;             // set: no rows of parts, but the sums of the source's columns
+                             // over runs of kPvSumRows rows, [runs][C]
 };
-// The source as rows of bf16 parts, and its transpose as such (dst's rows: columns).
-void pv_launch_pack(const PvPack& k, hipStream_t s);
-void pv_launch_pack_transposed(const PvPack& k, hipStream_t s);
+constexpr int kPvSumRows = 256;
+static inline int pv_sum_runs(int M) { return (M + kPvSumRows - 1) / kPvSumRows; }
+// Up to five at once.
+struct PvPacks {
+    PvPack job[5];
+    unsigned begin[6];  // the first workgroup of each
+    int n;
+    void add(const PvPack& k) { job[n++] = k; }
+};
+void pv_launch_packs(PvPacks& k, hipStream_t s);
+// Sums [runs][N] joined in a fixed order.
+void pv_launch_sum_runs(const float* runs, int n, int N, float* out, hipStream_t s);
 
-// out (+)= a b^T in bf16 parts: out = sum + add (dense [M][N] fp32, or NULL)
+// out (+)= the product of bf16 parts: out = sum + add (dense [M][N] fp32, or NULL); a along
+// k or across it, b across it
 struct PvPlain {
     PvRows out;
     const float* add;
 };
-void pv_launch_plain(const PvProduct& p, const PvPlain& e, hipStream_t s);
+void pv_launch_plain(const PvProduct& p, bool a_across, const PvPlain& e, hipStream_t s);
 
 // Pieces of a workspace, one behind another.
 struct PvCarve {
@@ -487,23 +558,21 @@ struct PvCarve {
         return p;
     }
 };
-static inline PvPanel pv_take_panel(PvCarve& c, size_t rows, size_t cols, int parts) {
+static inline PvPanel pv_take_panel(PvCarve& c, int rows, int cols, int parts) {
     PvPanel p;
     p.pitch = pv_up(cols, 64) * 2;
-    p.part_bytes = pv_align256(rows * p.pitch);
+    p.part_bytes = pv_align256((size_t)rows * p.pitch);
     p.parts = parts;
+    p.rows = rows;
     p.p = (const uint8_t*)c.take(p.part_bytes * parts);
     return p;
 }
 static inline PvPack pv_pack_of(const void* src, PvKind kind, size_t ld, int R, int C,
                                 const PvPanel& to) {
     return PvPack{src, kind, ld, R, C, nullptr, nullptr, to.parts, (uint8_t*)to.p, to.pitch,
-                  to.part_bytes};
+                  to.part_bytes, to.rows, nullptr};
 }
-
-// Sums [parts][N] joined in a fixed order, and column sums of rows of channels (a linear
-// layer's bias gradient).
-void pv_launch_sum_parts(const float* partial, int parts, int N, float* out, hipStream_t s);
-size_t pv_column_sum_bytes(int M, int N);
-void pv_launch_column_sum(const PvRows& x, int M, int N, float* partial, float* out,
-                          hipStream_t s);
+static inline PvPack pv_sums_of(const PvRows& x, int R, int C, float* sums) {
+    return PvPack{x.p, x.bf16 ? kPvBf16 : kPvF32, (size_t)x.ld, R, C, nullptr, nullptr, 0, nullptr,
+                  0, 0, 0, sums};
+}
