@@ -248,7 +248,8 @@ struct Plan {
 };
 
 bool direct(const PvRows& r, int K) {
-    return r.bf16 && K % 64 == 0 && r.ld % 8 == 0 && pv_aligned16(r.p);
+    return r.bf16 && K % 64 == 0 && r.ld % 8 == 0 && pv_aligned16(r.p) &&
+           (size_t)r.ld * 2 <= kPvMostPitch;
 }
 
 template <class T>

@@ -130,39 +130,61 @@ __device__ __forceinline__ void pv_wait_loads() {
     __builtin_amdgcn_s_waitcnt((VM & 15) | (7 << 4) | ((VM >> 4) << 14));
 }
 
+// Workgroup barrier between the stages' uses: what it orders has been waited for (by
+// pv_wait_loads), so that it waits for nothing itself. (A fence would wait for every load
+// into LDS under way, whichever stage it fills.)
+__device__ __forceinline__ void pv_stage_barrier() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("" ::: "memory");
+}
+
 // Where the loads of an operand's slices come from: SIZE rows (columns, across k) from
 // `at` on of the `limit` that it has, Q loads of 16 bytes a lane.
+// Every address is one of the workgroup's and 32 bits of a lane's (kPvMostPitch), which
+// costs no vector instruction a load.
+constexpr size_t kPvMostPitch = ((size_t)1 << 32) / 256 - 256;
 template <bool ACROSS, bool B, int SIZE, int THREADS>
 struct PvSource {
     static constexpr int Q = SIZE * 8 / THREADS;
     static constexpr int kPieces = ACROSS ? SIZE / 8 : 8;  // of a row in LDS
-    const uint8_t* g[Q];
+    const uint8_t* base;
+    uint32_t off[Q];
     __device__ __forceinline__ static int row_of(int q, int wave, int lane) {
         return ((wave * Q + q) * 64 + lane) / kPieces;
     }
     __device__ __forceinline__ void enter(const PvPanel& p, int at, int limit, int wave,
                                           int lane) {
+        base = p.p + (ACROSS ? (size_t)at * 2 : (size_t)at * p.pitch);
 #pragma unroll
         for (int q = 0; q < Q; q++) {
             const int row = row_of(q, wave, lane), c = lane % kPieces;
             if constexpr (ACROSS) {
                 const int col = ((((c >> 1) ^ pv_key_across<SIZE>(row)) << 1) + (c & 1)) * 8;
-                g[q] = p.p + (size_t)min(at + col, ((limit + 7) & ~7) - 8) * 2;
+                off[q] = (uint32_t)row * (uint32_t)p.pitch +
+                         (uint32_t)min(col, ((limit + 7) & ~7) - 8 - at) * 2;
             } else {
                 const int key = B ? pv_key_b(row) : pv_key_a(row);
-                g[q] = p.p + (size_t)min(at + row, limit - 1) * p.pitch + (c ^ key) * 16;
+                off[q] = (uint32_t)min(row, limit - 1 - at) * (uint32_t)p.pitch + (c ^ key) * 16;
             }
         }
     }
-    __device__ __forceinline__ void load(const PvPanel& p, int part, int k, int q, int wave,
-                                         int lane, uint8_t* lds) const {
-        const uint8_t* from = g[q] + part * p.part_bytes;
-        if constexpr (ACROSS)
-            from += (size_t)min(k * kDeep + row_of(q, wave, lane), p.rows - 1) * p.pitch;
-        else
-            from += (size_t)k * kSlice;
+    // where a slice lies
+    __device__ __forceinline__ const uint8_t* slice(const PvPanel& p, int part, int k) const {
+        return base + part * p.part_bytes +
+               (size_t)k * (ACROSS ? kDeep * p.pitch : (size_t)kSlice);
+    }
+    __device__ __forceinline__ void load(const PvPanel& p, const uint8_t* from, int k, int q,
+                                         int wave, int lane, uint8_t* lds) const {
+        uint32_t o = off[q];
+        if constexpr (ACROSS) {  // rows past the last are read as that one
+            const int past = k * kDeep + row_of(q, wave, lane) - (p.rows - 1);
+            if ((k + 1) * kDeep > p.rows) o -= (uint32_t)max(past, 0) * (uint32_t)p.pitch;
+        }
         __builtin_amdgcn_global_load_lds(
-            (const void __attribute__((address_space(1)))*)from,
+            (const void __attribute__((address_space(1)))*)(from + o),
             (void __attribute__((address_space(3)))*)(lds + (wave * Q + q) * 1024), 16, 0, 0);
     }
 };
@@ -201,7 +223,8 @@ pv_product_kernel(PvProduct p, Epi epi) {
     __shared__ __align__(16) uint8_t lb0[SB], lb1[SB], lb2[ST > 2 ? SB : 16], lb3[ST > 3 ? SB : 16];
     typedef typename PvAcc<I8>::type Acc;
     constexpr int MI = T::MI;
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r = lane & 15, h = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, r = lane & 15, h = lane >> 4;
     const int wm = wave % T::WM * (16 * MI), wn = wave / T::WM * 64;
     // each XCD (workgroups go round them) takes a run of the launch's tiles
     const uint32_t run = (p.count + 7) / 8, step = gridDim.x >> 3;
@@ -222,24 +245,36 @@ pv_product_kernel(PvProduct p, Epi epi) {
         from_a.enter(p.a, m0, p.M, wave, lane);
         from_b.enter(p.b, n0, p.N, wave, lane);
     };
-    // load q of a slice's Q; the last one moves on to the next slice
+    // The loads of a slice, one at a time: where it lies, load q of Q, on to the next one.
+    const uint8_t *slice_a, *slice_b;
+    auto fetch_begin = [&]() {
+        slice_a = from_a.slice(p.a, (p.pa >> (4 * pair)) & 15, k);
+        slice_b = from_b.slice(p.b, (p.pb >> (4 * pair)) & 15, k);
+    };
     auto fetch_one = [&](auto q, uint8_t* la, uint8_t* lb) {
         if constexpr (q < QA)
-            from_a.load(p.a, (p.pa >> (4 * pair)) & 15, k, q, wave, lane, la);
+            from_a.load(p.a, slice_a, k, q, wave, lane, la);
         else
-            from_b.load(p.b, (p.pb >> (4 * pair)) & 15, k, q - QA, wave, lane, lb);
-        if (q == Q - 1 && ++k == p.slices) {
+            from_b.load(p.b, slice_b, k, q - QA, wave, lane, lb);
+    };
+    auto fetch_end = [&]() {
+        if (++k == p.slices) {
             k = 0;
-            pair++;
+            pair = pair + 1 < p.pairs ? pair + 1 : 0;
         }
     };
     auto fetch = [&](uint8_t* la, uint8_t* lb) {
+        fetch_begin();
         pv_each<Q>([&](auto q) { fetch_one(q, la, lb); });
+        fetch_end();
     };
-    auto first = [&]() {  // the first ST - 1 slices of a tile
-        if (t0 < t1) fetch(la0, lb0);
-        if (ST > 2 && t0 + 1 < t1) fetch(la1, lb1);
-        if (ST > 3 && t0 + 2 < t1) fetch(la2, lb2);
+    // The first ST - 1 slices of a tile. (Some of other slices, where it has fewer: loads
+    // that may not have been issued would be waited for with all others.)
+    auto first = [&]() {
+        if (t0 >= t1) return;
+        fetch(la0, lb0);
+        if constexpr (ST > 2) fetch(la1, lb1);
+        if constexpr (ST > 3) fetch(la2, lb2);
     };
     auto load_a = [&](const uint8_t* la, int i, int half) {
         if constexpr (TA) {
@@ -266,10 +301,8 @@ pv_product_kernel(PvProduct p, Epi epi) {
         for (int j = 0; j < 4; j++)
 #pragma unroll
             for (int i = 0; i < MI; i++) acc[j][i] = Acc{0, 0, 0, 0};
-        // The products of a slice in la, lb. The loads of a later one go between them: at
-        // once, they would hold every wave up for the time that they take to be issued.
-        auto multiply = [&](const uint8_t* la, const uint8_t* lb, uint8_t* na, uint8_t* nb,
-                            bool fetching) {
+        // The products of a slice in la, lb; `between` goes between them.
+        auto multiply = [&](const uint8_t* la, const uint8_t* lb, auto between) {
             pv_u32x4 fa[MI], fb[4];
             pv_each<4>([&](auto j) { fb[j] = load_b(lb, j, 0); });
             pv_each<MI>([&](auto i) { fa[i] = load_a(la, i, 0); });
@@ -291,45 +324,87 @@ pv_product_kernel(PvProduct p, Epi epi) {
                         if constexpr (i == MI - 1)
                             pv_each<4>([&](auto j) { fb[j] = load_b(lb, j, 1); });
                         fa[i] = load_a(la, i, 1);
-                        constexpr int q0 = i * Q / MI, q1 = (i + 1) * Q / MI;
-                        if (fetching)
-                            pv_each<q1 - q0>([&](auto q) {
-                                fetch_one(std::integral_constant<int, q0 + q>(), na, nb);
-                            });
+                        between(i);
                     }
                     __builtin_amdgcn_sched_barrier(0);
                 });
             });
         };
-        // one slice, in la, lb; na, nb, read before this barrier, take the one ST - 1 on
-        auto slice = [&](int t, const uint8_t* la, const uint8_t* lb, uint8_t* na, uint8_t* nb) {
-            if (t + ST - 2 < t1)  // this wave's part of it has landed
-                pv_wait_loads<(ST - 2) * Q>();
-            else
-                pv_wait_loads<0>();
-            pv_lds_barrier();
-            multiply(la, lb, na, nb, t + ST - 1 < t1);
+        // A slice in la, lb, while na, nb, read before the barrier, take the one ST - 1 on.
+        // Its loads go between the products: at once, they would hold every wave up for the
+        // time that they take to be issued.
+        auto steady = [&](const uint8_t* la, const uint8_t* lb, uint8_t* na, uint8_t* nb) {
+            pv_wait_loads<(ST - 2) * Q>();  // this wave's part of the slice has landed
+            pv_stage_barrier();
+            fetch_begin();
+            multiply(la, lb, [&](auto i) {
+                constexpr int q0 = i * Q / MI, q1 = (i + 1) * Q / MI;
+                pv_each<q1 - q0>([&](auto q) {
+                    fetch_one(std::integral_constant<int, q0 + q>(), na, nb);
+                });
+            });
+            fetch_end();
         };
-        for (int t = t0; t < t1; t += ST) {
-            if constexpr (ST == 2) {
-                slice(t, la0, lb0, la1, lb1);
-                if (t + 1 < t1) slice(t + 1, la1, lb1, la0, lb0);
-            } else if constexpr (ST == 3) {
-                slice(t, la0, lb0, la2, lb2);
-                if (t + 1 < t1) slice(t + 1, la1, lb1, la0, lb0);
-                if (t + 2 < t1) slice(t + 2, la2, lb2, la1, lb1);
-            } else {
-                slice(t, la0, lb0, la3, lb3);
-                if (t + 1 < t1) slice(t + 1, la1, lb1, la0, lb0);
-                if (t + 2 < t1) slice(t + 2, la2, lb2, la1, lb1);
-                if (t + 3 < t1) slice(t + 3, la3, lb3, la2, lb2);
+        // one of the last slices of a tile, which may have no later one to load
+        auto last = [&](int t, const uint8_t* la, const uint8_t* lb, uint8_t* na, uint8_t* nb) {
+            if (t >= t1) return;
+            pv_wait_loads<0>();
+            pv_stage_barrier();
+            if (t + ST - 1 < t1) fetch(na, nb);
+            multiply(la, lb, [](auto) {});
+        };
+        // either, where the sums leave no registers for two forms of the loop
+        auto any = [&](int t, const uint8_t* la, const uint8_t* lb, uint8_t* na, uint8_t* nb) {
+            if (t >= t1) return;
+            pv_wait_loads<0>();
+            pv_stage_barrier();
+            const bool more = t + 1 < t1;
+            if (more) fetch_begin();
+            multiply(la, lb, [&](auto i) {
+                constexpr int q0 = i * Q / MI, q1 = (i + 1) * Q / MI;
+                if (more)
+                    pv_each<q1 - q0>([&](auto q) {
+                        fetch_one(std::integral_constant<int, q0 + q>(), na, nb);
+                    });
+            });
+            if (more) fetch_end();
+        };
+        int t = t0;
+        if constexpr (ST == 2) {
+            for (; t < t1; t += 2) {
+                any(t, la0, lb0, la1, lb1);
+                any(t + 1, la1, lb1, la0, lb0);
+            }
+        } else if constexpr (ST == 3) {
+            for (; t + 4 < t1; t += 3) {
+                steady(la0, lb0, la2, lb2);
+                steady(la1, lb1, la0, lb0);
+                steady(la2, lb2, la1, lb1);
+            }
+            last(t, la0, lb0, la2, lb2);
+            last(t + 1, la1, lb1, la0, lb0);
+            last(t + 2, la2, lb2, la1, lb1);
+            last(t + 3, la0, lb0, la2, lb2);
+        } else {
+            for (; t + 6 < t1; t += 4) {
+                steady(la0, lb0, la3, lb3);
+                steady(la1, lb1, la0, lb0);
+                steady(la2, lb2, la1, lb1);
+                steady(la3, lb3, la2, lb2);
+            }
+            for (; t < t1; t += 4) {
+                last(t, la0, lb0, la3, lb3);
+                last(t + 1, la1, lb1, la0, lb0);
+                last(t + 2, la2, lb2, la1, lb1);
+                last(t + 3, la3, lb3, la2, lb2);
             }
         }
         const int em = m0 + wm, en = n0 + wn, es = split;
         idx += step;
         const bool more = idx < end;
         if (more) {
-            pv_lds_barrier();  // nothing reads the stages any more
+            pv_wait_loads<63>();
+            pv_stage_barrier();  // nothing reads the stages any more
             enter();
             first();
         }
