@@ -35,53 +35,90 @@ __device__ __forceinline__ uint32_t quantise(float v, float s, float inv, float 
     return q & 255u;
 }
 
-// N consecutive values of a row as bits of floats, zeros past its end.
-template <bool XB>
-__device__ __forceinline__ void load8(const PvRows& x, size_t row, int c0, int K, float (&v)[8]) {
-    if (c0 + 8 <= K) {
-        if constexpr (XB) {
-            const pv_u32x4 w = *(const pv_u32x4_any*)((const uint16_t*)x.p + row * x.ld + c0);
-#pragma unroll
-            for (int i = 0; i < 8; i++)
-                v[i] = __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
-        } else {
-            const float* p = (const float*)x.p + row * x.ld + c0;
-            const pv_u32x4 w = *(const pv_u32x4_any*)p, y = *(const pv_u32x4_any*)(p + 4);
-#pragma unroll
-            for (int i = 0; i < 8; i++) v[i] = __uint_as_float(i < 4 ? w[i] : y[i - 4]);
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; i++)
-            v[i] = c0 + i < K ? pv_load_one(x.p, XB, row * x.ld + c0 + i) : 0.f;
-    }
-}
-__device__ __forceinline__ uint32_t top8(const float (&v)[8]) {
-    uint32_t m = 0;
-#pragma unroll
-    for (int i = 0; i < 8; i++) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
-    return m;
-}
-__device__ __forceinline__ uint2 bytes8(const float (&v)[8], float s) {
-    uint2 o = {0, 0};
-    if (!(s == s)) return o;
-    const float inv = 1.f / s, half = 0.5f * s;
-#pragma unroll
-    for (int i = 0; i < 4; i++) {
-        o.x |= quantise(v[i], s, inv, half) << (8 * i);
-        o.y |= quantise(v[4 + i], s, inv, half) << (8 * i);
-    }
-    return o;
-}
-
 struct MaxBits {
     __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t b) const {
         return max(a, b);
     }
 };
 
-// A row in the registers of a team of TEAM lanes (a wave, or the workgroup): V vectors
-// of eight a lane. A longer row is read twice.
+// Eight consecutive values as they lie in memory.
+template <bool XB>
+struct Raw {
+    pv_u32x4 w[XB ? 1 : 2];
+    __device__ __forceinline__ float get(int i) const {
+        if constexpr (XB)
+            return __uint_as_float(i & 1 ? w[0][i / 2] & 0xffff0000u : w[0][i / 2] << 16);
+        else
+            return __uint_as_float(w[i / 4][i % 4]);
+    }
+    __device__ __forceinline__ void load(const PvRows& x, size_t row, int c0, int K) {
+        const char* p = (const char*)x.p + (row * x.ld + c0) * (XB ? 2 : 4);
+        if (c0 + 8 <= K) {
+            w[0] = *(const pv_u32x4_any*)p;
+            if constexpr (!XB) w[1] = *(const pv_u32x4_any*)(p + 16);
+            return;
+        }
+        uint32_t e[8];
+#pragma unroll
+        for (int i = 0; i < 8; i++)
+            e[i] = c0 + i < K ? (XB ? (uint32_t)((const uint16_t*)p)[i] : ((const uint32_t*)p)[i])
+                              : 0u;
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            if constexpr (XB) {
+                w[0][i] = e[2 * i] | (e[2 * i + 1] << 16);
+            } else {
+                w[0][i] = e[i];
+                w[1][i] = e[4 + i];
+            }
+        }
+    }
+    // the largest magnitude's bits, as a float's
+    __device__ __forceinline__ uint32_t top() const {
+        if constexpr (XB) {
+            typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+            u16x2 m = {0, 0};
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                const uint32_t u = w[0][i] & 0x7fff7fffu;
+                u16x2 v;
+                __builtin_memcpy(&v, &u, 4);
+                m = __builtin_elementwise_max(m, v);
+            }
+            return (uint32_t)(m[0] > m[1] ? m[0] : m[1]) << 16;
+        } else {
+            uint32_t m = 0;
+#pragma unroll
+            for (int i = 0; i < 8; i++) m = max(m, w[i / 4][i % 4] & 0x7fffffffu);
+            return m;
+        }
+    }
+    __device__ __forceinline__ uint2 bytes(float s, float inv, float half) const {
+        float t[8], far = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            t[i] = __builtin_fmaf(get(i), inv, 0x1.8p23f);
+            far = fmaxf(far, __builtin_fabsf(__builtin_fmaf(-(t[i] - 0x1.8p23f), s, get(i))));
+        }
+        uint32_t q[8];
+#pragma unroll
+        for (int i = 0; i < 8; i++) q[i] = __float_as_uint(t[i]);
+        if (far >= half) {  // a border, or a quotient that rounded across one
+#pragma unroll
+            for (int i = 0; i < 8; i++) q[i] = quantise(get(i), s, inv, half);
+        }
+        // the low bytes of the eight
+        const uint32_t a = __builtin_amdgcn_perm(q[1], q[0], 0x0c0c0400u),
+                       b = __builtin_amdgcn_perm(q[3], q[2], 0x0c0c0400u),
+                       c = __builtin_amdgcn_perm(q[5], q[4], 0x0c0c0400u),
+                       d = __builtin_amdgcn_perm(q[7], q[6], 0x0c0c0400u);
+        return uint2{a | (b << 16), c | (d << 16)};
+    }
+};
+
+// A row in the registers of a wave or of the workgroup (TEAM lanes, V vectors of eight a
+// lane); of a longer one the rest is read twice. Bound by memory, next by some ten
+// instructions a value.
 template <bool XB, int TEAM, int V>
 __global__ __launch_bounds__(kThreads) void pv_int8_quantise_kernel(PvRows x, int M, int K,
                                                                     int8_t* q, float* scale) {
@@ -92,17 +129,19 @@ __global__ __launch_bounds__(kThreads) void pv_int8_quantise_kernel(PvRows x, in
          row0 += (size_t)gridDim.x * kRows) {
         const size_t row = row0 + threadIdx.x / TEAM;
         const bool live = row < (size_t)M;
-        float v[V][8];
+        Raw<XB> v[V];
         uint32_t top = 0;
         if (live) {
 #pragma unroll
-            for (int u = 0; u < V; u++) load8<XB>(x, row, (u * TEAM + lane) * 8, K, v[u]);
+            for (int u = 0; u < V; u++)
+                if (u * TEAM * 8 < K) v[u].load(x, row, (u * TEAM + lane) * 8, K);
 #pragma unroll
-            for (int u = 0; u < V; u++) top = max(top, top8(v[u]));
+            for (int u = 0; u < V; u++)
+                if (u * TEAM * 8 < K) top = max(top, v[u].top());
             for (int c0 = (V * TEAM + lane) * 8; c0 < K; c0 += TEAM * 8) {
-                float w[8];
-                load8<XB>(x, row, c0, K, w);
-                top = max(top, top8(w));
+                Raw<XB> w;
+                w.load(x, row, c0, K);
+                top = max(top, w.top());
             }
         }
         top = wave_reduce(top, MaxBits());
@@ -117,15 +156,23 @@ __global__ __launch_bounds__(kThreads) void pv_int8_quantise_kernel(PvRows x, in
         const float s = row_scale_of(top);
         if (lane == 0) scale[row] = s;
         int8_t* o = q + row * K128;
+        const float inv = 1.f / s, half = 0.5f * s;
+        if (!(s == s)) {  // a row that is not finite
+            for (int c0 = lane * 8; c0 < K128; c0 += TEAM * 8) *(uint2*)(o + c0) = uint2{0, 0};
+            continue;
+        }
 #pragma unroll
         for (int u = 0; u < V; u++) {
             const int c0 = (u * TEAM + lane) * 8;
-            if (c0 < K128) *(uint2*)(o + c0) = bytes8(v[u], s);
+            if (c0 < K)
+                *(uint2*)(o + c0) = v[u].bytes(s, inv, half);
+            else if (c0 < K128)
+                *(uint2*)(o + c0) = uint2{0, 0};
         }
         for (int c0 = (V * TEAM + lane) * 8; c0 < K128; c0 += TEAM * 8) {
-            float w[8];
-            load8<XB>(x, row, c0, K, w);
-            *(uint2*)(o + c0) = bytes8(w, s);
+            Raw<XB> w;
+            w.load(x, row, c0, K);
+            *(uint2*)(o + c0) = w.bytes(s, inv, half);
         }
     }
 }
@@ -195,44 +242,66 @@ struct LinearEpi {
 // Few rows: a workgroup takes 16 rows by 16 columns. Its eight waves take the rows'
 // largest values, then a share of the 64-value pieces each, which a wave quantises in
 // registers where they are its matrix operand: lane (r, h) holds row r's values 16 h ..
-// of a piece. Their sums meet in LDS; one launch, no workspace.
+// of a piece. Their sums meet in LDS; one launch, no workspace. Latency: a wave's first
+// pieces are under way while the rows' scales are found.
 constexpr int kFewThreads = 512;
 template <bool XB>
 __global__ __launch_bounds__(kFewThreads) void pv_int8_few_kernel(PvRows x, int M, int K, int N,
                                                                   const int8_t* w,
                                                                   LinearEpi epi) {
-    constexpr int kWaves = kFewThreads / 64;
-    __shared__ float scales[16];
+    constexpr int kWaves = kFewThreads / 64, kAhead = 4;
+    __shared__ uint32_t tops[16];
     __shared__ int part[kWaves][256];
     const int K128 = (K + kSlice - 1) / kSlice * kSlice, pieces = (K + 63) / 64;
     const int nt = (N + 15) / 16;
     const int m0 = (int)(blockIdx.x / nt) * 16, n0 = (int)(blockIdx.x % nt) * 16;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r = lane & 15, h = lane >> 4;
     const int rows = min(16, M - m0);
-    for (int i = wave; i < 16; i += kWaves) {
-        uint32_t top = 0;
-        if (i < rows)
-            for (int c0 = lane * 8; c0 < K; c0 += 512) {
-                float v[8];
-                load8<XB>(x, m0 + i, c0, K, v);
-                top = max(top, top8(v));
-            }
-        top = wave_reduce(top, MaxBits());
-        if (lane == 0) scales[i] = row_scale_of(top);
-    }
-    __syncthreads();
-    const float s = scales[r];
     const size_t row = min(m0 + r, M - 1);
     const int8_t* gw = w + (size_t)min(n0 + r, N - 1) * K128 + h * 16;
+    pv_i32x4 fw[kAhead];
+    Raw<XB> v[kAhead][2];
+    auto load = [&](int k) {
+#pragma unroll
+        for (int u = 0; u < kAhead; u++) {
+            const int at = min(k + u * kWaves, pieces - 1) * 64;
+            fw[u] = *(const pv_i32x4*)(gw + at);
+            v[u][0].load(x, row, at + h * 16, K);
+            v[u][1].load(x, row, at + h * 16 + 8, K);
+        }
+    };
+    load(wave);
+    if (threadIdx.x < 16) tops[threadIdx.x] = 0;
+    __syncthreads();
+    const int chunks = (K + 511) / 512;
+    for (int u = wave; u < rows * chunks; u += kWaves) {
+        const int i = u / chunks, c0 = (u - i * chunks) * 512 + lane * 8;
+        uint32_t top = 0;
+        if (c0 < K) {
+            Raw<XB> t;
+            t.load(x, m0 + i, c0, K);
+            top = t.top();
+        }
+        top = wave_reduce(top, MaxBits());
+        if (lane == 0) atomicMax(&tops[i], top);  // whole numbers: no order
+    }
+    __syncthreads();
+    const float s = row_scale_of(tops[r]);
+    const bool finite = s == s;
+    const float inv = 1.f / s, half = 0.5f * s;
     pv_i32x4 acc = {0, 0, 0, 0};
-    for (int k = wave; k < pieces; k += kWaves) {
-        const pv_i32x4 fw = *(const pv_i32x4*)(gw + k * 64);
-        float v[2][8];
-        load8<XB>(x, row, k * 64 + h * 16, K, v[0]);
-        load8<XB>(x, row, k * 64 + h * 16 + 8, K, v[1]);
-        const uint2 a = bytes8(v[0], s), b = bytes8(v[1], s);
-        const pv_i32x4 fx = {(int)a.x, (int)a.y, (int)b.x, (int)b.y};
-        acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw, fx, acc, 0, 0, 0);
+    for (int k = wave; k < pieces; k += kWaves * kAhead) {
+        if (k != wave) load(k);
+#pragma unroll
+        for (int u = 0; u < kAhead; u++) {
+            if (k + u * kWaves >= pieces) break;
+            pv_i32x4 fx = {0, 0, 0, 0};
+            if (finite) {
+                const uint2 a = v[u][0].bytes(s, inv, half), b = v[u][1].bytes(s, inv, half);
+                fx = pv_i32x4{(int)a.x, (int)a.y, (int)b.x, (int)b.y};
+            }
+            acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw[u], fx, acc, 0, 0, 0);
+        }
     }
 #pragma unroll
     for (int i = 0; i < 4; i++) part[wave][r * 16 + 4 * h + i] = acc[i];
@@ -242,7 +311,7 @@ __global__ __launch_bounds__(kFewThreads) void pv_int8_few_kernel(PvRows x, int 
         int sum = 0;
 #pragma unroll
         for (int u = 0; u < kWaves; u++) sum += part[u][threadIdx.x];
-        const float sm = scales[i], sn = epi.col_scale[n0 + c];
+        const float sm = row_scale_of(tops[i]), sn = epi.col_scale[n0 + c];
         const float v = LinearEpi::value(sum, sm, sn, epi.bias ? epi.bias[n0 + c] : 0.f,
                                          LinearEpi::tame(sm) && LinearEpi::tame(sn));
         pv_store_one(epi.out.p, epi.out.bf16, (size_t)(m0 + i) * epi.out.ld + n0 + c,
@@ -331,17 +400,21 @@ BwdWs carve_bwd(void* base, int M, int K, int N, bool dy_bf16, bool dx_bf16, boo
 
 template <bool XB>
 void run_quantise(const PvRows& x, int M, int K, int8_t* q, float* scale, hipStream_t s) {
-    const int rows = K <= 2048 ? 4 : 1;
-    const dim3 grid(pv_blocks(M, rows));
-    if (K <= 512)
-        hipLaunchKernelGGL((pv_int8_quantise_kernel<XB, 64, 1>), grid, dim3(kThreads), 0, s, x, M,
+    auto run = [&](auto kernel, int team) {
+        hipLaunchKernelGGL(kernel, dim3(pv_blocks(M, kThreads / team)), dim3(kThreads), 0, s, x, M,
                            K, q, scale);
-    else if (K <= 2048)
-        hipLaunchKernelGGL((pv_int8_quantise_kernel<XB, 64, 4>), grid, dim3(kThreads), 0, s, x, M,
-                           K, q, scale);
+    };
+    // A wave a row up to 5120 channels. Few rows of many: a workgroup each.
+    if (K > 5120 || (K > 1024 && M <= 256))
+        run(pv_int8_quantise_kernel<XB, 256, 4>, 256);
+    else if (K <= 512)
+        run(pv_int8_quantise_kernel<XB, 64, 1>, 64);
+    else if (K <= 1024)
+        run(pv_int8_quantise_kernel<XB, 64, 2>, 64);
+    else if (K <= 2560)
+        run(pv_int8_quantise_kernel<XB, 64, 5>, 64);
     else
-        hipLaunchKernelGGL((pv_int8_quantise_kernel<XB, 256, 4>), grid, dim3(kThreads), 0, s, x, M,
-                           K, q, scale);
+        run(pv_int8_quantise_kernel<XB, 64, 10>, 64);
 }
 
 }  // namespace
@@ -443,10 +516,12 @@ pvconv_status pv_launch_int8_linear_bwd(const PvRows& dy, const int8_t* rows,
         packs.add(a);
         packs.add(pv_pack_of(rows, kPvInt8, qk, M, K, w.q));
     }
-    if (dbias && M > 0) packs.add(pv_sums_of(dy, M, N, w.sums));
+    // (sums of one run are whole)
+    const int runs = pv_sum_runs(M);
+    if (dbias && M > 0) packs.add(pv_sums_of(dy, M, N, runs == 1 ? dbias : w.sums));
     pv_launch_packs(packs, s);
     if (want_dx) pv_launch_plain(w.dx, false, PvPlain{dx, nullptr}, s);
     if (dw) pv_launch_plain(w.dw, true, PvPlain{PvRows{dw, false, K}, nullptr}, s);
-    if (dbias) pv_launch_sum_runs(w.sums, pv_sum_runs(M), N, dbias, s);
+    if (dbias && runs != 1) pv_launch_sum_runs(w.sums, runs, N, dbias, s);
     return pv_launch_status();
 }

@@ -77,10 +77,12 @@ struct CeEpi {
     __device__ __forceinline__ void tile(const PvProduct& p, int mw, int nw, int lane,
                                          const pv_f32x4 (&acc)[4][MI]) const {
         const int r = lane & 15, h = lane >> 4, nb = nw + 8 * h;
+        // a class past the last has the logit -inf, and so takes no part
         float b[16], cs[16];
 #pragma unroll
         for (int q = 0; q < 16; q++) {
-            b[q] = c.bias ? c.bias[min(pv_col(nb, q), p.N - 1)] : 0.f;
+            const int n = pv_col(nb, q);
+            b[q] = n < p.N ? (c.bias ? c.bias[n] : 0.f) : -kInf;
             cs[q] = 0.f;
         }
         const bool grads = MODE == kGrad || (MODE == kWhole && (c.dz.p || c.sums));
@@ -89,17 +91,12 @@ struct CeEpi {
             const int m = mw + 16 * i + r, mc = min(m, p.M - 1);
             const int label = c.labels[mc];
             const bool known = label >= 0 && label < c.V;
-            // which of the lane's sixteen classes the label is, if any
+            // which of the lane's sixteen classes the label is, if any (few lanes have it)
             const unsigned to = (unsigned)label - (unsigned)(c.v0 + nb);
             const int at = to < 8u ? (int)to : to - 32u < 8u ? (int)to - 24 : -1;
             float z[16];
 #pragma unroll
-            for (int q = 0; q < 16; q++) {
-                z[q] = acc[q >> 2][i][q & 3] + b[q];
-                // columns past the last hold a copy of it: a logit that is not a number
-                // there would stay one
-                if (pv_col(nb, q) >= p.N) z[q] = -kInf;
-            }
+            for (int q = 0; q < 16; q++) z[q] = acc[q >> 2][i][q & 3] + b[q];
             float lse = 0.f;
             if constexpr (MODE != kGrad) {
                 float top = z[0];
@@ -110,9 +107,11 @@ struct CeEpi {
                 const float about = top == -kInf ? 0.f : top;
                 float sum = 0.f, zl = 0.f;
 #pragma unroll
-                for (int q = 0; q < 16; q++) {
-                    sum += __expf(z[q] - about);
-                    if (q == at) zl = z[q];
+                for (int q = 0; q < 16; q++) sum += __expf(z[q] - about);
+                if (at >= 0) {
+#pragma unroll
+                    for (int q = 0; q < 16; q++)
+                        if (q == at) zl = z[q];
                 }
                 sum = lanes_sum(sum);
                 if constexpr (MODE == kStats) {
@@ -136,11 +135,18 @@ struct CeEpi {
                 float g = m < p.M && known && lse != -kInf ? 1.f : 0.f;
                 if (g != 0.f && c.weight) g = c.weight[mc];
 #pragma unroll
-                for (int q = 0; q < 16; q++) {
-                    const float e = __expf(z[q] - lse) - (q == at ? 1.f : 0.f);
-                    z[q] = g == 0.f || pv_col(nb, q) >= p.N ? 0.f : g * e;
-                    cs[q] += z[q];
+                for (int q = 0; q < 16; q++) z[q] = g * __expf(z[q] - lse);
+                if (at >= 0) {
+#pragma unroll
+                    for (int q = 0; q < 16; q++)
+                        if (q == at) z[q] -= g;
                 }
+                if (g == 0.f) {  // whatever the logits are
+#pragma unroll
+                    for (int q = 0; q < 16; q++) z[q] = 0.f;
+                }
+#pragma unroll
+                for (int q = 0; q < 16; q++) cs[q] += z[q];
                 if (c.dz.p) {
                     store(0, m, nb, z);
                     if constexpr (PARTS)

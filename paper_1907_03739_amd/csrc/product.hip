@@ -12,26 +12,27 @@ __device__ __forceinline__ float load_kind(const void* src, PvKind kind, size_t 
 }
 
 // Eight consecutive columns of a row from c0 on, zeros from C on.
+template <PvKind KIND>
 __device__ __forceinline__ void load8(const PvPack& k, size_t row, int c0, float (&v)[8]) {
     const size_t from = row * k.ld + c0;
-    if (c0 + 8 <= k.C && k.kind == kPvBf16) {
+    if (c0 + 8 > k.C) {
+#pragma unroll
+        for (int i = 0; i < 8; i++) v[i] = c0 + i < k.C ? load_kind(k.src, KIND, from + i) : 0.f;
+    } else if constexpr (KIND == kPvBf16) {
         const pv_u32x4 w = *(const pv_u32x4_any*)((const uint16_t*)k.src + from);
 #pragma unroll
         for (int i = 0; i < 8; i++)
             v[i] = __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
-    } else if (c0 + 8 <= k.C && k.kind == kPvF32) {
+    } else if constexpr (KIND == kPvF32) {
         const pv_u32x4 w = *(const pv_u32x4_any*)((const float*)k.src + from);
         const pv_u32x4 y = *(const pv_u32x4_any*)((const float*)k.src + from + 4);
 #pragma unroll
         for (int i = 0; i < 8; i++) v[i] = __uint_as_float(i < 4 ? w[i] : y[i - 4]);
-    } else if (c0 + 8 <= k.C) {  // quantised rows begin on 128 bytes
+    } else {  // quantised rows begin on 128 bytes
         const uint2 w = *(const uint2*)((const int8_t*)k.src + from);
 #pragma unroll
         for (int i = 0; i < 8; i++)
             v[i] = (float)(int8_t)((i < 4 ? w.x : w.y) >> (8 * (i & 3)));
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; i++) v[i] = c0 + i < k.C ? load_kind(k.src, k.kind, from + i) : 0.f;
     }
 }
 
@@ -47,53 +48,65 @@ __device__ __forceinline__ uint32_t next_part(float& v) {
 }
 
 // Rows of parts: eight consecutive columns a thread, both ends of the traffic in 16-byte
-// pieces. Bound by memory: 32768 x 2304 bytes to bf16 move 226 MB.
+// pieces, a power of two of threads a row. Bound by memory.
+template <PvKind KIND>
 __device__ __forceinline__ void pack_rows(const PvPack& k, size_t block, size_t blocks) {
-    const size_t per = k.pitch / 16, total = per * k.rows;
-    for (size_t at = block * kThreads + threadIdx.x; at < total; at += blocks * kThreads) {
-        const size_t row = at / per;
-        const int c0 = (int)(at - row * per) * 8;
-        float v[8];
-        if (row < (size_t)k.R) {
-            load8(k, row, c0, v);
-            if (k.row_scale) {
-                const float rs = k.row_scale[row];
+    const int per = (int)(k.pitch / 16);
+    int shift = 0;  // of the threads of a row
+    while (shift < 8 && (1 << shift) < per) shift++;
+    const int lead = threadIdx.x >> shift, first = threadIdx.x & ((1 << shift) - 1);
+    const size_t rows = (size_t)kThreads >> shift;
+    for (size_t row = block * rows + lead; row < (size_t)k.rows; row += blocks * rows) {
+        const float rs = k.row_scale && row < (size_t)k.R ? k.row_scale[row] : 1.f;
+        for (int piece = first; piece < per; piece += 1 << shift) {
+            const int c0 = piece * 8;
+            float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            if (row < (size_t)k.R) {
+                load8<KIND>(k, row, c0, v);
+                if (k.row_scale) {
 #pragma unroll
-                for (int i = 0; i < 8; i++) v[i] = c0 + i < k.C ? v[i] * rs : 0.f;
+                    for (int i = 0; i < 8; i++) v[i] = c0 + i < k.C ? v[i] * rs : 0.f;
+                }
+                if (k.col_scale) {
+#pragma unroll
+                    for (int i = 0; i < 8; i++)
+                        v[i] = c0 + i < k.C ? v[i] * k.col_scale[c0 + i] : 0.f;
+                }
             }
-            if (k.col_scale) {
-#pragma unroll
-                for (int i = 0; i < 8; i++) v[i] *= k.col_scale[min(c0 + i, k.C - 1)];
+            uint8_t* to = k.dst + row * k.pitch + (size_t)c0 * 2;
+            if (KIND != kPvF32 && k.parts == 1 && !k.row_scale && !k.col_scale) {
+                *(pv_u32x4*)to = pv_u32x4{pv_pack_bf16x2(v[0], v[1]), pv_pack_bf16x2(v[2], v[3]),
+                                          pv_pack_bf16x2(v[4], v[5]), pv_pack_bf16x2(v[6], v[7])};
+                continue;
             }
-        } else {
+            for (int part = 0; part < k.parts; part++) {
+                uint32_t q[8];
 #pragma unroll
-            for (int i = 0; i < 8; i++) v[i] = 0.f;
-        }
-        for (int part = 0; part < k.parts; part++) {
-            uint32_t q[8];
-#pragma unroll
-            for (int i = 0; i < 8; i++) q[i] = c0 + i < k.C ? next_part(v[i]) : 0u;
-            *(pv_u32x4*)(k.dst + part * k.part_bytes + row * k.pitch + (size_t)c0 * 2) =
-                pv_u32x4{q[0] | (q[1] << 16), q[2] | (q[3] << 16), q[4] | (q[5] << 16),
-                         q[6] | (q[7] << 16)};
+                for (int i = 0; i < 8; i++) q[i] = next_part(v[i]);
+                *(pv_u32x4*)(to + part * k.part_bytes) =
+                    pv_u32x4{q[0] | (q[1] << 16), q[2] | (q[3] << 16), q[4] | (q[5] << 16),
+                             q[6] | (q[7] << 16)};
+            }
         }
     }
 }
 
 // Sums of 64 columns over runs of rows, in 64 bits: eight columns a thread, every 32nd row.
+template <PvKind KIND>
 __device__ __forceinline__ void sum_columns(const PvPack& k, size_t block, size_t blocks,
                                             double (*part)[72]) {
-    const size_t nb = (k.C + 63) / 64, total = nb * ((k.R + kPvSumRows - 1) / kPvSumRows);
+    const size_t nb = (k.C + 63) / 64, total = nb * ((k.R + k.rows - 1) / k.rows);
     const int group = threadIdx.x & 7, lead = threadIdx.x >> 3;
     for (size_t t = block; t < total; t += blocks) {
         const int c0 = (int)(t % nb) * 64 + group * 8;
-        const size_t r0 = t / nb * kPvSumRows;
-        const int rows = (int)min((size_t)kPvSumRows, (size_t)k.R - r0);
+        const size_t r0 = t / nb * k.rows;
+        const int rows = (int)min((size_t)k.rows, (size_t)k.R - r0);
         double s[8] = {0., 0., 0., 0., 0., 0., 0., 0.};
         if (c0 < k.C)
+#pragma unroll 4
             for (int i = lead; i < rows; i += 32) {
                 float v[8];
-                load8(k, r0 + i, c0, v);
+                load8<KIND>(k, r0 + i, c0, v);
 #pragma unroll
                 for (int q = 0; q < 8; q++) s[q] += (double)v[q];
             }
@@ -121,10 +134,19 @@ __global__ __launch_bounds__(kThreads) void pv_packs_kernel(PvPacks k) {
     int j = 0;
     while (j + 1 < k.n && blockIdx.x >= k.begin[j + 1]) j++;
     const size_t block = blockIdx.x - k.begin[j], blocks = k.begin[j + 1] - k.begin[j];
-    if (k.job[j].sums)
-        sum_columns(k.job[j], block, blocks, part);
-    else
-        pack_rows(k.job[j], block, blocks);
+    const PvPack& job = k.job[j];
+    if (job.sums) {
+        if (job.kind == kPvBf16)
+            sum_columns<kPvBf16>(job, block, blocks, part);
+        else
+            sum_columns<kPvF32>(job, block, blocks, part);
+    } else if (job.kind == kPvBf16) {
+        pack_rows<kPvBf16>(job, block, blocks);
+    } else if (job.kind == kPvF32) {
+        pack_rows<kPvF32>(job, block, blocks);
+    } else {
+        pack_rows<kPvInt8>(job, block, blocks);
+    }
 }
 
 struct PlainEpi {
@@ -166,16 +188,24 @@ struct PlainEpi {
     }
 };
 
-// A wave a column: 64 runs at a time in 64 bits, in a fixed order.
+// A wave a column: 64 runs at a time in 64 bits, in a fixed order, eight loads in flight.
 __global__ __launch_bounds__(kThreads) void pv_sum_runs_kernel(const float* runs, int n, int N,
                                                                float* out) {
-    const int c = (int)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int c = (int)blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
     if (c >= N) return;
     double s = 0.;
-    for (int i = threadIdx.x & 63; i < n; i += 64) s += (double)runs[(size_t)i * N + c];
+    for (int i0 = 0; i0 < n; i0 += 512) {
+        float v[8];
+#pragma unroll
+        for (int u = 0; u < 8; u++)
+            v[u] = runs[(size_t)min(i0 + 64 * u + lane, n - 1) * N + c];
+#pragma unroll
+        for (int u = 0; u < 8; u++)
+            if (i0 + 64 * u + lane < n) s += (double)v[u];
+    }
 #pragma unroll
     for (int w = 1; w < 64; w <<= 1) s += __shfl_xor(s, w);
-    if ((threadIdx.x & 63) == 0) out[c] = (float)s;
+    if (lane == 0) out[c] = (float)s;
 }
 
 }  // namespace
@@ -184,8 +214,9 @@ void pv_launch_packs(PvPacks& k, hipStream_t s) {
     k.begin[0] = 0;
     for (int j = 0; j < k.n; j++) {
         const PvPack& p = k.job[j];
+        const size_t per = p.pitch / 16 > kThreads ? kThreads : p.pitch / 16;
         const size_t blocks = p.sums ? (size_t)pv_sum_runs(p.R) * ((p.C + 63) / 64)
-                                     : (p.pitch / 16 * p.rows + kThreads - 1) / kThreads;
+                                     : (per * p.rows + kThreads - 1) / kThreads;
         k.begin[j + 1] = k.begin[j] + (unsigned)(blocks < (1u << 16) ? blocks : 1u << 16);
     }
     if (k.n && k.begin[k.n])
