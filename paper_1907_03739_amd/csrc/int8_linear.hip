@@ -116,12 +116,23 @@ struct Raw {
     }
 };
 
+// Where bytes go: rows of whole blocks, or (a product's own copy) block by block, each
+// block of all rows, so that the rows which a product reads at a time lie side by side:
+// 128 bytes of rows 5 KB apart came from memory at 2.6 TB/s.
+struct Layout {
+    size_t row, block;
+    __device__ __forceinline__ size_t at(size_t r, int c) const {
+        return r * row + (size_t)(c / kSlice) * block + c % kSlice;
+    }
+};
+
 // A row in the registers of a wave or of the workgroup (TEAM lanes, V vectors of eight a
 // lane); of a longer one the rest is read twice. Bound by memory, next by some ten
 // instructions a value.
 template <bool XB, int TEAM, int V>
 __global__ __launch_bounds__(kThreads) void pv_int8_quantise_kernel(PvRows x, int M, int K,
-                                                                    int8_t* q, float* scale) {
+                                                                    int8_t* q, float* scale,
+                                                                    Layout to) {
     __shared__ uint32_t tops[kThreads / 64];
     const int K128 = (K + kSlice - 1) / kSlice * kSlice, lane = threadIdx.x % TEAM;
     constexpr int kRows = kThreads / TEAM;
@@ -155,24 +166,24 @@ __global__ __launch_bounds__(kThreads) void pv_int8_quantise_kernel(PvRows x, in
         if (!live) continue;
         const float s = row_scale_of(top);
         if (lane == 0) scale[row] = s;
-        int8_t* o = q + row * K128;
         const float inv = 1.f / s, half = 0.5f * s;
         if (!(s == s)) {  // a row that is not finite
-            for (int c0 = lane * 8; c0 < K128; c0 += TEAM * 8) *(uint2*)(o + c0) = uint2{0, 0};
+            for (int c0 = lane * 8; c0 < K128; c0 += TEAM * 8)
+                *(uint2*)(q + to.at(row, c0)) = uint2{0, 0};
             continue;
         }
 #pragma unroll
         for (int u = 0; u < V; u++) {
             const int c0 = (u * TEAM + lane) * 8;
             if (c0 < K)
-                *(uint2*)(o + c0) = v[u].bytes(s, inv, half);
+                *(uint2*)(q + to.at(row, c0)) = v[u].bytes(s, inv, half);
             else if (c0 < K128)
-                *(uint2*)(o + c0) = uint2{0, 0};
+                *(uint2*)(q + to.at(row, c0)) = uint2{0, 0};
         }
         for (int c0 = (V * TEAM + lane) * 8; c0 < K128; c0 += TEAM * 8) {
             Raw<XB> w;
             w.load(x, row, c0, K);
-            *(uint2*)(o + c0) = w.bytes(s, inv, half);
+            *(uint2*)(q + to.at(row, c0)) = w.bytes(s, inv, half);
         }
     }
 }
@@ -202,20 +213,19 @@ struct LinearEpi {
     __device__ __forceinline__ void tile(const PvProduct& p, int mw, int nw, int lane,
                                          const pv_i32x4 (&acc)[4][MI]) const {
         const int r = lane & 15, nb = nw + 8 * (lane >> 4);
-        float sn[16], b[16];
+        float sn[16], b[16], sms[MI];
+#pragma unroll
+        for (int i = 0; i < MI; i++) sms[i] = row_scale[min(mw + 16 * i + r, p.M - 1)];
+        pv_load_columns(col_scale, nb, p.N, 1.f, sn);
+        pv_load_columns(bias, nb, p.N, 0.f, b);
         bool fast = true;
 #pragma unroll
-        for (int q = 0; q < 16; q++) {
-            const int at = min(pv_col(nb, q), p.N - 1);
-            sn[q] = col_scale[at];
-            b[q] = bias ? bias[at] : 0.f;
-            fast = fast && tame(sn[q]);
-        }
+        for (int q = 0; q < 16; q++) fast = fast && tame(sn[q]);
 #pragma unroll
         for (int i = 0; i < MI; i++) {
             const int m = mw + 16 * i + r;
             if (m >= p.M) continue;
-            const float sm = row_scale[m];
+            const float sm = sms[i];
             float v[16];
             if (fast && tame(sm)) {
 #pragma unroll
@@ -322,11 +332,10 @@ __global__ __launch_bounds__(kFewThreads) void pv_int8_few_kernel(PvRows x, int 
 constexpr int kFewTiles = 256;
 bool few(int M, int N) { return (size_t)((M + 15) / 16) * ((N + 15) / 16) <= kFewTiles; }
 
-PvProduct product_of(const int8_t* q, int M, int K, const int8_t* w, int N) {
+PvProduct product_of(const int8_t* q, const Layout& rows, int M, int K, const int8_t* w, int N) {
     PvProduct p{};
-    const size_t pitch = pv_up(K, kSlice);
-    p.a = PvPanel{(const uint8_t*)q, pitch, 0, 1, M};
-    p.b = PvPanel{(const uint8_t*)w, pitch, 0, 1, N};
+    p.a = PvPanel{(const uint8_t*)q, rows.row, 0, 1, M, rows.block};
+    p.b = PvPanel{(const uint8_t*)w, pv_up(K, kSlice), 0, 1, N, kSlice};
     p.M = M;
     p.N = N;
     p.slices = pv_slices(K, kSlice);
@@ -348,7 +357,7 @@ LinearWs carve_linear(void* base, int M, int K, int N, bool rows_given) {
         w.q = (int8_t*)c.take((size_t)M * pv_up(K, kSlice));
         w.scale = (float*)c.take((size_t)M * 4);
     }
-    w.partial = (uint32_t*)c.take(pv_partial_bytes(product_of(nullptr, M, K, nullptr, N)));
+    w.partial = (uint32_t*)c.take(pv_partial_bytes(product_of(nullptr, Layout{}, M, K, nullptr, N)));
     w.total = c.off;
     return w;
 }
@@ -399,10 +408,11 @@ BwdWs carve_bwd(void* base, int M, int K, int N, bool dy_bf16, bool dx_bf16, boo
 }
 
 template <bool XB>
-void run_quantise(const PvRows& x, int M, int K, int8_t* q, float* scale, hipStream_t s) {
+void run_quantise(const PvRows& x, int M, int K, int8_t* q, float* scale, const Layout& to,
+                  hipStream_t s) {
     auto run = [&](auto kernel, int team) {
         hipLaunchKernelGGL(kernel, dim3(pv_blocks(M, kThreads / team)), dim3(kThreads), 0, s, x, M,
-                           K, q, scale);
+                           K, q, scale, to);
     };
     // A wave a row up to 5120 channels. Few rows of many: a workgroup each.
     if (K > 5120 || (K > 1024 && M <= 256))
@@ -419,13 +429,17 @@ void run_quantise(const PvRows& x, int M, int K, int8_t* q, float* scale, hipStr
 
 }  // namespace
 
+static pvconv_status quantise_to(const PvRows& x, int M, int K, int8_t* q, float* scale,
+                                 const Layout& to, hipStream_t s) {
+    if (x.bf16)
+        run_quantise<true>(x, M, K, q, scale, to, s);
+    else
+        run_quantise<false>(x, M, K, q, scale, to, s);
+    return pv_launch_status();
+}
 pvconv_status pv_launch_int8_quantize(const PvRows& x, int M, int K, int8_t* q, float* scale,
                                       hipStream_t s) {
-    if (x.bf16)
-        run_quantise<true>(x, M, K, q, scale, s);
-    else
-        run_quantise<false>(x, M, K, q, scale, s);
-    return pv_launch_status();
+    return quantise_to(x, M, K, q, scale, Layout{pv_up(K, kSlice), kSlice}, s);
 }
 
 size_t pv_int8_linear_ws_bytes(int M, int K, int N, bool rows_given) {
@@ -433,10 +447,10 @@ size_t pv_int8_linear_ws_bytes(int M, int K, int N, bool rows_given) {
     return carve_linear(nullptr, M, K, N, rows_given).total;
 }
 
-static pvconv_status run_rows(const int8_t* q, const float* scale, int M, int K, int N,
+static pvconv_status run_rows(const int8_t* q, const Layout& rows, int M, int K, int N,
                               const int8_t* weight, const LinearEpi& epi, uint32_t* partial,
                               hipStream_t s) {
-    PvProduct p = product_of(q, M, K, weight, N);
+    PvProduct p = product_of(q, rows, M, K, weight, N);
     p.partial = partial;
     pv_run_product<true, false, false>(p, epi, s);
     return pv_launch_status();
@@ -464,14 +478,16 @@ pvconv_status pv_launch_int8_linear(const PvRows& x, int M, int K, int N, const 
         return pv_launch_status();
     }
     const LinearWs w = carve_linear(ws, M, K, N, rows != nullptr);
+    Layout to{pv_up(K, kSlice), kSlice};
     if (!rows) {
+        to = Layout{kSlice, (size_t)M * kSlice};
         rows = w.q;
         row_scale = w.scale;
         epi.row_scale = w.scale;
     }
-    const pvconv_status st = pv_launch_int8_quantize(x, M, K, rows, row_scale, s);
+    const pvconv_status st = quantise_to(x, M, K, rows, row_scale, to, s);
     if (st != PVCONV_OK) return st;
-    return run_rows(rows, row_scale, M, K, N, weight, epi, w.partial, s);
+    return run_rows(rows, to, M, K, N, weight, epi, w.partial, s);
 }
 
 pvconv_status pv_launch_int8_linear_rows(const int8_t* rows, const float* row_scale, int M, int K,
@@ -479,7 +495,7 @@ pvconv_status pv_launch_int8_linear_rows(const int8_t* rows, const float* row_sc
                                          const float* bias, int act, float slope, const PvRows& y,
                                          void* ws, hipStream_t s) {
     const LinearWs w = carve_linear(ws, M, K, N, true);
-    return run_rows(rows, row_scale, M, K, N, weight,
+    return run_rows(rows, Layout{pv_up(K, kSlice), kSlice}, M, K, N, weight,
                     epi_of(row_scale, scale, bias, act, slope, y), w.partial, s);
 }
 

@@ -79,17 +79,23 @@ struct CeEpi {
         const int r = lane & 15, h = lane >> 4, nb = nw + 8 * h;
         // a class past the last has the logit -inf, and so takes no part
         float b[16], cs[16];
+        pv_load_columns(c.bias, nb, p.N, -kInf, b);
 #pragma unroll
-        for (int q = 0; q < 16; q++) {
-            const int n = pv_col(nb, q);
-            b[q] = n < p.N ? (c.bias ? c.bias[n] : 0.f) : -kInf;
-            cs[q] = 0.f;
-        }
+        for (int q = 0; q < 16; q++) cs[q] = 0.f;
         const bool grads = MODE == kGrad || (MODE == kWhole && (c.dz.p || c.sums));
+        // what the rows need, all of it under way at once
+        int labels[MI];
+        float lses[MI], weights[MI];
 #pragma unroll
         for (int i = 0; i < MI; i++) {
-            const int m = mw + 16 * i + r, mc = min(m, p.M - 1);
-            const int label = c.labels[mc];
+            const int m = min(mw + 16 * i + r, p.M - 1);
+            labels[i] = c.labels[m];
+            lses[i] = MODE == kGrad ? c.lse[m] : 0.f;
+            weights[i] = MODE != kStats && c.weight ? c.weight[m] : 1.f;
+        }
+#pragma unroll
+        for (int i = 0; i < MI; i++) {
+            const int m = mw + 16 * i + r, label = labels[i];
             const bool known = label >= 0 && label < c.V;
             // which of the lane's sixteen classes the label is, if any (few lanes have it)
             const unsigned to = (unsigned)label - (unsigned)(c.v0 + nb);
@@ -129,11 +135,10 @@ struct CeEpi {
                     }
                 }
             } else {
-                lse = c.lse[mc];
+                lse = lses[i];
             }
             if (MODE != kStats && grads) {
-                float g = m < p.M && known && lse != -kInf ? 1.f : 0.f;
-                if (g != 0.f && c.weight) g = c.weight[mc];
+                const float g = m < p.M && known && lse != -kInf ? weights[i] : 0.f;
 #pragma unroll
                 for (int q = 0; q < 16; q++) z[q] = g * __expf(z[q] - lse);
                 if (at >= 0) {
@@ -200,9 +205,14 @@ __global__ __launch_bounds__(kThreads) void pv_ce_join_kernel(Join j) {
             sum = sum * __expf(top - about) + s * __expf(t - about);
             top = to;
         };
-        for (int k = lane; k < j.nb; k += TEAM) {
-            const float2 v = j.stats[m * j.nb + k];
-            add(v.x, v.y);
+        for (int k0 = 0; k0 < j.nb; k0 += 8 * TEAM) {
+            float2 v[8];
+#pragma unroll
+            for (int u = 0; u < 8; u++)
+                v[u] = j.stats[m * j.nb + min(k0 + u * TEAM + lane, j.nb - 1)];
+#pragma unroll
+            for (int u = 0; u < 8; u++)
+                if (k0 + u * TEAM + lane < j.nb) add(v[u].x, v[u].y);
         }
 #pragma unroll
         for (int w = 1; w < TEAM; w <<= 1) {
@@ -304,7 +314,7 @@ Plan carve(void* base, const PvLinearCe& a, bool forward, bool grads, bool may_d
         if (pack)
             to = pv_take_panel(c, rows, a.K, parts_of(r.bf16));
         else
-            to = PvPanel{(const uint8_t*)r.p, (size_t)r.ld * 2, 0, 1, rows};
+            to = PvPanel{(const uint8_t*)r.p, (size_t)r.ld * 2, 0, 1, rows, kSlice};
     };
     operand(a.x, a.M, p.x, p.pack_x);
     operand(a.w, a.V, p.w, p.pack_w);

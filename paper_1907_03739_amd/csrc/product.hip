@@ -52,8 +52,9 @@ __device__ __forceinline__ uint32_t next_part(float& v) {
 template <PvKind KIND>
 __device__ __forceinline__ void pack_rows(const PvPack& k, size_t block, size_t blocks) {
     const int per = (int)(k.pitch / 16);
-    int shift = 0;  // of the threads of a row
-    while (shift < 8 && (1 << shift) < per) shift++;
+    // the threads of a row: as many as leave an eighth of them idle at most
+    int shift = 8;
+    while (shift > 3 && ((per + (1 << shift) - 1) >> shift << shift) > per + per / 8) shift--;
     const int lead = threadIdx.x >> shift, first = threadIdx.x & ((1 << shift) - 1);
     const size_t rows = (size_t)kThreads >> shift;
     for (size_t row = block * rows + lead; row < (size_t)k.rows; row += blocks * rows) {
@@ -208,15 +209,31 @@ __global__ __launch_bounds__(kThreads) void pv_sum_runs_kernel(const float* runs
     if (lane == 0) out[c] = (float)s;
 }
 
+// The same, a thread a column: many columns, whose neighbours lie side by side.
+__global__ __launch_bounds__(kThreads) void pv_sum_runs_wide_kernel(const float* runs, int n,
+                                                                    int N, float* out) {
+    const int c = (int)blockIdx.x * kThreads + threadIdx.x;
+    if (c >= N) return;
+    double s = 0.;
+    for (int i0 = 0; i0 < n; i0 += 8) {
+        float v[8];
+#pragma unroll
+        for (int u = 0; u < 8; u++) v[u] = runs[(size_t)min(i0 + u, n - 1) * N + c];
+#pragma unroll
+        for (int u = 0; u < 8; u++)
+            if (i0 + u < n) s += (double)v[u];
+    }
+    out[c] = (float)s;
+}
+
 }  // namespace
 
 void pv_launch_packs(PvPacks& k, hipStream_t s) {
     k.begin[0] = 0;
     for (int j = 0; j < k.n; j++) {
         const PvPack& p = k.job[j];
-        const size_t per = p.pitch / 16 > kThreads ? kThreads : p.pitch / 16;
         const size_t blocks = p.sums ? (size_t)pv_sum_runs(p.R) * ((p.C + 63) / 64)
-                                     : (per * p.rows + kThreads - 1) / kThreads;
+                                     : (p.pitch / 16 * p.rows + 2 * kThreads - 1) / (2 * kThreads);
         k.begin[j + 1] = k.begin[j] + (unsigned)(blocks < (1u << 16) ? blocks : 1u << 16);
     }
     if (k.n && k.begin[k.n])
@@ -224,8 +241,12 @@ void pv_launch_packs(PvPacks& k, hipStream_t s) {
 }
 
 void pv_launch_sum_runs(const float* runs, int n, int N, float* out, hipStream_t s) {
-    hipLaunchKernelGGL(pv_sum_runs_kernel, dim3((N + 3) / 4), dim3(kThreads), 0, s, runs, n, N,
-                       out);
+    if (N >= 4096)
+        hipLaunchKernelGGL(pv_sum_runs_wide_kernel, dim3((N + kThreads - 1) / kThreads),
+                           dim3(kThreads), 0, s, runs, n, N, out);
+    else
+        hipLaunchKernelGGL(pv_sum_runs_kernel, dim3((N + 3) / 4), dim3(kThreads), 0, s, runs, n, N,
+                           out);
 }
 
 void pv_launch_plain(const PvProduct& p, bool a_across, const PvPlain& e, hipStream_t s) {

@@ -35,6 +35,7 @@ struct PvPanel {  // rows at p + part * part_bytes + row * pitch
     size_t pitch, part_bytes;
     int parts;
     int rows;  // that may be read (used across k)
+    size_t slice_bytes;  // from one slice to the next (along k)
 };
 struct PvProduct {
     PvPanel a, b;
@@ -174,7 +175,7 @@ struct PvSource {
     // where a slice lies
     __device__ __forceinline__ const uint8_t* slice(const PvPanel& p, int part, int k) const {
         return base + part * p.part_bytes +
-               (size_t)k * (ACROSS ? kDeep * p.pitch : (size_t)kSlice);
+               (size_t)k * (ACROSS ? kDeep * p.pitch : p.slice_bytes);
     }
     __device__ __forceinline__ void load(const PvPanel& p, const uint8_t* from, int k, int q,
                                          int wave, int lane, uint8_t* lds) const {
@@ -434,6 +435,24 @@ pv_product_kernel(PvProduct p, Epi epi) {
         if (!more) return;
     }
 }
+// Sixteen values of columns, as a lane has them: `none` from N on, or where there are none.
+__device__ __forceinline__ void pv_load_columns(const float* from, int nb, int N, float none,
+                                                float (&v)[16]) {
+#pragma unroll
+    for (int a = 0; a < 2; a++) {
+        const int n = nb + 32 * a;
+        if (from && n + 8 <= N) {
+            const pv_u32x4 x = *(const pv_u32x4_any*)(from + n),
+                           y = *(const pv_u32x4_any*)(from + n + 4);
+#pragma unroll
+            for (int i = 0; i < 8; i++) v[8 * a + i] = __uint_as_float(i < 4 ? x[i] : y[i - 4]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; i++)
+                v[8 * a + i] = n + i < N ? (from ? from[n + i] : 0.f) : none;
+        }
+    }
+}
 // The column of value q (of sixteen) of a lane whose first one is nb = nw + 8 h: acc[q >>
 // 2][i][q & 3].
 __device__ __forceinline__ int pv_col(int nb, int q) { return nb + 32 * (q >> 3) + (q & 7); }
@@ -689,6 +708,7 @@ static inline PvPanel pv_take_panel(PvCarve& c, int rows, int cols, int parts) {
     p.part_bytes = pv_align256((size_t)rows * p.pitch);
     p.parts = parts;
     p.rows = rows;
+    p.slice_bytes = kSlice;
     p.p = (const uint8_t*)c.take(p.part_bytes * parts);
     return p;
 }
