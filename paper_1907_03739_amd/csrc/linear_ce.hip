@@ -53,6 +53,9 @@ __device__ __forceinline__ uint32_t next_part2(float& a, float& b) {
     return w;
 }
 
+// a branch of the wave: as one of its lanes, the compiler takes both sides
+__device__ __forceinline__ bool any_lane(bool b) { return __builtin_amdgcn_ballot_w64(b) != 0; }
+
 enum Mode { kStats, kWhole, kGrad };
 
 // PARTS: dz in more than one bf16 part somewhere (what remains of it is then held too).
@@ -114,10 +117,9 @@ struct CeEpi {
                 float sum = 0.f, zl = 0.f;
 #pragma unroll
                 for (int q = 0; q < 16; q++) sum += __expf(z[q] - about);
-                if (at >= 0) {
+                if (any_lane(at >= 0)) {
 #pragma unroll
-                    for (int q = 0; q < 16; q++)
-                        if (q == at) zl = z[q];
+                    for (int q = 0; q < 16; q++) zl = q == at ? z[q] : zl;
                 }
                 sum = lanes_sum(sum);
                 if constexpr (MODE == kStats) {
@@ -141,14 +143,13 @@ struct CeEpi {
                 const float g = m < p.M && known && lse != -kInf ? weights[i] : 0.f;
 #pragma unroll
                 for (int q = 0; q < 16; q++) z[q] = g * __expf(z[q] - lse);
-                if (at >= 0) {
+                if (any_lane(at >= 0)) {
 #pragma unroll
-                    for (int q = 0; q < 16; q++)
-                        if (q == at) z[q] -= g;
+                    for (int q = 0; q < 16; q++) z[q] -= q == at ? g : 0.f;
                 }
-                if (g == 0.f) {  // whatever the logits are
+                if (any_lane(g == 0.f)) {  // 0, whatever the logits are
 #pragma unroll
-                    for (int q = 0; q < 16; q++) z[q] = 0.f;
+                    for (int q = 0; q < 16; q++) z[q] = g == 0.f ? 0.f : z[q];
                 }
 #pragma unroll
                 for (int q = 0; q < 16; q++) cs[q] += z[q];
@@ -164,10 +165,14 @@ struct CeEpi {
             // lane r is left with the sum of column r
 #pragma unroll
             for (int w = 8; w; w >>= 1) {
-                const bool up = r & w;
+                // (by masks: of two elements chosen by the lane the compiler makes one
+                // that it looks for among all)
+                const uint32_t up = r & w ? ~0u : 0u;
 #pragma unroll
                 for (int q = 0; q < w; q++) {
-                    const float keep = up ? cs[q + w] : cs[q], give = up ? cs[q] : cs[q + w];
+                    const uint32_t x = __float_as_uint(cs[q]), y = __float_as_uint(cs[q + w]);
+                    const float keep = __uint_as_float((y & up) | (x & ~up)),
+                                give = __uint_as_float((x & up) | (y & ~up));
                     cs[q] = keep + __shfl_xor(give, w);
                 }
             }
@@ -277,6 +282,7 @@ int row_blocks(int M, int size) {  // as many as waves have rows
         case kPvL: return row_blocks_of<PvTileL>(M);
         case kPvG: return row_blocks_of<PvTileG>(M);
         case kPvM: return row_blocks_of<PvTileM>(M);
+        case kPvD: return row_blocks_of<PvTileD>(M);
         case kPvN: return row_blocks_of<PvTileN>(M);
         default: return row_blocks_of<PvTileS>(M);
     }
@@ -288,7 +294,7 @@ constexpr unsigned sizes_of(int mode, bool parts) {
     const unsigned narrow = 1u << kPvS | 1u << kPvN;
     if (mode == kWhole) return narrow;
     if (mode == kStats) return kPvAnySize;
-    return narrow | 1u << kPvM | (parts ? 0u : 1u << kPvG);
+    return narrow | 1u << kPvM | (parts ? 0u : 1u << kPvG | 1u << kPvD);
 }
 // The product of x with n classes from v0 on.
 PvProduct logits_of(const PvPanel& x, const PvPanel& w, int M, int K, int v0, int n,

@@ -75,9 +75,10 @@ struct PvTile {
 typedef PvTile<2, 4, 8, 2, 1> PvTileL;  // 256 x 256
 typedef PvTile<4, 2, 4, 3, 1> PvTileG;  // 256 x 128
 typedef PvTile<2, 2, 4, 4, 1> PvTileM;  // 128 x 128
+typedef PvTile<2, 2, 4, 2, 2> PvTileD;  // 128 x 128, two workgroups a CU
 typedef PvTile<4, 1, 2, 4, 1> PvTileN;  // 128 x 64
 typedef PvTile<2, 1, 2, 4, 2> PvTileS;  // 64 x 64
-enum PvSize { kPvS, kPvN, kPvM, kPvG, kPvL };
+enum PvSize { kPvS, kPvN, kPvM, kPvG, kPvL, kPvD };
 
 // The tile of index idx: eight tiles of rows by the columns in turn, so that an XCD,
 // which works on neighbours at a time, has both operands in its L2.
@@ -510,10 +511,11 @@ static constexpr PvSizeCost kPvCosts[] = {
     {kPvL, PvTileL::TM, PvTileL::TN, PvTileL::kWorkgroups, 1.4f, 6.f},
     {kPvG, PvTileG::TM, PvTileG::TN, PvTileG::kWorkgroups, 0.82f, 4.5f},
     {kPvM, PvTileM::TM, PvTileM::TN, PvTileM::kWorkgroups, 0.62f, 3.5f},
+    {kPvD, PvTileD::TM, PvTileD::TN, PvTileD::kWorkgroups, 1.15f, 5.f},
     {kPvN, PvTileN::TM, PvTileN::TN, PvTileN::kWorkgroups, 0.43f, 3.f},
     {kPvS, PvTileS::TM, PvTileS::TN, PvTileS::kWorkgroups, 0.42f, 3.f},
 };
-static inline void pv_plan(PvProduct& p, bool may_split, unsigned sizes = 31) {
+static inline void pv_plan(PvProduct& p, bool may_split, unsigned sizes = 63) {
     const int all = p.slices * p.pairs;
     float best = 0.f;
     for (const PvSizeCost& c : kPvCosts) {
@@ -639,7 +641,7 @@ static void pv_run_tiles(PvProduct p, const Epi& epi, hipStream_t s) {
                            dim3(256), 0, s, p, epi);
 }
 // SIZES: the tiles (1 << PvSize) that the plan may have chosen
-constexpr unsigned kPvAnySize = 31;
+constexpr unsigned kPvAnySize = 63;
 template <bool I8, bool TA, bool TB, unsigned SIZES = kPvAnySize, class Epi>
 static void pv_run_product(const PvProduct& p, const Epi& epi, hipStream_t s) {
     if constexpr (SIZES >> kPvL & 1)
@@ -648,6 +650,8 @@ static void pv_run_product(const PvProduct& p, const Epi& epi, hipStream_t s) {
         if (p.size == kPvG) pv_run_tiles<I8, TA, TB, PvTileG>(p, epi, s);
     if constexpr (SIZES >> kPvM & 1)
         if (p.size == kPvM) pv_run_tiles<I8, TA, TB, PvTileM>(p, epi, s);
+    if constexpr (SIZES >> kPvD & 1)
+        if (p.size == kPvD) pv_run_tiles<I8, TA, TB, PvTileD>(p, epi, s);
     if constexpr (SIZES >> kPvN & 1)
         if (p.size == kPvN) pv_run_tiles<I8, TA, TB, PvTileN>(p, epi, s);
     if constexpr (SIZES >> kPvS & 1)
