@@ -185,8 +185,8 @@ pvconv_status pvconv_int8_linear_rows(const int8_t* rows, const float* row_scale
 /*   dx[m,k] = sum_n dy[m,n] scale_n weight[n,k]                             */
 /*   dw[n,k] = sum_m dy[m,n] row_scale_m rows[m,k],  dbias_n = sum_m dy[m,n] */
 /* An fp32 output has fp32 sums of products good to 24 bits; for a bf16 dx of */
-/* more than 256 rows, dy scale_n is rounded to bf16 first (of fewer: to 16  */
-/* bits).                                                                    */
+/* more than 256 rows, one factor (scale_n weight of a bf16 dy, dy scale_n of */
+/* an fp32 one) is rounded to bf16 first (of fewer: to 16 bits).             */
 /*  dy [M][N] (dy_dt), dy_ld; dx out [M][K] (dx_dt), dx_ld, or NULL (weight, */
 /*  scale then unused); dw out [N][K] fp32 or NULL (rows, row_scale then     */
 /*  unused); dbias out [N] fp32 or NULL                                      */

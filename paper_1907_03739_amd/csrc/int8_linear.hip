@@ -362,23 +362,26 @@ LinearWs carve_linear(void* base, int M, int K, int N, bool rows_given) {
     return w;
 }
 
-// Parts that a gradient's scaled operand needs: one rounded part for a bf16 result of
-// rows enough to average it, else the two that hold 8 by 8 bits for a bf16 dy, three for
-// 32 bits.
+// Parts of a gradient's scaled operand: for a bf16 result one rounded part, of few rows
+// (which would not average it) two. For an fp32 one, the two that hold 8 by 8 bits where
+// dy is bf16, else three.
 constexpr int kFewRows = 256;
 int parts_of(bool out_bf16, bool dy_bf16, int M) {
     if (out_bf16) return M <= kFewRows ? 2 : 1;
     return dy_bf16 ? 2 : 3;
 }
 
+// dx = dy W: of a bf16 dy as it is by the scaled weight, in parts; of an fp32 one in
+// parts, scaled, by the weight's whole numbers. dw = (dy s)^T q.
 struct BwdWs {
     PvPanel dys, w, dym, q;
+    bool pack_dy;
     PvProduct dx, dw;
     float* sums;
     size_t total;
 };
-BwdWs carve_bwd(void* base, int M, int K, int N, bool dy_bf16, bool dx_bf16, bool want_dx,
-                bool want_dw, bool want_db) {
+BwdWs carve_bwd(void* base, const PvRows& dy, int M, int K, int N, bool dx_bf16, bool want_dx,
+                bool want_dw, bool want_db, bool may_direct) {
     PvCarve c{(char*)base, 0};
     BwdWs w{};
     auto product = [&](PvProduct& p, const PvPanel& a, const PvPanel& b, int rows, int cols,
@@ -393,12 +396,14 @@ BwdWs carve_bwd(void* base, int M, int K, int N, bool dy_bf16, bool dx_bf16, boo
         p.partial = (uint32_t*)c.take(pv_partial_bytes(p));
     };
     if (want_dx && M > 0) {
-        w.dys = pv_take_panel(c, M, N, parts_of(dx_bf16, dy_bf16, M));
-        w.w = pv_take_panel(c, N, K, 1);
+        const int parts = parts_of(dx_bf16, dy.bf16, M);
+        w.pack_dy = !(may_direct && pv_in_place(dy, N));
+        w.dys = w.pack_dy ? pv_take_panel(c, M, N, dy.bf16 ? 1 : parts) : pv_panel_of(dy, M);
+        w.w = pv_take_panel(c, N, K, dy.bf16 ? parts : 1);
         product(w.dx, w.dys, w.w, M, K, N);
     }
     if (want_dw) {  // both operands across k: dy's rows are padded with zeros
-        w.dym = pv_take_panel(c, (int)pv_up(M, kDeep), N, parts_of(false, dy_bf16, M));
+        w.dym = pv_take_panel(c, (int)pv_up(M, kDeep), N, parts_of(false, dy.bf16, M));
         w.q = pv_take_panel(c, M, K, 1);
         product(w.dw, w.dym, w.q, N, K, M);
     }
@@ -502,8 +507,8 @@ pvconv_status pv_launch_int8_linear_rows(const int8_t* rows, const float* row_sc
 size_t pv_int8_linear_bwd_ws_bytes(int M, int K, int N) {
     size_t most = 0;  // that any of the types takes
     for (int types = 0; types < 4; types++) {
-        const size_t n =
-            carve_bwd(nullptr, M, K, N, types & 1, types & 2, true, true, true).total;
+        const PvRows dy{nullptr, (types & 1) != 0, N};
+        const size_t n = carve_bwd(nullptr, dy, M, K, N, types & 2, true, true, true, false).total;
         most = most > n ? most : n;
     }
     return most;
@@ -514,17 +519,21 @@ pvconv_status pv_launch_int8_linear_bwd(const PvRows& dy, const int8_t* rows,
                                         const int8_t* weight, const float* scale,
                                         const PvRows& dx, float* dw, float* dbias, void* ws,
                                         hipStream_t s) {
-    const BwdWs w = carve_bwd(ws, M, K, N, dy.bf16, dx.bf16, dx.p != nullptr, dw != nullptr,
-                              dbias != nullptr);
+    const BwdWs w = carve_bwd(ws, dy, M, K, N, dx.bf16, dx.p != nullptr, dw != nullptr,
+                              dbias != nullptr, true);
     const PvKind kind = dy.bf16 ? kPvBf16 : kPvF32;
     const size_t qk = pv_up(K, kSlice);
     const bool want_dx = dx.p && M > 0;
     PvPacks packs{};
     if (want_dx) {
-        PvPack a = pv_pack_of(dy.p, kind, dy.ld, M, N, w.dys);
-        a.col_scale = scale;
-        packs.add(a);
-        packs.add(pv_pack_of(weight, kPvInt8, qk, N, K, w.w));
+        PvPack a = pv_pack_of(dy.p, kind, dy.ld, M, N, w.dys),
+               b = pv_pack_of(weight, kPvInt8, qk, N, K, w.w);
+        if (dy.bf16)
+            b.row_scale = scale;
+        else
+            a.col_scale = scale;
+        if (w.pack_dy) packs.add(a);
+        packs.add(b);
     }
     if (dw && M > 0) {
         PvPack a = pv_pack_of(dy.p, kind, dy.ld, M, N, w.dym);

@@ -268,11 +268,6 @@ struct Plan {
     size_t total;
 };
 
-bool direct(const PvRows& r, int K) {
-    return r.bf16 && K % 64 == 0 && r.ld % 8 == 0 && pv_aligned16(r.p) &&
-           (size_t)r.ld * 2 <= kPvMostPitch;
-}
-
 template <class T>
 int row_blocks_of(int M) {
     return (int)(pv_up(M, T::TM) / (16 * T::MI));
@@ -316,11 +311,11 @@ Plan carve(void* base, const PvLinearCe& a, bool forward, bool grads, bool may_d
     Plan p{};
     p.whole = a.V <= kWholeClasses;
     auto operand = [&](const PvRows& r, int rows, PvPanel& to, bool& pack) {
-        pack = !(may_direct && direct(r, a.K));
+        pack = !(may_direct && pv_in_place(r, a.K));
         if (pack)
             to = pv_take_panel(c, rows, a.K, parts_of(r.bf16));
         else
-            to = PvPanel{(const uint8_t*)r.p, (size_t)r.ld * 2, 0, 1, rows, kSlice};
+            to = pv_panel_of(r, rows);
     };
     operand(a.x, a.M, p.x, p.pack_x);
     operand(a.w, a.V, p.w, p.pack_w);

@@ -52,9 +52,11 @@ __device__ __forceinline__ uint32_t next_part(float& v) {
 template <PvKind KIND>
 __device__ __forceinline__ void pack_rows(const PvPack& k, size_t block, size_t blocks) {
     const int per = (int)(k.pitch / 16);
-    // the threads of a row: as many as leave an eighth of them idle at most
+    // the threads of a row: as many as leave an eighth of them idle at most, of few rows a
+    // third
+    const int idle = k.rows <= 4096 ? per / 3 : per / 8;
     int shift = 8;
-    while (shift > 3 && ((per + (1 << shift) - 1) >> shift << shift) > per + per / 8) shift--;
+    while (shift > 3 && ((per + (1 << shift) - 1) >> shift << shift) > per + idle) shift--;
     const int lead = threadIdx.x >> shift, first = threadIdx.x & ((1 << shift) - 1);
     const size_t rows = (size_t)kThreads >> shift;
     for (size_t row = block * rows + lead; row < (size_t)k.rows; row += blocks * rows) {
@@ -64,7 +66,7 @@ __device__ __forceinline__ void pack_rows(const PvPack& k, size_t block, size_t 
             float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
             if (row < (size_t)k.R) {
                 load8<KIND>(k, row, c0, v);
-                if (k.row_scale) {
+                if (k.row_scale) {  // (NaN for a row that was not finite)
 #pragma unroll
                     for (int i = 0; i < 8; i++) v[i] = c0 + i < k.C ? v[i] * rs : 0.f;
                 }

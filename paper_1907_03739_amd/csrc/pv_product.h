@@ -521,7 +521,10 @@ static inline void pv_plan(PvProduct& p, bool may_split, unsigned sizes = 63) {
     for (const PvSizeCost& c : kPvCosts) {
         if (!(sizes >> c.size & 1)) continue;
         const size_t tiles = pv_tiles_of(p.M, p.N, c.tm, c.tn);
-        for (int n = 1; n == 1 || (may_split && n <= 256 && all / n >= 4); n += n < 8 ? 1 : n / 4) {
+        // (split no further than one round of workgroups, and into runs of four slices)
+        for (int n = 1; n == 1 || (may_split && tiles * (size_t)(n - 1) < (size_t)c.slots &&
+                                   all / n >= 4);
+             n += n < 8 ? 1 : n / 4) {
             const int per = n == 1 ? all : (all + n - 1) / n;
             const int splits = per ? (all + per - 1) / per : 1;
             const size_t rounds = (tiles * splits + c.slots - 1) / c.slots;
@@ -715,6 +718,14 @@ static inline PvPanel pv_take_panel(PvCarve& c, int rows, int cols, int parts) {
     p.slice_bytes = kSlice;
     p.p = (const uint8_t*)c.take(p.part_bytes * parts);
     return p;
+}
+// Whether rows of C channels are an operand as they lie, and the operand that they are.
+static inline bool pv_in_place(const PvRows& r, int C) {
+    return r.bf16 && C % kDeep == 0 && r.ld % 8 == 0 && pv_aligned16(r.p) &&
+           (size_t)r.ld * 2 <= kPvMostPitch;
+}
+static inline PvPanel pv_panel_of(const PvRows& r, int rows) {
+    return PvPanel{(const uint8_t*)r.p, (size_t)r.ld * 2, 0, 1, rows, kSlice};
 }
 static inline PvPack pv_pack_of(const void* src, PvKind kind, size_t ld, int R, int C,
                                 const PvPanel& to) {
