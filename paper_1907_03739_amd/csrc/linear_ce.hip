@@ -279,6 +279,7 @@ int row_blocks(int M, int size) {  // as many as waves have rows
         case kPvM: return row_blocks_of<PvTileM>(M);
         case kPvD: return row_blocks_of<PvTileD>(M);
         case kPvN: return row_blocks_of<PvTileN>(M);
+        case kPvP: return row_blocks_of<PvTileP>(M);
         default: return row_blocks_of<PvTileS>(M);
     }
 }
@@ -286,7 +287,7 @@ int row_blocks(int M, int size) {  // as many as waves have rows
 // sums of the largest tiles there are no registers for dz, of the next none for what its
 // first part leaves.
 constexpr unsigned sizes_of(int mode, bool parts) {
-    const unsigned narrow = 1u << kPvS | 1u << kPvN;
+    const unsigned narrow = 1u << kPvS | 1u << kPvN | 1u << kPvP;
     if (mode == kWhole) return narrow;
     if (mode == kStats) return kPvAnySize;
     return narrow | 1u << kPvM | (parts ? 0u : 1u << kPvG | 1u << kPvD);

@@ -78,7 +78,8 @@ typedef PvTile<2, 2, 4, 4, 1> PvTileM;  // 128 x 128
 typedef PvTile<2, 2, 4, 2, 2> PvTileD;  // 128 x 128, two workgroups a CU
 typedef PvTile<4, 1, 2, 4, 1> PvTileN;  // 128 x 64
 typedef PvTile<2, 1, 2, 4, 2> PvTileS;  // 64 x 64
-enum PvSize { kPvS, kPvN, kPvM, kPvG, kPvL, kPvD };
+typedef PvTile<4, 1, 1, 2, 1> PvTileP;  // 64 x 64, all parts of a slice in a stage
+enum PvSize { kPvS, kPvN, kPvM, kPvG, kPvL, kPvD, kPvP };
 
 // The tile of index idx: eight tiles of rows by the columns in turn, so that an XCD,
 // which works on neighbours at a time, has both operands in its L2.
@@ -209,6 +210,32 @@ __device__ __forceinline__ pv_u32x4 pv_load_across(const uint8_t* lds, int k0, i
         v[2 * s + 1] = u[1];
     }
     return v;
+}
+
+// a split's sums of a wave's tile
+template <int MI, class Acc>
+__device__ __forceinline__ void pv_store_partial(const PvProduct& p, int split, int mw, int nw,
+                                                 int lane, const Acc (&acc)[4][MI]) {
+    uint32_t* part = p.partial + (size_t)split * p.M * p.N;
+    const int r = lane & 15, h = lane >> 4;
+#pragma unroll
+    for (int i = 0; i < MI; i++) {
+        const int m = mw + 16 * i + r;
+        if (m >= p.M) continue;
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            const int n = nw + 32 * (j >> 1) + 8 * h + 4 * (j & 1);
+            uint32_t* o = part + (size_t)m * p.N + n;
+            pv_u32x4 v;
+            __builtin_memcpy(&v, &acc[j][i], 16);
+            if (n + 4 <= p.N)
+                *(pv_u32x4_any*)o = v;
+            else
+#pragma unroll
+                for (int e = 0; e < 4; e++)
+                    if (n + e < p.N) o[e] = v[e];
+        }
+    }
 }
 
 // The epilogue gets acc[j][i][e]: row mw + 16 i + r, column nw + 32 (j >> 1) + 8 h + 4
@@ -411,31 +438,124 @@ pv_product_kernel(PvProduct p, Epi epi) {
             first();
         }
         if (p.splits > 1) {
-            uint32_t* part = p.partial + (size_t)es * p.M * p.N;
-#pragma unroll
-            for (int i = 0; i < MI; i++) {
-                const int m = em + 16 * i + r;
-                if (m >= p.M) continue;
-#pragma unroll
-                for (int j = 0; j < 4; j++) {
-                    const int n = en + 32 * (j >> 1) + 8 * h + 4 * (j & 1);
-                    uint32_t* o = part + (size_t)m * p.N + n;
-                    pv_u32x4 v;
-                    __builtin_memcpy(&v, &acc[j][i], 16);
-                    if (n + 4 <= p.N)
-                        *(pv_u32x4_any*)o = v;
-                    else
-#pragma unroll
-                        for (int e = 0; e < 4; e++)
-                            if (n + e < p.N) o[e] = v[e];
-                }
-            }
+            pv_store_partial<MI>(p, es, em, en, lane, acc);
         } else {
             epi.template tile<MI>(p, em, en, lane, acc);
         }
         if (!more) return;
     }
 }
+// The same product in tiles of 64 x 64 whose stages hold every part of a slice: a step of
+// 64 k's is one barrier for all pairs of parts (999 x 323 x 1003 in 32 bits: 36 steps of a
+// pair each took 16 us), and a part is loaded once for all pairs that it is in.
+template <bool TA, bool TB, int PA, int PB, class Epi>
+__global__ __launch_bounds__(PvTileP::kThreads, 1) void pv_parts_kernel(PvProduct p, Epi epi) {
+    typedef PvTileP T;
+    constexpr int SA = T::TM * kSlice, SB = T::TN * kSlice, MI = T::MI;
+    __shared__ __align__(16) uint8_t la0[PA * SA], la1[PA * SA], lb0[PB * SB], lb1[PB * SB];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, r = lane & 15, h = lane >> 4;
+    const int wm = wave * 16;
+    const uint32_t run = (p.count + 7) / 8, step = gridDim.x >> 3;
+    const uint32_t end = min(run * ((blockIdx.x & 7) + 1), p.count);
+    uint32_t idx = run * (blockIdx.x & 7) + (blockIdx.x >> 3);
+    if (idx >= end) return;
+    int split, m0, n0, k, k1;
+    PvSource<TA, false, T::TM, T::kThreads> from_a;
+    PvSource<TB, true, T::TN, T::kThreads> from_b;
+    constexpr int QA = decltype(from_a)::Q, QB = decltype(from_b)::Q;
+    auto enter = [&]() {
+        pv_tile_of<T>(p, p.first + idx, split, m0, n0);
+        k = split * p.per / p.pairs;  // (whole steps)
+        k1 = min(k + p.per / p.pairs, p.slices);
+        from_a.enter(p.a, m0, p.M, wave, lane);
+        from_b.enter(p.b, n0, p.N, wave, lane);
+    };
+    auto fetch = [&](int at, uint8_t* la, uint8_t* lb) {
+        pv_each<PA>([&](auto part) {
+            const uint8_t* from = from_a.slice(p.a, part, at);
+            pv_each<QA>([&](auto q) {
+                from_a.load(p.a, from, at, q, wave, lane, la + part * SA);
+            });
+        });
+        pv_each<PB>([&](auto part) {
+            const uint8_t* from = from_b.slice(p.b, part, at);
+            pv_each<QB>([&](auto q) {
+                from_b.load(p.b, from, at, q, wave, lane, lb + part * SB);
+            });
+        });
+    };
+    auto load_a = [&](const uint8_t* la, int half) {
+        if constexpr (TA) {
+            return pv_load_across<T::TM>(la, 32 * half, wm + 4 * (lane & 3), lane);
+        } else {
+            const int row = wm + r;
+            return *(const pv_u32x4*)(la + row * kSlice + ((h + 4 * half) ^ pv_key_a(row)) * 16);
+        }
+    };
+    auto load_b = [&](const uint8_t* lb, int j, int half) {
+        if constexpr (TB) {
+            return pv_load_across<T::TN>(lb, 32 * half,
+                                         32 * (j >> 1) + 8 * (lane & 3) + 4 * (j & 1), lane);
+        } else {
+            const int row = 32 * (j >> 1) + 8 * (r >> 2) + 4 * (j & 1) + (r & 3);
+            return *(const pv_u32x4*)(lb + row * kSlice + ((h + 4 * half) ^ pv_key_b(row)) * 16);
+        }
+    };
+    enter();
+    if (k < k1) fetch(k, la0, lb0);
+    for (;;) {
+        pv_f32x4 acc[4][MI];
+#pragma unroll
+        for (int j = 0; j < 4; j++) acc[j][0] = pv_f32x4{0.f, 0.f, 0.f, 0.f};
+        constexpr int kOrders = PA < 3 && PB < 3 ? 2 : 3;  // as pv_pairs
+        auto one = [&](const uint8_t* la, const uint8_t* lb, uint8_t* na, uint8_t* nb) {
+            if (k >= k1) return;
+            pv_wait_loads<0>();
+            pv_stage_barrier();
+            if (k + 1 < k1) fetch(k + 1, na, nb);
+            pv_each<2>([&](auto half) {
+                pv_u32x4 fa[PA], fb[PB][4];
+                pv_each<PA>([&](auto i) { fa[i] = load_a(la + i * SA, half); });
+                pv_each<PB>([&](auto i) {
+                    pv_each<4>([&](auto j) { fb[i][j] = load_b(lb + i * SB, j, half); });
+                });
+                pv_each<PA>([&](auto x) {
+                    pv_each<PB>([&](auto y) {
+                        if constexpr (x + y < kOrders)
+                            pv_each<4>([&](auto j) {
+                                pv_b16x8 va, vb;
+                                __builtin_memcpy(&va, &fa[x], 16);
+                                __builtin_memcpy(&vb, &fb[y][j], 16);
+                                acc[j][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                                    vb, va, acc[j][0], 0, 0, 0);
+                            });
+                    });
+                });
+            });
+            k++;
+        };
+        while (k < k1) {
+            one(la0, lb0, la1, lb1);
+            one(la1, lb1, la0, lb0);
+        }
+        const int em = m0 + wm, en = n0, es = split;
+        idx += step;
+        const bool more = idx < end;
+        if (more) {
+            pv_wait_loads<63>();
+            pv_stage_barrier();  // nothing reads the stages any more
+            enter();
+            if (k < k1) fetch(k, la0, lb0);
+        }
+        if (p.splits > 1)
+            pv_store_partial<MI>(p, es, em, en, lane, acc);
+        else
+            epi.template tile<MI>(p, em, en, lane, acc);
+        if (!more) return;
+    }
+}
+
 // Sixteen values of columns, as a lane has them: `none` from N on, or where there are none.
 __device__ __forceinline__ void pv_load_columns(const float* from, int nb, int N, float none,
                                                 float (&v)[16]) {
@@ -515,17 +635,21 @@ static constexpr PvSizeCost kPvCosts[] = {
     {kPvN, PvTileN::TM, PvTileN::TN, PvTileN::kWorkgroups, 0.43f, 3.f},
     {kPvS, PvTileS::TM, PvTileS::TN, PvTileS::kWorkgroups, 0.42f, 3.f},
 };
-static inline void pv_plan(PvProduct& p, bool may_split, unsigned sizes = 63) {
+// The pairs of operands that PvTileP is built for.
+static constexpr bool pv_all_parts(int a, int b) {
+    return (a == 3 && (b == 3 || b == 1)) || (a == 1 && b == 3);
+}
+static inline void pv_plan(PvProduct& p, bool may_split, unsigned sizes = 127) {
     const int all = p.slices * p.pairs;
     float best = 0.f;
-    for (const PvSizeCost& c : kPvCosts) {
-        if (!(sizes >> c.size & 1)) continue;
+    auto choose = [&](const PvSizeCost& c) {
         const size_t tiles = pv_tiles_of(p.M, p.N, c.tm, c.tn);
         // (split no further than one round of workgroups, and into runs of four slices)
         for (int n = 1; n == 1 || (may_split && tiles * (size_t)(n - 1) < (size_t)c.slots &&
                                    all / n >= 4);
              n += n < 8 ? 1 : n / 4) {
-            const int per = n == 1 ? all : (all + n - 1) / n;
+            int per = n == 1 ? all : (all + n - 1) / n;
+            if (c.size == kPvP) per = (per + p.pairs - 1) / p.pairs * p.pairs;  // whole steps
             const int splits = per ? (all + per - 1) / per : 1;
             const size_t rounds = (tiles * splits + c.slots - 1) / c.slots;
             float us = (float)rounds * ((float)per * c.slice + c.rest);
@@ -537,7 +661,12 @@ static inline void pv_plan(PvProduct& p, bool may_split, unsigned sizes = 63) {
                 p.splits = splits;
             }
         }
-    }
+    };
+    for (const PvSizeCost& c : kPvCosts)
+        if (sizes >> c.size & 1) choose(c);
+    if ((sizes >> kPvP & 1) && pv_all_parts(p.a.parts, p.b.parts) && p.pairs > 1)
+        choose(PvSizeCost{kPvP, PvTileP::TM, PvTileP::TN, PvTileP::kWorkgroups,
+                          0.07f + 0.25f / p.pairs, 3.f});
 }
 static inline size_t pv_partial_bytes(const PvProduct& p) {
     return p.splits > 1 ? (size_t)p.splits * p.M * p.N * 4 : 0;
@@ -624,27 +753,33 @@ static inline unsigned pv_blocks(size_t items, int per) {
 }
 
 constexpr size_t kPvTilesALaunch = (size_t)1 << 30;
-template <bool I8, bool TA, bool TB, class T, class Epi>
-static void pv_run_tiles(PvProduct p, const Epi& epi, hipStream_t s) {
+template <class T, class Kernel, class Epi>
+static void pv_launch_tiles(Kernel kernel, PvProduct p, const Epi& epi, hipStream_t s) {
     const size_t tiles = pv_tiles_of(p.M, p.N, T::TM, T::TN) * p.splits;
     for (size_t t = 0; t < tiles; t += kPvTilesALaunch) {
         p.first = (uint32_t)t;
         p.count = (uint32_t)(tiles - t < kPvTilesALaunch ? tiles - t : kPvTilesALaunch);
         const unsigned most = (p.count + 7) / 8 * 8;
-        hipLaunchKernelGGL((pv_product_kernel<I8, TA, TB, T, Epi>),
-                           dim3(most < T::kWorkgroups ? most : T::kWorkgroups), dim3(T::kThreads),
-                           0, s, p, epi);
+        hipLaunchKernelGGL(kernel, dim3(most < T::kWorkgroups ? most : T::kWorkgroups),
+                           dim3(T::kThreads), 0, s, p, epi);
     }
-    const size_t results = (size_t)p.M * p.N;
-    if (p.splits > 16 || (p.splits > 1 && results < (1u << 18)))
-        hipLaunchKernelGGL((pv_join_kernel<I8, Epi>), dim3(pv_blocks(results, 64)), dim3(256), 0, s,
-                           p, epi);
-    else if (p.splits > 1)
-        hipLaunchKernelGGL((pv_join_wide_kernel<I8, Epi>), dim3(pv_blocks(results, 1024)),
-                           dim3(256), 0, s, p, epi);
 }
+template <bool I8, bool TA, bool TB, class T, class Epi>
+static void pv_run_tiles(const PvProduct& p, const Epi& epi, hipStream_t s) {
+    pv_launch_tiles<T>(pv_product_kernel<I8, TA, TB, T, Epi>, p, epi, s);
+}
+template <bool TA, bool TB, class Epi>
+static void pv_run_parts(const PvProduct& p, const Epi& epi, hipStream_t s) {
+    if (p.a.parts == 3 && p.b.parts == 3)
+        pv_launch_tiles<PvTileP>(pv_parts_kernel<TA, TB, 3, 3, Epi>, p, epi, s);
+    else if (p.a.parts == 3)
+        pv_launch_tiles<PvTileP>(pv_parts_kernel<TA, TB, 3, 1, Epi>, p, epi, s);
+    else
+        pv_launch_tiles<PvTileP>(pv_parts_kernel<TA, TB, 1, 3, Epi>, p, epi, s);
+}
+
 // SIZES: the tiles (1 << PvSize) that the plan may have chosen
-constexpr unsigned kPvAnySize = 63;
+constexpr unsigned kPvAnySize = 127;
 template <bool I8, bool TA, bool TB, unsigned SIZES = kPvAnySize, class Epi>
 static void pv_run_product(const PvProduct& p, const Epi& epi, hipStream_t s) {
     if constexpr (SIZES >> kPvL & 1)
@@ -659,6 +794,15 @@ static void pv_run_product(const PvProduct& p, const Epi& epi, hipStream_t s) {
         if (p.size == kPvN) pv_run_tiles<I8, TA, TB, PvTileN>(p, epi, s);
     if constexpr (SIZES >> kPvS & 1)
         if (p.size == kPvS) pv_run_tiles<I8, TA, TB, PvTileS>(p, epi, s);
+    if constexpr (!I8 && (SIZES >> kPvP & 1))
+        if (p.size == kPvP) pv_run_parts<TA, TB>(p, epi, s);
+    const size_t results = (size_t)p.M * p.N;
+    if (p.splits > 16 || (p.splits > 1 && results < (1u << 18)))
+        hipLaunchKernelGGL((pv_join_kernel<I8, Epi>), dim3(pv_blocks(results, 64)), dim3(256), 0, s,
+                           p, epi);
+    else if (p.splits > 1)
+        hipLaunchKernelGGL((pv_join_wide_kernel<I8, Epi>), dim3(pv_blocks(results, 1024)),
+                           dim3(256), 0, s, p, epi);
 }
 
 // ---- operands (product.hip) ------------------------------------------------
