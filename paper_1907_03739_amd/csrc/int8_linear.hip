@@ -254,12 +254,10 @@ struct LinearEpi {
 // registers where they are its matrix operand: lane (r, h) holds row r's values 16 h ..
 // of a piece. Their sums meet in LDS; one launch, no workspace. Latency: a wave's first
 // pieces are under way while the rows' scales are found.
-constexpr int kFewThreads = 512;
-template <bool XB>
-__global__ __launch_bounds__(kFewThreads) void pv_int8_few_kernel(PvRows x, int M, int K, int N,
-                                                                  const int8_t* w,
-                                                                  LinearEpi epi) {
-    constexpr int kWaves = kFewThreads / 64, kAhead = 4;
+template <bool XB, int THREADS>
+__global__ __launch_bounds__(THREADS) void pv_int8_few_kernel(PvRows x, int M, int K, int N,
+                                                              const int8_t* w, LinearEpi epi) {
+    constexpr int kWaves = THREADS / 64, kAhead = 4;
     __shared__ uint32_t tops[16];
     __shared__ int part[kWaves][256];
     const int K128 = (K + kSlice - 1) / kSlice * kSlice, pieces = (K + 63) / 64;
@@ -284,16 +282,24 @@ __global__ __launch_bounds__(kFewThreads) void pv_int8_few_kernel(PvRows x, int 
     if (threadIdx.x < 16) tops[threadIdx.x] = 0;
     __syncthreads();
     const int chunks = (K + 511) / 512;
-    for (int u = wave; u < rows * chunks; u += kWaves) {
-        const int i = u / chunks, c0 = (u - i * chunks) * 512 + lane * 8;
-        uint32_t top = 0;
-        if (c0 < K) {
-            Raw<XB> t;
-            t.load(x, m0 + i, c0, K);
-            top = t.top();
+    for (int u0 = wave; u0 < rows * chunks; u0 += kWaves * kAhead) {
+        uint32_t top[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; u++) {
+            const int at = u0 + u * kWaves, i = at / chunks, c0 = (at - i * chunks) * 512 + lane * 8;
+            top[u] = 0;
+            if (i < rows && c0 < K) {
+                Raw<XB> t;
+                t.load(x, m0 + i, c0, K);
+                top[u] = t.top();
+            }
         }
-        top = wave_reduce(top, MaxBits());
-        if (lane == 0) atomicMax(&tops[i], top);  // whole numbers: no order
+#pragma unroll
+        for (int u = 0; u < kAhead; u++) {
+            const int i = (u0 + u * kWaves) / chunks;
+            const uint32_t most = wave_reduce(top[u], MaxBits());
+            if (lane == 0 && i < rows) atomicMax(&tops[i], most);  // whole numbers: no order
+        }
     }
     __syncthreads();
     const float s = row_scale_of(tops[r]);
@@ -328,9 +334,33 @@ __global__ __launch_bounds__(kFewThreads) void pv_int8_few_kernel(PvRows x, int 
                      activate(v, epi.neg, epi.relu));
     }
 }
-// as long as each of its workgroups has a CU to itself
-constexpr int kFewTiles = 256;
-bool few(int M, int N) { return (size_t)((M + 15) / 16) * ((N + 15) / 16) <= kFewTiles; }
+// Up to two of its workgroups a CU, unless each has many rows of many channels to find the
+// largest of (few / apart, us: 64 x 64 -> 64 5.6 / 8.6; 512 x 323 -> 256, 512 workgroups,
+// 9.1 / 9.4 and a launch; 2048 x 323 -> 128, 1024 of them, 16.7 / 9.7; 64 x 4928 -> 64
+// 15.7 / 10.8).
+constexpr int kFewTiles = 512, kFewChannels = 2560;
+bool few(int M, int K, int N) {
+    return (size_t)((M + 15) / 16) * ((N + 15) / 16) <= kFewTiles && (K <= kFewChannels || M <= 4);
+}
+
+void run_few(const PvRows& x, int M, int K, int N, const int8_t* weight, const LinearEpi& epi,
+             hipStream_t s) {
+    const unsigned tiles = (unsigned)((M + 15) / 16 * ((N + 15) / 16));
+    auto run = [&](auto kernel, int threads) {
+        hipLaunchKernelGGL(kernel, dim3(tiles), dim3(threads), 0, s, x, M, K, N, weight, epi);
+    };
+    if (K > 1024 && tiles <= 256) {  // one workgroup a CU: more waves to share the pieces
+        if (x.bf16)
+            run(pv_int8_few_kernel<true, 1024>, 1024);
+        else
+            run(pv_int8_few_kernel<false, 1024>, 1024);
+    } else {
+        if (x.bf16)
+            run(pv_int8_few_kernel<true, 512>, 512);
+        else
+            run(pv_int8_few_kernel<false, 512>, 512);
+    }
+}
 
 PvProduct product_of(const int8_t* q, const Layout& rows, int M, int K, const int8_t* w, int N) {
     PvProduct p{};
@@ -448,7 +478,7 @@ pvconv_status pv_launch_int8_quantize(const PvRows& x, int M, int K, int8_t* q, 
 }
 
 size_t pv_int8_linear_ws_bytes(int M, int K, int N, bool rows_given) {
-    if (!rows_given && few(M, N)) return 0;
+    if (!rows_given && few(M, K, N)) return 0;
     return carve_linear(nullptr, M, K, N, rows_given).total;
 }
 
@@ -458,6 +488,7 @@ static pvconv_status run_rows(const int8_t* q, const Layout& rows, int M, int K,
     PvProduct p = product_of(q, rows, M, K, weight, N);
     p.partial = partial;
     pv_run_product<true, false, false>(p, epi, s);
+    pv_run_join<true>(p, epi, s);
     return pv_launch_status();
 }
 
@@ -472,14 +503,8 @@ pvconv_status pv_launch_int8_linear(const PvRows& x, int M, int K, int N, const 
                                     const PvRows& y, int8_t* rows, float* row_scale, void* ws,
                                     hipStream_t s) {
     LinearEpi epi = epi_of(row_scale, scale, bias, act, slope, y);
-    if (!rows && few(M, N)) {
-        const dim3 grid((unsigned)((M + 15) / 16 * ((N + 15) / 16)));
-        if (x.bf16)
-            hipLaunchKernelGGL((pv_int8_few_kernel<true>), grid, dim3(kFewThreads), 0, s, x, M, K,
-                               N, weight, epi);
-        else
-            hipLaunchKernelGGL((pv_int8_few_kernel<false>), grid, dim3(kFewThreads), 0, s, x, M, K,
-                               N, weight, epi);
+    if (!rows && few(M, K, N)) {
+        run_few(x, M, K, N, weight, epi, s);
         return pv_launch_status();
     }
     const LinearWs w = carve_linear(ws, M, K, N, rows != nullptr);
@@ -545,8 +570,10 @@ pvconv_status pv_launch_int8_linear_bwd(const PvRows& dy, const int8_t* rows,
     const int runs = pv_sum_runs(M);
     if (dbias && M > 0) packs.add(pv_sums_of(dy, M, N, runs == 1 ? dbias : w.sums));
     pv_launch_packs(packs, s);
-    if (want_dx) pv_launch_plain(w.dx, false, PvPlain{dx, nullptr}, s);
-    if (dw) pv_launch_plain(w.dw, true, PvPlain{PvRows{dw, false, K}, nullptr}, s);
-    if (dbias && runs != 1) pv_launch_sum_runs(w.sums, runs, N, dbias, s);
+    const PvSums none{nullptr, 0, 0, nullptr},
+        sums{w.sums, runs, N, dbias && runs != 1 ? dbias : nullptr};
+    if (want_dx) pv_launch_plain(w.dx, false, PvPlain{dx, nullptr}, dw ? none : sums, s);
+    if (dw) pv_launch_plain(w.dw, true, PvPlain{PvRows{dw, false, K}, nullptr}, sums, s);
+    if (!want_dx && !dw) pv_launch_sum_runs(sums, s);
     return pv_launch_status();
 }

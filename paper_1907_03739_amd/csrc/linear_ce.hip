@@ -476,11 +476,14 @@ pvconv_status pv_launch_linear_ce(const PvLinearCe& a, bool forward, void* ws, h
         const size_t pitch = pv_up(n, 64) * 2;
         c.dz = DzPanel{(uint8_t*)p.dz.p, pitch, p.dz.part_bytes, p.dz.parts, p.dz.rows};
         const PvProduct z = logits(v0, n, p.grad_sizes);
+        const PvSums none{nullptr, 0, 0, nullptr},
+            sums{p.sums, row_blocks(a.M, z.size), n, a.dbias ? a.dbias + v0 : nullptr};
+        const bool dx = a.dx.p && a.M > 0;
         if (p.whole && forward)
             run_logits<kWhole>(z, c, p.parts, s);
         else
             run_logits<kGrad>(z, c, p.parts, s);
-        if (a.dx.p && a.M > 0) {
+        if (dx) {
             PvProduct q = p.dx;
             q.a.pitch = pitch;
             q.b.p += (size_t)v0 * q.b.pitch;
@@ -490,7 +493,7 @@ pvconv_status pv_launch_linear_ce(const PvLinearCe& a, bool forward, void* ws, h
             q.partial = p.partial;
             const bool last = v0 + n == a.V;
             pv_launch_plain(q, false, PvPlain{last ? a.dx : PvRows{p.acc, false, a.K},
-                                              v0 ? p.acc : nullptr}, s);
+                                              v0 ? p.acc : nullptr}, a.dw.p ? none : sums, s);
         }
         if (a.dw.p) {
             PvProduct q = p.dw;
@@ -500,9 +503,9 @@ pvconv_status pv_launch_linear_ce(const PvLinearCe& a, bool forward, void* ws, h
             q.partial = p.partial;
             const size_t es = a.dw.bf16 ? 2 : 4;
             pv_launch_plain(q, true, PvPlain{PvRows{(char*)a.dw.p + (size_t)v0 * a.dw.ld * es,
-                                                    a.dw.bf16, a.dw.ld}, nullptr}, s);
+                                                    a.dw.bf16, a.dw.ld}, nullptr}, sums, s);
         }
-        if (a.dbias) pv_launch_sum_runs(p.sums, row_blocks(a.M, z.size), n, a.dbias + v0, s);
+        if (!dx && !a.dw.p) pv_launch_sum_runs(sums, s);
     }
     return pv_launch_status();
 }

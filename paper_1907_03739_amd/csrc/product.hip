@@ -192,41 +192,51 @@ struct PlainEpi {
 };
 
 // A wave a column: 64 runs at a time in 64 bits, in a fixed order, eight loads in flight.
-__global__ __launch_bounds__(kThreads) void pv_sum_runs_kernel(const float* runs, int n, int N,
-                                                               float* out) {
-    const int c = (int)blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-    if (c >= N) return;
+__device__ __forceinline__ void sum_runs(const PvSums& k, unsigned block) {
+    const int c = (int)block * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+    if (c >= k.N) return;
     double s = 0.;
-    for (int i0 = 0; i0 < n; i0 += 512) {
+    for (int i0 = 0; i0 < k.n; i0 += 512) {
         float v[8];
 #pragma unroll
         for (int u = 0; u < 8; u++)
-            v[u] = runs[(size_t)min(i0 + 64 * u + lane, n - 1) * N + c];
+            v[u] = k.runs[(size_t)min(i0 + 64 * u + lane, k.n - 1) * k.N + c];
 #pragma unroll
         for (int u = 0; u < 8; u++)
-            if (i0 + 64 * u + lane < n) s += (double)v[u];
+            if (i0 + 64 * u + lane < k.n) s += (double)v[u];
     }
 #pragma unroll
     for (int w = 1; w < 64; w <<= 1) s += __shfl_xor(s, w);
-    if (lane == 0) out[c] = (float)s;
+    if (lane == 0) k.out[c] = (float)s;
+}
+__global__ __launch_bounds__(kThreads) void pv_sum_runs_kernel(PvSums k) {
+    sum_runs(k, blockIdx.x);
+}
+// a product's splits and column sums
+__global__ __launch_bounds__(kThreads) void pv_finish_kernel(PvProduct p, PlainEpi epi, PvSums k,
+                                                             unsigned sums) {
+    if (blockIdx.x < sums)
+        sum_runs(k, blockIdx.x);
+    else
+        pv_join<false>(p, epi, blockIdx.x - sums, gridDim.x - sums);
 }
 
 // The same, a thread a column: many columns, whose neighbours lie side by side.
-__global__ __launch_bounds__(kThreads) void pv_sum_runs_wide_kernel(const float* runs, int n,
-                                                                    int N, float* out) {
+__global__ __launch_bounds__(kThreads) void pv_sum_runs_wide_kernel(PvSums k) {
     const int c = (int)blockIdx.x * kThreads + threadIdx.x;
-    if (c >= N) return;
+    if (c >= k.N) return;
     double s = 0.;
-    for (int i0 = 0; i0 < n; i0 += 8) {
+    for (int i0 = 0; i0 < k.n; i0 += 8) {
         float v[8];
 #pragma unroll
-        for (int u = 0; u < 8; u++) v[u] = runs[(size_t)min(i0 + u, n - 1) * N + c];
+        for (int u = 0; u < 8; u++) v[u] = k.runs[(size_t)min(i0 + u, k.n - 1) * k.N + c];
 #pragma unroll
         for (int u = 0; u < 8; u++)
-            if (i0 + u < n) s += (double)v[u];
+            if (i0 + u < k.n) s += (double)v[u];
     }
-    out[c] = (float)s;
+    k.out[c] = (float)s;
 }
+constexpr int kWideSums = 4096;  // columns
 
 }  // namespace
 
@@ -242,19 +252,28 @@ void pv_launch_packs(PvPacks& k, hipStream_t s) {
         hipLaunchKernelGGL(pv_packs_kernel, dim3(k.begin[k.n]), dim3(kThreads), 0, s, k);
 }
 
-void pv_launch_sum_runs(const float* runs, int n, int N, float* out, hipStream_t s) {
-    if (N >= 4096)
-        hipLaunchKernelGGL(pv_sum_runs_wide_kernel, dim3((N + kThreads - 1) / kThreads),
-                           dim3(kThreads), 0, s, runs, n, N, out);
+void pv_launch_sum_runs(const PvSums& k, hipStream_t s) {
+    if (!k.out) return;
+    if (k.N >= kWideSums)
+        hipLaunchKernelGGL(pv_sum_runs_wide_kernel, dim3((k.N + kThreads - 1) / kThreads),
+                           dim3(kThreads), 0, s, k);
     else
-        hipLaunchKernelGGL(pv_sum_runs_kernel, dim3((N + 3) / 4), dim3(kThreads), 0, s, runs, n, N,
-                           out);
+        hipLaunchKernelGGL(pv_sum_runs_kernel, dim3((k.N + 3) / 4), dim3(kThreads), 0, s, k);
 }
 
-void pv_launch_plain(const PvProduct& p, bool a_across, const PvPlain& e, hipStream_t s) {
+void pv_launch_plain(const PvProduct& p, bool a_across, const PvPlain& e, const PvSums& sums,
+                     hipStream_t s) {
     const PlainEpi epi{e, p.N};
     if (a_across)
         pv_run_product<false, true, true>(p, epi, s);
     else
         pv_run_product<false, false, true>(p, epi, s);
+    if (sums.out && sums.N < kWideSums && p.splits > 1 && pv_join_narrow(p)) {
+        const unsigned blocks = (unsigned)(sums.N + 3) / 4;
+        hipLaunchKernelGGL(pv_finish_kernel, dim3(blocks + pv_blocks((size_t)p.M * p.N, 64)),
+                           dim3(kThreads), 0, s, p, epi, sums, blocks);
+        return;
+    }
+    pv_run_join<false>(p, epi, s);
+    pv_launch_sum_runs(sums, s);
 }

@@ -653,7 +653,7 @@ static inline void pv_plan(PvProduct& p, bool may_split, unsigned sizes = 127) {
             const int splits = per ? (all + per - 1) / per : 1;
             const size_t rounds = (tiles * splits + c.slots - 1) / c.slots;
             float us = (float)rounds * ((float)per * c.slice + c.rest);
-            if (splits > 1) us += 3.f + (float)splits * (float)p.M * (float)p.N * (8.f / 4e6f);
+            if (splits > 1) us += 4.f + (float)splits * (float)p.M * (float)p.N * (8.f / 4e6f);
             if (best == 0.f || us < best) {
                 best = us;
                 p.size = c.size;
@@ -666,7 +666,7 @@ static inline void pv_plan(PvProduct& p, bool may_split, unsigned sizes = 127) {
         if (sizes >> c.size & 1) choose(c);
     if ((sizes >> kPvP & 1) && pv_all_parts(p.a.parts, p.b.parts) && p.pairs > 1)
         choose(PvSizeCost{kPvP, PvTileP::TM, PvTileP::TN, PvTileP::kWorkgroups,
-                          0.07f + 0.25f / p.pairs, 3.f});
+                          0.1f + 0.6f / p.pairs, 3.f});
 }
 static inline size_t pv_partial_bytes(const PvProduct& p) {
     return p.splits > 1 ? (size_t)p.splits * p.M * p.N * 4 : 0;
@@ -676,14 +676,15 @@ static inline size_t pv_partial_bytes(const PvProduct& p) {
 // four waves take a quarter of the splits each, eight loads in flight. (50 x 128 results of
 // 103 splits, one thread a result: 15.8 us.)
 template <bool I8, class Epi>
-__global__ __launch_bounds__(256) void pv_join_kernel(PvProduct p, Epi epi) {
+__device__ __forceinline__ void pv_join(const PvProduct& p, const Epi& epi, size_t block,
+                                        size_t blocks) {
     constexpr int kAhead = 8;
     typedef typename std::conditional<I8, int, float>::type Sum;
     __shared__ Sum part[4][64];
     const size_t total = (size_t)p.M * p.N;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, quarter = (p.splits + 3) / 4;
     const int k0 = wave * quarter, k1 = min(k0 + quarter, p.splits);
-    for (size_t at0 = (size_t)blockIdx.x * 64; at0 < total; at0 += (size_t)gridDim.x * 64) {
+    for (size_t at0 = block * 64; at0 < total; at0 += blocks * 64) {
         const size_t at = min(at0 + lane, total - 1);
         Sum s = 0;
         for (int k = k0; k < k1; k += kAhead) {
@@ -708,6 +709,13 @@ __global__ __launch_bounds__(256) void pv_join_kernel(PvProduct p, Epi epi) {
         }
         __syncthreads();
     }
+}
+template <bool I8, class Epi>
+__global__ __launch_bounds__(256) void pv_join_kernel(PvProduct p, Epi epi) {
+    pv_join<I8>(p, epi, blockIdx.x, gridDim.x);
+}
+static inline bool pv_join_narrow(const PvProduct& p) {
+    return p.splits > 16 || (size_t)p.M * p.N < (1u << 18);
 }
 // The same where there are many results of few splits: four neighbours a thread.
 template <bool I8, class Epi>
@@ -796,11 +804,16 @@ static void pv_run_product(const PvProduct& p, const Epi& epi, hipStream_t s) {
         if (p.size == kPvS) pv_run_tiles<I8, TA, TB, PvTileS>(p, epi, s);
     if constexpr (!I8 && (SIZES >> kPvP & 1))
         if (p.size == kPvP) pv_run_parts<TA, TB>(p, epi, s);
+}
+// The splits' sums of a product that has some.
+template <bool I8, class Epi>
+static void pv_run_join(const PvProduct& p, const Epi& epi, hipStream_t s) {
+    if (p.splits <= 1) return;
     const size_t results = (size_t)p.M * p.N;
-    if (p.splits > 16 || (p.splits > 1 && results < (1u << 18)))
+    if (pv_join_narrow(p))
         hipLaunchKernelGGL((pv_join_kernel<I8, Epi>), dim3(pv_blocks(results, 64)), dim3(256), 0, s,
                            p, epi);
-    else if (p.splits > 1)
+    else
         hipLaunchKernelGGL((pv_join_wide_kernel<I8, Epi>), dim3(pv_blocks(results, 1024)),
                            dim3(256), 0, s, p, epi);
 }
@@ -822,7 +835,7 @@ struct PvPack {
                              // over runs of `rows` rows, [runs][C]
 };
 // rows of a run, and how many there are (one: the sums are whole)
-static inline int pv_sum_rows(int M) { return M <= 512 ? 512 : 256; }
+static inline int pv_sum_rows(int M) { return M <= 1024 ? 1024 : 256; }
 static inline int pv_sum_runs(int M) { return (M + pv_sum_rows(M) - 1) / pv_sum_rows(M); }
 // Up to five at once.
 struct PvPacks {
@@ -832,16 +845,24 @@ struct PvPacks {
     void add(const PvPack& k) { job[n++] = k; }
 };
 void pv_launch_packs(PvPacks& k, hipStream_t s);
-// Sums [runs][N] joined in a fixed order.
-void pv_launch_sum_runs(const float* runs, int n, int N, float* out, hipStream_t s);
-
 // out (+)= the product of bf16 parts: out = sum + add (dense [M][N] fp32, or NULL); a along
 // k or across it, b across it
 struct PvPlain {
     PvRows out;
     const float* add;
 };
-void pv_launch_plain(const PvProduct& p, bool a_across, const PvPlain& e, hipStream_t s);
+// `sums`: column sums to be joined too, in the launch that joins the splits' sums if there
+// is one.
+struct PvSums {
+    const float* runs;
+    int n, N;
+    float* out;  // or NULL: none
+};
+void pv_launch_plain(const PvProduct& p, bool a_across, const PvPlain& e, const PvSums& sums,
+                     hipStream_t s);
+
+// Sums [n][N] of runs joined in a fixed order.
+void pv_launch_sum_runs(const PvSums& sums, hipStream_t s);
 
 // Pieces of a workspace, one behind another.
 struct PvCarve {
