@@ -65,7 +65,11 @@ static inline void pv_pairs(PvProduct& p, int parts_a, int parts_b) {
 }
 
 // Tiles: WM x WN waves of 16 MI rows by 64 columns each; ST stages of slices in LDS, ST -
-// 1 of them under way while one is multiplied.
+// 1 of them under way while one is multiplied. What a slice takes, beside what the matrix
+// cores need for it, is the way of 32 to 64 KB from the L2 into LDS and a barrier: the more
+// products a byte feeds, the nearer to their rate (bf16, us: 8192 x 5003 -> 2048 129 in
+// tiles of 256 x 256, 1.3 PFLOP/s, 152, 221, 293 and 358 in the smaller ones); few tiles
+// need the small ones to fill the chip (1024 x 1024 x 1024: 27, 17, 13, 9.6, 9.6).
 template <int WM_, int WN_, int MI_, int ST_, int PER_CU_>
 struct PvTile {
     static constexpr int WM = WM_, WN = WN_, MI = MI_, ST = ST_;
@@ -75,11 +79,10 @@ struct PvTile {
 typedef PvTile<2, 4, 8, 2, 1> PvTileL;  // 256 x 256
 typedef PvTile<4, 2, 4, 3, 1> PvTileG;  // 256 x 128
 typedef PvTile<2, 2, 4, 4, 1> PvTileM;  // 128 x 128
-typedef PvTile<2, 2, 4, 2, 2> PvTileD;  // 128 x 128, two workgroups a CU
 typedef PvTile<4, 1, 2, 4, 1> PvTileN;  // 128 x 64
 typedef PvTile<2, 1, 2, 4, 2> PvTileS;  // 64 x 64
 typedef PvTile<4, 1, 1, 2, 1> PvTileP;  // 64 x 64, all parts of a slice in a stage
-enum PvSize { kPvS, kPvN, kPvM, kPvG, kPvL, kPvD, kPvP };
+enum PvSize { kPvS, kPvN, kPvM, kPvG, kPvL, kPvP };
 
 // The tile of index idx: eight tiles of rows by the columns in turn, so that an XCD,
 // which works on neighbours at a time, has both operands in its L2.
@@ -622,7 +625,12 @@ static inline size_t pv_tiles_of(int M, int N, int tm, int tn) {
 }
 // The tiles that a product takes and how many ways its slices are split, by the time that
 // each choice is expected to take: rounds of workgroups, each its slices and an epilogue,
-// and the splits' sums written, read and joined.
+// and the splits' sums written, read and joined. The times a slice and the rest are those
+// of unsplit products of 35 sizes, each timed in every size of tile and up to twelve
+// splits; the choice took at most 1.25 times the best one there, 1.03 in the median. (512 x 2304 by 32768 deep,
+// us: 256 x 128 in seven 85, 256 x 256 in twelve 90, unsplit 242 to 724; 4096 x 512 by
+// 49999: 256 x 256 in eight 202, unsplit 404 to 1230; 8192 x 5003 -> 2048: unsplit 129, in
+// two 212.)
 struct PvSizeCost {
     int size, tm, tn, slots;
     float slice, rest;  // us
@@ -631,7 +639,6 @@ static constexpr PvSizeCost kPvCosts[] = {
     {kPvL, PvTileL::TM, PvTileL::TN, PvTileL::kWorkgroups, 1.4f, 6.f},
     {kPvG, PvTileG::TM, PvTileG::TN, PvTileG::kWorkgroups, 0.82f, 4.5f},
     {kPvM, PvTileM::TM, PvTileM::TN, PvTileM::kWorkgroups, 0.62f, 3.5f},
-    {kPvD, PvTileD::TM, PvTileD::TN, PvTileD::kWorkgroups, 1.15f, 5.f},
     {kPvN, PvTileN::TM, PvTileN::TN, PvTileN::kWorkgroups, 0.43f, 3.f},
     {kPvS, PvTileS::TM, PvTileS::TN, PvTileS::kWorkgroups, 0.42f, 3.f},
 };
@@ -639,7 +646,7 @@ static constexpr PvSizeCost kPvCosts[] = {
 static constexpr bool pv_all_parts(int a, int b) {
     return (a == 3 && (b == 3 || b == 1)) || (a == 1 && b == 3);
 }
-static inline void pv_plan(PvProduct& p, bool may_split, unsigned sizes = 127) {
+static inline void pv_plan(PvProduct& p, bool may_split, unsigned sizes = 63) {
     const int all = p.slices * p.pairs;
     float best = 0.f;
     auto choose = [&](const PvSizeCost& c) {
@@ -666,7 +673,7 @@ static inline void pv_plan(PvProduct& p, bool may_split, unsigned sizes = 127) {
         if (sizes >> c.size & 1) choose(c);
     if ((sizes >> kPvP & 1) && pv_all_parts(p.a.parts, p.b.parts) && p.pairs > 1)
         choose(PvSizeCost{kPvP, PvTileP::TM, PvTileP::TN, PvTileP::kWorkgroups,
-                          0.1f + 0.6f / p.pairs, 3.f});
+                          p.pairs > 3 ? 0.18f : 0.22f, 3.f});
 }
 static inline size_t pv_partial_bytes(const PvProduct& p) {
     return p.splits > 1 ? (size_t)p.splits * p.M * p.N * 4 : 0;
@@ -787,7 +794,7 @@ static void pv_run_parts(const PvProduct& p, const Epi& epi, hipStream_t s) {
 }
 
 // SIZES: the tiles (1 << PvSize) that the plan may have chosen
-constexpr unsigned kPvAnySize = 127;
+constexpr unsigned kPvAnySize = 63;
 template <bool I8, bool TA, bool TB, unsigned SIZES = kPvAnySize, class Epi>
 static void pv_run_product(const PvProduct& p, const Epi& epi, hipStream_t s) {
     if constexpr (SIZES >> kPvL & 1)
@@ -796,8 +803,6 @@ static void pv_run_product(const PvProduct& p, const Epi& epi, hipStream_t s) {
         if (p.size == kPvG) pv_run_tiles<I8, TA, TB, PvTileG>(p, epi, s);
     if constexpr (SIZES >> kPvM & 1)
         if (p.size == kPvM) pv_run_tiles<I8, TA, TB, PvTileM>(p, epi, s);
-    if constexpr (SIZES >> kPvD & 1)
-        if (p.size == kPvD) pv_run_tiles<I8, TA, TB, PvTileD>(p, epi, s);
     if constexpr (SIZES >> kPvN & 1)
         if (p.size == kPvN) pv_run_tiles<I8, TA, TB, PvTileN>(p, epi, s);
     if constexpr (SIZES >> kPvS & 1)
