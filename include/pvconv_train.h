@@ -184,9 +184,9 @@ pvconv_status pvconv_int8_linear_rows(const int8_t* rows, const float* row_scale
 /* scale weight, from the kept rows:                                         */
 /*   dx[m,k] = sum_n dy[m,n] scale_n weight[n,k]                             */
 /*   dw[n,k] = sum_m dy[m,n] row_scale_m rows[m,k],  dbias_n = sum_m dy[m,n] */
-/* An fp32 output has fp32 sums of products good to 24 bits; for a bf16 dx of */
-/* more than 256 rows, one factor (scale_n weight of a bf16 dy, dy scale_n of */
-/* an fp32 one) is rounded to bf16 first (of fewer: to 16 bits).             */
+/* An fp32 output has fp32 sums of products good to 24 bits; for a bf16 dx,  */
+/* one factor (scale_n weight of a bf16 dy, dy scale_n of an fp32 one) is    */
+/* rounded to bf16 first, of up to 256 rows or 2^16 values of it to 16 bits. */
 /*  dy [M][N] (dy_dt), dy_ld; dx out [M][K] (dx_dt), dx_ld, or NULL (weight, */
 /*  scale then unused); dw out [N][K] fp32 or NULL (rows, row_scale then     */
 /*  unused); dbias out [N] fp32 or NULL                                      */
@@ -262,8 +262,8 @@ pvconv_status pvconv_distill_topk_backward(const void* z, pvconv_dtype z_dt, int
 /* weight 0 has dz = 0; x and W should be finite all the same, as dz         */
 /* multiplies them.                                                          */
 /* fp32 operands are multiplied to 24 bits, bf16 ones exactly, sums are fp32. */
-/* For a bf16 dx (dw) of more than 256 rows, dz is rounded to bf16 first; of */
-/* fewer, and the other factor always, to 16 bits. For an fp32 one, dz is    */
+/* For a bf16 dx (dw), dz is rounded to bf16 first; of up to 256 rows or 64   */
+/* classes, and the other factor always, to 16 bits. For an fp32 one, dz is  */
 /* taken to 24 bits.                                                         */
 /*  x       [M][K] (x_dt), row stride x_ld;  w [V][K] (w_dt), row stride w_ld */
 /*  bias    [V] fp32 or NULL;  labels [M] int32;  row_weight [M] fp32 or     */

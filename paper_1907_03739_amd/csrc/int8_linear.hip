@@ -268,8 +268,10 @@ struct LinearEpi {
 // pieces are under way while the rows' scales are found.
 template <bool XB, int THREADS>
 __global__ __launch_bounds__(THREADS) void pv_int8_few_kernel(PvRows x, int M, int K, int N,
-                                                              const int8_t* w, LinearEpi epi) {
-    constexpr int kWaves = THREADS / 64, kAhead = 4;
+                                                              const int8_t* w, LinearEpi epi,
+                                                              int8_t* keep, float* keep_scale) {
+    // pieces under way: as many as registers hold
+    constexpr int kWaves = THREADS / 64, kAhead = XB || THREADS < 1024 ? 4 : 3;
     __shared__ uint32_t tops[16];
     __shared__ int part[kWaves][256];
     const int K128 = (K + kSlice - 1) / kSlice * kSlice, pieces = (K + 63) / 64;
@@ -317,6 +319,12 @@ __global__ __launch_bounds__(THREADS) void pv_int8_few_kernel(PvRows x, int M, i
     const float s = row_scale_of(tops[r]);
     const bool finite = s == s;
     const float inv = 1.f / s, half = 0.5f * s;
+    // the first workgroup of a row of tiles keeps its rows, if they are wanted
+    int8_t* kept = keep && n0 == 0 && r < rows ? keep + row * K128 + h * 16 : nullptr;
+    if (kept && wave == 0) {
+        if (h == 0) keep_scale[row] = s;
+        if (pieces * 64 < K128) *(pv_i32x4*)(kept + pieces * 64) = pv_i32x4{0, 0, 0, 0};
+    }
     pv_i32x4 acc = {0, 0, 0, 0};
     for (int k = wave; k < pieces; k += kWaves * kAhead) {
         if (k != wave) load(k);
@@ -328,6 +336,7 @@ __global__ __launch_bounds__(THREADS) void pv_int8_few_kernel(PvRows x, int M, i
                 const uint2 a = v[u][0].bytes(s, inv, half), b = v[u][1].bytes(s, inv, half);
                 fx = pv_i32x4{(int)a.x, (int)a.y, (int)b.x, (int)b.y};
             }
+            if (kept) *(pv_i32x4*)(kept + (k + u * kWaves) * 64) = fx;
             acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw[u], fx, acc, 0, 0, 0);
         }
     }
@@ -356,10 +365,11 @@ bool few(int M, int K, int N) {
 }
 
 void run_few(const PvRows& x, int M, int K, int N, const int8_t* weight, const LinearEpi& epi,
-             hipStream_t s) {
+             int8_t* rows, float* row_scale, hipStream_t s) {
     const unsigned tiles = (unsigned)((M + 15) / 16 * ((N + 15) / 16));
     auto run = [&](auto kernel, int threads) {
-        hipLaunchKernelGGL(kernel, dim3(tiles), dim3(threads), 0, s, x, M, K, N, weight, epi);
+        hipLaunchKernelGGL(kernel, dim3(tiles), dim3(threads), 0, s, x, M, K, N, weight, epi,
+                           rows, row_scale);
     };
     if (K > 1024 && tiles <= 256) {  // one workgroup a CU: more waves to share the pieces
         if (x.bf16)
@@ -404,12 +414,14 @@ LinearWs carve_linear(void* base, int M, int K, int N, bool rows_given) {
     return w;
 }
 
-// Parts of a gradient's scaled operand: for a bf16 result one rounded part, of few rows
-// (which would not average it) two. For an fp32 one, the two that hold 8 by 8 bits where
-// dy is bf16, else three.
+// Parts of dx's scaled operand (the weight of a bf16 dy, else dy): for a bf16 result one
+// rounded part, or two where few values would not average what the rounding leaves. For
+// an fp32 one, the two that hold 8 by 8 bits where dy is bf16, else three.
 constexpr int kFewRows = 256;
-int parts_of(bool out_bf16, bool dy_bf16, int M) {
-    if (out_bf16) return M <= kFewRows ? 2 : 1;
+constexpr size_t kFewValues = 1 << 16;
+int parts_of(bool out_bf16, bool dy_bf16, int M, int K, int N) {
+    if (out_bf16)
+        return M <= kFewRows || (size_t)N * (dy_bf16 ? K : M) <= kFewValues ? 2 : 1;
     return dy_bf16 ? 2 : 3;
 }
 
@@ -438,14 +450,14 @@ BwdWs carve_bwd(void* base, const PvRows& dy, int M, int K, int N, bool dx_bf16,
         p.partial = (uint32_t*)c.take(pv_partial_bytes(p));
     };
     if (want_dx && M > 0) {
-        const int parts = parts_of(dx_bf16, dy.bf16, M);
+        const int parts = parts_of(dx_bf16, dy.bf16, M, K, N);
         w.pack_dy = !(may_direct && pv_in_place(dy, N));
         w.dys = w.pack_dy ? pv_take_panel(c, M, N, dy.bf16 ? 1 : parts) : pv_panel_of(dy, M);
         w.w = pv_take_panel(c, N, K, dy.bf16 ? parts : 1);
         product(w.dx, w.dys, w.w, M, K, N);
     }
     if (want_dw) {  // both operands across k: dy's rows are padded with zeros
-        w.dym = pv_take_panel(c, (int)pv_up(M, kDeep), N, parts_of(false, dy.bf16, M));
+        w.dym = pv_take_panel(c, (int)pv_up(M, kDeep), N, dy.bf16 ? 2 : 3);
         w.q = pv_take_panel(c, M, K, 1);
         product(w.dw, w.dym, w.q, N, K, M);
     }
@@ -515,8 +527,8 @@ pvconv_status pv_launch_int8_linear(const PvRows& x, int M, int K, int N, const 
                                     const PvRows& y, int8_t* rows, float* row_scale, void* ws,
                                     hipStream_t s) {
     LinearEpi epi = epi_of(row_scale, scale, bias, act, slope, y);
-    if (!rows && few(M, K, N)) {
-        run_few(x, M, K, N, weight, epi, s);
+    if (few(M, K, N)) {
+        run_few(x, M, K, N, weight, epi, rows, row_scale, s);
         return pv_launch_status();
     }
     const LinearWs w = carve_linear(ws, M, K, N, rows != nullptr);

@@ -255,10 +255,13 @@ constexpr size_t kStatsBytes = (size_t)1 << 26;
 
 int parts_of(bool bf16) { return bf16 ? 1 : 3; }
 // Parts of dz for a gradient: 24 bits for an fp32 one; one rounding for a bf16 one, two
-// parts where few rows would not average it (a row's dz at its label scales its whole
-// gradient). The other factor of a bf16 gradient is rounded to 16 bits.
+// parts where few rows or classes would not average it (a row's dz at its label scales its
+// whole gradient; of few classes, whose dz add up to 0, the gradient is a difference). The
+// other factor of a bf16 gradient is rounded to 16 bits.
 constexpr int kFewRows = 256;
-int dz_parts_of(bool bf16, int M) { return !bf16 ? 3 : M <= kFewRows ? 2 : 1; }
+int dz_parts_of(bool bf16, int M, int V) {
+    return !bf16 ? 3 : M <= kFewRows || V <= kWholeClasses ? 2 : 1;
+}
 int factor_parts_of(bool out_bf16, bool bf16) { return bf16 ? 1 : out_bf16 ? 2 : 3; }
 
 struct Plan {
@@ -343,7 +346,8 @@ Plan carve(void* base, const PvLinearCe& a, bool forward, bool grads, bool may_d
         return p;
     }
     const bool want_dx = a.dx.p != nullptr, want_dw = a.dw.p != nullptr;
-    const int px = dz_parts_of(a.dx.bf16, a.M), pw = dz_parts_of(a.dw.bf16, a.M);
+    const int px = dz_parts_of(a.dx.bf16, a.M, a.V),
+              pw = dz_parts_of(a.dw.bf16, a.M, a.V);
     // (of both, wanted or not: the workspace of fewer gradients is then no larger)
     const size_t per = pv_up(a.M > 0 ? a.M : 1, 64) * 2 * (px > pw ? px : pw);
     size_t n = kPieceBytes / per / 256 * 256;

@@ -49,12 +49,13 @@ struct PvProduct {
 };
 
 // The pairs of parts of two operands that a product needs: to 24 bits, or to 16 where
-// neither has three parts.
+// neither has three parts. The smallest products come first, the first parts' last: their
+// sum alone is rounded at its size.
 static inline void pv_pairs(PvProduct& p, int parts_a, int parts_b) {
     p.pairs = 0;
     p.pa = p.pb = 0;
     const int orders = parts_a < 3 && parts_b < 3 ? 2 : 3;
-    for (int order = 0; order < orders; order++)
+    for (int order = orders - 1; order >= 0; order--)
         for (int i = 0; i <= order; i++) {
             const int j = order - i;
             if (i >= parts_a || j >= parts_b) continue;
@@ -508,9 +509,10 @@ __global__ __launch_bounds__(PvTileP::kThreads, 1) void pv_parts_kernel(PvProduc
     enter();
     if (k < k1) fetch(k, la0, lb0);
     for (;;) {
-        pv_f32x4 acc[4][MI];
+        // the sums of first parts, and of the others, whose digits would be lost in them
+        pv_f32x4 acc[4][MI], rest[4];
 #pragma unroll
-        for (int j = 0; j < 4; j++) acc[j][0] = pv_f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int j = 0; j < 4; j++) acc[j][0] = rest[j] = pv_f32x4{0.f, 0.f, 0.f, 0.f};
         constexpr int kOrders = PA < 3 && PB < 3 ? 2 : 3;  // as pv_pairs
         auto one = [&](const uint8_t* la, const uint8_t* lb, uint8_t* na, uint8_t* nb) {
             if (k >= k1) return;
@@ -530,8 +532,8 @@ __global__ __launch_bounds__(PvTileP::kThreads, 1) void pv_parts_kernel(PvProduc
                                 pv_b16x8 va, vb;
                                 __builtin_memcpy(&va, &fa[x], 16);
                                 __builtin_memcpy(&vb, &fb[y][j], 16);
-                                acc[j][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                                    vb, va, acc[j][0], 0, 0, 0);
+                                pv_f32x4& to = x + y == 0 ? acc[j][0] : rest[j];
+                                to = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vb, va, to, 0, 0, 0);
                             });
                     });
                 });
@@ -542,6 +544,8 @@ __global__ __launch_bounds__(PvTileP::kThreads, 1) void pv_parts_kernel(PvProduc
             one(la0, lb0, la1, lb1);
             one(la1, lb1, la0, lb0);
         }
+#pragma unroll
+        for (int j = 0; j < 4; j++) acc[j][0] += rest[j];
         const int em = m0 + wm, en = n0, es = split;
         idx += step;
         const bool more = idx < end;

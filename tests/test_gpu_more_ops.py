@@ -169,3 +169,46 @@ def test_a_long_run_of_rows_past_32_bits():
     b = pv.pvconv_linear_cross_entropy(dense, w, label, want_grad=True)
     for p, q in zip(a, b):
         assert torch.equal(p, q)
+
+
+@pytest.mark.parametrize("M,K,N", [(1, 9, 3), (65, 130, 64), (257, 64, 65), (700, 300, 2100),
+                                   (3000, 70, 50), (64, 2000, 9000), (9000, 128, 300)])
+def test_the_workspace_that_is_asked_for_is_all_that_is_used(M, K, N):
+    guard = 1 << 16
+
+    def fenced(need):
+        buf = torch.full((need + 2 * guard,), 0xAB, dtype=torch.uint8, device="cuda")
+        return buf, buf[guard:guard + need]
+
+    def whole(buf, need):
+        return (buf[:guard] == 0xAB).all() and (buf[guard + need:] == 0xAB).all()
+    for xd in (torch.bfloat16, torch.float32):
+        for wd in (torch.bfloat16, torch.float32):
+            x, _, b, label, dy = _tensors(M, K, N, 5, xd)
+            w = _tensors(M, K, N, 6, wd)[1]
+            q = [int(t is torch.bfloat16) for t in (xd, wd)]
+            for grad in (False, True):
+                need = pv._lib.pvconv_linear_cross_entropy_workspace_size(M, K, N, *q, *q, grad)
+                buf, ws = fenced(need)
+                got = pv.pvconv_linear_cross_entropy(x, w, label, bias=b, want_grad=grad,
+                                                     workspace=ws if need else None)
+                assert whole(buf, need)
+            for off in ("want_dx", "want_dw", "want_dbias"):
+                one = pv.pvconv_linear_cross_entropy_backward(x, w, label, got[1], bias=b,
+                                                              workspace=ws, **{off: False})
+                assert whole(buf, need) and sum(t is not None for t in one) == 2
+        wq, wsc = pv.pvconv_int8_quantize(w)
+        need = pv._lib.pvconv_int8_linear_workspace_size(M, K, N)
+        buf, ws = fenced(need)
+        y = pv.pvconv_int8_linear(x, wq, wsc, workspace=ws if need else None)
+        assert whole(buf, need)
+        need = pv._lib.pvconv_int8_linear_rows_workspace_size(M, K, N)
+        buf, ws = fenced(need)
+        z, rows, scale = pv.pvconv_int8_linear(x, wq, wsc, want_rows=True,
+                                               workspace=ws if need else None)
+        assert whole(buf, need) and torch.equal(y, z)
+        need = pv._lib.pvconv_int8_linear_backward_workspace_size(M, K, N)
+        buf, ws = fenced(need)
+        for od in (torch.bfloat16, torch.float32):
+            pv.pvconv_int8_linear_backward(dy, rows, scale, wq, wsc, K, out_dtype=od, workspace=ws)
+            assert whole(buf, need)
