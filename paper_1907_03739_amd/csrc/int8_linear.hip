@@ -431,6 +431,7 @@ struct BwdWs {
     PvPanel dys, w, dym, q;
     bool pack_dy;
     PvProduct dx, dw;
+    bool pair;  // the two in one launch
     float* sums;
     size_t total;
 };
@@ -438,28 +439,41 @@ BwdWs carve_bwd(void* base, const PvRows& dy, int M, int K, int N, bool dx_bf16,
                 bool want_dw, bool want_db, bool may_direct) {
     PvCarve c{(char*)base, 0};
     BwdWs w{};
-    auto product = [&](PvProduct& p, const PvPanel& a, const PvPanel& b, int rows, int cols,
-                       int depth) {
-        p.a = a;
-        p.b = b;
+    const int parts = parts_of(dx_bf16, dy.bf16, M, K, N);
+    auto plan = [&](PvProduct& p, int parts_a, int parts_b, int rows, int cols, int depth) {
+        p.a.parts = parts_a;
+        p.b.parts = parts_b;
         p.M = rows;
         p.N = cols;
         p.slices = pv_slices(depth, kDeep);
-        pv_pairs(p, a.parts, b.parts);
+        pv_pairs(p, parts_a, parts_b);
         pv_plan(p, true);
+    };
+    plan(w.dx, dy.bf16 ? 1 : parts, dy.bf16 ? parts : 1, M, K, N);
+    plan(w.dw, dy.bf16 ? 2 : 3, 1, N, K, M);
+    // (dw's plan is that of both, with an fp32 dx, whichever is wanted of whatever type: one
+    // gradient alone has the same bits)
+    PvProduct most{};
+    plan(most, dy.bf16 ? 1 : 3, dy.bf16 ? 2 : 1, M, K, N);
+    const int pair = pv_pair_size(most, w.dw);
+    if (pair >= 0) pv_take_pair(w.dw, pair);
+    w.pair = pair >= 0 && (pair != kPvP || w.dx.a.parts == 3);
+    if (w.pair) pv_take_pair(w.dx, pair);
+    auto take = [&](PvProduct& p, const PvPanel& a, const PvPanel& b) {
+        p.a = a;
+        p.b = b;
         p.partial = (uint32_t*)c.take(pv_partial_bytes(p));
     };
     if (want_dx && M > 0) {
-        const int parts = parts_of(dx_bf16, dy.bf16, M, K, N);
         w.pack_dy = !(may_direct && pv_in_place(dy, N));
         w.dys = w.pack_dy ? pv_take_panel(c, M, N, dy.bf16 ? 1 : parts) : pv_panel_of(dy, M);
         w.w = pv_take_panel(c, N, K, dy.bf16 ? parts : 1);
-        product(w.dx, w.dys, w.w, M, K, N);
+        take(w.dx, w.dys, w.w);
     }
     if (want_dw) {  // both operands across k: dy's rows are padded with zeros
         w.dym = pv_take_panel(c, (int)pv_up(M, kDeep), N, dy.bf16 ? 2 : 3);
         w.q = pv_take_panel(c, M, K, 1);
-        product(w.dw, w.dym, w.q, N, K, M);
+        take(w.dw, w.dym, w.q);
     }
     if (want_db) w.sums = (float*)c.take((size_t)pv_sum_runs(M) * N * 4);
     w.total = c.off;
@@ -596,8 +610,13 @@ pvconv_status pv_launch_int8_linear_bwd(const PvRows& dy, const int8_t* rows,
     pv_launch_packs(packs, s);
     const PvSums none{nullptr, 0, 0, nullptr},
         sums{w.sums, runs, N, dbias && runs != 1 ? dbias : nullptr};
-    if (want_dx) pv_launch_plain(w.dx, false, PvPlain{dx, nullptr}, dw ? none : sums, s);
-    if (dw) pv_launch_plain(w.dw, true, PvPlain{PvRows{dw, false, K}, nullptr}, sums, s);
-    if (!want_dx && !dw) pv_launch_sum_runs(sums, s);
+    const PvPlain to_dx{dx, nullptr}, to_dw{PvRows{dw, false, K}, nullptr};
+    if (want_dx && dw && w.pair) {
+        pv_launch_pair(w.dx, to_dx, w.dw, to_dw, sums, s);
+    } else {
+        if (want_dx) pv_launch_plain(w.dx, false, to_dx, dw ? none : sums, s);
+        if (dw) pv_launch_plain(w.dw, true, to_dw, sums, s);
+        if (!want_dx && !dw) pv_launch_sum_runs(sums, s);
+    }
     return pv_launch_status();
 }

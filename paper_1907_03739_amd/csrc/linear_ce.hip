@@ -272,6 +272,7 @@ struct Plan {
     int forward_classes, classes;  // a piece's
     PvPanel dz;
     PvProduct dx, dw;         // of a piece of `classes`
+    int pair;                 // the tile in which the two are one launch, or -1
     float2 *stats, *run;
     float *zlab, *lse, *sums, *acc;
     uint32_t* partial;
@@ -355,8 +356,9 @@ Plan carve(void* base, const PvLinearCe& a, bool forward, bool grads, bool may_d
     p.classes = n >= (size_t)a.V ? a.V : (int)n;
     p.parts = px > 1 || pw > 1;
     p.grad_sizes = sizes_of(p.whole ? kWhole : kGrad, p.parts);
-    auto product = [&](PvProduct& q, const PvPanel& x, const PvPanel& y, int rows, int cols,
-                       int depth) {
+    // (of both, wanted or not: one alone has the same bits)
+    auto plan = [&](PvProduct& q, const PvPanel& x, const PvPanel& y, int rows, int cols,
+                    int depth) {
         q.a = x;
         q.b = y;
         q.M = rows;
@@ -365,21 +367,29 @@ Plan carve(void* base, const PvLinearCe& a, bool forward, bool grads, bool may_d
         pv_pairs(q, x.parts, y.parts);
         pv_plan(q, true);
     };
+    PvPanel dz{}, w = p.w, x = p.x;
+    if (want_dx || want_dw)
+        dz = p.dz = pv_take_panel(c, (int)pv_up(a.M, kDeep), p.classes,
+                                  want_dx && want_dw ? (px > pw ? px : pw) : want_dx ? px : pw);
+    dz.parts = px;
+    if (a.dx.bf16 && w.parts > 2) w.parts = 2;
+    plan(p.dx, dz, w, a.M, a.K, p.classes);
+    dz.parts = pw;
+    if (a.dw.bf16 && x.parts > 2) x.parts = 2;
+    plan(p.dw, dz, x, p.classes, a.K, a.M);
+    p.pair = p.classes < a.V ? -1 : pv_pair_size(p.dx, p.dw);
+    if (p.pair >= 0) {
+        pv_take_pair(p.dx, p.pair);
+        pv_take_pair(p.dw, p.pair);
+    }
     // the splits' sums of a whole piece and of the last one, which may have fewer classes
     size_t partial = 0;
     const int tail = a.V % p.classes;
-    auto sums = [&](PvProduct q) {
+    auto sums = [&](const PvProduct& q) {
         const size_t b = pv_partial_bytes(q);
         partial = partial > b ? partial : b;
     };
-    const int pz = want_dx && want_dw ? (px > pw ? px : pw) : want_dx ? px : pw;
-    if (want_dx || want_dw)
-        p.dz = pv_take_panel(c, (int)pv_up(a.M, kDeep), p.classes, pz);
     if (want_dx) {
-        PvPanel dz = p.dz, w = p.w;
-        dz.parts = px;
-        if (a.dx.bf16 && w.parts > 2) w.parts = 2;
-        product(p.dx, dz, w, a.M, a.K, p.classes);
         sums(p.dx);
         if (tail) {
             PvProduct q = p.dx;
@@ -390,10 +400,6 @@ Plan carve(void* base, const PvLinearCe& a, bool forward, bool grads, bool may_d
         if (p.classes < a.V) p.acc = (float*)c.take((size_t)a.M * a.K * 4);
     }
     if (want_dw) {
-        PvPanel dz = p.dz, x = p.x;
-        dz.parts = pw;
-        if (a.dw.bf16 && x.parts > 2) x.parts = 2;
-        product(p.dw, dz, x, p.classes, a.K, a.M);
         sums(p.dw);
         if (tail) {
             PvProduct q = p.dw;
@@ -488,34 +494,32 @@ pvconv_status pv_launch_linear_ce(const PvLinearCe& a, bool forward, void* ws, h
         const PvProduct z = logits(v0, n, p.grad_sizes);
         const PvSums none{nullptr, 0, 0, nullptr},
             sums{p.sums, row_blocks(a.M, z.size), n, a.dbias ? a.dbias + v0 : nullptr};
-        const bool dx = a.dx.p && a.M > 0;
+        const bool dx = a.dx.p && a.M > 0, dw = a.dw.p;
         if (p.whole && forward)
             run_logits<kWhole>(z, c, p.parts, s);
         else
             run_logits<kGrad>(z, c, p.parts, s);
-        if (dx) {
-            PvProduct q = p.dx;
-            q.a.pitch = pitch;
-            q.b.p += (size_t)v0 * q.b.pitch;
-            q.b.rows = n;
-            q.slices = pv_slices(n, kDeep);
-            pv_plan(q, true);
-            q.partial = p.partial;
-            const bool last = v0 + n == a.V;
-            pv_launch_plain(q, false, PvPlain{last ? a.dx : PvRows{p.acc, false, a.K},
-                                              v0 ? p.acc : nullptr}, a.dw.p ? none : sums, s);
+        PvProduct to_dx = p.dx, to_dw = p.dw;
+        to_dx.a.pitch = to_dw.a.pitch = pitch;
+        to_dx.partial = to_dw.partial = p.partial;  // one after the other
+        to_dx.b.p += (size_t)v0 * to_dx.b.pitch;
+        to_dx.b.rows = n;
+        if (n < p.classes) {
+            to_dx.slices = pv_slices(n, kDeep);
+            pv_plan(to_dx, true);
+            to_dw.M = n;
+            pv_plan(to_dw, true);
         }
-        if (a.dw.p) {
-            PvProduct q = p.dw;
-            q.a.pitch = pitch;
-            q.M = n;
-            pv_plan(q, true);
-            q.partial = p.partial;
-            const size_t es = a.dw.bf16 ? 2 : 4;
-            pv_launch_plain(q, true, PvPlain{PvRows{(char*)a.dw.p + (size_t)v0 * a.dw.ld * es,
-                                                    a.dw.bf16, a.dw.ld}, nullptr}, sums, s);
+        const PvPlain out_dx{v0 + n == a.V ? a.dx : PvRows{p.acc, false, a.K}, v0 ? p.acc : nullptr},
+            out_dw{PvRows{(char*)a.dw.p + (size_t)v0 * a.dw.ld * (a.dw.bf16 ? 2 : 4), a.dw.bf16,
+                          a.dw.ld}, nullptr};
+        if (dx && dw && p.pair >= 0) {
+            pv_launch_pair(to_dx, out_dx, to_dw, out_dw, sums, s);
+        } else {
+            if (dx) pv_launch_plain(to_dx, false, out_dx, dw ? none : sums, s);
+            if (dw) pv_launch_plain(to_dw, true, out_dw, sums, s);
+            if (!dx && !dw) pv_launch_sum_runs(sums, s);
         }
-        if (!dx && !a.dw.p) pv_launch_sum_runs(sums, s);
     }
     return pv_launch_status();
 }

@@ -192,9 +192,8 @@ struct PlainEpi {
 };
 
 // A wave a column: 64 runs at a time in 64 bits, in a fixed order, eight loads in flight.
-__device__ __forceinline__ void sum_runs(const PvSums& k, unsigned block) {
-    const int c = (int)block * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-    if (c >= k.N) return;
+__device__ __forceinline__ void sum_run(const PvSums& k, int c) {
+    const int lane = threadIdx.x & 63;
     double s = 0.;
     for (int i0 = 0; i0 < k.n; i0 += 512) {
         float v[8];
@@ -208,6 +207,10 @@ __device__ __forceinline__ void sum_runs(const PvSums& k, unsigned block) {
 #pragma unroll
     for (int w = 1; w < 64; w <<= 1) s += __shfl_xor(s, w);
     if (lane == 0) k.out[c] = (float)s;
+}
+__device__ __forceinline__ void sum_runs(const PvSums& k, unsigned block) {
+    const int c = (int)block * 4 + (threadIdx.x >> 6);
+    if (c < k.N) sum_run(k, c);
 }
 __global__ __launch_bounds__(kThreads) void pv_sum_runs_kernel(PvSums k) {
     sum_runs(k, blockIdx.x);
@@ -237,6 +240,47 @@ __global__ __launch_bounds__(kThreads) void pv_sum_runs_wide_kernel(PvSums k) {
     k.out[c] = (float)s;
 }
 constexpr int kWideSums = 4096;  // columns
+
+// Two products, the first's a along k, the second's across it, a workgroup a tile, and
+// column sums, in one launch. Products of few tiles leave CUs idle, and a launch costs as
+// much as one of them.
+struct Pair {
+    PvProduct x, y;
+    PlainEpi ex, ey;
+    uint32_t x_blocks, y_blocks;
+    PvSums sums;
+};
+__device__ __forceinline__ bool pair_sums(const Pair& k, int waves) {
+    const uint32_t products = k.x_blocks + k.y_blocks;
+    if (blockIdx.x < products) return false;
+    for (int c = (int)(blockIdx.x - products) * waves + (int)(threadIdx.x >> 6); c < k.sums.N;
+         c += (int)(gridDim.x - products) * waves)
+        sum_run(k.sums, c);
+    return true;
+}
+__global__ __launch_bounds__(PvTileS::kThreads, 1) void pv_pair_kernel(Pair k) {
+    typedef PvTileS T;
+    constexpr int SA = T::TM * kSlice, SB = T::TN * kSlice;
+    __shared__ __align__(16) uint8_t la0[SA], la1[SA], la2[SA], la3[SA];
+    __shared__ __align__(16) uint8_t lb0[SB], lb1[SB], lb2[SB], lb3[SB];
+    const PvStages lds{la0, la1, la2, la3, lb0, lb1, lb2, lb3};
+    if (pair_sums(k, T::kThreads / 64)) return;
+    if (blockIdx.x < k.x_blocks)
+        pv_product_tiles<false, false, true, T>(k.x, k.ex, blockIdx.x, k.x_blocks, lds);
+    else
+        pv_product_tiles<false, true, true, T>(k.y, k.ey, blockIdx.x - k.x_blocks, k.y_blocks, lds);
+}
+template <int PB>
+__global__ __launch_bounds__(PvTileP::kThreads, 1) void pv_pair_parts_kernel(Pair k) {
+    constexpr int SA = 3 * PvTileP::TM * kSlice, SB = PB * PvTileP::TN * kSlice;
+    __shared__ __align__(16) uint8_t la0[SA], la1[SA], lb0[SB], lb1[SB];
+    if (pair_sums(k, PvTileP::kThreads / 64)) return;
+    if (blockIdx.x < k.x_blocks)
+        pv_parts_tiles<false, true, 3, PB>(k.x, k.ex, blockIdx.x, k.x_blocks, la0, la1, lb0, lb1);
+    else
+        pv_parts_tiles<true, true, 3, PB>(k.y, k.ey, blockIdx.x - k.x_blocks, k.y_blocks, la0, la1,
+                                          lb0, lb1);
+}
 
 }  // namespace
 
@@ -276,4 +320,58 @@ void pv_launch_plain(const PvProduct& p, bool a_across, const PvPlain& e, const 
     }
     pv_run_join<false>(p, epi, s);
     pv_launch_sum_runs(sums, s);
+}
+
+// Unsplit, one round of workgroups (some of them for column sums), and expected to take no
+// longer than one after the other.
+constexpr float kLaunch = 3.f;  // us
+constexpr size_t kSumBlocks = 8;
+int pv_pair_size(const PvProduct& x, const PvProduct& y) {
+    float best = x.us + y.us + kLaunch;
+    int size = -1;
+    auto choose = [&](const PvSizeCost& c) {
+        const size_t blocks = pv_up(pv_tiles_of(x.M, x.N, c.tm, c.tn), 8) +
+                              pv_up(pv_tiles_of(y.M, y.N, c.tm, c.tn), 8) + kSumBlocks;
+        const int xs = x.slices * x.pairs, ys = y.slices * y.pairs;
+        const float us = (float)(xs > ys ? xs : ys) * c.slice + c.rest;
+        if (blocks > (size_t)c.slots || us > best) return;
+        best = us;
+        size = c.size;
+    };
+    for (const PvSizeCost& c : kPvCosts)
+        if (c.size == kPvS) choose(c);
+    if (x.a.parts == 3 && y.a.parts == 3 && x.b.parts == y.b.parts &&
+        pv_all_parts(x.a.parts, x.b.parts))
+        choose(pv_parts_cost(x.pairs));
+    return size;
+}
+void pv_take_pair(PvProduct& p, int size) {
+    p.size = size;
+    p.per = p.slices * p.pairs;
+    p.splits = 1;
+}
+void pv_launch_pair(const PvProduct& x, const PvPlain& ex, const PvProduct& y, const PvPlain& ey,
+                    const PvSums& sums, hipStream_t s) {
+    Pair k{x, y, PlainEpi{ex, x.N}, PlainEpi{ey, y.N}, 0, 0, sums};
+    auto run = [&](auto kernel, auto tile) {
+        typedef decltype(tile) T;
+        auto tiles = [](PvProduct& p) {
+            p.first = 0;
+            p.count = (uint32_t)pv_tiles_of(p.M, p.N, T::TM, T::TN);
+            return (uint32_t)pv_up(p.count, 8);
+        };
+        k.x_blocks = tiles(k.x);
+        k.y_blocks = tiles(k.y);
+        const unsigned products = k.x_blocks + k.y_blocks, waves = T::kThreads / 64,
+                       most = T::kWorkgroups - products;
+        unsigned more = sums.out ? ((unsigned)sums.N + waves - 1) / waves : 0;
+        if (more > most) more = most;
+        hipLaunchKernelGGL(kernel, dim3(products + more), dim3(T::kThreads), 0, s, k);
+    };
+    if (x.size == kPvS)
+        run(pv_pair_kernel, PvTileS());
+    else if (x.b.parts == 3)
+        run(pv_pair_parts_kernel<3>, PvTileP());
+    else
+        run(pv_pair_parts_kernel<1>, PvTileP());
 }

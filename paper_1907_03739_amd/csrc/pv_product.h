@@ -44,6 +44,7 @@ struct PvProduct {
     uint32_t pa, pb;     // pair t multiplies part (pa >> 4t) & 15 of a by that of b
     int size;            // PvSize
     int splits, per;     // slices (of all pairs) a split; partial sums where splits > 1
+    float us;            // that the plan is expected to take
     uint32_t* partial;   // [splits][M][N], 32-bit words
     uint32_t first, count;  // the tiles of this launch (pv_run_tiles)
 };
@@ -242,27 +243,32 @@ __device__ __forceinline__ void pv_store_partial(const PvProduct& p, int split, 
     }
 }
 
+// Stages, arrays of their own in LDS: the loads into one are then seen not to touch what is
+// read of another, and are not waited for.
+struct PvStages {
+    uint8_t *a0, *a1, *a2, *a3, *b0, *b1, *b2, *b3;
+};
+
 // The epilogue gets acc[j][i][e]: row mw + 16 i + r, column nw + 32 (j >> 1) + 8 h + 4
 // (j & 1) + e (r = lane & 15, h = lane >> 4). A workgroup takes several tiles in turn: the
 // first slices of the next one are under way during the epilogue.
 template <bool I8, bool TA, bool TB, class T, class Epi>
-__global__ __launch_bounds__(T::kThreads, T::kThreads* T::kWorkgroups / 256 / 256) void
-pv_product_kernel(PvProduct p, Epi epi) {
+__device__ __forceinline__ void pv_product_tiles(const PvProduct& p, const Epi& epi,
+                                                 uint32_t block, uint32_t blocks,
+                                                 const PvStages& lds) {
     static_assert(!I8 || (!TA && !TB), "the transposing loads are of 16 bits");
-    // stages, arrays of their own: the loads into one are then seen not to touch what is
-    // read of another, and are not waited for
-    constexpr int SA = T::TM * kSlice, SB = T::TN * kSlice, ST = T::ST;
-    __shared__ __align__(16) uint8_t la0[SA], la1[SA], la2[ST > 2 ? SA : 16], la3[ST > 3 ? SA : 16];
-    __shared__ __align__(16) uint8_t lb0[SB], lb1[SB], lb2[ST > 2 ? SB : 16], lb3[ST > 3 ? SB : 16];
+    constexpr int ST = T::ST;
+    uint8_t *const la0 = lds.a0, *const la1 = lds.a1, *const la2 = lds.a2, *const la3 = lds.a3;
+    uint8_t *const lb0 = lds.b0, *const lb1 = lds.b1, *const lb2 = lds.b2, *const lb3 = lds.b3;
     typedef typename PvAcc<I8>::type Acc;
     constexpr int MI = T::MI;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lane = threadIdx.x & 63, r = lane & 15, h = lane >> 4;
     const int wm = wave % T::WM * (16 * MI), wn = wave / T::WM * 64;
     // each XCD (workgroups go round them) takes a run of the launch's tiles
-    const uint32_t run = (p.count + 7) / 8, step = gridDim.x >> 3;
-    const uint32_t end = min(run * ((blockIdx.x & 7) + 1), p.count);
-    uint32_t idx = run * (blockIdx.x & 7) + (blockIdx.x >> 3);
+    const uint32_t run = (p.count + 7) / 8, step = blocks >> 3;
+    const uint32_t end = min(run * ((block & 7) + 1), p.count);
+    uint32_t idx = run * (block & 7) + (block >> 3);
     if (idx >= end) return;
 
     int split, m0, n0, t0, t1, pair, k;
@@ -449,20 +455,32 @@ pv_product_kernel(PvProduct p, Epi epi) {
         if (!more) return;
     }
 }
+template <bool I8, bool TA, bool TB, class T, class Epi>
+__global__ __launch_bounds__(T::kThreads, T::kThreads* T::kWorkgroups / 256 / 256) void
+pv_product_kernel(PvProduct p, Epi epi) {
+    constexpr int SA = T::TM * kSlice, SB = T::TN * kSlice, ST = T::ST;
+    __shared__ __align__(16) uint8_t la0[SA], la1[SA], la2[ST > 2 ? SA : 16], la3[ST > 3 ? SA : 16];
+    __shared__ __align__(16) uint8_t lb0[SB], lb1[SB], lb2[ST > 2 ? SB : 16], lb3[ST > 3 ? SB : 16];
+    pv_product_tiles<I8, TA, TB, T>(p, epi, blockIdx.x, gridDim.x,
+                                    PvStages{la0, la1, la2, la3, lb0, lb1, lb2, lb3});
+}
+
 // The same product in tiles of 64 x 64 whose stages hold every part of a slice: a step of
 // 64 k's is one barrier for all pairs of parts (999 x 323 x 1003 in 32 bits: 36 steps of a
 // pair each took 16 us), and a part is loaded once for all pairs that it is in.
 template <bool TA, bool TB, int PA, int PB, class Epi>
-__global__ __launch_bounds__(PvTileP::kThreads, 1) void pv_parts_kernel(PvProduct p, Epi epi) {
+__device__ __forceinline__ void pv_parts_tiles(const PvProduct& p, const Epi& epi, uint32_t block,
+                                               uint32_t blocks, uint8_t* const la0,
+                                               uint8_t* const la1, uint8_t* const lb0,
+                                               uint8_t* const lb1) {
     typedef PvTileP T;
     constexpr int SA = T::TM * kSlice, SB = T::TN * kSlice, MI = T::MI;
-    __shared__ __align__(16) uint8_t la0[PA * SA], la1[PA * SA], lb0[PB * SB], lb1[PB * SB];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lane = threadIdx.x & 63, r = lane & 15, h = lane >> 4;
     const int wm = wave * 16;
-    const uint32_t run = (p.count + 7) / 8, step = gridDim.x >> 3;
-    const uint32_t end = min(run * ((blockIdx.x & 7) + 1), p.count);
-    uint32_t idx = run * (blockIdx.x & 7) + (blockIdx.x >> 3);
+    const uint32_t run = (p.count + 7) / 8, step = blocks >> 3;
+    const uint32_t end = min(run * ((block & 7) + 1), p.count);
+    uint32_t idx = run * (block & 7) + (block >> 3);
     if (idx >= end) return;
     int split, m0, n0, k, k1;
     PvSource<TA, false, T::TM, T::kThreads> from_a;
@@ -563,6 +581,13 @@ __global__ __launch_bounds__(PvTileP::kThreads, 1) void pv_parts_kernel(PvProduc
     }
 }
 
+template <bool TA, bool TB, int PA, int PB, class Epi>
+__global__ __launch_bounds__(PvTileP::kThreads, 1) void pv_parts_kernel(PvProduct p, Epi epi) {
+    constexpr int SA = PA * PvTileP::TM * kSlice, SB = PB * PvTileP::TN * kSlice;
+    __shared__ __align__(16) uint8_t la0[SA], la1[SA], lb0[SB], lb1[SB];
+    pv_parts_tiles<TA, TB, PA, PB>(p, epi, blockIdx.x, gridDim.x, la0, la1, lb0, lb1);
+}
+
 // Sixteen values of columns, as a lane has them: `none` from N on, or where there are none.
 __device__ __forceinline__ void pv_load_columns(const float* from, int nb, int N, float none,
                                                 float (&v)[16]) {
@@ -650,6 +675,10 @@ static constexpr PvSizeCost kPvCosts[] = {
 static constexpr bool pv_all_parts(int a, int b) {
     return (a == 3 && (b == 3 || b == 1)) || (a == 1 && b == 3);
 }
+static inline PvSizeCost pv_parts_cost(int pairs) {
+    return PvSizeCost{kPvP, PvTileP::TM, PvTileP::TN, PvTileP::kWorkgroups,
+                      pairs > 3 ? 0.18f : 0.22f, 3.f};
+}
 static inline void pv_plan(PvProduct& p, bool may_split, unsigned sizes = 63) {
     const int all = p.slices * p.pairs;
     float best = 0.f;
@@ -670,14 +699,14 @@ static inline void pv_plan(PvProduct& p, bool may_split, unsigned sizes = 63) {
                 p.size = c.size;
                 p.per = per;
                 p.splits = splits;
+                p.us = us;
             }
         }
     };
     for (const PvSizeCost& c : kPvCosts)
         if (sizes >> c.size & 1) choose(c);
     if ((sizes >> kPvP & 1) && pv_all_parts(p.a.parts, p.b.parts) && p.pairs > 1)
-        choose(PvSizeCost{kPvP, PvTileP::TM, PvTileP::TN, PvTileP::kWorkgroups,
-                          p.pairs > 3 ? 0.18f : 0.22f, 3.f});
+        choose(pv_parts_cost(p.pairs));
 }
 static inline size_t pv_partial_bytes(const PvProduct& p) {
     return p.splits > 1 ? (size_t)p.splits * p.M * p.N * 4 : 0;
@@ -869,6 +898,13 @@ struct PvSums {
 };
 void pv_launch_plain(const PvProduct& p, bool a_across, const PvPlain& e, const PvSums& sums,
                      hipStream_t s);
+// Two of them that do not depend on each other, x's a along k, y's across it, as one launch:
+// the size of tile in which they are that (-1: none), and its plan, which either has when
+// it is run alone too, so that its bits are the same.
+int pv_pair_size(const PvProduct& x, const PvProduct& y);
+void pv_take_pair(PvProduct& p, int size);
+void pv_launch_pair(const PvProduct& x, const PvPlain& ex, const PvProduct& y, const PvPlain& ey,
+                    const PvSums& sums, hipStream_t s);
 
 // Sums [n][N] of runs joined in a fixed order.
 void pv_launch_sum_runs(const PvSums& sums, hipStream_t s);
