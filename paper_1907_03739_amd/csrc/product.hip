@@ -17,7 +17,10 @@ __device__ __forceinline__ void load8(const PvPack& k, size_t row, int c0, float
     const size_t from = row * k.ld + c0;
     if (c0 + 8 > k.C) {
 #pragma unroll
-        for (int i = 0; i < 8; i++) v[i] = c0 + i < k.C ? load_kind(k.src, KIND, from + i) : 0.f;
+        for (int i = 0; i < 8; i++)  // (no branches, which would wait for one after another)
+            v[i] = load_kind(k.src, KIND, row * k.ld + min(c0 + i, k.C - 1));
+#pragma unroll
+        for (int i = 0; i < 8; i++) v[i] = c0 + i < k.C ? v[i] : 0.f;
     } else if constexpr (KIND == kPvBf16) {
         const pv_u32x4 w = *(const pv_u32x4_any*)((const uint16_t*)k.src + from);
 #pragma unroll
@@ -47,16 +50,21 @@ __device__ __forceinline__ uint32_t next_part(float& v) {
     return h;
 }
 
+// log2 of the threads of a row of `per` pieces: as many as leave an eighth of them idle at
+// most, of few rows a third.
+__host__ __device__ inline int pack_shift(int per, int rows) {
+    const int idle = rows <= 4096 ? per / 3 : per / 8;
+    int shift = 8;
+    while (shift > 3 && ((per + (1 << shift) - 1) >> shift << shift) > per + idle) shift--;
+    return shift;
+}
+
 // Rows of parts: eight consecutive columns a thread, both ends of the traffic in 16-byte
 // pieces, a power of two of threads a row. Bound by memory.
 template <PvKind KIND>
 __device__ __forceinline__ void pack_rows(const PvPack& k, size_t block, size_t blocks) {
     const int per = (int)(k.pitch / 16);
-    // the threads of a row: as many as leave an eighth of them idle at most, of few rows a
-    // third
-    const int idle = k.rows <= 4096 ? per / 3 : per / 8;
-    int shift = 8;
-    while (shift > 3 && ((per + (1 << shift) - 1) >> shift << shift) > per + idle) shift--;
+    const int shift = pack_shift(per, k.rows);
     const int lead = threadIdx.x >> shift, first = threadIdx.x & ((1 << shift) - 1);
     const size_t rows = (size_t)kThreads >> shift;
     for (size_t row = block * rows + lead; row < (size_t)k.rows; row += blocks * rows) {
@@ -94,38 +102,45 @@ __device__ __forceinline__ void pack_rows(const PvPack& k, size_t block, size_t 
     }
 }
 
-// Sums of 64 columns over runs of rows, in 64 bits: eight columns a thread, every 32nd row.
+// Sums of columns over runs of rows, in 64 bits: eight columns a thread, 64 a workgroup,
+// whose 32 threads take every 32nd row of a column, four of them under way; of a single run,
+// which would leave most CUs idle, eight columns and 256 threads.
+__host__ __device__ inline int sum_groups(int R) { return pv_sum_runs(R) == 1 ? 1 : 8; }
 template <PvKind KIND>
 __device__ __forceinline__ void sum_columns(const PvPack& k, size_t block, size_t blocks,
                                             double (*part)[72]) {
-    const size_t nb = (k.C + 63) / 64, total = nb * ((k.R + k.rows - 1) / k.rows);
-    const int group = threadIdx.x & 7, lead = threadIdx.x >> 3;
+    const int groups = sum_groups(k.R), leads = kThreads / groups;
+    const size_t nb = (k.C + 8 * groups - 1) / (8 * groups),
+                 total = nb * ((k.R + k.rows - 1) / k.rows);
+    const int group = threadIdx.x & (groups - 1), lead = threadIdx.x / groups;
+    constexpr int kAhead = 4;
     for (size_t t = block; t < total; t += blocks) {
-        const int c0 = (int)(t % nb) * 64 + group * 8;
+        const int c0 = ((int)(t % nb) * groups + group) * 8;
         const size_t r0 = t / nb * k.rows;
         const int rows = (int)min((size_t)k.rows, (size_t)k.R - r0);
         double s[8] = {0., 0., 0., 0., 0., 0., 0., 0.};
         if (c0 < k.C)
-#pragma unroll 4
-            for (int i = lead; i < rows; i += 32) {
-                float v[8];
-                load8<KIND>(k, r0 + i, c0, v);
+            for (int i = lead; i < rows; i += leads * kAhead) {
+                float v[kAhead][8];
 #pragma unroll
-                for (int q = 0; q < 8; q++) s[q] += (double)v[q];
+                for (int u = 0; u < kAhead; u++)
+                    load8<KIND>(k, r0 + min(i + leads * u, rows - 1), c0, v[u]);
+#pragma unroll
+                for (int u = 0; u < kAhead; u++)
+                    if (i + leads * u < rows)
+#pragma unroll
+                        for (int q = 0; q < 8; q++) s[q] += (double)v[u][q];
             }
-        // the eight threads of a wave that have the same columns, then the four waves
+        // the threads of a wave that have the same columns, then the four waves
+        for (int w = groups; w < 64; w <<= 1)
 #pragma unroll
-        for (int q = 0; q < 8; q++) {
-            s[q] += __shfl_xor(s[q], 8);
-            s[q] += __shfl_xor(s[q], 16);
-            s[q] += __shfl_xor(s[q], 32);
-        }
-        if ((lead & 7) == 0)
+            for (int q = 0; q < 8; q++) s[q] += __shfl_xor(s[q], w);
+        if ((int)(threadIdx.x & 63) < groups)
 #pragma unroll
-            for (int q = 0; q < 8; q++) part[lead >> 3][group * 8 + q] = s[q];
+            for (int q = 0; q < 8; q++) part[threadIdx.x >> 6][group * 8 + q] = s[q];
         __syncthreads();
-        const int c = (int)(t % nb) * 64 + (int)threadIdx.x;
-        if (threadIdx.x < 64 && c < k.C)
+        const int c = (int)(t % nb) * groups * 8 + (int)threadIdx.x;
+        if ((int)threadIdx.x < groups * 8 && c < k.C)
             k.sums[t / nb * k.C + c] = (float)(((part[0][threadIdx.x] + part[1][threadIdx.x]) +
                                                 part[2][threadIdx.x]) + part[3][threadIdx.x]);
         __syncthreads();
@@ -273,23 +288,29 @@ __global__ __launch_bounds__(PvTileS::kThreads, 1) void pv_pair_kernel(Pair k) {
 template <int PB>
 __global__ __launch_bounds__(PvTileP::kThreads, 1) void pv_pair_parts_kernel(Pair k) {
     constexpr int SA = 3 * PvTileP::TM * kSlice, SB = PB * PvTileP::TN * kSlice;
-    __shared__ __align__(16) uint8_t la0[SA], la1[SA], lb0[SB], lb1[SB];
+    __shared__ __align__(16) uint8_t la0[SA], la1[SA], la2[SA], lb0[SB], lb1[SB], lb2[SB];
+    const PvStages lds{la0, la1, la2, nullptr, lb0, lb1, lb2, nullptr};
     if (pair_sums(k, PvTileP::kThreads / 64)) return;
     if (blockIdx.x < k.x_blocks)
-        pv_parts_tiles<false, true, 3, PB>(k.x, k.ex, blockIdx.x, k.x_blocks, la0, la1, lb0, lb1);
+        pv_parts_tiles<false, true, 3, PB>(k.x, k.ex, blockIdx.x, k.x_blocks, lds);
     else
-        pv_parts_tiles<true, true, 3, PB>(k.y, k.ey, blockIdx.x - k.x_blocks, k.y_blocks, la0, la1,
-                                          lb0, lb1);
+        pv_parts_tiles<true, true, 3, PB>(k.y, k.ey, blockIdx.x - k.x_blocks, k.y_blocks, lds);
 }
 
 }  // namespace
 
+constexpr size_t kOneStep = 2048;  // workgroups: all of them at once
 void pv_launch_packs(PvPacks& k, hipStream_t s) {
     k.begin[0] = 0;
     for (int j = 0; j < k.n; j++) {
         const PvPack& p = k.job[j];
-        const size_t blocks = p.sums ? (size_t)pv_sum_runs(p.R) * ((p.C + 63) / 64)
-                                     : (p.pitch / 16 * p.rows + 2 * kThreads - 1) / (2 * kThreads);
+        const int columns = 8 * sum_groups(p.R);
+        size_t blocks = (size_t)pv_sum_runs(p.R) * ((p.C + columns - 1) / columns);
+        if (!p.sums) {  // a step each, of many rows two
+            const int rows = kThreads >> pack_shift((int)(p.pitch / 16), p.rows);
+            blocks = ((size_t)p.rows + rows - 1) / rows;
+            if (blocks > kOneStep) blocks = blocks < 2 * kOneStep ? kOneStep : blocks / 2;
+        }
         k.begin[j + 1] = k.begin[j] + (unsigned)(blocks < (1u << 16) ? blocks : 1u << 16);
     }
     if (k.n && k.begin[k.n])

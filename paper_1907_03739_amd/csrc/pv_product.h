@@ -83,7 +83,7 @@ typedef PvTile<4, 2, 4, 3, 1> PvTileG;  // 256 x 128
 typedef PvTile<2, 2, 4, 4, 1> PvTileM;  // 128 x 128
 typedef PvTile<4, 1, 2, 4, 1> PvTileN;  // 128 x 64
 typedef PvTile<2, 1, 2, 4, 2> PvTileS;  // 64 x 64
-typedef PvTile<4, 1, 1, 2, 1> PvTileP;  // 64 x 64, all parts of a slice in a stage
+typedef PvTile<4, 1, 1, 3, 1> PvTileP;  // 64 x 64, all parts of a slice in a stage
 enum PvSize { kPvS, kPvN, kPvM, kPvG, kPvL, kPvP };
 
 // The tile of index idx: eight tiles of rows by the columns in turn, so that an XCD,
@@ -184,13 +184,18 @@ struct PvSource {
         return base + part * p.part_bytes +
                (size_t)k * (ACROSS ? kDeep * p.pitch : p.slice_bytes);
     }
-    __device__ __forceinline__ void load(const PvPanel& p, const uint8_t* from, int k, int q,
-                                         int wave, int lane, uint8_t* lds) const {
+    // where load q of slice k lies in it
+    __device__ __forceinline__ uint32_t offset(const PvPanel& p, int k, int q, int wave,
+                                               int lane) const {
         uint32_t o = off[q];
         if constexpr (ACROSS) {  // rows past the last are read as that one
             const int past = k * kDeep + row_of(q, wave, lane) - (p.rows - 1);
             if ((k + 1) * kDeep > p.rows) o -= (uint32_t)max(past, 0) * (uint32_t)p.pitch;
         }
+        return o;
+    }
+    __device__ __forceinline__ static void load(const uint8_t* from, uint32_t o, int q, int wave,
+                                                uint8_t* lds) {
         __builtin_amdgcn_global_load_lds(
             (const void __attribute__((address_space(1)))*)(from + o),
             (void __attribute__((address_space(3)))*)(lds + (wave * Q + q) * 1024), 16, 0, 0);
@@ -200,21 +205,28 @@ struct PvSource {
 // The matrix operand of a lane out of an operand across k: eight k's of one of sixteen
 // columns, whose four groups of four begin at the columns `col` of the lanes 0 .. 3.
 template <int COLS>
-__device__ __forceinline__ pv_u32x4 pv_load_across(const uint8_t* lds, int k0, int col, int lane) {
+__device__ __forceinline__ int pv_across_at(int k, int col) {
+    return k * (COLS * 2) + (((col >> 4) ^ pv_key_across<COLS>(k)) << 5) + (col & 15) * 2;
+}
+template <int COLS>
+__device__ __forceinline__ pv_u32x4 pv_load_across_at(const uint8_t* lds, const int (&at)[2]) {
     pv_u32x4 v;
 #pragma unroll
     for (int s = 0; s < 2; s++) {
-        const int k = k0 + 8 * (lane >> 4) + 4 * s + ((lane >> 2) & 3);
-        const uint8_t* p = lds + k * (COLS * 2) +
-                           (((col >> 4) ^ pv_key_across<COLS>(k)) << 5) + (col & 15) * 2;
         const pv_s16x4 t = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (pv_s16x4 __attribute__((address_space(3)))*)p);
+            (pv_s16x4 __attribute__((address_space(3)))*)(lds + at[s]));
         uint32_t u[2];
         __builtin_memcpy(u, &t, 8);
         v[2 * s] = u[0];
         v[2 * s + 1] = u[1];
     }
     return v;
+}
+template <int COLS>
+__device__ __forceinline__ pv_u32x4 pv_load_across(const uint8_t* lds, int k0, int col, int lane) {
+    const int k = k0 + 8 * (lane >> 4) + ((lane >> 2) & 3);
+    const int at[2] = {pv_across_at<COLS>(k, col), pv_across_at<COLS>(k + 4, col)};
+    return pv_load_across_at<COLS>(lds, at);
 }
 
 // a split's sums of a wave's tile
@@ -292,9 +304,9 @@ __device__ __forceinline__ void pv_product_tiles(const PvProduct& p, const Epi& 
     };
     auto fetch_one = [&](auto q, uint8_t* la, uint8_t* lb) {
         if constexpr (q < QA)
-            from_a.load(p.a, slice_a, k, q, wave, lane, la);
+            from_a.load(slice_a, from_a.offset(p.a, k, q, wave, lane), q, wave, la);
         else
-            from_b.load(p.b, slice_b, k, q - QA, wave, lane, lb);
+            from_b.load(slice_b, from_b.offset(p.b, k, q - QA, wave, lane), q - QA, wave, lb);
     };
     auto fetch_end = [&]() {
         if (++k == p.slices) {
@@ -470,10 +482,10 @@ pv_product_kernel(PvProduct p, Epi epi) {
 // pair each took 16 us), and a part is loaded once for all pairs that it is in.
 template <bool TA, bool TB, int PA, int PB, class Epi>
 __device__ __forceinline__ void pv_parts_tiles(const PvProduct& p, const Epi& epi, uint32_t block,
-                                               uint32_t blocks, uint8_t* const la0,
-                                               uint8_t* const la1, uint8_t* const lb0,
-                                               uint8_t* const lb1) {
+                                               uint32_t blocks, const PvStages& lds) {
     typedef PvTileP T;
+    uint8_t *const la0 = lds.a0, *const la1 = lds.a1, *const la2 = lds.a2;
+    uint8_t *const lb0 = lds.b0, *const lb1 = lds.b1, *const lb2 = lds.b2;
     constexpr int SA = T::TM * kSlice, SB = T::TN * kSlice, MI = T::MI;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lane = threadIdx.x & 63, r = lane & 15, h = lane >> 4;
@@ -494,49 +506,72 @@ __device__ __forceinline__ void pv_parts_tiles(const PvProduct& p, const Epi& ep
         from_b.enter(p.b, n0, p.N, wave, lane);
     };
     auto fetch = [&](int at, uint8_t* la, uint8_t* lb) {
-        pv_each<PA>([&](auto part) {
-            const uint8_t* from = from_a.slice(p.a, part, at);
-            pv_each<QA>([&](auto q) {
-                from_a.load(p.a, from, at, q, wave, lane, la + part * SA);
+        pv_each<QA>([&](auto q) {
+            const uint32_t o = from_a.offset(p.a, at, q, wave, lane);
+            pv_each<PA>([&](auto part) {
+                from_a.load(from_a.slice(p.a, part, at), o, q, wave, la + part * SA);
             });
         });
-        pv_each<PB>([&](auto part) {
-            const uint8_t* from = from_b.slice(p.b, part, at);
-            pv_each<QB>([&](auto q) {
-                from_b.load(p.b, from, at, q, wave, lane, lb + part * SB);
+        pv_each<QB>([&](auto q) {
+            const uint32_t o = from_b.offset(p.b, at, q, wave, lane);
+            pv_each<PB>([&](auto part) {
+                from_b.load(from_b.slice(p.b, part, at), o, q, wave, lb + part * SB);
             });
         });
+    };
+    // Where a lane's values of either half of a slice lie, as numbers that the compiler does
+    // not take apart: behind a chain of more than four sums it no longer sees which array is
+    // read, and waits for the loads into every other one.
+    static_assert(T::TM == 64 && T::TN == 64, "keys of k's bits 1 and 3");
+    auto whole = [](int at) {
+        asm("" : "+v"(at));
+        return at;
+    };
+    auto across = [&](int half, int col) {
+        return whole(pv_across_at<64>(32 * half + 8 * h + ((lane >> 2) & 3), col));
+    };
+    auto along = [&](int half, int row, int key) {
+        return whole(row * kSlice + ((h + 4 * half) ^ key) * 16);
+    };
+    int at_a[2], at_b[2][4];
+    pv_each<2>([&](auto half) {
+        const int row = wm + r;
+        at_a[half] = TA ? across(half, wm + 4 * (lane & 3)) : along(half, row, pv_key_a(row));
+        pv_each<4>([&](auto j) {
+            const int row = 32 * (j >> 1) + 8 * (r >> 2) + 4 * (j & 1) + (r & 3);
+            at_b[half][j] = TB ? across(half, 32 * (j >> 1) + 8 * (lane & 3) + 4 * (j & 1))
+                               : along(half, row, pv_key_b(row));
+        });
+    });
+    auto load_operand = [](auto is_across, const uint8_t* lds, int at) {
+        if constexpr (is_across) {
+            const int four[2] = {at, at + 4 * 128};
+            return pv_load_across_at<64>(lds, four);
+        } else {
+            return *(const pv_u32x4*)(lds + at);
+        }
     };
     auto load_a = [&](const uint8_t* la, int half) {
-        if constexpr (TA) {
-            return pv_load_across<T::TM>(la, 32 * half, wm + 4 * (lane & 3), lane);
-        } else {
-            const int row = wm + r;
-            return *(const pv_u32x4*)(la + row * kSlice + ((h + 4 * half) ^ pv_key_a(row)) * 16);
-        }
+        return load_operand(std::integral_constant<bool, TA>(), la, at_a[half]);
     };
     auto load_b = [&](const uint8_t* lb, int j, int half) {
-        if constexpr (TB) {
-            return pv_load_across<T::TN>(lb, 32 * half,
-                                         32 * (j >> 1) + 8 * (lane & 3) + 4 * (j & 1), lane);
-        } else {
-            const int row = 32 * (j >> 1) + 8 * (r >> 2) + 4 * (j & 1) + (r & 3);
-            return *(const pv_u32x4*)(lb + row * kSlice + ((h + 4 * half) ^ pv_key_b(row)) * 16);
-        }
+        return load_operand(std::integral_constant<bool, TB>(), lb, at_b[half][j]);
+    };
+    // (of a single step, a second one: see pv_product_tiles)
+    auto first = [&]() {
+        if (k >= k1) return;
+        fetch(k, la0, lb0);
+        fetch(min(k + 1, p.slices - 1), la1, lb1);
     };
     enter();
-    if (k < k1) fetch(k, la0, lb0);
+    first();
     for (;;) {
         // the sums of first parts, and of the others, whose digits would be lost in them
         pv_f32x4 acc[4][MI], rest[4];
 #pragma unroll
         for (int j = 0; j < 4; j++) acc[j][0] = rest[j] = pv_f32x4{0.f, 0.f, 0.f, 0.f};
         constexpr int kOrders = PA < 3 && PB < 3 ? 2 : 3;  // as pv_pairs
-        auto one = [&](const uint8_t* la, const uint8_t* lb, uint8_t* na, uint8_t* nb) {
-            if (k >= k1) return;
-            pv_wait_loads<0>();
-            pv_stage_barrier();
-            if (k + 1 < k1) fetch(k + 1, na, nb);
+        auto multiply = [&](const uint8_t* la, const uint8_t* lb) {
             pv_each<2>([&](auto half) {
                 pv_u32x4 fa[PA], fb[PB][4];
                 pv_each<PA>([&](auto i) { fa[i] = load_a(la + i * SA, half); });
@@ -558,20 +593,38 @@ __device__ __forceinline__ void pv_parts_tiles(const PvProduct& p, const Epi& ep
             });
             k++;
         };
-        while (k < k1) {
-            one(la0, lb0, la1, lb1);
-            one(la1, lb1, la0, lb0);
+        auto steady = [&](const uint8_t* la, const uint8_t* lb, uint8_t* na, uint8_t* nb) {
+            pv_wait_loads<PA * QA + PB * QB>();  // all but those of the next step
+            pv_stage_barrier();
+            fetch(k + 2, na, nb);
+            multiply(la, lb);
+        };
+        auto last = [&](const uint8_t* la, const uint8_t* lb, uint8_t* na, uint8_t* nb) {
+            if (k >= k1) return;
+            pv_wait_loads<0>();
+            pv_stage_barrier();
+            if (k + 2 < k1) fetch(k + 2, na, nb);
+            multiply(la, lb);
+        };
+        while (k + 4 < k1) {
+            steady(la0, lb0, la2, lb2);
+            steady(la1, lb1, la0, lb0);
+            steady(la2, lb2, la1, lb1);
         }
+        last(la0, lb0, la2, lb2);
+        last(la1, lb1, la0, lb0);
+        last(la2, lb2, la1, lb1);
+        last(la0, lb0, la2, lb2);
 #pragma unroll
         for (int j = 0; j < 4; j++) acc[j][0] += rest[j];
         const int em = m0 + wm, en = n0, es = split;
         idx += step;
         const bool more = idx < end;
         if (more) {
-            pv_wait_loads<63>();
+            pv_wait_loads<0>();  // (none is: for the compiler's count of them)
             pv_stage_barrier();  // nothing reads the stages any more
             enter();
-            if (k < k1) fetch(k, la0, lb0);
+            first();
         }
         if (p.splits > 1)
             pv_store_partial<MI>(p, es, em, en, lane, acc);
@@ -584,8 +637,9 @@ __device__ __forceinline__ void pv_parts_tiles(const PvProduct& p, const Epi& ep
 template <bool TA, bool TB, int PA, int PB, class Epi>
 __global__ __launch_bounds__(PvTileP::kThreads, 1) void pv_parts_kernel(PvProduct p, Epi epi) {
     constexpr int SA = PA * PvTileP::TM * kSlice, SB = PB * PvTileP::TN * kSlice;
-    __shared__ __align__(16) uint8_t la0[SA], la1[SA], lb0[SB], lb1[SB];
-    pv_parts_tiles<TA, TB, PA, PB>(p, epi, blockIdx.x, gridDim.x, la0, la1, lb0, lb1);
+    __shared__ __align__(16) uint8_t la0[SA], la1[SA], la2[SA], lb0[SB], lb1[SB], lb2[SB];
+    pv_parts_tiles<TA, TB, PA, PB>(p, epi, blockIdx.x, gridDim.x,
+                                   PvStages{la0, la1, la2, nullptr, lb0, lb1, lb2, nullptr});
 }
 
 // Sixteen values of columns, as a lane has them: `none` from N on, or where there are none.
@@ -873,8 +927,8 @@ struct PvPack {
                              // over runs of `rows` rows, [runs][C]
 };
 // rows of a run, and how many there are (one: the sums are whole)
-static inline int pv_sum_rows(int M) { return M <= 1024 ? 1024 : 256; }
-static inline int pv_sum_runs(int M) { return (M + pv_sum_rows(M) - 1) / pv_sum_rows(M); }
+__host__ __device__ static inline int pv_sum_rows(int M) { return M <= 1024 ? 1024 : 256; }
+__host__ __device__ static inline int pv_sum_runs(int M) { return (M + pv_sum_rows(M) - 1) / pv_sum_rows(M); }
 // Up to five at once.
 struct PvPacks {
     PvPack job[5];
