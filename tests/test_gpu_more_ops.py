@@ -6,6 +6,8 @@ import pytest
 import torch
 
 from paper_1907_03739_amd import binding as pv
+from test_gpu_int8 import test_backward_from_kept_rows as _backward_from_kept_rows
+from test_gpu_linear_ce import test_loss_and_gradients as _loss_and_gradients
 from test_gpu_train_ops import put
 
 pytestmark = pytest.mark.gpu
@@ -212,3 +214,22 @@ def test_the_workspace_that_is_asked_for_is_all_that_is_used(M, K, N):
         for od in (torch.bfloat16, torch.float32):
             pv.pvconv_int8_linear_backward(dy, rows, scale, wq, wsc, K, out_dtype=od, workspace=ws)
             assert whole(buf, need)
+
+
+# products of dx and dw that are one launch and, beside them, ones that are two: single rows
+# and columns, tiles that fill the chip's workgroups or just do not, column sums of one run
+# and of several, of few columns and of many
+SMALL_STEPS = [(1, 1, 1), (64, 64, 64), (65, 65, 65), (999, 323, 1003), (1025, 323, 1003),
+               (1100, 48, 4200), (2000, 100, 300), (2300, 700, 130), (6000, 64, 64)]
+
+
+@pytest.mark.parametrize("yd,xd", [("f32", "f32"), ("bf16", "bf16"), ("f32", "bf16")])
+@pytest.mark.parametrize("M,K,N", SMALL_STEPS)
+def test_gradients_of_small_steps_from_kept_rows(M, K, N, yd, xd):
+    _backward_from_kept_rows(M, K, N, yd, xd, 0, 0)
+
+
+@pytest.mark.parametrize("xd,wd", [("f32", "f32"), ("bf16", "bf16"), ("f32", "bf16")])
+@pytest.mark.parametrize("M,K,V", SMALL_STEPS)
+def test_gradients_of_small_steps_of_the_loss(M, K, V, xd, wd):
+    _loss_and_gradients(M, K, V, xd, wd, xd, wd, True, 0, 0)
