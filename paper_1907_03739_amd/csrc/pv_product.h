@@ -521,7 +521,6 @@ __device__ __forceinline__ void pv_parts_tiles(const PvProduct& p, const Epi& ep
                 from_b.load(from_b.slice(p.b, part, at), o, q, wave, lb + part * SB);
             });
         });
-        __builtin_amdgcn_sched_barrier(0);  // in this order: they are waited for by count
     };
     // Where a lane's values of either half of a slice lie, as numbers that the compiler does
     // not take apart: behind a chain of more than four sums it no longer sees which array is
@@ -565,6 +564,7 @@ __device__ __forceinline__ void pv_parts_tiles(const PvProduct& p, const Epi& ep
     auto first = [&]() {
         if (k >= k1) return;
         fetch(k, la0, lb0);
+        __builtin_amdgcn_sched_barrier(0);  // in this order: they are waited for by count
         fetch(min(k + 1, p.slices - 1), la1, lb1);
     };
     enter();
