@@ -184,9 +184,8 @@ pvconv_status pvconv_int8_linear_rows(const int8_t* rows, const float* row_scale
 /* scale weight, from the kept rows:                                         */
 /*   dx[m,k] = sum_n dy[m,n] scale_n weight[n,k]                             */
 /*   dw[n,k] = sum_m dy[m,n] row_scale_m rows[m,k],  dbias_n = sum_m dy[m,n] */
-/* An fp32 output has fp32 sums of products good to 24 bits; for a bf16 dx,  */
-/* one factor (scale_n weight of a bf16 dy, dy scale_n of an fp32 one) is    */
-/* rounded to bf16 first, of up to 256 rows or 2^16 values of it to 16 bits. */
+/* Sums are fp32, of products that are exact (bf16 dy) or good to 24 bits    */
+/* (fp32 dy; for a bf16 dx, dy scale_n is rounded to 16 bits first).         */
 /*  dy [M][N] (dy_dt), dy_ld; dx out [M][K] (dx_dt), dx_ld, or NULL (weight, */
 /*  scale then unused); dw out [N][K] fp32 or NULL (rows, row_scale then     */
 /*  unused); dbias out [N] fp32 or NULL                                      */

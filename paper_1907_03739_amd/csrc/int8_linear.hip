@@ -14,8 +14,8 @@
 // slices of products.
 //
 // The gradients are products of bf16 parts, from the bytes and scales that the forward
-// kept: with bf16 dy, dx takes dy as it lies by the weight times its scales (15 bits: one
-// rounded part, or two), dw takes dy s in the two parts that hold its 16 bits. 32768 x 2304
+// kept: with bf16 dy, dx takes dy as it lies by the weight times its scales (15 bits, two
+// parts), dw takes dy s in the two parts that hold its 16 bits. 32768 x 2304
 // -> 512: operands 74 us (4.4 TB/s), dx 109 (0.71 PFLOP/s), dw 183 (two parts: 0.85).
 #include "pv_product.h"
 #include "pv_wave.h"
@@ -414,16 +414,12 @@ LinearWs carve_linear(void* base, int M, int K, int N, bool rows_given) {
     return w;
 }
 
-// Parts of dx's scaled operand (the weight of a bf16 dy, else dy): for a bf16 result one
-// rounded part, or two where few values would not average what the rounding leaves. For
-// an fp32 one, the two that hold 8 by 8 bits where dy is bf16, else three.
-constexpr int kFewRows = 256;
-constexpr size_t kFewValues = 1 << 16;
-int parts_of(bool out_bf16, bool dy_bf16, int M, int K, int N) {
-    if (out_bf16)
-        return M <= kFewRows || (size_t)N * (dy_bf16 ? K : M) <= kFewValues ? 2 : 1;
-    return dy_bf16 ? 2 : 3;
-}
+// Parts of dx's scaled operand (the weight of a bf16 dy, else dy): the two that hold its 15
+// bits where dy is bf16; of an fp32 dy three, for a bf16 result two, which leave 2^-16 of a
+// term where the result's rounding is 2^-8. (One rounded part leaves 2^-8 of a term more,
+// at whatever number of rows: a row's sum has as many as it has channels, and one of
+// them may carry it. The step of 32768 x 2304 -> 512 takes 453 us with it, 535 without.)
+int parts_of(bool out_bf16, bool dy_bf16) { return out_bf16 || dy_bf16 ? 2 : 3; }
 
 // dx = dy W: of a bf16 dy as it is by the scaled weight, in parts; of an fp32 one in
 // parts, scaled, by the weight's whole numbers. dw = (dy s)^T q.
@@ -439,7 +435,7 @@ BwdWs carve_bwd(void* base, const PvRows& dy, int M, int K, int N, bool dx_bf16,
                 bool want_dw, bool want_db, bool may_direct) {
     PvCarve c{(char*)base, 0};
     BwdWs w{};
-    const int parts = parts_of(dx_bf16, dy.bf16, M, K, N);
+    const int parts = parts_of(dx_bf16, dy.bf16);
     auto plan = [&](PvProduct& p, int parts_a, int parts_b, int rows, int cols, int depth) {
         p.a.parts = parts_a;
         p.b.parts = parts_b;
