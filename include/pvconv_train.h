@@ -261,9 +261,8 @@ pvconv_status pvconv_distill_topk_backward(const void* z, pvconv_dtype z_dt, int
 /* weight 0 has dz = 0; x and W should be finite all the same, as dz         */
 /* multiplies them.                                                          */
 /* fp32 operands are multiplied to 24 bits, bf16 ones exactly, sums are fp32. */
-/* For a bf16 dx (dw), dz is rounded to bf16 first; of up to 256 rows or 64   */
-/* classes, and the other factor always, to 16 bits. For an fp32 one, dz is  */
-/* taken to 24 bits.                                                         */
+/* For a bf16 dx (dw), dz and an fp32 W (x) are rounded to 16 bits first; for */
+/* an fp32 one they are taken to 24.                                         */
 /*  x       [M][K] (x_dt), row stride x_ld;  w [V][K] (w_dt), row stride w_ld */
 /*  bias    [V] fp32 or NULL;  labels [M] int32;  row_weight [M] fp32 or     */
 /*          NULL (1)                                                         */

@@ -65,8 +65,7 @@ __device__ __forceinline__ bool any_lane(bool b) { return __builtin_amdgcn_ballo
 
 enum Mode { kStats, kWhole, kGrad };
 
-// PARTS: dz in more than one bf16 part somewhere (what remains of it is then held too).
-template <int MODE, bool PARTS>
+template <int MODE>
 struct CeEpi {
     Ce c;
 
@@ -160,11 +159,8 @@ struct CeEpi {
                 }
 #pragma unroll
                 for (int q = 0; q < 16; q++) cs[q] += z[q];
-                if (c.dz.p) {
-                    store(0, m, nb, z);
-                    if constexpr (PARTS)
-                        for (int part = 1; part < c.dz.parts; part++) store(part, m, nb, z);
-                }
+                if (c.dz.p)
+                    for (int part = 0; part < c.dz.parts; part++) store(part, m, nb, z);
             }
         }
         if (MODE != kStats && grads && c.sums) {
@@ -254,20 +250,19 @@ constexpr int kLeastClasses = 2048;
 constexpr size_t kStatsBytes = (size_t)1 << 26;
 
 int parts_of(bool bf16) { return bf16 ? 1 : 3; }
-// Parts of dz for a gradient: 24 bits for an fp32 one; one rounding for a bf16 one, two
-// parts where few rows or classes would not average it (a row's dz at its label scales its
-// whole gradient; of few classes, whose dz add up to 0, the gradient is a difference). The
-// other factor of a bf16 gradient is rounded to 16 bits.
-constexpr int kFewRows = 256;
-int dz_parts_of(bool bf16, int M, int V) {
-    return !bf16 ? 3 : M <= kFewRows || V <= kWholeClasses ? 2 : 1;
-}
+// Parts of dz for a gradient: 24 bits for an fp32 one; for a bf16 one two parts, which leave
+// 2^-16 of a term where the result's rounding is 2^-8. (One part leaves 2^-8 of a term more,
+// which nothing averages: a row's dz at its label scales the row's whole dx, and rows of
+// one weight and small probabilities round alike, which scales their whole dw. The steps of
+// 4096 x 512, 49999 classes, and 8192 x 2048, 5003, take 1024 and 679 us with it, 1612 and
+// 1063 without.) The other factor of a bf16 gradient is rounded to 16 bits too.
+int dz_parts_of(bool bf16) { return bf16 ? 2 : 3; }
 int factor_parts_of(bool out_bf16, bool bf16) { return bf16 ? 1 : out_bf16 ? 2 : 3; }
 
 struct Plan {
     PvPanel x, w;             // what every product takes
     bool pack_x, pack_w;
-    bool whole, parts;        // parts: dz in more than one
+    bool whole;
     unsigned grad_sizes;
     int forward_classes, classes;  // a piece's
     PvPanel dz;
@@ -278,6 +273,14 @@ struct Plan {
     uint32_t* partial;
     size_t total;
 };
+
+// Bytes from a row of dz to the next: whole slices, not a multiple of 4 KB, whose rows would
+// lie in few of the memory's channels (4096 x 512, 49999 classes, the first piece's 64 KB
+// apart: the step takes 1743 us, 1612 with a slice more).
+size_t dz_pitch(int classes) {
+    const size_t pitch = pv_up(classes, kDeep) * 2;
+    return pitch % 4096 ? pitch : pitch + kSlice;
+}
 
 template <class T>
 int row_blocks_of(int M) {
@@ -294,13 +297,13 @@ int row_blocks(int M, int size) {  // as many as waves have rows
     }
 }
 // The tiles of an epilogue. A wave that has whole rows has all of 64 columns; beside the
-// sums of the largest tiles there are no registers for dz, of the next none for what its
-// first part leaves.
-constexpr unsigned sizes_of(int mode, bool parts) {
+// sums of the largest tiles there are no registers for dz. (dz of 4096 x 512, 32768 classes,
+// us: 317 in 256 x 128, 354 in 128 x 128.)
+constexpr unsigned sizes_of(int mode) {
     const unsigned narrow = 1u << kPvS | 1u << kPvN | 1u << kPvP;
     if (mode == kWhole) return narrow;
     if (mode == kStats) return kPvAnySize;
-    return narrow | 1u << kPvM | (parts ? 0u : 1u << kPvG);
+    return narrow | 1u << kPvM | 1u << kPvG;
 }
 // The product of x with n classes from v0 on.
 PvProduct logits_of(const PvPanel& x, const PvPanel& w, int M, int K, int v0, int n,
@@ -347,15 +350,13 @@ Plan carve(void* base, const PvLinearCe& a, bool forward, bool grads, bool may_d
         return p;
     }
     const bool want_dx = a.dx.p != nullptr, want_dw = a.dw.p != nullptr;
-    const int px = dz_parts_of(a.dx.bf16, a.M, a.V),
-              pw = dz_parts_of(a.dw.bf16, a.M, a.V);
+    const int px = dz_parts_of(a.dx.bf16), pw = dz_parts_of(a.dw.bf16);
     // (of both, wanted or not: the workspace of fewer gradients is then no larger)
     const size_t per = pv_up(a.M > 0 ? a.M : 1, 64) * 2 * (px > pw ? px : pw);
     size_t n = kPieceBytes / per / 256 * 256;
     if (n < (size_t)kLeastClasses) n = kLeastClasses;
     p.classes = n >= (size_t)a.V ? a.V : (int)n;
-    p.parts = px > 1 || pw > 1;
-    p.grad_sizes = sizes_of(p.whole ? kWhole : kGrad, p.parts);
+    p.grad_sizes = sizes_of(p.whole ? kWhole : kGrad);
     // (of both, wanted or not: one alone has the same bits)
     auto plan = [&](PvProduct& q, const PvPanel& x, const PvPanel& y, int rows, int cols,
                     int depth) {
@@ -369,7 +370,7 @@ Plan carve(void* base, const PvLinearCe& a, bool forward, bool grads, bool may_d
     };
     PvPanel dz{}, w = p.w, x = p.x;
     if (want_dx || want_dw)
-        dz = p.dz = pv_take_panel(c, (int)pv_up(a.M, kDeep), p.classes,
+        dz = p.dz = pv_take_panel(c, (int)pv_up(a.M, kDeep), (int)(dz_pitch(p.classes) / 2),
                                   want_dx && want_dw ? (px > pw ? px : pw) : want_dx ? px : pw);
     dz.parts = px;
     if (a.dx.bf16 && w.parts > 2) w.parts = 2;
@@ -423,16 +424,8 @@ Plan carve(void* base, const PvLinearCe& a, bool forward, bool grads, bool may_d
 }
 
 template <int MODE>
-void run_logits(const PvProduct& p, const Ce& c, bool parts, hipStream_t s) {
-    if constexpr (MODE == kWhole) {
-        pv_run_product<false, false, false, sizes_of(MODE, true)>(p, CeEpi<MODE, true>{c}, s);
-    } else if constexpr (MODE == kStats) {
-        pv_run_product<false, false, false>(p, CeEpi<MODE, false>{c}, s);
-    } else if (parts) {
-        pv_run_product<false, false, false, sizes_of(MODE, true)>(p, CeEpi<MODE, true>{c}, s);
-    } else {
-        pv_run_product<false, false, false, sizes_of(MODE, false)>(p, CeEpi<MODE, false>{c}, s);
-    }
+void run_logits(const PvProduct& p, const Ce& c, hipStream_t s) {
+    pv_run_product<false, false, false, sizes_of(MODE)>(p, CeEpi<MODE>{c}, s);
 }
 
 }  // namespace
@@ -467,7 +460,7 @@ pvconv_status pv_launch_linear_ce(const PvLinearCe& a, bool forward, void* ws, h
             c.stats = p.stats;
             c.nb = (n + 63) / 64;
             c.zlab = p.zlab;
-            run_logits<kStats>(logits(v0, n, kPvAnySize), c, false, s);
+            run_logits<kStats>(logits(v0, n, sizes_of(kStats)), c, s);
             const Join j{p.stats, c.nb, a.M, a.V, p.run, v0 == 0, v0 + n == a.V, a.labels, p.zlab,
                          a.loss, lse};
             if (a.M > 0) {
@@ -481,7 +474,7 @@ pvconv_status pv_launch_linear_ce(const PvLinearCe& a, bool forward, void* ws, h
         }
     } else if (forward && !grads) {
         c.bias = a.bias;
-        run_logits<kWhole>(logits(0, a.V, sizes_of(kWhole, true)), c, false, s);
+        run_logits<kWhole>(logits(0, a.V, sizes_of(kWhole)), c, s);
     }
     if (!grads) return pv_launch_status();
     for (int v0 = 0; v0 < a.V; v0 += p.classes) {
@@ -489,16 +482,16 @@ pvconv_status pv_launch_linear_ce(const PvLinearCe& a, bool forward, void* ws, h
         c.v0 = v0;
         c.bias = a.bias ? a.bias + v0 : nullptr;
         c.sums = p.sums;
-        const size_t pitch = pv_up(n, 64) * 2;
+        const size_t pitch = dz_pitch(n);
         c.dz = DzPanel{(uint8_t*)p.dz.p, pitch, p.dz.part_bytes, p.dz.parts, p.dz.rows};
         const PvProduct z = logits(v0, n, p.grad_sizes);
         const PvSums none{nullptr, 0, 0, nullptr},
             sums{p.sums, row_blocks(a.M, z.size), n, a.dbias ? a.dbias + v0 : nullptr};
         const bool dx = a.dx.p && a.M > 0, dw = a.dw.p;
         if (p.whole && forward)
-            run_logits<kWhole>(z, c, p.parts, s);
+            run_logits<kWhole>(z, c, s);
         else
-            run_logits<kGrad>(z, c, p.parts, s);
+            run_logits<kGrad>(z, c, s);
         PvProduct to_dx = p.dx, to_dw = p.dw;
         to_dx.a.pitch = to_dw.a.pitch = pitch;
         to_dx.partial = to_dw.partial = p.partial;  // one after the other
