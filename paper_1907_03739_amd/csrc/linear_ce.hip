@@ -291,7 +291,6 @@ int row_blocks(int M, int size) {  // as many as waves have rows
         case kPvL: return row_blocks_of<PvTileL>(M);
         case kPvG: return row_blocks_of<PvTileG>(M);
         case kPvM: return row_blocks_of<PvTileM>(M);
-        case kPvN: return row_blocks_of<PvTileN>(M);
         case kPvP: return row_blocks_of<PvTileP>(M);
         default: return row_blocks_of<PvTileS>(M);
     }
@@ -300,7 +299,7 @@ int row_blocks(int M, int size) {  // as many as waves have rows
 // sums of the largest tiles there are no registers for dz. (dz of 4096 x 512, 32768 classes,
 // us: 317 in 256 x 128, 354 in 128 x 128.)
 constexpr unsigned sizes_of(int mode) {
-    const unsigned narrow = 1u << kPvS | 1u << kPvN | 1u << kPvP;
+    const unsigned narrow = 1u << kPvS | 1u << kPvP;
     if (mode == kWhole) return narrow;
     if (mode == kStats) return kPvAnySize;
     return narrow | 1u << kPvM | 1u << kPvG;

@@ -70,8 +70,9 @@ static inline void pv_pairs(PvProduct& p, int parts_a, int parts_b) {
 // 1 of them under way while one is multiplied. What a slice takes, beside what the matrix
 // cores need for it, is the way of 32 to 64 KB from the L2 into LDS and a barrier: the more
 // products a byte feeds, the nearer to their rate (bf16, us: 8192 x 5003 -> 2048 129 in
-// tiles of 256 x 256, 1.3 PFLOP/s, 152, 221, 293 and 358 in the smaller ones); few tiles
-// need the small ones to fill the chip (1024 x 1024 x 1024: 27, 17, 13, 9.6, 9.6).
+// tiles of 256 x 256, 1.3 PFLOP/s, 152, 221 and 358 in the smaller ones); few tiles need
+// the small ones to fill the chip (1024 x 1024 x 1024: 27, 17, 13 and 9.6). 128 x 64 would
+// never be faster than 64 x 64, of which two fit a CU: 0.43 us a slice for 0.42.
 template <int WM_, int WN_, int MI_, int ST_, int PER_CU_>
 struct PvTile {
     static constexpr int WM = WM_, WN = WN_, MI = MI_, ST = ST_;
@@ -81,10 +82,10 @@ struct PvTile {
 typedef PvTile<2, 4, 8, 2, 1> PvTileL;  // 256 x 256
 typedef PvTile<4, 2, 4, 3, 1> PvTileG;  // 256 x 128
 typedef PvTile<2, 2, 4, 4, 1> PvTileM;  // 128 x 128
-typedef PvTile<4, 1, 2, 4, 1> PvTileN;  // 128 x 64
 typedef PvTile<2, 1, 2, 4, 2> PvTileS;  // 64 x 64
 typedef PvTile<4, 1, 1, 3, 1> PvTileP;  // 64 x 64, all parts of a slice in a stage
-enum PvSize { kPvS, kPvN, kPvM, kPvG, kPvL, kPvP };
+enum PvSize { kPvS, kPvM, kPvG, kPvL, kPvP };
+constexpr unsigned kPvAnySize = 31;  // 1 << each
 
 // The tile of index idx: eight tiles of rows by the columns in turn, so that an XCD,
 // which works on neighbours at a time, has both operands in its L2.
@@ -726,7 +727,6 @@ static constexpr PvSizeCost kPvCosts[] = {
     {kPvL, PvTileL::TM, PvTileL::TN, PvTileL::kWorkgroups, 1.4f, 6.f},
     {kPvG, PvTileG::TM, PvTileG::TN, PvTileG::kWorkgroups, 0.82f, 4.5f},
     {kPvM, PvTileM::TM, PvTileM::TN, PvTileM::kWorkgroups, 0.62f, 3.5f},
-    {kPvN, PvTileN::TM, PvTileN::TN, PvTileN::kWorkgroups, 0.43f, 3.f},
     {kPvS, PvTileS::TM, PvTileS::TN, PvTileS::kWorkgroups, 0.42f, 3.f},
 };
 // The pairs of operands that PvTileP is built for.
@@ -737,7 +737,7 @@ static inline PvSizeCost pv_parts_cost(int pairs) {
     return PvSizeCost{kPvP, PvTileP::TM, PvTileP::TN, PvTileP::kWorkgroups,
                       pairs > 3 ? 0.18f : 0.22f, 3.f};
 }
-static inline void pv_plan(PvProduct& p, bool may_split, unsigned sizes = 63) {
+static inline void pv_plan(PvProduct& p, bool may_split, unsigned sizes = kPvAnySize) {
     const int all = p.slices * p.pairs;
     float best = 0.f;
     auto choose = [&](const PvSizeCost& c) {
@@ -880,12 +880,11 @@ static void pv_run_parts(const PvProduct& p, const Epi& epi, hipStream_t s) {
         pv_launch_tiles<PvTileP>(pv_parts_kernel<TA, TB, 3, 3, Epi>, p, epi, s);
     else if (p.a.parts == 3)
         pv_launch_tiles<PvTileP>(pv_parts_kernel<TA, TB, 3, 1, Epi>, p, epi, s);
-    else
+    else if constexpr (!TB)  // (what lies across the sum as b follows an a of several parts)
         pv_launch_tiles<PvTileP>(pv_parts_kernel<TA, TB, 1, 3, Epi>, p, epi, s);
 }
 
 // SIZES: the tiles (1 << PvSize) that the plan may have chosen
-constexpr unsigned kPvAnySize = 63;
 template <bool I8, bool TA, bool TB, unsigned SIZES = kPvAnySize, class Epi>
 static void pv_run_product(const PvProduct& p, const Epi& epi, hipStream_t s) {
     if constexpr (SIZES >> kPvL & 1)
@@ -894,8 +893,6 @@ static void pv_run_product(const PvProduct& p, const Epi& epi, hipStream_t s) {
         if (p.size == kPvG) pv_run_tiles<I8, TA, TB, PvTileG>(p, epi, s);
     if constexpr (SIZES >> kPvM & 1)
         if (p.size == kPvM) pv_run_tiles<I8, TA, TB, PvTileM>(p, epi, s);
-    if constexpr (SIZES >> kPvN & 1)
-        if (p.size == kPvN) pv_run_tiles<I8, TA, TB, PvTileN>(p, epi, s);
     if constexpr (SIZES >> kPvS & 1)
         if (p.size == kPvS) pv_run_tiles<I8, TA, TB, PvTileS>(p, epi, s);
     if constexpr (!I8 && (SIZES >> kPvP & 1))
