@@ -483,17 +483,21 @@ void run_quantise(const PvRows& x, int M, int K, int8_t* q, float* scale, const 
         hipLaunchKernelGGL(kernel, dim3(pv_blocks(M, kThreads / team)), dim3(kThreads), 0, s, x, M,
                            K, q, scale, to);
     };
-    // A wave a row up to 5120 channels. Few rows of many: a workgroup each.
-    if (K > 5120 || (K > 1024 && M <= 256))
+    // A wave a row up to 3584 channels, of which it holds as many as the row has, up to 2560; a
+    // workgroup a row of more, and where there are few rows. (us, a wave that holds 512,
+    // 1024 or 2560 / a workgroup. bf16, 32768 x 512: 13.5, 14.6, 21 / 54; 1000: 21, 21, 27 / 57;
+    // 2560: 47, 46, 48 / 67; 3500: -, 86, 80 / 91; 4096: 100, 100, 88 / 83; 4928: 130, 128, 119 /
+    // 101. fp32, 32768 x 2560: 103, 94, 83 / 89; 4096: 172, 164, 137 / 124. bf16, 4096 x 2560: -,
+    // 9.3, 10.2 / 13; 1024 x 1100: -, 4.9, 5 / 4.7; x 4928: -, 10.2, 10.2 / 6.8; 256 x 2048: 4.9,
+    // 4.9, 5.1 / 3.4.)
+    if (K > 3584 || (K > 1024 && M <= 1024))
         run(pv_int8_quantise_kernel<XB, 256, 4>, 256);
     else if (K <= 512)
         run(pv_int8_quantise_kernel<XB, 64, 1>, 64);
     else if (K <= 1024)
         run(pv_int8_quantise_kernel<XB, 64, 2>, 64);
-    else if (K <= 2560)
-        run(pv_int8_quantise_kernel<XB, 64, 5>, 64);
     else
-        run(pv_int8_quantise_kernel<XB, 64, 10>, 64);
+        run(pv_int8_quantise_kernel<XB, 64, 5>, 64);
 }
 
 }  // namespace
