@@ -261,7 +261,7 @@ struct LinearEpi {
     }
 };
 
-// Few rows: a workgroup takes 16 rows by 16 columns. Its eight waves take the rows'
+// Few rows: a workgroup takes 16 rows by 16 columns. Its 8 or 16 waves take the rows'
 // largest values, then a share of the 64-value pieces each, which a wave quantises in
 // registers where they are its matrix operand: lane (r, h) holds row r's values 16 h ..
 // of a piece. Their sums meet in LDS; one launch, no workspace. Latency: a wave's first
@@ -355,13 +355,16 @@ __global__ __launch_bounds__(THREADS) void pv_int8_few_kernel(PvRows x, int M, i
                      activate(v, epi.neg, epi.relu));
     }
 }
-// Up to two of its workgroups a CU, unless each has many rows of many channels to find the
-// largest of (few / apart, us: 64 x 64 -> 64 5.6 / 8.6; 512 x 323 -> 256, 512 workgroups,
-// 9.1 / 9.4 and a launch; 2048 x 323 -> 128, 1024 of them, 16.7 / 9.7; 64 x 4928 -> 64
-// 15.7 / 10.8).
-constexpr int kFewTiles = 512, kFewChannels = 2560;
+// Where its one launch is the shorter call. (us, few / quantiser, product and join: a call of
+// many; a replay of a graph, which has no launches to wait for. 1 x 4928 -> 256, fp32: 10.3 /
+// 18.3; 9.3 / 10.2. 4 x 8192 -> 256: 16 / 18.3; 16.2 / 10.7; x 12000: 20.9 / 18.5. 16 x 2560 -> 256:
+// 12 / 18.1; 12.2 / 9.9; x 4928: 20.5 / 18.2. 256 x 2560 -> 256, 256 workgroups: 12.2 / 18.1; 12.5
+// / 11.3. Two a CU, 512 x 323 -> 256: 11.6 / 15; 11.7 / 8.5; 512 x 1024: 15.5 / 15.1; x 1536:
+// 17.6 / 15; 4 x 2048 -> 8192: 11.6 / 17.6; x 4096: 20.1 / 18.)
 bool few(int M, int K, int N) {
-    return (size_t)((M + 15) / 16) * ((N + 15) / 16) <= kFewTiles && (K <= kFewChannels || M <= 4);
+    const size_t tiles = (size_t)((M + 15) / 16) * ((N + 15) / 16);
+    if (tiles > 512) return false;
+    return K <= (tiles <= 256 ? (M <= 4 ? 8192 : 2560) : M <= 4 ? 2560 : 1024);
 }
 
 void run_few(const PvRows& x, int M, int K, int N, const int8_t* weight, const LinearEpi& epi,
