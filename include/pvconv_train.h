@@ -260,7 +260,10 @@ pvconv_status pvconv_distill_topk_backward(const void* z, pvconv_dtype z_dt, int
 /* part. A NaN or +inf logit makes its row's lse, loss and dz NaN. A row of  */
 /* weight 0 has dz = 0; x and W should be finite all the same, as dz         */
 /* multiplies them.                                                          */
-/* fp32 operands are multiplied to 24 bits, bf16 ones exactly, sums are fp32. */
+/* fp32 operands are multiplied to 24 bits, bf16 ones exactly, sums are fp32, */
+/* an exponential is off by 2^-24 |z - lse| of itself. What of a factor of a  */
+/* gradient lies below 2^-133 is left out: row weights below some 2^-110 cost */
+/* digits.                                                                   */
 /* For a bf16 dx (dw), dz and an fp32 W (x) are rounded to 16 bits first; for */
 /* an fp32 one they are taken to 24.                                         */
 /*  x       [M][K] (x_dt), row stride x_ld;  w [V][K] (w_dt), row stride w_ld */
@@ -271,7 +274,12 @@ pvconv_status pvconv_distill_topk_backward(const void* z, pvconv_dtype z_dt, int
 /*          dbias out [V] fp32; each NULL where not wanted                   */
 /* 0 <= M <= 2^24, 1 <= K <= PVCONV_CE_MAX_CHANNELS, 1 <= V <=               */
 /* PVCONV_MAX_CLASSES. The workspace sizes are those of a call with every    */
-/* gradient (want_grad) or none; for a backward, want_grad.                  */
+/* gradient (want_grad) or none; for a backward, want_grad. They hold x and W */
+/* in parts (2 bytes a bf16 value, 6 an fp32 one, K up to 64s; not used for   */
+/* bf16 rows of 64s of channels on 16 bytes), for a piece of the classes 8    */
+/* bytes a row and 64 classes of statistics (64 MB or 4096 classes) and, with */
+/* gradients, 4 or 6 bytes of dz a row and class (512 MB or 2048 classes),    */
+/* fp32 sums of dx where there are several pieces, and sums of split products. */
 /* ------------------------------------------------------------------------- */
 #define PVCONV_CE_MAX_CHANNELS 65536
 size_t pvconv_linear_cross_entropy_workspace_size(int M, int K, int V, pvconv_dtype x_dt,

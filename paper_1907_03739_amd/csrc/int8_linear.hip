@@ -7,16 +7,16 @@
 // when the sum becomes a float, by its scale, its bias and its type.
 //
 // Two launches, the quantiser and the product (pv_product.h), but for few rows. The scale
-// of a row needs the whole row, and rows of 5 KB do not fit a workgroup's LDS by the 256
-// that a product wants: 32768 x 4928 -> 256, bf16, is 94 us at 5.1 TB/s and 50 us of
-// product, which reads the 161 MB of bytes twice over its columns; the bytes of x alone
-// would take 51. 32768 x 512 -> 2048: 13 + 57, 134 MB written at 2.3 TB/s behind four
-// slices of products.
+// of a row needs the whole row before its first product: 32768 x 4928 -> 256, bf16, is 101
+// us at 4.8 TB/s and 47 us of product, which reads the 161 MB of bytes twice over its
+// columns; x alone would take 51. (One launch whose workgroups keep the bytes of 16 or 32
+// such rows in LDS has not been tried.) 32768 x 512 -> 2048: 13 + 57, 134 MB written at 2.3
+// TB/s behind four slices of products.
 //
 // The gradients are products of bf16 parts, from the bytes and scales that the forward
 // kept: with bf16 dy, dx takes dy as it lies by the weight times its scales (15 bits, two
 // parts), dw takes dy s in the two parts that hold its 16 bits. 32768 x 2304
-// -> 512: operands 74 us (4.4 TB/s), dx 109 (0.71 PFLOP/s), dw 183 (two parts: 0.85).
+// -> 512: operands 76 us (4.4 TB/s), dx 185 (two parts: 0.83 PFLOP/s), dw 191 (0.81).
 #include "pv_product.h"
 #include "pv_wave.h"
 

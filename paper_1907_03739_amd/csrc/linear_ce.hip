@@ -11,10 +11,13 @@
 //
 // Multiplying twice is cheaper than keeping the logits up to some thousand channels: in 32
 // bits, as a difference of logits needs them, they would be written and read at 8 bytes of
-// memory for 2 K operations. 4096 x 512, 49999 classes, bf16, us: statistics 266 (0.79
-// PFLOP/s), dz 325 (0.65), dx 214 (0.98), dw 248 (0.85). The first two are bound by their
-// epilogues beside eight slices of products: some nine vector instructions a logit, the
-// exponential at a quarter of their rate among them.
+// memory for 2 K operations. 4096 x 512, 49999 classes, bf16, us: statistics 259 (0.81
+// PFLOP/s), dz 403 (0.52), dx of its two parts 441 (0.95), dw 467 (0.90). The first two are
+// bound by their epilogues beside eight slices of products: the matrix cores work 36 and
+// 22 % of the time, the vector ones 27 and 29 (some nine instructions a logit, the
+// exponential at a quarter of their rate among them), one after the other in most waves.
+// The exponential is the hardware's power of two: off by 2^-24 |z - lse| of itself, as a
+// rounding of z would make it.
 #include "pv_product.h"
 #include "pv_wave.h"
 
@@ -257,7 +260,6 @@ int parts_of(bool bf16) { return bf16 ? 1 : 3; }
 // 4096 x 512, 49999 classes, and 8192 x 2048, 5003, take 1024 and 679 us with it, 1612 and
 // 1063 without.) The other factor of a bf16 gradient is rounded to 16 bits too.
 int dz_parts_of(bool bf16) { return bf16 ? 2 : 3; }
-int factor_parts_of(bool out_bf16, bool bf16) { return bf16 ? 1 : out_bf16 ? 2 : 3; }
 
 struct Plan {
     PvPanel x, w;             // what every product takes
@@ -372,7 +374,7 @@ Plan carve(void* base, const PvLinearCe& a, bool forward, bool grads, bool may_d
         dz = p.dz = pv_take_panel(c, (int)pv_up(a.M, kDeep), (int)(dz_pitch(p.classes) / 2),
                                   want_dx && want_dw ? (px > pw ? px : pw) : want_dx ? px : pw);
     dz.parts = px;
-    if (a.dx.bf16 && w.parts > 2) w.parts = 2;
+    if (a.dx.bf16 && w.parts > 2) w.parts = 2;  // (of the three that are there)
     plan(p.dx, dz, w, a.M, a.K, p.classes);
     dz.parts = pw;
     if (a.dw.bf16 && x.parts > 2) x.parts = 2;

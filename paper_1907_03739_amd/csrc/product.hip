@@ -260,7 +260,7 @@ constexpr int kWideSums = 4096;  // columns
 // column sums, in one launch. Products of few tiles leave CUs idle, and a launch costs as
 // much as one of them. (us, two products, what joins their splits, sums / in one: 999 x 323,
 // 1003 classes, fp32: 14 + 4 + 16 + 4 + 3 / 26; 777 x 203 -> 99, fp32: 4.5 + 5.2 + 2.9 /
-// 13, two launches fewer.)
+// 13, two launches fewer; since with three stages of parts 21 and 11.)
 struct Pair {
     PvProduct x, y;
     PlainEpi ex, ey;

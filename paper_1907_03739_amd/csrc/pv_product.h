@@ -10,7 +10,9 @@
 // A 32-bit value can be an operand in up to three bf16 parts, h = bf16(v), m =
 // bf16(v - h), l = bf16(v - h - m): 24 bits in all. The product of such operands
 // is a sum of products of parts (a pair of parts is a run of slices like any
-// other); hh + hm + mh + mm + hl + lh leaves out terms below 2^-26 of a product.
+// other); hh + hm + mh + mm + hl + lh leaves out ml and lm, up to 2^-24 of a product
+// together (a second part is up to 2^-8 of its value, a third 2^-17), and ll. Two parts are
+// 16 bits: hh + hm + mh. What lies below 2^-133, the smallest bf16 number, is in no part.
 #pragma once
 
 #include <type_traits>
@@ -713,12 +715,10 @@ static inline size_t pv_tiles_of(int M, int N, int tm, int tn) {
 }
 // The tiles that a product takes and how many ways its slices are split, by the time that
 // each choice is expected to take: rounds of workgroups, each its slices and an epilogue,
-// and the splits' sums written, read and joined. The times a slice and the rest are those
-// of unsplit products of 35 sizes, each timed in every size of tile and up to twelve
-// splits; the choice took at most 1.25 times the best one there, 1.03 in the median. (512 x 2304 by 32768 deep,
-// us: 256 x 128 in seven 85, 256 x 256 in twelve 90, unsplit 242 to 724; 4096 x 512 by
-// 49999: 256 x 256 in eight 202, unsplit 404 to 1230; 8192 x 5003 -> 2048: unsplit 129, in
-// two 212.)
+// and the splits' sums written, read and joined. The times a slice and the rest are fitted
+// to unsplit products in every size of tile. (512 x 2304 by 32768 deep, us: 256 x 128 in
+// seven 85, 256 x 256 in twelve 90, unsplit 242 to 724; 4096 x 512 by 49999: 256 x 256 in
+// eight 202, unsplit 404 to 1230; 8192 x 5003 -> 2048: unsplit 129, in two 212.)
 struct PvSizeCost {
     int size, tm, tn, slots;
     float slice, rest;  // us

@@ -13,10 +13,11 @@ quantised once a step, and once for serving; activations and their gradients are
 bf16, logits and parameter gradients fp32.
 
 Between forward and backward a layer in 8-bit floating point keeps its input and
-its output before the norm, in bf16. A layer in 8-bit integers keeps the quantised
-rows of its input, a quarter of those bytes: the backward multiplies them again
-for the output, which has the forward's bits, and takes the weight's gradient from
-them.
+its output before the norm, in bf16: 2 (C_in + C_out) bytes a point. A layer in 8-bit
+integers keeps the quantised rows of its input, 4 bytes and C_in rounded up to 128s:
+a quarter where both widths are alike and wide, more where C_in is small (64 to 64:
+132 for 256; 32 to 24: 132 for 112). The backward multiplies them again for the
+output, which has the forward's bits, and takes the weight's gradient from them.
 
 Every arithmetic step runs in libpvconv through the calls of the binding; this
 module only lays out device buffers and orders the calls.
@@ -173,8 +174,9 @@ class DeviceStudent:
                     lengths: Optional[torch.Tensor] = None, want_dx: bool = False):
         """Forward and backward of sum(row_weight * cross-entropy of the labels):
         labels [B*N] int32, outside the classes: no loss, no gradient -> what step()
-        returns. The last layer multiplies its fp32 weight as it is, and its logits
-        are never stored. The points past a cloud's length as for step()."""
+        returns. The last layer multiplies its fp32 weight and the bf16 features as
+        they are (step() trains it as logits() serves it, in 8 bits), and its logits are
+        never stored. The points past a cloud's length as for step()."""
         model = self._train_model(len(self.gamma))
         saved = []
         h = self._hidden(x, model, lengths, saved)
