@@ -185,7 +185,8 @@ pvconv_status pvconv_int8_linear_rows(const int8_t* rows, const float* row_scale
 /*   dx[m,k] = sum_n dy[m,n] scale_n weight[n,k]                             */
 /*   dw[n,k] = sum_m dy[m,n] row_scale_m rows[m,k],  dbias_n = sum_m dy[m,n] */
 /* Sums are fp32, of products that are exact (bf16 dy) or good to 24 bits    */
-/* (fp32 dy; for a bf16 dx, dy scale_n is rounded to 16 bits first).         */
+/* (fp32 dy; for a bf16 dx, dy scale_n is rounded to 16 bits first). scale_n  */
+/* weight and dy row_scale are formed in 32 bits and should be finite there.  */
 /*  dy [M][N] (dy_dt), dy_ld; dx out [M][K] (dx_dt), dx_ld, or NULL (weight, */
 /*  scale then unused); dw out [N][K] fp32 or NULL (rows, row_scale then     */
 /*  unused); dbias out [N] fp32 or NULL                                      */
